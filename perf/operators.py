@@ -1,0 +1,369 @@
+"""Measured calls of the 8-bit integer operators: what a program that serves an
+int8 checkpoint (codes and row scales, as the decoder gives them back) runs.
+
+A case's `op` is the operator:
+
+* linear: activations quantised per token, times int8 weight matrices that share
+  them (q, k and v, or one matrix), with the scales of tokens and output channels
+  and an optional bias applied, in the activations' type or another;
+* route: a router's logits to experts, weights and the order of the experts' rows;
+* experts: the gated feed-forward of a mixture layer with int8 experts: for every
+  token the weighted sum of its experts' down(silu(gate x) * up x), the
+  activations quantised per token before each product.
+"""
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+SIZE = {"bf16": 2, "fp16": 2, "fp32": 4}
+TINY = 1e-30  # a row whose largest magnitude is below this counts as zeros
+
+
+def _linear(name, m, k, n, kv=0, x="bf16", out="", scales="fp16", bias=False):
+    """kv: two more matrices of that many rows share x (0: none)."""
+    return {"name": name, "op": "linear", "m": m, "k": k, "n": n, "kv": kv, "x": x,
+            "out": out or x, "scales": scales, "bias": bias}
+
+
+def _route(name, tokens, experts, k, x="bf16", score="softmax", bias=False, groups=1,
+           top_groups=1, group_top=1, renorm=True, scale=1.0, pad=0, off=0):
+    """pad: trailing tokens with nothing to route; off: experts that are masked."""
+    return {"name": name, "op": "route", "tokens": tokens, "experts": experts, "k": k, "x": x,
+            "score": score, "bias": bias, "groups": groups, "top_groups": top_groups,
+            "group_top": group_top, "renorm": renorm, "scale": scale, "pad": pad, "off": off}
+
+
+def _experts(name, tokens, experts, k, hidden, ffn, x="bf16", scales="fp16", pad=0):
+    return {"name": name, "op": "experts", "tokens": tokens, "experts": experts, "k": k,
+            "hidden": hidden, "ffn": ffn, "x": x, "scales": scales, "pad": pad}
+
+
+def listed():
+    return [
+        # one token through q, k and v of an 8B layer: the smallest product, bound by latency
+        _linear("linear-token", 1, 4096, 4096, kv=1024),
+        # a decode batch of odd size through an up projection of a 70B layer: bound by the weights
+        _linear("linear-batch", 13, 8192, 28672, x="fp16", bias=True),
+        # odd sizes throughout (no row of the weights aligned), 32-bit activations and results
+        _linear("linear-odd", 333, 5461, 2047, x="fp32", scales="fp32", bias=True),
+        # a chunk of a prompt through a down projection of a 70B layer
+        _linear("linear-chunk", 512, 28672, 8192, x="fp16", out="bf16", scales="bf16"),
+        # a batch of long prompts through an up projection of a 70B layer: bound by the arithmetic
+        _linear("linear-prompt", 8192, 8192, 28672),
+        # one token, few experts: the smallest routing
+        _route("route-token", 1, 8, 2),
+        # a prompt over many experts in groups, sigmoid scores with a bias for balance
+        _route("route-groups", 4096, 256, 8, x="fp32", score="sigmoid", bias=True, groups=8,
+               top_groups=4, group_top=2, scale=2.5),
+        # a large batch, an odd number of experts, some masked, and padded tokens
+        _route("route-odd", 32771, 61, 6, x="fp16", renorm=False, pad=1000, off=3),
+        # one token through a layer of many small experts
+        _experts("experts-token", 1, 64, 6, 2048, 1408),
+        # odd sizes, another type, a padded batch
+        _experts("experts-odd", 203, 7, 3, 1537, 2051, x="fp16", scales="fp32", pad=11),
+        # a decode batch through a layer of eight large experts: all of their weights are read
+        _experts("experts-batch", 32, 8, 2, 6144, 16384),
+        # a prompt through the same layer: bound by the arithmetic
+        _experts("experts-prompt", 4096, 8, 2, 6144, 16384),
+    ]
+
+
+def _spread(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi):
+    """A width: mostly whole blocks of 128, at times odd."""
+    v = _spread(rng, lo, hi)
+    return v if rng.random() < 0.3 or v < 192 else v // 128 * 128
+
+
+def draw(rng):
+    op = rng.choice(["linear", "linear", "route", "experts"])
+    x = rng.choice(["bf16", "bf16", "fp16", "fp32"])
+    scales = rng.choice(["fp16", "fp16", "bf16", "fp32"])
+    if op == "linear":
+        c = _linear("", _spread(rng, 1, 8192), _size(rng, 256, 28672), _size(rng, 256, 28672),
+                    x=x, out=rng.choice([x, x, "bf16", "fp32"]), scales=scales,
+                    bias=rng.random() < 0.4)
+        while c["k"] * c["n"] > 8192 * 28672:
+            c["k"], c["n"] = max(256, c["k"] // 2), max(256, c["n"] // 2)
+        if rng.random() < 0.3:
+            c["kv"] = max(128, c["n"] // rng.choice([4, 5, 8]))
+            c["n"] -= 2 * (c["kv"] // 2)  # no more work than without k and v
+    elif op == "route":
+        groups = rng.choice([1, 1, 4, 8])
+        score = rng.choice(["softmax", "sigmoid"])
+        # A bias goes with sigmoid scores here: added to softmax scores it would make
+        # the choice between near scores depend on the order of the softmax's sum.
+        e = (_spread(rng, 4, 64) if groups > 1 else _spread(rng, 2, 512)) * groups
+        per = e // groups
+        keep = rng.randint(1, groups)
+        c = _route("", _spread(rng, 1, 32768), min(e, 512 // groups * groups),
+                   rng.randint(1, min(16, keep * min(per, 512 // groups))),
+                   x=x, score=score, bias=score == "sigmoid" and rng.random() < 0.7,
+                   groups=groups, top_groups=keep,
+                   group_top=2 if score == "sigmoid" and rng.random() < 0.5 and groups > 1 else 1,
+                   renorm=rng.random() < 0.7, scale=rng.choice([1.0, 1.0, 2.5]))
+        c["pad"] = rng.choice([0, 0, c["tokens"] // 9])
+        c["off"] = rng.choice([0, 0, c["experts"] // 10])
+    else:
+        e = rng.choice([4, 8, 8, 16, 32, 61, 64])
+        k = rng.randint(1, min(e, 8))
+        hidden = _size(rng, 512, 6144)
+        ffn = min(_size(rng, 512, 16384), 4 * hidden)
+        while e * hidden * ffn > 8 * 6144 * 16384:
+            hidden, ffn = hidden // 2, ffn // 2
+        tokens = min(_spread(rng, 1, 4096), max(1, 8192 * 6144 * 16384 // (k * hidden * ffn)))
+        # 16-bit results: in 32 bits they would show the few of the hidden layer's values
+        # that a sum's last bit moves to the next of its 127 steps
+        c = _experts("", tokens, e, k, hidden, ffn, x=rng.choice(["bf16", "bf16", "fp16"]),
+                     scales=scales,
+                     pad=rng.choice([0, 0, tokens // 9]))
+    del c["name"]
+    for size in ("m", "k", "n", "kv", "tokens", "hidden", "ffn"):
+        if c.get(size) == 24 * 128:
+            c[size] -= 1
+    return c
+
+
+# --- inputs -------------------------------------------------------------------
+
+def _gen(seed, j):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed * 1009 + j)
+    return g
+
+
+def _activations(g, rows, width, dtype):
+    """Normal values with a few columns 20 times larger, as a layer's inputs have them."""
+    x = torch.randn((rows, width), generator=g, device=DEV)
+    x[:, torch.randperm(width, generator=g, device=DEV)[:max(1, width // 1000)]] *= 20
+    return x.to(DTYPES[dtype])
+
+
+def _codes(g, n, k, dtype):
+    """int8 codes and row scales of Student-t (5 degrees of freedom) weights."""
+    w = torch.randn((n, k), generator=g, device=DEV)
+    s = torch.zeros_like(w)
+    for _ in range(5):
+        s.addcmul_(t := torch.randn((n, k), generator=g, device=DEV), t)
+    w.mul_(0.02).div_(s.div_(5).sqrt_())
+    scale = (w.abs().amax(dim=1) / 127).to(DTYPES[dtype])
+    return torch.round(w.div_(scale.float()[:, None])).clamp_(-127, 127).to(torch.int8), scale
+
+
+def _bank(g, experts, n, k, dtype):
+    """The same for a stack of experts."""
+    codes = torch.empty((experts, n, k), dtype=torch.int8, device=DEV)
+    scales = torch.empty((experts, n), dtype=DTYPES[dtype], device=DEV)
+    for e in range(experts):
+        codes[e], scales[e] = _codes(g, n, k, dtype)
+    return codes, scales
+
+
+def prepare(case, seed):
+    if case["op"] == "linear":
+        mats = [_codes(_gen(seed, 10 + j), n, case["k"], case["scales"])
+                for j, n in enumerate([case["n"]] + [case["kv"]] * 2) if n]
+        g = _gen(seed, 1)
+        return {"case": case, "x": _activations(g, case["m"], case["k"], case["x"]),
+                "w": [w for w, _ in mats], "scales": [s for _, s in mats],
+                "bias": [torch.randn(w.shape[0], generator=g, device=DEV).to(DTYPES[case["x"]])
+                         if case["bias"] else None for w, _ in mats]}
+    t, e = case["tokens"], case["experts"]
+    g = _gen(seed, 2)
+    # some experts are more popular than others
+    logits = torch.randn((t, e), generator=g, device=DEV) * 1.5 \
+        + torch.randn(e, generator=g, device=DEV) * 0.5
+    if case["op"] == "route":
+        logits[:, torch.randperm(e, generator=g, device=DEV)[:case["off"]]] = -math.inf
+        logits[t - case["pad"]:] = -math.inf
+        bias = torch.randn(e, generator=g, device=DEV) * 0.1 if case["bias"] else None
+        return {"case": case, "logits": logits.to(DTYPES[case["x"]]), "bias": bias}
+    top, ids = torch.topk(logits, case["k"], dim=1)
+    weights = torch.softmax(top, dim=1)
+    ids = ids.to(torch.int32)
+    ids[t - case["pad"]:] = -1
+    weights[t - case["pad"]:] = 0
+    order, offsets = _order(ids, e)
+    state = {"case": case, "x": _activations(g, t, case["hidden"], case["x"]), "ids": ids,
+             "weights": weights, "order": order, "offsets": offsets}
+    for j, (part, n, k) in enumerate((("gate", case["ffn"], case["hidden"]),
+                                      ("up", case["ffn"], case["hidden"]),
+                                      ("down", case["hidden"], case["ffn"]))):
+        state[part], state[part + "_scale"] = _bank(_gen(seed, 20 + j), e, n, k, case["scales"])
+    return state
+
+
+# --- the plain forms ----------------------------------------------------------
+
+def _quantised(x):
+    """int8 values (as 32-bit floats) and scales of x's rows."""
+    top = x.abs().amax(dim=-1, keepdim=True)
+    none = top < TINY
+    q = torch.round(x * torch.where(none, 0.0, 127.0 / top)).clamp(-127, 127)
+    return q, torch.where(none, 0.0, top / 127.0)
+
+
+def _product(q, scale, w, w_scale):
+    return q @ w.float().transpose(-1, -2) * scale * w_scale.float()[..., None, :]
+
+
+def _order(ids, experts):
+    """Slots sorted by expert, those without one last, and where each expert starts."""
+    flat = torch.where(ids < 0, experts, ids).flatten()
+    order = torch.sort(flat, stable=True)[1].to(torch.int32)
+    counts = (flat[:, None] == torch.arange(experts, device=DEV)).sum(dim=0)
+    offsets = torch.zeros(experts + 1, dtype=torch.int32, device=DEV)
+    offsets[1:] = torch.cumsum(counts, 0)
+    return order, offsets
+
+
+def _choose(case, logits, bias):
+    x = logits.float()
+    off = x == -math.inf
+    if case["score"] == "softmax":
+        e = torch.where(off, 0.0, torch.exp(x - x.amax(dim=1, keepdim=True)))
+        total = e.sum(dim=1, keepdim=True)
+        s = torch.where(total > 0, e / total, 0.0)
+        key = x  # grows with the score
+    else:
+        s = torch.where(off, 0.0, 1 / (1 + torch.exp(-x)))
+        key = torch.where(off, -math.inf, s if bias is None else s + bias)
+    if case["groups"] > 1:
+        parts = key.view(len(key), case["groups"], -1)
+        best = torch.sort(parts, dim=2, descending=True)[0][..., :case["group_top"]].sum(dim=2)
+        kept = torch.sort(best, dim=1, descending=True, stable=True)[1][:, :case["top_groups"]]
+        out = torch.ones_like(best, dtype=torch.bool).scatter_(1, kept, False)
+        key = torch.where(out[..., None], -math.inf, parts).flatten(1)
+    top, ids = torch.sort(key, dim=1, descending=True, stable=True)
+    top, ids = top[:, :case["k"]], ids[:, :case["k"]]
+    empty = top == -math.inf
+    w = torch.where(empty, 0.0, s.gather(1, ids))
+    if case["renorm"]:
+        total = w.sum(dim=1, keepdim=True)
+        w = torch.where(total > 0, w / total, 0.0)
+    return torch.where(empty, -1, ids).to(torch.int32), w * case["scale"]
+
+
+def _plain(state):
+    case = state["case"]
+    if case["op"] == "linear":
+        q, scale = _quantised(state["x"].float())
+        ys = [_product(q, scale, w, s) + (0.0 if b is None else b.float())
+              for w, s, b in zip(state["w"], state["scales"], state["bias"])]
+        return [y.to(DTYPES[case["out"]]) for y in ys]
+    if case["op"] == "route":
+        ids, weights = _choose(case, state["logits"], state["bias"])
+        order, offsets = _order(ids, case["experts"])
+        return {"ids": ids, "weights": weights, "offsets": offsets, "order": order}
+    # every expert for every token, with weight 0 where it is not the token's
+    t, e, ids = case["tokens"], case["experts"], state["ids"].long()
+    share = torch.zeros((t, e + 1), device=DEV).scatter_add_(1, torch.where(ids < 0, e, ids),
+                                                           state["weights"])[:, :e]
+    q, scale = _quantised(state["x"].float())
+    gate = _product(q, scale, state["gate"], state["gate_scale"])
+    h = gate / (1 + torch.exp(-gate)) * _product(q, scale, state["up"], state["up_scale"])
+    y = _product(*_quantised(h), state["down"], state["down_scale"])
+    return (y * share.T[..., None]).sum(dim=0).to(DTYPES[case["x"]])
+
+
+def run(state):
+    if not own:
+        return _plain(state)
+    from paper_2606_15789_amd import wc
+    case = state["case"]
+    if case["op"] == "linear":
+        return wc.linear_i8_torch(state["x"], state["w"], state["scales"], state["bias"],
+                                  dtype=DTYPES[case["out"]])
+    if case["op"] == "route":
+        r = wc.route_torch(state["logits"], case["k"], case["score"], state["bias"],
+                           groups=case["groups"], top_groups=case["top_groups"],
+                           group_top=case["group_top"], renormalize=case["renorm"],
+                           scale=case["scale"])
+        return {"ids": r.ids, "weights": r.weights, "offsets": r.offsets, "order": r.order}
+    routing = wc.Routing(state["ids"], state["weights"], state["offsets"], state["order"])
+    return wc.experts_i8_torch(state["x"], routing, state["gate"], state["gate_scale"],
+                               state["up"], state["up_scale"], state["down"],
+                               state["down_scale"])
+
+
+def work(case):
+    if case["op"] == "linear":
+        m, k, n = case["m"], case["k"], case["n"] + 2 * case["kv"]
+        side = SIZE[case["scales"]] + (SIZE[case["x"]] if case["bias"] else 0)
+        return {"bytes": m * k * SIZE[case["x"]] + n * k + n * side + m * n * SIZE[case["out"]], "flops": 2 * m * n * k}
+    t, e, k = case["tokens"], case["experts"], case["k"]
+    if case["op"] == "route":
+        return {"bytes": t * e * SIZE[case["x"]] + 12 * t * k + 4 * (e + 1)
+                + (4 * e if case["bias"] else 0), "flops": 0}
+    t -= case["pad"]
+    # the experts that k draws a token without replacement hit, were all alike
+    hit = e * (1 - (1 - k / e) ** t)
+    one = 3 * case["hidden"] * case["ffn"]
+    rows = hit * (2 * case["ffn"] + case["hidden"]) * SIZE[case["scales"]]
+    return {"bytes": hit * one + rows + (t + case["tokens"]) * case["hidden"] * SIZE[case["x"]]
+            + 12 * case["tokens"] * k, "flops": 2 * t * k * one}
+
+
+# --- the definitions in 64 bits -----------------------------------------------
+
+def _rows64(x):
+    """Rows rounded to 127 steps of their largest magnitude, as the values they stand for."""
+    step = x.abs().max(dim=1, keepdim=True)[0] / 127
+    step[step < TINY / 127] = math.inf  # rows of zeros
+    q = torch.round(x / step)
+    return torch.where(torch.isinf(step), torch.zeros_like(x), q * step)
+
+
+def _weights64(codes, scales):
+    return codes.double() * scales.double().unsqueeze(1)
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    if case["op"] == "linear":
+        x = _rows64(state["x"].double())
+        ys = []
+        for w, s, b in zip(state["w"], state["scales"], state["bias"]):
+            y = torch.mm(x, _weights64(w, s).t())
+            ys.append(y if b is None else y + b.double())
+        return ys
+    if case["op"] == "route":
+        x = state["logits"].double()
+        on = x > -math.inf
+        if case["score"] == "softmax":
+            s = torch.softmax(x.clamp_min(-1e300), dim=1) * on
+        else:
+            s = torch.sigmoid(x)
+        key = s + (0 if state["bias"] is None else state["bias"].double())
+        key[~on] = -math.inf
+        if case["groups"] > 1:
+            per = case["experts"] // case["groups"]
+            best = key.unflatten(1, (case["groups"], per)).topk(case["group_top"], dim=2)[0].sum(2)
+            rank = best.argsort(dim=1, descending=True, stable=True).argsort(dim=1)
+            key[(rank >= case["top_groups"]).repeat_interleave(per, dim=1)] = -math.inf
+        ids = key.argsort(dim=1, descending=True, stable=True)[:, :case["k"]]
+        w = torch.gather(s, 1, ids) * (torch.gather(key, 1, ids) > -math.inf)
+        if case["renorm"]:
+            w = w / w.sum(dim=1, keepdim=True).clamp_min(1e-300)
+        return {"ids": None, "weights": w * case["scale"], "offsets": None, "order": None}
+    x = _rows64(state["x"].double())
+    y = torch.zeros_like(x)
+    for e in range(case["experts"]):
+        mine = (state["ids"] == e).any(dim=1).nonzero()[:, 0]
+        if not len(mine):
+            continue
+        g = torch.mm(x[mine], _weights64(state["gate"][e], state["gate_scale"][e]).t())
+        u = torch.mm(x[mine], _weights64(state["up"][e], state["up_scale"][e]).t())
+        h = _rows64(g * torch.sigmoid(g) * u)
+        share = (state["weights"].double() * (state["ids"] == e)).sum(dim=1)[mine]
+        y[mine] += torch.mm(h, _weights64(state["down"][e], state["down_scale"][e]).t()) \
+            * share[:, None]
+    return y
