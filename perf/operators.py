@@ -207,8 +207,8 @@ def _quantised(x):
     """int8 values (as 32-bit floats) and scales of x's rows."""
     top = x.abs().amax(dim=-1, keepdim=True)
     none = top < TINY
-    q = torch.round(x * torch.where(none, 0.0, 127.0 / top)).clamp(-127, 127)
-    return q, torch.where(none, 0.0, top / 127.0)
+    q = torch.round(x * torch.where(none, 0.0, torch.full_like(top, 127.0) / top)).clamp(-127, 127)
+    return q, torch.where(none, 0.0, top / torch.full_like(top, 127.0))
 
 
 def _product(q, scale, w, w_scale):
