@@ -6,7 +6,9 @@
  * (wc_decode), or multiplies weights into activations while decoding them,
  * never writing them out (wc_gemv, wc_gemm: bf16 and fp8; wc_gemm_i8: int8;
  * wc_gemv_mx: MXFP4; wc_gemv_w4: int4 with group scales).  Compression runs on the host (wc_encode) or on the GPU
- * (wc_encode_device), to the same blob.
+ * (wc_encode_device), to the same blob.  The layers of a decoded int8 checkpoint
+ * run on wc_linear_i8 (activations quantised per token, scaled products),
+ * wc_route and wc_experts_i8 (a mixture layer's routing and experts).
  *
  * Paper: "Approaching Shannon Bound with Lossless LLM Weight Compression"
  * (Tan, Chen, Alonso, Wong, He).
@@ -499,6 +501,147 @@ wc_status wc_encode_device(const wc_dtensor* t, uint32_t n, const wc_params* p, 
  * Asynchronous; allocates nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
 wc_status wc_stream(const void* dev_src, uint64_t src_bytes, void* dev_dst, uint64_t dst_bytes,
                     uint32_t blocks, void* stream, uint64_t* read_bytes);
+
+/* --- 8-bit integer layers ----------------------------------------------------
+ * What a program runs on an int8 checkpoint (codes and per-row scales, the
+ * sq8 / W8A8 format of Sec. VI-A) once wc_decode has given it back: activations
+ * quantised per token, int8 products with the scales applied, routing to
+ * experts and the experts' feed-forward.  All device pointers, all on `stream`,
+ * asynchronous, allocating nothing.  Element types of activations, scales and
+ * results are WC_BF16, WC_FP16 or WC_FP32. */
+#define WC_FP32 8 /* 32-bit floats: an element type, not a storage format of wc_dtype */
+
+/* Bytes of a row of quantised activations of k elements: whole 128-byte blocks,
+ * zero past k. */
+#define WC_I8_ROW_BYTES(k) (((uint64_t)(k) + 127u) / 128u * 128u)
+
+/* wc_quantize_i8 -- rows of activations to int8, one scale a row.  With a =
+ * max |x| of a row: scale = a / 127, q = rint(x * (127 / a)), half to even, in
+ * fp32.  A row with a < 1e-30 gives zeros and scale 0; a row that holds an
+ * infinity or a NaN gives a scale that is one, so every product with it is NaN.
+ *   dev_x, x_dtype  m rows of k elements, `ldx` elements apart, aligned to the
+ *                   element (16-byte aligned rows are faster);
+ *   m, k            0..2^31 - 1 rows, 1..65536 columns;
+ *   dev_q           m rows of WC_I8_ROW_BYTES(k) bytes, 16-byte aligned;
+ *   dev_scale       m floats.
+ * Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_quantize_i8(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
+                         int8_t* dev_q, float* dev_scale, void* stream);
+
+/* One int8 matrix that multiplies quantised activations: y = (q W^T) * scale of
+ * the x row * scale of the W row + bias, summed exactly in int32, scaled in fp32
+ * and rounded once to y's type. */
+typedef struct {
+  const void* w;       /* n rows of k int8 codes, ldw bytes apart, any alignment */
+  const void* scale;   /* n row scales of scale_dtype */
+  const void* bias;    /* NULL, or n values of bias_dtype */
+  void* y;             /* m rows of n elements of y_dtype, ldy elements apart (NULL if m = 0) */
+  uint64_t ldw, ldy;
+  uint32_t n;
+  int32_t scale_dtype, bias_dtype, y_dtype;
+} wc_i8_job;
+
+/* wc_matmul_i8 -- the products of one batch of quantised activations with
+ * n_jobs (1..32) matrices, in one launch (two where a long k is split).
+ *   dev_q, dev_scale  what wc_quantize_i8 wrote for m rows of k (the padding of
+ *                     a row must be zero);
+ *   dev_workspace     at least wc_matmul_i8_workspace_bytes bytes, 256-byte
+ *                     aligned (NULL where that is 0); overwritten; calls that
+ *                     share it must not overlap in time.
+ * Nothing outside the matrices is read, whatever their strides.  m = 0 is a
+ * call that does nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_matmul_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
+                                       const wc_i8_job* jobs, uint64_t* bytes);
+wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, uint32_t m, uint32_t k,
+                       uint32_t n_jobs, const wc_i8_job* jobs, void* dev_workspace,
+                       uint64_t workspace_bytes, void* stream);
+
+/* wc_linear_i8 -- wc_quantize_i8 and wc_matmul_i8 in one call: linear layers
+ * that share their activations, e.g. q, k and v projections.  The quantised
+ * activations stay in the workspace.  Returns WC_EINVAL, WC_EHIP. */
+wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
+                                       const wc_i8_job* jobs, uint64_t* bytes);
+wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
+                       uint32_t n_jobs, const wc_i8_job* jobs, void* dev_workspace,
+                       uint64_t workspace_bytes, void* stream);
+
+#define WC_SCORE_SOFTMAX 0
+#define WC_SCORE_SIGMOID 1
+
+/* How wc_route chooses.  experts 1..512, k 1..min(32, experts); groups divides
+ * experts; top_groups 1..groups; group_top 1 or 2, at most experts / groups. */
+typedef struct {
+  uint32_t experts, k;
+  int32_t score;        /* WC_SCORE_* */
+  int32_t renormalize;  /* 0, or the chosen scores are divided by their sum */
+  uint32_t groups, top_groups, group_top;
+  float scale;          /* multiplies the weights */
+} wc_route_params;
+
+/* wc_route -- each token's experts, their weights, and the order of the
+ * experts' rows.  Scores s = softmax or sigmoid of a token's logits, in fp32;
+ * keys s + bias.  With groups > 1, each group of experts / groups neighbours is
+ * ranked by the sum of its group_top largest keys, and only the top_groups best
+ * take part.  The k largest keys are chosen, in order, ties to the lower index;
+ * weights are the chosen scores (not the keys), renormalised if asked, times
+ * scale.
+ *   An expert whose logit or bias is -inf is masked: it takes no part, in the
+ * softmax's sum either.  A token with fewer than k experts left has id -1 and
+ * weight 0 in its last slots.  A NaN logit of an expert that is not masked makes
+ * its token's weights NaN, and that expert is not chosen.
+ *   dev_logits, dtype  tokens rows of experts logits, ld elements apart;
+ *   dev_bias           NULL, or experts floats;
+ *   dev_ids            tokens x k int32;
+ *   dev_weights        tokens x k floats;
+ *   dev_offsets        experts + 1 int32: where each expert's rows start in the
+ *                      order (the last entry: slots that have an expert);
+ *   dev_order          tokens x k int32: slots (token * k + place) sorted by
+ *                      expert, by slot within one; slots without one last;
+ *   dev_workspace      at least wc_route_workspace_bytes bytes, 16-byte aligned.
+ * tokens * k < 2^31; tokens = 0 writes only the offsets.  The result is the same
+ * on every run.  Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_route_workspace_bytes(uint32_t tokens, const wc_route_params* p, uint64_t* bytes);
+wc_status wc_route(const void* dev_logits, int32_t dtype, uint32_t tokens, uint64_t ld,
+                   const wc_route_params* p, const float* dev_bias, int32_t* dev_ids,
+                   float* dev_weights, int32_t* dev_offsets, int32_t* dev_order,
+                   void* dev_workspace, uint64_t workspace_bytes, void* stream);
+
+/* The int8 matrices of a mixture layer's experts: for expert e, n rows of k
+ * codes at w + e * stride (no padding between rows), their scales at
+ * scale + e * n elements. */
+typedef struct {
+  const void* w;
+  const void* scale;
+  uint64_t stride;      /* bytes between experts, at least n * k */
+  int32_t scale_dtype, reserved;
+} wc_i8_experts;
+
+/* wc_experts_i8 -- the gated feed-forward of a mixture layer: for every token
+ * y = sum over its slots of weight * down(h), h = silu(gate x) * (up x), with the
+ * matrices of the slot's expert; x and h are quantised per token (as by
+ * wc_quantize_i8) before each product, h and the experts' results are held in
+ * fp32 in between, and the slots are added in their order, in fp32.
+ *   dev_x, dtype   tokens rows of hidden elements, ldx elements apart;
+ *   ids .. order   as wc_route writes them for tokens, experts and k.  Which
+ *                  rows an expert takes goes by offsets and order; a slot whose
+ *                  id is negative adds weight * 0;
+ *   gate, up       matrices of ffn rows of hidden columns; down: hidden rows of
+ *                  ffn columns (hidden, ffn 1..65536, experts 1..512);
+ *   dev_y          tokens rows of hidden elements of x's type, ldy apart;
+ *   dev_workspace  at least wc_experts_i8_workspace_bytes bytes, 256-byte
+ *                  aligned; overwritten; calls that share it must not overlap.
+ * Entries of offsets or order out of range are taken as the nearest in range:
+ * the result is then wrong, but nothing outside the arguments is touched.
+ * Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_experts_i8_workspace_bytes(uint32_t tokens, uint32_t k, uint32_t experts,
+                                        uint32_t hidden, uint32_t ffn, uint64_t* bytes);
+wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t tokens, uint64_t ldx,
+                        uint32_t k, uint32_t experts, uint32_t hidden, uint32_t ffn,
+                        const int32_t* dev_ids, const float* dev_weights,
+                        const int32_t* dev_offsets, const int32_t* dev_order,
+                        const wc_i8_experts* gate, const wc_i8_experts* up,
+                        const wc_i8_experts* down, void* dev_y, uint64_t ldy,
+                        void* dev_workspace, uint64_t workspace_bytes, void* stream);
 
 /* wc_free -- release a blob from wc_encode / wc_open.  NULL is a no-op. */
 void wc_free(wc_blob* b);

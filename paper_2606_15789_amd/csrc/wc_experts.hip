@@ -1,0 +1,272 @@
+// wc_experts.hip -- the feed-forward of a mixture layer with int8 experts:
+// wc_experts_i8.
+#include "wc_i8.h"
+
+namespace {
+
+using namespace wc_i8;
+
+constexpr int kRowWaves = 8;
+
+struct Bank {
+  uint64_t w, scale, stride;
+  int32_t scale_dtype;
+};
+struct ExpertArgs {
+  uint64_t offsets, order, ids, weights;
+  uint64_t xq, xscale;    // quantised x, by token
+  uint64_t h;             // fp32, by place in the order
+  uint64_t hq, hscale;    // quantised h
+  uint64_t out;           // experts' results, fp32, by slot
+  uint64_t y, ldy;
+  uint32_t tokens, k, experts, hidden, ffn, slots;
+  int32_t dtype;
+  Bank gate, up, down;
+};
+
+// Which expert the tile-th block of kRows places of the order belongs to, blocks
+// counted expert by expert: the places are [first, last).  False past the last
+// block.  Every wave works it out for itself.
+template <int kRows>
+__device__ __forceinline__ bool tile_of(const ExpertArgs& a, uint32_t tile, uint32_t& expert,
+                                        uint32_t& first, uint32_t& last) {
+  const uint32_t lane = threadIdx.x % 64;
+  uint32_t done = 0;
+  for (uint32_t e0 = 0; e0 < a.experts; e0 += 64) {
+    const uint32_t e = e0 + lane;
+    uint32_t from = 0, to = 0;
+    if (e < a.experts) {
+      from = min(uint32_t(max(global<const int32_t>(a.offsets)[e], 0)), a.slots);
+      to = min(uint32_t(max(global<const int32_t>(a.offsets)[e + 1], 0)), a.slots);
+    }
+    uint32_t blocks = to > from ? (to - from + kRows - 1) / kRows : 0, sum = blocks;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t v = uint32_t(__shfl_up(int(sum), d));
+      if (lane >= uint32_t(d)) sum += v;
+    }
+    const uint64_t past = __ballot(done + sum > tile);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      expert = e0 + uint32_t(at);
+      const uint32_t before = done + uint32_t(__shfl(int(sum - blocks), at));
+      first = uint32_t(__shfl(int(from), at)) + (tile - before) * kRows;
+      last = min(uint32_t(__shfl(int(to), at)), first + kRows);
+      return true;
+    }
+    done += uint32_t(__shfl(int(sum), 63));
+  }
+  return false;
+}
+
+__device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place) {
+  return min(uint32_t(max(global<const int32_t>(a.order)[place], 0)), a.slots - 1);
+}
+
+// 16 columns of an expert's result for up to 16 of its rows: kMats products that
+// share their rows (gate and up, or down alone), k split over the waves.
+template <int kMats>
+__device__ __forceinline__ void expert_product(global_ptr<const uint8_t> x, const uint64_t (&mats)[2],
+                                               uint32_t n, uint32_t k,
+                                               int32_t (&part)[kRowWaves][kMats * 256]) {
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane >> 4;
+  global_ptr<const uint8_t> w[kMats];
+  i32x4 acc[kMats];
+#pragma unroll
+  for (int t = 0; t < kMats; t++) {
+    w[t] = global<const uint8_t>(mats[t]) + uint64_t(n) * k + g * 32;
+    acc[t] = {0, 0, 0, 0};
+  }
+  const uint32_t whole = k / 128, blocks = (k + 127) / 128;
+  const auto step = [&](uint32_t b, int32_t left) {
+    const auto p = reinterpret_cast<global_ptr<const i32x4>>(x + g * 32 + uint64_t(b) * 128);
+    const i32x4 x0 = p[0], x1 = p[1];
+#pragma unroll
+    for (int t = 0; t < kMats; t++) {
+      const i32x4 w0 = load_codes(w[t] + uint64_t(b) * 128, left);
+      const i32x4 w1 = load_codes(w[t] + uint64_t(b) * 128 + 16, left - 16);
+      acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w0, x0, acc[t], 0, 0, 0);
+      acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w1, x1, acc[t], 0, 0, 0);
+    }
+  };
+  uint32_t b = wave;
+  for (; b < whole; b += kRowWaves) step(b, 32);
+  if (b < blocks) step(b, int32_t(k - b * 128) - int32_t(g * 32));
+#pragma unroll
+  for (int t = 0; t < kMats; t++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) part[wave][t * 256 + i * 64 + lane] = acc[t][i];
+  __syncthreads();
+}
+
+template <int kMats>
+__device__ __forceinline__ int32_t summed(const int32_t (&part)[kRowWaves][kMats * 256], int t,
+                                          uint32_t n, uint32_t m) {
+  const uint32_t at = uint32_t(t) * 256 + n % 4 * 64 + n / 4 * 16 + m;
+  int32_t sum = 0;
+#pragma unroll
+  for (int v = 0; v < kRowWaves; v++) sum += part[v][at];
+  return sum;
+}
+
+// h = silu(gate x) * (up x) of 16 columns for up to 16 places of the order.
+__global__ __launch_bounds__(64 * kRowWaves) void wc_experts_up_kernel(ExpertArgs a) {
+  __shared__ int32_t part[kRowWaves][2 * 256];
+  uint32_t e, first, last;
+  if (!tile_of<16>(a, blockIdx.x, e, first, last)) return;
+  const uint32_t n0 = blockIdx.y * 16, r = threadIdx.x % 16;
+  const uint32_t token = slot_at(a, min(first + r, last - 1)) / a.k;
+  const uint64_t mats[2] = {a.gate.w + e * a.gate.stride, a.up.w + e * a.up.stride};
+  expert_product<2>(global<const uint8_t>(a.xq) + token * WC_I8_ROW_BYTES(a.hidden), mats,
+                    min(n0 + r, a.ffn - 1), a.hidden, part);
+  for (uint32_t o = threadIdx.x; o < 256; o += 64 * kRowWaves) {
+    const uint32_t n = n0 + o % 16, place = first + o / 16;
+    if (n >= a.ffn || place >= last) continue;
+    const float xs = global<const float>(a.xscale)[slot_at(a, place) / a.k];
+    const uint64_t at = uint64_t(e) * a.ffn + n;
+    const float g = float(summed<2>(part, 0, o % 16, o / 16)) * xs *
+                    load_float(a.gate.scale, a.gate.scale_dtype, at);
+    const float u = float(summed<2>(part, 1, o % 16, o / 16)) * xs *
+                    load_float(a.up.scale, a.up.scale_dtype, at);
+    global<float>(a.h)[uint64_t(place) * a.ffn + n] = g / (1.0f + expf(-g)) * u;
+  }
+}
+
+// down(h) of 16 columns for up to 16 places, stored by slot.
+__global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertArgs a) {
+  __shared__ int32_t part[kRowWaves][256];
+  uint32_t e, first, last;
+  if (!tile_of<16>(a, blockIdx.x, e, first, last)) return;
+  const uint32_t n0 = blockIdx.y * 16, r = threadIdx.x % 16;
+  const uint64_t mats[2] = {a.down.w + e * a.down.stride, 0};
+  expert_product<1>(global<const uint8_t>(a.hq) + min(first + r, last - 1) * WC_I8_ROW_BYTES(a.ffn),
+                    mats, min(n0 + r, a.hidden - 1), a.ffn, part);
+  for (uint32_t o = threadIdx.x; o < 256; o += 64 * kRowWaves) {
+    const uint32_t n = n0 + o % 16, place = first + o / 16;
+    if (n >= a.hidden || place >= last) continue;
+    global<float>(a.out)[uint64_t(slot_at(a, place)) * a.hidden + n] =
+        float(summed<1>(part, 0, o % 16, o / 16)) * global<const float>(a.hscale)[place] *
+        load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
+  }
+}
+
+// y of one token: its slots' results in their order, times their weights.
+__global__ __launch_bounds__(256) void wc_experts_join_kernel(ExpertArgs a) {
+  const uint32_t token = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  if (n >= a.hidden) return;
+  float sum = 0.0f;
+  for (uint32_t j = 0; j < a.k; j++) {
+    const uint64_t slot = uint64_t(token) * a.k + j;
+    const float v = global<const int32_t>(a.ids)[slot] < 0
+                        ? 0.0f
+                        : global<const float>(a.out)[slot * a.hidden + n];
+    sum += global<const float>(a.weights)[slot] * v;
+  }
+  store_float(a.y, a.dtype, token * a.ldy + n, sum);
+}
+
+struct Workspace {
+  uint64_t xq, xscale, wide, hq, hscale, bytes;
+};
+Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
+  Workspace w{};
+  uint64_t at = 0;
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t here = at;
+    at += pad256(bytes);
+    return here;
+  };
+  w.xq = take(tokens * WC_I8_ROW_BYTES(hidden));
+  w.xscale = take(tokens * 4);
+  // h, and after its quantisation the experts' results
+  w.wide = take(tokens * k * (hidden > ffn ? hidden : ffn) * 4);
+  w.hq = take(tokens * k * WC_I8_ROW_BYTES(ffn));
+  w.hscale = take(tokens * k * 4);
+  w.bytes = at;
+  return w;
+}
+bool sizes_ok(uint32_t tokens, uint32_t k, uint32_t experts, uint32_t hidden, uint32_t ffn) {
+  return k >= 1 && experts >= 1 && experts <= kMaxExperts && k <= experts && hidden >= 1 &&
+         hidden <= kMaxK && ffn >= 1 && ffn <= kMaxK && uint64_t(tokens) * k < (1ull << 24);
+}
+bool bank_ok(const wc_i8_experts* b, uint64_t n, uint64_t k) {
+  return b && b->w && b->scale && float_ok(b->scale_dtype) && b->stride >= n * k &&
+         !(b->stride >> 40) && reinterpret_cast<uintptr_t>(b->scale) % size_of(b->scale_dtype) == 0;
+}
+Bank bank(const wc_i8_experts* b) {
+  return {reinterpret_cast<uint64_t>(b->w), reinterpret_cast<uint64_t>(b->scale), b->stride,
+          b->scale_dtype};
+}
+
+}  // namespace
+
+extern "C" wc_status wc_experts_i8_workspace_bytes(uint32_t tokens, uint32_t k, uint32_t experts,
+                                                   uint32_t hidden, uint32_t ffn, uint64_t* bytes) {
+  if (!bytes) return WC_EINVAL;
+  *bytes = 0;
+  if (!sizes_ok(tokens, k, experts, hidden, ffn)) return WC_EINVAL;
+  *bytes = layout(tokens, k, hidden, ffn).bytes;
+  return WC_OK;
+}
+
+extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t tokens, uint64_t ldx,
+                                   uint32_t k, uint32_t experts, uint32_t hidden, uint32_t ffn,
+                                   const int32_t* dev_ids, const float* dev_weights,
+                                   const int32_t* dev_offsets, const int32_t* dev_order,
+                                   const wc_i8_experts* gate, const wc_i8_experts* up,
+                                   const wc_i8_experts* down, void* dev_y, uint64_t ldy,
+                                   void* dev_workspace, uint64_t workspace_bytes, void* stream) {
+  if (!sizes_ok(tokens, k, experts, hidden, ffn) || !float_ok(dtype) || ldx < hidden || ldx >> 31 ||
+      ldy < hidden || ldy >> 31 || !bank_ok(gate, ffn, hidden) || !bank_ok(up, ffn, hidden) ||
+      !bank_ok(down, hidden, ffn))
+    return WC_EINVAL;
+  if (tokens == 0) return WC_OK;
+  const auto off = [](const void* p, uint32_t to) {
+    return !p || reinterpret_cast<uintptr_t>(p) % to != 0;
+  };
+  if (off(dev_x, size_of(dtype)) || off(dev_y, size_of(dtype)) || off(dev_ids, 4) ||
+      off(dev_weights, 4) || off(dev_offsets, 4) || off(dev_order, 4))
+    return WC_EINVAL;
+  const Workspace w = layout(tokens, k, hidden, ffn);
+  if (off(dev_workspace, 256) || workspace_bytes < w.bytes) return WC_EINVAL;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const uint64_t ws = reinterpret_cast<uint64_t>(dev_workspace);
+  const uint32_t slots = tokens * k;
+  ExpertArgs a{};
+  a.offsets = reinterpret_cast<uint64_t>(dev_offsets);
+  a.order = reinterpret_cast<uint64_t>(dev_order);
+  a.ids = reinterpret_cast<uint64_t>(dev_ids);
+  a.weights = reinterpret_cast<uint64_t>(dev_weights);
+  a.xq = ws + w.xq;
+  a.xscale = ws + w.xscale;
+  a.h = a.out = ws + w.wide;
+  a.hq = ws + w.hq;
+  a.hscale = ws + w.hscale;
+  a.y = reinterpret_cast<uint64_t>(dev_y);
+  a.ldy = ldy;
+  a.tokens = tokens;
+  a.k = k;
+  a.experts = experts;
+  a.hidden = hidden;
+  a.ffn = ffn;
+  a.slots = slots;
+  a.dtype = dtype;
+  a.gate = bank(gate);
+  a.up = bank(up);
+  a.down = bank(down);
+  if (!launch_quantize(dev_x, dtype, tokens, hidden, ldx, reinterpret_cast<void*>(a.xq),
+                       reinterpret_cast<float*>(a.xscale), st))
+    return WC_EHIP;
+  // every expert that has rows ends in at most one block that is not full
+  const uint32_t blocks = slots / 16 + (experts < slots ? experts : slots);
+  const dim3 threads(64 * kRowWaves);
+  hipLaunchKernelGGL(wc_experts_up_kernel, dim3(blocks, (ffn + 15) / 16), threads, 0, st, a);
+  if (hipGetLastError() != hipSuccess) return WC_EHIP;
+  if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, ffn,
+                       reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st))
+    return WC_EHIP;
+  hipLaunchKernelGGL(wc_experts_down_kernel, dim3(blocks, (hidden + 15) / 16), threads, 0, st, a);
+  if (hipGetLastError() != hipSuccess) return WC_EHIP;
+  hipLaunchKernelGGL(wc_experts_join_kernel, dim3(tokens, (hidden + 255) / 256), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
+}

@@ -1,0 +1,102 @@
+// wc_i8.h -- device helpers of the 8-bit integer layers: element types, the
+// int8 rows' loads and the quantisation of one row.
+#pragma once
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include "wc_internal.h"
+
+namespace wc_i8 {
+
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(1)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Pointers into global memory: said so, since an address from a table of
+// arguments is a generic one to the compiler, and a flat access waits for LDS too.
+template <class T>
+using global_ptr = T __attribute__((address_space(1)))*;
+template <class T>
+__device__ __forceinline__ global_ptr<T> global(uint64_t address) {
+  return reinterpret_cast<global_ptr<T>>(address);
+}
+
+constexpr uint32_t kMaxK = 65536;     // |x w| <= 2^14: no int32 sum overflows
+constexpr uint32_t kMaxExperts = 512;
+constexpr uint32_t kMaxJobs = 32;
+constexpr float kTinyRow = 1e-30f;    // rows below it count as zeros
+
+inline bool float_ok(int32_t dt) { return dt == WC_BF16 || dt == WC_FP16 || dt == WC_FP32; }
+inline uint32_t size_of(int32_t dt) { return dt == WC_FP32 ? 4u : 2u; }
+inline uint64_t pad256(uint64_t x) { return (x + 255) & ~uint64_t(255); }
+
+__device__ __forceinline__ float bf16_to_float(uint32_t h) { return __uint_as_float(h << 16); }
+__device__ __forceinline__ float fp16_to_float(uint32_t h) {
+  return float(__builtin_bit_cast(_Float16, uint16_t(h)));
+}
+// to nearest, ties to even; a NaN stays one
+__device__ __forceinline__ uint32_t float_to_bf16(float f) {
+  const uint32_t b = __float_as_uint(f);
+  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return (b >> 16) | 0x40u;
+  return (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
+}
+__device__ __forceinline__ uint32_t float_to_fp16(float f) {
+  return __builtin_bit_cast(uint16_t, _Float16(f));
+}
+
+// element i of the elements of type dt at address p
+__device__ __forceinline__ float load_float(uint64_t p, int32_t dt, uint64_t i) {
+  if (dt == WC_FP32) return global<const float>(p)[i];
+  const uint32_t h = global<const uint16_t>(p)[i];
+  return dt == WC_BF16 ? bf16_to_float(h) : fp16_to_float(h);
+}
+__device__ __forceinline__ void store_float(uint64_t p, int32_t dt, uint64_t i, float v) {
+  if (dt == WC_FP32)
+    global<float>(p)[i] = v;
+  else
+    global<uint16_t>(p)[i] = uint16_t(dt == WC_BF16 ? float_to_bf16(v) : float_to_fp16(v));
+}
+
+// 16 bytes of an int8 row, of which `valid` are inside it (the others come back
+// as zeros and are not read); any alignment.
+__device__ __forceinline__ i32x4 load_codes(global_ptr<const uint8_t> p, int32_t valid) {
+  if (valid >= 16) return __builtin_bit_cast(i32x4, *reinterpret_cast<global_ptr<const u32x4u>>(p));
+  i32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 16; i++)
+    if (i < valid) v[i / 4] |= int32_t(uint32_t(p[i]) << (8 * (i % 4)));
+  return v;
+}
+
+// The scale of a row and the factor to its codes, from the bits of its largest
+// magnitude (a NaN's are above an infinity's, which are above any number's).
+struct RowScale {
+  float scale, inverse;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t max_bits) {
+  const float top = __uint_as_float(max_bits);
+  if (top < kTinyRow) return {0.0f, 0.0f};
+  return {top / 127.0f, 127.0f / top};
+}
+// rint(x * inverse), half to even, as a byte; NaN gives 0
+__device__ __forceinline__ uint32_t code_of(float x, float inverse) {
+  const float r = __builtin_rintf(x * inverse);
+  return r == r ? uint32_t(int32_t(fminf(fmaxf(r, -127.0f), 127.0f))) & 0xFFu : 0u;
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = max(v, uint32_t(__shfl_xor(int(v), d)));
+  return v;
+}
+
+// Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes
+// (wc_i8.hip); false on a launch error.
+bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
+                     float* scale, hipStream_t stream);
+
+}  // namespace wc_i8

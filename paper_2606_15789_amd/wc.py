@@ -8,10 +8,12 @@ numpy / torch objects to the plain pointers and sizes of the C ABI declared in
 
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import operator
 import os
 import struct
+from collections import namedtuple
 
 import numpy as np
 
@@ -27,7 +29,10 @@ DERR = {1: "WC_DERR_INDEX", 2: "WC_DERR_STATE", 4: "WC_DERR_CURSOR", 8: "WC_DERR
 EXPORTS = ["wc_analyze", "wc_encode", "wc_open", "wc_decode", "wc_gemv", "wc_free",
            "wc_version", "wc_analyze_device", "wc_encode_device_bounds", "wc_encode_device",
            "wc_gemm_workspace_bytes", "wc_gemm", "wc_gemm_i8", "wc_gemv_mx", "wc_gemv_w4",
-           "wc_stream", "wc_analyze_device_static"]
+           "wc_stream", "wc_analyze_device_static", "wc_quantize_i8",
+           "wc_matmul_i8_workspace_bytes", "wc_matmul_i8", "wc_linear_i8_workspace_bytes",
+           "wc_linear_i8", "wc_route_workspace_bytes", "wc_route",
+           "wc_experts_i8_workspace_bytes", "wc_experts_i8"]
 
 ANALYZE_WORKSPACE_BYTES = 524288  # WC_ANALYZE_WORKSPACE_BYTES
 
@@ -67,6 +72,23 @@ class _Blob(C.Structure):
                 ("state_bytes", C.c_uint64), ("word_bytes", C.c_uint64),
                 ("pad_bytes", C.c_uint64), ("raw_bytes", C.c_uint64),
                 ("priv", C.c_void_p)]
+
+
+class _I8Job(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("scale", C.c_void_p), ("bias", C.c_void_p),
+                ("y", C.c_void_p), ("ldw", C.c_uint64), ("ldy", C.c_uint64), ("n", C.c_uint32),
+                ("scale_dtype", C.c_int32), ("bias_dtype", C.c_int32), ("y_dtype", C.c_int32)]
+
+
+class _RouteParams(C.Structure):
+    _fields_ = [("experts", C.c_uint32), ("k", C.c_uint32), ("score", C.c_int32),
+                ("renormalize", C.c_int32), ("groups", C.c_uint32), ("top_groups", C.c_uint32),
+                ("group_top", C.c_uint32), ("scale", C.c_float)]
+
+
+class _I8Experts(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("scale", C.c_void_p), ("stride", C.c_uint64),
+                ("scale_dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -129,6 +151,27 @@ def lib():
         L.wc_stream.argtypes = [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_uint32,
                                 C.c_void_p, C.POINTER(C.c_uint64)]
         L.wc_stream.restype = C.c_int
+        job, experts = C.POINTER(_I8Job), C.POINTER(_I8Experts)
+        L.wc_quantize_i8.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint32, C.c_uint64,
+                                     C.c_void_p, C.c_void_p, C.c_void_p]
+        L.wc_matmul_i8_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32, C.c_uint32, job,
+                                                   C.POINTER(C.c_uint64)]
+        L.wc_matmul_i8.argtypes = [C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, job,
+                                   C.c_void_p, C.c_uint64, C.c_void_p]
+        L.wc_linear_i8_workspace_bytes.argtypes = L.wc_matmul_i8_workspace_bytes.argtypes
+        L.wc_linear_i8.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint32, C.c_uint64,
+                                   C.c_uint32, job, C.c_void_p, C.c_uint64, C.c_void_p]
+        L.wc_route_workspace_bytes.argtypes = [C.c_uint32, C.POINTER(_RouteParams),
+                                               C.POINTER(C.c_uint64)]
+        L.wc_route.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint64,
+                               C.POINTER(_RouteParams)] + [C.c_void_p] * 6 + [C.c_uint64,
+                                                                              C.c_void_p]
+        L.wc_experts_i8_workspace_bytes.argtypes = [C.c_uint32] * 5 + [C.POINTER(C.c_uint64)]
+        L.wc_experts_i8.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint64] \
+            + [C.c_uint32] * 4 + [C.c_void_p] * 4 + [experts] * 3 \
+            + [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]
+        for name in EXPORTS[EXPORTS.index("wc_quantize_i8"):]:
+            getattr(L, name).restype = C.c_int
         L.wc_free.argtypes = [C.POINTER(_Blob)]
         L.wc_free.restype = None
         L.wc_version.restype = C.c_int32
@@ -660,3 +703,269 @@ def gemv_w4_torch(blob: Blob, dev_blob, tensors, scales, zeros, xs, ys=None, str
             [x.data_ptr() for x in xs], m, [y.data_ptr() for y in ys], stream.cuda_stream,
             err.data_ptr() if err is not None else 0)
     return ys
+
+
+# --- 8-bit integer layers -----------------------------------------------------
+# The layers of a decoded int8 checkpoint.  Matrices are int8 (or the uint8 buffers
+# decode_torch fills: the same bytes), activations, scales and results bfloat16,
+# float16 or float32.
+
+_FLOAT_TYPES = {"torch.bfloat16": 1, "torch.float16": 2, "torch.float32": 8}
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _float_type(t, what: str) -> int:
+    code = _FLOAT_TYPES.get(str(t if not hasattr(t, "dtype") else t.dtype))
+    if code is None:
+        raise ValueError(f"{what} must be bfloat16, float16 or float32")
+    return code
+
+
+def _rows(t, what: str, cols: int = -1) -> int:
+    """Row stride, in elements, of a 2-D device tensor whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a 2-D device tensor")
+    if cols >= 0 and t.shape[1] != cols:
+        raise ValueError(f"{what} has {t.shape[1]} columns, not {cols}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be next to each other")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t, n: int, what: str) -> int:
+    if not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{what} must be a contiguous device tensor of {n} elements")
+    return _float_type(t, what)
+
+
+def _codes(t, what: str):
+    if str(t.dtype) not in ("torch.int8", "torch.uint8"):
+        raise ValueError(f"{what} must be int8 codes")
+    return t
+
+
+def _stream_of(stream, device):
+    """The stream to launch on, and the context in which to allocate what the launch
+    uses, so that the allocator knows the stream that uses it."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device), contextlib.nullcontext()
+    return stream, torch.cuda.stream(stream)
+
+
+def _workspace(workspace, need: int, device):
+    import torch
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    if workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
+        raise ValueError(f"the workspace needs {need} contiguous bytes")
+    return workspace
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _size(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def i8_row_bytes(k: int) -> int:
+    """WC_I8_ROW_BYTES: bytes of a row of quantised activations."""
+    return (k + 127) // 128 * 128
+
+
+def quantize_i8_torch(x, q=None, scale=None, stream=None):
+    """wc_quantize_i8 of a 2-D tensor: (q, scale), q int8 of m x i8_row_bytes(k) (zero
+    past column k) and scale float32 of m; the row's values are q * scale."""
+    import torch
+    ld = _rows(x, "x")
+    dt = _float_type(x, "x")
+    m, k = x.shape
+    st, where = _stream_of(stream, x.device)
+    with where:
+        if q is None:
+            q = torch.empty((m, i8_row_bytes(k)), dtype=torch.int8, device=x.device)
+        if scale is None:
+            scale = torch.empty(m, dtype=torch.float32, device=x.device)
+    if tuple(q.shape) != (m, i8_row_bytes(k)) or q.dtype != torch.int8 or not q.is_contiguous():
+        raise ValueError(f"q must be a contiguous int8 tensor of {m} x {i8_row_bytes(k)}")
+    if scale.dtype != torch.float32 or scale.numel() != m or not scale.is_contiguous():
+        raise ValueError(f"scale must be {m} contiguous float32")
+    rc = lib().wc_quantize_i8(x.data_ptr(), dt, m, k, ld, q.data_ptr(), scale.data_ptr(),
+                              st.cuda_stream)
+    if rc:
+        raise WcError("wc_quantize_i8", rc)
+    return q, scale
+
+
+def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, device):
+    """ctypes wc_i8_job array and the ys (allocated where None)."""
+    import torch
+    n_jobs = len(ws)
+    if len(scales) != n_jobs or (biases is not None and len(biases) != n_jobs) or \
+            (ys is not None and len(ys) != n_jobs):
+        raise ValueError("one scale tensor, bias entry and y a matrix")
+    jobs = (_I8Job * max(1, n_jobs))()
+    out = []
+    for i, w in enumerate(ws):
+        ldw = _rows(_codes(w, "w"), "w", k)
+        n = w.shape[0]
+        y = torch.empty((m, n), dtype=dtype, device=device) if ys is None else ys[i]
+        out.append(y)
+        if tuple(y.shape) != (m, n):
+            raise ValueError(f"y must be {m} x {n}")
+        b = None if biases is None else biases[i]
+        jobs[i] = _I8Job(w.data_ptr(), scales[i].data_ptr(), _ptr(b), y.data_ptr(), ldw,
+                         _rows(y, "y"), n, _vector(scales[i], n, "a matrix's scale"),
+                         0 if b is None else _vector(b, n, "a bias"), _float_type(y, "y"))
+    return jobs, out
+
+
+def matmul_i8_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=None,
+                    workspace=None, stream=None):
+    """wc_matmul_i8: (q * scale) @ (W_i * scales_i)^T + biases_i for each int8 W_i (n_i x
+    k) of `ws`, with q and scale from quantize_i8_torch.  ys (of any float type, rows
+    contiguous) are allocated in `dtype` (bfloat16 if None) where None."""
+    import torch
+    m = q.shape[0]
+    if q.dtype != torch.int8 or not q.is_contiguous() or tuple(q.shape) != (m, i8_row_bytes(k)):
+        raise ValueError(f"q must be a contiguous int8 tensor of {i8_row_bytes(k)} columns")
+    if scale.dtype != torch.float32:
+        raise ValueError("scale must be float32")
+    _vector(scale, m, "scale")
+    st, where = _stream_of(stream, q.device)
+    need = C.c_uint64(0)
+    with where:
+        jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or torch.bfloat16, q.device)
+        rc = lib().wc_matmul_i8_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
+        if not rc:
+            workspace = _workspace(workspace, need.value, q.device)
+    if not rc:
+        rc = lib().wc_matmul_i8(q.data_ptr(), scale.data_ptr(), m, k, len(ws), jobs,
+                                _ptr(workspace), _size(workspace), st.cuda_stream)
+    if rc:
+        raise WcError("wc_matmul_i8", rc)
+    return ys
+
+
+def linear_i8_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=None,
+                    stream=None):
+    """wc_linear_i8: x quantised per row, then as matmul_i8_torch; `dtype` defaults to
+    x's type."""
+    ld = _rows(x, "x")
+    dt = _float_type(x, "x")
+    m, k = x.shape
+    st, where = _stream_of(stream, x.device)
+    need = C.c_uint64(0)
+    with where:
+        jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, x.device)
+        rc = lib().wc_linear_i8_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
+        if not rc:
+            workspace = _workspace(workspace, need.value, x.device)
+    if not rc:
+        rc = lib().wc_linear_i8(x.data_ptr(), dt, m, k, ld, len(ws), jobs, _ptr(workspace),
+                                _size(workspace), st.cuda_stream)
+    if rc:
+        raise WcError("wc_linear_i8", rc)
+    return ys
+
+
+# What wc_route writes: ids and weights (tokens x k), offsets (experts + 1), order
+# (tokens * k slots sorted by expert).
+Routing = namedtuple("Routing", "ids weights offsets order")
+
+
+def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int = 1,
+                top_groups: int = 1, group_top: int = 1, renormalize: bool = True,
+                scale: float = 1.0, out=None, workspace=None, stream=None) -> Routing:
+    """wc_route of a router's logits (tokens x experts); `bias` float32 of experts;
+    `out` a Routing to write into."""
+    import torch
+    ld = _rows(logits, "logits")
+    dt = _float_type(logits, "logits")
+    tokens, experts = logits.shape
+    if score not in SCORES:
+        raise ValueError(f"score must be one of {sorted(SCORES)}")
+    if bias is not None and _vector(bias, experts, "bias") != 8:
+        raise ValueError("bias must be float32")
+    dev = logits.device
+    st, where = _stream_of(stream, dev)
+    params = _RouteParams(experts, k, SCORES[score], int(renormalize), groups, top_groups,
+                          group_top, scale)
+    need = C.c_uint64(0)
+    rc = lib().wc_route_workspace_bytes(tokens, C.byref(params), C.byref(need))
+    if rc:
+        raise WcError("wc_route", rc)
+    with where:
+        if out is None:
+            out = Routing(torch.empty((tokens, k), dtype=torch.int32, device=dev),
+                          torch.empty((tokens, k), dtype=torch.float32, device=dev),
+                          torch.empty(experts + 1, dtype=torch.int32, device=dev),
+                          torch.empty(tokens * k, dtype=torch.int32, device=dev))
+        else:
+            _check_routing(out, tokens, k, experts)
+        workspace = _workspace(workspace, need.value, dev)
+    rc = lib().wc_route(logits.data_ptr(), dt, tokens, ld, C.byref(params), _ptr(bias),
+                        *(t.data_ptr() for t in out), _ptr(workspace), _size(workspace),
+                        st.cuda_stream)
+    if rc:
+        raise WcError("wc_route", rc)
+    return out
+
+
+def _check_routing(r, tokens: int, k: int, experts: int):
+    import torch
+    for t, shape, dtype, name in ((r.ids, (tokens, k), torch.int32, "ids"),
+                                  (r.weights, (tokens, k), torch.float32, "weights"),
+                                  (r.offsets, (experts + 1,), torch.int32, "offsets"),
+                                  (r.order, (tokens * k,), torch.int32, "order")):
+        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {shape}")
+
+
+def _bank(w, scale, experts: int, n: int, k: int, what: str):
+    _codes(w, what)
+    if tuple(w.shape) != (experts, n, k) or not w.is_cuda or not w[0].is_contiguous():
+        raise ValueError(f"{what} must be {experts} x {n} x {k} codes, contiguous in each expert")
+    if tuple(scale.shape) != (experts, n):
+        raise ValueError(f"the scales of {what} must be {experts} x {n}")
+    return _I8Experts(w.data_ptr(), scale.data_ptr(), w.stride(0) if experts > 1 else n * k,
+                      _vector(scale, experts * n, f"the scales of {what}"), 0)
+
+
+def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, down_scale,
+                     y=None, workspace=None, stream=None):
+    """wc_experts_i8: the feed-forward of a mixture layer.  x tokens x hidden; gate, up
+    int8 of experts x ffn x hidden, down of experts x hidden x ffn, with scales of
+    experts x rows; y of x's type."""
+    import torch
+    ld = _rows(x, "x")
+    dt = _float_type(x, "x")
+    tokens, hidden = x.shape
+    if gate.dim() != 3 or routing.ids.dim() != 2:
+        raise ValueError("gate must be experts x ffn x hidden, the ids tokens x k")
+    experts, ffn = gate.shape[:2]
+    k = routing.ids.shape[1]
+    _check_routing(routing, tokens, k, experts)
+    banks = (_bank(gate, gate_scale, experts, ffn, hidden, "gate"),
+             _bank(up, up_scale, experts, ffn, hidden, "up"),
+             _bank(down, down_scale, experts, hidden, ffn, "down"))
+    st, where = _stream_of(stream, x.device)
+    need = C.c_uint64(0)
+    rc = lib().wc_experts_i8_workspace_bytes(tokens, k, experts, hidden, ffn, C.byref(need))
+    if rc:
+        raise WcError("wc_experts_i8", rc)
+    with where:
+        if y is None:
+            y = torch.empty((tokens, hidden), dtype=x.dtype, device=x.device)
+        workspace = _workspace(workspace, need.value, x.device)
+    if tuple(y.shape) != (tokens, hidden) or y.dtype != x.dtype:
+        raise ValueError(f"y must be {tokens} x {hidden} of x's type")
+    rc = lib().wc_experts_i8(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
+                             *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
+                             y.data_ptr(), _rows(y, "y"), _ptr(workspace), _size(workspace),
+                             st.cuda_stream)
+    if rc:
+        raise WcError("wc_experts_i8", rc)
+    return y

@@ -1,0 +1,124 @@
+"""CPU: what the 8-bit layers' entry points refuse before anything is launched, and
+the workspace they ask for.  Pointers are made up and never followed."""
+import ctypes as C
+
+import pytest
+
+from paper_2606_15789_amd import wc
+
+EINVAL = -1
+A = 1 << 20  # an aligned address that is never read
+
+
+def _job(**more):
+    f = dict(w=A, scale=A, bias=None, y=A, ldw=64, ldy=8, n=8, scale_dtype=2, bias_dtype=0, y_dtype=1)
+    f.update(more)
+    return wc._I8Job(**f)
+
+
+def _jobs(*jobs):
+    return (wc._I8Job * max(1, len(jobs)))(*jobs)
+
+
+def test_quantize_refusals():
+    ok = [A, 1, 4, 64, 64, A, A, None]
+    for at, v in ((0, None), (0, A + 1), (1, 3), (1, 0), (3, 0), (3, 65537), (4, 63), (4, 1 << 31),
+                  (5, None), (5, A + 8), (6, None), (6, A + 2), (2, 1 << 31)):
+        args = list(ok)
+        args[at] = v
+        assert wc.lib().wc_quantize_i8(*args) == EINVAL, (at, v)
+    assert wc.lib().wc_quantize_i8(None, 1, 0, 64, 64, None, None, None) == 0  # no rows
+
+
+@pytest.mark.parametrize("bad", [
+    dict(w=None), dict(scale=None), dict(y=None), dict(n=0), dict(n=1 << 31), dict(ldw=63),
+    dict(ldw=1 << 31), dict(ldy=7), dict(ldy=1 << 31), dict(scale_dtype=3), dict(scale_dtype=0),
+    dict(y_dtype=5), dict(bias=A, bias_dtype=0), dict(scale=A + 1), dict(y=A + 1),
+    dict(bias=A + 2, bias_dtype=8), dict(y=A + 2, y_dtype=8)])
+def test_job_refusals(bad):
+    L = wc.lib()
+    need = C.c_uint64(7)
+    jobs = _jobs(_job(), _job(**bad))
+    assert L.wc_linear_i8_workspace_bytes(4, 64, 2, jobs, C.byref(need)) == EINVAL
+    assert need.value == 0
+    assert L.wc_matmul_i8_workspace_bytes(4, 64, 2, jobs, C.byref(need)) == EINVAL
+    assert L.wc_matmul_i8(A, A, 4, 64, 2, jobs, A, 1 << 30, None) == EINVAL
+    assert L.wc_linear_i8(A, 1, 4, 64, 64, 2, jobs, A, 1 << 30, None) == EINVAL
+
+
+def test_linear_refusals():
+    L = wc.lib()
+    need = C.c_uint64(0)
+    jobs = _jobs(_job())
+    assert L.wc_linear_i8_workspace_bytes(4, 64, 1, jobs, C.byref(need)) == 0
+    assert need.value >= 4 * wc.i8_row_bytes(64) + 16 and need.value % 256 == 0
+    for args in ((4, 64, 0, jobs), (4, 64, 33, jobs), (4, 0, 1, jobs), (4, 65537, 1, jobs),
+                 (1 << 31, 64, 1, jobs), (4, 64, 1, None)):
+        assert L.wc_linear_i8_workspace_bytes(*args, C.byref(need)) == EINVAL
+    assert L.wc_linear_i8_workspace_bytes(4, 64, 1, jobs, None) == EINVAL
+    n = wc.i8_row_bytes(64) * 4 + 256
+    for x, dt, ldx, ws, size in ((None, 1, 64, A, n), (A + 1, 1, 64, A, n), (A, 4, 64, A, n),
+                                 (A, 1, 63, A, n), (A, 1, 64, None, n), (A, 1, 64, A + 16, n),
+                                 (A, 1, 64, A, n - 1)):
+        assert L.wc_linear_i8(x, dt, 4, 64, ldx, 1, jobs, ws, size, None) == EINVAL
+    for q, s in ((None, A), (A, None), (A + 4, A), (A, A + 1)):
+        assert L.wc_matmul_i8(q, s, 4, 64, 1, jobs, A, 1 << 30, None) == EINVAL
+    none = _jobs(_job(y=None))
+    assert L.wc_matmul_i8(None, None, 0, 64, 1, none, None, 0, None) == 0
+    assert L.wc_linear_i8(None, 1, 0, 64, 64, 1, none, None, 0, None) == 0
+
+
+def test_route_refusals():
+    L = wc.lib()
+    need = C.c_uint64(0)
+
+    def params(**more):
+        f = dict(experts=16, k=2, score=0, renormalize=1, groups=1, top_groups=1, group_top=1, scale=1.0)
+        f.update(more)
+        return C.byref(wc._RouteParams(**f))
+    assert L.wc_route_workspace_bytes(10, params(), C.byref(need)) == 0
+    for bad in (dict(experts=0), dict(experts=513), dict(k=0), dict(k=17), dict(experts=64, k=33),
+                dict(score=2), dict(score=-1), dict(groups=0), dict(groups=3), dict(top_groups=0),
+                dict(top_groups=2), dict(group_top=0), dict(group_top=3),
+                dict(groups=16, top_groups=1, group_top=2), dict(scale=float("nan")),
+                dict(scale=float("inf"))):
+        assert L.wc_route_workspace_bytes(10, params(**bad), C.byref(need)) == EINVAL, bad
+    assert L.wc_route_workspace_bytes(1 << 30, params(), C.byref(need)) == EINVAL
+    assert L.wc_route_workspace_bytes(10, None, C.byref(need)) == EINVAL
+    ok = [A, 1, 4096, 16, params(), None, A, A, A, A, A, 1 << 30, None]
+    for at, v in ((0, None), (0, A + 1), (1, 6), (3, 15), (3, 1 << 31), (5, A + 2), (6, None),
+                  (7, None), (8, None), (9, None), (6, A + 1), (7, A + 1), (8, A + 2), (9, A + 3),
+                  (10, None), (10, A + 8), (11, 16)):
+        args = list(ok)
+        args[at] = v
+        assert L.wc_route(*args) == EINVAL, (at, v)
+
+
+def test_experts_refusals():
+    L = wc.lib()
+    need = C.c_uint64(0)
+    assert L.wc_experts_i8_workspace_bytes(4, 2, 8, 64, 32, C.byref(need)) == 0
+    size = need.value
+    assert size % 256 == 0
+    for args in ((4, 0, 8, 64, 32), (4, 9, 8, 64, 32), (4, 2, 0, 64, 32), (4, 2, 513, 64, 32),
+                 (4, 2, 8, 0, 32), (4, 2, 8, 65537, 32), (4, 2, 8, 64, 0), (4, 2, 8, 64, 65537),
+                 (1 << 24, 2, 8, 64, 32)):
+        assert L.wc_experts_i8_workspace_bytes(*args, C.byref(need)) == EINVAL, args
+
+    def bank(**more):
+        f = dict(w=A, scale=A, stride=64 * 32, scale_dtype=2, reserved=0)
+        f.update(more)
+        return C.byref(wc._I8Experts(**f))
+    ok = [A, 1, 4, 64, 2, 8, 64, 32, A, A, A, A, bank(), bank(), bank(), A, 64, A, size, None]
+    for at, v in ((0, None), (0, A + 1), (1, 3), (3, 63), (3, 1 << 31), (8, None), (9, None),
+                  (10, None), (11, A + 2), (12, None), (13, bank(w=None)), (14, bank(stride=2047)),
+                  (12, bank(scale=None)), (13, bank(scale_dtype=4)), (14, bank(scale=A + 1)),
+                  (12, bank(stride=1 << 40)), (15, None), (15, A + 1), (16, 63), (17, None),
+                  (17, A + 128), (18, size - 1)):
+        args = list(ok)
+        args[at] = v
+        assert L.wc_experts_i8(*args) == EINVAL, (at, v)
+    args = list(ok)
+    args[2] = 0
+    args[0] = args[15] = args[17] = None
+    assert L.wc_experts_i8(*args) == 0  # no tokens
