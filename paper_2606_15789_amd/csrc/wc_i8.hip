@@ -1,5 +1,5 @@
 // wc_i8.hip -- int8 linear layers: wc_quantize_i8, wc_matmul_i8, wc_linear_i8.
-#include "wc_i8.h"
+#include "wc_i8_tile.h"
 
 namespace {
 
@@ -35,12 +35,14 @@ __global__ __launch_bounds__(256) void wc_quantize_i8_kernel(uint64_t x, int32_t
 
 struct MatJob {
   uint64_t w, scale, bias, y, ldw, ldy;
+  uint64_t part;      // where k is split: its int32 sums, split by split
   uint32_t n, tile0;  // tile0: its first workgroup
-  int32_t scale_dtype, bias_dtype, y_dtype, reserved;
+  int32_t scale_dtype, bias_dtype, y_dtype;
+  uint32_t quads;     // four neighbours of y can be stored at once
 };
 struct MatArgs {
   uint64_t q, qscale;
-  uint32_t m, k, n_jobs, reserved;
+  uint32_t m, k, n_jobs, splits;
   MatJob job[kMaxJobs];
 };
 
@@ -103,6 +105,130 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_matmul_i8_rows_kernel(MatAr
   }
 }
 
+// y of four neighbouring columns from their sums.
+__device__ __forceinline__ void finish(const MatJob& J, uint32_t m, uint32_t n, f32x4 sum, float xs,
+                                       const float (&scale)[4], const float (&bias)[4]) {
+  const uint64_t at = m * J.ldy + n;
+  f32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; i++) v[i] = sum[i] * xs * scale[i] + bias[i];
+  if (J.quads && n + 4 <= J.n) {
+    if (J.y_dtype == WC_FP32) {
+      *reinterpret_cast<global_ptr<f32x4>>(global<float>(J.y) + at) = v;
+    } else {
+      uint32_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) h[i] = J.y_dtype == WC_BF16 ? float_to_bf16(v[i]) : float_to_fp16(v[i]);
+      *reinterpret_cast<global_ptr<u32x2>>(global<uint16_t>(J.y) + at) =
+          u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      if (n + i < J.n) store_float(J.y, J.y_dtype, at + i, v[i]);
+  }
+}
+__device__ __forceinline__ void column_scales(const MatJob& J, uint32_t n, float (&scale)[4],
+                                              float (&bias)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const uint32_t c = min(n + i, J.n - 1);
+    scale[i] = load_float(J.scale, J.scale_dtype, c);
+    bias[i] = J.bias ? load_float(J.bias, J.bias_dtype, c) : 0.0f;
+  }
+}
+
+// One tile of a job (and one part of k) a workgroup.
+template <class T, bool kDirect>
+__global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+  constexpr uint32_t kBM = T::kMT * 32 * T::kWM_, kBN = T::kNT * 32 * T::kWN_;
+  uint32_t j = 0;
+  while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
+  const MatJob J = a.job[j];
+  uint32_t mt, nt;
+  tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt);
+  const uint32_t m0 = mt * kBM, n0 = nt * kBN;
+  const uint32_t m_rows = min(kBM, a.m - m0), n_rows = min(kBN, J.n - n0);
+  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k)), all = row_bytes / kStage;
+  // this workgroup's part of the stages
+  const uint32_t each = all / a.splits, rest = all % a.splits, part = blockIdx.y;
+  const uint32_t s0 = part * each + min(part, rest), stages = each + (part < rest);
+  const uint32_t k0 = s0 * kStage;
+  const u32x4 xr = rows_rsrc(a.q + m0 * uint64_t(row_bytes) + k0, m_rows * row_bytes - k0);
+  uint32_t xoff[T::kXLoads];
+#pragma unroll
+  for (int i = 0; i < T::kXLoads; i++)
+    xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
+  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); };
+  i32x16 acc[T::kMT][T::kNT];
+  if constexpr (kDirect) {
+    const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw + k0, uint32_t((n_rows - 1) * J.ldw + a.k - k0));
+    uint32_t woff[T::kWLoads];
+#pragma unroll
+    for (int i = 0; i < T::kWLoads; i++)
+      woff[i] = min(T::row_of(i), n_rows - 1) * uint32_t(J.ldw) + T::byte_of();
+    T::product(lds, stages, load_x,
+               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * kStage); }, acc);
+  } else {
+    global_ptr<const uint8_t> w[T::kWLoads];
+#pragma unroll
+    for (int i = 0; i < T::kWLoads; i++)
+      w[i] = global<const uint8_t>(J.w) + (n0 + min(T::row_of(i), n_rows - 1)) * J.ldw + k0 + T::byte_of();
+    const int32_t left = int32_t(a.k - k0) - int32_t(T::byte_of());
+    T::product(lds, stages, load_x, [&](int i, uint32_t s, uint32_t) {
+      return load_codes(w[i] + uint64_t(s) * kStage, left - int32_t(s * kStage));
+    }, acc);
+  }
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  constexpr int kCols = T::kNT * 32;
+  const uint32_t nw = n0 + wave % T::kWN_ * kCols, mw = m0 + wave / T::kWN_ * (T::kMT * 32);
+  float scale[4], bias[4];
+  if (a.splits == 1) column_scales(J, nw + lane % (kCols / 4) * 4, scale, bias);
+#pragma unroll
+  for (int b = 0; b < T::kMT; b++) {
+    if (a.splits == 1) {
+      T::template rows_out<kCols>(
+          lds, [&](int c, int i) { return float(acc[b][c][i]); },
+          [&](uint32_t row, uint32_t col, f32x4 v) {
+            const uint32_t m = mw + b * 32 + row, n = nw + col;
+            if (m < a.m && n < J.n) finish(J, m, n, v, global<const float>(a.qscale)[m], scale, bias);
+          });
+    } else {
+      T::template rows_out<kCols>(
+          lds, [&](int c, int i) { return __int_as_float(acc[b][c][i]); },
+          [&](uint32_t row, uint32_t col, f32x4 v) {
+            const uint32_t m = mw + b * 32 + row, n = nw + col;
+            if (m >= a.m || n >= J.n) return;
+            const uint64_t pitch = (J.n + 3u) & ~3u;
+            *reinterpret_cast<global_ptr<f32x4>>(global<float>(J.part) +
+                                                 (uint64_t(part) * a.m + m) * pitch + n) = v;
+          });
+    }
+  }
+}
+
+// y from the sums of the parts of k.
+__global__ __launch_bounds__(256) void wc_matmul_i8_join_kernel(MatArgs a) {
+  const uint32_t j = blockIdx.z;
+  const MatJob J = a.job[j];
+  const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4;
+  if (n >= J.n) return;
+  const uint64_t pitch = (J.n + 3u) & ~3u;
+  float scale[4], bias[4];
+  column_scales(J, n, scale, bias);
+  for (uint32_t m = blockIdx.x; m < a.m; m += gridDim.x) {
+    i32x4 sum = {0, 0, 0, 0};
+    for (uint32_t p = 0; p < a.splits; p++)
+      sum += *reinterpret_cast<global_ptr<const i32x4>>(global<const int32_t>(J.part) +
+                                                        (uint64_t(p) * a.m + m) * pitch + n);
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = float(sum[i]);
+    finish(J, m, n, v, global<const float>(a.qscale)[m], scale, bias);
+  }
+}
+
 bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   if (!jobs || n_jobs < 1 || n_jobs > kMaxJobs || k < 1 || k > kMaxK || m > 0x7FFFFFFFu)
     return false;
@@ -130,20 +256,85 @@ bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx) {
          (m == 0 || (x && reinterpret_cast<uintptr_t>(x) % size_of(dt) == 0));
 }
 
+using Tile256 = Tile<256, 256, 2, 4>;
+using Tile128 = Tile<128, 128, 2, 2>;
+
+// Which kernel multiplies m rows, and in how many parts of k.
+enum class Kernel { kRows, kTile128, kTile256 };
+struct Plan {
+  Kernel kernel;
+  bool direct;      // every W can go to LDS as it is
+  uint32_t splits;
+  uint64_t part_bytes;
+};
+Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
+  Plan p{Kernel::kRows, true, 1, 0};
+  if (m <= 64) return p;
+  uint64_t tiles128 = 0, tiles256 = 0, sums = 0;
+  for (uint32_t i = 0; i < n_jobs; i++) {
+    const wc_i8_job& J = jobs[i];
+    // offsets within a tile's rows are 32-bit
+    if (J.ldw > (1u << 22)) return p;
+    p.direct = p.direct && k % 4 == 0 && J.ldw % 16 == 0 && reinterpret_cast<uintptr_t>(J.w) % 16 == 0;
+    tiles128 += uint64_t(m + 127) / 128 * ((J.n + 127) / 128);
+    tiles256 += uint64_t(m + 255) / 256 * ((J.n + 255) / 256);
+    sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
+  }
+  if (tiles128 > 0x7FFFFFFFu) return p;
+  p.kernel = tiles256 >= 192 ? Kernel::kTile256 : Kernel::kTile128;
+  const uint64_t tiles = p.kernel == Kernel::kTile256 ? tiles256 : tiles128;
+  const uint32_t stages = (k + kStage - 1) / kStage;
+  const uint64_t slots = p.kernel == Kernel::kTile256 ? 256 : 512;
+  while (tiles * p.splits * 2 <= slots && stages >= p.splits * 2 * 8) p.splits *= 2;
+  if (p.splits > 1) p.part_bytes = sums * p.splits;
+  return p;
+}
+
 wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, uint32_t n_jobs,
-                 const wc_i8_job* jobs, hipStream_t stream) {
+                 const wc_i8_job* jobs, const Plan& p, void* parts, hipStream_t stream) {
   MatArgs a{};
   a.q = reinterpret_cast<uint64_t>(q);
   a.qscale = reinterpret_cast<uint64_t>(scale);
   a.k = k;
   a.n_jobs = n_jobs;
-  uint32_t tiles = 0;
+  a.splits = p.splits;
+  uint32_t tiles = 0, widest = 0;
+  uint64_t part = reinterpret_cast<uint64_t>(parts);
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
+    const uint32_t size = size_of(J.y_dtype);
     a.job[i] = {reinterpret_cast<uint64_t>(J.w),    reinterpret_cast<uint64_t>(J.scale),
                 reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
-                J.ldw, J.ldy, J.n, tiles, J.scale_dtype, J.bias_dtype, J.y_dtype, 0};
-    tiles += (J.n + 15) / 16;
+                J.ldw, J.ldy, part, J.n, tiles, J.scale_dtype, J.bias_dtype, J.y_dtype,
+                J.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0};
+    if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
+    widest = J.n > widest ? J.n : widest;
+    tiles += p.kernel == Kernel::kRows      ? (J.n + 15) / 16
+             : p.kernel == Kernel::kTile128 ? (m + 127) / 128 * ((J.n + 127) / 128)
+                                            : (m + 255) / 256 * ((J.n + 255) / 256);
+  }
+  if (p.kernel != Kernel::kRows) {
+    a.m = m;
+    const dim3 grid(tiles, p.splits);
+    if (p.kernel == Kernel::kTile256) {
+      if (p.direct)
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile256, true>), grid, dim3(512), 0, stream, a);
+      else
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile256, false>), grid, dim3(512), 0, stream, a);
+    } else {
+      if (p.direct)
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile128, true>), grid, dim3(256), 0, stream, a);
+      else
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile128, false>), grid, dim3(256), 0, stream, a);
+    }
+    if (hipGetLastError() != hipSuccess) return WC_EHIP;
+    if (p.splits > 1) {
+      const uint32_t rows = m < 65536 ? m : 65536;
+      hipLaunchKernelGGL(wc_matmul_i8_join_kernel, dim3(rows, (widest + 1023) / 1024, n_jobs), dim3(256),
+                         0, stream, a);
+      if (hipGetLastError() != hipSuccess) return WC_EHIP;
+    }
+    return WC_OK;
   }
   // a grid's second axis holds 65535 blocks of 64 rows
   constexpr uint32_t kSlice = 65535u * 64;
@@ -194,20 +385,29 @@ extern "C" wc_status wc_matmul_i8_workspace_bytes(uint32_t m, uint32_t k, uint32
                                                   const wc_i8_job* jobs, uint64_t* bytes) {
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
-  return jobs_ok(m, k, n_jobs, jobs) ? WC_OK : WC_EINVAL;
+  if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
+  *bytes = plan_of(m, k, n_jobs, jobs).part_bytes;
+  return WC_OK;
 }
+
+namespace {
+bool workspace_ok(const void* p, uint64_t bytes, uint64_t need) {
+  return need == 0 || (p && reinterpret_cast<uintptr_t>(p) % 256 == 0 && bytes >= need);
+}
+}  // namespace
 
 extern "C" wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, uint32_t m,
                                   uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs,
                                   void* dev_workspace, uint64_t workspace_bytes, void* stream) {
-  (void)dev_workspace;
-  (void)workspace_bytes;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
   if (m == 0) return WC_OK;
   if (!dev_q || !dev_scale || reinterpret_cast<uintptr_t>(dev_q) % 16 ||
       reinterpret_cast<uintptr_t>(dev_scale) % 4)
     return WC_EINVAL;
-  return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, reinterpret_cast<hipStream_t>(stream));
+  const Plan p = plan_of(m, k, n_jobs, jobs);
+  if (!workspace_ok(dev_workspace, workspace_bytes, p.part_bytes)) return WC_EINVAL;
+  return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, p, dev_workspace,
+                reinterpret_cast<hipStream_t>(stream));
 }
 
 extern "C" wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
@@ -215,7 +415,8 @@ extern "C" wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
-  *bytes = pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)) + pad256(uint64_t(m) * 4);
+  *bytes = pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)) + pad256(uint64_t(m) * 4) +
+           plan_of(m, k, n_jobs, jobs).part_bytes;
   return WC_OK;
 }
 
@@ -227,11 +428,11 @@ extern "C" wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m
       wc_linear_i8_workspace_bytes(m, k, n_jobs, jobs, &need) != WC_OK)
     return WC_EINVAL;
   if (m == 0) return WC_OK;
-  if (!dev_workspace || reinterpret_cast<uintptr_t>(dev_workspace) % 256 || workspace_bytes < need)
-    return WC_EINVAL;
+  if (!workspace_ok(dev_workspace, workspace_bytes, need)) return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   int8_t* q = static_cast<int8_t*>(dev_workspace);
   float* scale = reinterpret_cast<float*>(q + pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)));
+  void* parts = reinterpret_cast<uint8_t*>(scale) + pad256(uint64_t(m) * 4);
   if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, scale, st)) return WC_EHIP;
-  return matmul(q, scale, m, k, n_jobs, jobs, st);
+  return matmul(q, scale, m, k, n_jobs, jobs, plan_of(m, k, n_jobs, jobs), parts, st);
 }
