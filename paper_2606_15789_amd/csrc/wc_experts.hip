@@ -1,12 +1,15 @@
 // wc_experts.hip -- the feed-forward of a mixture layer with int8 experts:
 // wc_experts_i8.
-#include "wc_i8.h"
+#include "wc_i8_tile.h"
 
 namespace {
 
 using namespace wc_i8;
 
 constexpr int kRowWaves = 8;
+
+// Rows of h and of the experts' results are whole groups of four floats.
+__host__ __device__ constexpr uint32_t pitch_of(uint32_t n) { return (n + 3u) & ~3u; }
 
 struct Bank {
   uint64_t w, scale, stride;
@@ -20,6 +23,7 @@ struct ExpertArgs {
   uint64_t out;           // experts' results, fp32, by slot
   uint64_t y, ldy;
   uint32_t tokens, k, experts, hidden, ffn, slots;
+  uint32_t blocks;        // upper bound of the tiles of places, tile kernels only
   int32_t dtype;
   Bank gate, up, down;
 };
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_up_kernel(ExpertArg
                     load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(summed<2>(part, 1, o % 16, o / 16)) * xs *
                     load_float(a.up.scale, a.up.scale_dtype, at);
-    global<float>(a.h)[uint64_t(place) * a.ffn + n] = g / (1.0f + expf(-g)) * u;
+    global<float>(a.h)[uint64_t(place) * pitch_of(a.ffn) + n] = g / (1.0f + expf(-g)) * u;
   }
 }
 
@@ -144,25 +148,169 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertA
   for (uint32_t o = threadIdx.x; o < 256; o += 64 * kRowWaves) {
     const uint32_t n = n0 + o % 16, place = first + o / 16;
     if (n >= a.hidden || place >= last) continue;
-    global<float>(a.out)[uint64_t(slot_at(a, place)) * a.hidden + n] =
+    global<float>(a.out)[uint64_t(slot_at(a, place)) * pitch_of(a.hidden) + n] =
         float(summed<1>(part, 0, o % 16, o / 16)) * global<const float>(a.hscale)[place] *
         load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
   }
 }
 
-// y of one token: its slots' results in their order, times their weights.
+// The same on tiles through LDS.  A wave's columns of W are 32 of gate and the same 32
+// of up, so that both products of a value of h meet in one lane.
+template <class T, bool kDirect>
+__global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+  static_assert(T::kNT == 2);
+  constexpr uint32_t kBM = T::kMT * 32 * T::kWM_, kCols = T::kWN_ * 32;
+  uint32_t mt, nt, e, first, last;
+  tile_at(blockIdx.x, a.blocks, (a.ffn + kCols - 1) / kCols, mt, nt);
+  if (!tile_of<kBM>(a, mt, e, first, last)) return;
+  e = __builtin_amdgcn_readfirstlane(e);
+  const uint32_t n0 = nt * kCols, k = a.hidden, row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
+  const uint32_t n_rows = min(kCols, a.ffn - n0), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const u32x4 xr = rows_rsrc(a.xq, uint32_t(a.tokens * uint64_t(row_bytes)));
+  uint32_t xoff[T::kXLoads];
+#pragma unroll
+  for (int i = 0; i < T::kXLoads; i++)
+    xoff[i] = slot_at(a, min(first + T::row_of(i), last - 1)) / a.k * row_bytes + T::byte_of();
+  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); };
+  // W row r of the tile: column r / 64 * 32 + r mod 32 of gate (r mod 64 < 32) or of up
+  const uint64_t gate = a.gate.w + e * a.gate.stride + uint64_t(n0) * k;
+  const uint64_t up = a.up.w + e * a.up.stride + uint64_t(n0) * k;
+  i32x16 acc[T::kMT][2];
+  if constexpr (kDirect) {
+    const u32x4 gr = rows_rsrc(gate, n_rows * k), ur = rows_rsrc(up, n_rows * k);
+    uint32_t woff[T::kWLoads];
+#pragma unroll
+    for (int i = 0; i < T::kWLoads; i++) {
+      const uint32_t r = T::row_of(i);
+      woff[i] = min(r / 64 * 32 + r % 32, n_rows - 1) * k + T::byte_of();
+    }
+    T::product(lds, row_bytes / kStage, load_x, [&](int i, uint32_t s, uint32_t to) {
+      load_lds((wave + T::kWaves * i) & 4 ? ur : gr, to, woff[i] + s * kStage);
+    }, acc);
+  } else {
+    global_ptr<const uint8_t> w[T::kWLoads];
+#pragma unroll
+    for (int i = 0; i < T::kWLoads; i++) {
+      const uint32_t r = T::row_of(i);
+      w[i] = global<const uint8_t>((wave + T::kWaves * i) & 4 ? up : gate) +
+             uint64_t(min(r / 64 * 32 + r % 32, n_rows - 1)) * k + T::byte_of();
+    }
+    const int32_t left = int32_t(k) - int32_t(T::byte_of());
+    T::product(lds, row_bytes / kStage, load_x, [&](int i, uint32_t s, uint32_t) {
+      return load_codes(w[i] + uint64_t(s) * kStage, left - int32_t(s * kStage));
+    }, acc);
+  }
+  const uint32_t lane = threadIdx.x % 64;
+  const uint32_t nw = n0 + wave % T::kWN_ * 32, mw = first + wave / T::kWN_ * (T::kMT * 32);
+  float gs[4], us[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const uint64_t at = uint64_t(e) * a.ffn + min(nw + lane % 8 * 4 + i, a.ffn - 1);
+    gs[i] = load_float(a.gate.scale, a.gate.scale_dtype, at);
+    us[i] = load_float(a.up.scale, a.up.scale_dtype, at);
+  }
+#pragma unroll
+  for (int b = 0; b < T::kMT; b++)
+    T::template rows_out<32>(
+        lds, [&](int c, int i) { return float(acc[b][c][i]); },
+        [&](uint32_t row, uint32_t col, auto get) {
+          const uint32_t place = mw + b * 32 + row, n = nw + col;
+          if (place >= last || n >= a.ffn) return;
+          const float xs = global<const float>(a.xscale)[slot_at(a, place) / a.k];
+          const f32x4 g4 = get(0), u4 = get(32);
+          f32x4 h;
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            const float g = g4[i] * xs * gs[i], u = u4[i] * xs * us[i];
+            h[i] = g / (1.0f + expf(-g)) * u;
+          }
+          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.h) +
+                                               uint64_t(place) * pitch_of(a.ffn) + n) = h;
+        });
+}
+
+template <class T, bool kDirect>
+__global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(ExpertArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+  constexpr uint32_t kBM = T::kMT * 32 * T::kWM_, kBN = T::kNT * 32 * T::kWN_;
+  uint32_t mt, nt, e, first, last;
+  tile_at(blockIdx.x, a.blocks, (a.hidden + kBN - 1) / kBN, mt, nt);
+  if (!tile_of<kBM>(a, mt, e, first, last)) return;
+  e = __builtin_amdgcn_readfirstlane(e);
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+  const uint32_t n0 = nt * kBN, k = a.ffn, row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
+  const uint32_t n_rows = min(kBN, a.hidden - n0), m_rows = last - first;
+  const u32x4 xr = rows_rsrc(a.hq + uint64_t(first) * row_bytes, m_rows * row_bytes);
+  uint32_t xoff[T::kXLoads];
+#pragma unroll
+  for (int i = 0; i < T::kXLoads; i++)
+    xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
+  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); };
+  const uint64_t down = a.down.w + e * a.down.stride + uint64_t(n0) * k;
+  i32x16 acc[T::kMT][T::kNT];
+  if constexpr (kDirect) {
+    const u32x4 wr = rows_rsrc(down, n_rows * k);
+    uint32_t woff[T::kWLoads];
+#pragma unroll
+    for (int i = 0; i < T::kWLoads; i++)
+      woff[i] = min(T::row_of(i), n_rows - 1) * k + T::byte_of();
+    T::product(lds, row_bytes / kStage, load_x,
+               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * kStage); }, acc);
+  } else {
+    global_ptr<const uint8_t> w[T::kWLoads];
+#pragma unroll
+    for (int i = 0; i < T::kWLoads; i++)
+      w[i] = global<const uint8_t>(down) + uint64_t(min(T::row_of(i), n_rows - 1)) * k + T::byte_of();
+    const int32_t left = int32_t(k) - int32_t(T::byte_of());
+    T::product(lds, row_bytes / kStage, load_x, [&](int i, uint32_t s, uint32_t) {
+      return load_codes(w[i] + uint64_t(s) * kStage, left - int32_t(s * kStage));
+    }, acc);
+  }
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  constexpr int kCols = T::kNT * 32;
+  const uint32_t nw = n0 + wave % T::kWN_ * kCols, mw = first + wave / T::kWN_ * (T::kMT * 32);
+  float scale[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    scale[i] = load_float(a.down.scale, a.down.scale_dtype,
+                          uint64_t(e) * a.hidden + min(nw + lane % (kCols / 4) * 4 + i, a.hidden - 1));
+#pragma unroll
+  for (int b = 0; b < T::kMT; b++)
+    T::template rows_out<kCols>(
+        lds, [&](int c, int i) { return float(acc[b][c][i]); },
+        [&](uint32_t row, uint32_t col, auto get) {
+          const uint32_t place = mw + b * 32 + row, n = nw + col;
+          if (place >= last || n >= a.hidden) return;
+          const float hs = global<const float>(a.hscale)[place];
+          f32x4 v = get(0);
+#pragma unroll
+          for (int i = 0; i < 4; i++) v[i] = v[i] * hs * scale[i];
+          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) + uint64_t(slot_at(a, place)) *
+                                               pitch_of(a.hidden) + n) = v;
+        });
+}
+
+// y of one token, four columns a thread: its slots' results in their order, times
+// their weights.
 __global__ __launch_bounds__(256) void wc_experts_join_kernel(ExpertArgs a) {
-  const uint32_t token = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  const uint32_t token = blockIdx.x, n = (blockIdx.y * 256 + threadIdx.x) * 4;
   if (n >= a.hidden) return;
-  float sum = 0.0f;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   for (uint32_t j = 0; j < a.k; j++) {
     const uint64_t slot = uint64_t(token) * a.k + j;
-    const float v = global<const int32_t>(a.ids)[slot] < 0
-                        ? 0.0f
-                        : global<const float>(a.out)[slot * a.hidden + n];
-    sum += global<const float>(a.weights)[slot] * v;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (global<const int32_t>(a.ids)[slot] >= 0)
+      v = *reinterpret_cast<global_ptr<const f32x4>>(global<const float>(a.out) +
+                                                     slot * pitch_of(a.hidden) + n);
+    const float w = global<const float>(a.weights)[slot];
+#pragma unroll
+    for (int i = 0; i < 4; i++) sum[i] += w * v[i];
   }
-  store_float(a.y, a.dtype, token * a.ldy + n, sum);
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    if (n + i < a.hidden) store_float(a.y, a.dtype, token * a.ldy + n + i, sum[i]);
 }
 
 struct Workspace {
@@ -179,7 +327,7 @@ Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
   w.xq = take(tokens * WC_I8_ROW_BYTES(hidden));
   w.xscale = take(tokens * 4);
   // h, and after its quantisation the experts' results
-  w.wide = take(tokens * k * (hidden > ffn ? hidden : ffn) * 4);
+  w.wide = take(tokens * k * pitch_of(uint32_t(hidden > ffn ? hidden : ffn)) * 4);
   w.hq = take(tokens * k * WC_I8_ROW_BYTES(ffn));
   w.hscale = take(tokens * k * 4);
   w.bytes = at;
@@ -196,6 +344,37 @@ bool bank_ok(const wc_i8_experts* b, uint64_t n, uint64_t k) {
 Bank bank(const wc_i8_experts* b) {
   return {reinterpret_cast<uint64_t>(b->w), reinterpret_cast<uint64_t>(b->scale), b->stride,
           b->scale_dtype};
+}
+
+bool aligned16(const wc_i8_experts* b) {
+  return reinterpret_cast<uintptr_t>(b->w) % 16 == 0 && b->stride % 16 == 0;
+}
+
+// Rows of the order to a tile, by the rows an expert has on average.
+int tile_rows(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden) {
+  // a tile finds x by 32-bit offsets
+  if (tokens * WC_I8_ROW_BYTES(hidden) >> 32) return 16;
+  const uint32_t average = slots / experts;
+  return average >= 384 ? 256 : average >= 24 ? 128 : 16;
+}
+
+template <class T>
+void start_up(const ExpertArgs& a, bool direct, hipStream_t st) {
+  const uint32_t cols = T::kWN_ * 32;
+  const dim3 grid(a.blocks * ((a.ffn + cols - 1) / cols)), block(T::kThreads);
+  if (direct)
+    hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, false>), grid, block, 0, st, a);
+}
+template <class T>
+void start_down(const ExpertArgs& a, bool direct, hipStream_t st) {
+  const uint32_t cols = T::kWN_ * T::kNT * 32;
+  const dim3 grid(a.blocks * ((a.hidden + cols - 1) / cols)), block(T::kThreads);
+  if (direct)
+    hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, false>), grid, block, 0, st, a);
 }
 
 }  // namespace
@@ -257,16 +436,27 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   if (!launch_quantize(dev_x, dtype, tokens, hidden, ldx, reinterpret_cast<void*>(a.xq),
                        reinterpret_cast<float*>(a.xscale), st))
     return WC_EHIP;
+  // h, quantised, and the experts' results; the rows that have an expert end at the last
+  // offset
+  const bool direct = hidden % 16 == 0 && ffn % 16 == 0 && aligned16(gate) && aligned16(up) &&
+                      aligned16(down);
+  const int rows = tile_rows(tokens, slots, experts, hidden);
   // every expert that has rows ends in at most one block that is not full
-  const uint32_t blocks = slots / 16 + (experts < slots ? experts : slots);
-  const dim3 threads(64 * kRowWaves);
-  hipLaunchKernelGGL(wc_experts_up_kernel, dim3(blocks, (ffn + 15) / 16), threads, 0, st, a);
+  a.blocks = slots / uint32_t(rows) + (experts < slots ? experts : slots);
+  if (rows == 256) start_up<Tile<256, 256, 2, 4>>(a, direct, st);
+  else if (rows == 128) start_up<Tile<128, 128, 2, 2>>(a, direct, st);
+  else
+    hipLaunchKernelGGL(wc_experts_up_kernel, dim3(a.blocks, (ffn + 15) / 16), dim3(64 * kRowWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
-  if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, ffn,
-                       reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st))
+  if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, pitch_of(ffn),
+                       reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st,
+                       dev_offsets + experts))
     return WC_EHIP;
-  hipLaunchKernelGGL(wc_experts_down_kernel, dim3(blocks, (hidden + 15) / 16), threads, 0, st, a);
+  if (rows == 256) start_down<Tile<256, 256, 2, 4>>(a, direct, st);
+  else if (rows == 128) start_down<Tile<128, 128, 2, 2>>(a, direct, st);
+  else
+    hipLaunchKernelGGL(wc_experts_down_kernel, dim3(a.blocks, (hidden + 15) / 16), dim3(64 * kRowWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
-  hipLaunchKernelGGL(wc_experts_join_kernel, dim3(tokens, (hidden + 255) / 256), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(wc_experts_join_kernel, dim3(tokens, (hidden + 1023) / 1024), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
 }

@@ -95,8 +95,9 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 }
 
 // Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes
-// (wc_i8.hip); false on a launch error.
+// (wc_i8.hip), or as many of them as the device int `rows` says; false on a launch
+// error.
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     float* scale, hipStream_t stream);
+                     float* scale, hipStream_t stream, const int32_t* rows = nullptr);
 
 }  // namespace wc_i8

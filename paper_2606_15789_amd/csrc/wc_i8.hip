@@ -5,32 +5,86 @@ namespace {
 
 using namespace wc_i8;
 
-// One workgroup a row: the largest magnitude, then the codes.  The bits of |x|
-// order as the numbers do, so the maximum is an integer one, which keeps a NaN
-// and does not depend on the order.
-__global__ __launch_bounds__(256) void wc_quantize_i8_kernel(uint64_t x, int32_t dt,
-                                                             uint32_t k, uint64_t ldx,
-                                                             uint8_t* __restrict__ q,
-                                                             float* __restrict__ scale) {
-  __shared__ uint32_t top[4];
-  const uint64_t row = blockIdx.x, first = row * ldx;
-  uint32_t t = 0;
-  for (uint32_t i = threadIdx.x; i < k; i += 256)
-    t = max(t, __float_as_uint(load_float(x, dt, first + i)) & 0x7FFFFFFFu);
-  t = wave_max(t);
-  if (threadIdx.x % 64 == 0) top[threadIdx.x / 64] = t;
-  __syncthreads();
-  const RowScale s = row_scale(max(max(top[0], top[1]), max(top[2], top[3])));
-  const uint32_t bytes = uint32_t(WC_I8_ROW_BYTES(k));
-  uint32_t* out = reinterpret_cast<uint32_t*>(q + row * bytes);
-  for (uint32_t i = threadIdx.x; i < bytes / 4; i += 256) {
-    uint32_t v = 0;
+struct QuantArgs {
+  uint64_t x, ldx, q, scale, rows;
+  uint32_t k, vector;  // vector: rows are 16-byte aligned
+};
+
+// One workgroup a row, which its threads hold in registers in units of eight elements
+// (thread t has units t, t + kThreads, ...): read once, its largest magnitude found,
+// written as codes.  The bits of |x| order as the numbers do, so the maximum is an
+// integer one, which keeps a NaN and does not depend on the order.
+template <int kThreads, int kUnits, int kType>
+__global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
+  constexpr int kWords = kType == WC_FP32 ? 8 : 4;  // to a unit
+  __shared__ uint32_t tops[kThreads / 64];
+  const uint64_t row = blockIdx.x;
+  if (a.rows && int32_t(blockIdx.x) >= *global<const int32_t>(a.rows)) return;
+  const uint64_t first = a.x + row * a.ldx * (kType == WC_FP32 ? 4 : 2);
+  const uint32_t units = uint32_t(WC_I8_ROW_BYTES(a.k)) / 8;
+  uint32_t v[kUnits][kWords];
 #pragma unroll
-    for (uint32_t j = 0; j < 4; j++)
-      if (4 * i + j < k) v |= code_of(load_float(x, dt, first + 4 * i + j), s.inverse) << (8 * j);
-    out[i] = v;
+  for (int u = 0; u < kUnits; u++) {
+    const uint32_t at = (threadIdx.x + u * kThreads) * 8;
+    if (a.vector && at + 8 <= a.k) {
+      const auto p = global<const u32x4>(first + at * (kType == WC_FP32 ? 4 : 2));
+#pragma unroll
+      for (int i = 0; i < kWords / 4; i++) {
+        const u32x4 w = p[i];
+#pragma unroll
+        for (int j = 0; j < 4; j++) v[u][4 * i + j] = w[j];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; i++) v[u][i] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        if (at + i >= a.k) continue;
+        if constexpr (kType == WC_FP32)
+          v[u][i] = global<const uint32_t>(first)[at + i];
+        else
+          v[u][i / 2] |= uint32_t(global<const uint16_t>(first)[at + i]) << (16 * (i % 2));
+      }
+    }
   }
-  if (threadIdx.x == 0) scale[row] = s.scale;
+  const auto value = [&](int u, int i) {
+    if constexpr (kType == WC_FP32) return __uint_as_float(v[u][i]);
+    const uint32_t h = i % 2 ? v[u][i / 2] >> 16 : v[u][i / 2] & 0xFFFFu;
+    return kType == WC_BF16 ? bf16_to_float(h) : fp16_to_float(h);
+  };
+  uint32_t top = 0;
+#pragma unroll
+  for (int u = 0; u < kUnits; u++)
+#pragma unroll
+    for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(value(u, i)) & 0x7FFFFFFFu);
+  top = wave_max(top);
+  if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; w++) top = max(top, tops[w]);
+  const RowScale s = row_scale(top);
+  const auto out = global<u32x2>(a.q + row * units * 8);
+#pragma unroll
+  for (int u = 0; u < kUnits; u++) {
+    const uint32_t unit = threadIdx.x + u * kThreads;
+    if (unit >= units) continue;
+    u32x2 c = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; i++) c[i / 4] |= code_of(value(u, i), s.inverse) << (8 * (i % 4));
+    out[unit] = c;
+  }
+  if (threadIdx.x == 0) global<float>(a.scale)[row] = s.scale;
+}
+
+template <int kThreads, int kUnits>
+void start_quantize(int32_t dt, uint32_t m, const QuantArgs& a, hipStream_t stream) {
+  const dim3 grid(m), block(kThreads);
+  if (dt == WC_BF16)
+    hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_BF16>), grid, block, 0, stream, a);
+  else if (dt == WC_FP16)
+    hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP16>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP32>), grid, block, 0, stream, a);
 }
 
 struct MatJob {
@@ -190,19 +244,19 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
     if (a.splits == 1) {
       T::template rows_out<kCols>(
           lds, [&](int c, int i) { return float(acc[b][c][i]); },
-          [&](uint32_t row, uint32_t col, f32x4 v) {
+          [&](uint32_t row, uint32_t col, auto get) {
             const uint32_t m = mw + b * 32 + row, n = nw + col;
-            if (m < a.m && n < J.n) finish(J, m, n, v, global<const float>(a.qscale)[m], scale, bias);
+            if (m < a.m && n < J.n) finish(J, m, n, get(0), global<const float>(a.qscale)[m], scale, bias);
           });
     } else {
       T::template rows_out<kCols>(
           lds, [&](int c, int i) { return __int_as_float(acc[b][c][i]); },
-          [&](uint32_t row, uint32_t col, f32x4 v) {
+          [&](uint32_t row, uint32_t col, auto get) {
             const uint32_t m = mw + b * 32 + row, n = nw + col;
             if (m >= a.m || n >= J.n) return;
             const uint64_t pitch = (J.n + 3u) & ~3u;
             *reinterpret_cast<global_ptr<f32x4>>(global<float>(J.part) +
-                                                 (uint64_t(part) * a.m + m) * pitch + n) = v;
+                                                 (uint64_t(part) * a.m + m) * pitch + n) = get(0);
           });
     }
   }
@@ -359,10 +413,20 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
 namespace wc_i8 {
 
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     float* scale, hipStream_t stream) {
-  hipLaunchKernelGGL(wc_quantize_i8_kernel, dim3(m), dim3(256), 0, stream,
-                     reinterpret_cast<uint64_t>(x), dt, k, ldx,
-                     static_cast<uint8_t*>(q), scale);
+                     float* scale, hipStream_t stream, const int32_t* rows) {
+  const uint32_t size = size_of(dt);
+  const QuantArgs a = {reinterpret_cast<uint64_t>(x), ldx, reinterpret_cast<uint64_t>(q),
+                       reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(rows), k,
+                       reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * size % 16 == 0};
+  // few rows: more threads to each
+  if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, m, a, stream);
+  else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, m, a, stream);
+  else if (k <= 2048) start_quantize<256, 1>(dt, m, a, stream);
+  else if (k <= 4096) start_quantize<256, 2>(dt, m, a, stream);
+  else if (k <= 8192) start_quantize<256, 4>(dt, m, a, stream);
+  else if (k <= 16384) start_quantize<256, 8>(dt, m, a, stream);
+  else if (k <= 32768) start_quantize<1024, 4>(dt, m, a, stream);
+  else start_quantize<1024, 8>(dt, m, a, stream);
   return hipGetLastError() == hipSuccess;
 }
 

@@ -124,15 +124,16 @@ struct Tile {
   // The results of one 32-row block of x through the wave's own part of LDS, so that
   // rows are written whole: `value(block, i)` is this lane's result i of the given 32
   // columns (W row 8 (i / 4) + 4 (lane / 32) + i mod 4 of x row lane mod 32);
-  // `store(row, column, values)` takes four neighbours of kCols columns.
-  template <int kCols, class Value, class Store>
+  // `store(row, column, get)` writes four neighbouring columns of the first kOut, where
+  // get(first) are the four values from column first + column on.
+  template <int kOut, class Value, class Store>
   static __device__ __forceinline__ void rows_out(uint8_t* lds, Value value, Store store) {
-    constexpr int kRow = kCols + 4;  // floats: rows a bank apart
+    constexpr int kRow = kNT * 32 + 4;  // floats: rows a bank apart
     static_assert(kWaves * 32 * kRow * 4 <= kLds);
     const uint32_t lane = threadIdx.x % 64;
     float* t = reinterpret_cast<float*>(lds) + threadIdx.x / 64 * (32 * kRow);
 #pragma unroll
-    for (int c = 0; c < kCols / 32; c++)
+    for (int c = 0; c < kNT; c++)
 #pragma unroll
       for (int g = 0; g < 4; g++) {
         f32x4 v;
@@ -141,11 +142,13 @@ struct Tile {
         *reinterpret_cast<f32x4*>(t + lane % 32 * kRow + c * 32 + g * 8 + lane / 32 * 4) = v;
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int kLanes = kCols / 4;  // lanes to a row
+    constexpr int kLanes = kOut / 4;  // lanes to a row
 #pragma unroll
     for (int r = 0; r < 32; r += 64 / kLanes) {
       const uint32_t row = r + lane / kLanes, col = lane % kLanes * 4;
-      store(row, col, *reinterpret_cast<const f32x4*>(t + row * kRow + col));
+      store(row, col, [&](int first) {
+        return *reinterpret_cast<const f32x4*>(t + row * kRow + first + col);
+      });
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
