@@ -1,6 +1,6 @@
 // wc_experts.hip -- the feed-forward of a mixture layer with int8 experts:
 // wc_experts_i8.
-#include "wc_i8_tile.h"
+#include "wc_i8_ring.h"
 
 namespace {
 
@@ -150,6 +150,76 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertA
     if (n >= a.hidden || place >= last) continue;
     global<float>(a.out)[uint64_t(slot_at(a, place)) * pitch_of(a.hidden) + n] =
         float(summed<1>(part, 0, o % 16, o / 16)) * global<const float>(a.hscale)[place] *
+        load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
+  }
+}
+
+// The same from rings of whole lines.  The sixteen rows of a product's W are eight of
+// gate and the same eight of up.
+template <int kX>
+using ExpertRing = Ring<1, kX, 4, 4>;
+
+template <int kX>
+__global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_kernel(ExpertArgs a) {
+  using R = ExpertRing<kX>;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
+  uint32_t e, first, last;
+  if (!tile_of<kX>(a, blockIdx.x, e, first, last)) return;
+  e = __builtin_amdgcn_readfirstlane(e);
+  const uint32_t n0 = blockIdx.y * 8, n_rows = min(8u, a.ffn - n0), k = a.hidden;
+  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
+  const u32x4 gr = rows_rsrc(a.gate.w + e * a.gate.stride + uint64_t(n0) * k, n_rows * k);
+  const u32x4 ur = rows_rsrc(a.up.w + e * a.up.stride + uint64_t(n0) * k, n_rows * k);
+  const u32x4 xr = rows_rsrc(a.xq, uint32_t(a.tokens * uint64_t(row_bytes)));
+  const uint32_t woff = min(R::row_of(), n_rows - 1) * k + R::byte_of();
+  uint32_t xoff[kX / 8];
+#pragma unroll
+  for (int i = 0; i < kX / 8; i++)
+    xoff[i] = slot_at(a, min(first + 8 * i + R::row_of(), last - 1)) / a.k * row_bytes + R::byte_of();
+  i32x4 acc[1];
+  R::product(lds, row_bytes / kStage,
+             [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
+             [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff + at); }, acc);
+  R::gather(lds, acc);
+  for (uint32_t o = threadIdx.x; o < 8 * kX; o += R::kThreads) {
+    const uint32_t n = n0 + o % 8, place = first + o / 8;
+    if (n >= a.ffn || place >= last) continue;
+    const float xs = global<const float>(a.xscale)[slot_at(a, place) / a.k];
+    const uint64_t at = uint64_t(e) * a.ffn + n;
+    const float g = float(R::sum(lds, o % 8, o / 8)) * xs * load_float(a.gate.scale, a.gate.scale_dtype, at);
+    const float u = float(R::sum(lds, 8 + o % 8, o / 8)) * xs * load_float(a.up.scale, a.up.scale_dtype, at);
+    global<float>(a.h)[uint64_t(place) * pitch_of(a.ffn) + n] = g / (1.0f + expf(-g)) * u;
+  }
+}
+
+template <int kX>
+__global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring_kernel(ExpertArgs a) {
+  using R = ExpertRing<kX>;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
+  uint32_t e, first, last;
+  if (!tile_of<kX>(a, blockIdx.x, e, first, last)) return;
+  e = __builtin_amdgcn_readfirstlane(e);
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+  const uint32_t n0 = blockIdx.y * 16, n_rows = min(16u, a.hidden - n0), k = a.ffn;
+  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(k)), m_rows = last - first;
+  const u32x4 wr = rows_rsrc(a.down.w + e * a.down.stride + uint64_t(n0) * k, n_rows * k);
+  const u32x4 xr = rows_rsrc(a.hq + uint64_t(first) * row_bytes, m_rows * row_bytes);
+  uint32_t woff[2], xoff[kX / 8];
+#pragma unroll
+  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * k + R::byte_of();
+#pragma unroll
+  for (int i = 0; i < kX / 8; i++) xoff[i] = min(8 * i + R::row_of(), m_rows - 1) * row_bytes + R::byte_of();
+  i32x4 acc[1];
+  R::product(lds, row_bytes / kStage,
+             [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
+             [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc);
+  R::gather(lds, acc);
+  for (uint32_t o = threadIdx.x; o < 16 * kX; o += R::kThreads) {
+    const uint32_t n = n0 + o % 16, place = first + o / 16;
+    if (n >= a.hidden || place >= last) continue;
+    global<float>(a.out)[uint64_t(slot_at(a, place)) * pitch_of(a.hidden) + n] =
+        float(R::sum(lds, o % 16, o / 16)) * global<const float>(a.hscale)[place] *
         load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
   }
 }
@@ -351,11 +421,14 @@ bool aligned16(const wc_i8_experts* b) {
 }
 
 // Rows of the order to a tile, by the rows an expert has on average.
-int tile_rows(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden) {
+int tile_rows(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden, bool direct) {
   // a tile finds x by 32-bit offsets
-  if (tokens * WC_I8_ROW_BYTES(hidden) >> 32) return 16;
+  if (tokens * WC_I8_ROW_BYTES(hidden) >> 32) return 0;
   const uint32_t average = slots / experts;
-  return average >= 384 ? 256 : average >= 24 ? 128 : 16;
+  if (average >= 384) return 256;
+  if (average >= 24) return 128;
+  // a token takes an expert once
+  return !direct ? 0 : tokens <= 8 ? 8 : 16;
 }
 
 template <class T>
@@ -440,13 +513,19 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   // offset
   const bool direct = hidden % 16 == 0 && ffn % 16 == 0 && aligned16(gate) && aligned16(up) &&
                       aligned16(down);
-  const int rows = tile_rows(tokens, slots, experts, hidden);
+  const int rows = tile_rows(tokens, slots, experts, hidden, direct);
   // every expert that has rows ends in at most one block that is not full
-  a.blocks = slots / uint32_t(rows) + (experts < slots ? experts : slots);
+  a.blocks = slots / uint32_t(rows ? rows : 16) + (experts < slots ? experts : slots);
+  const uint32_t up_cols = rows ? 8 : 16;
+  const dim3 up_grid(a.blocks, (ffn + up_cols - 1) / up_cols), down_grid(a.blocks, (hidden + 15) / 16);
   if (rows == 256) start_up<Tile<256, 256, 2, 4>>(a, direct, st);
   else if (rows == 128) start_up<Tile<128, 128, 2, 2>>(a, direct, st);
+  else if (rows == 16)
+    hipLaunchKernelGGL((wc_experts_up_ring_kernel<16>), up_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
+  else if (rows == 8)
+    hipLaunchKernelGGL((wc_experts_up_ring_kernel<8>), up_grid, dim3(ExpertRing<8>::kThreads), 0, st, a);
   else
-    hipLaunchKernelGGL(wc_experts_up_kernel, dim3(a.blocks, (ffn + 15) / 16), dim3(64 * kRowWaves), 0, st, a);
+    hipLaunchKernelGGL(wc_experts_up_kernel, up_grid, dim3(64 * kRowWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
   if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, pitch_of(ffn),
                        reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st,
@@ -454,8 +533,12 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
     return WC_EHIP;
   if (rows == 256) start_down<Tile<256, 256, 2, 4>>(a, direct, st);
   else if (rows == 128) start_down<Tile<128, 128, 2, 2>>(a, direct, st);
+  else if (rows == 16)
+    hipLaunchKernelGGL((wc_experts_down_ring_kernel<16>), down_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
+  else if (rows == 8)
+    hipLaunchKernelGGL((wc_experts_down_ring_kernel<8>), down_grid, dim3(ExpertRing<8>::kThreads), 0, st, a);
   else
-    hipLaunchKernelGGL(wc_experts_down_kernel, dim3(a.blocks, (hidden + 15) / 16), dim3(64 * kRowWaves), 0, st, a);
+    hipLaunchKernelGGL(wc_experts_down_kernel, down_grid, dim3(64 * kRowWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
   hipLaunchKernelGGL(wc_experts_join_kernel, dim3(tokens, (hidden + 1023) / 1024), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;

@@ -1,5 +1,5 @@
 // wc_i8.hip -- int8 linear layers: wc_quantize_i8, wc_matmul_i8, wc_linear_i8.
-#include "wc_i8_tile.h"
+#include "wc_i8_ring.h"
 
 namespace {
 
@@ -159,6 +159,39 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_matmul_i8_rows_kernel(MatAr
   }
 }
 
+// A few rows of x: 16 kNT rows of W a workgroup.
+template <class R, int kNT, int kX>
+__global__ __launch_bounds__(R::kThreads) void wc_matmul_i8_ring_kernel(MatArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
+  uint32_t j = 0;
+  while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
+  const MatJob J = a.job[j];
+  const uint32_t n0 = (blockIdx.x - J.tile0) * (16 * kNT), n_rows = min(16u * kNT, J.n - n0);
+  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k));
+  const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw, uint32_t((n_rows - 1) * J.ldw + a.k));
+  const u32x4 xr = rows_rsrc(a.q, a.m * row_bytes);
+  uint32_t woff[2 * kNT], xoff[kX / 8];
+#pragma unroll
+  for (int i = 0; i < 2 * kNT; i++)
+    woff[i] = min(8 * i + R::row_of(), n_rows - 1) * uint32_t(J.ldw) + R::byte_of();
+#pragma unroll
+  for (int i = 0; i < kX / 8; i++)
+    xoff[i] = min(8 * i + R::row_of(), a.m - 1) * row_bytes + R::byte_of();
+  i32x4 acc[kNT];
+  R::product(lds, row_bytes / kStage,
+             [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
+             [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc);
+  R::gather(lds, acc);
+  for (uint32_t o = threadIdx.x; o < 16 * kNT * kX; o += R::kThreads) {
+    const uint32_t n = o % (16 * kNT), m = o / (16 * kNT);
+    if (n >= n_rows || m >= a.m) continue;
+    float y = float(R::sum(lds, n, m)) * global<const float>(a.qscale)[m] *
+              load_float(J.scale, J.scale_dtype, n0 + n);
+    if (J.bias) y += load_float(J.bias, J.bias_dtype, n0 + n);
+    store_float(J.y, J.y_dtype, m * J.ldy + n0 + n, y);
+  }
+}
+
 // y of four neighbouring columns from their sums.
 __device__ __forceinline__ void finish(const MatJob& J, uint32_t m, uint32_t n, f32x4 sum, float xs,
                                        const float (&scale)[4], const float (&bias)[4]) {
@@ -310,11 +343,15 @@ bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx) {
          (m == 0 || (x && reinterpret_cast<uintptr_t>(x) % size_of(dt) == 0));
 }
 
+// m = 13, k = 8192, n = 28672: 16 rows of W, 4 waves, 4 stages 43.9 us (5.4 TB/s); 2 waves
+// of 8 stages 52.0, 8 waves of 4 48.9, 4 of 6 50.1; 32 rows, 4 waves, 3 stages 56.4; 64
+// rows 49.4.  At m = 1 40.9 us, 5.75 TB/s, what a plain streaming kernel reaches.
+constexpr int kRingRows = 16, kRingWaves = 4, kRingStages = 4;
 using Tile256 = Tile<256, 256, 2, 4>;
 using Tile128 = Tile<128, 128, 2, 2>;
 
 // Which kernel multiplies m rows, and in how many parts of k.
-enum class Kernel { kRows, kTile128, kTile256 };
+enum class Kernel { kRows, kRing, kTile128, kTile256 };
 struct Plan {
   Kernel kernel;
   bool direct;      // every W can go to LDS as it is
@@ -323,7 +360,6 @@ struct Plan {
 };
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   Plan p{Kernel::kRows, true, 1, 0};
-  if (m <= 64) return p;
   uint64_t tiles128 = 0, tiles256 = 0, sums = 0;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
@@ -334,6 +370,11 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
     tiles256 += uint64_t(m + 255) / 256 * ((J.n + 255) / 256);
     sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
   }
+  if (m <= 16) {
+    if (p.direct) p.kernel = Kernel::kRing;
+    return p;
+  }
+  if (m <= 64) return p;
   if (tiles128 > 0x7FFFFFFFu) return p;
   p.kernel = tiles256 >= 192 ? Kernel::kTile256 : Kernel::kTile128;
   const uint64_t tiles = p.kernel == Kernel::kTile256 ? tiles256 : tiles128;
@@ -342,6 +383,12 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   while (tiles * p.splits * 2 <= slots && stages >= p.splits * 2 * 8) p.splits *= 2;
   if (p.splits > 1) p.part_bytes = sums * p.splits;
   return p;
+}
+
+template <int kNT, int kX, int kW, int kS>
+void start_ring(uint32_t tiles, const MatArgs& a, hipStream_t stream) {
+  using R = Ring<kNT, kX, kW, kS>;
+  hipLaunchKernelGGL((wc_matmul_i8_ring_kernel<R, kNT, kX>), dim3(tiles), dim3(R::kThreads), 0, stream, a);
 }
 
 wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, uint32_t n_jobs,
@@ -364,8 +411,15 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
     tiles += p.kernel == Kernel::kRows      ? (J.n + 15) / 16
+             : p.kernel == Kernel::kRing    ? (J.n + kRingRows - 1) / kRingRows
              : p.kernel == Kernel::kTile128 ? (m + 127) / 128 * ((J.n + 127) / 128)
                                             : (m + 255) / 256 * ((J.n + 255) / 256);
+  }
+  if (p.kernel == Kernel::kRing) {
+    a.m = m;
+    if (m <= 8) start_ring<kRingRows / 16, 8, kRingWaves, kRingStages>(tiles, a, stream);
+    else start_ring<kRingRows / 16, 16, kRingWaves, kRingStages>(tiles, a, stream);
+    return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
   }
   if (p.kernel != Kernel::kRows) {
     a.m = m;

@@ -2,8 +2,8 @@
 // through LDS: C[n][m] = sum_k W[n][k] x[m][k] on v_mfma_i32_32x32x32_i8.
 //
 // A stage is 128 bytes of k of every row of the tile.  Both operands go from
-// memory to LDS without passing through registers (buffer_load ... lds), one stage
-// ahead of the products.  A row's eight 16-byte chunks are stored in the order
+// memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1
+// stages ahead of the products.  A row's eight 16-byte chunks are stored in the order
 // chunk ^ (row mod 8): the eight lanes that read LDS together, the same chunk of
 // eight rows next to each other, then touch all banks once.
 #pragma once
@@ -30,14 +30,14 @@ __device__ __forceinline__ void load_lds(u32x4 rs, uint32_t lds, uint32_t offset
                : "memory");
 }
 
-// kBM rows of x by kBN rows of W, kWM x kWN waves.
-template <int kBM, int kBN, int kWM, int kWN>
+// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages in LDS.
+template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2>
 struct Tile {
   static constexpr int kWM_ = kWM, kWN_ = kWN, kWaves = kWM * kWN, kThreads = 64 * kWaves;
   static constexpr int kMT = kBM / kWM / 32, kNT = kBN / kWN / 32;  // 32 x 32 blocks to a wave
   static constexpr int kXLoads = kBM / 8 / kWaves, kWLoads = kBN / 8 / kWaves;
   static constexpr int kBuffer = (kBM + kBN) * kStage;
-  static constexpr int kLds = 2 * kBuffer;
+  static constexpr int kLds = kDepth * kBuffer, kRows = kBM, kCols = kBN;
   static_assert(kBM % (8 * kWaves) == 0 && kBN % (8 * kWaves) == 0);
 
   // Row of the tile and byte of its stage that load i of this lane brings: each
@@ -47,6 +47,16 @@ struct Tile {
   }
   static __device__ __forceinline__ uint32_t byte_of() {
     return ((threadIdx.x % 8) ^ (threadIdx.x % 64 / 8)) * 16;
+  }
+
+  // Waits for all but the loads of the newest `later` stages (kN at most), then for the
+  // other waves.
+  template <int kN>
+  static __device__ __forceinline__ void arrive(uint32_t later) {
+    if constexpr (kN > 0) {
+      if (later < kN) return arrive<kN - 1>(later);
+    }
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kN * (kXLoads + kWLoads)) : "memory");
   }
 
   // `load_x(i, stage, lds)` and `load_w(i, stage, lds)` start load i of a stage's rows
@@ -67,8 +77,8 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[m][n][i] = 0;
     i32x4 held[kDirect ? 1 : kWLoads];
-    const auto start = [&](uint32_t s) {
-      const uint32_t to = __builtin_amdgcn_readfirstlane(base + (s & 1) * kBuffer + wave * 1024);
+    const auto start = [&](uint32_t s, uint32_t slot) {
+      const uint32_t to = __builtin_amdgcn_readfirstlane(base + slot * kBuffer + wave * 1024);
 #pragma unroll
       for (int i = 0; i < kXLoads; i++) load_x(i, s, to + uint32_t(i) * kThreads * 16);
 #pragma unroll
@@ -78,28 +88,35 @@ struct Tile {
         else held[i] = load_w(i, s, there);
       }
     };
-    const auto keep = [&](uint32_t s) {
+    const auto keep = [&](uint32_t slot) {
       if constexpr (!kDirect) {
-        uint8_t* to = lds + (s & 1) * kBuffer + kBM * kStage + threadIdx.x * 16;
+        uint8_t* to = lds + slot * kBuffer + kBM * kStage + threadIdx.x * 16;
 #pragma unroll
         for (int i = 0; i < kWLoads; i++)
           *reinterpret_cast<i32x4*>(to + i * kThreads * 16) = held[i];
       }
     };
+    // stages ahead: one where W comes through registers
+    constexpr uint32_t kAhead = kDirect ? kDepth - 1 : 1;
     uint32_t at[4];
 #pragma unroll
     for (int k = 0; k < 4; k++)
       at[k] = lane % 32 * kStage + ((2 * k + lane / 32) ^ (lane & 7)) * 16;
     const uint32_t xrow = wm * (kBM / kWM) * kStage, wrow = (kBM + wn * (kBN / kWN)) * kStage;
-    start(0);
-    keep(0);
+#pragma unroll
+    for (uint32_t s = 0; s < kAhead; s++)
+      if (s < stages) {
+        start(s, s);
+        keep(s);
+      }
+    uint32_t slot = 0, next = kAhead;
     for (uint32_t s = 0; s < stages; s++) {
-      // this wave's loads of stage s are in LDS and its reads of stage s - 1 done, and so
-      // with the other waves behind the barrier
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      const bool more = s + 1 < stages;
-      if (more) start(s + 1);
-      const uint8_t* b = lds + (s & 1) * kBuffer;
+      // this wave's loads of stage s are in LDS and its reads of the stage that the next
+      // loads replace are done, and so with the other waves behind the barrier
+      arrive<kDirect ? int(kAhead) - 1 : 0>(stages - 1 - s);
+      const bool more = s + kAhead < stages;
+      if (more) start(s + kAhead, next);
+      const uint8_t* b = lds + slot * kBuffer;
 #pragma unroll
       for (int k = 0; k < 4; k++) {
         i32x4 x[kMT], w[kNT];
@@ -115,7 +132,9 @@ struct Tile {
           for (int n = 0; n < kNT; n++)
             acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[n], x[m], acc[m][n], 0, 0, 0);
       }
-      if (more) keep(s + 1);
+      if (more) keep(next);
+      slot = slot + 1 < kDepth ? slot + 1 : 0;
+      next = next + 1 < kDepth ? next + 1 : 0;
     }
     // the waves leave together: LDS is free for the results
     __syncthreads();
