@@ -88,10 +88,21 @@ __device__ __forceinline__ uint32_t code_of(float x, float inverse) {
   return r == r ? uint32_t(int32_t(fminf(fmaxf(r, -127.0f), 127.0f))) & 0xFFu : 0u;
 }
 
+// The value of the lane a data-parallel move takes it from, 0 where there is none: within
+// sixteen lanes from kCtrl - 0x110 lanes below, or (0x142, 0x143) the last lane of the
+// sixteen or thirty-two below.
+template <int kCtrl, int kRows = 0xF>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), kCtrl, kRows, 0xF, false));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v = max(v, uint32_t(__shfl_xor(int(v), d)));
-  return v;
+  v = max(v, moved<0x111>(v));
+  v = max(v, moved<0x112>(v));
+  v = max(v, moved<0x114>(v));
+  v = max(v, moved<0x118>(v));
+  v = max(v, moved<0x142, 0xA>(v));
+  v = max(v, moved<0x143, 0xC>(v));
+  return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
 }
 
 // Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes

@@ -96,6 +96,7 @@ struct MatJob {
 };
 struct MatArgs {
   uint64_t q, qscale;
+  uint64_t x, ldx;  // not quantised yet, where the kernel does that itself
   uint32_t m, k, n_jobs, splits;
   MatJob job[kMaxJobs];
 };
@@ -159,34 +160,51 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_matmul_i8_rows_kernel(MatAr
   }
 }
 
-// A few rows of x: 16 kNT rows of W a workgroup.
-template <class R, int kNT, int kX>
-__global__ __launch_bounds__(R::kThreads) void wc_matmul_i8_ring_kernel(MatArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
+// A few rows of x: 16 rows of W a workgroup.
+// m = 13, k = 8192, n = 28672: 16 rows of W, 4 waves, 4 stages 43.9 us (5.4 TB/s); 2 waves
+// of 8 stages 52.0, 8 waves of 4 48.9, 4 of 6 50.1; 32 rows, 4 waves, 3 stages 56.4; 64
+// rows 49.4.  At m = 1 40.9 us, 5.75 TB/s, what a plain streaming kernel reaches.
+//   kX = 0: x comes as it is, and every
+// workgroup quantises it for itself while its first rows of W are on their way.
+template <int kX>
+using MatRing = Ring<1, kX, 4, 4>;
+
+template <int kX, int kType>
+__global__ __launch_bounds__(MatRing<kX>::kThreads) void wc_matmul_i8_ring_kernel(MatArgs a) {
+  using R = MatRing<kX>;
+  constexpr uint32_t kRows = kX ? kX : 16;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  __shared__ float scales[16];
+  __shared__ uint32_t tops[16];
   uint32_t j = 0;
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
   const MatJob J = a.job[j];
-  const uint32_t n0 = (blockIdx.x - J.tile0) * (16 * kNT), n_rows = min(16u * kNT, J.n - n0);
+  const uint32_t n0 = (blockIdx.x - J.tile0) * 16, n_rows = min(16u, J.n - n0);
   const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k));
   const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw, uint32_t((n_rows - 1) * J.ldw + a.k));
-  const u32x4 xr = rows_rsrc(a.q, a.m * row_bytes);
-  uint32_t woff[2 * kNT], xoff[kX / 8];
+  const u32x4 xr = rows_rsrc(a.q, kX ? a.m * row_bytes : 0u);
+  uint32_t woff[2], xoff[2];
 #pragma unroll
-  for (int i = 0; i < 2 * kNT; i++)
+  for (int i = 0; i < 2; i++) {
     woff[i] = min(8 * i + R::row_of(), n_rows - 1) * uint32_t(J.ldw) + R::byte_of();
-#pragma unroll
-  for (int i = 0; i < kX / 8; i++)
     xoff[i] = min(8 * i + R::row_of(), a.m - 1) * row_bytes + R::byte_of();
-  i32x4 acc[kNT];
+  }
+  i32x4 acc[1];
   R::product(lds, row_bytes / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
-             [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc);
+             [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc, [&] {
+               if constexpr (kX == 0)
+                 hold_rows<R::kThreads, kType, 2>(
+                     a.m, a.k, [&](uint32_t r) { return a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2); },
+                     lds + R::kLds, scales, tops);
+               return typename R::Held{lds + R::kLds, row_bytes, a.m};
+             });
   R::gather(lds, acc);
-  for (uint32_t o = threadIdx.x; o < 16 * kNT * kX; o += R::kThreads) {
-    const uint32_t n = o % (16 * kNT), m = o / (16 * kNT);
+  for (uint32_t o = threadIdx.x; o < 16 * kRows; o += R::kThreads) {
+    const uint32_t n = o % 16, m = o / 16;
     if (n >= n_rows || m >= a.m) continue;
-    float y = float(R::sum(lds, n, m)) * global<const float>(a.qscale)[m] *
-              load_float(J.scale, J.scale_dtype, n0 + n);
+    const float xs = kX ? global<const float>(a.qscale)[m] : scales[m];
+    float y = float(R::sum(lds, n, m)) * xs * load_float(J.scale, J.scale_dtype, n0 + n);
     if (J.bias) y += load_float(J.bias, J.bias_dtype, n0 + n);
     store_float(J.y, J.y_dtype, m * J.ldy + n0 + n, y);
   }
@@ -343,26 +361,31 @@ bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx) {
          (m == 0 || (x && reinterpret_cast<uintptr_t>(x) % size_of(dt) == 0));
 }
 
-// m = 13, k = 8192, n = 28672: 16 rows of W, 4 waves, 4 stages 43.9 us (5.4 TB/s); 2 waves
-// of 8 stages 52.0, 8 waves of 4 48.9, 4 of 6 50.1; 32 rows, 4 waves, 3 stages 56.4; 64
-// rows 49.4.  At m = 1 40.9 us, 5.75 TB/s, what a plain streaming kernel reaches.
-constexpr int kRingRows = 16, kRingWaves = 4, kRingStages = 4;
 using Tile256 = Tile<256, 256, 2, 4>;
 using Tile128 = Tile<128, 128, 2, 2>;
+
+// Quantising in the product's own launch saves a launch (2 us, 4 on the host) and costs
+// every workgroup the row: linear at m = 1, k = 4096, n = 6144 9.7 us against 11.2,
+// n = 14336 15.4 and 17.0, but k = 8192, n = 28672 45.3 and 43.7; m = 2, k = 4096, n =
+// 6144 12.0 and 11.1 (less than the host's time for the launch), k = 8192, n = 8192 20.0
+// and 17.4.
+constexpr uint64_t kHoldAlways = 4096, kHoldSmall = 8192, kHoldSmallWeights = 32u << 20;
 
 // Which kernel multiplies m rows, and in how many parts of k.
 enum class Kernel { kRows, kRing, kTile128, kTile256 };
 struct Plan {
   Kernel kernel;
   bool direct;      // every W can go to LDS as it is
+  bool hold;        // the kernel can quantise x itself
   uint32_t splits;
   uint64_t part_bytes;
 };
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
-  Plan p{Kernel::kRows, true, 1, 0};
-  uint64_t tiles128 = 0, tiles256 = 0, sums = 0;
+  Plan p{Kernel::kRows, true, false, 1, 0};
+  uint64_t tiles128 = 0, tiles256 = 0, sums = 0, weights = 0;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
+    weights += uint64_t(J.n) * k;
     // offsets within a tile's rows are 32-bit
     if (J.ldw > (1u << 22)) return p;
     p.direct = p.direct && k % 4 == 0 && J.ldw % 16 == 0 && reinterpret_cast<uintptr_t>(J.w) % 16 == 0;
@@ -372,6 +395,9 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   }
   if (m <= 16) {
     if (p.direct) p.kernel = Kernel::kRing;
+    const uint64_t held = m * WC_I8_ROW_BYTES(k);
+    p.hold = p.direct && k % 8 == 0 &&
+             (held <= kHoldAlways || (held <= kHoldSmall && weights <= kHoldSmallWeights));
     return p;
   }
   if (m <= 64) return p;
@@ -385,15 +411,19 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   return p;
 }
 
-template <int kNT, int kX, int kW, int kS>
+template <int kX, int kType = 0>
 void start_ring(uint32_t tiles, const MatArgs& a, hipStream_t stream) {
-  using R = Ring<kNT, kX, kW, kS>;
-  hipLaunchKernelGGL((wc_matmul_i8_ring_kernel<R, kNT, kX>), dim3(tiles), dim3(R::kThreads), 0, stream, a);
+  const uint32_t held = kX ? 0 : a.m * uint32_t(WC_I8_ROW_BYTES(a.k));
+  hipLaunchKernelGGL((wc_matmul_i8_ring_kernel<kX, kType>), dim3(tiles), dim3(MatRing<kX>::kThreads),
+                     MatRing<kX>::kLds + held, stream, a);
 }
 
 wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, uint32_t n_jobs,
-                 const wc_i8_job* jobs, const Plan& p, void* parts, hipStream_t stream) {
+                 const wc_i8_job* jobs, const Plan& p, void* parts, hipStream_t stream,
+                 const void* x = nullptr, int32_t x_dtype = 0, uint64_t ldx = 0) {
   MatArgs a{};
+  a.x = reinterpret_cast<uint64_t>(x);
+  a.ldx = ldx;
   a.q = reinterpret_cast<uint64_t>(q);
   a.qscale = reinterpret_cast<uint64_t>(scale);
   a.k = k;
@@ -411,14 +441,17 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
     tiles += p.kernel == Kernel::kRows      ? (J.n + 15) / 16
-             : p.kernel == Kernel::kRing    ? (J.n + kRingRows - 1) / kRingRows
+             : p.kernel == Kernel::kRing    ? (J.n + 15) / 16
              : p.kernel == Kernel::kTile128 ? (m + 127) / 128 * ((J.n + 127) / 128)
                                             : (m + 255) / 256 * ((J.n + 255) / 256);
   }
   if (p.kernel == Kernel::kRing) {
     a.m = m;
-    if (m <= 8) start_ring<kRingRows / 16, 8, kRingWaves, kRingStages>(tiles, a, stream);
-    else start_ring<kRingRows / 16, 16, kRingWaves, kRingStages>(tiles, a, stream);
+    if (p.hold && x_dtype == WC_BF16) start_ring<0, WC_BF16>(tiles, a, stream);
+    else if (p.hold && x_dtype == WC_FP16) start_ring<0, WC_FP16>(tiles, a, stream);
+    else if (p.hold) start_ring<0, WC_FP32>(tiles, a, stream);
+    else if (m <= 8) start_ring<8>(tiles, a, stream);
+    else start_ring<16>(tiles, a, stream);
     return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
   }
   if (p.kernel != Kernel::kRows) {
@@ -522,7 +555,8 @@ extern "C" wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, u
   if (!dev_q || !dev_scale || reinterpret_cast<uintptr_t>(dev_q) % 16 ||
       reinterpret_cast<uintptr_t>(dev_scale) % 4)
     return WC_EINVAL;
-  const Plan p = plan_of(m, k, n_jobs, jobs);
+  Plan p = plan_of(m, k, n_jobs, jobs);
+  p.hold = false;
   if (!workspace_ok(dev_workspace, workspace_bytes, p.part_bytes)) return WC_EINVAL;
   return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, p, dev_workspace,
                 reinterpret_cast<hipStream_t>(stream));
@@ -551,6 +585,8 @@ extern "C" wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m
   int8_t* q = static_cast<int8_t*>(dev_workspace);
   float* scale = reinterpret_cast<float*>(q + pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)));
   void* parts = reinterpret_cast<uint8_t*>(scale) + pad256(uint64_t(m) * 4);
-  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, scale, st)) return WC_EHIP;
-  return matmul(q, scale, m, k, n_jobs, jobs, plan_of(m, k, n_jobs, jobs), parts, st);
+  Plan p = plan_of(m, k, n_jobs, jobs);
+  p.hold = p.hold && reinterpret_cast<uintptr_t>(dev_x) % 16 == 0 && ldx * size_of(x_dtype) % 16 == 0;
+  if (!p.hold && !launch_quantize(dev_x, x_dtype, m, k, ldx, q, scale, st)) return WC_EHIP;
+  return matmul(q, scale, m, k, n_jobs, jobs, p, parts, st, dev_x, x_dtype, ldx);
 }

@@ -14,6 +14,7 @@
 namespace wc_i8 {
 
 // kNT blocks of 16 rows of W, kX (8 or 16) rows of x, kW waves, kS stages to a ring.
+// kX = 0: x is held in LDS, quantised there by the workgroup itself (hold_rows).
 template <int kNT, int kX, int kW, int kS>
 struct Ring {
   static constexpr int kThreads = 64 * kW;
@@ -40,9 +41,15 @@ struct Ring {
   // acc = the products of this wave's blocks wave, wave + kW, ... of `blocks`;
   // `load_w(i, offset, lds)` starts W's rows 8 i .. 8 i + 7, `load_x(i, offset, lds)`
   // x's, at byte `offset` of their rows.
-  template <class LoadX, class LoadW>
+  // Once the first loads are on their way `ready()` is called; it gives the rows of x
+  // held in LDS (kX = 0), `pitch` apart and `rows` of them.
+  struct Held {
+    const uint8_t* x;
+    uint32_t pitch, rows;
+  };
+  template <class LoadX, class LoadW, class Ready>
   static __device__ __forceinline__ void product(uint8_t* lds, uint32_t blocks, LoadX load_x,
-                                                 LoadW load_w, i32x4 (&acc)[kNT]) {
+                                                 LoadW load_w, i32x4 (&acc)[kNT], Ready ready) {
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     uint8_t* mine = lds + wave * kWave;
@@ -58,14 +65,21 @@ struct Ring {
 #pragma unroll
       for (int i = 0; i < kX / 8; i++) load_x(i, at, to + (2 * kNT + i) * 1024);
     };
-    // chunk lane / 16 (and four on) of row lane mod 16; of eight rows of x, mod 8
-    const uint32_t r = lane % 16, c0 = (lane / 16) ^ (r % 8), c1 = (lane / 16 + 4) ^ (r % 8);
-    const uint32_t w0 = r * kStage + c0 * 16, w1 = r * kStage + c1 * 16;
-    const uint32_t xr = 16 * kNT * kStage + r % kX * kStage;
-    const uint32_t x0 = xr + c0 * 16, x1 = xr + c1 * 16;
 #pragma unroll
     for (uint32_t j = 0; j < kS - 1; j++)
       if (j < count) start(j, j);
+    const Held held = ready();
+    // chunk lane / 16 (and four on) of row lane mod 16; of kX rows of x, mod kX
+    const uint32_t r = lane % 16, c0 = (lane / 16) ^ (r % 8), c1 = (lane / 16 + 4) ^ (r % 8);
+    const uint32_t w0 = r * kStage + c0 * 16, w1 = r * kStage + c1 * 16;
+    uint32_t x0, x1;
+    if constexpr (kX > 0) {
+      const uint32_t xr = 16 * kNT * kStage + r % kX * kStage;
+      x0 = xr + c0 * 16, x1 = xr + c1 * 16;
+    } else {
+      const uint32_t row = min(r, held.rows - 1), at = row * held.pitch + wave * kStage;
+      x0 = at + ((lane / 16) ^ (row % 8)) * 16, x1 = at + ((lane / 16 + 4) ^ (row % 8)) * 16;
+    }
     uint32_t slot = 0;
     for (uint32_t j = 0; j < count; j++) {
       // the ring's oldest stage was read before this one's products were started
@@ -73,8 +87,9 @@ struct Ring {
       const uint32_t left = count - 1 - j;
       wait_for<kS - 1>(left < kS - 1 ? left : kS - 1);
       const uint8_t* s = mine + slot * kStageBytes;
-      const i32x4 a0 = *reinterpret_cast<const i32x4*>(s + x0);
-      const i32x4 a1 = *reinterpret_cast<const i32x4*>(s + x1);
+      const uint8_t* x = kX > 0 ? s : held.x + j * (kW * kStage);
+      const i32x4 a0 = *reinterpret_cast<const i32x4*>(x + x0);
+      const i32x4 a1 = *reinterpret_cast<const i32x4*>(x + x1);
 #pragma unroll
       for (int n = 0; n < kNT; n++) {
         const i32x4 b0 = *reinterpret_cast<const i32x4*>(s + w0 + n * 16 * kStage);
@@ -108,5 +123,76 @@ struct Ring {
     return v;
   }
 };
+
+// Quantise `rows` rows of x into LDS, chunk c of each 128-byte block of row r at chunk
+// c ^ (r mod 8); `row_at(r)` is a row's address, 16-byte aligned, k elements (a multiple
+// of 8) of type kType.  A thread's first kKeep units of eight elements are on their way
+// at once and stay in registers; any more are read again, from the caches.  scales, tops:
+// LDS, one a row.
+template <int kThreads, int kType, int kKeep, class RowAt>
+__device__ __forceinline__ void hold_rows(uint32_t rows, uint32_t k, RowAt row_at, uint8_t* to,
+                                          float* scales, uint32_t* tops) {
+  constexpr int kWords = kType == WC_FP32 ? 8 : 4;
+  const uint32_t pitch = uint32_t(WC_I8_ROW_BYTES(k)), units = pitch / 8, all = rows * units;
+  if (threadIdx.x < rows) tops[threadIdx.x] = 0;
+  const auto load = [&](uint32_t unit, uint32_t (&v)[kWords]) {
+    const uint32_t u = min(unit, all - 1), row = rows == 1 ? 0 : u / units;
+    const uint32_t at = (u - row * units) * 8;
+    const auto p = global<const u32x4>(row_at(row) + min(at, k - 8) * uint64_t(kType == WC_FP32 ? 4 : 2));
+#pragma unroll
+    for (int i = 0; i < kWords / 4; i++) {
+      const u32x4 a = p[i];
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[4 * i + j] = at < k ? a[j] : 0u;
+    }
+  };
+  const auto value = [&](const uint32_t (&v)[kWords], int i) {
+    if constexpr (kType == WC_FP32) return __uint_as_float(v[i]);
+    const uint32_t h = i % 2 ? v[i / 2] >> 16 : v[i / 2] & 0xFFFFu;
+    return kType == WC_BF16 ? bf16_to_float(h) : fp16_to_float(h);
+  };
+  const auto measure = [&](uint32_t unit, const uint32_t (&v)[kWords]) {
+    const uint32_t row = rows == 1 ? 0 : min(unit, all - 1) / units;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(value(v, i)) & 0x7FFFFFFFu);
+    // a wave's units are of one row, or of two where it passes a row's end
+    const uint32_t lowest = __builtin_amdgcn_readfirstlane(row);
+    const uint32_t here = wave_max(row == lowest ? top : 0u);
+    if (threadIdx.x % 64 == 0) atomicMax(&tops[lowest], here);
+    if (row != lowest) atomicMax(&tops[row], top);
+  };
+  const auto store = [&](uint32_t unit, const uint32_t (&v)[kWords]) {
+    if (unit >= all) return;
+    const uint32_t row = rows == 1 ? 0 : unit / units, at = (unit - row * units) * 8;
+    const float inverse = row_scale(tops[row]).inverse;
+    u32x2 c = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; i++) c[i / 4] |= code_of(value(v, i), inverse) << (8 * (i % 4));
+    *reinterpret_cast<u32x2*>(to + row * pitch + at / 128 * 128 + ((at / 16 % 8) ^ (row % 8)) * 16 +
+                              at % 16) = c;
+  };
+  uint32_t v[kKeep][kWords];
+#pragma unroll
+  for (int u = 0; u < kKeep; u++) load(threadIdx.x + u * kThreads, v[u]);
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kKeep; u++) measure(threadIdx.x + u * kThreads, v[u]);
+  for (uint32_t unit = threadIdx.x + kKeep * kThreads; unit - threadIdx.x < all; unit += kThreads) {
+    uint32_t w[kWords];
+    load(unit, w);
+    measure(unit, w);
+  }
+  __syncthreads();
+  if (threadIdx.x < rows) scales[threadIdx.x] = row_scale(tops[threadIdx.x]).scale;
+#pragma unroll
+  for (int u = 0; u < kKeep; u++) store(threadIdx.x + u * kThreads, v[u]);
+  for (uint32_t unit = threadIdx.x + kKeep * kThreads; unit < all; unit += kThreads) {
+    uint32_t w[kWords];
+    load(unit, w);
+    store(unit, w);
+  }
+  __syncthreads();
+}
 
 }  // namespace wc_i8

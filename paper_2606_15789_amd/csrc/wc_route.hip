@@ -7,10 +7,17 @@ namespace {
 
 using namespace wc_i8;
 
-constexpr int kTokenWaves = 4;         // tokens to a workgroup of the choice
+constexpr int kTokenWaves = 4;         // waves to a workgroup of the choice
 constexpr uint32_t kSortThreads = 1024;
 constexpr uint32_t kSortSlots = 2048;  // slots to a workgroup of the sort
 constexpr uint32_t kMaxChosen = 32;
+// Blocks of the sort up to which each counts all slots itself, in place of a launch that
+// counts: 512 tokens of 8 slots (2 blocks) 13.9 us against 15.0, 1500 (6) 17.7 and 16.5,
+// but the host has a launch less.
+constexpr uint32_t kSelfCount = 4;
+// Tokens from which four share a wave where they fit: 32768 of 61 experts 20.3 us against
+// 24.0, 4096 11.7 and 11.1.
+constexpr uint32_t kManyTokens = 16384;
 
 struct RouteArgs {
   uint64_t logits, bias, ids, weights, ld;
@@ -19,35 +26,75 @@ struct RouteArgs {
   float scale;
 };
 
-struct Best {
-  float key;
-  uint32_t at;
-};
-// The larger key, the lower index among equals.
-__device__ __forceinline__ Best better(Best a, Best b) {
-  return b.key > a.key || (b.key == a.key && b.at < a.at) ? b : a;
+// Reductions over kLanes neighbouring lanes (16, 32 or 64), every lane gets the result:
+// rotations within the sixteen lanes of a row, then the rows by readlane.
+template <int kLanes, class Op>
+__device__ __forceinline__ uint32_t reduced(uint32_t v, Op op) {
+  v = op(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x128, 0xF, 0xF, false)));
+  v = op(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x124, 0xF, 0xF, false)));
+  v = op(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x122, 0xF, 0xF, false)));
+  v = op(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x121, 0xF, 0xF, false)));
+  if constexpr (kLanes == 16) return v;
+  const auto row = [&](int lane) { return uint32_t(__builtin_amdgcn_readlane(int(v), lane)); };
+  const uint32_t low = op(row(0), row(16)), high = op(row(32), row(48));
+  if constexpr (kLanes == 32) return threadIdx.x % 64 < 32 ? low : high;
+  return op(low, high);
 }
-__device__ __forceinline__ Best wave_best(Best b) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2)
-    b = better(b, {__shfl_xor(b.key, d), uint32_t(__shfl_xor(int(b.at), d))});
-  return b;
+template <int kLanes>
+__device__ __forceinline__ uint32_t top_of(uint32_t v) {
+  return reduced<kLanes>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
-__device__ __forceinline__ float wave_sum(float v) {
+template <int kLanes>
+__device__ __forceinline__ float sum_of(float v) {
+  return __uint_as_float(reduced<kLanes>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+// The lanes of this lane's group for which `on` holds, from bit 0 on.
+template <int kLanes>
+__device__ __forceinline__ uint64_t votes(bool on) {
+  const uint64_t all = __ballot(on);
+  if constexpr (kLanes == 64) return all;
+  return all >> (threadIdx.x % 64 / kLanes * kLanes) & ((1ull << kLanes) - 1);
+}
+// Numbers in order as unsigned ones; -0 as 0, NaN as -inf.
+__device__ __forceinline__ uint32_t ordered(float f) {
+  const uint32_t b = __float_as_uint(f == f ? f + 0.0f : -__builtin_inff());
+  return b >> 31 ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t kNone = 0x007FFFFFu;  // ordered(-inf)
+
+// The greatest of all the lanes' key[i] (the expert or group lane + kLanes i), the lowest
+// index among equals; its place, or -1 if nothing is above -inf (`floor`).  That key is
+// taken out.
+template <int kLanes, int kPer>
+__device__ __forceinline__ int32_t take_best(uint32_t (&key)[kPer], uint32_t floor) {
+  uint32_t best = key[0];
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
+  for (int i = 1; i < kPer; i++) best = max(best, key[i]);
+  best = top_of<kLanes>(best);
+  int32_t at = -1;
+#pragma unroll
+  for (int i = 0; i < kPer; i++) {
+    const uint64_t v = votes<kLanes>(key[i] == best);
+    if (at < 0 && v) at = i * kLanes + __builtin_ctzll(v);
+  }
+  if (best <= floor) at = -1;
+  const int32_t lane = int32_t(threadIdx.x % kLanes);
+#pragma unroll
+  for (int i = 0; i < kPer; i++)
+    if (at == i * kLanes + lane) key[i] = 0;
+  return at;
 }
 
-// One wave a token, experts lane + 64 i in its registers.  A softmax without a
-// bias chooses by the logits, which are in the scores' order, so no two of them
-// fall together by rounding.
-template <int kPer>
-__global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(RouteArgs a) {
-  __shared__ float keys[kTokenWaves][64 * kPer];
-  __shared__ uint8_t kept[kTokenWaves][64 * kPer];
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const uint32_t token = blockIdx.x * kTokenWaves + wave;
+// The choice of one token by kLanes lanes: expert lane + kLanes i in register i.  A softmax
+// without a bias chooses by the logits, which are in the scores' order, so no two of them
+// fall together by rounding.  Lane j < k gets slot j's expert and weight.  Bound by the
+// chain of k reductions; all lanes of a wave work on as many tokens as fit it.
+template <int kLanes, int kPer>
+__device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float* scratch,
+                                       int32_t& id, float& weight) {
+  const uint32_t lane = threadIdx.x % kLanes;
   const bool live = token < a.tokens;
   const float ninf = -__builtin_inff();
   float s[kPer], key[kPer];
@@ -55,7 +102,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(Route
   float top = ninf;
 #pragma unroll
   for (int i = 0; i < kPer; i++) {
-    const uint32_t e = lane + 64 * i;
+    const uint32_t e = lane + kLanes * i;
     float x = ninf, b = 0.0f;
     if (live && e < a.experts) {
       x = load_float(a.logits, a.dtype, token * a.ld + e);
@@ -69,8 +116,8 @@ __global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(Route
   }
   const bool soft = a.score == WC_SCORE_SOFTMAX;
   if (soft) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const uint32_t best = top_of<kLanes>(ordered(top));
+    top = __uint_as_float(best >> 31 ? best & 0x7FFFFFFFu : ~best);
   }
   const bool by_logits = soft && !a.bias && (a.groups == 1 || a.group_top == 1);
   float total = 0.0f;
@@ -85,88 +132,87 @@ __global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(Route
     else if (off) key[i] = ninf;
   }
   if (soft) {
-    total = wave_sum(total);
+    total = sum_of<kLanes>(total);
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
       s[i] = total != 0.0f ? s[i] / total : 0.0f;
       if (!by_logits && key[i] != ninf) key[i] += s[i];
     }
   }
+  uint32_t rank[kPer];
 #pragma unroll
-  for (int i = 0; i < kPer; i++)
-    if (key[i] != key[i]) key[i] = ninf;
+  for (int i = 0; i < kPer; i++) rank[i] = ordered(key[i]);
   if (a.groups > 1) {
+    // the keys, then a flag for each group, in LDS of this token's own
     const uint32_t per = a.experts / a.groups;
 #pragma unroll
-    for (int i = 0; i < kPer; i++) {
-      keys[wave][lane + 64 * i] = key[i];
-      kept[wave][lane + 64 * i] = 0;
-    }
-    __syncthreads();
-    float best[kPer];
+    for (int i = 0; i < kPer; i++) scratch[lane + kLanes * i] = key[i] == key[i] ? key[i] : ninf;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    uint32_t best[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
-      const uint32_t g = lane + 64 * i;
+      const uint32_t g = lane + kLanes * i;
       float first = ninf, second = ninf;
       if (g < a.groups)
+#pragma unroll 4
         for (uint32_t j = 0; j < per; j++) {
-          const float v = keys[wave][g * per + j];
+          const float v = scratch[g * per + j];
           second = fmaxf(second, fminf(first, v));
           first = fmaxf(first, v);
         }
-      best[i] = a.group_top == 2 ? first + second : first;
+      best[i] = g < a.groups ? ordered(a.group_top == 2 ? first + second : first) : 0;
     }
-    uint32_t taken = 0;  // bit i: group lane + 64 i
-    for (uint32_t n = 0; n < a.top_groups; n++) {
-      Best b = {ninf, 0xFFFFFFFFu};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int i = 0; i < kPer; i++)
-        if (lane + 64 * i < a.groups && !(taken >> i & 1)) b = better(b, {best[i], lane + 64 * i});
-      b = wave_best(b);
-      if (b.at % 64 == lane && b.at < a.groups) {
-        taken |= 1u << (b.at / 64);
-        kept[wave][b.at] = 1;
-      }
+    for (int i = 0; i < kPer; i++) scratch[lane + kLanes * i] = 0.0f;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (uint32_t n = 0; n < a.top_groups; n++) {
+      const int32_t g = take_best<kLanes, kPer>(best, 0);
+      if (g >= 0) scratch[g] = 1.0f;
     }
-    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
-      const uint32_t e = lane + 64 * i;
-      if (e < a.experts && !kept[wave][e / per]) key[i] = ninf;
+      const uint32_t e = lane + kLanes * i;
+      if (e < a.experts && scratch[e / per] == 0.0f) rank[i] = kNone;
     }
   }
-  int32_t id = -1;
-  float weight = 0.0f;
+  id = -1;
+  weight = 0.0f;
   for (uint32_t n = 0; n < a.k; n++) {
-    Best b = {ninf, 0xFFFFFFFFu};
+    const int32_t at = take_best<kLanes, kPer>(rank, kNone);
+    float mine = s[0];
 #pragma unroll
-    for (int i = 0; i < kPer; i++) b = better(b, {key[i], lane + 64 * i});
-    b = wave_best(b);
-    if (b.key == ninf) break;
-    float mine = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kPer; i++)
-      if (b.at == lane + 64 * i) {
-        mine = s[i];
-        key[i] = ninf;
-      }
-    mine = __shfl(mine, int(b.at % 64));
-    if (lane == n) {
-      id = int32_t(b.at);
+    for (int i = 1; i < kPer; i++)
+      if (at / kLanes == i) mine = s[i];
+    mine = __shfl(mine, at & (kLanes - 1), kLanes);
+    if (lane == n && at >= 0) {
+      id = at;
       weight = mine;
     }
   }
   if (a.renormalize) {
-    const float sum = wave_sum(weight);
+    // lanes past k have none
+    const float sum = sum_of<kLanes>(weight);
     weight = sum != 0.0f ? weight / sum : 0.0f;
   }
   weight *= a.scale;
-  if (__ballot(bad)) weight = __builtin_nanf("");
+  if (votes<kLanes>(bad)) weight = __builtin_nanf("");
   if (live && lane < a.k) {
     const uint64_t at = uint64_t(token) * a.k + lane;
     global<int32_t>(a.ids)[at] = id;
     global<float>(a.weights)[at] = weight;
   }
+}
+
+template <int kLanes, int kPer>
+__global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(RouteArgs a) {
+  constexpr uint32_t kTokens = 64 * kTokenWaves / kLanes;
+  __shared__ float scratch[kTokens][kLanes * kPer];
+  const uint32_t t = threadIdx.x / kLanes;
+  int32_t id;
+  float weight;
+  choose<kLanes, kPer>(a, blockIdx.x * kTokens + t, scratch[t], id, weight);
 }
 
 struct SortArgs {
@@ -193,35 +239,59 @@ __global__ __launch_bounds__(kSortThreads) void wc_route_count_kernel(SortArgs a
 
 // The stable order of one block's slots: each expert's first place (all experts
 // before it, all blocks before this one, all waves before this wave), then the
-// rank of a slot among its wave's with the same expert.
-__global__ __launch_bounds__(kSortThreads) void wc_route_order_kernel(SortArgs a) {
+// rank of a slot among its wave's with the same expert.  `class_at(slot)` is a slot's
+// expert.
+struct SortShared {
+  uint32_t next[kSortThreads / 64][kMaxExperts + 1];
+  uint32_t all[kMaxExperts + 1], before[kMaxExperts + 1], wave_total[kSortThreads / 64];
+};
+template <class ClassAt>
+__device__ __forceinline__ void sort_block(const SortArgs& a, SortShared& sh, uint32_t block,
+                                           ClassAt class_at) {
   constexpr uint32_t kWaves = kSortThreads / 64, kEach = kSortSlots / kWaves;
-  __shared__ uint32_t next[kWaves][kMaxExperts + 1], wave_total[kWaves];
   const uint32_t t = threadIdx.x, lane = t % 64, wave = t / 64, classes = a.experts + 1;
   for (uint32_t w = 0; w < kWaves; w++)
-    for (uint32_t e = t; e < classes; e += kSortThreads) next[w][e] = 0;
+    for (uint32_t e = t; e < classes; e += kSortThreads) sh.next[w][e] = 0;
+  for (uint32_t e = t; e < classes; e += kSortThreads) sh.all[e] = sh.before[e] = 0;
   __syncthreads();
-  const uint32_t first = blockIdx.x * kSortSlots + wave * kEach;
+  const uint32_t first = block * kSortSlots + wave * kEach;
   uint32_t mine[kEach / 64];
 #pragma unroll
   for (uint32_t i = 0; i < kEach / 64; i++) {
     const uint32_t slot = first + i * 64 + lane;
-    mine[i] = slot < a.slots ? class_of(a, slot) : 0xFFFFFFFFu;
-    if (slot < a.slots) atomicAdd(&next[wave][mine[i]], 1u);
+    mine[i] = slot < a.slots ? class_at(slot) : 0xFFFFFFFFu;
+    if (slot < a.slots) atomicAdd(&sh.next[wave][mine[i]], 1u);
+  }
+  if (a.blocks > 1 && !a.hist) {
+    // few blocks: each counts them all for itself
+    const uint32_t mine_from = block * kSortSlots;
+#pragma unroll 4
+    for (uint32_t slot = t; slot < a.slots; slot += kSortThreads) {
+      const uint32_t c = class_at(slot);
+      atomicAdd(slot < mine_from ? &sh.before[c] : &sh.all[c], 1u);
+    }
+  } else if (a.blocks > 1) {
+    // each expert's slots in all blocks, and in those before this one: the blocks over as
+    // many threads to an expert as there are
+    const uint32_t sets = kSortThreads / classes, set = t / classes, e = t - set * classes;
+    if (set < sets) {
+      uint32_t all = 0, before = 0;
+#pragma unroll 4
+      for (uint32_t b = set; b < a.blocks; b += sets) {
+        const uint32_t n = global<const uint32_t>(a.hist)[uint64_t(b) * classes + e];
+        (b < block ? before : all) += n;
+      }
+      atomicAdd(&sh.all[e], all);
+      atomicAdd(&sh.before[e], before);
+    }
   }
   __syncthreads();
-  // a thread an expert: its slots in all blocks, and in the blocks before this one
-  uint32_t all = 0, before = 0;
+  uint32_t all = 0;
   if (t < classes) {
-    if (a.blocks == 1) {
-      for (uint32_t w = 0; w < kWaves; w++) all += next[w][t];
-    } else {
-      for (uint32_t b = 0; b < a.blocks; b++) {
-        const uint32_t n = global<const uint32_t>(a.hist)[uint64_t(b) * classes + t];
-        all += n;
-        before += b < blockIdx.x ? n : 0;
-      }
-    }
+    if (a.blocks > 1)
+      all = sh.all[t] + sh.before[t];
+    else
+      for (uint32_t w = 0; w < kWaves; w++) all += sh.next[w][t];
   }
   // exclusive scan over the experts
   uint32_t sum = all;
@@ -230,21 +300,21 @@ __global__ __launch_bounds__(kSortThreads) void wc_route_order_kernel(SortArgs a
     const uint32_t v = uint32_t(__shfl_up(int(sum), d));
     if (lane >= uint32_t(d)) sum += v;
   }
-  if (lane == 63) wave_total[wave] = sum;
+  if (lane == 63) sh.wave_total[wave] = sum;
   __syncthreads();
   uint32_t start = sum - all;
-  for (uint32_t w = 0; w < wave; w++) start += wave_total[w];
+  for (uint32_t w = 0; w < wave; w++) start += sh.wave_total[w];
   if (t < classes) {
-    if (blockIdx.x == 0) global<int32_t>(a.offsets)[t] = int32_t(start);
-    uint32_t at = start + before;
+    if (block == 0) global<int32_t>(a.offsets)[t] = int32_t(start);
+    uint32_t at = start + sh.before[t];
     for (uint32_t w = 0; w < kWaves; w++) {
-      const uint32_t n = next[w][t];
-      next[w][t] = at;
+      const uint32_t n = sh.next[w][t];
+      sh.next[w][t] = at;
       at += n;
     }
   }
   __syncthreads();
-  volatile uint32_t* const mine_next = next[wave];  // lanes read what another lane wrote
+  volatile uint32_t* const next = sh.next[wave];  // lanes read what another lane wrote
 #pragma unroll
   for (uint32_t i = 0; i < kEach / 64; i++) {
     const bool on = mine[i] != 0xFFFFFFFFu;
@@ -255,14 +325,47 @@ __global__ __launch_bounds__(kSortThreads) void wc_route_order_kernel(SortArgs a
     }
     if (on) {
       const uint32_t rank = uint32_t(__popcll(same & ((1ull << lane) - 1)));
-      const uint32_t place = mine_next[mine[i]] + rank;
+      const uint32_t place = next[mine[i]] + rank;
       global<int32_t>(a.order)[place] = int32_t(first + i * 64 + lane);
     }
     __builtin_amdgcn_wave_barrier();
-    if (on && !(same >> lane >> 1))
-      mine_next[mine[i]] = mine_next[mine[i]] + uint32_t(__popcll(same));
+    if (on && !(same >> lane >> 1)) next[mine[i]] = next[mine[i]] + uint32_t(__popcll(same));
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+__global__ __launch_bounds__(kSortThreads) void wc_route_order_kernel(SortArgs a) {
+  __shared__ SortShared sh;
+  sort_block(a, sh, blockIdx.x, [&](uint32_t slot) { return class_of(a, slot); });
+}
+
+// Few tokens: all of it by one workgroup.
+template <int kLanes, int kPer>
+__global__ __launch_bounds__(kSortThreads) void wc_route_small_kernel(RouteArgs a, SortArgs s) {
+  constexpr uint32_t kTokens = kSortThreads / kLanes;
+  __shared__ SortShared sh;
+  __shared__ float scratch[kTokens][kLanes * kPer];
+  __shared__ uint16_t classes[kSortSlots];
+  const uint32_t t = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  for (uint32_t first = 0; first < a.tokens; first += kTokens) {
+    int32_t id;
+    float weight;
+    choose<kLanes, kPer>(a, first + t, scratch[t], id, weight);
+    if (first + t < a.tokens && lane < a.k)
+      classes[(first + t) * a.k + lane] = uint16_t(id < 0 ? int32_t(a.experts) : id);
+  }
+  __syncthreads();
+  sort_block(s, sh, 0, [&](uint32_t slot) { return uint32_t(classes[slot]); });
+}
+
+template <int kLanes, int kPer>
+void start_choice(const RouteArgs& a, const SortArgs& s, bool small, hipStream_t st) {
+  constexpr uint32_t kTokens = 64 * kTokenWaves / kLanes;
+  if (small)
+    hipLaunchKernelGGL((wc_route_small_kernel<kLanes, kPer>), dim3(1), dim3(kSortThreads), 0, st, a, s);
+  else
+    hipLaunchKernelGGL((wc_route_choose_kernel<kLanes, kPer>), dim3((a.tokens + kTokens - 1) / kTokens),
+                       dim3(64 * kTokenWaves), 0, st, a);
 }
 
 bool params_ok(uint32_t tokens, const wc_route_params* p) {
@@ -283,7 +386,7 @@ extern "C" wc_status wc_route_workspace_bytes(uint32_t tokens, const wc_route_pa
   *bytes = 0;
   if (!params_ok(tokens, p)) return WC_EINVAL;
   const uint32_t blocks = sort_blocks(tokens * p->k);
-  if (blocks > 1) *bytes = uint64_t(blocks) * (p->experts + 1) * 4;
+  if (blocks > kSelfCount) *bytes = uint64_t(blocks) * (p->experts + 1) * 4;
   return WC_OK;
 }
 
@@ -309,21 +412,28 @@ extern "C" wc_status wc_route(const void* dev_logits, int32_t dtype, uint32_t to
                        reinterpret_cast<uint64_t>(dev_ids), reinterpret_cast<uint64_t>(dev_weights),
                        ld, tokens, p->experts, p->k, p->groups, p->top_groups, p->group_top, dtype,
                        p->score, p->renormalize, p->scale};
-  if (tokens) {
-    const dim3 grid((tokens + kTokenWaves - 1) / kTokenWaves), block(64 * kTokenWaves);
-    switch ((p->experts + 63) / 64) {
-      case 1: hipLaunchKernelGGL((wc_route_choose_kernel<1>), grid, block, 0, st, a); break;
-      case 2: hipLaunchKernelGGL((wc_route_choose_kernel<2>), grid, block, 0, st, a); break;
-      case 3: case 4: hipLaunchKernelGGL((wc_route_choose_kernel<4>), grid, block, 0, st, a); break;
-      default: hipLaunchKernelGGL((wc_route_choose_kernel<8>), grid, block, 0, st, a); break;
-    }
-    if (hipGetLastError() != hipSuccess) return WC_EHIP;
-  }
   const SortArgs s = {a.ids, reinterpret_cast<uint64_t>(dev_offsets),
                       reinterpret_cast<uint64_t>(dev_order),
-                      reinterpret_cast<uint64_t>(dev_workspace), tokens * p->k, p->experts,
+                      need ? reinterpret_cast<uint64_t>(dev_workspace) : 0, tokens * p->k, p->experts,
                       sort_blocks(tokens * p->k)};
-  if (s.blocks > 1) {
+  const uint32_t e = p->experts;
+  // small: one workgroup's round of choices, or two where a token takes one register (32
+  // tokens of 64 experts 8.4 us against 6.7 in two launches, which the host takes 4 us
+  // more for)
+  const uint32_t lanes = e <= 16 && p->k <= 16 ? 16 : e <= 32 ? 32 : 64;
+  const bool small = tokens <= (e <= 64 ? 2u : 1u) * kSortThreads / lanes && s.slots <= kSortSlots;
+  if (tokens) {
+    if (lanes == 16) start_choice<16, 1>(a, s, small, st);
+    else if (lanes == 32) start_choice<32, 1>(a, s, small, st);
+    else if (e <= 64 && p->k <= 16 && tokens >= kManyTokens) start_choice<16, 4>(a, s, false, st);
+    else if (e <= 64) start_choice<64, 1>(a, s, small, st);
+    else if (e <= 128) start_choice<64, 2>(a, s, small, st);
+    else if (e <= 256) start_choice<64, 4>(a, s, small, st);
+    else start_choice<64, 8>(a, s, small, st);
+    if (hipGetLastError() != hipSuccess) return WC_EHIP;
+    if (small) return WC_OK;
+  }
+  if (s.hist) {
     hipLaunchKernelGGL(wc_route_count_kernel, dim3(s.blocks), dim3(kSortThreads), 0, st, s);
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
   }

@@ -151,7 +151,8 @@ def lib():
         L.wc_stream.argtypes = [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_uint32,
                                 C.c_void_p, C.POINTER(C.c_uint64)]
         L.wc_stream.restype = C.c_int
-        job, experts = C.POINTER(_I8Job), C.POINTER(_I8Experts)
+        job = C.c_void_p  # wc_i8_job array: packed bytes or a ctypes array
+        experts = C.POINTER(_I8Experts)
         L.wc_quantize_i8.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint32, C.c_uint64,
                                      C.c_void_p, C.c_void_p, C.c_void_p]
         L.wc_matmul_i8_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32, C.c_uint32, job,
@@ -710,12 +711,23 @@ def gemv_w4_torch(blob: Blob, dev_blob, tensors, scales, zeros, xs, ys=None, str
 # decode_torch fills: the same bytes), activations, scales and results bfloat16,
 # float16 or float32.
 
-_FLOAT_TYPES = {"torch.bfloat16": 1, "torch.float16": 2, "torch.float32": 8}
+_NO_CONTEXT = contextlib.nullcontext()
 SCORES = {"softmax": 0, "sigmoid": 1}
+_floats, _ints = {}, ()
+
+
+def _types():
+    """C types of the float element types; filled at the first call, with torch."""
+    global _floats, _ints
+    if not _floats:
+        import torch
+        _ints = (torch.int8, torch.uint8)
+        _floats = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 8}
+    return _floats
 
 
 def _float_type(t, what: str) -> int:
-    code = _FLOAT_TYPES.get(str(t if not hasattr(t, "dtype") else t.dtype))
+    code = _types().get(t.dtype)
     if code is None:
         raise ValueError(f"{what} must be bfloat16, float16 or float32")
     return code
@@ -723,34 +735,36 @@ def _float_type(t, what: str) -> int:
 
 def _rows(t, what: str, cols: int = -1) -> int:
     """Row stride, in elements, of a 2-D device tensor whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{what} must be a 2-D device tensor")
-    if cols >= 0 and t.shape[1] != cols:
-        raise ValueError(f"{what} has {t.shape[1]} columns, not {cols}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if cols >= 0 and shape[1] != cols:
+        raise ValueError(f"{what} has {shape[1]} columns, not {cols}")
+    if stride[1] != 1 and shape[1] > 1:
         raise ValueError(f"{what}: the elements of a row must be next to each other")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
 def _vector(t, n: int, what: str) -> int:
-    if not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+    if t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{what} must be a contiguous device tensor of {n} elements")
     return _float_type(t, what)
 
 
 def _codes(t, what: str):
-    if str(t.dtype) not in ("torch.int8", "torch.uint8"):
+    _types()
+    if t.dtype not in _ints:
         raise ValueError(f"{what} must be int8 codes")
     return t
 
 
 def _stream_of(stream, device):
-    """The stream to launch on, and the context in which to allocate what the launch
-    uses, so that the allocator knows the stream that uses it."""
+    """The stream handle to launch on, and the context in which to allocate what the
+    launch uses, so that the allocator knows the stream that uses it."""
     import torch
     if stream is None:
-        return torch.cuda.current_stream(device), contextlib.nullcontext()
-    return stream, torch.cuda.stream(stream)
+        return torch._C._cuda_getCurrentRawStream(device.index), _NO_CONTEXT
+    return stream.cuda_stream, torch.cuda.stream(stream)
 
 
 def _workspace(workspace, need: int, device):
@@ -793,33 +807,45 @@ def quantize_i8_torch(x, q=None, scale=None, stream=None):
     if scale.dtype != torch.float32 or scale.numel() != m or not scale.is_contiguous():
         raise ValueError(f"scale must be {m} contiguous float32")
     rc = lib().wc_quantize_i8(x.data_ptr(), dt, m, k, ld, q.data_ptr(), scale.data_ptr(),
-                              st.cuda_stream)
+                              st)
     if rc:
         raise WcError("wc_quantize_i8", rc)
     return q, scale
 
 
+_JOB = struct.Struct("=6QI3i")  # wc_i8_job
+
+
 def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, device):
-    """ctypes wc_i8_job array and the ys (allocated where None)."""
-    import torch
+    """The wc_i8_job array, packed, and the ys (allocated where None)."""
     n_jobs = len(ws)
     if len(scales) != n_jobs or (biases is not None and len(biases) != n_jobs) or \
             (ys is not None and len(ys) != n_jobs):
         raise ValueError("one scale tensor, bias entry and y a matrix")
-    jobs = (_I8Job * max(1, n_jobs))()
-    out = []
-    for i, w in enumerate(ws):
-        ldw = _rows(_codes(w, "w"), "w", k)
+    floats = _types()
+    jobs, out = [], []
+    for i in range(n_jobs):
+        w, s = ws[i], scales[i]
+        ldw = _rows(w, "w", k)
+        if w.dtype not in _ints:
+            raise ValueError("w must be int8 codes")
         n = w.shape[0]
-        y = torch.empty((m, n), dtype=dtype, device=device) if ys is None else ys[i]
-        out.append(y)
-        if tuple(y.shape) != (m, n):
-            raise ValueError(f"y must be {m} x {n}")
+        st = _vector(s, n, "a matrix's scale")
         b = None if biases is None else biases[i]
-        jobs[i] = _I8Job(w.data_ptr(), scales[i].data_ptr(), _ptr(b), y.data_ptr(), ldw,
-                         _rows(y, "y"), n, _vector(scales[i], n, "a matrix's scale"),
-                         0 if b is None else _vector(b, n, "a bias"), _float_type(y, "y"))
-    return jobs, out
+        bp, bt = (0, 0) if b is None else (b.data_ptr(), _vector(b, n, "a bias"))
+        if ys is None:
+            y, ldy = w.new_empty((m, n), dtype=dtype), n
+        else:
+            y = ys[i]
+            if y.shape != (m, n):
+                raise ValueError(f"y must be {m} x {n}")
+            ldy = _rows(y, "y")
+        yt = floats.get(y.dtype)
+        if yt is None:
+            raise ValueError("y must be bfloat16, float16 or float32")
+        out.append(y)
+        jobs.append(_JOB.pack(w.data_ptr(), s.data_ptr(), bp, y.data_ptr(), ldw, ldy, n, st, bt, yt))
+    return b"".join(jobs), out
 
 
 def matmul_i8_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=None,
@@ -843,7 +869,7 @@ def matmul_i8_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=No
             workspace = _workspace(workspace, need.value, q.device)
     if not rc:
         rc = lib().wc_matmul_i8(q.data_ptr(), scale.data_ptr(), m, k, len(ws), jobs,
-                                _ptr(workspace), _size(workspace), st.cuda_stream)
+                                _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_matmul_i8", rc)
     return ys
@@ -865,7 +891,7 @@ def linear_i8_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
             workspace = _workspace(workspace, need.value, x.device)
     if not rc:
         rc = lib().wc_linear_i8(x.data_ptr(), dt, m, k, ld, len(ws), jobs, _ptr(workspace),
-                                _size(workspace), st.cuda_stream)
+                                _size(workspace), st)
     if rc:
         raise WcError("wc_linear_i8", rc)
     return ys
@@ -899,16 +925,15 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
         raise WcError("wc_route", rc)
     with where:
         if out is None:
-            out = Routing(torch.empty((tokens, k), dtype=torch.int32, device=dev),
-                          torch.empty((tokens, k), dtype=torch.float32, device=dev),
-                          torch.empty(experts + 1, dtype=torch.int32, device=dev),
-                          torch.empty(tokens * k, dtype=torch.int32, device=dev))
+            new = logits.new_empty
+            out = Routing(new((tokens, k), dtype=torch.int32), new((tokens, k), dtype=torch.float32),
+                          new(experts + 1, dtype=torch.int32), new(tokens * k, dtype=torch.int32))
         else:
             _check_routing(out, tokens, k, experts)
         workspace = _workspace(workspace, need.value, dev)
     rc = lib().wc_route(logits.data_ptr(), dt, tokens, ld, C.byref(params), _ptr(bias),
                         *(t.data_ptr() for t in out), _ptr(workspace), _size(workspace),
-                        st.cuda_stream)
+                        st)
     if rc:
         raise WcError("wc_route", rc)
     return out
@@ -920,17 +945,19 @@ def _check_routing(r, tokens: int, k: int, experts: int):
                                   (r.weights, (tokens, k), torch.float32, "weights"),
                                   (r.offsets, (experts + 1,), torch.int32, "offsets"),
                                   (r.order, (tokens * k,), torch.int32, "order")):
-        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
             raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {shape}")
 
 
 def _bank(w, scale, experts: int, n: int, k: int, what: str):
     _codes(w, what)
-    if tuple(w.shape) != (experts, n, k) or not w.is_cuda or not w[0].is_contiguous():
+    stride = w.stride()
+    if w.shape != (experts, n, k) or not w.is_cuda or (k > 1 and stride[2] != 1) or \
+            (n > 1 and stride[1] != k):
         raise ValueError(f"{what} must be {experts} x {n} x {k} codes, contiguous in each expert")
-    if tuple(scale.shape) != (experts, n):
+    if scale.shape != (experts, n):
         raise ValueError(f"the scales of {what} must be {experts} x {n}")
-    return _I8Experts(w.data_ptr(), scale.data_ptr(), w.stride(0) if experts > 1 else n * k,
+    return _I8Experts(w.data_ptr(), scale.data_ptr(), stride[0] if experts > 1 else n * k,
                       _vector(scale, experts * n, f"the scales of {what}"), 0)
 
 
@@ -958,14 +985,14 @@ def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
         raise WcError("wc_experts_i8", rc)
     with where:
         if y is None:
-            y = torch.empty((tokens, hidden), dtype=x.dtype, device=x.device)
+            y = x.new_empty((tokens, hidden))
         workspace = _workspace(workspace, need.value, x.device)
     if tuple(y.shape) != (tokens, hidden) or y.dtype != x.dtype:
         raise ValueError(f"y must be {tokens} x {hidden} of x's type")
     rc = lib().wc_experts_i8(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
                              *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
                              y.data_ptr(), _rows(y, "y"), _ptr(workspace), _size(workspace),
-                             st.cuda_stream)
+                             st)
     if rc:
         raise WcError("wc_experts_i8", rc)
     return y
