@@ -399,33 +399,34 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
 #pragma unroll
   for (int i = 0; i < T::kXLoads; i++)
     xoff[i] = slot_at(a, min(first + T::row_of(i), last - 1)) / a.k * row_bytes + T::byte_of();
-  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); };
+  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
   // W row r of the tile: column r / 64 * 32 + r mod 32 of gate (r mod 64 < 32) or of up
   const uint64_t gate = a.gate.w + e * a.gate.stride + uint64_t(n0) * k;
   const uint64_t up = a.up.w + e * a.up.stride + uint64_t(n0) * k;
   i32x16 acc[T::kMT][2];
   if constexpr (kDirect) {
-    const u32x4 gr = rows_rsrc(gate, n_rows * k), ur = rows_rsrc(up, n_rows * k);
+    u32x4 wr[T::kWLoads];
     uint32_t woff[T::kWLoads];
 #pragma unroll
     for (int i = 0; i < T::kWLoads; i++) {
       const uint32_t r = T::row_of(i);
+      wr[i] = rows_rsrc(T::first_row(i) & 32 ? up : gate, n_rows * k);
       woff[i] = min(r / 64 * 32 + r % 32, n_rows - 1) * k + T::byte_of();
     }
-    T::product(lds, row_bytes / kStage, load_x, [&](int i, uint32_t s, uint32_t to) {
-      load_lds((wave + T::kWaves * i) & 4 ? ur : gr, to, woff[i] + s * kStage);
+    T::product(lds, row_bytes / T::kBytes, load_x, [&](int i, uint32_t s, uint32_t to) {
+      load_lds(wr[i], to, woff[i] + s * T::kBytes);
     }, acc);
   } else {
     global_ptr<const uint8_t> w[T::kWLoads];
 #pragma unroll
     for (int i = 0; i < T::kWLoads; i++) {
       const uint32_t r = T::row_of(i);
-      w[i] = global<const uint8_t>((wave + T::kWaves * i) & 4 ? up : gate) +
+      w[i] = global<const uint8_t>(T::first_row(i) & 32 ? up : gate) +
              uint64_t(min(r / 64 * 32 + r % 32, n_rows - 1)) * k + T::byte_of();
     }
     const int32_t left = int32_t(k) - int32_t(T::byte_of());
-    T::product(lds, row_bytes / kStage, load_x, [&](int i, uint32_t s, uint32_t) {
-      return load_codes(w[i] + uint64_t(s) * kStage, left - int32_t(s * kStage));
+    T::product(lds, row_bytes / T::kBytes, load_x, [&](int i, uint32_t s, uint32_t) {
+      return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
     }, acc);
   }
   const uint32_t lane = threadIdx.x % 64;
@@ -474,7 +475,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
 #pragma unroll
   for (int i = 0; i < T::kXLoads; i++)
     xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
-  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); };
+  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
   const uint64_t down = a.down.w + e * a.down.stride + uint64_t(n0) * k;
   i32x16 acc[T::kMT][T::kNT];
   if constexpr (kDirect) {
@@ -483,16 +484,16 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
 #pragma unroll
     for (int i = 0; i < T::kWLoads; i++)
       woff[i] = min(T::row_of(i), n_rows - 1) * k + T::byte_of();
-    T::product(lds, row_bytes / kStage, load_x,
-               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * kStage); }, acc);
+    T::product(lds, row_bytes / T::kBytes, load_x,
+               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
   } else {
     global_ptr<const uint8_t> w[T::kWLoads];
 #pragma unroll
     for (int i = 0; i < T::kWLoads; i++)
       w[i] = global<const uint8_t>(down) + uint64_t(min(T::row_of(i), n_rows - 1)) * k + T::byte_of();
     const int32_t left = int32_t(k) - int32_t(T::byte_of());
-    T::product(lds, row_bytes / kStage, load_x, [&](int i, uint32_t s, uint32_t) {
-      return load_codes(w[i] + uint64_t(s) * kStage, left - int32_t(s * kStage));
+    T::product(lds, row_bytes / T::kBytes, load_x, [&](int i, uint32_t s, uint32_t) {
+      return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
     }, acc);
   }
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;

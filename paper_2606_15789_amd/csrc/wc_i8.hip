@@ -255,17 +255,17 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt);
   const uint32_t m0 = mt * kBM, n0 = nt * kBN;
   const uint32_t m_rows = min(kBM, a.m - m0), n_rows = min(kBN, J.n - n0);
-  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k)), all = row_bytes / kStage;
+  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k)), all = row_bytes / T::kBytes;
   // this workgroup's part of the stages
   const uint32_t each = all / a.splits, rest = all % a.splits, part = blockIdx.y;
   const uint32_t s0 = part * each + min(part, rest), stages = each + (part < rest);
-  const uint32_t k0 = s0 * kStage;
+  const uint32_t k0 = s0 * T::kBytes;
   const u32x4 xr = rows_rsrc(a.q + m0 * uint64_t(row_bytes) + k0, m_rows * row_bytes - k0);
   uint32_t xoff[T::kXLoads];
 #pragma unroll
   for (int i = 0; i < T::kXLoads; i++)
     xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
-  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); };
+  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
   i32x16 acc[T::kMT][T::kNT];
   if constexpr (kDirect) {
     const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw + k0, uint32_t((n_rows - 1) * J.ldw + a.k - k0));
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
     for (int i = 0; i < T::kWLoads; i++)
       woff[i] = min(T::row_of(i), n_rows - 1) * uint32_t(J.ldw) + T::byte_of();
     T::product(lds, stages, load_x,
-               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * kStage); }, acc);
+               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
   } else {
     global_ptr<const uint8_t> w[T::kWLoads];
 #pragma unroll
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
       w[i] = global<const uint8_t>(J.w) + (n0 + min(T::row_of(i), n_rows - 1)) * J.ldw + k0 + T::byte_of();
     const int32_t left = int32_t(a.k - k0) - int32_t(T::byte_of());
     T::product(lds, stages, load_x, [&](int i, uint32_t s, uint32_t) {
-      return load_codes(w[i] + uint64_t(s) * kStage, left - int32_t(s * kStage));
+      return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
     }, acc);
   }
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -363,6 +363,18 @@ bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx) {
 
 using Tile256 = Tile<256, 256, 2, 4>;
 using Tile128 = Tile<128, 128, 2, 2>;
+using Tile64 = Tile<64, 128, 1, 4, 3>;
+using Tile32 = Tile<32, 128, 1, 4, 4>;
+#ifdef WC_TUNE
+using TileA = Tile<128, 128, 2, 2, 3>;
+using TileB = Tile<256, 256, 2, 4, 5, 64>;
+using TileC = Tile<256, 256, 2, 4, 4, 64>;
+using TileD = Tile<128, 128, 2, 4, 4>;
+using TileE = Tile<64, 128, 1, 4, 4>;
+using TileF = Tile<64, 64, 1, 2, 4>;
+using TileG = Tile<256, 128, 4, 2, 3>;
+using TileH = Tile<256, 128, 4, 2, 6, 64>;
+#endif
 
 // Quantising in the product's own launch saves a launch (2 us, 4 on the host) and costs
 // every workgroup the row: linear at m = 1, k = 4096, n = 6144 9.7 us against 11.2,
@@ -372,7 +384,11 @@ using Tile128 = Tile<128, 128, 2, 2>;
 constexpr uint64_t kHoldAlways = 4096, kHoldSmall = 8192, kHoldSmallWeights = 32u << 20;
 
 // Which kernel multiplies m rows, and in how many parts of k.
-enum class Kernel { kRows, kRing, kTile128, kTile256 };
+enum class Kernel { kRows, kRing, kTile32, kTile64, kTile128, kTile256
+#ifdef WC_TUNE
+, kA, kB, kC, kD, kE, kF, kG, kH
+#endif
+};
 struct Plan {
   Kernel kernel;
   bool direct;      // every W can go to LDS as it is
@@ -380,6 +396,12 @@ struct Plan {
   uint32_t splits;
   uint64_t part_bytes;
 };
+}  // namespace
+#ifdef WC_TUNE
+#include <cstdlib>
+#include <cstdio>
+#endif
+namespace {
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   Plan p{Kernel::kRows, true, false, 1, 0};
   uint64_t tiles128 = 0, tiles256 = 0, sums = 0, weights = 0;
@@ -393,6 +415,14 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
     tiles256 += uint64_t(m + 255) / 256 * ((J.n + 255) / 256);
     sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
   }
+#ifdef WC_TUNE
+  if (const char* e = getenv("WC_PLAN")) {
+    int kn = 0, sp = 1;
+    if (sscanf(e, "%d,%d", &kn, &sp) == 2) {
+      p.kernel = Kernel(kn); p.splits = sp; if (sp > 1) p.part_bytes = sums * sp; return p;
+    }
+  }
+#endif
   if (m <= 16) {
     if (p.direct) p.kernel = Kernel::kRing;
     const uint64_t held = m * WC_I8_ROW_BYTES(k);
@@ -409,6 +439,35 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   while (tiles * p.splits * 2 <= slots && stages >= p.splits * 2 * 8) p.splits *= 2;
   if (p.splits > 1) p.part_bytes = sums * p.splits;
   return p;
+}
+
+// f(Tile) for the kernel's tile.
+template <class F>
+void with_tile(Kernel kernel, F f) {
+  switch (kernel) {
+    case Kernel::kTile32: return f(Tile32{});
+    case Kernel::kTile64: return f(Tile64{});
+    case Kernel::kTile128: return f(Tile128{});
+    case Kernel::kTile256: return f(Tile256{});
+#ifdef WC_TUNE
+    case Kernel::kA: return f(TileA{});
+    case Kernel::kB: return f(TileB{});
+    case Kernel::kC: return f(TileC{});
+    case Kernel::kD: return f(TileD{});
+    case Kernel::kE: return f(TileE{});
+    case Kernel::kF: return f(TileF{});
+    case Kernel::kG: return f(TileG{});
+    case Kernel::kH: return f(TileH{});
+#endif
+    default: return;
+  }
+}
+uint32_t tiles_of(Kernel kernel, uint32_t m, uint32_t n) {
+  uint32_t tiles = (n + 15) / 16;
+  with_tile(kernel, [&](auto t) {
+    tiles = (m + t.kRows - 1) / t.kRows * ((n + t.kCols - 1) / t.kCols);
+  });
+  return tiles;
 }
 
 template <int kX, int kType = 0>
@@ -440,10 +499,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
                 J.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0};
     if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
-    tiles += p.kernel == Kernel::kRows      ? (J.n + 15) / 16
-             : p.kernel == Kernel::kRing    ? (J.n + 15) / 16
-             : p.kernel == Kernel::kTile128 ? (m + 127) / 128 * ((J.n + 127) / 128)
-                                            : (m + 255) / 256 * ((J.n + 255) / 256);
+    tiles += tiles_of(p.kernel, m, J.n);
   }
   if (p.kernel == Kernel::kRing) {
     a.m = m;
@@ -457,17 +513,13 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
   if (p.kernel != Kernel::kRows) {
     a.m = m;
     const dim3 grid(tiles, p.splits);
-    if (p.kernel == Kernel::kTile256) {
+    with_tile(p.kernel, [&](auto t) {
+      using T = decltype(t);
       if (p.direct)
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile256, true>), grid, dim3(512), 0, stream, a);
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, true>), grid, dim3(T::kThreads), 0, stream, a);
       else
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile256, false>), grid, dim3(512), 0, stream, a);
-    } else {
-      if (p.direct)
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile128, true>), grid, dim3(256), 0, stream, a);
-      else
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<Tile128, false>), grid, dim3(256), 0, stream, a);
-    }
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, false>), grid, dim3(T::kThreads), 0, stream, a);
+    });
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
     if (p.splits > 1) {
       const uint32_t rows = m < 65536 ? m : 65536;

@@ -1,12 +1,14 @@
 // wc_i8_tile.h -- the int8 matrix product of one tile by one workgroup, operands
 // through LDS: C[n][m] = sum_k W[n][k] x[m][k] on v_mfma_i32_32x32x32_i8.
 //
-// A stage is 128 bytes of k of every row of the tile.  Both operands go from
+// A stage is kK (64 or 128) bytes of k of every row of the tile.  Both operands go from
 // memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1
-// stages ahead of the products.  A row's eight 16-byte chunks are stored in the order
-// chunk ^ (row mod 8): the eight lanes that read LDS together, the same chunk of
-// eight rows next to each other, then touch all banks once.
+// stages ahead of the products.  A row's 16-byte chunks are stored in the order
+// chunk ^ turn(row): the eight lanes that read LDS together, the same chunk of eight rows
+// next to each other, then touch all banks once.
 #pragma once
+
+#include <utility>
 
 #include "wc_i8.h"
 
@@ -14,7 +16,7 @@ namespace wc_i8 {
 
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kStage = 128;  // bytes of k to a stage
+constexpr int kStage = 128;  // bytes of k to a block of a row
 
 // A raw buffer of `bytes` bytes: reads past them give zeros.
 __device__ __forceinline__ u32x4 rows_rsrc(uint64_t base, uint32_t bytes) {
@@ -30,33 +32,36 @@ __device__ __forceinline__ void load_lds(u32x4 rs, uint32_t lds, uint32_t offset
                : "memory");
 }
 
-// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages in LDS.
-template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2>
+// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages of kK bytes in LDS.
+template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2, int kK = 128>
 struct Tile {
   static constexpr int kWM_ = kWM, kWN_ = kWN, kWaves = kWM * kWN, kThreads = 64 * kWaves;
   static constexpr int kMT = kBM / kWM / 32, kNT = kBN / kWN / 32;  // 32 x 32 blocks to a wave
-  static constexpr int kXLoads = kBM / 8 / kWaves, kWLoads = kBN / 8 / kWaves;
-  static constexpr int kBuffer = (kBM + kBN) * kStage;
+  static constexpr int kBytes = kK, kEach = 1024 / kK;  // rows to a load of a wave
+  static constexpr int kXLoads = kBM / kEach / kWaves, kWLoads = kBN / kEach / kWaves;
+  static constexpr int kBuffer = (kBM + kBN) * kK;
   static constexpr int kLds = kDepth * kBuffer, kRows = kBM, kCols = kBN;
-  static_assert(kBM % (8 * kWaves) == 0 && kBN % (8 * kWaves) == 0);
+  static_assert(kK == 64 || kK == 128);
+  static_assert(kBM % (kEach * kWaves) == 0 && kBN % (kEach * kWaves) == 0 && kLds <= 160 * 1024);
 
-  // Row of the tile and byte of its stage that load i of this lane brings: each
-  // load of a wave is 8 rows.
+  // Row of the tile and byte of its stage that load i of this lane brings.
+  static __device__ __forceinline__ uint32_t first_row(int i) {
+    return kEach * (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) + kWaves * i);
+  }
   static __device__ __forceinline__ uint32_t row_of(int i) {
-    return 8 * (threadIdx.x / 64 + kWaves * i) + threadIdx.x % 64 / 8;
+    return first_row(i) + threadIdx.x % 64 / (kK / 16);
+  }
+  static __device__ __forceinline__ uint32_t turn(uint32_t row) {
+    return kK == 128 ? row & 7 : (row >> 2) & 3;
   }
   static __device__ __forceinline__ uint32_t byte_of() {
-    return ((threadIdx.x % 8) ^ (threadIdx.x % 64 / 8)) * 16;
+    return ((threadIdx.x % (kK / 16)) ^ turn(threadIdx.x % 64 / (kK / 16))) * 16;
   }
 
-  // Waits for all but the loads of the newest `later` stages (kN at most), then for the
-  // other waves.
-  template <int kN>
-  static __device__ __forceinline__ void arrive(uint32_t later) {
-    if constexpr (kN > 0) {
-      if (later < kN) return arrive<kN - 1>(later);
-    }
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kN * (kXLoads + kWLoads)) : "memory");
+  // Waits for all but the loads of the newest kLater stages, then for the other waves.
+  template <int kLater>
+  static __device__ __forceinline__ void arrive() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater * (kXLoads + kWLoads)) : "memory");
   }
 
   // `load_x(i, stage, lds)` and `load_w(i, stage, lds)` start load i of a stage's rows
@@ -76,66 +81,98 @@ struct Tile {
       for (int n = 0; n < kNT; n++)
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[m][n][i] = 0;
-    i32x4 held[kDirect ? 1 : kWLoads];
-    const auto start = [&](uint32_t s, uint32_t slot) {
+    // stages ahead: one where W comes through registers
+    constexpr uint32_t kAhead = kDirect ? kDepth - 1 : 1, kSlots = kAhead + 1;
+    constexpr int kAll = kXLoads + (kDirect ? kWLoads : 0);
+    // Load i of a stage.  Stages past the last are loaded too: the buffers' ends bound
+    // them, nothing reads them, and the loop has no branches.
+    const auto start = [&](int i, uint32_t s, uint32_t slot) {
       const uint32_t to = __builtin_amdgcn_readfirstlane(base + slot * kBuffer + wave * 1024);
+      if (i < kXLoads) load_x(i, s, to + uint32_t(i) * kThreads * 16);
+      else load_w(i - kXLoads, s, to + kBM * kK + uint32_t(i - kXLoads) * kThreads * 16);
+    };
+    i32x4 held[kDirect ? 1 : kWLoads];
+    const auto hold = [&](uint32_t s) {
+      if constexpr (!kDirect) {
 #pragma unroll
-      for (int i = 0; i < kXLoads; i++) load_x(i, s, to + uint32_t(i) * kThreads * 16);
-#pragma unroll
-      for (int i = 0; i < kWLoads; i++) {
-        const uint32_t there = to + kBM * kStage + uint32_t(i) * kThreads * 16;
-        if constexpr (kDirect) load_w(i, s, there);
-        else held[i] = load_w(i, s, there);
+        for (int i = 0; i < kWLoads; i++) held[i] = load_w(i, s, 0u);
       }
     };
     const auto keep = [&](uint32_t slot) {
       if constexpr (!kDirect) {
-        uint8_t* to = lds + slot * kBuffer + kBM * kStage + threadIdx.x * 16;
+        uint8_t* to = lds + slot * kBuffer + kBM * kK + threadIdx.x * 16;
 #pragma unroll
         for (int i = 0; i < kWLoads; i++)
           *reinterpret_cast<i32x4*>(to + i * kThreads * 16) = held[i];
       }
     };
-    // stages ahead: one where W comes through registers
-    constexpr uint32_t kAhead = kDirect ? kDepth - 1 : 1;
-    uint32_t at[4];
+    constexpr int kQuarters = kK / 32;
+    uint32_t at[kQuarters];
 #pragma unroll
-    for (int k = 0; k < 4; k++)
-      at[k] = lane % 32 * kStage + ((2 * k + lane / 32) ^ (lane & 7)) * 16;
-    const uint32_t xrow = wm * (kBM / kWM) * kStage, wrow = (kBM + wn * (kBN / kWN)) * kStage;
+    for (int k = 0; k < kQuarters; k++)
+      at[k] = lane % 32 * kK + ((2 * k + lane / 32) ^ turn(lane)) * 16;
+    const uint32_t xrow = wm * (kBM / kWM) * kK, wrow = (kBM + wn * (kBN / kWN)) * kK;
+    i32x4 x[2][kMT], w[2][kNT];  // operands of two 32-byte quarters of a block
+    const auto read = [&](int set, const uint8_t* b, int k, int i) {
+      if (i < kNT) w[set][i] = *reinterpret_cast<const i32x4*>(b + wrow + at[k] + i * 32 * kK);
+      else x[set][i - kNT] = *reinterpret_cast<const i32x4*>(b + xrow + at[k] + (i - kNT) * 32 * kK);
+    };
+    // The products of one quarter, operand set `set`.  Between them, in the order written:
+    // the reads of the next quarter k of the stage in `slot`, and loads kFrom .. kTo - 1 of
+    // stage `s`, so that the matrix unit never waits for a queue of either to drain.
+    const auto quarter = [&]<int kFrom, int kTo>(int set, uint32_t slot, int k, uint32_t s, uint32_t to,
+                                                 std::integer_sequence<int, kFrom, kTo>) {
+      const uint8_t* b = lds + slot * kBuffer;
+      constexpr int kProducts = kMT * kNT, kReads = kMT + kNT;
+#pragma unroll
+      for (int p = 0; p < kProducts; p++) {
+        const int m = p / kNT, n = p % kNT;
+        acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[set][n], x[set][m], acc[m][n], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kReads; i++)
+          if (i * kProducts / kReads == p) read(set ^ 1, b, k, i);
+#pragma unroll
+        for (int i = kFrom; i < kTo; i++)
+          if ((i - kFrom) * kProducts / (kTo - kFrom) == p) start(i, s, to);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    constexpr int kHalf = kAll / 2;
+    using First = std::integer_sequence<int, 0, kHalf>;
+    using Second = std::integer_sequence<int, kHalf, kAll>;
+    using None = std::integer_sequence<int, 0, 0>;
 #pragma unroll
     for (uint32_t s = 0; s < kAhead; s++)
-      if (s < stages) {
-        start(s, s);
-        keep(s);
-      }
-    uint32_t slot = 0, next = kAhead;
+#pragma unroll
+      for (int i = 0; i < kAll; i++) start(i, s, s);
+    hold(0);
+    keep(0);
+    arrive<kDirect ? int(kAhead) - 1 : 0>();
+#pragma unroll
+    for (int i = 0; i < kHalf; i++) start(i, kAhead, kAhead);
+    hold(1);
+#pragma unroll
+    for (int i = 0; i < kMT + kNT; i++) read(0, lds, 0, i);
+    uint32_t slot = 0, fill = kAhead;  // the stage's place, and that of the one it loads
     for (uint32_t s = 0; s < stages; s++) {
-      // this wave's loads of stage s are in LDS and its reads of the stage that the next
-      // loads replace are done, and so with the other waves behind the barrier
-      arrive<kDirect ? int(kAhead) - 1 : 0>(stages - 1 - s);
-      const bool more = s + kAhead < stages;
-      if (more) start(s + kAhead, next);
-      const uint8_t* b = lds + slot * kBuffer;
+      quarter(0, slot, 1, s + kAhead, fill, Second{});
 #pragma unroll
-      for (int k = 0; k < 4; k++) {
-        i32x4 x[kMT], w[kNT];
-#pragma unroll
-        for (int m = 0; m < kMT; m++)
-          x[m] = *reinterpret_cast<const i32x4*>(b + xrow + at[k] + m * 32 * kStage);
-#pragma unroll
-        for (int n = 0; n < kNT; n++)
-          w[n] = *reinterpret_cast<const i32x4*>(b + wrow + at[k] + n * 32 * kStage);
-#pragma unroll
-        for (int m = 0; m < kMT; m++)
-#pragma unroll
-          for (int n = 0; n < kNT; n++)
-            acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[n], x[m], acc[m][n], 0, 0, 0);
+      for (int k = 1; k < kQuarters - 1; k++) quarter(k & 1, slot, k + 1, 0, 0, None{});
+      // Before the last quarter's products: the next stage's loads of this wave are in LDS
+      // and its reads of this stage done, and so with the other waves behind the barrier.
+      // The stage after those in flight then replaces this one.
+      keep(fill);
+      // lgkmcnt(0) as the compiler knows it: no waits for these operands further on
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      arrive<kDirect ? int(kAhead) - 1 : 0>();
+      fill = slot;
+      slot = slot + 1 < kSlots ? slot + 1 : 0;
+      if constexpr (!kDirect) {
+        if (s + 2 < stages) hold(s + 2);
       }
-      if (more) keep(next);
-      slot = slot + 1 < kDepth ? slot + 1 : 0;
-      next = next + 1 < kDepth ? next + 1 : 0;
+      quarter(1, slot, 0, s + 1 + kAhead, fill, First{});
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // the waves leave together: LDS is free for the results
     __syncthreads();
   }
