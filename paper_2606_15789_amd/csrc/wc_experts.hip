@@ -386,8 +386,9 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
 template <class T, bool kDirect>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
-  static_assert(T::kNT == 2);
-  constexpr uint32_t kBM = T::kMT * 32 * T::kWM_, kCols = T::kWN_ * 32;
+  __shared__ float scales[T::kRows];  // of the tile's rows of x
+  static_assert(T::kNT == 2 && T::kRows <= T::kThreads);
+  constexpr uint32_t kBM = T::kRows, kCols = T::kWN_ * 32;
   uint32_t mt, nt, e, first, last;
   tile_at(blockIdx.x, a.blocks, (a.ffn + kCols - 1) / kCols, mt, nt);
   if (!tile_of<kBM>(a, mt, e, first, last)) return;
@@ -400,6 +401,9 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
   for (int i = 0; i < T::kXLoads; i++)
     xoff[i] = slot_at(a, min(first + T::row_of(i), last - 1)) / a.k * row_bytes + T::byte_of();
   const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
+  // a load among the stores at the end would wait for all stores before it
+  const float row_scale =
+      global<const float>(a.xscale)[slot_at(a, min(first + threadIdx.x % kBM, last - 1)) / a.k];
   // W row r of the tile: column r / 64 * 32 + r mod 32 of gate (r mod 64 < 32) or of up
   const uint64_t gate = a.gate.w + e * a.gate.stride + uint64_t(n0) * k;
   const uint64_t up = a.up.w + e * a.up.stride + uint64_t(n0) * k;
@@ -438,14 +442,19 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
     gs[i] = load_float(a.gate.scale, a.gate.scale_dtype, at);
     us[i] = load_float(a.up.scale, a.up.scale_dtype, at);
   }
+  if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
+  __syncthreads();
+  // no branches: rows and columns past the last go nowhere
+  const uint32_t pitch = pitch_of(a.ffn) * 4;
+  const u32x4 to = rows_rsrc(a.h + first * uint64_t(pitch), (last - first) * pitch);
+  const uint32_t column = nw + lane % 8 * 4, out = column < a.ffn ? column * 4 : kNowhere;
 #pragma unroll
   for (int b = 0; b < T::kMT; b++)
     T::template rows_out<32>(
         lds, [&](int c, int i) { return float(acc[b][c][i]); },
-        [&](uint32_t row, uint32_t col, auto get) {
-          const uint32_t place = mw + b * 32 + row, n = nw + col;
-          if (place >= last || n >= a.ffn) return;
-          const float xs = global<const float>(a.xscale)[slot_at(a, place) / a.k];
+        [&](uint32_t r, uint32_t, auto get) {
+          const uint32_t row = mw - first + b * 32 + r;
+          const float xs = scales[row];
           const f32x4 g4 = get(0), u4 = get(32);
           f32x4 h;
 #pragma unroll
@@ -453,15 +462,17 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
             const float g = g4[i] * xs * gs[i], u = u4[i] * xs * us[i];
             h[i] = g / (1.0f + expf(-g)) * u;
           }
-          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.h) +
-                                               uint64_t(place) * pitch_of(a.ffn) + n) = h;
+          store_rows(to, out + row * pitch, __builtin_bit_cast(u32x4, h));
         });
 }
 
 template <class T, bool kDirect>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
-  constexpr uint32_t kBM = T::kMT * 32 * T::kWM_, kBN = T::kNT * 32 * T::kWN_;
+  __shared__ float scales[T::kRows];   // of the tile's rows of h, and their slots
+  __shared__ uint32_t slots[T::kRows];
+  static_assert(T::kRows <= T::kThreads);
+  constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
   uint32_t mt, nt, e, first, last;
   tile_at(blockIdx.x, a.blocks, (a.hidden + kBN - 1) / kBN, mt, nt);
   if (!tile_of<kBM>(a, mt, e, first, last)) return;
@@ -476,6 +487,10 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   for (int i = 0; i < T::kXLoads; i++)
     xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
   const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
+  // a load among the stores at the end would wait for all stores before it
+  const uint32_t place0 = min(first + threadIdx.x % kBM, last - 1);
+  const float row_scale = global<const float>(a.hscale)[place0];
+  const uint32_t row_slot = slot_at(a, place0);
   const uint64_t down = a.down.w + e * a.down.stride + uint64_t(n0) * k;
   i32x16 acc[T::kMT][T::kNT];
   if constexpr (kDirect) {
@@ -504,19 +519,26 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   for (int i = 0; i < 4; i++)
     scale[i] = load_float(a.down.scale, a.down.scale_dtype,
                           uint64_t(e) * a.hidden + min(nw + lane % (kCols / 4) * 4 + i, a.hidden - 1));
+  if (threadIdx.x < kBM) {
+    scales[threadIdx.x] = row_scale;
+    slots[threadIdx.x] = first + threadIdx.x < last ? row_slot : a.slots;
+  }
+  __syncthreads();
+  // no branches: rows and columns past the last go to a row of their own
+  const uint32_t column = nw + lane % (kCols / 4) * 4, pitch = pitch_of(a.hidden);
+  const bool inside = column < a.hidden;
 #pragma unroll
   for (int b = 0; b < T::kMT; b++)
     T::template rows_out<kCols>(
         lds, [&](int c, int i) { return float(acc[b][c][i]); },
-        [&](uint32_t row, uint32_t col, auto get) {
-          const uint32_t place = mw + b * 32 + row, n = nw + col;
-          if (place >= last || n >= a.hidden) return;
-          const float hs = global<const float>(a.hscale)[place];
+        [&](uint32_t r, uint32_t, auto get) {
+          const uint32_t row = mw - first + b * 32 + r;
+          const float hs = scales[row];
           f32x4 v = get(0);
 #pragma unroll
           for (int i = 0; i < 4; i++) v[i] = v[i] * hs * scale[i];
-          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) + uint64_t(slot_at(a, place)) *
-                                               pitch_of(a.hidden) + n) = v;
+          const uint64_t at = inside ? uint64_t(slots[row]) * pitch + column : uint64_t(a.slots) * pitch;
+          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) + at) = v;
         });
 }
 
@@ -554,8 +576,8 @@ Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
   };
   w.xq = take(tokens * WC_I8_ROW_BYTES(hidden));
   w.xscale = take(tokens * 4);
-  // h, and after its quantisation the experts' results
-  w.wide = take(tokens * k * pitch_of(uint32_t(hidden > ffn ? hidden : ffn)) * 4);
+  // h, and after its quantisation the experts' results and a row for what is past them
+  w.wide = take((tokens * k + 1) * pitch_of(uint32_t(hidden > ffn ? hidden : ffn)) * 4);
   w.hq = take(tokens * k * WC_I8_ROW_BYTES(ffn));
   w.hscale = take(tokens * k * 4);
   w.bytes = at;

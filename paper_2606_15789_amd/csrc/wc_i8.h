@@ -40,12 +40,15 @@ __device__ __forceinline__ float fp16_to_float(uint32_t h) {
 }
 // to nearest, ties to even; a NaN stays one
 __device__ __forceinline__ uint32_t float_to_bf16(float f) {
-  const uint32_t b = __float_as_uint(f);
-  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return (b >> 16) | 0x40u;
-  return (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
+  return __builtin_bit_cast(uint16_t, __bf16(f));
 }
 __device__ __forceinline__ uint32_t float_to_fp16(float f) {
   return __builtin_bit_cast(uint16_t, _Float16(f));
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t floats_to_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
 
 // element i of the elements of type dt at address p

@@ -92,7 +92,7 @@ struct MatJob {
   uint64_t part;      // where k is split: its int32 sums, split by split
   uint32_t n, tile0;  // tile0: its first workgroup
   int32_t scale_dtype, bias_dtype, y_dtype;
-  uint32_t quads;     // four neighbours of y can be stored at once
+  uint32_t quads;     // y's columns are whole aligned groups of four
 };
 struct MatArgs {
   uint64_t q, qscale;
@@ -221,11 +221,12 @@ __device__ __forceinline__ void finish(const MatJob& J, uint32_t m, uint32_t n, 
     if (J.y_dtype == WC_FP32) {
       *reinterpret_cast<global_ptr<f32x4>>(global<float>(J.y) + at) = v;
     } else {
-      uint32_t h[4];
-#pragma unroll
-      for (int i = 0; i < 4; i++) h[i] = J.y_dtype == WC_BF16 ? float_to_bf16(v[i]) : float_to_fp16(v[i]);
-      *reinterpret_cast<global_ptr<u32x2>>(global<uint16_t>(J.y) + at) =
-          u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+      u32x2 h;
+      if (J.y_dtype == WC_BF16)
+        h = {floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])};
+      else
+        h = {float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16, float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16};
+      *reinterpret_cast<global_ptr<u32x2>>(global<uint16_t>(J.y) + at) = h;
     }
   } else {
 #pragma unroll
@@ -243,11 +244,46 @@ __device__ __forceinline__ void column_scales(const MatJob& J, uint32_t n, float
   }
 }
 
+// A wave's results to rows of type kType (0: the int32 sums), where the columns fill whole
+// groups of four: without a branch, so that the reads from LDS and the stores of all rows
+// overlap.  What is past the last row or column goes nowhere.
+template <class T, int kType>
+__device__ __forceinline__ void tile_out(uint8_t* lds, const i32x16 (&acc)[T::kMT][T::kNT], u32x4 to,
+                                         uint32_t pitch, uint32_t row0, uint32_t column, bool inside,
+                                         const float* scales, const float (&scale)[4],
+                                         const float (&bias)[4]) {
+  constexpr uint32_t kSize = kType == 0 || kType == WC_FP32 ? 4 : 2;
+  const uint32_t lane = inside ? column * kSize : kNowhere;
+#pragma unroll
+  for (int b = 0; b < T::kMT; b++)
+    T::template rows_out<T::kNT * 32>(
+        lds,
+        [&](int c, int i) { return kType ? float(acc[b][c][i]) : __int_as_float(acc[b][c][i]); },
+        [&](uint32_t r, uint32_t, auto get) {
+          const uint32_t row = row0 + b * 32 + r;
+          f32x4 v = get(0);
+          if constexpr (kType != 0) {
+            const float xs = scales[row];
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] = v[i] * xs * scale[i] + bias[i];
+          }
+          const uint32_t at = lane + row * pitch;
+          if constexpr (kSize == 4)
+            store_rows(to, at, __builtin_bit_cast(u32x4, v));
+          else if constexpr (kType == WC_BF16)
+            store_rows(to, at, u32x2{floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])});
+          else
+            store_rows(to, at, u32x2{float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16,
+                                     float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16});
+        });
+}
+
 // One tile of a job (and one part of k) a workgroup.
 template <class T, bool kDirect>
 __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
-  constexpr uint32_t kBM = T::kMT * 32 * T::kWM_, kBN = T::kNT * 32 * T::kWN_;
+  __shared__ float scales[T::kRows];  // of the tile's rows of x
+  constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
   uint32_t j = 0;
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
   const MatJob J = a.job[j];
@@ -266,6 +302,8 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   for (int i = 0; i < T::kXLoads; i++)
     xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
   const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
+  // a load among the stores at the end would wait for all stores before it
+  const float row_scale = global<const float>(a.qscale)[m0 + min(threadIdx.x, m_rows - 1)];
   i32x16 acc[T::kMT][T::kNT];
   if constexpr (kDirect) {
     const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw + k0, uint32_t((n_rows - 1) * J.ldw + a.k - k0));
@@ -290,27 +328,33 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   const uint32_t nw = n0 + wave % T::kWN_ * kCols, mw = m0 + wave / T::kWN_ * (T::kMT * 32);
   float scale[4], bias[4];
   if (a.splits == 1) column_scales(J, nw + lane % (kCols / 4) * 4, scale, bias);
-#pragma unroll
-  for (int b = 0; b < T::kMT; b++) {
-    if (a.splits == 1) {
-      T::template rows_out<kCols>(
-          lds, [&](int c, int i) { return float(acc[b][c][i]); },
-          [&](uint32_t row, uint32_t col, auto get) {
-            const uint32_t m = mw + b * 32 + row, n = nw + col;
-            if (m < a.m && n < J.n) finish(J, m, n, get(0), global<const float>(a.qscale)[m], scale, bias);
-          });
-    } else {
-      T::template rows_out<kCols>(
-          lds, [&](int c, int i) { return __int_as_float(acc[b][c][i]); },
-          [&](uint32_t row, uint32_t col, auto get) {
-            const uint32_t m = mw + b * 32 + row, n = nw + col;
-            if (m >= a.m || n >= J.n) return;
-            const uint64_t pitch = (J.n + 3u) & ~3u;
-            *reinterpret_cast<global_ptr<f32x4>>(global<float>(J.part) +
-                                                 (uint64_t(part) * a.m + m) * pitch + n) = get(0);
-          });
-    }
+  if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
+  __syncthreads();
+  const uint32_t row0 = mw - m0, column = nw - n0 + lane % (kCols / 4) * 4;
+  const bool inside = n0 + column < J.n;
+  if (a.splits > 1) {
+    const uint64_t pitch = ((J.n + 3u) & ~3u) * 4;
+    const u32x4 to = rows_rsrc(J.part + (uint64_t(part) * a.m + m0) * pitch + n0 * 4ull,
+                               uint32_t(m_rows * pitch - n0 * 4ull));
+    return tile_out<T, 0>(lds, acc, to, uint32_t(pitch), row0, column, inside, scales, scale, bias);
   }
+  if (J.quads) {
+    const uint32_t size = J.y_dtype == WC_FP32 ? 4 : 2, pitch = uint32_t(J.ldy) * size;
+    const u32x4 to = rows_rsrc(J.y + (m0 * J.ldy + n0) * size, (m_rows - 1) * pitch + n_rows * size);
+    if (J.y_dtype == WC_BF16)
+      return tile_out<T, WC_BF16>(lds, acc, to, pitch, row0, column, inside, scales, scale, bias);
+    if (J.y_dtype == WC_FP16)
+      return tile_out<T, WC_FP16>(lds, acc, to, pitch, row0, column, inside, scales, scale, bias);
+    return tile_out<T, WC_FP32>(lds, acc, to, pitch, row0, column, inside, scales, scale, bias);
+  }
+#pragma unroll
+  for (int b = 0; b < T::kMT; b++)
+    T::template rows_out<kCols>(
+        lds, [&](int c, int i) { return float(acc[b][c][i]); },
+        [&](uint32_t row, uint32_t col, auto get) {
+          const uint32_t m = mw + b * 32 + row, n = nw + col;
+          if (m < a.m && n < J.n) finish(J, m, n, get(0), scales[m - m0], scale, bias);
+        });
 }
 
 // y from the sums of the parts of k.
@@ -367,7 +411,7 @@ using Tile64 = Tile<64, 128, 1, 4, 3>;
 using Tile32 = Tile<32, 128, 1, 4, 4>;
 #ifdef WC_TUNE
 using TileA = Tile<128, 128, 2, 2, 3>;
-using TileB = Tile<256, 256, 2, 4, 5, 64>;
+using TileB = Tile<256, 256, 2, 4, 3, 64>;
 using TileC = Tile<256, 256, 2, 4, 4, 64>;
 using TileD = Tile<128, 128, 2, 4, 4>;
 using TileE = Tile<64, 128, 1, 4, 4>;
@@ -496,7 +540,8 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     a.job[i] = {reinterpret_cast<uint64_t>(J.w),    reinterpret_cast<uint64_t>(J.scale),
                 reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
                 J.ldw, J.ldy, part, J.n, tiles, J.scale_dtype, J.bias_dtype, J.y_dtype,
-                J.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0};
+                J.n % 4 == 0 && J.ldy % 4 == 0 && J.ldy < (1u << 20) &&
+                    reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0};
     if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
     tiles += tiles_of(p.kernel, m, J.n);

@@ -32,6 +32,17 @@ __device__ __forceinline__ void load_lds(u32x4 rs, uint32_t lds, uint32_t offset
                : "memory");
 }
 
+// 8 or 16 bytes to rs + offset; nothing where that is past the buffer's end.
+__device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, u32x2 v) {
+  __builtin_amdgcn_raw_buffer_store_b64(v, __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<void*>(uint64_t(rs[1]) << 32 | rs[0]), (short)0, (int)rs[2], (int)rs[3]), offset, 0, 0);
+}
+__device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, u32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<void*>(uint64_t(rs[1]) << 32 | rs[0]), (short)0, (int)rs[2], (int)rs[3]), offset, 0, 0);
+}
+constexpr uint32_t kNowhere = 0x80000000u;  // an offset past the end of every buffer here
+
 // kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages of kK bytes in LDS.
 template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2, int kK = 128>
 struct Tile {
