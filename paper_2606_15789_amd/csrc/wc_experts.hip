@@ -64,6 +64,20 @@ __device__ __forceinline__ bool tile_of(const ExpertArgs& a, uint32_t tile, uint
   return false;
 }
 
+// How many blocks of kRows places the experts' rows fill.
+template <int kRows>
+__device__ __forceinline__ uint32_t tile_count(const ExpertArgs& a) {
+  uint32_t blocks = 0;
+  for (uint32_t e = threadIdx.x % 64; e < a.experts; e += 64) {
+    const uint32_t from = min(uint32_t(max(global<const int32_t>(a.offsets)[e], 0)), a.slots);
+    const uint32_t to = min(uint32_t(max(global<const int32_t>(a.offsets)[e + 1], 0)), a.slots);
+    blocks += to > from ? (to - from + kRows - 1) / kRows : 0;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) blocks += uint32_t(__shfl_xor(int(blocks), d));
+  return min(uint32_t(__builtin_amdgcn_readfirstlane(blocks)), a.blocks);
+}
+
 __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place) {
   return min(uint32_t(max(global<const int32_t>(a.order)[place], 0)), a.slots - 1);
 }
@@ -390,7 +404,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
   static_assert(T::kNT == 2 && T::kRows <= T::kThreads);
   constexpr uint32_t kBM = T::kRows, kCols = T::kWN_ * 32;
   uint32_t mt, nt, e, first, last;
-  tile_at(blockIdx.x, a.blocks, (a.ffn + kCols - 1) / kCols, mt, nt);
+  if (!tile_at(blockIdx.x, tile_count<kBM>(a), (a.ffn + kCols - 1) / kCols, mt, nt)) return;
   if (!tile_of<kBM>(a, mt, e, first, last)) return;
   e = __builtin_amdgcn_readfirstlane(e);
   const uint32_t n0 = nt * kCols, k = a.hidden, row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
@@ -417,7 +431,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
       wr[i] = rows_rsrc(T::first_row(i) & 32 ? up : gate, n_rows * k);
       woff[i] = min(r / 64 * 32 + r % 32, n_rows - 1) * k + T::byte_of();
     }
-    T::product(lds, row_bytes / T::kBytes, load_x, [&](int i, uint32_t s, uint32_t to) {
+    T::product(lds, row_bytes / T::kBytes, last - first, load_x, [&](int i, uint32_t s, uint32_t to) {
       load_lds(wr[i], to, woff[i] + s * T::kBytes);
     }, acc);
   } else {
@@ -429,7 +443,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
              uint64_t(min(r / 64 * 32 + r % 32, n_rows - 1)) * k + T::byte_of();
     }
     const int32_t left = int32_t(k) - int32_t(T::byte_of());
-    T::product(lds, row_bytes / T::kBytes, load_x, [&](int i, uint32_t s, uint32_t) {
+    T::product(lds, row_bytes / T::kBytes, last - first, load_x, [&](int i, uint32_t s, uint32_t) {
       return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
     }, acc);
   }
@@ -474,7 +488,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   static_assert(T::kRows <= T::kThreads);
   constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
   uint32_t mt, nt, e, first, last;
-  tile_at(blockIdx.x, a.blocks, (a.hidden + kBN - 1) / kBN, mt, nt);
+  if (!tile_at(blockIdx.x, tile_count<kBM>(a), (a.hidden + kBN - 1) / kBN, mt, nt)) return;
   if (!tile_of<kBM>(a, mt, e, first, last)) return;
   e = __builtin_amdgcn_readfirstlane(e);
   first = __builtin_amdgcn_readfirstlane(first);
@@ -499,7 +513,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
 #pragma unroll
     for (int i = 0; i < T::kWLoads; i++)
       woff[i] = min(T::row_of(i), n_rows - 1) * k + T::byte_of();
-    T::product(lds, row_bytes / T::kBytes, load_x,
+    T::product(lds, row_bytes / T::kBytes, last - first, load_x,
                [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
   } else {
     global_ptr<const uint8_t> w[T::kWLoads];
@@ -507,7 +521,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
     for (int i = 0; i < T::kWLoads; i++)
       w[i] = global<const uint8_t>(down) + uint64_t(min(T::row_of(i), n_rows - 1)) * k + T::byte_of();
     const int32_t left = int32_t(k) - int32_t(T::byte_of());
-    T::product(lds, row_bytes / T::kBytes, load_x, [&](int i, uint32_t s, uint32_t) {
+    T::product(lds, row_bytes / T::kBytes, last - first, load_x, [&](int i, uint32_t s, uint32_t) {
       return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
     }, acc);
   }
@@ -596,8 +610,9 @@ Bank bank(const wc_i8_experts* b) {
           b->scale_dtype};
 }
 
-bool aligned16(const wc_i8_experts* b) {
-  return reinterpret_cast<uintptr_t>(b->w) % 16 == 0 && b->stride % 16 == 0;
+// loads to LDS take whole dwords
+bool aligned4(const wc_i8_experts* b) {
+  return reinterpret_cast<uintptr_t>(b->w) % 4 == 0 && b->stride % 4 == 0;
 }
 
 // Slot by slot, while that reads no expert's rows twice much (E = 64, k = 6, 2048 x 1408):
@@ -693,11 +708,10 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   a.gate = bank(gate);
   a.up = bank(up);
   a.down = bank(down);
-  const bool direct = hidden % 16 == 0 && ffn % 16 == 0 && aligned16(gate) && aligned16(up) &&
-                      aligned16(down);
+  const bool direct = hidden % 4 == 0 && ffn % 4 == 0 && aligned4(gate) && aligned4(up) && aligned4(down);
   const uint64_t hold_x = WC_I8_ROW_BYTES(hidden), hold_h = k * WC_I8_ROW_BYTES(ffn);
   const bool vector = reinterpret_cast<uintptr_t>(dev_x) % 16 == 0 && ldx * size_of(dtype) % 16 == 0;
-  if (direct && vector && tokens <= kSlotTokens && slots <= experts && k <= kSlots && hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
+  if (direct && vector && hidden % 8 == 0 && tokens <= kSlotTokens && slots <= experts && ffn % 8 == 0 && k <= kSlots && hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
     const dim3 grid((ffn + 7) / 8, slots), block(SlotRing::kThreads);
     const uint32_t held = SlotRing::kLds + uint32_t(hold_x);
     if (dtype == WC_BF16)

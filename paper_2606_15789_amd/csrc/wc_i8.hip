@@ -1,4 +1,7 @@
 // wc_i8.hip -- int8 linear layers: wc_quantize_i8, wc_matmul_i8, wc_linear_i8.
+#include <algorithm>
+#include <cmath>
+
 #include "wc_i8_ring.h"
 
 namespace {
@@ -288,7 +291,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
   const MatJob J = a.job[j];
   uint32_t mt, nt;
-  tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt);
+  if (!tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt)) return;
   const uint32_t m0 = mt * kBM, n0 = nt * kBN;
   const uint32_t m_rows = min(kBM, a.m - m0), n_rows = min(kBN, J.n - n0);
   const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k)), all = row_bytes / T::kBytes;
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
 #pragma unroll
     for (int i = 0; i < T::kWLoads; i++)
       woff[i] = min(T::row_of(i), n_rows - 1) * uint32_t(J.ldw) + T::byte_of();
-    T::product(lds, stages, load_x,
+    T::product(lds, stages, m_rows, load_x,
                [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
   } else {
     global_ptr<const uint8_t> w[T::kWLoads];
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
     for (int i = 0; i < T::kWLoads; i++)
       w[i] = global<const uint8_t>(J.w) + (n0 + min(T::row_of(i), n_rows - 1)) * J.ldw + k0 + T::byte_of();
     const int32_t left = int32_t(a.k - k0) - int32_t(T::byte_of());
-    T::product(lds, stages, load_x, [&](int i, uint32_t s, uint32_t) {
+    T::product(lds, stages, m_rows, load_x, [&](int i, uint32_t s, uint32_t) {
       return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
     }, acc);
   }
@@ -405,20 +408,11 @@ bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx) {
          (m == 0 || (x && reinterpret_cast<uintptr_t>(x) % size_of(dt) == 0));
 }
 
+using Tile64 = Tile<64, 64, 1, 2, 4>;
+using Tile64Wide = Tile<64, 128, 1, 4, 4>;
+using Tile128 = Tile<128, 128, 2, 2, 3>;
+using Tile256Half = Tile<256, 128, 4, 2, 3>;
 using Tile256 = Tile<256, 256, 2, 4>;
-using Tile128 = Tile<128, 128, 2, 2>;
-using Tile64 = Tile<64, 128, 1, 4, 3>;
-using Tile32 = Tile<32, 128, 1, 4, 4>;
-#ifdef WC_TUNE
-using TileA = Tile<128, 128, 2, 2, 3>;
-using TileB = Tile<256, 256, 2, 4, 3, 64>;
-using TileC = Tile<256, 256, 2, 4, 4, 64>;
-using TileD = Tile<128, 128, 2, 4, 4>;
-using TileE = Tile<64, 128, 1, 4, 4>;
-using TileF = Tile<64, 64, 1, 2, 4>;
-using TileG = Tile<256, 128, 4, 2, 3>;
-using TileH = Tile<256, 128, 4, 2, 6, 64>;
-#endif
 
 // Quantising in the product's own launch saves a launch (2 us, 4 on the host) and costs
 // every workgroup the row: linear at m = 1, k = 4096, n = 6144 9.7 us against 11.2,
@@ -428,11 +422,7 @@ using TileH = Tile<256, 128, 4, 2, 6, 64>;
 constexpr uint64_t kHoldAlways = 4096, kHoldSmall = 8192, kHoldSmallWeights = 32u << 20;
 
 // Which kernel multiplies m rows, and in how many parts of k.
-enum class Kernel { kRows, kRing, kTile32, kTile64, kTile128, kTile256
-#ifdef WC_TUNE
-, kA, kB, kC, kD, kE, kF, kG, kH
-#endif
-};
+enum class Kernel { kRows, kRing, kTile64, kTile64Wide, kTile128, kTile256Half, kTile256 };
 struct Plan {
   Kernel kernel;
   bool direct;      // every W can go to LDS as it is
@@ -440,69 +430,15 @@ struct Plan {
   uint32_t splits;
   uint64_t part_bytes;
 };
-}  // namespace
-#ifdef WC_TUNE
-#include <cstdlib>
-#include <cstdio>
-#endif
-namespace {
-Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
-  Plan p{Kernel::kRows, true, false, 1, 0};
-  uint64_t tiles128 = 0, tiles256 = 0, sums = 0, weights = 0;
-  for (uint32_t i = 0; i < n_jobs; i++) {
-    const wc_i8_job& J = jobs[i];
-    weights += uint64_t(J.n) * k;
-    // offsets within a tile's rows are 32-bit
-    if (J.ldw > (1u << 22)) return p;
-    p.direct = p.direct && k % 4 == 0 && J.ldw % 16 == 0 && reinterpret_cast<uintptr_t>(J.w) % 16 == 0;
-    tiles128 += uint64_t(m + 127) / 128 * ((J.n + 127) / 128);
-    tiles256 += uint64_t(m + 255) / 256 * ((J.n + 255) / 256);
-    sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
-  }
-#ifdef WC_TUNE
-  if (const char* e = getenv("WC_PLAN")) {
-    int kn = 0, sp = 1;
-    if (sscanf(e, "%d,%d", &kn, &sp) == 2) {
-      p.kernel = Kernel(kn); p.splits = sp; if (sp > 1) p.part_bytes = sums * sp; return p;
-    }
-  }
-#endif
-  if (m <= 16) {
-    if (p.direct) p.kernel = Kernel::kRing;
-    const uint64_t held = m * WC_I8_ROW_BYTES(k);
-    p.hold = p.direct && k % 8 == 0 &&
-             (held <= kHoldAlways || (held <= kHoldSmall && weights <= kHoldSmallWeights));
-    return p;
-  }
-  if (m <= 64) return p;
-  if (tiles128 > 0x7FFFFFFFu) return p;
-  p.kernel = tiles256 >= 192 ? Kernel::kTile256 : Kernel::kTile128;
-  const uint64_t tiles = p.kernel == Kernel::kTile256 ? tiles256 : tiles128;
-  const uint32_t stages = (k + kStage - 1) / kStage;
-  const uint64_t slots = p.kernel == Kernel::kTile256 ? 256 : 512;
-  while (tiles * p.splits * 2 <= slots && stages >= p.splits * 2 * 8) p.splits *= 2;
-  if (p.splits > 1) p.part_bytes = sums * p.splits;
-  return p;
-}
-
 // f(Tile) for the kernel's tile.
 template <class F>
 void with_tile(Kernel kernel, F f) {
   switch (kernel) {
-    case Kernel::kTile32: return f(Tile32{});
     case Kernel::kTile64: return f(Tile64{});
+    case Kernel::kTile64Wide: return f(Tile64Wide{});
     case Kernel::kTile128: return f(Tile128{});
+    case Kernel::kTile256Half: return f(Tile256Half{});
     case Kernel::kTile256: return f(Tile256{});
-#ifdef WC_TUNE
-    case Kernel::kA: return f(TileA{});
-    case Kernel::kB: return f(TileB{});
-    case Kernel::kC: return f(TileC{});
-    case Kernel::kD: return f(TileD{});
-    case Kernel::kE: return f(TileE{});
-    case Kernel::kF: return f(TileF{});
-    case Kernel::kG: return f(TileG{});
-    case Kernel::kH: return f(TileH{});
-#endif
     default: return;
   }
 }
@@ -512,6 +448,69 @@ uint32_t tiles_of(Kernel kernel, uint32_t m, uint32_t n) {
     tiles = (m + t.kRows - 1) / t.kRows * ((n + t.kCols - 1) / t.kCols);
   });
   return tiles;
+}
+
+// What a tile's kernel takes, in us, as measured on whole rounds of workgroups (256 of
+// them, or 512 where two fit a compute unit): a stage of 128 bytes of k, one workgroup's
+// and two's, and all else of a round.  m = 1000, k = n = 8192 (256 tiles of 256 x 128)
+// comes to 64.5 and measured 64.5, on 512 tiles of 128 x 128 86 and 83, 128 of 256 x 256
+// 109 and 96; m = 512, k = 28672, n = 8192 in two parts of 256 x 128 128 and 124, four of
+// 256 x 256 134 and 132; m = 333, k = n = 8192 on 128 x 128 43 and 39; m = 32, k = n =
+// 4096 on 64 x 64 13.3 and 13.2, in four parts 12.1 and 12.2.
+struct TileCost {
+  Kernel kernel;
+  double stage, stage_of_two, round;
+};
+constexpr TileCost kCosts[] = {{Kernel::kTile64, 0.26, 0.34, 5.0},
+                               {Kernel::kTile64Wide, 0.36, 0.0, 4.8},
+                               {Kernel::kTile128, 0.60, 0.0, 4.5},
+                               {Kernel::kTile256Half, 0.90, 0.0, 6.9},
+                               {Kernel::kTile256, 1.55, 0.0, 10.2}};
+constexpr double kUnits = 256, kJoin = 4.0, kBytesPerUs = 4e6, kReadPerUs = 5e6;
+
+Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
+  Plan p{Kernel::kRows, true, false, 1, 0};
+  uint64_t sums = 0, weights = 0, tiles64 = 0;
+  for (uint32_t i = 0; i < n_jobs; i++) {
+    const wc_i8_job& J = jobs[i];
+    weights += uint64_t(J.n) * k;
+    // offsets within a tile's rows are 32-bit
+    if (J.ldw > (1u << 22)) return p;
+    // loads to LDS take whole dwords
+    p.direct = p.direct && k % 4 == 0 && J.ldw % 4 == 0 && reinterpret_cast<uintptr_t>(J.w) % 4 == 0;
+    tiles64 += uint64_t(m + 63) / 64 * ((J.n + 63) / 64);
+    sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
+  }
+  if (m <= 16) {
+    if (p.direct) p.kernel = Kernel::kRing;
+    const uint64_t held = m * WC_I8_ROW_BYTES(k);
+    p.hold = p.direct && k % 8 == 0 &&
+             (held <= kHoldAlways || (held <= kHoldSmall && weights <= kHoldSmallWeights));
+    return p;
+  }
+  if (tiles64 > 0x7FFFFFFFu) return p;
+  const uint32_t stages = (k + kStage - 1) / kStage;
+  double best = 0;
+  for (const TileCost& c : kCosts) {
+    double tiles = 0;
+    for (uint32_t i = 0; i < n_jobs; i++) tiles += tiles_of(c.kernel, m, jobs[i].n);
+    for (uint32_t splits : {1u, 2u, 3u, 4u, 6u, 8u}) {
+      if (splits > 1 && stages < 4 * splits) break;
+      const double groups = tiles * splits;
+      const bool two = c.stage_of_two > 0 && groups > kUnits;
+      const double rounds = std::ceil(groups / (two ? 2 * kUnits : kUnits));
+      double us = rounds * (c.round + (stages + splits - 1) / splits * (two ? c.stage_of_two : c.stage));
+      us = std::max(us, double(weights) / kReadPerUs);
+      if (splits > 1) us += kJoin + 2.0 * double(sums) * splits / kBytesPerUs;
+      if (best == 0 || us < best) {
+        best = us;
+        p.kernel = c.kernel;
+        p.splits = splits;
+      }
+    }
+  }
+  if (p.splits > 1) p.part_bytes = sums * p.splits;
+  return p;
 }
 
 template <int kX, int kType = 0>

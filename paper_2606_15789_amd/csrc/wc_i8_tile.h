@@ -78,9 +78,12 @@ struct Tile {
   // `load_x(i, stage, lds)` and `load_w(i, stage, lds)` start load i of a stage's rows
   // of x and W.  A W whose rows cannot go to LDS as they are comes through registers:
   // load_w then gives load i's 16 bytes, which are stored after the products.
+  // Waves all of whose rows of x are past the first `rows` only load: the other wave of
+  // their SIMD has the matrix unit to itself.
   template <class LoadX, class LoadW>
-  static __device__ __forceinline__ void product(uint8_t* lds, uint32_t stages, LoadX load_x,
-                                                 LoadW load_w, i32x16 (&acc)[kMT][kNT]) {
+  static __device__ __forceinline__ void product(uint8_t* lds, uint32_t stages, uint32_t rows,
+                                                 LoadX load_x, LoadW load_w,
+                                                 i32x16 (&acc)[kMT][kNT]) {
     constexpr bool kDirect = __is_same(decltype(load_w(0, 0u, 0u)), void);
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t wm = wave / kWN, wn = wave % kWN;
@@ -165,6 +168,24 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kMT + kNT; i++) read(0, lds, 0, i);
     uint32_t slot = 0, fill = kAhead;  // the stage's place, and that of the one it loads
+    if (__builtin_amdgcn_readfirstlane(wm) * (kBM / kWM) >= rows) {
+      for (uint32_t s = 0; s < stages; s++) {
+#pragma unroll
+        for (int i = kHalf; i < kAll; i++) start(i, s + kAhead, fill);
+        keep(fill);
+        arrive<kDirect ? int(kAhead) - 1 : 0>();
+        fill = slot;
+        slot = slot + 1 < kSlots ? slot + 1 : 0;
+        if constexpr (!kDirect) {
+          if (s + 2 < stages) hold(s + 2);
+        }
+#pragma unroll
+        for (int i = 0; i < kHalf; i++) start(i, s + 1 + kAhead, fill);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      return;
+    }
     for (uint32_t s = 0; s < stages; s++) {
       quarter(0, slot, 1, s + kAhead, fill, Second{});
 #pragma unroll
@@ -224,17 +245,20 @@ struct Tile {
 // Which tile a workgroup takes, so that those that run at once on one of the eight
 // dies (workgroup i goes to die i mod 8, each with its own L2) share rows: each die
 // takes a run of the tiles, ordered in bands of kBand tiles of x rows, W tile by W
-// tile within a band.
-__device__ __forceinline__ void tile_at(uint32_t id, uint32_t m_tiles, uint32_t n_tiles,
+// tile within a band.  The tiles may be fewer than the workgroups (false for those
+// without one): the dies' shares are still even.
+__device__ __forceinline__ bool tile_at(uint32_t id, uint32_t m_tiles, uint32_t n_tiles,
                                         uint32_t& m, uint32_t& n) {
   constexpr uint32_t kDies = 8, kBand = 8;
   const uint32_t all = m_tiles * n_tiles, each = all / kDies, rest = all % kDies;
   const uint32_t die = id % kDies;
+  if (id / kDies >= each + (die < rest)) return false;
   const uint32_t t = die * each + min(die, rest) + id / kDies;
   const uint32_t band = t / (kBand * n_tiles), first = band * kBand;
   const uint32_t high = min(kBand, m_tiles - first), in = t - first * n_tiles;
   m = first + in % high;
   n = in / high;
+  return true;
 }
 
 }  // namespace wc_i8
