@@ -21,6 +21,7 @@ struct ExpertArgs {
   uint64_t xq, xscale;    // quantised x, by token
   uint64_t h;             // fp32, by place in the order
   uint64_t hq, hscale;    // quantised h
+  uint64_t xcopies, hcopies;  // both shifted, where rows of the matrices need it
   uint64_t out;           // experts' results, fp32, by slot
   uint64_t y, ldy;
   uint32_t tokens, k, experts, hidden, ffn, slots;
@@ -181,29 +182,34 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_k
   uint32_t e, first, last;
   if (!tile_of<kX>(a, blockIdx.x, e, first, last)) return;
   e = __builtin_amdgcn_readfirstlane(e);
-  const uint32_t n0 = blockIdx.y * 8, n_rows = min(8u, a.ffn - n0), k = a.hidden;
-  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
-  const u32x4 gr = rows_rsrc(a.gate.w + e * a.gate.stride + uint64_t(n0) * k, n_rows * k);
-  const u32x4 ur = rows_rsrc(a.up.w + e * a.up.stride + uint64_t(n0) * k, n_rows * k);
-  const u32x4 xr = rows_rsrc(a.xq, uint32_t(a.tokens * uint64_t(row_bytes)));
-  const uint32_t woff = min(R::row_of(), n_rows - 1) * k + R::byte_of();
+  const uint32_t k = a.hidden, step = steps_of(k), blocks = ((a.ffn + step - 1) / step + 7) / 8;
+  const uint32_t class0 = blockIdx.y / blocks, r0 = blockIdx.y % blocks * 8;
+  const ClassRows G = class_rows(a.gate.w + e * a.gate.stride, k, a.ffn, k, step, class0);
+  const ClassRows U = class_rows(a.up.w + e * a.up.stride, k, a.ffn, k, step, class0);
+  if (r0 >= G.rows) return;
+  const uint32_t n_rows = min(8u, G.rows - r0);
+  const Shifted X = shifted(a.xq, a.xcopies, a.tokens, k, G.shift);
+  const u32x4 gr = rows_rsrc(G.base + r0 * uint64_t(G.pitch), (n_rows - 1) * G.pitch + G.bytes);
+  const u32x4 ur = rows_rsrc(U.base + r0 * uint64_t(G.pitch), (n_rows - 1) * G.pitch + G.bytes);
+  const u32x4 xr = rows_rsrc(X.base, a.tokens * X.pitch);
+  const uint32_t woff = min(R::row_of(), n_rows - 1) * G.pitch + R::byte_of();
   uint32_t xoff[kX / 8];
 #pragma unroll
   for (int i = 0; i < kX / 8; i++)
-    xoff[i] = slot_at(a, min(first + 8 * i + R::row_of(), last - 1)) / a.k * row_bytes + R::byte_of();
+    xoff[i] = slot_at(a, min(first + 8 * i + R::row_of(), last - 1)) / a.k * X.pitch + R::byte_of();
   i32x4 acc[1];
-  R::product(lds, row_bytes / kStage,
+  R::product(lds, (G.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
              [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff + at); }, acc,
              [] { return typename R::Held{}; });
   R::gather(lds, acc);
   for (uint32_t o = threadIdx.x; o < 8 * kX; o += R::kThreads) {
-    const uint32_t n = n0 + o % 8, place = first + o / 8;
-    if (n >= a.ffn || place >= last) continue;
+    const uint32_t r = o % 8, n = class0 + (r0 + r) * step, place = first + o / 8;
+    if (r >= n_rows || place >= last) continue;
     const float xs = global<const float>(a.xscale)[slot_at(a, place) / a.k];
     const uint64_t at = uint64_t(e) * a.ffn + n;
-    const float g = float(R::sum(lds, o % 8, o / 8)) * xs * load_float(a.gate.scale, a.gate.scale_dtype, at);
-    const float u = float(R::sum(lds, 8 + o % 8, o / 8)) * xs * load_float(a.up.scale, a.up.scale_dtype, at);
+    const float g = float(R::sum(lds, r, o / 8)) * xs * load_float(a.gate.scale, a.gate.scale_dtype, at);
+    const float u = float(R::sum(lds, 8 + r, o / 8)) * xs * load_float(a.up.scale, a.up.scale_dtype, at);
     global<float>(a.h)[uint64_t(place) * pitch_of(a.ffn) + n] = g / (1.0f + expf(-g)) * u;
   }
 }
@@ -217,26 +223,30 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring
   e = __builtin_amdgcn_readfirstlane(e);
   first = __builtin_amdgcn_readfirstlane(first);
   last = __builtin_amdgcn_readfirstlane(last);
-  const uint32_t n0 = blockIdx.y * 16, n_rows = min(16u, a.hidden - n0), k = a.ffn;
-  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(k)), m_rows = last - first;
-  const u32x4 wr = rows_rsrc(a.down.w + e * a.down.stride + uint64_t(n0) * k, n_rows * k);
-  const u32x4 xr = rows_rsrc(a.hq + uint64_t(first) * row_bytes, m_rows * row_bytes);
+  const uint32_t k = a.ffn, step = steps_of(k), blocks = ((a.hidden + step - 1) / step + 15) / 16;
+  const uint32_t class0 = blockIdx.y / blocks, r0 = blockIdx.y % blocks * 16;
+  const ClassRows C = class_rows(a.down.w + e * a.down.stride, k, a.hidden, k, step, class0);
+  if (r0 >= C.rows) return;
+  const uint32_t n_rows = min(16u, C.rows - r0), m_rows = last - first;
+  const Shifted X = shifted(a.hq, a.hcopies, a.slots, k, C.shift);
+  const u32x4 wr = rows_rsrc(C.base + r0 * uint64_t(C.pitch), (n_rows - 1) * C.pitch + C.bytes);
+  const u32x4 xr = rows_rsrc(X.base + uint64_t(first) * X.pitch, m_rows * X.pitch);
   uint32_t woff[2], xoff[kX / 8];
 #pragma unroll
-  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * k + R::byte_of();
+  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of();
 #pragma unroll
-  for (int i = 0; i < kX / 8; i++) xoff[i] = min(8 * i + R::row_of(), m_rows - 1) * row_bytes + R::byte_of();
+  for (int i = 0; i < kX / 8; i++) xoff[i] = min(8 * i + R::row_of(), m_rows - 1) * X.pitch + R::byte_of();
   i32x4 acc[1];
-  R::product(lds, row_bytes / kStage,
+  R::product(lds, (C.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
              [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc,
              [] { return typename R::Held{}; });
   R::gather(lds, acc);
   for (uint32_t o = threadIdx.x; o < 16 * kX; o += R::kThreads) {
-    const uint32_t n = n0 + o % 16, place = first + o / 16;
-    if (n >= a.hidden || place >= last) continue;
+    const uint32_t r = o % 16, n = class0 + (r0 + r) * step, place = first + o / 16;
+    if (r >= n_rows || place >= last) continue;
     global<float>(a.out)[uint64_t(slot_at(a, place)) * pitch_of(a.hidden) + n] =
-        float(R::sum(lds, o % 16, o / 16)) * global<const float>(a.hscale)[place] *
+        float(R::sum(lds, r, o / 16)) * global<const float>(a.hscale)[place] *
         load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
   }
 }
@@ -396,78 +406,73 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
 }
 
 // The same on tiles through LDS.  A wave's columns of W are 32 of gate and the same 32
-// of up, so that both products of a value of h meet in one lane.
-template <class T, bool kDirect>
+// of up, so that both products of a value of h meet in one lane.  kQuads: the tile's
+// columns are neighbours (a class of rows is all of them).
+template <class T, bool kQuads>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];  // of the tile's rows of x
   static_assert(T::kNT == 2 && T::kRows <= T::kThreads);
   constexpr uint32_t kBM = T::kRows, kCols = T::kWN_ * 32;
+  const uint32_t k = a.hidden, step = kQuads ? 1 : steps_of(k);
+  // classes of the same columns one after another, so that their stores meet in a cache
+  const uint32_t blocks = ((a.ffn + step - 1) / step + kCols - 1) / kCols;
   uint32_t mt, nt, e, first, last;
-  if (!tile_at(blockIdx.x, tile_count<kBM>(a), (a.ffn + kCols - 1) / kCols, mt, nt)) return;
+  if (!tile_at(blockIdx.x, tile_count<kBM>(a), blocks * step, mt, nt)) return;
   if (!tile_of<kBM>(a, mt, e, first, last)) return;
   e = __builtin_amdgcn_readfirstlane(e);
-  const uint32_t n0 = nt * kCols, k = a.hidden, row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
-  const uint32_t n_rows = min(kCols, a.ffn - n0), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const u32x4 xr = rows_rsrc(a.xq, uint32_t(a.tokens * uint64_t(row_bytes)));
-  uint32_t xoff[T::kXLoads];
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+  const uint32_t class0 = nt % step, r0 = nt / step * kCols;
+  const ClassRows G = class_rows(a.gate.w + e * a.gate.stride, k, a.ffn, k, step, class0);
+  const ClassRows U = class_rows(a.up.w + e * a.up.stride, k, a.ffn, k, step, class0);
+  if (r0 >= G.rows) return;
+  const uint32_t n_rows = min(kCols, G.rows - r0);
+  const Shifted X = shifted(a.xq, a.xcopies, a.tokens, k, G.shift);
+  const u32x4 xr = rows_rsrc(X.base, a.tokens * X.pitch);
+  uint32_t xoff[T::kXLoads], woff[T::kWLoads];
 #pragma unroll
   for (int i = 0; i < T::kXLoads; i++)
-    xoff[i] = slot_at(a, min(first + T::row_of(i), last - 1)) / a.k * row_bytes + T::byte_of();
-  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
+    xoff[i] = slot_at(a, min(first + T::row_of(i), last - 1)) / a.k * X.pitch + T::byte_of();
   // a load among the stores at the end would wait for all stores before it
   const float row_scale =
       global<const float>(a.xscale)[slot_at(a, min(first + threadIdx.x % kBM, last - 1)) / a.k];
   // W row r of the tile: column r / 64 * 32 + r mod 32 of gate (r mod 64 < 32) or of up
-  const uint64_t gate = a.gate.w + e * a.gate.stride + uint64_t(n0) * k;
-  const uint64_t up = a.up.w + e * a.up.stride + uint64_t(n0) * k;
-  i32x16 acc[T::kMT][2];
-  if constexpr (kDirect) {
-    u32x4 wr[T::kWLoads];
-    uint32_t woff[T::kWLoads];
+  u32x4 wr[T::kWLoads];
 #pragma unroll
-    for (int i = 0; i < T::kWLoads; i++) {
-      const uint32_t r = T::row_of(i);
-      wr[i] = rows_rsrc(T::first_row(i) & 32 ? up : gate, n_rows * k);
-      woff[i] = min(r / 64 * 32 + r % 32, n_rows - 1) * k + T::byte_of();
-    }
-    T::product(lds, row_bytes / T::kBytes, last - first, load_x, [&](int i, uint32_t s, uint32_t to) {
-      load_lds(wr[i], to, woff[i] + s * T::kBytes);
-    }, acc);
-  } else {
-    global_ptr<const uint8_t> w[T::kWLoads];
-#pragma unroll
-    for (int i = 0; i < T::kWLoads; i++) {
-      const uint32_t r = T::row_of(i);
-      w[i] = global<const uint8_t>(T::first_row(i) & 32 ? up : gate) +
-             uint64_t(min(r / 64 * 32 + r % 32, n_rows - 1)) * k + T::byte_of();
-    }
-    const int32_t left = int32_t(k) - int32_t(T::byte_of());
-    T::product(lds, row_bytes / T::kBytes, last - first, load_x, [&](int i, uint32_t s, uint32_t) {
-      return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
-    }, acc);
+  for (int i = 0; i < T::kWLoads; i++) {
+    const uint32_t r = T::row_of(i);
+    wr[i] = rows_rsrc((T::first_row(i) & 32 ? U.base : G.base) + r0 * uint64_t(G.pitch),
+                      (n_rows - 1) * G.pitch + G.bytes);
+    woff[i] = min(r / 64 * 32 + r % 32, n_rows - 1) * G.pitch + T::byte_of();
   }
-  const uint32_t lane = threadIdx.x % 64;
-  const uint32_t nw = n0 + wave % T::kWN_ * 32, mw = first + wave / T::kWN_ * (T::kMT * 32);
+  i32x16 acc[T::kMT][2];
+  T::product(lds, (G.bytes + T::kBytes - 1) / T::kBytes, last - first,
+             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
+             [&](int i, uint32_t s, uint32_t to) { load_lds(wr[i], to, woff[i] + s * T::kBytes); }, acc);
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const uint32_t column = wave % T::kWN_ * 32 + lane % 8 * 4, row0 = wave / T::kWN_ * (T::kMT * 32);
   float gs[4], us[4];
+  uint32_t out[4];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const uint64_t at = uint64_t(e) * a.ffn + min(nw + lane % 8 * 4 + i, a.ffn - 1);
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t n = class0 + (r0 + column + i) * step;
+    const uint64_t at = uint64_t(e) * a.ffn + min(n, a.ffn - 1);
     gs[i] = load_float(a.gate.scale, a.gate.scale_dtype, at);
     us[i] = load_float(a.up.scale, a.up.scale_dtype, at);
+    out[i] = column + (kQuads ? 0 : i) < n_rows ? n * 4 : kNowhere;
   }
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
   __syncthreads();
   // no branches: rows and columns past the last go nowhere
   const uint32_t pitch = pitch_of(a.ffn) * 4;
   const u32x4 to = rows_rsrc(a.h + first * uint64_t(pitch), (last - first) * pitch);
-  const uint32_t column = nw + lane % 8 * 4, out = column < a.ffn ? column * 4 : kNowhere;
 #pragma unroll
   for (int b = 0; b < T::kMT; b++)
     T::template rows_out<32>(
         lds, [&](int c, int i) { return float(acc[b][c][i]); },
         [&](uint32_t r, uint32_t, auto get) {
-          const uint32_t row = mw - first + b * 32 + r;
+          const uint32_t row = row0 + b * 32 + r;
           const float xs = scales[row];
           const f32x4 g4 = get(0), u4 = get(32);
           f32x4 h;
@@ -476,83 +481,88 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
             const float g = g4[i] * xs * gs[i], u = u4[i] * xs * us[i];
             h[i] = g / (1.0f + expf(-g)) * u;
           }
-          store_rows(to, out + row * pitch, __builtin_bit_cast(u32x4, h));
+          if constexpr (kQuads) {
+            store_rows(to, out[0] + row * pitch, __builtin_bit_cast(u32x4, h));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) store_rows(to, out[i] + row * pitch, __float_as_uint(h[i]));
+          }
         });
 }
 
-template <class T, bool kDirect>
+template <class T, bool kQuads>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];   // of the tile's rows of h, and their slots
   __shared__ uint32_t slots[T::kRows];
   static_assert(T::kRows <= T::kThreads);
   constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
+  const uint32_t k = a.ffn, step = kQuads ? 1 : steps_of(k);
+  const uint32_t blocks = ((a.hidden + step - 1) / step + kBN - 1) / kBN;
   uint32_t mt, nt, e, first, last;
-  if (!tile_at(blockIdx.x, tile_count<kBM>(a), (a.hidden + kBN - 1) / kBN, mt, nt)) return;
+  if (!tile_at(blockIdx.x, tile_count<kBM>(a), blocks * step, mt, nt)) return;
   if (!tile_of<kBM>(a, mt, e, first, last)) return;
   e = __builtin_amdgcn_readfirstlane(e);
   first = __builtin_amdgcn_readfirstlane(first);
   last = __builtin_amdgcn_readfirstlane(last);
-  const uint32_t n0 = nt * kBN, k = a.ffn, row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
-  const uint32_t n_rows = min(kBN, a.hidden - n0), m_rows = last - first;
-  const u32x4 xr = rows_rsrc(a.hq + uint64_t(first) * row_bytes, m_rows * row_bytes);
-  uint32_t xoff[T::kXLoads];
+  const uint32_t class0 = nt % step, r0 = nt / step * kBN, m_rows = last - first;
+  const ClassRows C = class_rows(a.down.w + e * a.down.stride, k, a.hidden, k, step, class0);
+  if (r0 >= C.rows) return;
+  const uint32_t n_rows = min(kBN, C.rows - r0);
+  const Shifted X = shifted(a.hq, a.hcopies, a.slots, k, C.shift);
+  const u32x4 xr = rows_rsrc(X.base + uint64_t(first) * X.pitch, m_rows * X.pitch);
+  const u32x4 wr = rows_rsrc(C.base + r0 * uint64_t(C.pitch), (n_rows - 1) * C.pitch + C.bytes);
+  uint32_t xoff[T::kXLoads], woff[T::kWLoads];
 #pragma unroll
-  for (int i = 0; i < T::kXLoads; i++)
-    xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
-  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
+  for (int i = 0; i < T::kXLoads; i++) xoff[i] = min(T::row_of(i), m_rows - 1) * X.pitch + T::byte_of();
+#pragma unroll
+  for (int i = 0; i < T::kWLoads; i++) woff[i] = min(T::row_of(i), n_rows - 1) * C.pitch + T::byte_of();
   // a load among the stores at the end would wait for all stores before it
-  const uint32_t place0 = min(first + threadIdx.x % kBM, last - 1);
-  const float row_scale = global<const float>(a.hscale)[place0];
-  const uint32_t row_slot = slot_at(a, place0);
-  const uint64_t down = a.down.w + e * a.down.stride + uint64_t(n0) * k;
+  const uint32_t place = min(first + threadIdx.x % kBM, last - 1);
+  const float row_scale = global<const float>(a.hscale)[place];
+  const uint32_t row_slot = slot_at(a, place);
   i32x16 acc[T::kMT][T::kNT];
-  if constexpr (kDirect) {
-    const u32x4 wr = rows_rsrc(down, n_rows * k);
-    uint32_t woff[T::kWLoads];
-#pragma unroll
-    for (int i = 0; i < T::kWLoads; i++)
-      woff[i] = min(T::row_of(i), n_rows - 1) * k + T::byte_of();
-    T::product(lds, row_bytes / T::kBytes, last - first, load_x,
-               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
-  } else {
-    global_ptr<const uint8_t> w[T::kWLoads];
-#pragma unroll
-    for (int i = 0; i < T::kWLoads; i++)
-      w[i] = global<const uint8_t>(down) + uint64_t(min(T::row_of(i), n_rows - 1)) * k + T::byte_of();
-    const int32_t left = int32_t(k) - int32_t(T::byte_of());
-    T::product(lds, row_bytes / T::kBytes, last - first, load_x, [&](int i, uint32_t s, uint32_t) {
-      return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
-    }, acc);
-  }
+  T::product(lds, (C.bytes + T::kBytes - 1) / T::kBytes, m_rows,
+             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
+             [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   constexpr int kCols = T::kNT * 32;
-  const uint32_t nw = n0 + wave % T::kWN_ * kCols, mw = first + wave / T::kWN_ * (T::kMT * 32);
+  const uint32_t column = wave % T::kWN_ * kCols + lane % (kCols / 4) * 4;
+  const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32), pitch = pitch_of(a.hidden);
+  // no branches: rows and columns past the last go to a row of their own
+  const uint64_t nowhere = uint64_t(a.slots) * pitch;
   float scale[4];
+  uint32_t out[4];
 #pragma unroll
-  for (int i = 0; i < 4; i++)
-    scale[i] = load_float(a.down.scale, a.down.scale_dtype,
-                          uint64_t(e) * a.hidden + min(nw + lane % (kCols / 4) * 4 + i, a.hidden - 1));
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t n = class0 + (r0 + column + i) * step;
+    scale[i] = load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + min(n, a.hidden - 1));
+    out[i] = column + (kQuads ? 0 : i) < n_rows ? n : kNowhere;
+  }
   if (threadIdx.x < kBM) {
     scales[threadIdx.x] = row_scale;
     slots[threadIdx.x] = first + threadIdx.x < last ? row_slot : a.slots;
   }
   __syncthreads();
-  // no branches: rows and columns past the last go to a row of their own
-  const uint32_t column = nw + lane % (kCols / 4) * 4, pitch = pitch_of(a.hidden);
-  const bool inside = column < a.hidden;
 #pragma unroll
   for (int b = 0; b < T::kMT; b++)
     T::template rows_out<kCols>(
         lds, [&](int c, int i) { return float(acc[b][c][i]); },
         [&](uint32_t r, uint32_t, auto get) {
-          const uint32_t row = mw - first + b * 32 + r;
+          const uint32_t row = row0 + b * 32 + r;
           const float hs = scales[row];
+          const uint64_t at = uint64_t(slots[row]) * pitch;
           f32x4 v = get(0);
 #pragma unroll
           for (int i = 0; i < 4; i++) v[i] = v[i] * hs * scale[i];
-          const uint64_t at = inside ? uint64_t(slots[row]) * pitch + column : uint64_t(a.slots) * pitch;
-          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) + at) = v;
+          if constexpr (kQuads) {
+            *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) +
+                                                 (out[0] != kNowhere ? at + out[0] : nowhere)) = v;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+              global<float>(a.out)[out[i] != kNowhere ? at + out[i] : nowhere] = v[i];
+          }
         });
 }
 
@@ -578,7 +588,7 @@ __global__ __launch_bounds__(256) void wc_experts_join_kernel(ExpertArgs a) {
 }
 
 struct Workspace {
-  uint64_t xq, xscale, wide, hq, hscale, bytes;
+  uint64_t xq, xscale, wide, hq, hscale, xcopies, hcopies, bytes;
 };
 Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
   Workspace w{};
@@ -594,6 +604,8 @@ Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
   w.wide = take((tokens * k + 1) * pitch_of(uint32_t(hidden > ffn ? hidden : ffn)) * 4);
   w.hq = take(tokens * k * WC_I8_ROW_BYTES(ffn));
   w.hscale = take(tokens * k * 4);
+  if (hidden % 4) w.xcopies = take(copies_bytes(tokens, hidden));
+  if (ffn % 4) w.hcopies = take(copies_bytes(tokens * k, ffn));
   w.bytes = at;
   return w;
 }
@@ -610,9 +622,10 @@ Bank bank(const wc_i8_experts* b) {
           b->scale_dtype};
 }
 
-// loads to LDS take whole dwords
-bool aligned4(const wc_i8_experts* b) {
-  return reinterpret_cast<uintptr_t>(b->w) % 4 == 0 && b->stride % 4 == 0;
+// Whether the rows of an expert's matrix start where the workspace has a copy of what
+// multiplies them: at whole dwords where k is whole ones.
+bool reached(const wc_i8_experts* b, uint32_t k) {
+  return k % 4 || (reinterpret_cast<uintptr_t>(b->w) % 4 == 0 && b->stride % 4 == 0);
 }
 
 // Slot by slot, while that reads no expert's rows twice much (E = 64, k = 6, 2048 x 1408):
@@ -622,32 +635,31 @@ constexpr uint32_t kSlotTokens = 4, kHoldBytes = 12 * 1024;
 
 // Rows of the order to a tile, by the rows an expert has on average.
 int tile_rows(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden, bool direct) {
-  // a tile finds x by 32-bit offsets
-  if (tokens * WC_I8_ROW_BYTES(hidden) >> 32) return 0;
+  // tiles find x by 32-bit offsets
+  if (!direct || tokens * WC_I8_ROW_BYTES(hidden + 3) >> 32) return 0;
   const uint32_t average = slots / experts;
   if (average >= 384) return 256;
   if (average >= 24) return 128;
   // a token takes an expert once
-  return !direct ? 0 : tokens <= 8 ? 8 : 16;
+  return tokens <= 8 ? 8 : 16;
 }
 
-template <class T>
-void start_up(const ExpertArgs& a, bool direct, hipStream_t st) {
-  const uint32_t cols = T::kWN_ * 32;
-  const dim3 grid(a.blocks * ((a.ffn + cols - 1) / cols)), block(T::kThreads);
-  if (direct)
-    hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, true>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, false>), grid, block, 0, st, a);
+uint32_t columns(uint32_t n, uint32_t step, uint32_t each) {
+  return step * (((n + step - 1) / step + each - 1) / each);
 }
 template <class T>
-void start_down(const ExpertArgs& a, bool direct, hipStream_t st) {
-  const uint32_t cols = T::kWN_ * T::kNT * 32;
-  const dim3 grid(a.blocks * ((a.hidden + cols - 1) / cols)), block(T::kThreads);
-  if (direct)
-    hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, true>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, false>), grid, block, 0, st, a);
+void start_up(const ExpertArgs& a, hipStream_t st) {
+  const uint32_t step = steps_of(a.hidden);
+  const dim3 grid(a.blocks * columns(a.ffn, step, T::kWN_ * 32)), block(T::kThreads);
+  if (step == 1) hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, false>), grid, block, 0, st, a);
+}
+template <class T>
+void start_down(const ExpertArgs& a, hipStream_t st) {
+  const uint32_t step = steps_of(a.ffn);
+  const dim3 grid(a.blocks * columns(a.hidden, step, T::kCols)), block(T::kThreads);
+  if (step == 1) hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, false>), grid, block, 0, st, a);
 }
 
 }  // namespace
@@ -696,6 +708,8 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   a.h = a.out = ws + w.wide;
   a.hq = ws + w.hq;
   a.hscale = ws + w.hscale;
+  a.xcopies = ws + w.xcopies;
+  a.hcopies = ws + w.hcopies;
   a.y = reinterpret_cast<uint64_t>(dev_y);
   a.ldy = ldy;
   a.tokens = tokens;
@@ -708,10 +722,14 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   a.gate = bank(gate);
   a.up = bank(up);
   a.down = bank(down);
-  const bool direct = hidden % 4 == 0 && ffn % 4 == 0 && aligned4(gate) && aligned4(up) && aligned4(down);
+  // gate and up rows of one column share their x, so they have to start alike
+  const bool direct = reached(gate, hidden) && reached(up, hidden) && reached(down, ffn) &&
+                      (reinterpret_cast<uintptr_t>(gate->w) - reinterpret_cast<uintptr_t>(up->w)) % 4 == 0 &&
+                      (gate->stride - up->stride) % 4 == 0;
   const uint64_t hold_x = WC_I8_ROW_BYTES(hidden), hold_h = k * WC_I8_ROW_BYTES(ffn);
   const bool vector = reinterpret_cast<uintptr_t>(dev_x) % 16 == 0 && ldx * size_of(dtype) % 16 == 0;
-  if (direct && vector && hidden % 8 == 0 && tokens <= kSlotTokens && slots <= experts && ffn % 8 == 0 && k <= kSlots && hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
+  if (direct && vector && hidden % 8 == 0 && ffn % 8 == 0 && tokens <= kSlotTokens &&
+      slots <= experts && k <= kSlots && hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
     const dim3 grid((ffn + 7) / 8, slots), block(SlotRing::kThreads);
     const uint32_t held = SlotRing::kLds + uint32_t(hold_x);
     if (dtype == WC_BF16)
@@ -729,13 +747,16 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   if (!launch_quantize(dev_x, dtype, tokens, hidden, ldx, reinterpret_cast<void*>(a.xq),
                        reinterpret_cast<float*>(a.xscale), st))
     return WC_EHIP;
+  if (hidden % 4 && !launch_shift(reinterpret_cast<const void*>(a.xq), tokens, hidden,
+                                  reinterpret_cast<void*>(a.xcopies), st))
+    return WC_EHIP;
   const int rows = tile_rows(tokens, slots, experts, hidden, direct);
   // every expert that has rows ends in at most one block that is not full
   a.blocks = slots / uint32_t(rows ? rows : 16) + (experts < slots ? experts : slots);
-  const uint32_t up_cols = rows ? 8 : 16;
-  const dim3 up_grid(a.blocks, (ffn + up_cols - 1) / up_cols), down_grid(a.blocks, (hidden + 15) / 16);
-  if (rows == 256) start_up<Tile<256, 256, 2, 4>>(a, direct, st);
-  else if (rows == 128) start_up<Tile<128, 128, 2, 2>>(a, direct, st);
+  const dim3 up_grid(a.blocks, rows ? columns(ffn, steps_of(hidden), 8) : (ffn + 15) / 16);
+  const dim3 down_grid(a.blocks, rows ? columns(hidden, steps_of(ffn), 16) : (hidden + 15) / 16);
+  if (rows == 256) start_up<Tile<256, 256, 2, 4>>(a, st);
+  else if (rows == 128) start_up<Tile<128, 128, 2, 2>>(a, st);
   else if (rows == 16)
     hipLaunchKernelGGL((wc_experts_up_ring_kernel<16>), up_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
   else if (rows == 8)
@@ -747,8 +768,11 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
                        reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st,
                        dev_offsets + experts))
     return WC_EHIP;
-  if (rows == 256) start_down<Tile<256, 256, 2, 4>>(a, direct, st);
-  else if (rows == 128) start_down<Tile<128, 128, 2, 2>>(a, direct, st);
+  if (ffn % 4 && !launch_shift(reinterpret_cast<const void*>(a.hq), slots, ffn,
+                               reinterpret_cast<void*>(a.hcopies), st, dev_offsets + experts))
+    return WC_EHIP;
+  if (rows == 256) start_down<Tile<256, 256, 2, 4>>(a, st);
+  else if (rows == 128) start_down<Tile<128, 128, 2, 2>>(a, st);
   else if (rows == 16)
     hipLaunchKernelGGL((wc_experts_down_ring_kernel<16>), down_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
   else if (rows == 8)

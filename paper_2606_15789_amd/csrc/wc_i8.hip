@@ -1,6 +1,7 @@
 // wc_i8.hip -- int8 linear layers: wc_quantize_i8, wc_matmul_i8, wc_linear_i8.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "wc_i8_ring.h"
 
@@ -90,15 +91,34 @@ void start_quantize(int32_t dt, uint32_t m, const QuantArgs& a, hipStream_t stre
     hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP32>), grid, block, 0, stream, a);
 }
 
+// Word i of three copies of a row of q, shifted by one, two and three bytes.
+__global__ __launch_bounds__(256) void wc_shift_i8_kernel(uint64_t q, uint64_t copies, uint64_t limit,
+                                                          uint32_t m, uint32_t k) {
+  const uint64_t row = blockIdx.x;
+  if (limit && int32_t(blockIdx.x) >= *global<const int32_t>(limit)) return;
+  const uint32_t words = uint32_t(WC_I8_ROW_BYTES(k)) / 4, wide = uint32_t(WC_I8_ROW_BYTES(k + 3)) / 4;
+  const auto from = global<const uint32_t>(q) + row * words;
+  for (uint32_t i = threadIdx.x; i < wide; i += 256) {
+    const uint32_t low = i && i <= words ? from[i - 1] : 0u, high = i < words ? from[i] : 0u;
+    const uint64_t both = uint64_t(high) << 32 | low;
+#pragma unroll
+    for (uint32_t s = 1; s <= 3; s++)
+      global<uint32_t>(copies)[((s - 1) * uint64_t(m) + row) * wide + i] = uint32_t(both >> (32 - 8 * s));
+  }
+}
+
 struct MatJob {
   uint64_t w, scale, bias, y, ldw, ldy;
   uint64_t part;      // where k is split: its int32 sums, split by split
   uint32_t n, tile0;  // tile0: its first workgroup
   int32_t scale_dtype, bias_dtype, y_dtype;
   uint32_t quads;     // y's columns are whole aligned groups of four
+  uint32_t step;      // classes of rows (class_rows)
+  uint32_t reserved;
 };
 struct MatArgs {
   uint64_t q, qscale;
+  uint64_t copies;  // of q, shifted
   uint64_t x, ldx;  // not quantised yet, where the kernel does that itself
   uint32_t m, k, n_jobs, splits;
   MatJob job[kMaxJobs];
@@ -163,12 +183,11 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_matmul_i8_rows_kernel(MatAr
   }
 }
 
-// A few rows of x: 16 rows of W a workgroup.
-// m = 13, k = 8192, n = 28672: 16 rows of W, 4 waves, 4 stages 43.9 us (5.4 TB/s); 2 waves
+// A few rows of x: 16 rows of W a workgroup.  m = 13, k = 8192, n = 28672: 16 rows of W, 4 waves, 4 stages 43.9 us (5.4 TB/s); 2 waves
 // of 8 stages 52.0, 8 waves of 4 48.9, 4 of 6 50.1; 32 rows, 4 waves, 3 stages 56.4; 64
 // rows 49.4.  At m = 1 40.9 us, 5.75 TB/s, what a plain streaming kernel reaches.
-//   kX = 0: x comes as it is, and every
-// workgroup quantises it for itself while its first rows of W are on their way.
+// kX = 0: x comes as it is, and every workgroup quantises it for itself while its first
+// rows of W are on their way.
 template <int kX>
 using MatRing = Ring<1, kX, 4, 4>;
 
@@ -182,34 +201,38 @@ __global__ __launch_bounds__(MatRing<kX>::kThreads) void wc_matmul_i8_ring_kerne
   uint32_t j = 0;
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
   const MatJob J = a.job[j];
-  const uint32_t n0 = (blockIdx.x - J.tile0) * 16, n_rows = min(16u, J.n - n0);
-  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k));
-  const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw, uint32_t((n_rows - 1) * J.ldw + a.k));
-  const u32x4 xr = rows_rsrc(a.q, kX ? a.m * row_bytes : 0u);
+  const uint32_t blocks = ((J.n + J.step - 1) / J.step + 15) / 16;  // to a class of rows
+  const uint32_t tile = blockIdx.x - J.tile0, first = tile / blocks, r0 = tile % blocks * 16;
+  const ClassRows C = class_rows(J.w, J.ldw, J.n, a.k, J.step, first);
+  if (r0 >= C.rows) return;
+  const uint32_t n_rows = min(16u, C.rows - r0);
+  const Shifted X = shifted(a.q, a.copies, a.m, a.k, C.shift);
+  const u32x4 wr = rows_rsrc(C.base + r0 * uint64_t(C.pitch), (n_rows - 1) * C.pitch + C.bytes);
+  const u32x4 xr = rows_rsrc(X.base, kX ? a.m * X.pitch : 0u);
   uint32_t woff[2], xoff[2];
 #pragma unroll
   for (int i = 0; i < 2; i++) {
-    woff[i] = min(8 * i + R::row_of(), n_rows - 1) * uint32_t(J.ldw) + R::byte_of();
-    xoff[i] = min(8 * i + R::row_of(), a.m - 1) * row_bytes + R::byte_of();
+    woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of();
+    xoff[i] = min(8 * i + R::row_of(), a.m - 1) * X.pitch + R::byte_of();
   }
   i32x4 acc[1];
-  R::product(lds, row_bytes / kStage,
+  R::product(lds, (C.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
              [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc, [&] {
                if constexpr (kX == 0)
                  hold_rows<R::kThreads, kType, 2>(
                      a.m, a.k, [&](uint32_t r) { return a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2); },
                      lds + R::kLds, scales, tops);
-               return typename R::Held{lds + R::kLds, row_bytes, a.m};
+               return typename R::Held{lds + R::kLds, X.pitch, a.m};
              });
   R::gather(lds, acc);
   for (uint32_t o = threadIdx.x; o < 16 * kRows; o += R::kThreads) {
-    const uint32_t n = o % 16, m = o / 16;
-    if (n >= n_rows || m >= a.m) continue;
+    const uint32_t r = o % 16, m = o / 16, n = first + (r0 + r) * J.step;
+    if (r >= n_rows || m >= a.m) continue;
     const float xs = kX ? global<const float>(a.qscale)[m] : scales[m];
-    float y = float(R::sum(lds, n, m)) * xs * load_float(J.scale, J.scale_dtype, n0 + n);
-    if (J.bias) y += load_float(J.bias, J.bias_dtype, n0 + n);
-    store_float(J.y, J.y_dtype, m * J.ldy + n0 + n, y);
+    float y = float(R::sum(lds, r, m)) * xs * load_float(J.scale, J.scale_dtype, n);
+    if (J.bias) y += load_float(J.bias, J.bias_dtype, n);
+    store_float(J.y, J.y_dtype, m * J.ldy + n, y);
   }
 }
 
@@ -237,26 +260,25 @@ __device__ __forceinline__ void finish(const MatJob& J, uint32_t m, uint32_t n, 
       if (n + i < J.n) store_float(J.y, J.y_dtype, at + i, v[i]);
   }
 }
-__device__ __forceinline__ void column_scales(const MatJob& J, uint32_t n, float (&scale)[4],
-                                              float (&bias)[4]) {
+// Scales and biases of columns n, n + step, ..
+__device__ __forceinline__ void column_scales(const MatJob& J, uint32_t n, uint32_t step,
+                                              float (&scale)[4], float (&bias)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const uint32_t c = min(n + i, J.n - 1);
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t c = min(n + i * step, J.n - 1);
     scale[i] = load_float(J.scale, J.scale_dtype, c);
     bias[i] = J.bias ? load_float(J.bias, J.bias_dtype, c) : 0.0f;
   }
 }
 
-// A wave's results to rows of type kType (0: the int32 sums), where the columns fill whole
-// groups of four: without a branch, so that the reads from LDS and the stores of all rows
-// overlap.  What is past the last row or column goes nowhere.
-template <class T, int kType>
+// A wave's results to rows of type kType (0: the int32 sums), four neighbours at once
+// (kQuads) or each at its own offset `lane`.  Without a branch, so that the reads from LDS
+// and the stores of all rows overlap: what is past the last row or column goes nowhere.
+template <class T, int kType, bool kQuads>
 __device__ __forceinline__ void tile_out(uint8_t* lds, const i32x16 (&acc)[T::kMT][T::kNT], u32x4 to,
-                                         uint32_t pitch, uint32_t row0, uint32_t column, bool inside,
+                                         uint32_t pitch, uint32_t row0, const uint32_t (&lane)[4],
                                          const float* scales, const float (&scale)[4],
                                          const float (&bias)[4]) {
-  constexpr uint32_t kSize = kType == 0 || kType == WC_FP32 ? 4 : 2;
-  const uint32_t lane = inside ? column * kSize : kNowhere;
 #pragma unroll
   for (int b = 0; b < T::kMT; b++)
     T::template rows_out<T::kNT * 32>(
@@ -270,19 +292,34 @@ __device__ __forceinline__ void tile_out(uint8_t* lds, const i32x16 (&acc)[T::kM
 #pragma unroll
             for (int i = 0; i < 4; i++) v[i] = v[i] * xs * scale[i] + bias[i];
           }
-          const uint32_t at = lane + row * pitch;
-          if constexpr (kSize == 4)
-            store_rows(to, at, __builtin_bit_cast(u32x4, v));
-          else if constexpr (kType == WC_BF16)
-            store_rows(to, at, u32x2{floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])});
-          else
-            store_rows(to, at, u32x2{float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16,
-                                     float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16});
+          if constexpr (kType == 0 || kType == WC_FP32) {
+            if constexpr (kQuads) {
+              store_rows(to, lane[0] + row * pitch, __builtin_bit_cast(u32x4, v));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; i++)
+                store_rows(to, lane[i] + row * pitch, __float_as_uint(v[i]));
+            }
+          } else {
+            const u32x2 h = kType == WC_BF16
+                                ? u32x2{floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])}
+                                : u32x2{float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16,
+                                        float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16};
+            if constexpr (kQuads) {
+              store_rows(to, lane[0] + row * pitch, h);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; i++)
+                store_rows(to, lane[i] + row * pitch, uint16_t(h[i / 2] >> (16 * (i % 2))));
+            }
+          }
+          // row after row: all of them at once are more than the registers hold
+          if constexpr (!kQuads) __builtin_amdgcn_sched_barrier(0);
         });
 }
 
 // One tile of a job (and one part of k) a workgroup.
-template <class T, bool kDirect>
+template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];  // of the tile's rows of x
@@ -290,74 +327,70 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   uint32_t j = 0;
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
   const MatJob J = a.job[j];
+  // classes of the same columns one after another, so that their stores meet in a cache
+  const uint32_t blocks = ((J.n + J.step - 1) / J.step + kBN - 1) / kBN;
   uint32_t mt, nt;
-  if (!tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt)) return;
-  const uint32_t m0 = mt * kBM, n0 = nt * kBN;
-  const uint32_t m_rows = min(kBM, a.m - m0), n_rows = min(kBN, J.n - n0);
-  const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(a.k)), all = row_bytes / T::kBytes;
+  if (!tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, blocks * J.step, mt, nt)) return;
+  const uint32_t m0 = mt * kBM, m_rows = min(kBM, a.m - m0), first = nt % J.step, r0 = nt / J.step * kBN;
+  const ClassRows C = class_rows(J.w, J.ldw, J.n, a.k, J.step, first);
+  if (r0 >= C.rows) return;
+  const uint32_t n_rows = min(kBN, C.rows - r0);
+  const Shifted X = shifted(a.q, a.copies, a.m, a.k, C.shift);
   // this workgroup's part of the stages
+  const uint32_t all = (C.bytes + T::kBytes - 1) / T::kBytes;
   const uint32_t each = all / a.splits, rest = all % a.splits, part = blockIdx.y;
   const uint32_t s0 = part * each + min(part, rest), stages = each + (part < rest);
   const uint32_t k0 = s0 * T::kBytes;
-  const u32x4 xr = rows_rsrc(a.q + m0 * uint64_t(row_bytes) + k0, m_rows * row_bytes - k0);
-  uint32_t xoff[T::kXLoads];
+  const u32x4 xr = rows_rsrc(X.base + m0 * uint64_t(X.pitch) + k0, m_rows * X.pitch - k0);
+  const u32x4 wr = rows_rsrc(C.base + r0 * uint64_t(C.pitch) + k0, (n_rows - 1) * C.pitch + C.bytes - k0);
+  uint32_t xoff[T::kXLoads], woff[T::kWLoads];
 #pragma unroll
-  for (int i = 0; i < T::kXLoads; i++)
-    xoff[i] = min(T::row_of(i), m_rows - 1) * row_bytes + T::byte_of();
-  const auto load_x = [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); };
+  for (int i = 0; i < T::kXLoads; i++) xoff[i] = min(T::row_of(i), m_rows - 1) * X.pitch + T::byte_of();
+#pragma unroll
+  for (int i = 0; i < T::kWLoads; i++) woff[i] = min(T::row_of(i), n_rows - 1) * C.pitch + T::byte_of();
   // a load among the stores at the end would wait for all stores before it
   const float row_scale = global<const float>(a.qscale)[m0 + min(threadIdx.x, m_rows - 1)];
-  i32x16 acc[T::kMT][T::kNT];
-  if constexpr (kDirect) {
-    const u32x4 wr = rows_rsrc(J.w + n0 * J.ldw + k0, uint32_t((n_rows - 1) * J.ldw + a.k - k0));
-    uint32_t woff[T::kWLoads];
-#pragma unroll
-    for (int i = 0; i < T::kWLoads; i++)
-      woff[i] = min(T::row_of(i), n_rows - 1) * uint32_t(J.ldw) + T::byte_of();
-    T::product(lds, stages, m_rows, load_x,
-               [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
-  } else {
-    global_ptr<const uint8_t> w[T::kWLoads];
-#pragma unroll
-    for (int i = 0; i < T::kWLoads; i++)
-      w[i] = global<const uint8_t>(J.w) + (n0 + min(T::row_of(i), n_rows - 1)) * J.ldw + k0 + T::byte_of();
-    const int32_t left = int32_t(a.k - k0) - int32_t(T::byte_of());
-    T::product(lds, stages, m_rows, load_x, [&](int i, uint32_t s, uint32_t) {
-      return load_codes(w[i] + uint64_t(s) * T::kBytes, left - int32_t(s * T::kBytes));
-    }, acc);
-  }
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   constexpr int kCols = T::kNT * 32;
-  const uint32_t nw = n0 + wave % T::kWN_ * kCols, mw = m0 + wave / T::kWN_ * (T::kMT * 32);
-  float scale[4], bias[4];
-  if (a.splits == 1) column_scales(J, nw + lane % (kCols / 4) * 4, scale, bias);
+  const uint32_t column = wave % T::kWN_ * kCols + lane % (kCols / 4) * 4;
+  i32x16 acc[T::kMT][T::kNT];
+  T::product(lds, stages, m_rows,
+             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
+             [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
+  float scale[4] = {}, bias[4] = {};
+  if (a.splits == 1) column_scales(J, first + (r0 + column) * J.step, J.step, scale, bias);
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
   __syncthreads();
-  const uint32_t row0 = mw - m0, column = nw - n0 + lane % (kCols / 4) * 4;
-  const bool inside = n0 + column < J.n;
-  if (a.splits > 1) {
-    const uint64_t pitch = ((J.n + 3u) & ~3u) * 4;
-    const u32x4 to = rows_rsrc(J.part + (uint64_t(part) * a.m + m0) * pitch + n0 * 4ull,
-                               uint32_t(m_rows * pitch - n0 * 4ull));
-    return tile_out<T, 0>(lds, acc, to, uint32_t(pitch), row0, column, inside, scales, scale, bias);
-  }
-  if (J.quads) {
-    const uint32_t size = J.y_dtype == WC_FP32 ? 4 : 2, pitch = uint32_t(J.ldy) * size;
-    const u32x4 to = rows_rsrc(J.y + (m0 * J.ldy + n0) * size, (m_rows - 1) * pitch + n_rows * size);
-    if (J.y_dtype == WC_BF16)
-      return tile_out<T, WC_BF16>(lds, acc, to, pitch, row0, column, inside, scales, scale, bias);
-    if (J.y_dtype == WC_FP16)
-      return tile_out<T, WC_FP16>(lds, acc, to, pitch, row0, column, inside, scales, scale, bias);
-    return tile_out<T, WC_FP32>(lds, acc, to, pitch, row0, column, inside, scales, scale, bias);
-  }
+  const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32);
+  const auto out = [&]<int kType, bool kQuads>(std::integer_sequence<int, kType>, std::bool_constant<kQuads>) {
+    constexpr uint32_t kSize = kType == 0 || kType == WC_FP32 ? 4 : 2;
+    const uint32_t pitch = kType ? uint32_t(J.ldy) * kSize : ((J.n + 3u) & ~3u) * 4;
+    const uint64_t row = kType ? J.y + m0 * uint64_t(pitch) : J.part + (uint64_t(part) * a.m + m0) * pitch;
+    const uint32_t column0 = (first + r0 * J.step) * kSize;
+    // to the last column of the last row, or of its group of four
+    const uint32_t end = ((n_rows - 1) * J.step + 1) * kSize;
+    const u32x4 to = rows_rsrc(row + column0, (m_rows - 1) * pitch + (kQuads ? (end + 4 * kSize - 1) / (4 * kSize) * (4 * kSize) : end));
+    uint32_t at[4];
 #pragma unroll
-  for (int b = 0; b < T::kMT; b++)
-    T::template rows_out<kCols>(
-        lds, [&](int c, int i) { return float(acc[b][c][i]); },
-        [&](uint32_t row, uint32_t col, auto get) {
-          const uint32_t m = mw + b * 32 + row, n = nw + col;
-          if (m < a.m && n < J.n) finish(J, m, n, get(0), scales[m - m0], scale, bias);
-        });
+    for (uint32_t i = 0; i < 4; i++)
+      at[i] = column + (kQuads ? 0 : i) < n_rows ? (column + i) * J.step * kSize : kNowhere;
+    tile_out<T, kType, kQuads>(lds, acc, to, pitch, row0, at, scales, scale, bias);
+  };
+  const auto typed = [&](auto type) {
+    if (J.quads) out(type, std::true_type{});
+    else out(type, std::false_type{});
+  };
+  if (a.splits > 1) {
+    // a row of sums ends in a whole group of four
+    if (J.step == 1) out(std::integer_sequence<int, 0>{}, std::true_type{});
+    else out(std::integer_sequence<int, 0>{}, std::false_type{});
+  } else if (J.y_dtype == WC_BF16) {
+    typed(std::integer_sequence<int, WC_BF16>{});
+  } else if (J.y_dtype == WC_FP16) {
+    typed(std::integer_sequence<int, WC_FP16>{});
+  } else {
+    typed(std::integer_sequence<int, WC_FP32>{});
+  }
 }
 
 // y from the sums of the parts of k.
@@ -368,7 +401,7 @@ __global__ __launch_bounds__(256) void wc_matmul_i8_join_kernel(MatArgs a) {
   if (n >= J.n) return;
   const uint64_t pitch = (J.n + 3u) & ~3u;
   float scale[4], bias[4];
-  column_scales(J, n, scale, bias);
+  column_scales(J, n, 1, scale, bias);
   for (uint32_t m = blockIdx.x; m < a.m; m += gridDim.x) {
     i32x4 sum = {0, 0, 0, 0};
     for (uint32_t p = 0; p < a.splits; p++)
@@ -425,8 +458,8 @@ constexpr uint64_t kHoldAlways = 4096, kHoldSmall = 8192, kHoldSmallWeights = 32
 enum class Kernel { kRows, kRing, kTile64, kTile64Wide, kTile128, kTile256Half, kTile256 };
 struct Plan {
   Kernel kernel;
-  bool direct;      // every W can go to LDS as it is
   bool hold;        // the kernel can quantise x itself
+  bool copies;      // some rows of W do not start with a dword
   uint32_t splits;
   uint64_t part_bytes;
 };
@@ -442,10 +475,12 @@ void with_tile(Kernel kernel, F f) {
     default: return;
   }
 }
-uint32_t tiles_of(Kernel kernel, uint32_t m, uint32_t n) {
-  uint32_t tiles = (n + 15) / 16;
+// Workgroups for m rows of x and a matrix of n rows in `step` classes.
+uint32_t tiles_of(Kernel kernel, uint32_t m, uint32_t n, uint32_t step) {
+  const uint32_t each = (n + step - 1) / step;
+  uint32_t tiles = step * ((each + 15) / 16);
   with_tile(kernel, [&](auto t) {
-    tiles = (m + t.kRows - 1) / t.kRows * ((n + t.kCols - 1) / t.kCols);
+    tiles = (m + t.kRows - 1) / t.kRows * (step * ((each + t.kCols - 1) / t.kCols));
   });
   return tiles;
 }
@@ -469,31 +504,35 @@ constexpr TileCost kCosts[] = {{Kernel::kTile64, 0.26, 0.34, 5.0},
 constexpr double kUnits = 256, kJoin = 4.0, kBytesPerUs = 4e6, kReadPerUs = 5e6;
 
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
-  Plan p{Kernel::kRows, true, false, 1, 0};
+  Plan p{Kernel::kRows, false, false, 1, 0};
   uint64_t sums = 0, weights = 0, tiles64 = 0;
+  bool narrow = true;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
     weights += uint64_t(J.n) * k;
-    // offsets within a tile's rows are 32-bit
-    if (J.ldw > (1u << 22)) return p;
-    // loads to LDS take whole dwords
-    p.direct = p.direct && k % 4 == 0 && J.ldw % 4 == 0 && reinterpret_cast<uintptr_t>(J.w) % 4 == 0;
-    tiles64 += uint64_t(m + 63) / 64 * ((J.n + 63) / 64);
+    // offsets within a tile are 32-bit
+    if (J.ldw > (1u << 20)) return p;
+    narrow = narrow && J.n < (1u << 20) && J.ldy < (1u << 20);
+    p.copies = p.copies || J.ldw % 4 || reinterpret_cast<uintptr_t>(J.w) % 4;
+    tiles64 += uint64_t(m + 63) / 64 * (J.n / 64 + 4);
     sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
   }
   if (m <= 16) {
-    if (p.direct) p.kernel = Kernel::kRing;
+    p.kernel = Kernel::kRing;
     const uint64_t held = m * WC_I8_ROW_BYTES(k);
-    p.hold = p.direct && k % 8 == 0 &&
+    p.hold = !p.copies && k % 8 == 0 &&
              (held <= kHoldAlways || (held <= kHoldSmall && weights <= kHoldSmallWeights));
     return p;
   }
-  if (tiles64 > 0x7FFFFFFFu) return p;
+  if (!narrow || tiles64 > 0x7FFFFFFFu) {
+    p.copies = false;
+    return p;
+  }
   const uint32_t stages = (k + kStage - 1) / kStage;
   double best = 0;
   for (const TileCost& c : kCosts) {
     double tiles = 0;
-    for (uint32_t i = 0; i < n_jobs; i++) tiles += tiles_of(c.kernel, m, jobs[i].n);
+    for (uint32_t i = 0; i < n_jobs; i++) tiles += tiles_of(c.kernel, m, jobs[i].n, steps_of(jobs[i].ldw));
     for (uint32_t splits : {1u, 2u, 3u, 4u, 6u, 8u}) {
       if (splits > 1 && stages < 4 * splits) break;
       const double groups = tiles * splits;
@@ -513,6 +552,11 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   return p;
 }
 
+// The copies of q, then the sums of the parts of k.
+uint64_t workspace_of(const Plan& p, uint32_t m, uint32_t k) {
+  return (p.copies ? copies_bytes(m, k) : 0) + p.part_bytes;
+}
+
 template <int kX, int kType = 0>
 void start_ring(uint32_t tiles, const MatArgs& a, hipStream_t stream) {
   const uint32_t held = kX ? 0 : a.m * uint32_t(WC_I8_ROW_BYTES(a.k));
@@ -521,9 +565,13 @@ void start_ring(uint32_t tiles, const MatArgs& a, hipStream_t stream) {
 }
 
 wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, uint32_t n_jobs,
-                 const wc_i8_job* jobs, const Plan& p, void* parts, hipStream_t stream,
+                 const wc_i8_job* jobs, const Plan& p, void* workspace, hipStream_t stream,
                  const void* x = nullptr, int32_t x_dtype = 0, uint64_t ldx = 0) {
   MatArgs a{};
+  if (p.copies) {
+    if (!launch_shift(q, m, k, workspace, stream)) return WC_EHIP;
+    a.copies = reinterpret_cast<uint64_t>(workspace);
+  }
   a.x = reinterpret_cast<uint64_t>(x);
   a.ldx = ldx;
   a.q = reinterpret_cast<uint64_t>(q);
@@ -532,18 +580,19 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
   a.n_jobs = n_jobs;
   a.splits = p.splits;
   uint32_t tiles = 0, widest = 0;
-  uint64_t part = reinterpret_cast<uint64_t>(parts);
+  uint64_t part = reinterpret_cast<uint64_t>(workspace) + (p.copies ? copies_bytes(m, k) : 0);
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
     const uint32_t size = size_of(J.y_dtype);
     a.job[i] = {reinterpret_cast<uint64_t>(J.w),    reinterpret_cast<uint64_t>(J.scale),
                 reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
                 J.ldw, J.ldy, part, J.n, tiles, J.scale_dtype, J.bias_dtype, J.y_dtype,
-                J.n % 4 == 0 && J.ldy % 4 == 0 && J.ldy < (1u << 20) &&
-                    reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0};
+                steps_of(J.ldw) == 1 && J.n % 4 == 0 && J.ldy % 4 == 0 &&
+                    reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0,
+                p.kernel == Kernel::kRows ? 1u : steps_of(J.ldw), 0};
     if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
-    tiles += tiles_of(p.kernel, m, J.n);
+    tiles += tiles_of(p.kernel, m, J.n, a.job[i].step);
   }
   if (p.kernel == Kernel::kRing) {
     a.m = m;
@@ -559,10 +608,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     const dim3 grid(tiles, p.splits);
     with_tile(p.kernel, [&](auto t) {
       using T = decltype(t);
-      if (p.direct)
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, true>), grid, dim3(T::kThreads), 0, stream, a);
-      else
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, false>), grid, dim3(T::kThreads), 0, stream, a);
+      hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T>), grid, dim3(T::kThreads), 0, stream, a);
     });
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
     if (p.splits > 1) {
@@ -613,6 +659,13 @@ bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t
   return hipGetLastError() == hipSuccess;
 }
 
+bool launch_shift(const void* q, uint32_t m, uint32_t k, void* copies, hipStream_t stream,
+                  const int32_t* limit) {
+  hipLaunchKernelGGL(wc_shift_i8_kernel, dim3(m), dim3(256), 0, stream, reinterpret_cast<uint64_t>(q),
+                     reinterpret_cast<uint64_t>(copies), reinterpret_cast<uint64_t>(limit), m, k);
+  return hipGetLastError() == hipSuccess;
+}
+
 }  // namespace wc_i8
 
 extern "C" wc_status wc_quantize_i8(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k,
@@ -633,7 +686,7 @@ extern "C" wc_status wc_matmul_i8_workspace_bytes(uint32_t m, uint32_t k, uint32
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
-  *bytes = plan_of(m, k, n_jobs, jobs).part_bytes;
+  *bytes = workspace_of(plan_of(m, k, n_jobs, jobs), m, k);
   return WC_OK;
 }
 
@@ -653,7 +706,7 @@ extern "C" wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, u
     return WC_EINVAL;
   Plan p = plan_of(m, k, n_jobs, jobs);
   p.hold = false;
-  if (!workspace_ok(dev_workspace, workspace_bytes, p.part_bytes)) return WC_EINVAL;
+  if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p, m, k))) return WC_EINVAL;
   return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, p, dev_workspace,
                 reinterpret_cast<hipStream_t>(stream));
 }
@@ -664,7 +717,7 @@ extern "C" wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32
   *bytes = 0;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
   *bytes = pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)) + pad256(uint64_t(m) * 4) +
-           plan_of(m, k, n_jobs, jobs).part_bytes;
+           workspace_of(plan_of(m, k, n_jobs, jobs), m, k);
   return WC_OK;
 }
 

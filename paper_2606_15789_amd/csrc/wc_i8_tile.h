@@ -32,14 +32,22 @@ __device__ __forceinline__ void load_lds(u32x4 rs, uint32_t lds, uint32_t offset
                : "memory");
 }
 
-// 8 or 16 bytes to rs + offset; nothing where that is past the buffer's end.
+// Values to rs + offset; nothing where that is past the buffer's end.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t as_rsrc(u32x4 rs) {
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(uint64_t(rs[1]) << 32 | rs[0]),
+                                           (short)0, (int)rs[2], (int)rs[3]);
+}
+__device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, uint16_t v) {
+  __builtin_amdgcn_raw_buffer_store_b16(v, as_rsrc(rs), offset, 0, 0);
+}
+__device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, uint32_t v) {
+  __builtin_amdgcn_raw_buffer_store_b32(v, as_rsrc(rs), offset, 0, 0);
+}
 __device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, u32x2 v) {
-  __builtin_amdgcn_raw_buffer_store_b64(v, __builtin_amdgcn_make_buffer_rsrc(
-      reinterpret_cast<void*>(uint64_t(rs[1]) << 32 | rs[0]), (short)0, (int)rs[2], (int)rs[3]), offset, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b64(v, as_rsrc(rs), offset, 0, 0);
 }
 __device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, u32x4 v) {
-  __builtin_amdgcn_raw_buffer_store_b128(v, __builtin_amdgcn_make_buffer_rsrc(
-      reinterpret_cast<void*>(uint64_t(rs[1]) << 32 | rs[0]), (short)0, (int)rs[2], (int)rs[3]), offset, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(v, as_rsrc(rs), offset, 0, 0);
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset past the end of every buffer here
 
@@ -76,15 +84,13 @@ struct Tile {
   }
 
   // `load_x(i, stage, lds)` and `load_w(i, stage, lds)` start load i of a stage's rows
-  // of x and W.  A W whose rows cannot go to LDS as they are comes through registers:
-  // load_w then gives load i's 16 bytes, which are stored after the products.
+  // of x and W.
   // Waves all of whose rows of x are past the first `rows` only load: the other wave of
   // their SIMD has the matrix unit to itself.
   template <class LoadX, class LoadW>
   static __device__ __forceinline__ void product(uint8_t* lds, uint32_t stages, uint32_t rows,
                                                  LoadX load_x, LoadW load_w,
                                                  i32x16 (&acc)[kMT][kNT]) {
-    constexpr bool kDirect = __is_same(decltype(load_w(0, 0u, 0u)), void);
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t wm = wave / kWN, wn = wave % kWN;
     const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>(
@@ -95,30 +101,14 @@ struct Tile {
       for (int n = 0; n < kNT; n++)
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[m][n][i] = 0;
-    // stages ahead: one where W comes through registers
-    constexpr uint32_t kAhead = kDirect ? kDepth - 1 : 1, kSlots = kAhead + 1;
-    constexpr int kAll = kXLoads + (kDirect ? kWLoads : 0);
+    constexpr uint32_t kAhead = kDepth - 1;
+    constexpr int kAll = kXLoads + kWLoads;
     // Load i of a stage.  Stages past the last are loaded too: the buffers' ends bound
     // them, nothing reads them, and the loop has no branches.
     const auto start = [&](int i, uint32_t s, uint32_t slot) {
       const uint32_t to = __builtin_amdgcn_readfirstlane(base + slot * kBuffer + wave * 1024);
       if (i < kXLoads) load_x(i, s, to + uint32_t(i) * kThreads * 16);
       else load_w(i - kXLoads, s, to + kBM * kK + uint32_t(i - kXLoads) * kThreads * 16);
-    };
-    i32x4 held[kDirect ? 1 : kWLoads];
-    const auto hold = [&](uint32_t s) {
-      if constexpr (!kDirect) {
-#pragma unroll
-        for (int i = 0; i < kWLoads; i++) held[i] = load_w(i, s, 0u);
-      }
-    };
-    const auto keep = [&](uint32_t slot) {
-      if constexpr (!kDirect) {
-        uint8_t* to = lds + slot * kBuffer + kBM * kK + threadIdx.x * 16;
-#pragma unroll
-        for (int i = 0; i < kWLoads; i++)
-          *reinterpret_cast<i32x4*>(to + i * kThreads * 16) = held[i];
-      }
     };
     constexpr int kQuarters = kK / 32;
     uint32_t at[kQuarters];
@@ -159,12 +149,9 @@ struct Tile {
     for (uint32_t s = 0; s < kAhead; s++)
 #pragma unroll
       for (int i = 0; i < kAll; i++) start(i, s, s);
-    hold(0);
-    keep(0);
-    arrive<kDirect ? int(kAhead) - 1 : 0>();
+    arrive<int(kAhead) - 1>();
 #pragma unroll
     for (int i = 0; i < kHalf; i++) start(i, kAhead, kAhead);
-    hold(1);
 #pragma unroll
     for (int i = 0; i < kMT + kNT; i++) read(0, lds, 0, i);
     uint32_t slot = 0, fill = kAhead;  // the stage's place, and that of the one it loads
@@ -172,13 +159,9 @@ struct Tile {
       for (uint32_t s = 0; s < stages; s++) {
 #pragma unroll
         for (int i = kHalf; i < kAll; i++) start(i, s + kAhead, fill);
-        keep(fill);
-        arrive<kDirect ? int(kAhead) - 1 : 0>();
+        arrive<int(kAhead) - 1>();
         fill = slot;
-        slot = slot + 1 < kSlots ? slot + 1 : 0;
-        if constexpr (!kDirect) {
-          if (s + 2 < stages) hold(s + 2);
-        }
+        slot = slot + 1 < kDepth ? slot + 1 : 0;
 #pragma unroll
         for (int i = 0; i < kHalf; i++) start(i, s + 1 + kAhead, fill);
       }
@@ -193,15 +176,11 @@ struct Tile {
       // Before the last quarter's products: the next stage's loads of this wave are in LDS
       // and its reads of this stage done, and so with the other waves behind the barrier.
       // The stage after those in flight then replaces this one.
-      keep(fill);
       // lgkmcnt(0) as the compiler knows it: no waits for these operands further on
       __builtin_amdgcn_s_waitcnt(0xC07F);
-      arrive<kDirect ? int(kAhead) - 1 : 0>();
+      arrive<int(kAhead) - 1>();
       fill = slot;
-      slot = slot + 1 < kSlots ? slot + 1 : 0;
-      if constexpr (!kDirect) {
-        if (s + 2 < stages) hold(s + 2);
-      }
+      slot = slot + 1 < kDepth ? slot + 1 : 0;
       quarter(1, slot, 0, s + 1 + kAhead, fill, First{});
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -241,6 +220,38 @@ struct Tile {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 };
+
+// Rows of an int8 matrix that start at the same byte of a dword: rows first, first +
+// step, ... of n rows `ld` bytes apart, step 1, 2 or 4.  Loads to LDS take whole dwords, so
+// such a row is read from the dword it starts in, and multiplied by x shifted as far.
+__host__ __device__ constexpr uint32_t steps_of(uint64_t ld) { return ld % 4 == 0 ? 1 : ld % 2 == 0 ? 2 : 4; }
+struct ClassRows {
+  uint64_t base;                      // of the dword that row `first` starts in
+  uint32_t pitch, rows, shift, bytes;  // bytes: of a row and its shift, whole dwords
+};
+__device__ __forceinline__ ClassRows class_rows(uint64_t w, uint64_t ld, uint32_t n, uint32_t k,
+                                                uint32_t step, uint32_t first) {
+  const uint64_t at = w + first * ld;
+  const uint32_t shift = uint32_t(at & 3);
+  return {at - shift, uint32_t(ld) * step, (n - first + step - 1) / step, shift, (k + shift + 3) & ~3u};
+}
+// Quantised activations: rows of WC_I8_ROW_BYTES(k) bytes, and where a matrix needs them
+// three copies of WC_I8_ROW_BYTES(k + 3), shifted by one to three bytes.
+struct Shifted {
+  uint64_t base;
+  uint32_t pitch;
+};
+__device__ __forceinline__ Shifted shifted(uint64_t q, uint64_t copies, uint64_t rows, uint32_t k,
+                                           uint32_t shift) {
+  if (!shift) return {q, uint32_t(WC_I8_ROW_BYTES(k))};
+  const uint32_t pitch = uint32_t(WC_I8_ROW_BYTES(k + 3));
+  return {copies + (shift - 1) * (rows * pitch), pitch};
+}
+inline uint64_t copies_bytes(uint64_t rows, uint64_t k) { return pad256(3 * rows * WC_I8_ROW_BYTES(k + 3)); }
+// Make the three copies of m rows (or as many as the device int `limit` says); false on a
+// launch error (wc_i8.hip).
+bool launch_shift(const void* q, uint32_t m, uint32_t k, void* copies, hipStream_t stream,
+                  const int32_t* limit = nullptr);
 
 // Which tile a workgroup takes, so that those that run at once on one of the eight
 // dies (workgroup i goes to die i mod 8, each with its own L2) share rows: each die

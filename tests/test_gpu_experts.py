@@ -114,7 +114,8 @@ def _run(dev, x, r, layer, **more):
     (17, 2, 2, 100, 300), (65, 5, 3, 272, 96), (33, 64, 6, 256, 160), (128, 3, 2, 515, 129),
     (300, 8, 2, 384, 512), (520, 4, 2, 256, 640), (40, 100, 1, 31, 17), (2, 16, 4, 2048, 1408),
     (1200, 2, 1, 160, 144), (800, 2, 2, 272, 304), (900, 2, 1, 131, 77),
-    (2, 8, 2, 84, 60), (20, 4, 2, 140, 92), (300, 4, 2, 204, 132)])
+    (2, 8, 2, 84, 60), (20, 4, 2, 140, 92), (300, 4, 2, 204, 132),
+    (300, 4, 2, 203, 130), (4, 4, 2, 129, 66), (1300, 3, 1, 97, 258)])
 def test_sizes(dev, dtype, tokens, E, k, hidden, ffn):
     g = torch.Generator().manual_seed(tokens + E)
     x = torch.randn((tokens, hidden), generator=g).to(DT[dtype])

@@ -103,7 +103,8 @@ SIZES = [(1, 1, 1), (1, 16, 16), (1, 127, 15), (2, 128, 17), (15, 129, 31), (16,
          (17, 256, 33), (31, 1000, 100), (33, 64, 1), (63, 384, 255), (64, 4096, 48),
          (65, 515, 257), (100, 1, 300), (129, 130, 128), (200, 2048, 520), (256, 1024, 256),
          (257, 1153, 700), (700, 640, 1030), (1, 65536, 40), (40, 65535, 20), (1, 4096, 4099),
-         (3, 30000, 17), (1, 132, 50), (9, 1004, 70), (40, 260, 90), (300, 1460, 300), (600, 2052, 516)]
+         (3, 30000, 17), (1, 132, 50), (9, 1004, 70), (40, 260, 90), (300, 1460, 300), (600, 2052, 516),
+         (1, 4097, 3), (16, 126, 2), (16, 257, 1), (30, 1023, 301), (128, 1290, 66), (520, 2049, 1027)]
 
 
 @pytest.mark.parametrize("m,k,n", SIZES)
