@@ -16,7 +16,7 @@ struct Bank {
   int32_t scale_dtype;
 };
 struct ExpertArgs {
-  uint64_t offsets, order, ids, weights;
+  uint64_t table, order, ids, weights;
   uint64_t x, ldx;
   uint64_t xq, xscale;    // quantised x, by token
   uint64_t h;             // fp32, by place in the order
@@ -25,58 +25,22 @@ struct ExpertArgs {
   uint64_t out;           // experts' results, fp32, by slot
   uint64_t y, ldy;
   uint32_t tokens, k, experts, hidden, ffn, slots;
-  uint32_t blocks;        // upper bound of the tiles of places, tile kernels only
+  uint32_t blocks;        // upper bound of the blocks of places
   int32_t dtype;
   Bank gate, up, down;
 };
 
-// Which expert the tile-th block of kRows places of the order belongs to, blocks
-// counted expert by expert: the places are [first, last).  False past the last
-// block.  Every wave works it out for itself.
-template <int kRows>
-__device__ __forceinline__ bool tile_of(const ExpertArgs& a, uint32_t tile, uint32_t& expert,
-                                        uint32_t& first, uint32_t& last) {
-  const uint32_t lane = threadIdx.x % 64;
-  uint32_t done = 0;
-  for (uint32_t e0 = 0; e0 < a.experts; e0 += 64) {
-    const uint32_t e = e0 + lane;
-    uint32_t from = 0, to = 0;
-    if (e < a.experts) {
-      from = min(uint32_t(max(global<const int32_t>(a.offsets)[e], 0)), a.slots);
-      to = min(uint32_t(max(global<const int32_t>(a.offsets)[e + 1], 0)), a.slots);
-    }
-    uint32_t blocks = to > from ? (to - from + kRows - 1) / kRows : 0, sum = blocks;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t v = uint32_t(__shfl_up(int(sum), d));
-      if (lane >= uint32_t(d)) sum += v;
-    }
-    const uint64_t past = __ballot(done + sum > tile);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      expert = e0 + uint32_t(at);
-      const uint32_t before = done + uint32_t(__shfl(int(sum - blocks), at));
-      first = uint32_t(__shfl(int(from), at)) + (tile - before) * kRows;
-      last = min(uint32_t(__shfl(int(to), at)), first + kRows);
-      return true;
-    }
-    done += uint32_t(__shfl(int(sum), 63));
-  }
-  return false;
+// The block-th block of places (Blocks): false past the last.
+struct Place {
+  uint32_t expert, first, last;
+};
+__device__ __forceinline__ uint32_t block_count(const ExpertArgs& a) {
+  return __builtin_amdgcn_readfirstlane(*global<const uint32_t>(a.table));
 }
-
-// How many blocks of kRows places the experts' rows fill.
-template <int kRows>
-__device__ __forceinline__ uint32_t tile_count(const ExpertArgs& a) {
-  uint32_t blocks = 0;
-  for (uint32_t e = threadIdx.x % 64; e < a.experts; e += 64) {
-    const uint32_t from = min(uint32_t(max(global<const int32_t>(a.offsets)[e], 0)), a.slots);
-    const uint32_t to = min(uint32_t(max(global<const int32_t>(a.offsets)[e + 1], 0)), a.slots);
-    blocks += to > from ? (to - from + kRows - 1) / kRows : 0;
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) blocks += uint32_t(__shfl_xor(int(blocks), d));
-  return min(uint32_t(__builtin_amdgcn_readfirstlane(blocks)), a.blocks);
+__device__ __forceinline__ Place block_at(const ExpertArgs& a, uint32_t block) {
+  const u32x4 v = global<const u32x4>(a.table)[block + 1];
+  return {uint32_t(__builtin_amdgcn_readfirstlane(v[0])), uint32_t(__builtin_amdgcn_readfirstlane(v[1])),
+          uint32_t(__builtin_amdgcn_readfirstlane(v[2]))};
 }
 
 __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place) {
@@ -132,8 +96,8 @@ __device__ __forceinline__ int32_t summed(const int32_t (&part)[kRowWaves][kMats
 // h = silu(gate x) * (up x) of 16 columns for up to 16 places of the order.
 __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_up_kernel(ExpertArgs a) {
   __shared__ int32_t part[kRowWaves][2 * 256];
-  uint32_t e, first, last;
-  if (!tile_of<16>(a, blockIdx.x, e, first, last)) return;
+  if (blockIdx.x >= block_count(a)) return;
+  const auto [e, first, last] = block_at(a, blockIdx.x);
   const uint32_t n0 = blockIdx.y * 16, r = threadIdx.x % 16;
   const uint32_t token = slot_at(a, min(first + r, last - 1)) / a.k;
   const uint64_t mats[2] = {a.gate.w + e * a.gate.stride, a.up.w + e * a.up.stride};
@@ -155,8 +119,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_up_kernel(ExpertArg
 // down(h) of 16 columns for up to 16 places, stored by slot.
 __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertArgs a) {
   __shared__ int32_t part[kRowWaves][256];
-  uint32_t e, first, last;
-  if (!tile_of<16>(a, blockIdx.x, e, first, last)) return;
+  if (blockIdx.x >= block_count(a)) return;
+  const auto [e, first, last] = block_at(a, blockIdx.x);
   const uint32_t n0 = blockIdx.y * 16, r = threadIdx.x % 16;
   const uint64_t mats[2] = {a.down.w + e * a.down.stride, 0};
   expert_product<1>(global<const uint8_t>(a.hq) + min(first + r, last - 1) * WC_I8_ROW_BYTES(a.ffn),
@@ -179,9 +143,8 @@ template <int kX>
 __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_kernel(ExpertArgs a) {
   using R = ExpertRing<kX>;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
-  uint32_t e, first, last;
-  if (!tile_of<kX>(a, blockIdx.x, e, first, last)) return;
-  e = __builtin_amdgcn_readfirstlane(e);
+  if (blockIdx.x >= block_count(a)) return;
+  const auto [e, first, last] = block_at(a, blockIdx.x);
   const uint32_t k = a.hidden, step = steps_of(k), blocks = ((a.ffn + step - 1) / step + 7) / 8;
   const uint32_t class0 = blockIdx.y / blocks, r0 = blockIdx.y % blocks * 8;
   const ClassRows G = class_rows(a.gate.w + e * a.gate.stride, k, a.ffn, k, step, class0);
@@ -218,11 +181,8 @@ template <int kX>
 __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring_kernel(ExpertArgs a) {
   using R = ExpertRing<kX>;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
-  uint32_t e, first, last;
-  if (!tile_of<kX>(a, blockIdx.x, e, first, last)) return;
-  e = __builtin_amdgcn_readfirstlane(e);
-  first = __builtin_amdgcn_readfirstlane(first);
-  last = __builtin_amdgcn_readfirstlane(last);
+  if (blockIdx.x >= block_count(a)) return;
+  const auto [e, first, last] = block_at(a, blockIdx.x);
   const uint32_t k = a.ffn, step = steps_of(k), blocks = ((a.hidden + step - 1) / step + 15) / 16;
   const uint32_t class0 = blockIdx.y / blocks, r0 = blockIdx.y % blocks * 16;
   const ClassRows C = class_rows(a.down.w + e * a.down.stride, k, a.hidden, k, step, class0);
@@ -417,12 +377,9 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
   const uint32_t k = a.hidden, step = kQuads ? 1 : steps_of(k);
   // classes of the same columns one after another, so that their stores meet in a cache
   const uint32_t blocks = ((a.ffn + step - 1) / step + kCols - 1) / kCols;
-  uint32_t mt, nt, e, first, last;
-  if (!tile_at(blockIdx.x, tile_count<kBM>(a), blocks * step, mt, nt)) return;
-  if (!tile_of<kBM>(a, mt, e, first, last)) return;
-  e = __builtin_amdgcn_readfirstlane(e);
-  first = __builtin_amdgcn_readfirstlane(first);
-  last = __builtin_amdgcn_readfirstlane(last);
+  uint32_t mt, nt;
+  if (!tile_at(blockIdx.x, block_count(a), blocks * step, mt, nt)) return;
+  const auto [e, first, last] = block_at(a, mt);
   const uint32_t class0 = nt % step, r0 = nt / step * kCols;
   const ClassRows G = class_rows(a.gate.w + e * a.gate.stride, k, a.ffn, k, step, class0);
   const ClassRows U = class_rows(a.up.w + e * a.up.stride, k, a.ffn, k, step, class0);
@@ -499,12 +456,9 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
   const uint32_t k = a.ffn, step = kQuads ? 1 : steps_of(k);
   const uint32_t blocks = ((a.hidden + step - 1) / step + kBN - 1) / kBN;
-  uint32_t mt, nt, e, first, last;
-  if (!tile_at(blockIdx.x, tile_count<kBM>(a), blocks * step, mt, nt)) return;
-  if (!tile_of<kBM>(a, mt, e, first, last)) return;
-  e = __builtin_amdgcn_readfirstlane(e);
-  first = __builtin_amdgcn_readfirstlane(first);
-  last = __builtin_amdgcn_readfirstlane(last);
+  uint32_t mt, nt;
+  if (!tile_at(blockIdx.x, block_count(a), blocks * step, mt, nt)) return;
+  const auto [e, first, last] = block_at(a, mt);
   const uint32_t class0 = nt % step, r0 = nt / step * kBN, m_rows = last - first;
   const ClassRows C = class_rows(a.down.w + e * a.down.stride, k, a.hidden, k, step, class0);
   if (r0 >= C.rows) return;
@@ -587,10 +541,15 @@ __global__ __launch_bounds__(256) void wc_experts_join_kernel(ExpertArgs a) {
     if (n + i < a.hidden) store_float(a.y, a.dtype, token * a.ldy + n + i, sum[i]);
 }
 
+// Blocks of `rows` places: every expert that has places ends in one that may not be full.
+uint64_t most_blocks(uint32_t slots, uint32_t experts, uint32_t rows) {
+  return uint64_t(slots) / rows + (experts < slots ? experts : slots);
+}
+
 struct Workspace {
-  uint64_t xq, xscale, wide, hq, hscale, xcopies, hcopies, bytes;
+  uint64_t xq, xscale, wide, hq, hscale, xcopies, hcopies, table, bytes;
 };
-Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
+Workspace layout(uint64_t tokens, uint64_t k, uint64_t experts, uint64_t hidden, uint64_t ffn) {
   Workspace w{};
   uint64_t at = 0;
   const auto take = [&](uint64_t bytes) {
@@ -598,6 +557,7 @@ Workspace layout(uint64_t tokens, uint64_t k, uint64_t hidden, uint64_t ffn) {
     at += pad256(bytes);
     return here;
   };
+  w.table = take((1 + most_blocks(uint32_t(tokens * k), uint32_t(experts), 8)) * 16);
   w.xq = take(tokens * WC_I8_ROW_BYTES(hidden));
   w.xscale = take(tokens * 4);
   // h, and after its quantisation the experts' results and a row for what is past them
@@ -633,15 +593,40 @@ bool reached(const wc_i8_experts* b, uint32_t k) {
 // 33.7 at two, 43.4 and 52.8 at four.
 constexpr uint32_t kSlotTokens = 4, kHoldBytes = 12 * 1024;
 
-// Rows of the order to a tile, by the rows an expert has on average.
-int tile_rows(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden, bool direct) {
+using Tile64 = Tile<64, 128, 1, 2, 3>;
+using Tile128 = Tile<128, 128, 2, 2, 3>;
+using Tile256 = Tile<256, 256, 2, 4>;
+template <class F>
+void with_tile(int tile, F f) {
+  switch (tile) {
+    case 1: return f(Tile64{});
+    case 2: return f(Tile128{});
+    case 3: return f(Tile256{});
+    default: return;
+  }
+}
+
+// The kernel, by the rows an expert has on average: a tile (0: none) of `rows` places, or
+// rings of 8 or 16, or (0) the one for matrices at any address.
+struct Chosen {
+  int tile;
+  uint32_t rows;
+};
+Chosen choose(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden, uint32_t ffn,
+              bool direct) {
   // tiles find x by 32-bit offsets
-  if (!direct || tokens * WC_I8_ROW_BYTES(hidden + 3) >> 32) return 0;
+  if (!direct || tokens * WC_I8_ROW_BYTES(hidden + 3) >> 32) return {0, 0};
+  // us on rings, and tiles of 64, 128 and 256 places (8 experts of 4096 x 14336, 2 a token;
+  // 64 of 2048 x 1408, 6 a token; 8 of 6144 x 16384):
+  //   average 4: 283 (8 experts), 274, 269, 392; 6: 152, 132, 161, 169; 8: 558, 473, 506, 578;
+  //   32: 594, 294, 313, 400; 64: 943, 375, 337, 428, and 609, 202, 205, 214;
+  //   150: -, 559, 518, 500; 187: -, 342, 330, 287; 1024: -, 4370, 3613, 2760
   const uint32_t average = slots / experts;
-  if (average >= 384) return 256;
-  if (average >= 24) return 128;
+  if (average >= 120) return {3, 256};
+  if (average >= 64) return {2, 128};
+  if (average >= 4) return {1, 64};
   // a token takes an expert once
-  return tokens <= 8 ? 8 : 16;
+  return {0, tokens <= 8 ? 8u : 16u};
 }
 
 uint32_t columns(uint32_t n, uint32_t step, uint32_t each) {
@@ -669,7 +654,7 @@ extern "C" wc_status wc_experts_i8_workspace_bytes(uint32_t tokens, uint32_t k, 
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
   if (!sizes_ok(tokens, k, experts, hidden, ffn)) return WC_EINVAL;
-  *bytes = layout(tokens, k, hidden, ffn).bytes;
+  *bytes = layout(tokens, k, experts, hidden, ffn).bytes;
   return WC_OK;
 }
 
@@ -691,13 +676,13 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   if (off(dev_x, size_of(dtype)) || off(dev_y, size_of(dtype)) || off(dev_ids, 4) ||
       off(dev_weights, 4) || off(dev_offsets, 4) || off(dev_order, 4))
     return WC_EINVAL;
-  const Workspace w = layout(tokens, k, hidden, ffn);
+  const Workspace w = layout(tokens, k, experts, hidden, ffn);
   if (off(dev_workspace, 256) || workspace_bytes < w.bytes) return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const uint64_t ws = reinterpret_cast<uint64_t>(dev_workspace);
   const uint32_t slots = tokens * k;
   ExpertArgs a{};
-  a.offsets = reinterpret_cast<uint64_t>(dev_offsets);
+  a.table = ws + w.table;
   a.order = reinterpret_cast<uint64_t>(dev_order);
   a.ids = reinterpret_cast<uint64_t>(dev_ids);
   a.weights = reinterpret_cast<uint64_t>(dev_weights);
@@ -744,19 +729,21 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
                        DownSlotRing::kLds + uint32_t(hold_h) + k * DownSlotRing::kThreads, st, a);
     return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
   }
+  const Chosen kernel = choose(tokens, slots, experts, hidden, ffn, direct);
+  const uint32_t rows = kernel.rows;
+  const uint32_t block_rows = rows ? rows : 16;
+  a.blocks = uint32_t(most_blocks(slots, experts, block_rows));
+  const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(dev_offsets), experts, slots, block_rows,
+                         a.blocks};
   if (!launch_quantize(dev_x, dtype, tokens, hidden, ldx, reinterpret_cast<void*>(a.xq),
-                       reinterpret_cast<float*>(a.xscale), st))
+                       reinterpret_cast<float*>(a.xscale), st, nullptr, &blocks))
     return WC_EHIP;
   if (hidden % 4 && !launch_shift(reinterpret_cast<const void*>(a.xq), tokens, hidden,
                                   reinterpret_cast<void*>(a.xcopies), st))
     return WC_EHIP;
-  const int rows = tile_rows(tokens, slots, experts, hidden, direct);
-  // every expert that has rows ends in at most one block that is not full
-  a.blocks = slots / uint32_t(rows ? rows : 16) + (experts < slots ? experts : slots);
   const dim3 up_grid(a.blocks, rows ? columns(ffn, steps_of(hidden), 8) : (ffn + 15) / 16);
   const dim3 down_grid(a.blocks, rows ? columns(hidden, steps_of(ffn), 16) : (hidden + 15) / 16);
-  if (rows == 256) start_up<Tile<256, 256, 2, 4>>(a, st);
-  else if (rows == 128) start_up<Tile<128, 128, 2, 2>>(a, st);
+  if (kernel.tile) with_tile(kernel.tile, [&](auto t) { start_up<decltype(t)>(a, st); });
   else if (rows == 16)
     hipLaunchKernelGGL((wc_experts_up_ring_kernel<16>), up_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
   else if (rows == 8)
@@ -771,8 +758,7 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   if (ffn % 4 && !launch_shift(reinterpret_cast<const void*>(a.hq), slots, ffn,
                                reinterpret_cast<void*>(a.hcopies), st, dev_offsets + experts))
     return WC_EHIP;
-  if (rows == 256) start_down<Tile<256, 256, 2, 4>>(a, st);
-  else if (rows == 128) start_down<Tile<128, 128, 2, 2>>(a, st);
+  if (kernel.tile) with_tile(kernel.tile, [&](auto t) { start_down<decltype(t)>(a, st); });
   else if (rows == 16)
     hipLaunchKernelGGL((wc_experts_down_ring_kernel<16>), down_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
   else if (rows == 8)

@@ -108,10 +108,19 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
 }
 
+// Which places of the experts' order a workgroup multiplies: blocks of `rows` places,
+// counted expert by expert.  Entry 0 of the table holds the number of blocks, entry b + 1
+// block b's {expert, first place, past the last place, 0}.
+struct Blocks {
+  uint64_t table, offsets;
+  uint32_t experts, slots, rows, most;
+};
+
 // Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes
-// (wc_i8.hip), or as many of them as the device int `rows` says; false on a launch
-// error.
+// (wc_i8.hip), or as many of them as the device int `limit` says; with `blocks`, one more
+// workgroup writes its table.  False on a launch error.
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     float* scale, hipStream_t stream, const int32_t* rows = nullptr);
+                     float* scale, hipStream_t stream, const int32_t* limit = nullptr,
+                     const Blocks* blocks = nullptr);
 
 }  // namespace wc_i8

@@ -10,9 +10,52 @@ namespace {
 using namespace wc_i8;
 
 struct QuantArgs {
-  uint64_t x, ldx, q, scale, rows;
-  uint32_t k, vector;  // vector: rows are 16-byte aligned
+  uint64_t x, ldx, q, scale, limit;
+  uint32_t m, k, vector;  // vector: rows are 16-byte aligned
+  Blocks blocks;
 };
+
+// The table of `Blocks`, by one workgroup.
+template <int kThreads>
+__device__ __forceinline__ void write_blocks(const Blocks& b, uint32_t (&starts)[kMaxExperts + 1]) {
+  const auto offset = [&](uint32_t e) -> uint32_t {
+    const int32_t at = global<const int32_t>(b.offsets)[e];
+    return at < 0 ? 0u : uint32_t(at) < b.slots ? uint32_t(at) : b.slots;
+  };
+  for (uint32_t e = threadIdx.x; e < b.experts; e += kThreads) {
+    const uint32_t from = offset(e), to = offset(e + 1);
+    starts[e + 1] = to > from ? (to - from + b.rows - 1) / b.rows : 0;
+  }
+  if (threadIdx.x == 0) starts[0] = 0;
+  __syncthreads();
+  // the blocks before each expert
+  if (threadIdx.x < 64) {
+    uint32_t before = 0;
+    for (uint32_t e0 = 1; e0 <= b.experts; e0 += 64) {
+      const uint32_t e = e0 + threadIdx.x;
+      uint32_t sum = e <= b.experts ? starts[e] : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint32_t v = uint32_t(__shfl_up(int(sum), d));
+        if (threadIdx.x >= uint32_t(d)) sum += v;
+      }
+      if (e <= b.experts) starts[e] = before + sum;
+      before += uint32_t(__shfl(int(sum), 63));
+    }
+  }
+  __syncthreads();
+  const uint32_t all = min(starts[b.experts], b.most);
+  if (threadIdx.x == 0) *global<u32x4>(b.table) = u32x4{all, 0, 0, 0};
+  for (uint32_t t = threadIdx.x; t < all; t += kThreads) {
+    uint32_t low = 0, high = b.experts;  // starts[low] <= t < starts[high]
+    while (high - low > 1) {
+      const uint32_t middle = (low + high) / 2;
+      (starts[middle] <= t ? low : high) = middle;
+    }
+    const uint32_t first = offset(low) + (t - starts[low]) * b.rows, end = offset(low + 1);
+    global<u32x4>(b.table)[t + 1] = u32x4{low, first, end < first + b.rows ? end : first + b.rows, 0u};
+  }
+}
 
 // One workgroup a row, which its threads hold in registers in units of eight elements
 // (thread t has units t, t + kThreads, ...): read once, its largest magnitude found,
@@ -23,7 +66,11 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
   constexpr int kWords = kType == WC_FP32 ? 8 : 4;  // to a unit
   __shared__ uint32_t tops[kThreads / 64];
   const uint64_t row = blockIdx.x;
-  if (a.rows && int32_t(blockIdx.x) >= *global<const int32_t>(a.rows)) return;
+  if (blockIdx.x == a.m) {
+    __shared__ uint32_t starts[kMaxExperts + 1];
+    return write_blocks<kThreads>(a.blocks, starts);
+  }
+  if (a.limit && int32_t(blockIdx.x) >= *global<const int32_t>(a.limit)) return;
   const uint64_t first = a.x + row * a.ldx * (kType == WC_FP32 ? 4 : 2);
   const uint32_t units = uint32_t(WC_I8_ROW_BYTES(a.k)) / 8;
   uint32_t v[kUnits][kWords];
@@ -82,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
 
 template <int kThreads, int kUnits>
 void start_quantize(int32_t dt, uint32_t m, const QuantArgs& a, hipStream_t stream) {
-  const dim3 grid(m), block(kThreads);
+  const dim3 grid(m + (a.blocks.table != 0)), block(kThreads);
   if (dt == WC_BF16)
     hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_BF16>), grid, block, 0, stream, a);
   else if (dt == WC_FP16)
@@ -642,11 +689,12 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
 namespace wc_i8 {
 
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     float* scale, hipStream_t stream, const int32_t* rows) {
+                     float* scale, hipStream_t stream, const int32_t* limit, const Blocks* blocks) {
   const uint32_t size = size_of(dt);
   const QuantArgs a = {reinterpret_cast<uint64_t>(x), ldx, reinterpret_cast<uint64_t>(q),
-                       reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(rows), k,
-                       reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * size % 16 == 0};
+                       reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(limit), m, k,
+                       reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * size % 16 == 0,
+                       blocks ? *blocks : Blocks{}};
   // few rows: more threads to each
   if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, m, a, stream);
   else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, m, a, stream);
