@@ -736,10 +736,8 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(dev_offsets), experts, slots, block_rows,
                          a.blocks};
   if (!launch_quantize(dev_x, dtype, tokens, hidden, ldx, reinterpret_cast<void*>(a.xq),
-                       reinterpret_cast<float*>(a.xscale), st, nullptr, &blocks))
-    return WC_EHIP;
-  if (hidden % 4 && !launch_shift(reinterpret_cast<const void*>(a.xq), tokens, hidden,
-                                  reinterpret_cast<void*>(a.xcopies), st))
+                       reinterpret_cast<float*>(a.xscale), st, nullptr, &blocks,
+                       hidden % 4 ? reinterpret_cast<void*>(a.xcopies) : nullptr))
     return WC_EHIP;
   const dim3 up_grid(a.blocks, rows ? columns(ffn, steps_of(hidden), 8) : (ffn + 15) / 16);
   const dim3 down_grid(a.blocks, rows ? columns(hidden, steps_of(ffn), 16) : (hidden + 15) / 16);
@@ -753,10 +751,8 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
   if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, pitch_of(ffn),
                        reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st,
-                       dev_offsets + experts))
-    return WC_EHIP;
-  if (ffn % 4 && !launch_shift(reinterpret_cast<const void*>(a.hq), slots, ffn,
-                               reinterpret_cast<void*>(a.hcopies), st, dev_offsets + experts))
+                       dev_offsets + experts, nullptr,
+                       ffn % 4 ? reinterpret_cast<void*>(a.hcopies) : nullptr))
     return WC_EHIP;
   if (kernel.tile) with_tile(kernel.tile, [&](auto t) { start_down<decltype(t)>(a, st); });
   else if (rows == 16)

@@ -13,6 +13,7 @@ namespace wc_i8 {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(1)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -118,9 +119,10 @@ struct Blocks {
 
 // Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes
 // (wc_i8.hip), or as many of them as the device int `limit` says; with `blocks`, one more
-// workgroup writes its table.  False on a launch error.
+// workgroup writes its table; with `copies`, their shifted copies (wc_i8_tile.h) too.
+// False on a launch error.
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
                      float* scale, hipStream_t stream, const int32_t* limit = nullptr,
-                     const Blocks* blocks = nullptr);
+                     const Blocks* blocks = nullptr, void* copies = nullptr);
 
 }  // namespace wc_i8

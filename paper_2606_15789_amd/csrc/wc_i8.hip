@@ -11,7 +11,8 @@ using namespace wc_i8;
 
 struct QuantArgs {
   uint64_t x, ldx, q, scale, limit;
-  uint32_t m, k, vector;  // vector: rows are 16-byte aligned
+  uint64_t copies;  // three shifted copies of q (Shifted), or none
+  uint32_t m, k;
   Blocks blocks;
 };
 
@@ -77,8 +78,9 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
 #pragma unroll
   for (int u = 0; u < kUnits; u++) {
     const uint32_t at = (threadIdx.x + u * kThreads) * 8;
-    if (a.vector && at + 8 <= a.k) {
-      const auto p = global<const u32x4>(first + at * (kType == WC_FP32 ? 4 : 2));
+    if (at + 8 <= a.k) {
+      // rows at any element: as the codes of W, loads of any alignment
+      const auto p = global<const u32x4u>(first + at * (kType == WC_FP32 ? 4 : 2));
 #pragma unroll
       for (int i = 0; i < kWords / 4; i++) {
         const u32x4 w = p[i];
@@ -115,16 +117,34 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
   for (int w = 0; w < kThreads / 64; w++) top = max(top, tops[w]);
   const RowScale s = row_scale(top);
   const auto out = global<u32x2>(a.q + row * units * 8);
+  u32x2 codes[kUnits];
 #pragma unroll
   for (int u = 0; u < kUnits; u++) {
     const uint32_t unit = threadIdx.x + u * kThreads;
-    if (unit >= units) continue;
     u32x2 c = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; i++) c[i / 4] |= code_of(value(u, i), s.inverse) << (8 * (i % 4));
-    out[unit] = c;
+    codes[u] = c;
+    if (unit < units) out[unit] = c;
   }
   if (threadIdx.x == 0) global<float>(a.scale)[row] = s.scale;
+  if (!a.copies) return;
+  // The shifted copies: every unit at its place and one to three bytes, then zeros to the
+  // row's end and before its start.  What passes a row's end are zeros of padding, at the
+  // zeros before the next row (the last row's: in the workspace's padding).
+  const uint32_t wide = uint32_t(WC_I8_ROW_BYTES(a.k + 3)) / 8;
+#pragma unroll
+  for (uint32_t by = 1; by <= 3; by++) {
+    const uint64_t to = a.copies + ((by - 1) * uint64_t(a.m) + row) * wide * 8 + by;
+#pragma unroll
+    for (int u = 0; u < kUnits; u++) {
+      const uint32_t unit = threadIdx.x + u * kThreads;
+      if (unit < units) *global<u32x2u>(to + unit * 8) = codes[u];
+    }
+    for (uint32_t unit = units + threadIdx.x; unit < wide; unit += kThreads)
+      *global<u32x2u>(to + unit * 8) = u32x2{0, 0};
+    if (threadIdx.x < by) *global<uint8_t>(to - by + threadIdx.x) = 0;
+  }
 }
 
 template <int kThreads, int kUnits>
@@ -139,10 +159,9 @@ void start_quantize(int32_t dt, uint32_t m, const QuantArgs& a, hipStream_t stre
 }
 
 // Word i of three copies of a row of q, shifted by one, two and three bytes.
-__global__ __launch_bounds__(256) void wc_shift_i8_kernel(uint64_t q, uint64_t copies, uint64_t limit,
-                                                          uint32_t m, uint32_t k) {
+__global__ __launch_bounds__(256) void wc_shift_i8_kernel(uint64_t q, uint64_t copies, uint32_t m,
+                                                          uint32_t k) {
   const uint64_t row = blockIdx.x;
-  if (limit && int32_t(blockIdx.x) >= *global<const int32_t>(limit)) return;
   const uint32_t words = uint32_t(WC_I8_ROW_BYTES(k)) / 4, wide = uint32_t(WC_I8_ROW_BYTES(k + 3)) / 4;
   const auto from = global<const uint32_t>(q) + row * words;
   for (uint32_t i = threadIdx.x; i < wide; i += 256) {
@@ -615,10 +634,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
                  const wc_i8_job* jobs, const Plan& p, void* workspace, hipStream_t stream,
                  const void* x = nullptr, int32_t x_dtype = 0, uint64_t ldx = 0) {
   MatArgs a{};
-  if (p.copies) {
-    if (!launch_shift(q, m, k, workspace, stream)) return WC_EHIP;
-    a.copies = reinterpret_cast<uint64_t>(workspace);
-  }
+  if (p.copies) a.copies = reinterpret_cast<uint64_t>(workspace);
   a.x = reinterpret_cast<uint64_t>(x);
   a.ldx = ldx;
   a.q = reinterpret_cast<uint64_t>(q);
@@ -689,12 +705,11 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
 namespace wc_i8 {
 
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     float* scale, hipStream_t stream, const int32_t* limit, const Blocks* blocks) {
-  const uint32_t size = size_of(dt);
+                     float* scale, hipStream_t stream, const int32_t* limit, const Blocks* blocks,
+                     void* copies) {
   const QuantArgs a = {reinterpret_cast<uint64_t>(x), ldx, reinterpret_cast<uint64_t>(q),
-                       reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(limit), m, k,
-                       reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * size % 16 == 0,
-                       blocks ? *blocks : Blocks{}};
+                       reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(limit),
+                       reinterpret_cast<uint64_t>(copies), m, k, blocks ? *blocks : Blocks{}};
   // few rows: more threads to each
   if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, m, a, stream);
   else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, m, a, stream);
@@ -704,13 +719,6 @@ bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t
   else if (k <= 16384) start_quantize<256, 8>(dt, m, a, stream);
   else if (k <= 32768) start_quantize<1024, 4>(dt, m, a, stream);
   else start_quantize<1024, 8>(dt, m, a, stream);
-  return hipGetLastError() == hipSuccess;
-}
-
-bool launch_shift(const void* q, uint32_t m, uint32_t k, void* copies, hipStream_t stream,
-                  const int32_t* limit) {
-  hipLaunchKernelGGL(wc_shift_i8_kernel, dim3(m), dim3(256), 0, stream, reinterpret_cast<uint64_t>(q),
-                     reinterpret_cast<uint64_t>(copies), reinterpret_cast<uint64_t>(limit), m, k);
   return hipGetLastError() == hipSuccess;
 }
 
@@ -755,8 +763,13 @@ extern "C" wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, u
   Plan p = plan_of(m, k, n_jobs, jobs);
   p.hold = false;
   if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p, m, k))) return WC_EINVAL;
-  return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, p, dev_workspace,
-                reinterpret_cast<hipStream_t>(stream));
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (p.copies) {
+    hipLaunchKernelGGL(wc_shift_i8_kernel, dim3(m), dim3(256), 0, st, reinterpret_cast<uint64_t>(dev_q),
+                       reinterpret_cast<uint64_t>(dev_workspace), m, k);
+    if (hipGetLastError() != hipSuccess) return WC_EHIP;
+  }
+  return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, p, dev_workspace, st);
 }
 
 extern "C" wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
@@ -784,6 +797,8 @@ extern "C" wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m
   void* parts = reinterpret_cast<uint8_t*>(scale) + pad256(uint64_t(m) * 4);
   Plan p = plan_of(m, k, n_jobs, jobs);
   p.hold = p.hold && reinterpret_cast<uintptr_t>(dev_x) % 16 == 0 && ldx * size_of(x_dtype) % 16 == 0;
-  if (!p.hold && !launch_quantize(dev_x, x_dtype, m, k, ldx, q, scale, st)) return WC_EHIP;
+  if (!p.hold && !launch_quantize(dev_x, x_dtype, m, k, ldx, q, scale, st, nullptr, nullptr,
+                                  p.copies ? parts : nullptr))
+    return WC_EHIP;
   return matmul(q, scale, m, k, n_jobs, jobs, p, parts, st, dev_x, x_dtype, ldx);
 }

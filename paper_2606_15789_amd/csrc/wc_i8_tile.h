@@ -247,11 +247,9 @@ __device__ __forceinline__ Shifted shifted(uint64_t q, uint64_t copies, uint64_t
   const uint32_t pitch = uint32_t(WC_I8_ROW_BYTES(k + 3));
   return {copies + (shift - 1) * (rows * pitch), pitch};
 }
-inline uint64_t copies_bytes(uint64_t rows, uint64_t k) { return pad256(3 * rows * WC_I8_ROW_BYTES(k + 3)); }
-// Make the three copies of m rows (or as many as the device int `limit` says); false on a
-// launch error (wc_i8.hip).
-bool launch_shift(const void* q, uint32_t m, uint32_t k, void* copies, hipStream_t stream,
-                  const int32_t* limit = nullptr);
+inline uint64_t copies_bytes(uint64_t rows, uint64_t k) {
+  return pad256(3 * rows * WC_I8_ROW_BYTES(k + 3) + 16);
+}
 
 // Which tile a workgroup takes, so that those that run at once on one of the eight
 // dies (workgroup i goes to die i mod 8, each with its own L2) share rows: each die

@@ -122,6 +122,7 @@ def test_linear_sizes(dev, m, k, n):
     y, = wc.matmul_i8_torch(*wc.quantize_i8_torch(x.to(dev)), k, [w.to(dev)], [ws.to(dev)])
     assert y.dtype == torch.bfloat16
     _check(y, q, s, w, ws, None)
+    assert torch.equal(y, wc.linear_i8_torch(x.to(dev), [w.to(dev)], [ws.to(dev)])[0])
 
 
 @pytest.mark.parametrize("m", [1, 20, 300])
