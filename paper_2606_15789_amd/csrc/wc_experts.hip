@@ -155,15 +155,16 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_k
   const u32x4 gr = rows_rsrc(G.base + r0 * uint64_t(G.pitch), (n_rows - 1) * G.pitch + G.bytes);
   const u32x4 ur = rows_rsrc(U.base + r0 * uint64_t(G.pitch), (n_rows - 1) * G.pitch + G.bytes);
   const u32x4 xr = rows_rsrc(X.base, a.tokens * X.pitch);
-  const uint32_t woff = min(R::row_of(), n_rows - 1) * G.pitch + R::byte_of();
+  const uint32_t row = min(R::row_of(), n_rows - 1) * G.pitch;
+  const uint32_t woff[2] = {row + R::byte_of(0), row + R::byte_of(1)};
   uint32_t xoff[kX / 8];
 #pragma unroll
   for (int i = 0; i < kX / 8; i++)
-    xoff[i] = slot_at(a, min(first + 8 * i + R::row_of(), last - 1)) / a.k * X.pitch + R::byte_of();
+    xoff[i] = slot_at(a, min(first + 8 * i + R::row_of(), last - 1)) / a.k * X.pitch + R::byte_of(i);
   i32x4 acc[1];
   R::product(lds, (G.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
-             [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff + at); }, acc,
+             [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff[i] + at); }, acc,
              [] { return typename R::Held{}; });
   R::gather(lds, acc);
   for (uint32_t o = threadIdx.x; o < 8 * kX; o += R::kThreads) {
@@ -193,9 +194,9 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring
   const u32x4 xr = rows_rsrc(X.base + uint64_t(first) * X.pitch, m_rows * X.pitch);
   uint32_t woff[2], xoff[kX / 8];
 #pragma unroll
-  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of();
+  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of(i);
 #pragma unroll
-  for (int i = 0; i < kX / 8; i++) xoff[i] = min(8 * i + R::row_of(), m_rows - 1) * X.pitch + R::byte_of();
+  for (int i = 0; i < kX / 8; i++) xoff[i] = min(8 * i + R::row_of(), m_rows - 1) * X.pitch + R::byte_of(i);
   i32x4 acc[1];
   R::product(lds, (C.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
@@ -232,10 +233,11 @@ __global__ __launch_bounds__(SlotRing::kThreads) void wc_experts_up_slot_kernel(
   const uint32_t row_bytes = uint32_t(WC_I8_ROW_BYTES(k));
   const u32x4 gr = rows_rsrc(a.gate.w + e * a.gate.stride + uint64_t(n0) * k, n_rows * k);
   const u32x4 ur = rows_rsrc(a.up.w + e * a.up.stride + uint64_t(n0) * k, n_rows * k);
-  const uint32_t woff = min(R::row_of(), n_rows - 1) * k + R::byte_of();
+  const uint32_t row = min(R::row_of(), n_rows - 1) * k;
+  const uint32_t woff[2] = {row + R::byte_of(0), row + R::byte_of(1)};
   i32x4 acc[1];
   R::product(lds, row_bytes / kStage, [](int, uint32_t, uint32_t) {},
-             [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff + at); }, acc, [&] {
+             [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff[i] + at); }, acc, [&] {
                hold_rows<R::kThreads, kType, 2>(
                    1, k, [&](uint32_t) { return a.x + slot / a.k * a.ldx * (kType == WC_FP32 ? 4 : 2); },
                    lds + R::kLds, scale, tops);
@@ -267,7 +269,7 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
   for (uint32_t i = threadIdx.x; i < a.k * kW * 16; i += R::kThreads) part[i] = 0;
   uint32_t woff[2];
 #pragma unroll
-  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * k + R::byte_of();
+  for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * k + R::byte_of(i);
   uint8_t* const mine = lds + wave * R::kWave;
   const uint32_t base = __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>(
       (__attribute__((address_space(3))) uint8_t*)mine)));
@@ -307,7 +309,8 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
       a.k, k, [&](uint32_t r) { return a.h + uint64_t(first + r) * pitch_of(k) * 4; }, lds + R::kLds,
       scales, tops);
   const uint32_t r = lane % 16;
-  const uint32_t w0 = r * kStage + ((lane / 16) ^ (r % 8)) * 16, w1 = r * kStage + ((lane / 16 + 4) ^ (r % 8)) * 16;
+  const uint32_t w0 = r * kStage + ((lane / 16) ^ R::turn(r)) * 16;
+  const uint32_t w1 = r * kStage + ((lane / 16 + 4) ^ R::turn(r)) * 16;
   i32x4 acc = {0, 0, 0, 0};
   const auto leave = [&](uint32_t slot) {
     // every column of the products is the one row of h

@@ -278,8 +278,8 @@ __global__ __launch_bounds__(MatRing<kX>::kThreads) void wc_matmul_i8_ring_kerne
   uint32_t woff[2], xoff[2];
 #pragma unroll
   for (int i = 0; i < 2; i++) {
-    woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of();
-    xoff[i] = min(8 * i + R::row_of(), a.m - 1) * X.pitch + R::byte_of();
+    woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of(i);
+    xoff[i] = min(8 * i + R::row_of(), a.m - 1) * X.pitch + R::byte_of(i);
   }
   i32x4 acc[1];
   R::product(lds, (C.bytes + kStage - 1) / kStage,

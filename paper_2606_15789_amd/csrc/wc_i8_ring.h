@@ -23,10 +23,11 @@ struct Ring {
   static constexpr int kLoads = 2 * kNT + kX / 8;  // of a wave to a stage
   static_assert(kW * kNT * 1024 <= kLds && kLds <= 160 * 1024);
 
-  // Row of its eight and byte of its line that this lane brings.
+  // Row of its eight and byte of its line that this lane brings in load i of W, or of x.
   static __device__ __forceinline__ uint32_t row_of() { return threadIdx.x % 64 / 8; }
-  static __device__ __forceinline__ uint32_t byte_of() {
-    return ((threadIdx.x % 8) ^ (threadIdx.x % 64 / 8)) * 16;
+  static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (row >> 1) & 7; }
+  static __device__ __forceinline__ uint32_t byte_of(int i) {
+    return ((threadIdx.x % 8) ^ turn(8 * i + row_of())) * 16;
   }
 
   template <int N>
@@ -70,12 +71,12 @@ struct Ring {
       if (j < count) start(j, j);
     const Held held = ready();
     // chunk lane / 16 (and four on) of row lane mod 16; of kX rows of x, mod kX
-    const uint32_t r = lane % 16, c0 = (lane / 16) ^ (r % 8), c1 = (lane / 16 + 4) ^ (r % 8);
+    const uint32_t r = lane % 16, c0 = (lane / 16) ^ turn(r), c1 = (lane / 16 + 4) ^ turn(r);
     const uint32_t w0 = r * kStage + c0 * 16, w1 = r * kStage + c1 * 16;
     uint32_t x0, x1;
     if constexpr (kX > 0) {
-      const uint32_t xr = 16 * kNT * kStage + r % kX * kStage;
-      x0 = xr + c0 * 16, x1 = xr + c1 * 16;
+      const uint32_t row = r % kX, xr = 16 * kNT * kStage + row * kStage;
+      x0 = xr + ((lane / 16) ^ turn(row)) * 16, x1 = xr + ((lane / 16 + 4) ^ turn(row)) * 16;
     } else {
       const uint32_t row = min(r, held.rows - 1), at = row * held.pitch + wave * kStage;
       x0 = at + ((lane / 16) ^ (row % 8)) * 16, x1 = at + ((lane / 16 + 4) ^ (row % 8)) * 16;

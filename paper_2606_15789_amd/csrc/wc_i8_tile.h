@@ -4,8 +4,9 @@
 // A stage is kK (64 or 128) bytes of k of every row of the tile.  Both operands go from
 // memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1
 // stages ahead of the products.  A row's 16-byte chunks are stored in the order
-// chunk ^ turn(row): the eight lanes that read LDS together, the same chunk of eight rows
-// next to each other, then touch all banks once.
+// chunk ^ turn(row): the sixteen lanes that read LDS together, the same chunk of sixteen
+// rows next to each other, then touch all 64 banks once (chunk ^ (row mod 8), which is
+// enough for eight lanes, took twice the cycles).
 #pragma once
 
 #include <utility>
@@ -71,10 +72,12 @@ struct Tile {
     return first_row(i) + threadIdx.x % 64 / (kK / 16);
   }
   static __device__ __forceinline__ uint32_t turn(uint32_t row) {
-    return kK == 128 ? row & 7 : (row >> 2) & 3;
+    return kK == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
   }
   static __device__ __forceinline__ uint32_t byte_of() {
-    return ((threadIdx.x % (kK / 16)) ^ turn(threadIdx.x % 64 / (kK / 16))) * 16;
+    // the same for every load: rows kWaves loads apart turn alike
+    static_assert(kWaves % 2 == 0);
+    return ((threadIdx.x % (kK / 16)) ^ turn(row_of(0))) * 16;
   }
 
   // Waits for all but the loads of the newest kLater stages, then for the other waves.
@@ -114,7 +117,7 @@ struct Tile {
     uint32_t at[kQuarters];
 #pragma unroll
     for (int k = 0; k < kQuarters; k++)
-      at[k] = lane % 32 * kK + ((2 * k + lane / 32) ^ turn(lane)) * 16;
+      at[k] = lane % 32 * kK + ((2 * k + lane / 32) ^ turn(lane % 32)) * 16;
     const uint32_t xrow = wm * (kBM / kWM) * kK, wrow = (kBM + wn * (kBN / kWN)) * kK;
     i32x4 x[2][kMT], w[2][kNT];  // operands of two 32-byte quarters of a block
     const auto read = [&](int set, const uint8_t* b, int k, int i) {
@@ -141,7 +144,9 @@ struct Tile {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    constexpr int kHalf = kAll / 2;
+    // two stages: all loads as early as they can be (1546 us against 1583 at m = 8192, k = 8192,
+    // n = 28672); more are spread over two quarters
+    constexpr int kHalf = kDepth == 2 ? kAll : kAll / 2;
     using First = std::integer_sequence<int, 0, kHalf>;
     using Second = std::integer_sequence<int, kHalf, kAll>;
     using None = std::integer_sequence<int, 0, 0>;
@@ -258,7 +263,7 @@ inline uint64_t copies_bytes(uint64_t rows, uint64_t k) {
 // without one): the dies' shares are still even.
 __device__ __forceinline__ bool tile_at(uint32_t id, uint32_t m_tiles, uint32_t n_tiles,
                                         uint32_t& m, uint32_t& n) {
-  constexpr uint32_t kDies = 8, kBand = 8;
+  constexpr uint32_t kDies = 8, kBand = 4;
   const uint32_t all = m_tiles * n_tiles, each = all / kDies, rest = all % kDies;
   const uint32_t die = id % kDies;
   if (id / kDies >= each + (die < rest)) return false;
