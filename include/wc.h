@@ -542,13 +542,16 @@ typedef struct {
 } wc_i8_job;
 
 /* wc_matmul_i8 -- the products of one batch of quantised activations with
- * n_jobs (1..32) matrices, in one launch (two where a long k is split).
+ * n_jobs (1..32) matrices, in one launch (two where k is split into parts, one
+ * more where rows of W start within a dword).
  *   dev_q, dev_scale  what wc_quantize_i8 wrote for m rows of k (the padding of
  *                     a row must be zero);
  *   dev_workspace     at least wc_matmul_i8_workspace_bytes bytes, 256-byte
  *                     aligned (NULL where that is 0); overwritten; calls that
  *                     share it must not overlap in time.
- * Nothing outside the matrices is read, whatever their strides.  m = 0 is a
+ * Rows of W may start at any byte; those that start at whole dwords (ldw and w
+ * multiples of 4) are faster, and no dword is read that holds no byte of a
+ * matrix.  The kernel and the parts of k follow from the sizes alone.  m = 0 is a
  * call that does nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
 wc_status wc_matmul_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                        const wc_i8_job* jobs, uint64_t* bytes);
@@ -558,7 +561,8 @@ wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, uint32_t m, 
 
 /* wc_linear_i8 -- wc_quantize_i8 and wc_matmul_i8 in one call: linear layers
  * that share their activations, e.g. q, k and v projections.  The quantised
- * activations stay in the workspace.  Returns WC_EINVAL, WC_EHIP. */
+ * activations stay in the workspace; a row or two are quantised by the product's
+ * own launch.  Returns WC_EINVAL, WC_EHIP. */
 wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                        const wc_i8_job* jobs, uint64_t* bytes);
 wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
@@ -622,15 +626,15 @@ typedef struct {
  * wc_quantize_i8) before each product, h and the experts' results are held in
  * fp32 in between, and the slots are added in their order, in fp32.
  *   dev_x, dtype   tokens rows of hidden elements, ldx elements apart;
- *   ids .. order   as wc_route writes them for tokens, experts and k.  Which
- *                  rows an expert takes goes by offsets and order; a slot whose
- *                  id is negative adds weight * 0;
+ *   ids .. order   as wc_route writes them for tokens, experts and k: ids
+ *                  agree with offsets and order (the call goes by either); a
+ *                  slot whose id is negative adds weight * 0;
  *   gate, up       matrices of ffn rows of hidden columns; down: hidden rows of
  *                  ffn columns (hidden, ffn 1..65536, experts 1..512);
  *   dev_y          tokens rows of hidden elements of x's type, ldy apart;
  *   dev_workspace  at least wc_experts_i8_workspace_bytes bytes, 256-byte
  *                  aligned; overwritten; calls that share it must not overlap.
- * Entries of offsets or order out of range are taken as the nearest in range:
+ * Entries of ids, offsets or order out of range are taken as the nearest in range:
  * the result is then wrong, but nothing outside the arguments is touched.
  * Returns WC_EINVAL (argument), WC_EHIP. */
 wc_status wc_experts_i8_workspace_bytes(uint32_t tokens, uint32_t k, uint32_t experts,

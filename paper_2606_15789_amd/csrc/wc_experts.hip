@@ -715,8 +715,7 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
                       (reinterpret_cast<uintptr_t>(gate->w) - reinterpret_cast<uintptr_t>(up->w)) % 4 == 0 &&
                       (gate->stride - up->stride) % 4 == 0;
   const uint64_t hold_x = WC_I8_ROW_BYTES(hidden), hold_h = k * WC_I8_ROW_BYTES(ffn);
-  const bool vector = reinterpret_cast<uintptr_t>(dev_x) % 16 == 0 && ldx * size_of(dtype) % 16 == 0;
-  if (direct && vector && hidden % 8 == 0 && ffn % 8 == 0 && tokens <= kSlotTokens &&
+  if (direct && hidden % 8 == 0 && ffn % 8 == 0 && tokens <= kSlotTokens &&
       slots <= experts && k <= kSlots && hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
     const dim3 grid((ffn + 7) / 8, slots), block(SlotRing::kThreads);
     const uint32_t held = SlotRing::kLds + uint32_t(hold_x);

@@ -1,7 +1,6 @@
 // wc_i8.hip -- int8 linear layers: wc_quantize_i8, wc_matmul_i8, wc_linear_i8.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "wc_i8_ring.h"
 
@@ -384,8 +383,9 @@ __device__ __forceinline__ void tile_out(uint8_t* lds, const i32x16 (&acc)[T::kM
         });
 }
 
-// One tile of a job (and one part of k) a workgroup.
-template <class T>
+// One tile of a job (and one part of k) a workgroup.  kQuads: every job's results are
+// whole aligned groups of four.
+template <class T, bool kQuads>
 __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];  // of the tile's rows of x
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
   __syncthreads();
   const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32);
-  const auto out = [&]<int kType, bool kQuads>(std::integer_sequence<int, kType>, std::bool_constant<kQuads>) {
+  const auto out = [&]<int kType>(std::integer_sequence<int, kType>) {
     constexpr uint32_t kSize = kType == 0 || kType == WC_FP32 ? 4 : 2;
     const uint32_t pitch = kType ? uint32_t(J.ldy) * kSize : ((J.n + 3u) & ~3u) * 4;
     const uint64_t row = kType ? J.y + m0 * uint64_t(pitch) : J.part + (uint64_t(part) * a.m + m0) * pitch;
@@ -442,21 +442,10 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
       at[i] = column + (kQuads ? 0 : i) < n_rows ? (column + i) * J.step * kSize : kNowhere;
     tile_out<T, kType, kQuads>(lds, acc, to, pitch, row0, at, scales, scale, bias);
   };
-  const auto typed = [&](auto type) {
-    if (J.quads) out(type, std::true_type{});
-    else out(type, std::false_type{});
-  };
-  if (a.splits > 1) {
-    // a row of sums ends in a whole group of four
-    if (J.step == 1) out(std::integer_sequence<int, 0>{}, std::true_type{});
-    else out(std::integer_sequence<int, 0>{}, std::false_type{});
-  } else if (J.y_dtype == WC_BF16) {
-    typed(std::integer_sequence<int, WC_BF16>{});
-  } else if (J.y_dtype == WC_FP16) {
-    typed(std::integer_sequence<int, WC_FP16>{});
-  } else {
-    typed(std::integer_sequence<int, WC_FP32>{});
-  }
+  if (a.splits > 1) out(std::integer_sequence<int, 0>{});
+  else if (J.y_dtype == WC_BF16) out(std::integer_sequence<int, WC_BF16>{});
+  else if (J.y_dtype == WC_FP16) out(std::integer_sequence<int, WC_FP16>{});
+  else out(std::integer_sequence<int, WC_FP32>{});
 }
 
 // y from the sums of the parts of k.
@@ -643,6 +632,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
   a.n_jobs = n_jobs;
   a.splits = p.splits;
   uint32_t tiles = 0, widest = 0;
+  bool quads = true;
   uint64_t part = reinterpret_cast<uint64_t>(workspace) + (p.copies ? copies_bytes(m, k) : 0);
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
@@ -656,6 +646,8 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
     tiles += tiles_of(p.kernel, m, J.n, a.job[i].step);
+    // a row of sums ends in a whole group of four
+    quads = quads && (p.splits > 1 ? a.job[i].step == 1 : a.job[i].quads);
   }
   if (p.kernel == Kernel::kRing) {
     a.m = m;
@@ -671,7 +663,10 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     const dim3 grid(tiles, p.splits);
     with_tile(p.kernel, [&](auto t) {
       using T = decltype(t);
-      hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T>), grid, dim3(T::kThreads), 0, stream, a);
+      if (quads)
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, true>), grid, dim3(T::kThreads), 0, stream, a);
+      else
+        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, false>), grid, dim3(T::kThreads), 0, stream, a);
     });
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
     if (p.splits > 1) {
@@ -777,8 +772,10 @@ extern "C" wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
-  *bytes = pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)) + pad256(uint64_t(m) * 4) +
-           workspace_of(plan_of(m, k, n_jobs, jobs), m, k);
+  const Plan p = plan_of(m, k, n_jobs, jobs);
+  // nothing where the product's kernel quantises x itself
+  if (!p.hold)
+    *bytes = pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)) + pad256(uint64_t(m) * 4) + workspace_of(p, m, k);
   return WC_OK;
 }
 
@@ -795,8 +792,7 @@ extern "C" wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m
   int8_t* q = static_cast<int8_t*>(dev_workspace);
   float* scale = reinterpret_cast<float*>(q + pad256(uint64_t(m) * WC_I8_ROW_BYTES(k)));
   void* parts = reinterpret_cast<uint8_t*>(scale) + pad256(uint64_t(m) * 4);
-  Plan p = plan_of(m, k, n_jobs, jobs);
-  p.hold = p.hold && reinterpret_cast<uintptr_t>(dev_x) % 16 == 0 && ldx * size_of(x_dtype) % 16 == 0;
+  const Plan p = plan_of(m, k, n_jobs, jobs);
   if (!p.hold && !launch_quantize(dev_x, x_dtype, m, k, ldx, q, scale, st, nullptr, nullptr,
                                   p.copies ? parts : nullptr))
     return WC_EHIP;

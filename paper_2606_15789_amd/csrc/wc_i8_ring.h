@@ -139,7 +139,7 @@ __device__ __forceinline__ void hold_rows(uint32_t rows, uint32_t k, RowAt row_a
   const auto load = [&](uint32_t unit, uint32_t (&v)[kWords]) {
     const uint32_t u = min(unit, all - 1), row = rows == 1 ? 0 : u / units;
     const uint32_t at = (u - row * units) * 8;
-    const auto p = global<const u32x4>(row_at(row) + min(at, k - 8) * uint64_t(kType == WC_FP32 ? 4 : 2));
+    const auto p = global<const u32x4u>(row_at(row) + min(at, k - 8) * uint64_t(kType == WC_FP32 ? 4 : 2));
 #pragma unroll
     for (int i = 0; i < kWords / 4; i++) {
       const u32x4 a = p[i];

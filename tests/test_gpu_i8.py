@@ -279,7 +279,8 @@ def test_refusals(dev):
            lambda: wc.linear_i8_torch(x, [w], [s], [s[:4]]),
            lambda: wc.linear_i8_torch(x, [w], [s, s]),
            lambda: wc.linear_i8_torch(x, [w], [s], ys=[torch.zeros((4, 7), device=dev)]),
-           lambda: wc.linear_i8_torch(x, [w], [s], workspace=torch.zeros(8, dtype=torch.uint8, device=dev)),
+           lambda: wc.linear_i8_torch(torch.zeros((40, 64), device=dev), [w], [s],
+                                      workspace=torch.zeros(8, dtype=torch.uint8, device=dev)),
            lambda: wc.linear_i8_torch(x.cpu(), [w], [s]),
            lambda: wc.quantize_i8_torch(x, q=torch.zeros((4, 64), dtype=torch.int8, device=dev)),
            lambda: wc.matmul_i8_torch(w, s, 64, [w], [s])]
