@@ -591,10 +591,14 @@ bool reached(const wc_i8_experts* b, uint32_t k) {
   return k % 4 || (reinterpret_cast<uintptr_t>(b->w) % 4 == 0 && b->stride % 4 == 0);
 }
 
-// Slot by slot, while that reads no expert's rows twice much (E = 64, k = 6, 2048 x 1408):
-// 20.6 us at one token against 25.2 on the five launches of the general path, 28.2 and
-// 33.7 at two, 43.4 and 52.8 at four.
-constexpr uint32_t kSlotTokens = 4, kHoldBytes = 12 * 1024;
+// Slot by slot, while few slots share an expert, whose rows are then read for each (or the
+// rows are few): 64 experts of 2048 x 1408, 6 a token, 20.6 us at one token against 25.2 on
+// the launches of the general path, 28.2 and 33.7 at two, 43.4 and 52.8 at four; of 4096 x
+// 2048, 8 a token, 40.4 and 46.8 at one, 127 (20 experts hit) and 118 (22 hit) at four.  A
+// workgroup holds all of a token's h: 8 experts of 6144 x 16384, 2 a token, would take 129
+// and take 119.
+constexpr uint32_t kSlotTokens = 4, kHoldBytes = 16 * 1024;
+constexpr uint64_t kSlotWeights = 64u << 20;
 
 using Tile64 = Tile<64, 128, 1, 2, 3>;
 using Tile128 = Tile<128, 128, 2, 2, 3>;
@@ -715,8 +719,10 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
                       (reinterpret_cast<uintptr_t>(gate->w) - reinterpret_cast<uintptr_t>(up->w)) % 4 == 0 &&
                       (gate->stride - up->stride) % 4 == 0;
   const uint64_t hold_x = WC_I8_ROW_BYTES(hidden), hold_h = k * WC_I8_ROW_BYTES(ffn);
-  if (direct && hidden % 8 == 0 && ffn % 8 == 0 && tokens <= kSlotTokens &&
-      slots <= experts && k <= kSlots && hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
+  const bool few = tokens == 1 || 2 * slots < experts ||
+                   (slots <= experts && 3ull * slots * hidden * ffn <= kSlotWeights);
+  if (direct && hidden % 8 == 0 && ffn % 8 == 0 && tokens <= kSlotTokens && few && k <= kSlots &&
+      hold_x <= kHoldBytes && hold_h <= kHoldBytes) {
     const dim3 grid((ffn + 7) / 8, slots), block(SlotRing::kThreads);
     const uint32_t held = SlotRing::kLds + uint32_t(hold_x);
     if (dtype == WC_BF16)
