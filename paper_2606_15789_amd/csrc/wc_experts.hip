@@ -8,9 +8,6 @@ using namespace wc_i8;
 
 constexpr int kRowWaves = 8;
 
-// Rows of h and of the experts' results are whole groups of four floats.
-__host__ __device__ constexpr uint32_t pitch_of(uint32_t n) { return (n + 3u) & ~3u; }
-
 struct Bank {
   uint64_t w, scale, stride;
   int32_t scale_dtype;
@@ -26,6 +23,7 @@ struct ExpertArgs {
   uint64_t y, ldy;
   uint32_t tokens, k, experts, hidden, ffn, slots;
   uint32_t blocks;        // upper bound of the blocks of places
+  uint32_t up_step, down_step;  // classes of the columns of h, of the results (row_pitch)
   int32_t dtype;
   Bank gate, up, down;
 };
@@ -112,7 +110,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_up_kernel(ExpertArg
                     load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(summed<2>(part, 1, o % 16, o / 16)) * xs *
                     load_float(a.up.scale, a.up.scale_dtype, at);
-    global<float>(a.h)[uint64_t(place) * pitch_of(a.ffn) + n] = g / (1.0f + expf(-g)) * u;
+    global<float>(a.h)[uint64_t(place) * row_pitch(a.ffn, 1) + n] = g / (1.0f + expf(-g)) * u;
   }
 }
 
@@ -128,7 +126,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertA
   for (uint32_t o = threadIdx.x; o < 256; o += 64 * kRowWaves) {
     const uint32_t n = n0 + o % 16, place = first + o / 16;
     if (n >= a.hidden || place >= last) continue;
-    global<float>(a.out)[uint64_t(slot_at(a, place)) * pitch_of(a.hidden) + n] =
+    global<float>(a.out)[uint64_t(slot_at(a, place)) * row_pitch(a.hidden, 1) + n] =
         float(summed<1>(part, 0, o % 16, o / 16)) * global<const float>(a.hscale)[place] *
         load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
   }
@@ -145,7 +143,7 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_k
   __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
   if (blockIdx.x >= block_count(a)) return;
   const auto [e, first, last] = block_at(a, blockIdx.x);
-  const uint32_t k = a.hidden, step = steps_of(k), blocks = ((a.ffn + step - 1) / step + 7) / 8;
+  const uint32_t k = a.hidden, step = a.up_step, blocks = ((a.ffn + step - 1) / step + 7) / 8;
   const uint32_t class0 = blockIdx.y / blocks, r0 = blockIdx.y % blocks * 8;
   const ClassRows G = class_rows(a.gate.w + e * a.gate.stride, k, a.ffn, k, step, class0);
   const ClassRows U = class_rows(a.up.w + e * a.up.stride, k, a.ffn, k, step, class0);
@@ -174,7 +172,8 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_k
     const uint64_t at = uint64_t(e) * a.ffn + n;
     const float g = float(R::sum(lds, r, o / 8)) * xs * load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(R::sum(lds, 8 + r, o / 8)) * xs * load_float(a.up.scale, a.up.scale_dtype, at);
-    global<float>(a.h)[uint64_t(place) * pitch_of(a.ffn) + n] = g / (1.0f + expf(-g)) * u;
+    global<float>(a.h)[uint64_t(place) * row_pitch(a.ffn, step) + class0 * class_pitch(a.ffn, step) + r0 + r] =
+        g / (1.0f + expf(-g)) * u;
   }
 }
 
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring
   __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kLds];
   if (blockIdx.x >= block_count(a)) return;
   const auto [e, first, last] = block_at(a, blockIdx.x);
-  const uint32_t k = a.ffn, step = steps_of(k), blocks = ((a.hidden + step - 1) / step + 15) / 16;
+  const uint32_t k = a.ffn, step = a.down_step, blocks = ((a.hidden + step - 1) / step + 15) / 16;
   const uint32_t class0 = blockIdx.y / blocks, r0 = blockIdx.y % blocks * 16;
   const ClassRows C = class_rows(a.down.w + e * a.down.stride, k, a.hidden, k, step, class0);
   if (r0 >= C.rows) return;
@@ -206,7 +205,8 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring
   for (uint32_t o = threadIdx.x; o < 16 * kX; o += R::kThreads) {
     const uint32_t r = o % 16, n = class0 + (r0 + r) * step, place = first + o / 16;
     if (r >= n_rows || place >= last) continue;
-    global<float>(a.out)[uint64_t(slot_at(a, place)) * pitch_of(a.hidden) + n] =
+    global<float>(a.out)[uint64_t(slot_at(a, place)) * row_pitch(a.hidden, step) +
+                         class0 * class_pitch(a.hidden, step) + r0 + r] =
         float(R::sum(lds, r, o / 16)) * global<const float>(a.hscale)[place] *
         load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + n);
   }
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(SlotRing::kThreads) void wc_experts_up_slot_kernel(
     const uint64_t at = uint64_t(e) * a.ffn + n;
     const float g = float(R::sum(lds, threadIdx.x, 0)) * scale[0] * load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(R::sum(lds, 8 + threadIdx.x, 0)) * scale[0] * load_float(a.up.scale, a.up.scale_dtype, at);
-    global<float>(a.h)[uint64_t(slot) * pitch_of(a.ffn) + n] = g / (1.0f + expf(-g)) * u;
+    global<float>(a.h)[uint64_t(slot) * row_pitch(a.ffn, 1) + n] = g / (1.0f + expf(-g)) * u;
   }
 }
 
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
       begun++;
     }
   hold_rows<R::kThreads, WC_FP32, 3>(
-      a.k, k, [&](uint32_t r) { return a.h + uint64_t(first + r) * pitch_of(k) * 4; }, lds + R::kLds,
+      a.k, k, [&](uint32_t r) { return a.h + uint64_t(first + r) * row_pitch(k, 1) * 4; }, lds + R::kLds,
       scales, tops);
   const uint32_t r = lane % 16;
   const uint32_t w0 = r * kStage + ((lane / 16) ^ R::turn(r)) * 16;
@@ -369,16 +369,14 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
 }
 
 // The same on tiles through LDS.  A wave's columns of W are 32 of gate and the same 32
-// of up, so that both products of a value of h meet in one lane.  kQuads: the tile's
-// columns are neighbours (a class of rows is all of them).
-template <class T, bool kQuads>
+// of up, so that both products of a value of h meet in one lane.
+template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];  // of the tile's rows of x
   static_assert(T::kNT == 2 && T::kRows <= T::kThreads);
   constexpr uint32_t kBM = T::kRows, kCols = T::kWN_ * 32;
-  const uint32_t k = a.hidden, step = kQuads ? 1 : steps_of(k);
-  // classes of the same columns one after another, so that their stores meet in a cache
+  const uint32_t k = a.hidden, step = a.up_step;
   const uint32_t blocks = ((a.ffn + step - 1) / step + kCols - 1) / kCols;
   uint32_t mt, nt;
   if (!tile_at(blockIdx.x, block_count(a), blocks * step, mt, nt)) return;
@@ -413,19 +411,19 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const uint32_t column = wave % T::kWN_ * 32 + lane % 8 * 4, row0 = wave / T::kWN_ * (T::kMT * 32);
   float gs[4], us[4];
-  uint32_t out[4];
+  const uint32_t out =
+      column < n_rows ? (class0 * class_pitch(a.ffn, step) + r0 + column) * 4 : kNowhere;
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
     const uint32_t n = class0 + (r0 + column + i) * step;
     const uint64_t at = uint64_t(e) * a.ffn + min(n, a.ffn - 1);
     gs[i] = load_float(a.gate.scale, a.gate.scale_dtype, at);
     us[i] = load_float(a.up.scale, a.up.scale_dtype, at);
-    out[i] = column + (kQuads ? 0 : i) < n_rows ? n * 4 : kNowhere;
   }
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
   __syncthreads();
   // no branches: rows and columns past the last go nowhere
-  const uint32_t pitch = pitch_of(a.ffn) * 4;
+  const uint32_t pitch = row_pitch(a.ffn, step) * 4;
   const u32x4 to = rows_rsrc(a.h + first * uint64_t(pitch), (last - first) * pitch);
 #pragma unroll
   for (int b = 0; b < T::kMT; b++)
@@ -441,23 +439,18 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
             const float g = g4[i] * xs * gs[i], u = u4[i] * xs * us[i];
             h[i] = g / (1.0f + expf(-g)) * u;
           }
-          if constexpr (kQuads) {
-            store_rows(to, out[0] + row * pitch, __builtin_bit_cast(u32x4, h));
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; i++) store_rows(to, out[i] + row * pitch, __float_as_uint(h[i]));
-          }
+          store_rows(to, out + row * pitch, __builtin_bit_cast(u32x4, h));
         });
 }
 
-template <class T, bool kQuads>
+template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];   // of the tile's rows of h, and their slots
   __shared__ uint32_t slots[T::kRows];
   static_assert(T::kRows <= T::kThreads);
   constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
-  const uint32_t k = a.ffn, step = kQuads ? 1 : steps_of(k);
+  const uint32_t k = a.ffn, step = a.down_step;
   const uint32_t blocks = ((a.hidden + step - 1) / step + kBN - 1) / kBN;
   uint32_t mt, nt;
   if (!tile_at(blockIdx.x, block_count(a), blocks * step, mt, nt)) return;
@@ -485,16 +478,16 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   constexpr int kCols = T::kNT * 32;
   const uint32_t column = wave % T::kWN_ * kCols + lane % (kCols / 4) * 4;
-  const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32), pitch = pitch_of(a.hidden);
+  const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32), pitch = row_pitch(a.hidden, step);
   // no branches: rows and columns past the last go to a row of their own
   const uint64_t nowhere = uint64_t(a.slots) * pitch;
+  const bool inside = column < n_rows;
+  const uint32_t out = class0 * class_pitch(a.hidden, step) + r0 + column;
   float scale[4];
-  uint32_t out[4];
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
     const uint32_t n = class0 + (r0 + column + i) * step;
     scale[i] = load_float(a.down.scale, a.down.scale_dtype, uint64_t(e) * a.hidden + min(n, a.hidden - 1));
-    out[i] = column + (kQuads ? 0 : i) < n_rows ? n : kNowhere;
   }
   if (threadIdx.x < kBM) {
     scales[threadIdx.x] = row_scale;
@@ -512,14 +505,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
           f32x4 v = get(0);
 #pragma unroll
           for (int i = 0; i < 4; i++) v[i] = v[i] * hs * scale[i];
-          if constexpr (kQuads) {
-            *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) +
-                                                 (out[0] != kNowhere ? at + out[0] : nowhere)) = v;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-              global<float>(a.out)[out[i] != kNowhere ? at + out[i] : nowhere] = v[i];
-          }
+          *reinterpret_cast<global_ptr<f32x4>>(global<float>(a.out) + (inside ? at + out : nowhere)) = v;
         });
 }
 
@@ -528,13 +514,20 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
 __global__ __launch_bounds__(256) void wc_experts_join_kernel(ExpertArgs a) {
   const uint32_t token = blockIdx.x, n = (blockIdx.y * 256 + threadIdx.x) * 4;
   if (n >= a.hidden) return;
+  const uint32_t each = class_pitch(a.hidden, a.down_step);
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   for (uint32_t j = 0; j < a.k; j++) {
     const uint64_t slot = uint64_t(token) * a.k + j;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (global<const int32_t>(a.ids)[slot] >= 0)
-      v = *reinterpret_cast<global_ptr<const f32x4>>(global<const float>(a.out) +
-                                                     slot * pitch_of(a.hidden) + n);
+    if (global<const int32_t>(a.ids)[slot] >= 0) {
+      const auto row = global<const float>(a.out) + slot * (a.down_step * each);
+      if (a.down_step == 1) {
+        v = *reinterpret_cast<global_ptr<const f32x4>>(row + n);
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; i++) v[i] = row[column_at(min(n + i, a.hidden - 1), a.down_step, each)];
+      }
+    }
     const float w = global<const float>(a.weights)[slot];
 #pragma unroll
     for (int i = 0; i < 4; i++) sum[i] += w * v[i];
@@ -564,7 +557,8 @@ Workspace layout(uint64_t tokens, uint64_t k, uint64_t experts, uint64_t hidden,
   w.xq = take(tokens * WC_I8_ROW_BYTES(hidden));
   w.xscale = take(tokens * 4);
   // h, and after its quantisation the experts' results and a row for what is past them
-  w.wide = take((tokens * k + 1) * pitch_of(uint32_t(hidden > ffn ? hidden : ffn)) * 4);
+  const uint64_t h = row_pitch(uint32_t(ffn), steps_of(hidden)), out = row_pitch(uint32_t(hidden), steps_of(ffn));
+  w.wide = take((tokens * k + 1) * (h > out ? h : out) * 4);
   w.hq = take(tokens * k * WC_I8_ROW_BYTES(ffn));
   w.hscale = take(tokens * k * 4);
   if (hidden % 4) w.xcopies = take(copies_bytes(tokens, hidden));
@@ -641,17 +635,13 @@ uint32_t columns(uint32_t n, uint32_t step, uint32_t each) {
 }
 template <class T>
 void start_up(const ExpertArgs& a, hipStream_t st) {
-  const uint32_t step = steps_of(a.hidden);
-  const dim3 grid(a.blocks * columns(a.ffn, step, T::kWN_ * 32)), block(T::kThreads);
-  if (step == 1) hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((wc_experts_up_tile_kernel<T, false>), grid, block, 0, st, a);
+  const dim3 grid(a.blocks * columns(a.ffn, a.up_step, T::kWN_ * 32));
+  hipLaunchKernelGGL((wc_experts_up_tile_kernel<T>), grid, dim3(T::kThreads), 0, st, a);
 }
 template <class T>
 void start_down(const ExpertArgs& a, hipStream_t st) {
-  const uint32_t step = steps_of(a.ffn);
-  const dim3 grid(a.blocks * columns(a.hidden, step, T::kCols)), block(T::kThreads);
-  if (step == 1) hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((wc_experts_down_tile_kernel<T, false>), grid, block, 0, st, a);
+  const dim3 grid(a.blocks * columns(a.hidden, a.down_step, T::kCols));
+  hipLaunchKernelGGL((wc_experts_down_tile_kernel<T>), grid, dim3(T::kThreads), 0, st, a);
 }
 
 }  // namespace
@@ -747,8 +737,10 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
                        reinterpret_cast<float*>(a.xscale), st, nullptr, &blocks,
                        hidden % 4 ? reinterpret_cast<void*>(a.xcopies) : nullptr))
     return WC_EHIP;
-  const dim3 up_grid(a.blocks, rows ? columns(ffn, steps_of(hidden), 8) : (ffn + 15) / 16);
-  const dim3 down_grid(a.blocks, rows ? columns(hidden, steps_of(ffn), 16) : (hidden + 15) / 16);
+  a.up_step = rows ? steps_of(hidden) : 1;
+  a.down_step = rows ? steps_of(ffn) : 1;
+  const dim3 up_grid(a.blocks, columns(ffn, a.up_step, rows ? 8 : 16));
+  const dim3 down_grid(a.blocks, columns(hidden, a.down_step, 16));
   if (kernel.tile) with_tile(kernel.tile, [&](auto t) { start_up<decltype(t)>(a, st); });
   else if (rows == 16)
     hipLaunchKernelGGL((wc_experts_up_ring_kernel<16>), up_grid, dim3(ExpertRing<16>::kThreads), 0, st, a);
@@ -757,10 +749,10 @@ extern "C" wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t to
   else
     hipLaunchKernelGGL(wc_experts_up_kernel, up_grid, dim3(64 * kRowWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
-  if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, pitch_of(ffn),
+  if (!launch_quantize(reinterpret_cast<const void*>(a.h), WC_FP32, slots, ffn, row_pitch(ffn, a.up_step),
                        reinterpret_cast<void*>(a.hq), reinterpret_cast<float*>(a.hscale), st,
                        dev_offsets + experts, nullptr,
-                       ffn % 4 ? reinterpret_cast<void*>(a.hcopies) : nullptr))
+                       ffn % 4 ? reinterpret_cast<void*>(a.hcopies) : nullptr, a.up_step))
     return WC_EHIP;
   if (kernel.tile) with_tile(kernel.tile, [&](auto t) { start_down<decltype(t)>(a, st); });
   else if (rows == 16)

@@ -109,6 +109,19 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
 }
 
+// Rows of intermediate results: n columns in `step` (1, 2 or 4) classes n mod step, one
+// class after another and each in whole groups of four, so that a tile, whose columns are
+// of one class, stores whole groups.
+__host__ __device__ constexpr uint32_t class_pitch(uint32_t n, uint32_t step) {
+  return ((n + step - 1) / step + 3) & ~3u;
+}
+__host__ __device__ constexpr uint32_t row_pitch(uint32_t n, uint32_t step) {
+  return step * class_pitch(n, step);
+}
+__device__ __forceinline__ uint32_t column_at(uint32_t column, uint32_t step, uint32_t each) {
+  return (column & (step - 1)) * each + column / step;
+}
+
 // Which places of the experts' order a workgroup multiplies: blocks of `rows` places,
 // counted expert by expert.  Entry 0 of the table holds the number of blocks, entry b + 1
 // block b's {expert, first place, past the last place, 0}.
@@ -120,9 +133,9 @@ struct Blocks {
 // Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes
 // (wc_i8.hip), or as many of them as the device int `limit` says; with `blocks`, one more
 // workgroup writes its table; with `copies`, their shifted copies (wc_i8_tile.h) too.
-// False on a launch error.
+// `step`: the columns' classes, fp32 rows only.  False on a launch error.
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
                      float* scale, hipStream_t stream, const int32_t* limit = nullptr,
-                     const Blocks* blocks = nullptr, void* copies = nullptr);
+                     const Blocks* blocks = nullptr, void* copies = nullptr, uint32_t step = 1);
 
 }  // namespace wc_i8

@@ -11,7 +11,7 @@ using namespace wc_i8;
 struct QuantArgs {
   uint64_t x, ldx, q, scale, limit;
   uint64_t copies;  // three shifted copies of q (Shifted), or none
-  uint32_t m, k;
+  uint32_t m, k, step;
   Blocks blocks;
 };
 
@@ -77,7 +77,15 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
 #pragma unroll
   for (int u = 0; u < kUnits; u++) {
     const uint32_t at = (threadIdx.x + u * kThreads) * 8;
-    if (at + 8 <= a.k) {
+    if (kType == WC_FP32 && a.step > 1) {
+      const uint32_t each = class_pitch(a.k, a.step);
+#pragma unroll
+      for (uint32_t i = 0; i < kWords; i++) {
+        const uint32_t n = min(at + i, a.k - 1);
+        const uint32_t w = global<const uint32_t>(first)[column_at(n, a.step, each)];
+        v[u][i] = at + i < a.k ? w : 0u;
+      }
+    } else if (at + 8 <= a.k) {
       // rows at any element: as the codes of W, loads of any alignment
       const auto p = global<const u32x4u>(first + at * (kType == WC_FP32 ? 4 : 2));
 #pragma unroll
@@ -186,6 +194,7 @@ struct MatArgs {
   uint64_t copies;  // of q, shifted
   uint64_t x, ldx;  // not quantised yet, where the kernel does that itself
   uint32_t m, k, n_jobs, splits;
+  uint32_t sums, reserved;  // sums: results are int32 sums for the join
   MatJob job[kMaxJobs];
 };
 
@@ -424,25 +433,30 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
              [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
              [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
   float scale[4] = {}, bias[4] = {};
-  if (a.splits == 1) column_scales(J, first + (r0 + column) * J.step, J.step, scale, bias);
+  if (!a.sums) column_scales(J, first + (r0 + column) * J.step, J.step, scale, bias);
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
   __syncthreads();
   const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32);
   const auto out = [&]<int kType>(std::integer_sequence<int, kType>) {
+    // sums are stored class by class, results where they belong
     constexpr uint32_t kSize = kType == 0 || kType == WC_FP32 ? 4 : 2;
-    const uint32_t pitch = kType ? uint32_t(J.ldy) * kSize : ((J.n + 3u) & ~3u) * 4;
+    constexpr bool kGroups = kQuads || kType == 0;
+    const uint32_t step = kType ? J.step : 1, sums = row_pitch(J.n, J.step) * 4;
+    const uint32_t pitch = kType ? uint32_t(J.ldy) * kSize : sums;
     const uint64_t row = kType ? J.y + m0 * uint64_t(pitch) : J.part + (uint64_t(part) * a.m + m0) * pitch;
-    const uint32_t column0 = (first + r0 * J.step) * kSize;
+    const uint32_t column0 =
+        (kType ? first + r0 * J.step : first * class_pitch(J.n, J.step) + r0) * kSize;
     // to the last column of the last row, or of its group of four
-    const uint32_t end = ((n_rows - 1) * J.step + 1) * kSize;
-    const u32x4 to = rows_rsrc(row + column0, (m_rows - 1) * pitch + (kQuads ? (end + 4 * kSize - 1) / (4 * kSize) * (4 * kSize) : end));
+    const uint32_t end = ((n_rows - 1) * step + 1) * kSize;
+    const uint32_t group = kGroups ? 4 * kSize : kSize;
+    const u32x4 to = rows_rsrc(row + column0, (m_rows - 1) * pitch + (end + group - 1) / group * group);
     uint32_t at[4];
 #pragma unroll
     for (uint32_t i = 0; i < 4; i++)
-      at[i] = column + (kQuads ? 0 : i) < n_rows ? (column + i) * J.step * kSize : kNowhere;
-    tile_out<T, kType, kQuads>(lds, acc, to, pitch, row0, at, scales, scale, bias);
+      at[i] = column + (kGroups ? 0 : i) < n_rows ? (column + i) * step * kSize : kNowhere;
+    tile_out<T, kType, kGroups>(lds, acc, to, pitch, row0, at, scales, scale, bias);
   };
-  if (a.splits > 1) out(std::integer_sequence<int, 0>{});
+  if (a.sums) out(std::integer_sequence<int, 0>{});
   else if (J.y_dtype == WC_BF16) out(std::integer_sequence<int, WC_BF16>{});
   else if (J.y_dtype == WC_FP16) out(std::integer_sequence<int, WC_FP16>{});
   else out(std::integer_sequence<int, WC_FP32>{});
@@ -454,14 +468,23 @@ __global__ __launch_bounds__(256) void wc_matmul_i8_join_kernel(MatArgs a) {
   const MatJob J = a.job[j];
   const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4;
   if (n >= J.n) return;
-  const uint64_t pitch = (J.n + 3u) & ~3u;
+  const uint32_t each = class_pitch(J.n, J.step), pitch = J.step * each;
+  uint32_t at[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++) at[i] = column_at(min(n + i, J.n - 1), J.step, each);
   float scale[4], bias[4];
   column_scales(J, n, 1, scale, bias);
   for (uint32_t m = blockIdx.x; m < a.m; m += gridDim.x) {
     i32x4 sum = {0, 0, 0, 0};
-    for (uint32_t p = 0; p < a.splits; p++)
-      sum += *reinterpret_cast<global_ptr<const i32x4>>(global<const int32_t>(J.part) +
-                                                        (uint64_t(p) * a.m + m) * pitch + n);
+    for (uint32_t p = 0; p < a.splits; p++) {
+      const auto row = global<const int32_t>(J.part) + (uint64_t(p) * a.m + m) * pitch;
+      if (J.step == 1) {
+        sum += *reinterpret_cast<global_ptr<const i32x4>>(row + n);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) sum[i] += row[at[i]];
+      }
+    }
     f32x4 v;
 #pragma unroll
     for (int i = 0; i < 4; i++) v[i] = float(sum[i]);
@@ -516,6 +539,7 @@ struct Plan {
   bool hold;        // the kernel can quantise x itself
   bool copies;      // some rows of W do not start with a dword
   uint32_t splits;
+  bool sums;        // int32 sums go to the workspace, and are joined
   uint64_t part_bytes;
 };
 // f(Tile) for the kernel's tile.
@@ -557,10 +581,12 @@ constexpr TileCost kCosts[] = {{Kernel::kTile64, 0.26, 0.34, 5.0},
                                {Kernel::kTile256Half, 0.90, 0.0, 6.9},
                                {Kernel::kTile256, 1.55, 0.0, 10.2}};
 constexpr double kUnits = 256, kJoin = 4.0, kBytesPerUs = 4e6, kReadPerUs = 5e6;
+// results of a class of rows, stored two or four apart (1000 x 8191: 30 us more)
+constexpr double kStridedPerUs = 2.7e5;
 
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
-  Plan p{Kernel::kRows, false, false, 1, 0};
-  uint64_t sums = 0, weights = 0, tiles64 = 0;
+  Plan p{Kernel::kRows, false, false, 1, false, 0};
+  uint64_t sums = 0, strided = 0, weights = 0, tiles64 = 0;
   bool narrow = true;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
@@ -570,7 +596,8 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
     narrow = narrow && J.n < (1u << 20) && J.ldy < (1u << 20);
     p.copies = p.copies || J.ldw % 4 || reinterpret_cast<uintptr_t>(J.w) % 4;
     tiles64 += uint64_t(m + 63) / 64 * (J.n / 64 + 4);
-    sums += uint64_t(m) * ((J.n + 3u) & ~3u) * 4;
+    sums += uint64_t(m) * row_pitch(J.n, steps_of(J.ldw)) * 4;
+    if (steps_of(J.ldw) > 1) strided += uint64_t(m) * J.n;
   }
   if (m <= 16) {
     p.kernel = Kernel::kRing;
@@ -595,15 +622,19 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
       const double rounds = std::ceil(groups / (two ? 2 * kUnits : kUnits));
       double us = rounds * (c.round + (stages + splits - 1) / splits * (two ? c.stage_of_two : c.stage));
       us = std::max(us, double(weights) / kReadPerUs);
-      if (splits > 1) us += kJoin + 2.0 * double(sums) * splits / kBytesPerUs;
+      const double join = kJoin + 2.0 * double(sums) * splits / kBytesPerUs;
+      const double apart = double(strided) / kStridedPerUs;
+      const bool joined = splits > 1 || join < apart;
+      us += joined ? join : apart;
       if (best == 0 || us < best) {
         best = us;
         p.kernel = c.kernel;
         p.splits = splits;
+        p.sums = joined;
       }
     }
   }
-  if (p.splits > 1) p.part_bytes = sums * p.splits;
+  if (p.sums) p.part_bytes = sums * p.splits;
   return p;
 }
 
@@ -631,6 +662,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
   a.k = k;
   a.n_jobs = n_jobs;
   a.splits = p.splits;
+  a.sums = p.sums;
   uint32_t tiles = 0, widest = 0;
   bool quads = true;
   uint64_t part = reinterpret_cast<uint64_t>(workspace) + (p.copies ? copies_bytes(m, k) : 0);
@@ -640,14 +672,13 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     a.job[i] = {reinterpret_cast<uint64_t>(J.w),    reinterpret_cast<uint64_t>(J.scale),
                 reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
                 J.ldw, J.ldy, part, J.n, tiles, J.scale_dtype, J.bias_dtype, J.y_dtype,
-                steps_of(J.ldw) == 1 && J.n % 4 == 0 && J.ldy % 4 == 0 &&
+                J.n % 4 == 0 && J.ldy % 4 == 0 &&
                     reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0,
                 p.kernel == Kernel::kRows ? 1u : steps_of(J.ldw), 0};
-    if (p.splits > 1) part += uint64_t(m) * ((J.n + 3u) & ~3u) * 4 * p.splits;
+    if (p.sums) part += uint64_t(m) * row_pitch(J.n, a.job[i].step) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
     tiles += tiles_of(p.kernel, m, J.n, a.job[i].step);
-    // a row of sums ends in a whole group of four
-    quads = quads && (p.splits > 1 ? a.job[i].step == 1 : a.job[i].quads);
+    quads = quads && (p.sums || (a.job[i].quads && a.job[i].step == 1));
   }
   if (p.kernel == Kernel::kRing) {
     a.m = m;
@@ -669,7 +700,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
         hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, false>), grid, dim3(T::kThreads), 0, stream, a);
     });
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
-    if (p.splits > 1) {
+    if (p.sums) {
       const uint32_t rows = m < 65536 ? m : 65536;
       hipLaunchKernelGGL(wc_matmul_i8_join_kernel, dim3(rows, (widest + 1023) / 1024, n_jobs), dim3(256),
                          0, stream, a);
@@ -701,10 +732,10 @@ namespace wc_i8 {
 
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
                      float* scale, hipStream_t stream, const int32_t* limit, const Blocks* blocks,
-                     void* copies) {
+                     void* copies, uint32_t step) {
   const QuantArgs a = {reinterpret_cast<uint64_t>(x), ldx, reinterpret_cast<uint64_t>(q),
                        reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(limit),
-                       reinterpret_cast<uint64_t>(copies), m, k, blocks ? *blocks : Blocks{}};
+                       reinterpret_cast<uint64_t>(copies), m, k, step, blocks ? *blocks : Blocks{}};
   // few rows: more threads to each
   if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, m, a, stream);
   else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, m, a, stream);
