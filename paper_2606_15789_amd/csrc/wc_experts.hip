@@ -607,6 +607,30 @@ void with_tile(int tile, F f) {
   }
 }
 
+uint32_t columns(uint32_t n, uint32_t step, uint32_t each) {
+  return step * (((n + step - 1) / step + each - 1) / each);
+}
+// What a tile's kernels take, in us: a stage of 128 bytes of k, one workgroup's and two's
+// where two fit a compute unit, and all else of a round of workgroups.  Taken so that the
+// least sum is the fastest tile, or within 2 % of it, at each of these (measured on tiles of
+// 64, 128 and 256 places, us; experts, of them a token's, width x inner width, tokens):
+//   7, 3, 1537 x 2051: 150 57, 52, 86; 203 58, 66, 88; 330 87, 70, 93
+//   7, 3, 2049 x 1365: 77 44, 46, 79; 256 62, 51, 84
+//   16, 4, 2048 x 1024: 500 81, 71, 75; 1000 112, 102, 82
+//   64, 6, 2048 x 1408: 43 132, 161, 169; 683 202, 205, 214; 1995 342, 330, 287
+//   8, 2, 4096 x 14336: 16 274, 269, 392; 128 294, 313, 400; 256 375, 337, 428;
+//     600 559, 518, 500; 4096 4370, 3613, 2760
+//   8, 2, 6144 x 16384: 32 473, 506, 578
+struct ExpertCost {
+  int tile;
+  uint32_t rows, up_columns, columns;
+  double stage, stage_of_two, round;
+};
+constexpr ExpertCost kExpertCosts[] = {{1, Tile64::kRows, Tile64::kWN_ * 32, Tile64::kCols, 0.55, 0.8, 5},
+                                       {2, Tile128::kRows, Tile128::kWN_ * 32, Tile128::kCols, 0.60, 0, 5},
+                                       {3, Tile256::kRows, Tile256::kWN_ * 32, Tile256::kCols, 1.55, 0, 9}};
+constexpr double kUnits = 256, kReadPerUs = 5e6;
+
 // The kernel, by the rows an expert has on average: a tile (0: none) of `rows` places, or
 // rings of 8 or 16, or (0) the one for matrices at any address.
 struct Chosen {
@@ -617,22 +641,34 @@ Chosen choose(uint64_t tokens, uint32_t slots, uint32_t experts, uint32_t hidden
               bool direct) {
   // tiles find x by 32-bit offsets
   if (!direct || tokens * WC_I8_ROW_BYTES(hidden + 3) >> 32) return {0, 0};
-  // us on rings, and tiles of 64, 128 and 256 places (8 experts of 4096 x 14336, 2 a token;
-  // 64 of 2048 x 1408, 6 a token; 8 of 6144 x 16384):
-  //   average 4: 283 (8 experts), 274, 269, 392; 6: 152, 132, 161, 169; 8: 558, 473, 506, 578;
-  //   32: 594, 294, 313, 400; 64: 943, 375, 337, 428, and 609, 202, 205, 214;
-  //   150: -, 559, 518, 500; 187: -, 342, 330, 287; 1024: -, 4370, 3613, 2760
   const uint32_t average = slots / experts;
-  if (average >= 120) return {3, 256};
-  if (average >= 64) return {2, 128};
-  if (average >= 4) return {1, 64};
-  // a token takes an expert once
-  return {0, tokens <= 8 ? 8u : 16u};
+  // a token takes an expert once.  Rings and the least tile, us: average 4 of 8 experts of
+  // 4096 x 14336 283 and 274, 6 of 64 of 2048 x 1408 152 and 132, 32 of the first 594 and 294
+  if (average < 4) return {0, tokens <= 8 ? 8u : 16u};
+  Chosen best{0, 0};
+  double least = 0;
+  const double hit = std::min(experts, slots);
+  for (const ExpertCost& c : kExpertCosts) {
+    // an expert's last block is half full, on average
+    const double blocks = hit * std::max(1.0, double(average) / c.rows + 0.5);
+    const auto product = [&](uint32_t n, uint32_t k, uint32_t each, uint32_t matrices) {
+      const double groups = blocks * columns(n, steps_of(k), each);
+      const bool two = c.stage_of_two > 0 && groups > kUnits;
+      const double rounds = groups / (two ? 2 * kUnits : kUnits);
+      const double us = (c.round + (k + 127) / 128 * (two ? c.stage_of_two : c.stage)) *
+                        // many rounds overlap
+                        (rounds < 4 ? std::ceil(rounds) : rounds + 0.5);
+      return std::max(us, hit * matrices * double(n) * k / kReadPerUs);
+    };
+    const double us = product(ffn, hidden, c.up_columns, 2) + product(hidden, ffn, c.columns, 1);
+    if (least == 0 || us < least) {
+      least = us;
+      best = {c.tile, c.rows};
+    }
+  }
+  return best;
 }
 
-uint32_t columns(uint32_t n, uint32_t step, uint32_t each) {
-  return step * (((n + step - 1) / step + each - 1) / each);
-}
 template <class T>
 void start_up(const ExpertArgs& a, hipStream_t st) {
   const dim3 grid(a.blocks * columns(a.ffn, a.up_step, T::kWN_ * 32));

@@ -115,7 +115,8 @@ def _run(dev, x, r, layer, **more):
     (300, 8, 2, 384, 512), (520, 4, 2, 256, 640), (40, 100, 1, 31, 17), (2, 16, 4, 2048, 1408),
     (1200, 2, 1, 160, 144), (800, 2, 2, 272, 304), (900, 2, 1, 131, 77),
     (2, 8, 2, 84, 60), (20, 4, 2, 140, 92), (300, 4, 2, 204, 132),
-    (300, 4, 2, 203, 130), (4, 4, 2, 129, 66), (1300, 3, 1, 97, 258)])
+    (300, 4, 2, 203, 130), (4, 4, 2, 129, 66), (1300, 3, 1, 97, 258),
+    (3000, 2, 1, 515, 640), (4100, 3, 2, 515, 386), (3000, 5, 2, 260, 1100), (6000, 3, 1, 256, 512)])
 def test_sizes(dev, dtype, tokens, E, k, hidden, ffn):
     g = torch.Generator().manual_seed(tokens + E)
     x = torch.randn((tokens, hidden), generator=g).to(DT[dtype])
@@ -159,6 +160,21 @@ def test_skewed_and_empty(dev, tokens):
     r.weights[0] = math.nan
     y = _run(dev, x, r, layer)
     assert bool(torch.isnan(y[0]).all()) and not bool(y[1:].any())
+
+
+def test_uneven_and_many(dev):
+    """Many rows to an expert on average, and one expert with 3, one with none."""
+    g = torch.Generator().manual_seed(11)
+    tokens, E, hidden, ffn = 4100, 5, 515, 386
+    layer = _layer(4, E, hidden, ffn)
+    x = torch.randn((tokens, hidden), generator=g).bfloat16()
+    ids = torch.tensor([[0, 3]]).repeat(tokens, 1)
+    ids[2000:, 1] = 4
+    ids[77:80, 0] = 1
+    ids[500::7, 1] = -1
+    weights = torch.where(ids < 0, torch.zeros(()), torch.rand((tokens, 2), generator=g))
+    r = _routing(ids, weights, E)
+    _check(_run(dev, x, r, layer), x, r, layer)
 
 
 @pytest.mark.parametrize("tokens", [4, 200])
