@@ -181,15 +181,13 @@ __device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float
   weight = 0.0f;
   for (uint32_t n = 0; n < a.k; n++) {
     const int32_t at = take_best<kLanes, kPer>(rank, kNone);
-    float mine = s[0];
+    if (lane == n) id = at;
+  }
+  // its score lies in register id / kLanes of lane id % kLanes
 #pragma unroll
-    for (int i = 1; i < kPer; i++)
-      if (at / kLanes == i) mine = s[i];
-    mine = __shfl(mine, at & (kLanes - 1), kLanes);
-    if (lane == n && at >= 0) {
-      id = at;
-      weight = mine;
-    }
+  for (int i = 0; i < kPer; i++) {
+    const float there = __shfl(s[i], id & (kLanes - 1), kLanes);
+    if (id >= 0 && id / kLanes == i) weight = there;
   }
   if (a.renormalize) {
     // lanes past k have none

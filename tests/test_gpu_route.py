@@ -205,7 +205,8 @@ def test_nan_and_infinity(dev, score):
 
 @pytest.mark.parametrize("tokens,experts,k", [(1000, 64, 8), (2048, 1, 1), (2049, 3, 1),
                                               (4099, 61, 7), (30000, 512, 16), (16384, 8, 2),
-                                              (17000, 61, 6), (5000, 200, 3), (900, 40, 9)])
+                                              (17000, 61, 6), (5000, 200, 3), (900, 40, 9),
+                                              (140000, 16, 16), (300000, 60, 5), (40000, 300, 2)])
 def test_order_of_many_slots(dev, tokens, experts, k):
     g = torch.Generator().manual_seed(tokens)
     x = torch.randn((tokens, experts), generator=g) + torch.randn(experts, generator=g)
