@@ -135,7 +135,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertA
 // The same from rings of whole lines.  The sixteen rows of a product's W are eight of
 // gate and the same eight of up.
 template <int kX>
-using ExpertRing = Ring<1, kX, 4, 4>;
+using ExpertRing = Ring<kX, 4, 4>;
 
 template <int kX>
 __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_kernel(ExpertArgs a) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_k
 #pragma unroll
   for (int i = 0; i < kX / 8; i++)
     xoff[i] = slot_at(a, min(first + 8 * i + R::row_of(), last - 1)) / a.k * X.pitch + R::byte_of(i);
-  i32x4 acc[1];
+  i32x4 acc;
   R::product(lds, (G.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
              [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff[i] + at); }, acc,
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring
   for (int i = 0; i < 2; i++) woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of(i);
 #pragma unroll
   for (int i = 0; i < kX / 8; i++) xoff[i] = min(8 * i + R::row_of(), m_rows - 1) * X.pitch + R::byte_of(i);
-  i32x4 acc[1];
+  i32x4 acc;
   R::product(lds, (C.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
              [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc,
@@ -216,8 +216,8 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_down_ring
 // two launches.  Every workgroup quantises the row of x, then of h, that it multiplies,
 // while its first rows of W are on their way; a token's slots are added where its
 // columns' sums meet.
-using SlotRing = Ring<1, 0, 4, 4>;
-using DownSlotRing = Ring<1, 0, 8, 3>;
+using SlotRing = Ring<0, 4, 4>;
+using DownSlotRing = Ring<0, 8, 3>;
 
 template <int kType>
 __global__ __launch_bounds__(SlotRing::kThreads) void wc_experts_up_slot_kernel(ExpertArgs a) {
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(SlotRing::kThreads) void wc_experts_up_slot_kernel(
   const u32x4 ur = rows_rsrc(a.up.w + e * a.up.stride + uint64_t(n0) * k, n_rows * k);
   const uint32_t row = min(R::row_of(), n_rows - 1) * k;
   const uint32_t woff[2] = {row + R::byte_of(0), row + R::byte_of(1)};
-  i32x4 acc[1];
+  i32x4 acc;
   R::product(lds, row_bytes / kStage, [](int, uint32_t, uint32_t) {},
              [&](int i, uint32_t at, uint32_t to) { load_lds(i ? ur : gr, to, woff[i] + at); }, acc, [&] {
                hold_rows<R::kThreads, kType, 2>(
@@ -405,9 +405,9 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
     woff[i] = min(r / 64 * 32 + r % 32, n_rows - 1) * G.pitch + T::byte_of();
   }
   i32x16 acc[T::kMT][2];
-  T::product(lds, (G.bytes + T::kBytes - 1) / T::kBytes, last - first,
-             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
-             [&](int i, uint32_t s, uint32_t to) { load_lds(wr[i], to, woff[i] + s * T::kBytes); }, acc);
+  T::product(lds, (G.bytes + kStage - 1) / kStage, last - first,
+             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); },
+             [&](int i, uint32_t s, uint32_t to) { load_lds(wr[i], to, woff[i] + s * kStage); }, acc);
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const uint32_t column = wave % T::kWN_ * 32 + lane % 8 * 4, row0 = wave / T::kWN_ * (T::kMT * 32);
   float gs[4], us[4];
@@ -472,9 +472,9 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   const float row_scale = global<const float>(a.hscale)[place];
   const uint32_t row_slot = slot_at(a, place);
   i32x16 acc[T::kMT][T::kNT];
-  T::product(lds, (C.bytes + T::kBytes - 1) / T::kBytes, m_rows,
-             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
-             [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
+  T::product(lds, (C.bytes + kStage - 1) / kStage, m_rows,
+             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); },
+             [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * kStage); }, acc);
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   constexpr int kCols = T::kNT * 32;
   const uint32_t column = wave % T::kWN_ * kCols + lane % (kCols / 4) * 4;

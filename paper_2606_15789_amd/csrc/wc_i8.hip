@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_matmul_i8_rows_kernel(MatAr
 // kX = 0: x comes as it is, and every workgroup quantises it for itself while its first
 // rows of W are on their way.
 template <int kX>
-using MatRing = Ring<1, kX, 4, 4>;
+using MatRing = Ring<kX, 4, 4>;
 
 template <int kX, int kType>
 __global__ __launch_bounds__(MatRing<kX>::kThreads) void wc_matmul_i8_ring_kernel(MatArgs a) {
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(MatRing<kX>::kThreads) void wc_matmul_i8_ring_kerne
     woff[i] = min(8 * i + R::row_of(), n_rows - 1) * C.pitch + R::byte_of(i);
     xoff[i] = min(8 * i + R::row_of(), a.m - 1) * X.pitch + R::byte_of(i);
   }
-  i32x4 acc[1];
+  i32x4 acc;
   R::product(lds, (C.bytes + kStage - 1) / kStage,
              [&](int i, uint32_t at, uint32_t to) { load_lds(xr, to, xoff[i] + at); },
              [&](int i, uint32_t at, uint32_t to) { load_lds(wr, to, woff[i] + at); }, acc, [&] {
@@ -412,10 +412,10 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   const uint32_t n_rows = min(kBN, C.rows - r0);
   const Shifted X = shifted(a.q, a.copies, a.m, a.k, C.shift);
   // this workgroup's part of the stages
-  const uint32_t all = (C.bytes + T::kBytes - 1) / T::kBytes;
+  const uint32_t all = (C.bytes + kStage - 1) / kStage;
   const uint32_t each = all / a.splits, rest = all % a.splits, part = blockIdx.y;
   const uint32_t s0 = part * each + min(part, rest), stages = each + (part < rest);
-  const uint32_t k0 = s0 * T::kBytes;
+  const uint32_t k0 = s0 * kStage;
   const u32x4 xr = rows_rsrc(X.base + m0 * uint64_t(X.pitch) + k0, m_rows * X.pitch - k0);
   const u32x4 wr = rows_rsrc(C.base + r0 * uint64_t(C.pitch) + k0, (n_rows - 1) * C.pitch + C.bytes - k0);
   uint32_t xoff[T::kXLoads], woff[T::kWLoads];
@@ -430,8 +430,8 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   const uint32_t column = wave % T::kWN_ * kCols + lane % (kCols / 4) * 4;
   i32x16 acc[T::kMT][T::kNT];
   T::product(lds, stages, m_rows,
-             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * T::kBytes); },
-             [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * T::kBytes); }, acc);
+             [&](int i, uint32_t s, uint32_t to) { load_lds(xr, to, xoff[i] + s * kStage); },
+             [&](int i, uint32_t s, uint32_t to) { load_lds(wr, to, woff[i] + s * kStage); }, acc);
   float scale[4] = {}, bias[4] = {};
   if (!a.sums) column_scales(J, first + (r0 + column) * J.step, J.step, scale, bias);
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;

@@ -13,15 +13,15 @@
 
 namespace wc_i8 {
 
-// kNT blocks of 16 rows of W, kX (8 or 16) rows of x, kW waves, kS stages to a ring.
+// 16 rows of W, kX (8 or 16) rows of x, kW waves, kS stages to a ring.
 // kX = 0: x is held in LDS, quantised there by the workgroup itself (hold_rows).
-template <int kNT, int kX, int kW, int kS>
+template <int kX, int kW, int kS>
 struct Ring {
   static constexpr int kThreads = 64 * kW;
-  static constexpr int kStageBytes = (16 * kNT + kX) * kStage;
+  static constexpr int kStageBytes = (16 + kX) * kStage;
   static constexpr int kWave = kS * kStageBytes, kLds = kW * kWave;
-  static constexpr int kLoads = 2 * kNT + kX / 8;  // of a wave to a stage
-  static_assert(kW * kNT * 1024 <= kLds && kLds <= 160 * 1024);
+  static constexpr int kLoads = 2 + kX / 8;  // of a wave to a stage
+  static_assert(kW * 1024 <= kLds && kLds <= 160 * 1024);
 
   // Row of its eight and byte of its line that this lane brings in load i of W, or of x.
   static __device__ __forceinline__ uint32_t row_of() { return threadIdx.x % 64 / 8; }
@@ -50,21 +50,20 @@ struct Ring {
   };
   template <class LoadX, class LoadW, class Ready>
   static __device__ __forceinline__ void product(uint8_t* lds, uint32_t blocks, LoadX load_x,
-                                                 LoadW load_w, i32x4 (&acc)[kNT], Ready ready) {
+                                                 LoadW load_w, i32x4& acc, Ready ready) {
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     uint8_t* mine = lds + wave * kWave;
     const uint32_t base = __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>(
         (__attribute__((address_space(3))) uint8_t*)mine)));
-#pragma unroll
-    for (int n = 0; n < kNT; n++) acc[n] = {0, 0, 0, 0};
+    acc = {0, 0, 0, 0};
     const uint32_t count = blocks > wave ? (blocks - wave + kW - 1) / kW : 0;
     const auto start = [&](uint32_t j, uint32_t slot) {
       const uint32_t to = base + slot * kStageBytes, at = (wave + j * kW) * kStage;
 #pragma unroll
-      for (int i = 0; i < 2 * kNT; i++) load_w(i, at, to + i * 1024);
+      for (int i = 0; i < 2; i++) load_w(i, at, to + i * 1024);
 #pragma unroll
-      for (int i = 0; i < kX / 8; i++) load_x(i, at, to + (2 * kNT + i) * 1024);
+      for (int i = 0; i < kX / 8; i++) load_x(i, at, to + (2 + i) * 1024);
     };
 #pragma unroll
     for (uint32_t j = 0; j < kS - 1; j++)
@@ -75,7 +74,7 @@ struct Ring {
     const uint32_t w0 = r * kStage + c0 * 16, w1 = r * kStage + c1 * 16;
     uint32_t x0, x1;
     if constexpr (kX > 0) {
-      const uint32_t row = r % kX, xr = 16 * kNT * kStage + row * kStage;
+      const uint32_t row = r % kX, xr = 16 * kStage + row * kStage;
       x0 = xr + ((lane / 16) ^ turn(row)) * 16, x1 = xr + ((lane / 16 + 4) ^ turn(row)) * 16;
     } else {
       const uint32_t row = min(r, held.rows - 1), at = row * held.pitch + wave * kStage;
@@ -91,13 +90,10 @@ struct Ring {
       const uint8_t* x = kX > 0 ? s : held.x + j * (kW * kStage);
       const i32x4 a0 = *reinterpret_cast<const i32x4*>(x + x0);
       const i32x4 a1 = *reinterpret_cast<const i32x4*>(x + x1);
-#pragma unroll
-      for (int n = 0; n < kNT; n++) {
-        const i32x4 b0 = *reinterpret_cast<const i32x4*>(s + w0 + n * 16 * kStage);
-        const i32x4 b1 = *reinterpret_cast<const i32x4*>(s + w1 + n * 16 * kStage);
-        acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b0, a0, acc[n], 0, 0, 0);
-        acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b1, a1, acc[n], 0, 0, 0);
-      }
+      const i32x4 b0 = *reinterpret_cast<const i32x4*>(s + w0);
+      const i32x4 b1 = *reinterpret_cast<const i32x4*>(s + w1);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b0, a0, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b1, a1, acc, 0, 0, 0);
       // the reads are done before the next stage's loads can reach their place
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       slot = slot + 1 < kS ? slot + 1 : 0;
@@ -105,22 +101,20 @@ struct Ring {
     __syncthreads();  // the rings are free for the sums
   }
 
-  // The sums of all waves: result (block n, W row, x row) for the caller's threads.
-  static __device__ __forceinline__ void gather(uint8_t* lds, const i32x4 (&acc)[kNT]) {
-    int32_t* part = reinterpret_cast<int32_t*>(lds) + threadIdx.x / 64 * (kNT * 256);
+  // The sums of all waves, for the caller's threads: sum(W row, x row).
+  static __device__ __forceinline__ void gather(uint8_t* lds, const i32x4& acc) {
+    int32_t* part = reinterpret_cast<int32_t*>(lds) + threadIdx.x / 64 * 256;
 #pragma unroll
-    for (int n = 0; n < kNT; n++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) part[n * 256 + i * 64 + threadIdx.x % 64] = acc[n][i];
+    for (int i = 0; i < 4; i++) part[i * 64 + threadIdx.x % 64] = acc[i];
     __syncthreads();
   }
   // lane l holds W rows 4 (l div 16) + i of x row l mod 16
   static __device__ __forceinline__ int32_t sum(const uint8_t* lds, uint32_t w_row, uint32_t x_row) {
     const int32_t* part = reinterpret_cast<const int32_t*>(lds);
-    const uint32_t at = w_row / 16 * 256 + w_row % 4 * 64 + w_row % 16 / 4 * 16 + x_row;
+    const uint32_t at = w_row % 4 * 64 + w_row / 4 * 16 + x_row;
     int32_t v = 0;
 #pragma unroll
-    for (int w = 0; w < kW; w++) v += part[w * (kNT * 256) + at];
+    for (int w = 0; w < kW; w++) v += part[w * 256 + at];
     return v;
   }
 };

@@ -1,7 +1,7 @@
 // wc_i8_tile.h -- the int8 matrix product of one tile by one workgroup, operands
 // through LDS: C[n][m] = sum_k W[n][k] x[m][k] on v_mfma_i32_32x32x32_i8.
 //
-// A stage is kK (64 or 128) bytes of k of every row of the tile.  Both operands go from
+// A stage is 128 bytes of k of every row of the tile.  Both operands go from
 // memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1
 // stages ahead of the products.  A row's 16-byte chunks are stored in the order
 // chunk ^ turn(row): the sixteen lanes that read LDS together, the same chunk of sixteen
@@ -52,16 +52,15 @@ __device__ __forceinline__ void store_rows(u32x4 rs, uint32_t offset, u32x4 v) {
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset past the end of every buffer here
 
-// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages of kK bytes in LDS.
-template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2, int kK = 128>
+// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages in LDS.
+template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2>
 struct Tile {
   static constexpr int kWM_ = kWM, kWN_ = kWN, kWaves = kWM * kWN, kThreads = 64 * kWaves;
   static constexpr int kMT = kBM / kWM / 32, kNT = kBN / kWN / 32;  // 32 x 32 blocks to a wave
-  static constexpr int kBytes = kK, kEach = 1024 / kK;  // rows to a load of a wave
+  static constexpr int kEach = 1024 / kStage;  // rows to a load of a wave
   static constexpr int kXLoads = kBM / kEach / kWaves, kWLoads = kBN / kEach / kWaves;
-  static constexpr int kBuffer = (kBM + kBN) * kK;
+  static constexpr int kBuffer = (kBM + kBN) * kStage;
   static constexpr int kLds = kDepth * kBuffer, kRows = kBM, kCols = kBN;
-  static_assert(kK == 64 || kK == 128);
   static_assert(kBM % (kEach * kWaves) == 0 && kBN % (kEach * kWaves) == 0 && kLds <= 160 * 1024);
 
   // Row of the tile and byte of its stage that load i of this lane brings.
@@ -69,15 +68,13 @@ struct Tile {
     return kEach * (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) + kWaves * i);
   }
   static __device__ __forceinline__ uint32_t row_of(int i) {
-    return first_row(i) + threadIdx.x % 64 / (kK / 16);
+    return first_row(i) + threadIdx.x % 64 / (kStage / 16);
   }
-  static __device__ __forceinline__ uint32_t turn(uint32_t row) {
-    return kK == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
-  }
+  static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (row >> 1) & 7; }
   static __device__ __forceinline__ uint32_t byte_of() {
     // the same for every load: rows kWaves loads apart turn alike
     static_assert(kWaves % 2 == 0);
-    return ((threadIdx.x % (kK / 16)) ^ turn(row_of(0))) * 16;
+    return ((threadIdx.x % (kStage / 16)) ^ turn(row_of(0))) * 16;
   }
 
   // Waits for all but the loads of the newest kLater stages, then for the other waves.
@@ -111,18 +108,18 @@ struct Tile {
     const auto start = [&](int i, uint32_t s, uint32_t slot) {
       const uint32_t to = __builtin_amdgcn_readfirstlane(base + slot * kBuffer + wave * 1024);
       if (i < kXLoads) load_x(i, s, to + uint32_t(i) * kThreads * 16);
-      else load_w(i - kXLoads, s, to + kBM * kK + uint32_t(i - kXLoads) * kThreads * 16);
+      else load_w(i - kXLoads, s, to + kBM * kStage + uint32_t(i - kXLoads) * kThreads * 16);
     };
-    constexpr int kQuarters = kK / 32;
+    constexpr int kQuarters = kStage / 32;
     uint32_t at[kQuarters];
 #pragma unroll
     for (int k = 0; k < kQuarters; k++)
-      at[k] = lane % 32 * kK + ((2 * k + lane / 32) ^ turn(lane % 32)) * 16;
-    const uint32_t xrow = wm * (kBM / kWM) * kK, wrow = (kBM + wn * (kBN / kWN)) * kK;
+      at[k] = lane % 32 * kStage + ((2 * k + lane / 32) ^ turn(lane % 32)) * 16;
+    const uint32_t xrow = wm * (kBM / kWM) * kStage, wrow = (kBM + wn * (kBN / kWN)) * kStage;
     i32x4 x[2][kMT], w[2][kNT];  // operands of two 32-byte quarters of a block
     const auto read = [&](int set, const uint8_t* b, int k, int i) {
-      if (i < kNT) w[set][i] = *reinterpret_cast<const i32x4*>(b + wrow + at[k] + i * 32 * kK);
-      else x[set][i - kNT] = *reinterpret_cast<const i32x4*>(b + xrow + at[k] + (i - kNT) * 32 * kK);
+      if (i < kNT) w[set][i] = *reinterpret_cast<const i32x4*>(b + wrow + at[k] + i * 32 * kStage);
+      else x[set][i - kNT] = *reinterpret_cast<const i32x4*>(b + xrow + at[k] + (i - kNT) * 32 * kStage);
     };
     // The products of one quarter, operand set `set`.  Between them, in the order written:
     // the reads of the next quarter k of the stage in `slot`, and loads kFrom .. kTo - 1 of
