@@ -90,7 +90,8 @@ __device__ __forceinline__ int32_t take_best(uint32_t (&key)[kPer], uint32_t flo
 // The choice of one token by kLanes lanes: expert lane + kLanes i in register i.  A softmax
 // without a bias chooses by the logits, which are in the scores' order, so no two of them
 // fall together by rounding.  Lane j < k gets slot j's expert and weight.  Bound by the
-// chain of k reductions; all lanes of a wave work on as many tokens as fit it.
+// chain of k reductions; all lanes of a wave work on as many tokens as fit it.  4096 tokens of
+// 256 experts, 8 of 4 of 8 groups, 11.8 us; 32771 of 61, 6 of them, 11.3.
 template <int kLanes, int kPer>
 __device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float* scratch,
                                        int32_t& id, float& weight) {
@@ -332,6 +333,9 @@ __device__ __forceinline__ void sort_block(const SortArgs& a, SortShared& sh, ui
   }
 }
 
+// 16 blocks of 257 classes 7.1 us, 97 of 62 6.8, with 4 each for the counts: chains of
+// latencies.  Counts from the choice's own workgroups save that launch, but make rows of
+// counts of 16 to 64 tokens, which this kernel then reads for 5 us and more.
 __global__ __launch_bounds__(kSortThreads) void wc_route_order_kernel(SortArgs a) {
   __shared__ SortShared sh;
   sort_block(a, sh, blockIdx.x, [&](uint32_t slot) { return class_of(a, slot); });
