@@ -542,8 +542,8 @@ typedef struct {
 } wc_i8_job;
 
 /* wc_matmul_i8 -- the products of one batch of quantised activations with
- * n_jobs (1..32) matrices, in one launch (two where k is split into parts, one
- * more where rows of W start within a dword).
+ * n_jobs (1..32) matrices, in one launch (two where k is split into parts or many
+ * rows' results lie apart, one more where rows of W start within a dword).
  *   dev_q, dev_scale  what wc_quantize_i8 wrote for m rows of k (the padding of
  *                     a row must be zero);
  *   dev_workspace     at least wc_matmul_i8_workspace_bytes bytes, 256-byte
