@@ -398,7 +398,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
   uint32_t mt, nt;
   if (!tile_at(blockIdx.x, block_count(a), blocks * step, mt, nt)) return;
   const auto [e, first, last] = block_at(a, mt);
-  const uint32_t class0 = nt % step, r0 = nt / step * kCols;
+  const uint32_t class0 = nt / blocks, r0 = nt % blocks * kCols;
   const ClassRows G = class_rows(a.gate.w + e * a.gate.stride, k, a.ffn, k, step, class0);
   const ClassRows U = class_rows(a.up.w + e * a.up.stride, k, a.ffn, k, step, class0);
   if (r0 >= G.rows) return;
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_down_tile_kernel(Exper
   uint32_t mt, nt;
   if (!tile_at(blockIdx.x, block_count(a), blocks * step, mt, nt)) return;
   const auto [e, first, last] = block_at(a, mt);
-  const uint32_t class0 = nt % step, r0 = nt / step * kBN, m_rows = last - first;
+  const uint32_t class0 = nt / blocks, r0 = nt % blocks * kBN, m_rows = last - first;
   const ClassRows C = class_rows(a.down.w + e * a.down.stride, k, a.hidden, k, step, class0);
   if (r0 >= C.rows) return;
   const uint32_t n_rows = min(kBN, C.rows - r0);

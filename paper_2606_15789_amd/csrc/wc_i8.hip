@@ -413,11 +413,15 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   uint32_t j = 0;
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].tile0) j++;
   const MatJob J = a.job[j];
-  // classes of the same columns one after another, so that their stores meet in a cache
+  // Classes of the same columns one after another, so that their stores meet in a cache;
+  // sums are stored class by class, and class after class their tiles share a copy of x
+  // (m = 4096, k = n = 8191: 352 us against 358).
   const uint32_t blocks = ((J.n + J.step - 1) / J.step + kBN - 1) / kBN;
   uint32_t mt, nt;
   if (!tile_at(blockIdx.x - J.tile0, (a.m + kBM - 1) / kBM, blocks * J.step, mt, nt)) return;
-  const uint32_t m0 = mt * kBM, m_rows = min(kBM, a.m - m0), first = nt % J.step, r0 = nt / J.step * kBN;
+  const uint32_t m0 = mt * kBM, m_rows = min(kBM, a.m - m0);
+  const uint32_t first = a.sums ? nt / blocks : nt % J.step;
+  const uint32_t r0 = (a.sums ? nt % blocks : nt / J.step) * kBN;
   const ClassRows C = class_rows(J.w, J.ldw, J.n, a.k, J.step, first);
   if (r0 >= C.rows) return;
   const uint32_t n_rows = min(kBN, C.rows - r0);
