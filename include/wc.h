@@ -551,7 +551,8 @@ typedef struct {
  *                     share it must not overlap in time.
  * Rows of W may start at any byte; those that start at whole dwords (ldw and w
  * multiples of 4) are faster, and no dword is read that holds no byte of a
- * matrix.  The kernel and the parts of k follow from the sizes alone.  m = 0 is a
+ * matrix.  The kernel and the parts of k follow from the sizes alone.
+ * The matrices have less than 2^27 rows together.  m = 0 is a
  * call that does nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
 wc_status wc_matmul_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                        const wc_i8_job* jobs, uint64_t* bytes);

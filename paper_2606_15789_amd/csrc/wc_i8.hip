@@ -11,7 +11,7 @@ using namespace wc_i8;
 struct QuantArgs {
   uint64_t x, ldx, q, scale, limit;
   uint64_t copies;  // three shifted copies of q (Shifted), or none
-  uint32_t m, k, step;
+  uint32_t m, k, step, first;  // first: this launch's
   Blocks blocks;
 };
 
@@ -67,12 +67,12 @@ template <int kThreads, int kUnits, int kType>
 __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
   constexpr int kWords = kType == WC_FP32 ? 8 : 4;  // to a unit
   __shared__ uint32_t tops[kThreads / 64];
-  const uint64_t row = blockIdx.x;
-  if (blockIdx.x == a.m) {
+  const uint64_t row = a.first + blockIdx.x;
+  if (row == a.m) {
     __shared__ uint32_t starts[kMaxExperts + 1];
     return write_blocks<kThreads>(a.blocks, starts);
   }
-  if (a.limit && int32_t(blockIdx.x) >= *global<const int32_t>(a.limit)) return;
+  if (a.limit && int32_t(row) >= *global<const int32_t>(a.limit)) return;
   const uint64_t first = a.x + row * a.ldx * (kType == WC_FP32 ? 4 : 2);
   const uint32_t units = uint32_t(WC_I8_ROW_BYTES(a.k)) / 8;
   uint32_t v[kUnits][kWords];
@@ -156,22 +156,28 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_i8_kernel(QuantArgs a) {
   }
 }
 
+// Rows to a launch: a grid's axis has less than 2^32 threads.
+constexpr uint32_t kLaunchRows = 1u << 21;
+
 template <int kThreads, int kUnits>
-void start_quantize(int32_t dt, uint32_t m, const QuantArgs& a, hipStream_t stream) {
-  const dim3 grid(m + (a.blocks.table != 0)), block(kThreads);
-  if (dt == WC_BF16)
-    hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_BF16>), grid, block, 0, stream, a);
-  else if (dt == WC_FP16)
-    hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP16>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP32>), grid, block, 0, stream, a);
+void start_quantize(int32_t dt, QuantArgs a, hipStream_t stream) {
+  const uint32_t rows = a.m + (a.blocks.table != 0);
+  for (; a.first < rows; a.first += kLaunchRows) {
+    const dim3 grid(std::min(rows - a.first, kLaunchRows)), block(kThreads);
+    if (dt == WC_BF16)
+      hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_BF16>), grid, block, 0, stream, a);
+    else if (dt == WC_FP16)
+      hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP16>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((wc_quantize_i8_kernel<kThreads, kUnits, WC_FP32>), grid, block, 0, stream, a);
+  }
 }
 
 // Word i of three copies of a row of q, shifted by one, two and three bytes, for codes that
 // were quantised by a call of their own.
 __global__ __launch_bounds__(256) void wc_shift_i8_kernel(uint64_t q, uint64_t copies, uint32_t m,
-                                                          uint32_t k) {
-  const uint64_t row = blockIdx.x;
+                                                          uint32_t k, uint32_t first) {
+  const uint64_t row = first + blockIdx.x;
   const uint32_t words = uint32_t(WC_I8_ROW_BYTES(k)) / 4, wide = uint32_t(WC_I8_ROW_BYTES(k + 3)) / 4;
   const auto from = global<const uint32_t>(q) + row * words;
   for (uint32_t i = threadIdx.x; i < wide; i += 256) {
@@ -527,7 +533,7 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
       return false;
     tiles += (uint64_t(J.n) + 15) / 16;
   }
-  return tiles < (1u << 24);
+  return tiles < (1u << 23);  // workgroups of 512 threads: less than 2^32 of them
 }
 
 bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx) {
@@ -571,11 +577,11 @@ void with_tile(Kernel kernel, F f) {
   }
 }
 // Workgroups for m rows of x and a matrix of n rows in `step` classes.
-uint32_t tiles_of(Kernel kernel, uint32_t m, uint32_t n, uint32_t step) {
+uint64_t tiles_of(Kernel kernel, uint32_t m, uint32_t n, uint32_t step) {
   const uint32_t each = (n + step - 1) / step;
-  uint32_t tiles = step * ((each + 15) / 16);
+  uint64_t tiles = step * ((each + 15) / 16);
   with_tile(kernel, [&](auto t) {
-    tiles = (m + t.kRows - 1) / t.kRows * (step * ((each + t.kCols - 1) / t.kCols));
+    tiles = uint64_t((m + t.kRows - 1) / t.kRows) * (step * ((each + t.kCols - 1) / t.kCols));
   });
   return tiles;
 }
@@ -602,7 +608,7 @@ constexpr double kStridedPerUs = 2.7e5;
 
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   Plan p{Kernel::kRows, false, false, 1, false, 0};
-  uint64_t sums = 0, strided = 0, weights = 0, tiles64 = 0;
+  uint64_t sums = 0, strided = 0, weights = 0;
   bool narrow = true;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
@@ -611,7 +617,6 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
     if (J.ldw > (1u << 20)) return p;
     narrow = narrow && J.n < (1u << 20) && J.ldy < (1u << 20);
     p.copies = p.copies || J.ldw % 4 || reinterpret_cast<uintptr_t>(J.w) % 4;
-    tiles64 += uint64_t(m + 63) / 64 * (J.n / 64 + 4);
     sums += uint64_t(m) * row_pitch(J.n, steps_of(J.ldw)) * 4;
     if (steps_of(J.ldw) > 1) strided += uint64_t(m) * J.n;
   }
@@ -622,18 +627,17 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
              (held <= kHoldAlways || (held <= kHoldSmall && weights <= kHoldSmallWeights));
     return p;
   }
-  if (!narrow || tiles64 > 0x7FFFFFFFu) {
-    p.copies = false;
-    return p;
-  }
   const uint32_t stages = (k + kStage - 1) / kStage;
   double best = 0;
   for (const TileCost& c : kCosts) {
-    double tiles = 0;
+    uint64_t tiles = 0, threads = 0;
+    with_tile(c.kernel, [&](auto t) { threads = t.kThreads; });
     for (uint32_t i = 0; i < n_jobs; i++) tiles += tiles_of(c.kernel, m, jobs[i].n, steps_of(jobs[i].ldw));
+    // a grid's axis has less than 2^32 threads
+    if (!narrow || tiles * threads >> 32) continue;
     for (uint32_t splits : {1u, 2u, 3u, 4u, 6u, 8u}) {
       if (splits > 1 && stages < 4 * splits) break;
-      const double groups = tiles * splits;
+      const double groups = double(tiles * splits);
       const bool two = c.stage_of_two > 0 && groups > kUnits;
       const double rounds = std::ceil(groups / (two ? 2 * kUnits : kUnits));
       double us = rounds * (c.round + (stages + splits - 1) / splits * (two ? c.stage_of_two : c.stage));
@@ -650,6 +654,7 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
       }
     }
   }
+  p.copies = p.copies && p.kernel != Kernel::kRows;
   if (p.sums) p.part_bytes = sums * p.splits;
   return p;
 }
@@ -693,7 +698,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
                 p.kernel == Kernel::kRows ? 1u : steps_of(J.ldw), 0};
     if (p.sums) part += uint64_t(m) * row_pitch(J.n, a.job[i].step) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
-    tiles += tiles_of(p.kernel, m, J.n, a.job[i].step);
+    tiles += uint32_t(tiles_of(p.kernel, m, J.n, a.job[i].step));
     quads = quads && (p.sums || (a.job[i].quads && a.job[i].step == 1));
   }
   if (p.kernel == Kernel::kRing) {
@@ -751,16 +756,16 @@ bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t
                      void* copies, uint32_t step) {
   const QuantArgs a = {reinterpret_cast<uint64_t>(x), ldx, reinterpret_cast<uint64_t>(q),
                        reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(limit),
-                       reinterpret_cast<uint64_t>(copies), m, k, step, blocks ? *blocks : Blocks{}};
+                       reinterpret_cast<uint64_t>(copies), m, k, step, 0, blocks ? *blocks : Blocks{}};
   // few rows: more threads to each
-  if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, m, a, stream);
-  else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, m, a, stream);
-  else if (k <= 2048) start_quantize<256, 1>(dt, m, a, stream);
-  else if (k <= 4096) start_quantize<256, 2>(dt, m, a, stream);
-  else if (k <= 8192) start_quantize<256, 4>(dt, m, a, stream);
-  else if (k <= 16384) start_quantize<256, 8>(dt, m, a, stream);
-  else if (k <= 32768) start_quantize<1024, 4>(dt, m, a, stream);
-  else start_quantize<1024, 8>(dt, m, a, stream);
+  if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, a, stream);
+  else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, a, stream);
+  else if (k <= 2048) start_quantize<256, 1>(dt, a, stream);
+  else if (k <= 4096) start_quantize<256, 2>(dt, a, stream);
+  else if (k <= 8192) start_quantize<256, 4>(dt, a, stream);
+  else if (k <= 16384) start_quantize<256, 8>(dt, a, stream);
+  else if (k <= 32768) start_quantize<1024, 4>(dt, a, stream);
+  else start_quantize<1024, 8>(dt, a, stream);
   return hipGetLastError() == hipSuccess;
 }
 
@@ -806,9 +811,10 @@ extern "C" wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, u
   p.hold = false;
   if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p, m, k))) return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  if (p.copies) {
-    hipLaunchKernelGGL(wc_shift_i8_kernel, dim3(m), dim3(256), 0, st, reinterpret_cast<uint64_t>(dev_q),
-                       reinterpret_cast<uint64_t>(dev_workspace), m, k);
+  for (uint32_t first = 0; p.copies && first < m; first += kLaunchRows) {
+    hipLaunchKernelGGL(wc_shift_i8_kernel, dim3(std::min(m - first, kLaunchRows)), dim3(256), 0, st,
+                       reinterpret_cast<uint64_t>(dev_q), reinterpret_cast<uint64_t>(dev_workspace), m, k,
+                       first);
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
   }
   return matmul(dev_q, dev_scale, m, k, n_jobs, jobs, p, dev_workspace, st);

@@ -1,4 +1,5 @@
 // wc_route.hip -- routing to experts: wc_route.
+#include <algorithm>
 #include <cmath>
 
 #include "wc_i8.h"
@@ -11,6 +12,7 @@ constexpr int kTokenWaves = 4;         // waves to a workgroup of the choice
 constexpr uint32_t kSortThreads = 1024;
 constexpr uint32_t kSortSlots = 2048;  // slots to a workgroup of the sort
 constexpr uint32_t kMaxChosen = 32;
+constexpr uint32_t kLaunchTokens = 1u << 24;  // a grid's axis has less than 2^32 threads
 // Blocks of the sort up to which each counts all slots itself, in place of a launch that
 // counts: 512 tokens of 8 slots (2 blocks) 13.9 us against 15.0, 1500 (6) 17.7 and 16.5,
 // but the host has a launch less.
@@ -22,6 +24,7 @@ constexpr uint32_t kManyTokens = 16384;
 struct RouteArgs {
   uint64_t logits, bias, ids, weights, ld;
   uint32_t tokens, experts, k, groups, top_groups, group_top;
+  uint32_t first;  // this launch's first token
   int32_t dtype, score, renormalize;
   float scale;
 };
@@ -211,7 +214,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(Route
   const uint32_t t = threadIdx.x / kLanes;
   int32_t id;
   float weight;
-  choose<kLanes, kPer>(a, blockIdx.x * kTokens + t, scratch[t], id, weight);
+  choose<kLanes, kPer>(a, a.first + blockIdx.x * kTokens + t, scratch[t], id, weight);
 }
 
 struct SortArgs {
@@ -361,13 +364,17 @@ __global__ __launch_bounds__(kSortThreads) void wc_route_small_kernel(RouteArgs 
 }
 
 template <int kLanes, int kPer>
-void start_choice(const RouteArgs& a, const SortArgs& s, bool small, hipStream_t st) {
+void start_choice(RouteArgs a, const SortArgs& s, bool small, hipStream_t st) {
   constexpr uint32_t kTokens = 64 * kTokenWaves / kLanes;
-  if (small)
+  if (small) {
     hipLaunchKernelGGL((wc_route_small_kernel<kLanes, kPer>), dim3(1), dim3(kSortThreads), 0, st, a, s);
-  else
-    hipLaunchKernelGGL((wc_route_choose_kernel<kLanes, kPer>), dim3((a.tokens + kTokens - 1) / kTokens),
+    return;
+  }
+  for (; a.first < a.tokens; a.first += kLaunchTokens) {
+    const uint32_t tokens = std::min(a.tokens - a.first, kLaunchTokens);
+    hipLaunchKernelGGL((wc_route_choose_kernel<kLanes, kPer>), dim3((tokens + kTokens - 1) / kTokens),
                        dim3(64 * kTokenWaves), 0, st, a);
+  }
 }
 
 bool params_ok(uint32_t tokens, const wc_route_params* p) {
@@ -412,7 +419,7 @@ extern "C" wc_status wc_route(const void* dev_logits, int32_t dtype, uint32_t to
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const RouteArgs a = {reinterpret_cast<uint64_t>(dev_logits), reinterpret_cast<uint64_t>(dev_bias),
                        reinterpret_cast<uint64_t>(dev_ids), reinterpret_cast<uint64_t>(dev_weights),
-                       ld, tokens, p->experts, p->k, p->groups, p->top_groups, p->group_top, dtype,
+                       ld, tokens, p->experts, p->k, p->groups, p->top_groups, p->group_top, 0, dtype,
                        p->score, p->renormalize, p->scale};
   const SortArgs s = {a.ids, reinterpret_cast<uint64_t>(dev_offsets),
                       reinterpret_cast<uint64_t>(dev_order),

@@ -296,3 +296,25 @@ def test_refusals(dev):
         with pytest.raises(wc.WcError):
             call()
     assert np.isfinite(wc.linear_i8_torch(x, [w], [s])[0].float().cpu().numpy()).all()
+
+
+def test_more_rows_than_a_launch_has_threads_for(dev):
+    """2^24 rows and a few: a grid of one workgroup of 256 threads to each is too large.
+
+    The codes are the formula's, on the device with the same fp32 operations; W's rows
+    start at every byte of a dword, so copies of x are made, beside the codes and from them.
+    """
+    m, k, n = (1 << 24) + 5, 3, 6
+    g = torch.Generator(device=dev).manual_seed(24)
+    x = torch.randn((m, k), generator=g, device=dev).half()
+    q, scale = wc.quantize_i8_torch(x)
+    top = x.float().abs().amax(dim=1)
+    want = torch.round(x.float() * (torch.full_like(top, 127.0) / top)[:, None])
+    assert torch.equal(q[:, :k].float(), want) and not bool(q[-70:, k:].any())
+    assert torch.equal(scale, top / torch.full_like(top, 127.0))
+    w, ws = _codes(_gen(1), n, k).to(dev), torch.rand(n, generator=_gen(2)).to(dev)
+    p = (want.double() @ w.double().T) * scale.double()[:, None] * ws.double()
+    for y in (wc.linear_i8_torch(x, [w], [ws], dtype=torch.float32)[0],
+              wc.matmul_i8_torch(q, scale, k, [w], [ws], dtype=torch.float32)[0]):
+        off = (y.double() - p).abs()
+        assert bool((off <= 1.01 * 5 * 2.0 ** -24 * p.abs() + LEAST[y.dtype]).all())

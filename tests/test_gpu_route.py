@@ -276,3 +276,20 @@ def test_refusals(dev):
                  lambda: wc.route_torch(torch.zeros((2, 64), device=dev), 33)):
         with pytest.raises(wc.WcError):
             call()
+
+
+def test_more_tokens_than_a_launch_has_threads_for(dev):
+    """2^26 tokens and a few, of a whole wave each."""
+    tokens, experts = (1 << 26) + 3, 33
+    x = torch.randint(-128, 128, (tokens, experts), dtype=torch.int8, device=dev).bfloat16()
+    r = wc.route_torch(x, 1, "sigmoid", bias=torch.arange(experts, device=dev) * -0.125)
+    at, ids = r.order.long(), r.ids[:, 0].long()
+    key = ids[at] * 2 ** 32 + at
+    assert bool((key[1:] > key[:-1]).all())
+    assert torch.equal(r.offsets[1:].long(), torch.bincount(ids, minlength=experts).cumsum(0))
+    for part in (slice(0, 1 << 20), slice((1 << 24) - 5, (1 << 24) + 5), slice(tokens - (1 << 20), tokens)):
+        keys = torch.sigmoid(x[part].double()) - torch.arange(experts, device=dev) * 0.125
+        top, best = keys.sort(dim=1, descending=True)
+        clear = top[:, 0] - top[:, 1] > 1e-6
+        assert float(clear.float().mean()) > 0.5
+        assert torch.equal(ids[part][clear], best[:, 0][clear])
