@@ -54,6 +54,14 @@ __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place)
   return min(uint32_t(max(global<const int32_t>(a.order)[place], 0)), a.slots - 1);
 }
 
+// g / (1 + exp(-g)) by the unit's own exponential and reciprocal, each within an ulp: with
+// the rounding of g log2(e) a relative error under 2^-23 (3 + |g|), of a value that goes to 8
+// bits next.  expf and a division took 2773 us, not 2704, at 4096 tokens of 8 experts of 6144 x
+// 16384, and 291, not 273, at 2000 tokens, 6 each, of 64 of 2048 x 1408.
+__device__ __forceinline__ float silu(float g) {
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+}
+
 // 16 columns of an expert's result for up to 16 of its rows: kMats products that
 // share their rows (gate and up, or down alone), k split over the waves.
 template <int kMats>
@@ -119,7 +127,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_up_kernel(ExpertArg
                     load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(summed<2>(part, 1, o % 16, o / 16)) * xs *
                     load_float(a.up.scale, a.up.scale_dtype, at);
-    global<float>(a.h)[uint64_t(place) * row_pitch(a.ffn, 1) + n] = g / (1.0f + expf(-g)) * u;
+    global<float>(a.h)[uint64_t(place) * row_pitch(a.ffn, 1) + n] = silu(g) * u;
   }
 }
 
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(ExpertRing<kX>::kThreads) void wc_experts_up_ring_k
     const float g = float(R::sum(lds, r, o / 8)) * xs * load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(R::sum(lds, 8 + r, o / 8)) * xs * load_float(a.up.scale, a.up.scale_dtype, at);
     global<float>(a.h)[uint64_t(place) * row_pitch(a.ffn, step) + class0 * class_pitch(a.ffn, step) + r0 + r] =
-        g / (1.0f + expf(-g)) * u;
+        silu(g) * u;
   }
 }
 
@@ -261,7 +269,7 @@ __global__ __launch_bounds__(SlotRing::kThreads) void wc_experts_up_slot_kernel(
     const uint64_t at = uint64_t(e) * a.ffn + n;
     const float g = float(R::sum(lds, threadIdx.x, 0)) * scale[0] * load_float(a.gate.scale, a.gate.scale_dtype, at);
     const float u = float(R::sum(lds, 8 + threadIdx.x, 0)) * scale[0] * load_float(a.up.scale, a.up.scale_dtype, at);
-    global<float>(a.h)[uint64_t(slot) * row_pitch(a.ffn, 1) + n] = g / (1.0f + expf(-g)) * u;
+    global<float>(a.h)[uint64_t(slot) * row_pitch(a.ffn, 1) + n] = silu(g) * u;
   }
 }
 
@@ -454,7 +462,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertA
 #pragma unroll
           for (int i = 0; i < 4; i++) {
             const float g = g4[i] * xs * gs[i], u = u4[i] * xs * us[i];
-            h[i] = g / (1.0f + expf(-g)) * u;
+            h[i] = silu(g) * u;
           }
           store_rows(to, out + row * pitch, __builtin_bit_cast(u32x4, h));
         });
