@@ -85,8 +85,8 @@ struct Tile {
 
   // `load_x(i, stage, lds)` and `load_w(i, stage, lds)` start load i of a stage's rows
   // of x and W.
-  // Waves all of whose rows of x are past the first `rows` only load: the other wave of
-  // their SIMD has the matrix unit to itself.
+  // Of a wave's blocks of 32 rows of x, those past the first `rows` are not multiplied; a wave
+  // without any only loads.  A block then takes the matrix unit, and the power, of its rows.
   template <class LoadX, class LoadW>
   static __device__ __forceinline__ void product(uint8_t* lds, uint32_t stages, uint32_t rows,
                                                  LoadX load_x, LoadW load_w,
@@ -124,10 +124,11 @@ struct Tile {
     // The products of one quarter, operand set `set`.  Between them, in the order written:
     // the reads of the next quarter k of the stage in `slot`, and loads kFrom .. kTo - 1 of
     // stage `s`, so that the matrix unit never waits for a queue of either to drain.
-    const auto quarter = [&]<int kFrom, int kTo>(int set, uint32_t slot, int k, uint32_t s, uint32_t to,
-                                                 std::integer_sequence<int, kFrom, kTo>) {
+    const auto quarter = [&]<int kLive, int kFrom, int kTo>(
+                             int set, uint32_t slot, int k, uint32_t s, uint32_t to,
+                             std::integer_sequence<int, kLive, kFrom, kTo>) {
       const uint8_t* b = lds + slot * kBuffer;
-      constexpr int kProducts = kMT * kNT, kReads = kMT + kNT;
+      constexpr int kProducts = kLive * kNT, kReads = kLive + kNT;
 #pragma unroll
       for (int p = 0; p < kProducts; p++) {
         const int m = p / kNT, n = p % kNT;
@@ -144,9 +145,6 @@ struct Tile {
     // two stages: all loads as early as they can be (1546 us against 1583 at m = 8192, k = 8192,
     // n = 28672); more are spread over two quarters
     constexpr int kHalf = kDepth == 2 ? kAll : kAll / 2;
-    using First = std::integer_sequence<int, 0, kHalf>;
-    using Second = std::integer_sequence<int, kHalf, kAll>;
-    using None = std::integer_sequence<int, 0, 0>;
 #pragma unroll
     for (uint32_t s = 0; s < kAhead; s++)
 #pragma unroll
@@ -154,10 +152,10 @@ struct Tile {
     arrive<int(kAhead) - 1>();
 #pragma unroll
     for (int i = 0; i < kHalf; i++) start(i, kAhead, kAhead);
-#pragma unroll
-    for (int i = 0; i < kMT + kNT; i++) read(0, lds, 0, i);
     uint32_t slot = 0, fill = kAhead;  // the stage's place, and that of the one it loads
-    if (__builtin_amdgcn_readfirstlane(wm) * (kBM / kWM) >= rows) {
+    const uint32_t row0 = __builtin_amdgcn_readfirstlane(wm) * (kBM / kWM);
+    const uint32_t live = rows > row0 ? (rows - row0 + 31) / 32 : 0;
+    if (live == 0) {
       for (uint32_t s = 0; s < stages; s++) {
 #pragma unroll
         for (int i = kHalf; i < kAll; i++) start(i, s + kAhead, fill);
@@ -171,20 +169,31 @@ struct Tile {
       __syncthreads();
       return;
     }
-    for (uint32_t s = 0; s < stages; s++) {
-      quarter(0, slot, 1, s + kAhead, fill, Second{});
+    const auto run = [&]<int kLive>(std::integer_sequence<int, kLive>) {
+      using First = std::integer_sequence<int, kLive, 0, kHalf>;
+      using Second = std::integer_sequence<int, kLive, kHalf, kAll>;
+      using None = std::integer_sequence<int, kLive, 0, 0>;
 #pragma unroll
-      for (int k = 1; k < kQuarters - 1; k++) quarter(k & 1, slot, k + 1, 0, 0, None{});
-      // Before the last quarter's products: the next stage's loads of this wave are in LDS
-      // and its reads of this stage done, and so with the other waves behind the barrier.
-      // The stage after those in flight then replaces this one.
-      // lgkmcnt(0) as the compiler knows it: no waits for these operands further on
-      __builtin_amdgcn_s_waitcnt(0xC07F);
-      arrive<int(kAhead) - 1>();
-      fill = slot;
-      slot = slot + 1 < kDepth ? slot + 1 : 0;
-      quarter(1, slot, 0, s + 1 + kAhead, fill, First{});
-    }
+      for (int i = 0; i < kLive + kNT; i++) read(0, lds, 0, i);
+      for (uint32_t s = 0; s < stages; s++) {
+        quarter(0, slot, 1, s + kAhead, fill, Second{});
+#pragma unroll
+        for (int k = 1; k < kQuarters - 1; k++) quarter(k & 1, slot, k + 1, 0, 0, None{});
+        // Before the last quarter's products: the next stage's loads of this wave are in LDS
+        // and its reads of this stage done, and so with the other waves behind the barrier.
+        // The stage after those in flight then replaces this one.
+        // lgkmcnt(0) as the compiler knows it: no waits for these operands further on
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        arrive<int(kAhead) - 1>();
+        fill = slot;
+        slot = slot + 1 < kDepth ? slot + 1 : 0;
+        quarter(1, slot, 0, s + 1 + kAhead, fill, First{});
+      }
+    };
+    if (live >= kMT) run(std::integer_sequence<int, kMT>{});
+    else if (kMT > 3 && live == 3) run(std::integer_sequence<int, (kMT > 3 ? 3 : 1)>{});
+    else if (kMT > 2 && live == 2) run(std::integer_sequence<int, (kMT > 2 ? 2 : 1)>{});
+    else run(std::integer_sequence<int, 1>{});
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // the waves leave together: LDS is free for the results
     __syncthreads();
