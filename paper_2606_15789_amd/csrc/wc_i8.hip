@@ -194,9 +194,7 @@ struct MatJob {
   uint64_t part;      // where k is split: its int32 sums, split by split
   uint32_t n, tile0;  // tile0: its first workgroup
   int32_t scale_dtype, bias_dtype, y_dtype;
-  uint32_t quads;     // y's columns are whole aligned groups of four
   uint32_t step;      // classes of rows (class_rows)
-  uint32_t reserved;
 };
 struct MatArgs {
   uint64_t q, qscale;
@@ -328,16 +326,16 @@ __device__ __forceinline__ void finish(const MatJob& J, uint32_t m, uint32_t n, 
   f32x4 v;
 #pragma unroll
   for (int i = 0; i < 4; i++) v[i] = sum[i] * xs * scale[i] + bias[i];
-  if (J.quads && n + 4 <= J.n) {
+  if (n + 4 <= J.n) {
     if (J.y_dtype == WC_FP32) {
-      *reinterpret_cast<global_ptr<f32x4>>(global<float>(J.y) + at) = v;
+      *reinterpret_cast<global_ptr<u32x4u>>(global<float>(J.y) + at) = __builtin_bit_cast(u32x4, v);
     } else {
       u32x2 h;
       if (J.y_dtype == WC_BF16)
         h = {floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])};
       else
         h = {float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16, float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16};
-      *reinterpret_cast<global_ptr<u32x2>>(global<uint16_t>(J.y) + at) = h;
+      *reinterpret_cast<global_ptr<u32x2u>>(global<uint16_t>(J.y) + at) = h;
     }
   } else {
 #pragma unroll
@@ -405,13 +403,13 @@ __device__ __forceinline__ void tile_out(uint8_t* lds, const i32x16 (&acc)[T::kM
 
 // y[m][n] = (sum_k x[m][k] W[n][k]) xs[m] ws[n] + b[n], one tile of a job (and one part of
 // k) a workgroup; the sums are exact, each result is rounded once to fp32 a factor, and once
-// to y's type.  kQuads: every job's results are whole aligned groups of four.
+// to y's type.
 // Bound by the matrix units, and they by the card's power: m = 8192, k = 8192, n = 28672 on
 // 256 x 256 1520 us, 2.53 POP/s, the units busy 72 % of the cycles at 1.67 GHz; m = 512, k =
 // 28672, n = 8192 on 256 x 128, two parts of k, 112 us, 2.15 POP/s.  The
 // larger the tile, the fewer bytes of L2 and LDS a product needs: as large as still leaves
 // tiles for all compute units (plan_of).
-template <class T, bool kQuads>
+template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
   __shared__ float scales[T::kRows];  // of the tile's rows of x
@@ -458,18 +456,19 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
   if (threadIdx.x < kBM) scales[threadIdx.x] = row_scale;
   __syncthreads();
   const uint32_t row0 = wave / T::kWN_ * (T::kMT * 32);
-  const auto out = [&]<int kType>(std::integer_sequence<int, kType>) {
-    // sums are stored class by class, results where they belong
+  // Results that are neighbours in y are stored in groups of four, at any element; class by
+  // class, and in the last tile of a row that ends within a group, one by one.  Sums are
+  // stored class by class, in whole groups.
+  const bool groups = J.step == 1 && n_rows % 4 == 0;
+  const auto out = [&]<int kType, int kGroups>(std::integer_sequence<int, kType, kGroups>) {
     constexpr uint32_t kSize = kType == 0 || kType == WC_FP32 ? 4 : 2;
-    constexpr bool kGroups = kQuads || kType == 0;
-    const uint32_t step = kType ? J.step : 1, sums = row_pitch(J.n, J.step) * 4;
+    const uint32_t step = kGroups ? 1 : J.step, sums = row_pitch(J.n, J.step) * 4;
     const uint32_t pitch = kType ? uint32_t(J.ldy) * kSize : sums;
     const uint64_t row = kType ? J.y + m0 * uint64_t(pitch) : J.part + (uint64_t(part) * a.m + m0) * pitch;
     const uint32_t column0 =
         (kType ? first + r0 * J.step : first * class_pitch(J.n, J.step) + r0) * kSize;
     // to the last column of the last row, or of its group of four
-    const uint32_t end = ((n_rows - 1) * step + 1) * kSize;
-    const uint32_t group = kGroups ? 4 * kSize : kSize;
+    const uint32_t end = ((n_rows - 1) * step + 1) * kSize, group = kGroups ? 4 * kSize : kSize;
     const u32x4 to = rows_rsrc(row + column0, (m_rows - 1) * pitch + (end + group - 1) / group * group);
     uint32_t at[4];
 #pragma unroll
@@ -477,14 +476,19 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_i8_tile_kernel(MatArgs 
       at[i] = column + (kGroups ? 0 : i) < n_rows ? (column + i) * step * kSize : kNowhere;
     tile_out<T, kType, kGroups>(lds, acc, to, pitch, row0, at, scales, scale, bias);
   };
-  if (a.sums) out(std::integer_sequence<int, 0>{});
-  else if (J.y_dtype == WC_BF16) out(std::integer_sequence<int, WC_BF16>{});
-  else if (J.y_dtype == WC_FP16) out(std::integer_sequence<int, WC_FP16>{});
-  else out(std::integer_sequence<int, WC_FP32>{});
+  const auto of_type = [&]<int kType>(std::integer_sequence<int, kType>) {
+    if (groups) out(std::integer_sequence<int, kType, 1>{});
+    else out(std::integer_sequence<int, kType, 0>{});
+  };
+  if (a.sums) out(std::integer_sequence<int, 0, 1>{});
+  else if (J.y_dtype == WC_BF16) of_type(std::integer_sequence<int, WC_BF16>{});
+  else if (J.y_dtype == WC_FP16) of_type(std::integer_sequence<int, WC_FP16>{});
+  else of_type(std::integer_sequence<int, WC_FP32>{});
 }
 
 // y from the sums of the parts of k, or, where W's rows are in classes, from one: each sum
-// read once, four columns a thread.  512 x 8192 of two parts 11.9 us (3.5 TB/s).
+// read once, four columns a thread (four of each class a thread, with loads of four, took a
+// third longer for want of threads).  512 x 8192 of two parts 11.9 us (3.5 TB/s).
 __global__ __launch_bounds__(256) void wc_matmul_i8_join_kernel(MatArgs a) {
   const uint32_t j = blockIdx.z;
   const MatJob J = a.job[j];
@@ -685,21 +689,16 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
   a.splits = p.splits;
   a.sums = p.sums;
   uint32_t tiles = 0, widest = 0;
-  bool quads = true;
   uint64_t part = reinterpret_cast<uint64_t>(workspace) + (p.copies ? copies_bytes(m, k) : 0);
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
-    const uint32_t size = size_of(J.y_dtype);
     a.job[i] = {reinterpret_cast<uint64_t>(J.w),    reinterpret_cast<uint64_t>(J.scale),
                 reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
                 J.ldw, J.ldy, part, J.n, tiles, J.scale_dtype, J.bias_dtype, J.y_dtype,
-                J.n % 4 == 0 && J.ldy % 4 == 0 &&
-                    reinterpret_cast<uintptr_t>(J.y) % (4 * size) == 0,
-                p.kernel == Kernel::kRows ? 1u : steps_of(J.ldw), 0};
+                p.kernel == Kernel::kRows ? 1u : steps_of(J.ldw)};
     if (p.sums) part += uint64_t(m) * row_pitch(J.n, a.job[i].step) * 4 * p.splits;
     widest = J.n > widest ? J.n : widest;
     tiles += uint32_t(tiles_of(p.kernel, m, J.n, a.job[i].step));
-    quads = quads && (p.sums || (a.job[i].quads && a.job[i].step == 1));
   }
   if (p.kernel == Kernel::kRing) {
     a.m = m;
@@ -715,10 +714,7 @@ wc_status matmul(const int8_t* q, const float* scale, uint32_t m, uint32_t k, ui
     const dim3 grid(tiles, p.splits);
     with_tile(p.kernel, [&](auto t) {
       using T = decltype(t);
-      if (quads)
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, true>), grid, dim3(T::kThreads), 0, stream, a);
-      else
-        hipLaunchKernelGGL((wc_matmul_i8_tile_kernel<T, false>), grid, dim3(T::kThreads), 0, stream, a);
+      hipLaunchKernelGGL(wc_matmul_i8_tile_kernel<T>, grid, dim3(T::kThreads), 0, stream, a);
     });
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
     if (p.sums) {
