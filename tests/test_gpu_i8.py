@@ -318,3 +318,20 @@ def test_more_rows_than_a_launch_has_threads_for(dev):
               wc.matmul_i8_torch(q, scale, k, [w], [ws], dtype=torch.float32)[0]):
         off = (y.double() - p).abs()
         assert bool((off <= 1.01 * 5 * 2.0 ** -24 * p.abs() + LEAST[y.dtype]).all())
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("m", [20, 130, 520])
+@pytest.mark.parametrize("n,off", [(140, 1), (140, 2), (268, 3), (77, 1), (301, 2), (5, 3)])
+def test_results_at_any_element(dev, dtype, m, n, off):
+    """y's rows start at any element of a larger matrix, nothing beside them is written."""
+    g = _gen(m + n)
+    k = 256
+    x = torch.randn((m, k), generator=g).half()
+    w, ws, b = _codes(g, n, k), torch.rand(n, generator=g) * 0.01, torch.randn(n, generator=g)
+    wide = torch.full((m + 2, n + 7), 7.0, dtype=DT[dtype], device=dev)
+    y = wide[1:m + 1, off:off + n]
+    wc.linear_i8_torch(x.to(dev), [w.to(dev)], [ws.to(dev)], [b.to(dev)], ys=[y])
+    _check(y, *_quantised(x), w, ws, b)
+    y.fill_(7.0)
+    assert bool((wide == 7.0).all())
