@@ -390,11 +390,10 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
 
 // The same on tiles through LDS.  A wave's columns of W are 32 of gate and the same 32
 // of up, so that both products of a value of h meet in one lane.  With few rows to an
-// expert bound by reading W: 8 experts of 6144 x 16384, 32 tokens 2 each, 297 us up (5.4
-// TB/s) and 160 down (5.0).  With many by the matrix units: 4096 tokens, 1652 us up (2.0
-// POP/s, the units busy 54 % of the cycles at 1.87 GHz: 48 stages to a tile, then 128 KB
-// of h from every compute unit at once) and 863 down (1.9; 864 tiles are 3.4 rounds of
-// workgroups).
+// expert bound by reading W: 8 experts of 6144 x 16384, 32 tokens 2 each, 287 us up (5.6
+// TB/s) and 159 down (5.1).  With many by the matrix units: 4096 tokens, 1551 us up (2.1
+// POP/s, the units busy 54 % of the cycles at 1.90 GHz; a stage of 128 bytes takes 1.65 us,
+// all else of a tile 13) and 858 down (1.9; 864 tiles are 3.4 rounds of workgroups).
 template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];

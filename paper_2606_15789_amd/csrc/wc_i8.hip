@@ -405,8 +405,8 @@ __device__ __forceinline__ void tile_out(uint8_t* lds, const i32x16 (&acc)[T::kM
 // k) a workgroup; the sums are exact, each result is rounded once to fp32 a factor, and once
 // to y's type.
 // Bound by the matrix units, and they by the card's power: m = 8192, k = 8192, n = 28672 on
-// 256 x 256 1520 us, 2.53 POP/s, the units busy 72 % of the cycles at 1.67 GHz; m = 512, k =
-// 28672, n = 8192 on 256 x 128, two parts of k, 112 us, 2.15 POP/s.  The
+// 256 x 256 1500 us, 2.56 POP/s, the units busy 71 % of the cycles at 1.7 GHz; m = 512, k =
+// 28672, n = 8192 on 256 x 128, two parts of k, 108 us, 2.23 POP/s.  The
 // larger the tile, the fewer bytes of L2 and LDS a product needs: as large as still leaves
 // tiles for all compute units (plan_of).
 template <class T>
