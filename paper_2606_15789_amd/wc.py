@@ -824,12 +824,17 @@ def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, device):
         raise ValueError("one scale tensor, bias entry and y a matrix")
     floats = _types()
     jobs, out = [], []
+    yt = floats.get(dtype)
     for i in range(n_jobs):
         w, s = ws[i], scales[i]
-        ldw = _rows(w, "w", k)
+        # (each look at a tensor costs the host as much as a microsecond's tenth)
+        shape, stride = w.shape, w.stride()
+        if len(shape) != 2 or shape[1] != k or not w.is_cuda or (stride[1] != 1 and k > 1):
+            _rows(w, "w", k)
         if w.dtype not in _ints:
             raise ValueError("w must be int8 codes")
-        n = w.shape[0]
+        n = shape[0]
+        ldw = stride[0] if n > 1 else k
         st = _vector(s, n, "a matrix's scale")
         b = None if biases is None else biases[i]
         bp, bt = (0, 0) if b is None else (b.data_ptr(), _vector(b, n, "a bias"))
@@ -840,7 +845,7 @@ def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, device):
             if y.shape != (m, n):
                 raise ValueError(f"y must be {m} x {n}")
             ldy = _rows(y, "y")
-        yt = floats.get(y.dtype)
+            yt = floats.get(y.dtype)
         if yt is None:
             raise ValueError("y must be bfloat16, float16 or float32")
         out.append(y)
@@ -886,6 +891,10 @@ def linear_i8_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
     need = C.c_uint64(0)
     with where:
         jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, x.device)
+        # one or two rows mostly need no workspace, and the call refuses those that do
+        if m <= 2 and workspace is None and \
+                not lib().wc_linear_i8(x.data_ptr(), dt, m, k, ld, len(ws), jobs, None, 0, st):
+            return ys
         rc = lib().wc_linear_i8_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
         if not rc:
             workspace = _workspace(workspace, need.value, x.device)
@@ -920,7 +929,9 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
     params = _RouteParams(experts, k, SCORES[score], int(renormalize), groups, top_groups,
                           group_top, scale)
     need = C.c_uint64(0)
-    rc = lib().wc_route_workspace_bytes(tokens, C.byref(params), C.byref(need))
+    # few slots need no workspace
+    rc = 0 if 0 < tokens * k <= 2048 and workspace is None else \
+        lib().wc_route_workspace_bytes(tokens, C.byref(params), C.byref(need))
     if rc:
         raise WcError("wc_route", rc)
     with where:
