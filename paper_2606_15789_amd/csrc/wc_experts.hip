@@ -297,32 +297,25 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
   int32_t ids = lane < a.k ? global<const int32_t>(a.ids)[first + lane] : -1;
   asm volatile("" : "+v"(ids));  // here, before loads that should not be waited for
   const auto id_of = [&](uint32_t s) { return __builtin_amdgcn_readlane(ids, int(s)); };
-  // This wave's blocks of k: every kW-th of all the slots' blocks, one slot after another.
-  struct At {
-    uint32_t slot, block;
-  };
-  const auto settle = [&](At& at) {
-    while (at.block >= blocks) at = {at.slot + 1, at.block - blocks};
-    // a slot without an expert has no products
-    while (at.slot < a.k && id_of(at.slot) < 0) at.slot++;
-  };
-  const auto start = [&](const At& at, uint32_t place) {
-    const uint32_t e = min(uint32_t(id_of(at.slot)), a.experts - 1);
+  const uint32_t used = uint32_t(__ballot(ids >= 0));
+  const auto start = [&](const SlotBlock& at, uint32_t place) {
+    const uint32_t e = min(uint32_t(id_of(at.slot())), a.experts - 1);
     const u32x4 wr = rows_rsrc(a.down.w + e * a.down.stride + uint64_t(n0) * k, n_rows * k);
     const uint32_t to = base + place * R::kStageBytes;
 #pragma unroll
     for (int i = 0; i < 2; i++) load_lds(wr, to + i * 1024, woff[i] + at.block * kStage);
   };
-  At ahead = {0, wave}, here = {0, wave};
-  settle(ahead);
-  settle(here);
+  // This wave's blocks of k: every kW-th of all the used slots' blocks.
+  SlotBlock ahead = {used, wave};
+  settle_block(ahead, blocks);
+  SlotBlock here = ahead;
   uint32_t begun = 0;
 #pragma unroll
   for (uint32_t j = 0; j < kS - 1; j++)
-    if (ahead.slot < a.k) {
+    if (ahead.left) {
       start(ahead, j);
       ahead.block += kW;
-      settle(ahead);
+      settle_block(ahead, blocks);
       begun++;
     }
   hold_rows<R::kThreads, WC_FP32, 3>(
@@ -338,23 +331,24 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
 #pragma unroll
       for (int i = 0; i < 4; i++) part[(slot * kW + wave) * 16 + lane / 16 * 4 + i] = acc[i];
   };
-  uint32_t place = 0, done = 0, slot = here.slot;
-  while (here.slot < a.k) {
-    if (ahead.slot < a.k) {
+  uint32_t place = 0, done = 0, slot = 0;
+  while (here.left) {
+    if (ahead.left) {
       start(ahead, place ? place - 1 : kS - 1);
       ahead.block += kW;
-      settle(ahead);
+      settle_block(ahead, blocks);
       begun++;
     }
     R::wait_for<kS - 1>(min(begun - 1 - done, kS - 1));
     const uint8_t* s = mine + place * R::kStageBytes;
-    const uint8_t* x = lds + R::kLds + here.slot * row_bytes + here.block * kStage;
-    if (here.slot != slot) {
-      leave(slot);
+    const uint32_t now = here.slot();
+    const uint8_t* x = lds + R::kLds + now * row_bytes + here.block * kStage;
+    if (now != slot) {
+      if (done) leave(slot);
       acc = {0, 0, 0, 0};
-      slot = here.slot;
+      slot = now;
     }
-    const uint32_t turn = here.slot % 8;
+    const uint32_t turn = now % 8;
     const i32x4 a0 = *reinterpret_cast<const i32x4*>(x + ((lane / 16) ^ turn) * 16);
     const i32x4 a1 = *reinterpret_cast<const i32x4*>(x + ((lane / 16 + 4) ^ turn) * 16);
     const i32x4 b0 = *reinterpret_cast<const i32x4*>(s + w0);
@@ -365,9 +359,9 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
     place = place + 1 < kS ? place + 1 : 0;
     done++;
     here.block += kW;
-    settle(here);
+    settle_block(here, blocks);
   }
-  if (slot < a.k) leave(slot);
+  if (done) leave(slot);
   __syncthreads();
   const uint32_t n = n0 + threadIdx.x;
   if (threadIdx.x < 16 && n < a.hidden) {

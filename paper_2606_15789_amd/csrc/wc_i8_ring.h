@@ -119,6 +119,19 @@ struct Ring {
   }
 };
 
+// A place among the blocks of a token's slots that have an expert, `blocks` to each, counted
+// one such slot after another: block `block` from the start of the lowest slot of `left`, the
+// set of those from there on.  settle_block moves it to the slot that block lies in (none
+// left: past the last).  Slots without an expert are in no set and have no blocks, so waves
+// stay as many blocks apart wherever a token's empty slots lie.
+struct SlotBlock {
+  uint32_t left, block;
+  __host__ __device__ __forceinline__ uint32_t slot() const { return uint32_t(__builtin_ctz(left)); }
+};
+__host__ __device__ __forceinline__ void settle_block(SlotBlock& at, uint32_t blocks) {
+  while (at.left && at.block >= blocks) at = {at.left & (at.left - 1), at.block - blocks};
+}
+
 // Quantise `rows` rows of x into LDS, chunk c of each 128-byte block of row r at chunk
 // c ^ (r mod 8); `row_at(r)` is a row's address, 16-byte aligned, k elements (a multiple
 // of 8) of type kType.  A thread's first kKeep units of eight elements are on their way

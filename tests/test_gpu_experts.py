@@ -283,3 +283,19 @@ def test_refusals(dev):
     none = wc.experts_i8_torch(torch.zeros((0, 64), device=dev),
                                wc.route_torch(torch.zeros((0, 4), device=dev), 2), *layer)
     assert tuple(none.shape) == (0, 64)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 4, 5, 10, 40, 300])
+@pytest.mark.parametrize("ffn", [8, 256, 768, 1024, 1408])
+def test_empty_slots_anywhere(dev, tokens, ffn):
+    """Empty slots before, between and after used ones, with weights of their own that count
+    for nothing: few tokens slot by slot, few rows to an expert, many."""
+    g = torch.Generator().manual_seed(tokens * ffn)
+    E, k, hidden = 40, 8, 256
+    layer = _layer(6, E, hidden, ffn)
+    x = torch.randn((tokens, hidden), generator=g).bfloat16()
+    for empty in (torch.tensor([1, 0, 0, 0, 0, 0, 0, 0]), torch.tensor([0, 0, 0, 1, 0, 0, 0, 0]),
+                  torch.tensor([1, 1, 1, 1, 1, 1, 1, 0]), torch.rand((tokens, k), generator=g) < 0.5):
+        ids = torch.where(empty.bool().expand(tokens, k), -1, _ids(g, tokens, E, k))
+        r = _routing(ids, torch.rand((tokens, k), generator=g), E)
+        _check(_run(dev, x, r, layer), x, r, layer)
