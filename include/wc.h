@@ -592,8 +592,11 @@ typedef struct {
  * scale.
  *   An expert whose logit or bias is -inf is masked: it takes no part, in the
  * softmax's sum either.  A token with fewer than k experts left has id -1 and
- * weight 0 in its last slots.  A NaN logit of an expert that is not masked makes
- * its token's weights NaN, and that expert is not chosen.
+ * weight 0 in its last slots.  A NaN logit or bias of an expert that is not masked
+ * makes its token's weights NaN; that expert is not chosen, nor a NaN logit in the
+ * softmax's sum, and the others are chosen as without it.  An infinite logit of a
+ * softmax makes its token's weights NaN too; the choice takes its score for 1 (as
+ * many as there are share that 1) and finite logits' scores for 0.
  *   dev_logits, dtype  tokens rows of experts logits, ld elements apart;
  *   dev_bias           NULL, or experts floats;
  *   dev_ids            tokens x k int32;

@@ -102,7 +102,8 @@ __device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float
   const bool live = token < a.tokens;
   const float ninf = -__builtin_inff();
   float s[kPer], key[kPer];
-  bool bad = false;
+  const bool soft = a.score == WC_SCORE_SOFTMAX;
+  bool bad = false;  // the weights are NaN; the choice goes by the other logits
   float top = ninf;
 #pragma unroll
   for (int i = 0; i < kPer; i++) {
@@ -118,18 +119,19 @@ __device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float
     if (x != ninf) bad = bad || x != x || b != b;
     top = fmaxf(top, x);
   }
-  const bool soft = a.score == WC_SCORE_SOFTMAX;
   if (soft) {
     const uint32_t best = top_of<kLanes>(ordered(top));
     top = __uint_as_float(best >> 31 ? best & 0x7FFFFFFFu : ~best);
+    bad = bad || top == -ninf;
   }
   const bool by_logits = soft && !a.bias && (a.groups == 1 || a.group_top == 1);
   float total = 0.0f;
 #pragma unroll
   for (int i = 0; i < kPer; i++) {
     const float x = s[i];
-    const bool off = x == ninf;
-    s[i] = off ? 0.0f : soft ? expf(x - top) : 1.0f / (1.0f + expf(-x));
+    const bool off = !(x > ninf);  // a NaN too: in no sum, and not chosen
+    // an infinite logit's x - top is a NaN, which the least of it and 0 is not
+    s[i] = off ? 0.0f : soft ? expf(fminf(x - top, 0.0f)) : 1.0f / (1.0f + expf(-x));
     total += s[i];
     if (by_logits) key[i] = x;
     else if (!soft) key[i] = off ? ninf : s[i] + key[i];

@@ -293,3 +293,41 @@ def test_more_tokens_than_a_launch_has_threads_for(dev):
         clear = top[:, 0] - top[:, 1] > 1e-6
         assert float(clear.float().mean()) > 0.5
         assert torch.equal(ids[part][clear], best[:, 0][clear])
+
+
+def _limits(x):
+    """Rows with an infinite logit as their limit: it has all of the softmax, equal ones
+    share it, and the others' scores are 0."""
+    out = torch.where(torch.isposinf(x), 0.0, torch.full_like(x, -2000.0))
+    out = torch.where(x.isnan() | torch.isneginf(x), x, out)
+    return torch.where(torch.isposinf(x).any(dim=1, keepdim=True), out, x)
+
+
+@pytest.mark.parametrize("experts", [16, 32, 64, 256, 512])
+@pytest.mark.parametrize("biased,groups,group_top", [(False, 4, 2), (True, 1, 1), (True, 4, 1), (True, 4, 2)])
+@pytest.mark.parametrize("renormalize", [False, True])
+def test_infinity_and_nan_among_scores(dev, experts, groups, group_top, renormalize, biased):
+    """Softmax keys that are scores: a token with an infinite or a NaN logit has NaN weights,
+    and still the experts that its other logits give."""
+    k = 6
+    x = _logits(7, experts, experts, step=1 / 64)
+    x[0, 11] = math.inf
+    x[1, [3, 9]] = math.inf
+    x[2, 5] = math.nan
+    x[3] = math.nan
+    x[4, [1, 6]] = math.inf
+    x[4, [0, 12]] = -math.inf
+    x[4, 13] = math.nan
+    x[5] = math.inf
+    bias = _logits(1, experts, 3, step=1 / 1024)[0] if biased else None
+    how = dict(groups=groups, top_groups=max(1, groups // 2), group_top=group_top, renormalize=renormalize)
+    r = wc.route_torch(x.to(dev), k, "softmax", None if bias is None else bias.to(dev), **how)
+    ids, weights, margins = plain(_limits(x).double(), k, bias=bias, **how)
+    # scores of 0, 1 and 1 / 2^n and the bias are exact, and so are their sums and ties
+    clear = torch.isposinf(x).any(dim=1) | (margins >= MARGIN)
+    assert torch.equal(r.ids.cpu()[clear], ids[clear])
+    assert torch.isnan(r.weights).all(dim=1).tolist() == [True] * 6 + [False]
+    assert bool(clear[6])
+    w = r.weights[6].cpu().double()
+    assert bool(((w - weights[6]).abs() <= (experts + k + 16) * 2.0 ** -24 * weights[6]).all())
+    check_order(r, experts)
