@@ -54,13 +54,11 @@ __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place)
   return min(uint32_t(max(global<const int32_t>(a.order)[place], 0)), a.slots - 1);
 }
 
-// g / (1 + exp(-g)) by the unit's own exponential and reciprocal, each within an ulp: with
-// the rounding of g log2(e) a relative error under 2^-23 (3 + |g|), of a value that goes to 8
-// bits next.  expf and a division took 2773 us, not 2704, at 4096 tokens of 8 experts of 6144 x
-// 16384, and 291, not 273, at 2000 tokens, 6 each, of 64 of 2048 x 1408.
-__device__ __forceinline__ float silu(float g) {
-  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
-}
+// g / (1 + exp(-g)), with an exponential of 1 ulp and a rounded division.  The unit's own
+// exponential, of g log2(e), and reciprocal would be off by 2^-23 (3 + |g|) and save a
+// fortieth: 2612 us for 2677 at 4096 tokens of 8 experts of 6144 x 16384, 2 each, 45.0 for
+// 46.1 at 203 of 7 of 1537 x 2051, 3 each.
+__device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
 
 // 16 columns of an expert's result for up to 16 of its rows: kMats products that
 // share their rows (gate and up, or down alone), k split over the waves.

@@ -299,3 +299,42 @@ def test_empty_slots_anywhere(dev, tokens, ffn):
         ids = torch.where(empty.bool().expand(tokens, k), -1, _ids(g, tokens, E, k))
         r = _routing(ids, torch.rand((tokens, k), generator=g), E)
         _check(_run(dev, x, r, layer), x, r, layer)
+
+
+@pytest.mark.parametrize("tokens,off", [(1, 0), (4, 0), (20, 0), (20, 1)])
+@pytest.mark.parametrize("low", [-80, -24])
+def test_silu_over_its_range(dev, tokens, off, low):
+    """h to fp32's precision, where the exponential is largest and where it is least: slot by
+    slot, few rows to an expert, many, and matrices that start at different bytes.
+
+    Expert e has one value of h, which reaches y's column e alone: gate x = 127/128 times a
+    code and up x = 8128, both exact.  h is an exponential (2 ulp, 2^-22), a sum, a quotient
+    and a product; then its code is 127, and h / 127, the down product, and the slot's weight
+    are a rounding each.  2^-22 + 6 2^-24 = 10 2^-24, and 1 % for products of these.
+    """
+    g = torch.Generator().manual_seed(tokens + low)
+    E, k, hidden, ffn = 64, 32, 64, 8
+    code = torch.cat([torch.tensor([low, 87, -1, 0, 1]), torch.randint(low, 88, (E - 5,), generator=g)])
+    gate, up = torch.zeros((2, E, ffn, hidden), dtype=torch.int8)
+    down = torch.zeros((E, hidden, ffn), dtype=torch.int8)
+    gate[:, 3, 5] = code.to(torch.int8)
+    up[:, 3, 5] = 1
+    down[torch.arange(E), torch.arange(E), 3] = 100
+    one = torch.ones((E, ffn))
+    layer = [(gate, one), (up, one * 8192), (down, torch.ones((E, hidden)))]
+    banks = [t.to(dev) for pair in layer for t in pair]
+    # gate at another byte of a dword than up, as a view of a larger buffer
+    flat = torch.zeros(gate.numel() + 16, dtype=torch.int8, device=dev)
+    flat[off:off + gate.numel()] = banks[0].flatten()
+    banks[0] = flat[off:off + gate.numel()].view(gate.shape)
+    x = torch.zeros((tokens, hidden))
+    x[:, 5] = 127 / 128  # its code 127, its scale 2^-7
+    r = _routing(_ids(g, tokens, E, k), torch.rand((tokens, k), generator=g) + 0.5, E)
+    y = wc.experts_i8_torch(x.to(dev), wc.Routing(*(t.to(dev) for t in r)), *banks).cpu().double()
+    a = code.double() * 127 / 128
+    h = a / (1 + torch.exp(-a)) * (127 / 128 * 8192)
+    assert bool(((h.abs() > 1e-29) | (h == 0)).all())  # none of them counts as a row of zeros
+    ref = torch.zeros((tokens, E), dtype=torch.float64)
+    ref.scatter_(1, r.ids.long(), r.weights.double() * (100 * h)[r.ids.long()])
+    assert bool(((y - ref).abs() <= 1.01 * 10 * 2.0 ** -24 * ref.abs()).all()), \
+        float(((y - ref).abs() / ref.abs().clamp_min(1e-300)).max())
