@@ -714,6 +714,7 @@ def gemv_w4_torch(blob: Blob, dev_blob, tensors, scales, zeros, xs, ys=None, str
 _NO_CONTEXT = contextlib.nullcontext()
 SCORES = {"softmax": 0, "sigmoid": 1}
 _floats, _ints = {}, ()
+_FP32 = 8  # WC_FP32
 
 
 def _types():
@@ -722,7 +723,7 @@ def _types():
     if not _floats:
         import torch
         _ints = (torch.int8, torch.uint8)
-        _floats = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 8}
+        _floats = {torch.bfloat16: 1, torch.float16: 2, torch.float32: _FP32}
     return _floats
 
 
@@ -733,11 +734,14 @@ def _float_type(t, what: str) -> int:
     return code
 
 
-def _rows(t, what: str, cols: int = -1) -> int:
-    """Row stride, in elements, of a 2-D device tensor whose rows are contiguous."""
+# The first tensor of a call says on which device it runs (get_device: -1 for host memory);
+# every other one has to be there.
+
+def _rows(t, what: str, dev: int, cols: int = -1) -> int:
+    """Row stride, in elements, of a 2-D tensor on device `dev` whose rows are contiguous."""
     shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{what} must be a 2-D device tensor")
+    if len(shape) != 2 or dev < 0 or t.get_device() != dev:
+        raise ValueError(f"{what} must be a 2-D tensor on {'a device' if dev < 0 else f'device {dev}'}")
     if cols >= 0 and shape[1] != cols:
         raise ValueError(f"{what} has {shape[1]} columns, not {cols}")
     if stride[1] != 1 and shape[1] > 1:
@@ -745,9 +749,9 @@ def _rows(t, what: str, cols: int = -1) -> int:
     return stride[0] if shape[0] > 1 else shape[1]
 
 
-def _vector(t, n: int, what: str) -> int:
-    if t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what} must be a contiguous device tensor of {n} elements")
+def _vector(t, n: int, what: str, dev: int) -> int:
+    if t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what} must be {n} contiguous elements on device {dev}")
     return _float_type(t, what)
 
 
@@ -764,6 +768,8 @@ def _stream_of(stream, device):
     import torch
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(device.index), _NO_CONTEXT
+    if stream.device_index != device.index:
+        raise ValueError(f"the stream must be one of device {device.index}")
     return stream.cuda_stream, torch.cuda.stream(stream)
 
 
@@ -771,8 +777,9 @@ def _workspace(workspace, need: int, device):
     import torch
     if workspace is None:
         return torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    if workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
-        raise ValueError(f"the workspace needs {need} contiguous bytes")
+    if workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous() or \
+            workspace.get_device() != device.index:
+        raise ValueError(f"the workspace needs {need} contiguous bytes on device {device.index}")
     return workspace
 
 
@@ -793,7 +800,8 @@ def quantize_i8_torch(x, q=None, scale=None, stream=None):
     """wc_quantize_i8 of a 2-D tensor: (q, scale), q int8 of m x i8_row_bytes(k) (zero
     past column k) and scale float32 of m; the row's values are q * scale."""
     import torch
-    ld = _rows(x, "x")
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
     dt = _float_type(x, "x")
     m, k = x.shape
     st, where = _stream_of(stream, x.device)
@@ -802,10 +810,11 @@ def quantize_i8_torch(x, q=None, scale=None, stream=None):
             q = torch.empty((m, i8_row_bytes(k)), dtype=torch.int8, device=x.device)
         if scale is None:
             scale = torch.empty(m, dtype=torch.float32, device=x.device)
-    if tuple(q.shape) != (m, i8_row_bytes(k)) or q.dtype != torch.int8 or not q.is_contiguous():
-        raise ValueError(f"q must be a contiguous int8 tensor of {m} x {i8_row_bytes(k)}")
-    if scale.dtype != torch.float32 or scale.numel() != m or not scale.is_contiguous():
-        raise ValueError(f"scale must be {m} contiguous float32")
+    if tuple(q.shape) != (m, i8_row_bytes(k)) or q.dtype != torch.int8 or not q.is_contiguous() or \
+            q.get_device() != dev:
+        raise ValueError(f"q must be a contiguous int8 tensor of {m} x {i8_row_bytes(k)} on device {dev}")
+    if _vector(scale, m, "scale", dev) != _FP32:
+        raise ValueError("scale must be float32")
     rc = lib().wc_quantize_i8(x.data_ptr(), dt, m, k, ld, q.data_ptr(), scale.data_ptr(),
                               st)
     if rc:
@@ -816,7 +825,7 @@ def quantize_i8_torch(x, q=None, scale=None, stream=None):
 _JOB = struct.Struct("=6QI3i")  # wc_i8_job
 
 
-def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, device):
+def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, dev: int):
     """The wc_i8_job array, packed, and the ys (allocated where None)."""
     n_jobs = len(ws)
     if len(scales) != n_jobs or (biases is not None and len(biases) != n_jobs) or \
@@ -829,22 +838,22 @@ def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, device):
         w, s = ws[i], scales[i]
         # (each look at a tensor costs the host as much as a microsecond's tenth)
         shape, stride = w.shape, w.stride()
-        if len(shape) != 2 or shape[1] != k or not w.is_cuda or (stride[1] != 1 and k > 1):
-            _rows(w, "w", k)
+        if len(shape) != 2 or shape[1] != k or w.get_device() != dev or (stride[1] != 1 and k > 1):
+            _rows(w, "w", dev, k)
         if w.dtype not in _ints:
             raise ValueError("w must be int8 codes")
         n = shape[0]
         ldw = stride[0] if n > 1 else k
-        st = _vector(s, n, "a matrix's scale")
+        st = _vector(s, n, "a matrix's scale", dev)
         b = None if biases is None else biases[i]
-        bp, bt = (0, 0) if b is None else (b.data_ptr(), _vector(b, n, "a bias"))
+        bp, bt = (0, 0) if b is None else (b.data_ptr(), _vector(b, n, "a bias", dev))
         if ys is None:
             y, ldy = w.new_empty((m, n), dtype=dtype), n
         else:
             y = ys[i]
             if y.shape != (m, n):
                 raise ValueError(f"y must be {m} x {n}")
-            ldy = _rows(y, "y")
+            ldy = _rows(y, "y", dev)
             yt = floats.get(y.dtype)
         if yt is None:
             raise ValueError("y must be bfloat16, float16 or float32")
@@ -859,16 +868,16 @@ def matmul_i8_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=No
     k) of `ws`, with q and scale from quantize_i8_torch.  ys (of any float type, rows
     contiguous) are allocated in `dtype` (bfloat16 if None) where None."""
     import torch
-    m = q.shape[0]
-    if q.dtype != torch.int8 or not q.is_contiguous() or tuple(q.shape) != (m, i8_row_bytes(k)):
-        raise ValueError(f"q must be a contiguous int8 tensor of {i8_row_bytes(k)} columns")
-    if scale.dtype != torch.float32:
+    dev, m = q.get_device(), q.shape[0]
+    if dev < 0 or q.dtype != torch.int8 or not q.is_contiguous() or \
+            tuple(q.shape) != (m, i8_row_bytes(k)):
+        raise ValueError(f"q must be a contiguous int8 device tensor of {i8_row_bytes(k)} columns")
+    if _vector(scale, m, "scale", dev) != _FP32:
         raise ValueError("scale must be float32")
-    _vector(scale, m, "scale")
     st, where = _stream_of(stream, q.device)
     need = C.c_uint64(0)
     with where:
-        jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or torch.bfloat16, q.device)
+        jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or torch.bfloat16, dev)
         rc = lib().wc_matmul_i8_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
         if not rc:
             workspace = _workspace(workspace, need.value, q.device)
@@ -884,13 +893,14 @@ def linear_i8_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
                     stream=None):
     """wc_linear_i8: x quantised per row, then as matmul_i8_torch; `dtype` defaults to
     x's type."""
-    ld = _rows(x, "x")
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
     dt = _float_type(x, "x")
     m, k = x.shape
     st, where = _stream_of(stream, x.device)
     need = C.c_uint64(0)
     with where:
-        jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, x.device)
+        jobs, ys = _i8_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, dev)
         # one or two rows mostly need no workspace, and the call refuses those that do
         if m <= 2 and workspace is None and \
                 not lib().wc_linear_i8(x.data_ptr(), dt, m, k, ld, len(ws), jobs, None, 0, st):
@@ -917,12 +927,13 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
     """wc_route of a router's logits (tokens x experts); `bias` float32 of experts;
     `out` a Routing to write into."""
     import torch
-    ld = _rows(logits, "logits")
+    on = logits.get_device()
+    ld = _rows(logits, "logits", on)
     dt = _float_type(logits, "logits")
     tokens, experts = logits.shape
     if score not in SCORES:
         raise ValueError(f"score must be one of {sorted(SCORES)}")
-    if bias is not None and _vector(bias, experts, "bias") != 8:
+    if bias is not None and _vector(bias, experts, "bias", on) != _FP32:
         raise ValueError("bias must be float32")
     dev = logits.device
     st, where = _stream_of(stream, dev)
@@ -940,7 +951,7 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
             out = Routing(new((tokens, k), dtype=torch.int32), new((tokens, k), dtype=torch.float32),
                           new(experts + 1, dtype=torch.int32), new(tokens * k, dtype=torch.int32))
         else:
-            _check_routing(out, tokens, k, experts)
+            _check_routing(out, tokens, k, experts, on)
         workspace = _workspace(workspace, need.value, dev)
     rc = lib().wc_route(logits.data_ptr(), dt, tokens, ld, C.byref(params), _ptr(bias),
                         *(t.data_ptr() for t in out), _ptr(workspace), _size(workspace),
@@ -950,26 +961,27 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
     return out
 
 
-def _check_routing(r, tokens: int, k: int, experts: int):
+def _check_routing(r, tokens: int, k: int, experts: int, dev: int):
     import torch
     for t, shape, dtype, name in ((r.ids, (tokens, k), torch.int32, "ids"),
                                   (r.weights, (tokens, k), torch.float32, "weights"),
                                   (r.offsets, (experts + 1,), torch.int32, "offsets"),
                                   (r.order, (tokens * k,), torch.int32, "order")):
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {shape}")
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of {shape} on device {dev}")
 
 
-def _bank(w, scale, experts: int, n: int, k: int, what: str):
+def _bank(w, scale, experts: int, n: int, k: int, what: str, dev: int):
     _codes(w, what)
     stride = w.stride()
-    if w.shape != (experts, n, k) or not w.is_cuda or (k > 1 and stride[2] != 1) or \
+    if w.shape != (experts, n, k) or w.get_device() != dev or (k > 1 and stride[2] != 1) or \
             (n > 1 and stride[1] != k):
-        raise ValueError(f"{what} must be {experts} x {n} x {k} codes, contiguous in each expert")
+        raise ValueError(f"{what} must be {experts} x {n} x {k} codes on device {dev}, contiguous in each "
+                         "expert")
     if scale.shape != (experts, n):
         raise ValueError(f"the scales of {what} must be {experts} x {n}")
     return _I8Experts(w.data_ptr(), scale.data_ptr(), stride[0] if experts > 1 else n * k,
-                      _vector(scale, experts * n, f"the scales of {what}"), 0)
+                      _vector(scale, experts * n, f"the scales of {what}", dev), 0)
 
 
 def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, down_scale,
@@ -978,17 +990,18 @@ def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
     int8 of experts x ffn x hidden, down of experts x hidden x ffn, with scales of
     experts x rows; y of x's type."""
     import torch
-    ld = _rows(x, "x")
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
     dt = _float_type(x, "x")
     tokens, hidden = x.shape
     if gate.dim() != 3 or routing.ids.dim() != 2:
         raise ValueError("gate must be experts x ffn x hidden, the ids tokens x k")
     experts, ffn = gate.shape[:2]
     k = routing.ids.shape[1]
-    _check_routing(routing, tokens, k, experts)
-    banks = (_bank(gate, gate_scale, experts, ffn, hidden, "gate"),
-             _bank(up, up_scale, experts, ffn, hidden, "up"),
-             _bank(down, down_scale, experts, hidden, ffn, "down"))
+    _check_routing(routing, tokens, k, experts, dev)
+    banks = (_bank(gate, gate_scale, experts, ffn, hidden, "gate", dev),
+             _bank(up, up_scale, experts, ffn, hidden, "up", dev),
+             _bank(down, down_scale, experts, hidden, ffn, "down", dev))
     st, where = _stream_of(stream, x.device)
     need = C.c_uint64(0)
     rc = lib().wc_experts_i8_workspace_bytes(tokens, k, experts, hidden, ffn, C.byref(need))
@@ -1000,9 +1013,10 @@ def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
         workspace = _workspace(workspace, need.value, x.device)
     if tuple(y.shape) != (tokens, hidden) or y.dtype != x.dtype:
         raise ValueError(f"y must be {tokens} x {hidden} of x's type")
+    ldy = _rows(y, "y", dev)
     rc = lib().wc_experts_i8(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
                              *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
-                             y.data_ptr(), _rows(y, "y"), _ptr(workspace), _size(workspace),
+                             y.data_ptr(), ldy, _ptr(workspace), _size(workspace),
                              st)
     if rc:
         raise WcError("wc_experts_i8", rc)

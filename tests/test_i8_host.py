@@ -1,6 +1,7 @@
 """CPU: what the 8-bit layers' entry points refuse before anything is launched, and
 the workspace they ask for.  Pointers are made up and never followed."""
 import ctypes as C
+import math
 
 import pytest
 
@@ -126,3 +127,126 @@ def test_experts_refusals():
     args[2] = 0
     args[0] = args[15] = args[17] = None
     assert L.wc_experts_i8(*args) == 0  # no tokens
+
+
+class _OnDevice:
+    """What a tensor on a device looks like to the checks of wc.py; nothing follows its
+    address."""
+
+    def __init__(self, shape, dtype, index=0):
+        torch = pytest.importorskip("torch")
+        self.shape, self.dtype, self.index = tuple(shape), dtype, index
+        self.is_cuda, self.device = True, torch.device("cuda", index)
+        self._size = torch.empty((), dtype=dtype).element_size()
+
+    def get_device(self):
+        return self.index
+
+    def stride(self):
+        return tuple(math.prod(self.shape[i + 1:]) for i in range(len(self.shape)))
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self._size
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return A
+
+    def new_empty(self, shape, dtype=None):
+        return _OnDevice(shape if isinstance(shape, tuple) else (shape,), dtype or self.dtype, self.index)
+
+
+class _Stream:
+    cuda_stream = 0
+    device_index = 0
+
+
+class _NoLibrary:
+    """Sizes and status of a library that must not launch anything."""
+
+    def __getattr__(self, name):
+        assert name.endswith("_workspace_bytes"), f"{name} was called"
+
+        def workspace_bytes(*args):
+            args[-1]._obj.value = 4096
+            return 0
+        return workspace_bytes
+
+
+def _calls(torch, at, put):
+    """Each torch entry point with everything on device 0, but argument `at`."""
+    i8, i32, f32, bf = torch.int8, torch.int32, torch.float32, torch.bfloat16
+
+    def t(name, shape, dtype):
+        return put(shape, dtype) if name == at else _OnDevice(shape, dtype)
+
+    def ws():
+        return t("workspace", (1 << 16,), torch.uint8)
+    st = _Stream()
+    m, k, n, E, F = 40, 64, 16, 8, 32
+    x, w = (lambda: t("x", (m, k), bf)), (lambda: t("w", (n, k), i8))
+    s, b = (lambda: t("w_scale", (n,), f32)), (lambda: t("bias", (n,), f32))
+    y, q, qs = (lambda: t("y", (m, n), bf)), (lambda: t("q", (m, 128), i8)), (lambda: t("q_scale", (m,), f32))
+
+    def routing():
+        return wc.Routing(t("ids", (m, 2), i32), t("weights", (m, 2), f32), t("offsets", (E + 1,), i32),
+                          t("order", (2 * m,), i32))
+    bank = (lambda: [t("gate", (E, F, k), i8), t("gate_scale", (E, F), f32), t("up", (E, F, k), i8),
+                     t("up_scale", (E, F), f32), t("down", (E, k, F), i8), t("down_scale", (E, k), f32)])
+    return {
+        "quantize": lambda: wc.quantize_i8_torch(x(), q=q(), scale=qs(), stream=st),
+        "matmul": lambda: wc.matmul_i8_torch(q(), qs(), k, [w()], [s()], [b()], ys=[y()], workspace=ws(),
+                                             stream=st),
+        "linear": lambda: wc.linear_i8_torch(x(), [w()], [s()], [b()], ys=[y()], workspace=ws(), stream=st),
+        "route": lambda: wc.route_torch(t("logits", (m, E), f32), 2, "sigmoid", t("route_bias", (E,), f32),
+                                        out=routing(), workspace=ws(), stream=st),
+        "experts": lambda: wc.experts_i8_torch(x(), routing(), *bank(), y=t("out", (m, k), bf),
+                                               workspace=ws(), stream=st),
+    }
+
+
+_ARGUMENTS = {"quantize": ["x", "q", "q_scale"],
+              "matmul": ["q", "q_scale", "w", "w_scale", "bias", "y", "workspace"],
+              "linear": ["x", "w", "w_scale", "bias", "y", "workspace"],
+              "route": ["logits", "route_bias", "ids", "weights", "offsets", "order", "workspace"],
+              "experts": ["x", "ids", "weights", "offsets", "order", "gate", "gate_scale", "up", "up_scale",
+                          "down", "down_scale", "out", "workspace"]}
+
+
+@pytest.mark.parametrize("call,argument", [(c, a) for c, names in _ARGUMENTS.items() for a in names])
+@pytest.mark.parametrize("where", ["host", "device 1"])
+def test_every_tensor_on_one_device(monkeypatch, call, argument, where):
+    """A tensor in host memory, or on another device than the others, is refused before
+    the library has its address."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(wc, "lib", lambda: _NoLibrary())
+
+    def put(shape, dtype):
+        return torch.zeros(shape, dtype=dtype) if where == "host" else _OnDevice(shape, dtype, 1)
+    with pytest.raises(ValueError):
+        _calls(torch, argument, put)[call]()
+
+
+@pytest.mark.parametrize("call", list(_ARGUMENTS))
+def test_tensors_on_one_device_pass_the_checks(monkeypatch, call):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(wc, "lib", lambda: _NoLibrary())
+    with pytest.raises(AssertionError, match="was called"):
+        _calls(torch, None, None)[call]()
+
+
+def test_a_stream_of_another_device(monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(wc, "lib", lambda: _NoLibrary())
+    monkeypatch.setattr(_Stream, "device_index", 1)
+    for call in _calls(torch, None, None).values():
+        with pytest.raises(ValueError):
+            call()
