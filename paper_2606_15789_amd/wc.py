@@ -763,11 +763,14 @@ def _codes(t, what: str):
 
 
 def _stream_of(stream, device):
-    """The stream handle to launch on, and the context in which to allocate what the
-    launch uses, so that the allocator knows the stream that uses it."""
+    """The stream handle to launch on, and the context in which to launch, so that the
+    device is the current one, and to allocate what the launch uses, so that the allocator
+    knows the stream that uses it."""
     import torch
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index), _NO_CONTEXT
+        index = device.index
+        return torch._C._cuda_getCurrentRawStream(index), \
+            _NO_CONTEXT if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
     if stream.device_index != device.index:
         raise ValueError(f"the stream must be one of device {device.index}")
     return stream.cuda_stream, torch.cuda.stream(stream)
@@ -810,13 +813,12 @@ def quantize_i8_torch(x, q=None, scale=None, stream=None):
             q = torch.empty((m, i8_row_bytes(k)), dtype=torch.int8, device=x.device)
         if scale is None:
             scale = torch.empty(m, dtype=torch.float32, device=x.device)
-    if tuple(q.shape) != (m, i8_row_bytes(k)) or q.dtype != torch.int8 or not q.is_contiguous() or \
-            q.get_device() != dev:
-        raise ValueError(f"q must be a contiguous int8 tensor of {m} x {i8_row_bytes(k)} on device {dev}")
-    if _vector(scale, m, "scale", dev) != _FP32:
-        raise ValueError("scale must be float32")
-    rc = lib().wc_quantize_i8(x.data_ptr(), dt, m, k, ld, q.data_ptr(), scale.data_ptr(),
-                              st)
+        if tuple(q.shape) != (m, i8_row_bytes(k)) or q.dtype != torch.int8 or \
+                not q.is_contiguous() or q.get_device() != dev:
+            raise ValueError(f"q must be a contiguous int8 tensor of {m} x {i8_row_bytes(k)} on device {dev}")
+        if _vector(scale, m, "scale", dev) != _FP32:
+            raise ValueError("scale must be float32")
+        rc = lib().wc_quantize_i8(x.data_ptr(), dt, m, k, ld, q.data_ptr(), scale.data_ptr(), st)
     if rc:
         raise WcError("wc_quantize_i8", rc)
     return q, scale
@@ -881,9 +883,8 @@ def matmul_i8_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=No
         rc = lib().wc_matmul_i8_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
         if not rc:
             workspace = _workspace(workspace, need.value, q.device)
-    if not rc:
-        rc = lib().wc_matmul_i8(q.data_ptr(), scale.data_ptr(), m, k, len(ws), jobs,
-                                _ptr(workspace), _size(workspace), st)
+            rc = lib().wc_matmul_i8(q.data_ptr(), scale.data_ptr(), m, k, len(ws), jobs,
+                                    _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_matmul_i8", rc)
     return ys
@@ -908,9 +909,8 @@ def linear_i8_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
         rc = lib().wc_linear_i8_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
         if not rc:
             workspace = _workspace(workspace, need.value, x.device)
-    if not rc:
-        rc = lib().wc_linear_i8(x.data_ptr(), dt, m, k, ld, len(ws), jobs, _ptr(workspace),
-                                _size(workspace), st)
+            rc = lib().wc_linear_i8(x.data_ptr(), dt, m, k, ld, len(ws), jobs, _ptr(workspace),
+                                    _size(workspace), st)
     if rc:
         raise WcError("wc_linear_i8", rc)
     return ys
@@ -953,9 +953,8 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
         else:
             _check_routing(out, tokens, k, experts, on)
         workspace = _workspace(workspace, need.value, dev)
-    rc = lib().wc_route(logits.data_ptr(), dt, tokens, ld, C.byref(params), _ptr(bias),
-                        *(t.data_ptr() for t in out), _ptr(workspace), _size(workspace),
-                        st)
+        rc = lib().wc_route(logits.data_ptr(), dt, tokens, ld, C.byref(params), _ptr(bias),
+                            *(t.data_ptr() for t in out), _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_route", rc)
     return out
@@ -1011,13 +1010,12 @@ def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
         if y is None:
             y = x.new_empty((tokens, hidden))
         workspace = _workspace(workspace, need.value, x.device)
-    if tuple(y.shape) != (tokens, hidden) or y.dtype != x.dtype:
-        raise ValueError(f"y must be {tokens} x {hidden} of x's type")
-    ldy = _rows(y, "y", dev)
-    rc = lib().wc_experts_i8(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
-                             *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
-                             y.data_ptr(), ldy, _ptr(workspace), _size(workspace),
-                             st)
+        if tuple(y.shape) != (tokens, hidden) or y.dtype != x.dtype:
+            raise ValueError(f"y must be {tokens} x {hidden} of x's type")
+        ldy = _rows(y, "y", dev)
+        rc = lib().wc_experts_i8(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
+                                 *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
+                                 y.data_ptr(), ldy, _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_experts_i8", rc)
     return y

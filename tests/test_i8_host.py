@@ -181,12 +181,12 @@ class _NoLibrary:
         return workspace_bytes
 
 
-def _calls(torch, at, put):
-    """Each torch entry point with everything on device 0, but argument `at`."""
+def _calls(torch, at, put, index=0):
+    """Each torch entry point with everything on device `index`, but argument `at`."""
     i8, i32, f32, bf = torch.int8, torch.int32, torch.float32, torch.bfloat16
 
     def t(name, shape, dtype):
-        return put(shape, dtype) if name == at else _OnDevice(shape, dtype)
+        return put(shape, dtype) if name == at else _OnDevice(shape, dtype, index)
 
     def ws():
         return t("workspace", (1 << 16,), torch.uint8)
@@ -250,3 +250,38 @@ def test_a_stream_of_another_device(monkeypatch):
     for call in _calls(torch, None, None).values():
         with pytest.raises(ValueError):
             call()
+
+
+def test_launches_with_the_tensors_device_current(monkeypatch):
+    """The current stream of a device that is not the current one: the library is called
+    while that device is."""
+    torch = pytest.importorskip("torch")
+    current, seen = [0], []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            current.append(self.index)
+
+        def __exit__(self, *_):
+            current.pop()
+
+    class Library(_NoLibrary):
+        def __getattr__(self, name):
+            if name.endswith("_workspace_bytes"):
+                return _NoLibrary.__getattr__(self, name)
+            return lambda *args: seen.append((name, current[-1])) or 0
+    monkeypatch.setattr(wc, "lib", lambda: Library())
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[-1], raising=False)
+    monkeypatch.setattr(_Stream, "__new__", lambda cls: None)  # the current stream
+
+    def on(index):
+        seen.clear()
+        for call in _calls(torch, None, None, index).values():
+            call()
+        return [device for _, device in seen]
+    assert on(0) == [0] * len(_ARGUMENTS) and on(1) == [1] * len(_ARGUMENTS)
