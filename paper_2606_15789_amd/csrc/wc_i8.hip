@@ -612,13 +612,14 @@ constexpr double kStridedPerUs = 2.7e5;
 
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_i8_job* jobs) {
   Plan p{Kernel::kRows, false, false, 1, false, 0};
+  // offsets within a tile are 32-bit; the kernel for more reads W at any byte, without copies
+  for (uint32_t i = 0; i < n_jobs; i++)
+    if (jobs[i].ldw > (1u << 20)) return p;
   uint64_t sums = 0, strided = 0, weights = 0;
   bool narrow = true;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_i8_job& J = jobs[i];
     weights += uint64_t(J.n) * k;
-    // offsets within a tile are 32-bit
-    if (J.ldw > (1u << 20)) return p;
     narrow = narrow && J.n < (1u << 20) && J.ldy < (1u << 20);
     p.copies = p.copies || J.ldw % 4 || reinterpret_cast<uintptr_t>(J.w) % 4;
     sums += uint64_t(m) * row_pitch(J.n, steps_of(J.ldw)) * 4;

@@ -285,3 +285,19 @@ def test_launches_with_the_tensors_device_current(monkeypatch):
             call()
         return [device for _, device in seen]
     assert on(0) == [0] * len(_ARGUMENTS) and on(1) == [1] * len(_ARGUMENTS)
+
+
+@pytest.mark.parametrize("m", [1, 16, 40, 700])
+def test_workspace_does_not_depend_on_the_jobs_order(m):
+    """A matrix past the tiles' offsets takes the kernel that needs no shifted copies of x,
+    and no workspace, whichever matrix is named first."""
+    L = wc.lib()
+    odd, far = _job(ldw=65, w=A + 1), _job(ldw=(1 << 20) + 4)
+    sizes = []
+    for jobs in ((odd, far), (far, odd), (odd, odd, far), (far, far)):
+        need = C.c_uint64(7)
+        assert L.wc_matmul_i8_workspace_bytes(m, 64, len(jobs), _jobs(*jobs), C.byref(need)) == 0
+        assert need.value == 0, jobs
+        assert L.wc_linear_i8_workspace_bytes(m, 64, len(jobs), _jobs(*jobs), C.byref(need)) == 0
+        sizes.append(need.value)
+    assert len(set(sizes)) == 1, sizes
