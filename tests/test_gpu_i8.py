@@ -335,3 +335,61 @@ def test_results_at_any_element(dev, dtype, m, n, off):
     _check(y, *_quantised(x), w, ws, b)
     y.fill_(7.0)
     assert bool((wide == 7.0).all())
+
+
+# Matrices past the tiles' 32-bit offsets: rows more than 2^20 bytes apart, 2^20 rows or
+# more, results 2^20 elements or more apart.
+
+@pytest.mark.parametrize("m", [1, 16, 17, 64, 200])
+@pytest.mark.parametrize("k,off", [(1, 0), (31, 3), (128, 0), (700, 1), (65536, 2)])
+def test_rows_far_apart(dev, m, k, off):
+    g = _gen(m + k)
+    n, far = 53, (1 << 20) + 5
+    wide = torch.randint(-128, 128, (n, far), dtype=torch.int8, device=dev)
+    far_w, near_w = wide[:, off:off + k], _codes(g, 21, k).to(dev)
+    ws = [torch.rand(n, generator=g) * 0.01, (torch.rand(21, generator=g) * 0.01).half()]
+    bias = torch.randn(n, generator=g).bfloat16()
+    x = torch.randn((m, k), generator=g).half()
+    q, s = _quantised(x)
+    yw = torch.full((m + 2, n + 3), 7.0, device=dev)
+    near_y = torch.zeros((m, 21), dtype=torch.bfloat16, device=dev)
+    wc.linear_i8_torch(x.to(dev), [far_w, near_w], [v.to(dev) for v in ws], [bias.to(dev), None],
+                       ys=[yw[1:-1, 1:1 + n], near_y])
+    _check(yw[1:-1, 1:1 + n], q, s, far_w.cpu(), ws[0], bias)
+    _check(near_y, q, s, near_w.cpu(), ws[1], None)
+    y, again = wc.matmul_i8_torch(*wc.quantize_i8_torch(x.to(dev)), k, [near_w, far_w],
+                                  [ws[1].to(dev), ws[0].to(dev)], [None, bias.to(dev)], dtype=torch.float32)
+    assert torch.equal(again, yw[1:-1, 1:1 + n])
+    _check(y, q, s, near_w.cpu(), ws[1], None)
+    yw[1:-1, 1:1 + n] = 7.0
+    assert bool((yw == 7.0).all())
+
+
+def test_many_columns(dev):
+    """2^20 + 3 rows of W; and results that far apart."""
+    g = _gen(20)
+    n, m, k = (1 << 20) + 3, 20, 24
+    w, ws = _codes(g, n, k), torch.rand(n, generator=g) * 0.01
+    x = torch.randn((m, k), generator=g)
+    y, = wc.linear_i8_torch(x.to(dev), [w.to(dev)], [ws.to(dev)])
+    _check(y, *_quantised(x), w, ws, None)
+    m = 70
+    x = torch.randn((m, k), generator=g)
+    wide = torch.full((m, n), 7.0, device=dev)
+    wc.linear_i8_torch(x.to(dev), [w[:50].to(dev)], [ws[:50].to(dev)], ys=[wide[:, 9:59]])
+    _check(wide[:, 9:59], *_quantised(x), w[:50], ws[:50], None)
+    wide[:, 9:59] = 7.0
+    assert bool((wide == 7.0).all())
+
+
+def test_rows_far_apart_and_many_of_x(dev):
+    """More rows of x than a grid's second axis has blocks for, the last ones a few."""
+    m, k, n = 65535 * 64 + 9, 3, 2
+    g = torch.Generator(device=dev).manual_seed(6)
+    x = torch.randn((m, k), generator=g, device=dev).half()
+    w = torch.randint(-128, 128, (n, (1 << 20) + 1), dtype=torch.int8, device=dev)[:, :k]
+    ws = torch.rand(n, generator=_gen(2)).to(dev)
+    y, = wc.linear_i8_torch(x, [w], [ws], dtype=torch.float32)
+    q, scale = wc.quantize_i8_torch(x)
+    p = (q[:, :k].double() @ w.double().T) * scale.double()[:, None] * ws.double()
+    assert bool(((y.double() - p).abs() <= 1.01 * 5 * 2.0 ** -24 * p.abs() + LEAST[y.dtype]).all())

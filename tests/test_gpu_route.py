@@ -331,3 +331,17 @@ def test_infinity_and_nan_among_scores(dev, experts, groups, group_top, renormal
     w = r.weights[6].cpu().double()
     assert bool(((w - weights[6]).abs() <= (experts + k + 16) * 2.0 ** -24 * weights[6]).all())
     check_order(r, experts)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("tokens,experts,k", [(6, 257, 10), (8, 511, 9), (11, 512, 32), (600, 512, 8)])
+def test_many_experts_in_bf16(dev, score, tokens, experts, k):
+    """512 numbers of bf16 that differ: 128 of either sign to each of two powers of two, up
+    to 4, where sigmoids of neighbours are 2^-13 apart."""
+    v = (1 + torch.arange(128) / 128.0)[None] * torch.tensor([[1.0], [2.0]])
+    v = torch.cat([v.flatten(), -v.flatten()])
+    g = torch.Generator().manual_seed(tokens)
+    x = v[torch.argsort(torch.rand((tokens, 512), generator=g), dim=1)][:, :experts].bfloat16()
+    assert torch.equal(x.float().sort(dim=1)[0].diff(dim=1) > 0, torch.ones((tokens, experts - 1), dtype=torch.bool))
+    r = wc.route_torch(x.to(dev), k, score)
+    _check(r, x, k, score=score)
