@@ -715,6 +715,7 @@ _NO_CONTEXT = contextlib.nullcontext()
 SCORES = {"softmax": 0, "sigmoid": 1}
 _floats, _ints = {}, ()
 _FP32 = 8  # WC_FP32
+_EINVAL = -1  # WC_EINVAL: here for sizes that ctypes would cut to 32 bits
 
 
 def _types():
@@ -807,6 +808,8 @@ def quantize_i8_torch(x, q=None, scale=None, stream=None):
     ld = _rows(x, "x", dev)
     dt = _float_type(x, "x")
     m, k = x.shape
+    if (m | k) >> 32:
+        raise WcError("wc_quantize_i8", _EINVAL)
     st, where = _stream_of(stream, x.device)
     with where:
         if q is None:
@@ -860,6 +863,8 @@ def _i8_jobs(m: int, k: int, ws, scales, biases, ys, dtype, dev: int):
         if yt is None:
             raise ValueError("y must be bfloat16, float16 or float32")
         out.append(y)
+        if n >> 32:
+            raise WcError("wc_matmul_i8", _EINVAL)
         jobs.append(_JOB.pack(w.data_ptr(), s.data_ptr(), bp, y.data_ptr(), ldw, ldy, n, st, bt, yt))
     return b"".join(jobs), out
 
@@ -876,6 +881,8 @@ def matmul_i8_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=No
         raise ValueError(f"q must be a contiguous int8 device tensor of {i8_row_bytes(k)} columns")
     if _vector(scale, m, "scale", dev) != _FP32:
         raise ValueError("scale must be float32")
+    if (m | k) >> 32:
+        raise WcError("wc_matmul_i8", _EINVAL)
     st, where = _stream_of(stream, q.device)
     need = C.c_uint64(0)
     with where:
@@ -898,6 +905,8 @@ def linear_i8_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
     ld = _rows(x, "x", dev)
     dt = _float_type(x, "x")
     m, k = x.shape
+    if (m | k) >> 32:
+        raise WcError("wc_linear_i8", _EINVAL)
     st, where = _stream_of(stream, x.device)
     need = C.c_uint64(0)
     with where:
@@ -935,6 +944,8 @@ def route_torch(logits, k: int, score: str = "softmax", bias=None, groups: int =
         raise ValueError(f"score must be one of {sorted(SCORES)}")
     if bias is not None and _vector(bias, experts, "bias", on) != _FP32:
         raise ValueError("bias must be float32")
+    if (tokens | experts | k | groups | top_groups | group_top) >> 32:
+        raise WcError("wc_route", _EINVAL)
     dev = logits.device
     st, where = _stream_of(stream, dev)
     params = _RouteParams(experts, k, SCORES[score], int(renormalize), groups, top_groups,
@@ -997,6 +1008,8 @@ def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
         raise ValueError("gate must be experts x ffn x hidden, the ids tokens x k")
     experts, ffn = gate.shape[:2]
     k = routing.ids.shape[1]
+    if (tokens | k | experts | hidden | ffn) >> 32:
+        raise WcError("wc_experts_i8", _EINVAL)
     _check_routing(routing, tokens, k, experts, dev)
     banks = (_bank(gate, gate_scale, experts, ffn, hidden, "gate", dev),
              _bank(up, up_scale, experts, ffn, hidden, "up", dev),

@@ -181,7 +181,7 @@ class _NoLibrary:
         return workspace_bytes
 
 
-def _calls(torch, at, put, index=0):
+def _calls(torch, at, put, index=0, m=40, k=64, n=16, F=32):
     """Each torch entry point with everything on device `index`, but argument `at`."""
     i8, i32, f32, bf = torch.int8, torch.int32, torch.float32, torch.bfloat16
 
@@ -191,7 +191,7 @@ def _calls(torch, at, put, index=0):
     def ws():
         return t("workspace", (1 << 16,), torch.uint8)
     st = _Stream()
-    m, k, n, E, F = 40, 64, 16, 8, 32
+    E = 8
     x, w = (lambda: t("x", (m, k), bf)), (lambda: t("w", (n, k), i8))
     s, b = (lambda: t("w_scale", (n,), f32)), (lambda: t("bias", (n,), f32))
     y, q, qs = (lambda: t("y", (m, n), bf)), (lambda: t("q", (m, 128), i8)), (lambda: t("q_scale", (m,), f32))
@@ -301,3 +301,32 @@ def test_workspace_does_not_depend_on_the_jobs_order(m):
         assert L.wc_linear_i8_workspace_bytes(m, 64, len(jobs), _jobs(*jobs), C.byref(need)) == 0
         sizes.append(need.value)
     assert len(set(sizes)) == 1, sizes
+
+
+BIG = 1 << 32
+
+
+@pytest.mark.parametrize("call,sizes", [
+    ("quantize", dict(m=BIG + 3)), ("matmul", dict(m=BIG + 3)), ("linear", dict(m=BIG + 1)),
+    ("linear", dict(m=BIG + 40, k=8)), ("linear", dict(k=BIG + 64)), ("linear", dict(n=BIG + 16)),
+    ("route", dict(m=BIG + 3)), ("experts", dict(m=BIG + 3)), ("experts", dict(k=BIG + 64)),
+    ("experts", dict(F=BIG + 32))])
+def test_sizes_past_32_bits(monkeypatch, call, sizes):
+    """Sizes that 32 bits do not hold are refused, not taken for what is left of them."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(wc, "lib", lambda: _NoLibrary())
+    with pytest.raises(wc.WcError):
+        _calls(torch, None, None, **sizes)[call]()
+
+
+@pytest.mark.parametrize("bad", [dict(k=BIG + 2), dict(k=-BIG + 2), dict(k=-1), dict(groups=BIG + 1),
+                                 dict(groups=-BIG + 1), dict(groups=2, top_groups=BIG + 1),
+                                 dict(group_top=BIG + 1)])
+def test_route_parameters_past_32_bits(monkeypatch, bad):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(wc, "lib", lambda: _NoLibrary())
+    how = dict(k=2)
+    how.update(bad)
+    for tokens in (0, 4):
+        with pytest.raises(wc.WcError):
+            wc.route_torch(_OnDevice((tokens, 16), torch.float32), stream=_Stream(), **how)
