@@ -17,6 +17,11 @@ constexpr uint32_t kLaunchTokens = 1u << 24;  // a grid's axis has less than 2^3
 // counts: 512 tokens of 8 slots (2 blocks) 13.9 us against 15.0, 1500 (6) 17.7 and 16.5,
 // but the host has a launch less.
 constexpr uint32_t kSelfCount = 4;
+// Counts (blocks of the sort times experts and one) from which they are summed up once, by a
+// launch more, and no longer by every block for itself.  With the launch and without, us: 8
+// experts 39.5 and 38.0 at 768 blocks, 65.9 and 70.0 at 1536; 61 experts 28.1 and 27.4 at 192,
+// 43.9 and 45.1 at 384; 256 experts 28.5 and 30.5 at 64; 512 experts 27.9 and 32.8 at 32.
+constexpr uint64_t kSumCounts = 16384;
 // Tokens from which four share a wave where they fit: 32768 of 61 experts 20.3 us against
 // 24.0, 4096 11.7 and 11.1.
 constexpr uint32_t kManyTokens = 16384;
@@ -222,6 +227,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(Route
 struct SortArgs {
   uint64_t ids, offsets, order, hist;
   uint32_t slots, experts, blocks;
+  uint32_t summed;  // hist holds sums over the blocks before each, and over all in one more row
 };
 __device__ __forceinline__ uint32_t class_of(const SortArgs& a, uint32_t slot) {
   const int32_t id = global<const int32_t>(a.ids)[slot];
@@ -239,6 +245,33 @@ __global__ __launch_bounds__(kSortThreads) void wc_route_count_kernel(SortArgs a
   __syncthreads();
   for (uint32_t e = threadIdx.x; e <= a.experts; e += kSortThreads)
     global<uint32_t>(a.hist)[uint64_t(blockIdx.x) * (a.experts + 1) + e] = count[e];
+}
+
+// Sums of the counts over the blocks, in place: 16 experts a workgroup, kSets runs of blocks.
+// What every block adds up for itself grows with the square of the blocks: 2^27 slots of 256
+// experts took 893 ms in all, and take 16.4.
+__global__ __launch_bounds__(kSortThreads) void wc_route_sum_kernel(SortArgs a) {
+  constexpr uint32_t kSets = kSortThreads / 16;
+  __shared__ uint32_t sums[kSets][16];
+  const uint32_t classes = a.experts + 1, set = threadIdx.x / 16, column = threadIdx.x % 16;
+  const uint32_t e = blockIdx.x * 16 + column, each = (a.blocks + kSets - 1) / kSets;
+  const uint32_t first = min(set * each, a.blocks), last = min(first + each, a.blocks);
+  const auto hist = global<uint32_t>(a.hist) + min(e, a.experts);
+  uint32_t sum = 0;
+#pragma unroll 8
+  for (uint32_t b = first; b < last; b++) sum += hist[uint64_t(b) * classes];
+  sums[set][column] = sum;
+  __syncthreads();
+  if (e >= classes) return;
+  uint32_t before = 0;
+  for (uint32_t s = 0; s < set; s++) before += sums[s][column];
+#pragma unroll 8
+  for (uint32_t b = first; b < last; b++) {
+    const uint32_t n = hist[uint64_t(b) * classes];
+    hist[uint64_t(b) * classes] = before;
+    before += n;
+  }
+  if (set == kSets - 1) hist[uint64_t(a.blocks) * classes] = before;
 }
 
 // The stable order of one block's slots: each expert's first place (all experts
@@ -273,6 +306,13 @@ __device__ __forceinline__ void sort_block(const SortArgs& a, SortShared& sh, ui
     for (uint32_t slot = t; slot < a.slots; slot += kSortThreads) {
       const uint32_t c = class_at(slot);
       atomicAdd(slot < mine_from ? &sh.before[c] : &sh.all[c], 1u);
+    }
+  } else if (a.summed) {
+    if (t < classes) {
+      const auto hist = global<const uint32_t>(a.hist) + t;
+      const uint32_t before = hist[uint64_t(block) * classes];
+      sh.before[t] = before;
+      sh.all[t] = hist[uint64_t(a.blocks) * classes] - before;
     }
   } else if (a.blocks > 1) {
     // each expert's slots in all blocks, and in those before this one: the blocks over as
@@ -388,6 +428,9 @@ bool params_ok(uint32_t tokens, const wc_route_params* p) {
          uint64_t(tokens) * p->k < (1ull << 31);
 }
 uint32_t sort_blocks(uint32_t slots) { return slots ? (slots + kSortSlots - 1) / kSortSlots : 1; }
+bool summed(uint32_t blocks, uint32_t experts) {
+  return blocks > kSelfCount && uint64_t(blocks) * (experts + 1) >= kSumCounts;
+}
 
 }  // namespace
 
@@ -397,7 +440,7 @@ extern "C" wc_status wc_route_workspace_bytes(uint32_t tokens, const wc_route_pa
   *bytes = 0;
   if (!params_ok(tokens, p)) return WC_EINVAL;
   const uint32_t blocks = sort_blocks(tokens * p->k);
-  if (blocks > kSelfCount) *bytes = uint64_t(blocks) * (p->experts + 1) * 4;
+  if (blocks > kSelfCount) *bytes = uint64_t(blocks + summed(blocks, p->experts)) * (p->experts + 1) * 4;
   return WC_OK;
 }
 
@@ -426,7 +469,7 @@ extern "C" wc_status wc_route(const void* dev_logits, int32_t dtype, uint32_t to
   const SortArgs s = {a.ids, reinterpret_cast<uint64_t>(dev_offsets),
                       reinterpret_cast<uint64_t>(dev_order),
                       need ? reinterpret_cast<uint64_t>(dev_workspace) : 0, tokens * p->k, p->experts,
-                      sort_blocks(tokens * p->k)};
+                      sort_blocks(tokens * p->k), summed(sort_blocks(tokens * p->k), p->experts)};
   const uint32_t e = p->experts;
   // small: one workgroup's round of choices, or two where a token takes one register (32
   // tokens of 64 experts 8.4 us against 6.7 in two launches, which the host takes 4 us
@@ -446,6 +489,10 @@ extern "C" wc_status wc_route(const void* dev_logits, int32_t dtype, uint32_t to
   }
   if (s.hist) {
     hipLaunchKernelGGL(wc_route_count_kernel, dim3(s.blocks), dim3(kSortThreads), 0, st, s);
+    if (hipGetLastError() != hipSuccess) return WC_EHIP;
+  }
+  if (s.summed) {
+    hipLaunchKernelGGL(wc_route_sum_kernel, dim3((e + 16) / 16), dim3(kSortThreads), 0, st, s);
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
   }
   hipLaunchKernelGGL(wc_route_order_kernel, dim3(s.blocks), dim3(kSortThreads), 0, st, s);

@@ -345,3 +345,41 @@ def test_many_experts_in_bf16(dev, score, tokens, experts, k):
     assert torch.equal(x.float().sort(dim=1)[0].diff(dim=1) > 0, torch.ones((tokens, experts - 1), dtype=torch.bool))
     r = wc.route_torch(x.to(dev), k, score)
     _check(r, x, k, score=score)
+
+
+@pytest.mark.parametrize("experts,k,blocks", [(512, 32, 31), (512, 32, 32), (255, 16, 63), (255, 16, 64),
+                                              (61, 8, 264), (61, 8, 265), (3, 2, 4095), (3, 2, 4096),
+                                              (16, 16, 963), (16, 16, 964), (1, 1, 8192), (300, 20, 700)])
+@pytest.mark.parametrize("last", [1, 2048])
+def test_order_where_counts_are_summed(dev, experts, k, blocks, last):
+    """Blocks of 2048 slots on both sides of 16384 counts, the last one full or begun."""
+    tokens = ((blocks - 1) * 2048 + last + k - 1) // k
+    g = torch.Generator(device=dev).manual_seed(blocks)
+    x = torch.randn((tokens, experts), generator=g, device=dev) \
+        + torch.randn(experts, generator=g, device=dev)
+    x[::7, experts // 2:] = -math.inf
+    r = wc.route_torch(x, k)
+    flat = torch.where(r.ids < 0, experts, r.ids).flatten().long()
+    assert torch.equal(r.order.long(), torch.sort(flat, stable=True)[1])
+    counts = torch.bincount(flat, minlength=experts + 1)[:experts]
+    assert torch.equal(r.offsets[1:].long(), counts.cumsum(0)) and int(r.offsets[0]) == 0
+    top, ids = torch.sort(x, dim=1, descending=True, stable=True)
+    assert torch.equal(r.ids.long(), torch.where(top == -math.inf, -1, ids)[:, :k])
+
+
+def test_time_grows_with_the_tokens(dev):
+    """Eight times the tokens, eight times the time: within half as much again for what the
+    caches no longer hold.  (A sort whose every block reads all blocks' counts takes 46 times.)"""
+    def us(tokens):
+        x = torch.randn((tokens, 256), device=dev, dtype=torch.bfloat16)
+        out = wc.route_torch(x, 8)
+        times = []
+        for _ in range(5):
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            wc.route_torch(x, 8, out=out)
+            end.record()
+            end.synchronize()
+            times.append(start.elapsed_time(end))
+        return min(times)
+    assert us(1 << 22) < 12 * us(1 << 19)
