@@ -754,9 +754,14 @@ bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t
   const QuantArgs a = {reinterpret_cast<uint64_t>(x), ldx, reinterpret_cast<uint64_t>(q),
                        reinterpret_cast<uint64_t>(scale), reinterpret_cast<uint64_t>(limit),
                        reinterpret_cast<uint64_t>(copies), m, k, step, 0, blocks ? *blocks : Blocks{}};
-  // few rows: more threads to each
-  if (m <= 256 && k > 2048 && k <= 8192) start_quantize<1024, 1>(dt, a, stream);
-  else if (m <= 256 && k > 2048 && k <= 16384) start_quantize<1024, 2>(dt, a, stream);
+  // Units of eight elements to a thread: as few threads as hold a row in eight units, but four
+  // times as many for few rows of more than 4096, which are latency.  us with 256 threads to a
+  // row and with 1024: 16 rows of 4096 bf16 2.26 and 2.64, 256 rows 2.68 and 2.97; 16 of 5000
+  // 3.06 and 2.71, 512 4.76 and 4.34, 1024 6.53 and 6.65; 16 of 8192 fp32 2.85 and 2.63, 512
+  // 6.08 and 5.61, 700 7.66 and 7.88; 16 of 16384 bf16 3.72 and 3.15, 512 7.98 and 7.45.
+  const bool few = m <= 512 && k > 4096;
+  if (few && k <= 8192) start_quantize<1024, 1>(dt, a, stream);
+  else if (few && k <= 16384) start_quantize<1024, 2>(dt, a, stream);
   else if (k <= 2048) start_quantize<256, 1>(dt, a, stream);
   else if (k <= 4096) start_quantize<256, 2>(dt, a, stream);
   else if (k <= 8192) start_quantize<256, 4>(dt, a, stream);

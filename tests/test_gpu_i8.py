@@ -393,3 +393,17 @@ def test_rows_far_apart_and_many_of_x(dev):
     q, scale = wc.quantize_i8_torch(x)
     p = (q[:, :k].double() @ w.double().T) * scale.double()[:, None] * ws.double()
     assert bool(((y.double() - p).abs() <= 1.01 * 5 * 2.0 ** -24 * p.abs() + LEAST[y.dtype]).all())
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("m", [511, 512, 513])
+@pytest.mark.parametrize("k", [2041, 2048, 2049, 4095, 4096, 4097, 8191, 8192, 8193, 16384, 16385, 32769])
+def test_quantize_at_its_bounds(dev, dtype, m, k):
+    """Both sides of every bound of the kernel's choice, codes and scales bit for bit."""
+    x = torch.randn((m, k), generator=torch.Generator(device=dev).manual_seed(k), device=dev).to(DT[dtype])
+    x[:, ::97] *= 30
+    q, s = wc.quantize_i8_torch(x)
+    top = x.float().abs().amax(dim=1)
+    assert torch.equal(s, top / torch.full_like(top, 127.0))
+    want = torch.round(x.float() * (torch.full_like(top, 127.0) / top)[:, None])
+    assert torch.equal(q[:, :k].float(), want) and not bool(q[:, k:].any())
