@@ -551,7 +551,9 @@ typedef struct {
  *                     share it must not overlap in time.
  * Rows of W may start at any byte; those that start at whole dwords (ldw and w
  * multiples of 4) are faster, and no dword is read that holds no byte of a
- * matrix.  The kernel and the parts of k follow from the sizes alone.
+ * matrix.  The kernel and the parts of k follow from the sizes alone.  Above 16
+ * rows the workspace may hold an int32 of every result, for each part of k, and where
+ * rows of W start within a dword three copies of the quantised activations.
  * The matrices have less than 2^27 rows together.  m = 0 is a
  * call that does nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
 wc_status wc_matmul_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
@@ -562,8 +564,10 @@ wc_status wc_matmul_i8(const int8_t* dev_q, const float* dev_scale, uint32_t m, 
 
 /* wc_linear_i8 -- wc_quantize_i8 and wc_matmul_i8 in one call: linear layers
  * that share their activations, e.g. q, k and v projections.  The quantised
- * activations stay in the workspace; a row or two are quantised by the product's
- * own launch.  Returns WC_EINVAL, WC_EHIP. */
+ * activations stay in the workspace.  Up to 16 rows with together at most 4096
+ * bytes of them (8192 with matrices of at most 32 MiB) are quantised by the product's
+ * own launch and need no workspace, if k is a multiple of 8 and all rows of W start
+ * at whole dwords.  Returns WC_EINVAL, WC_EHIP. */
 wc_status wc_linear_i8_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                        const wc_i8_job* jobs, uint64_t* bytes);
 wc_status wc_linear_i8(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
@@ -585,7 +589,10 @@ typedef struct {
 
 /* wc_route -- each token's experts, their weights, and the order of the
  * experts' rows.  Scores s = softmax or sigmoid of a token's logits, in fp32;
- * keys s + bias.  With groups > 1, each group of experts / groups neighbours is
+ * keys s + bias.  A softmax without a bias has the logits themselves for keys, which
+ * are in the scores' order and do not fall together where scores round to the same
+ * number; with groups ranked by two keys (group_top = 2) it has the scores, since
+ * those are added.  With groups > 1, each group of experts / groups neighbours is
  * ranked by the sum of its group_top largest keys, and only the top_groups best
  * take part.  The k largest keys are chosen, in order, ties to the lower index;
  * weights are the chosen scores (not the keys), renormalised if asked, times

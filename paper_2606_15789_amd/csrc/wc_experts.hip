@@ -61,7 +61,11 @@ __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place)
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
 
 // 16 columns of an expert's result for up to 16 of its rows: kMats products that
-// share their rows (gate and up, or down alone), k split over the waves.
+// share their rows (gate and up, or down alone), k split over the waves.  For matrices whose
+// rows start at other bytes of a dword than the copies of x, or than each other: each load
+// touches sixteen rows, which the L1 cache answers one line at a time.  32 tokens, 2 each, of
+// 8 experts of 4096 x 14336, gate a byte on: 292 us up (3.2 TB/s) and 113 down, 418 in all
+// against 281 on tiles; 256 tokens of 2048 x 1408 120 against 37.
 template <int kMats>
 __device__ __forceinline__ void expert_product(global_ptr<const uint8_t> x, const uint64_t (&mats)[2],
                                                uint32_t n, uint32_t k,
@@ -149,8 +153,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void wc_experts_down_kernel(ExpertA
 
 // The same from rings of whole lines, for few rows to an expert: bound by reading the
 // experts that were hit.  The sixteen rows of a product's W are eight of gate and the same
-// eight of up.  16 experts of 2048 x 1024, 8 tokens 4 each: 36 us for both products and
-// all around them, 2.2 TB/s of the weights hit.
+// eight of up.  16 experts of 2048 x 1024, 8 tokens 4 each: 13.8 us up and 9.0 down, 33 with
+// the three launches around them: latencies, at 2.7 TB/s of the weights hit.
 template <int kX>
 using ExpertRing = Ring<kX, 4, 4>;
 
@@ -383,9 +387,9 @@ __global__ __launch_bounds__(DownSlotRing::kThreads) void wc_experts_down_slot_k
 // The same on tiles through LDS.  A wave's columns of W are 32 of gate and the same 32
 // of up, so that both products of a value of h meet in one lane.  With few rows to an
 // expert bound by reading W: 8 experts of 6144 x 16384, 32 tokens 2 each, 287 us up (5.6
-// TB/s) and 159 down (5.1).  With many by the matrix units: 4096 tokens, 1551 us up (2.1
-// POP/s, the units busy 54 % of the cycles at 1.90 GHz; a stage of 128 bytes takes 1.65 us,
-// all else of a tile 13) and 858 down (1.9; 864 tiles are 3.4 rounds of workgroups).
+// TB/s) and 159 down (5.1).  With many by the matrix units: 4096 tokens, 1630 us up (2.0
+// POP/s, the units busy 52 % of the cycles at 1.87 GHz; a stage of 128 bytes takes 1.65 us,
+// a tile's 48 of them 79 of its some 91) and 855 down (1.9; 864 tiles are 3.4 rounds of workgroups).
 template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_up_tile_kernel(ExpertArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];

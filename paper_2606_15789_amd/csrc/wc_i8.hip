@@ -174,7 +174,8 @@ void start_quantize(int32_t dt, QuantArgs a, hipStream_t stream) {
 }
 
 // Word i of three copies of a row of q, shifted by one, two and three bytes, for codes that
-// were quantised by a call of their own.
+// were quantised by a call of their own.  Bound by memory: 4096 rows of 8191 22 us, 6 TB/s
+// read and written; 333 of 5461 6.3, a launch.
 __global__ __launch_bounds__(256) void wc_shift_i8_kernel(uint64_t q, uint64_t copies, uint32_t m,
                                                           uint32_t k, uint32_t first) {
   const uint64_t row = first + blockIdx.x;
@@ -211,7 +212,8 @@ constexpr int kRowWaves = 8;
 // blocks of 128 bytes.  A lane reads 32 bytes in a row of W and of x and feeds
 // two v_mfma_i32_16x16x64_i8: the sum runs over k in any order as long as both
 // operands agree.  For matrices past the other kernels' 32-bit offsets: each load touches
-// sixteen rows, which the L1 cache answers one line at a time (3.2 TB/s of W).
+// sixteen rows, which the L1 cache answers one line at a time (3.2 TB/s of W at best; k =
+// 8192, n = 3584, rows 2^20 + 5 bytes apart: 15.6 us up to 16 rows of x, 162 at 512).
 template <int kMT>
 __global__ __launch_bounds__(64 * kRowWaves) void wc_matmul_i8_rows_kernel(MatArgs a) {
   __shared__ int32_t part[kRowWaves][kMT * 256];

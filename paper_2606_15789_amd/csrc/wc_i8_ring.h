@@ -133,7 +133,7 @@ __host__ __device__ __forceinline__ void settle_block(SlotBlock& at, uint32_t bl
 }
 
 // Quantise `rows` rows of x into LDS, chunk c of each 128-byte block of row r at chunk
-// c ^ (r mod 8); `row_at(r)` is a row's address, 16-byte aligned, k elements (a multiple
+// c ^ (r mod 8); `row_at(r)` is a row's address, at any element, k elements (a multiple
 // of 8) of type kType.  A thread's first kKeep units of eight elements are on their way
 // at once and stay in registers; any more are read again, from the caches.  scales, tops:
 // LDS, one a row.

@@ -97,9 +97,12 @@ __device__ __forceinline__ int32_t take_best(uint32_t (&key)[kPer], uint32_t flo
 
 // The choice of one token by kLanes lanes: expert lane + kLanes i in register i.  A softmax
 // without a bias chooses by the logits, which are in the scores' order, so no two of them
-// fall together by rounding.  Lane j < k gets slot j's expert and weight.  Bound by the
-// chain of k reductions; all lanes of a wave work on as many tokens as fit it.  4096 tokens of
-// 256 experts, 8 of 4 of 8 groups, 11.8 us; 32771 of 61, 6 of them, 11.3.
+// fall together by rounding.  Lane j < k gets slot j's expert and weight.  All lanes of a wave
+// work on as many tokens as fit it.  32771 tokens of 61 experts, 6 of them, 11.0 us: bound by
+// issuing vector instructions, 91 % of the cycles (a ballot and a select for each register,
+// k times).  4096 of 256 experts, 8 of 4 of 8 groups, 11.9 us: 58 % of the cycles, with four
+// waves to a SIMD; the groups' keys read from LDS a fifth of them, two thirds of that in bank
+// conflicts (8 lanes, 32 words apart).
 template <int kLanes, int kPer>
 __device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float* scratch,
                                        int32_t& id, float& weight) {
