@@ -591,19 +591,19 @@ typedef struct {
  * experts' rows.  Scores s = softmax or sigmoid of a token's logits, in fp32;
  * keys s + bias.  A softmax without a bias has the logits themselves for keys, which
  * are in the scores' order and do not fall together where scores round to the same
- * number; with groups ranked by two keys (group_top = 2) it has the scores, since
- * those are added.  With groups > 1, each group of experts / groups neighbours is
- * ranked by the sum of its group_top largest keys, and only the top_groups best
- * take part.  The k largest keys are chosen, in order, ties to the lower index;
- * weights are the chosen scores (not the keys), renormalised if asked, times
- * scale.
+ * number; where groups are ranked by two keys (groups > 1, group_top = 2) it has the
+ * scores, since those are added.  With groups > 1, each group of experts / groups
+ * neighbours is ranked by the sum of its group_top largest keys, and only the
+ * top_groups best take part.  The k largest keys are chosen, in order, ties to the
+ * lower index; weights are the chosen scores (not the keys), renormalised if asked,
+ * times scale.
  *   An expert whose logit or bias is -inf is masked: it takes no part, in the
  * softmax's sum either.  A token with fewer than k experts left has id -1 and
  * weight 0 in its last slots.  A NaN logit or bias of an expert that is not masked
  * makes its token's weights NaN; that expert is not chosen, nor a NaN logit in the
  * softmax's sum, and the others are chosen as without it.  An infinite logit of a
- * softmax makes its token's weights NaN too; the choice takes its score for 1 (as
- * many as there are share that 1) and finite logits' scores for 0.
+ * softmax makes its token's weights NaN too; where keys hold scores, the choice takes
+ * its score for 1 (shared by as many as there are) and finite logits' scores for 0.
  *   dev_logits, dtype  tokens rows of experts logits, ld elements apart;
  *   dev_bias           NULL, or experts floats;
  *   dev_ids            tokens x k int32;
