@@ -130,6 +130,48 @@ struct Blocks {
   uint32_t experts, slots, rows, most;
 };
 
+// The table of `Blocks`, by one workgroup.
+template <int kThreads>
+__device__ __forceinline__ void write_blocks(const Blocks& b, uint32_t (&starts)[kMaxExperts + 1]) {
+  const auto offset = [&](uint32_t e) -> uint32_t {
+    const int32_t at = global<const int32_t>(b.offsets)[e];
+    return at < 0 ? 0u : uint32_t(at) < b.slots ? uint32_t(at) : b.slots;
+  };
+  for (uint32_t e = threadIdx.x; e < b.experts; e += kThreads) {
+    const uint32_t from = offset(e), to = offset(e + 1);
+    starts[e + 1] = to > from ? (to - from + b.rows - 1) / b.rows : 0;
+  }
+  if (threadIdx.x == 0) starts[0] = 0;
+  __syncthreads();
+  // the blocks before each expert
+  if (threadIdx.x < 64) {
+    uint32_t before = 0;
+    for (uint32_t e0 = 1; e0 <= b.experts; e0 += 64) {
+      const uint32_t e = e0 + threadIdx.x;
+      uint32_t sum = e <= b.experts ? starts[e] : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint32_t v = uint32_t(__shfl_up(int(sum), d));
+        if (threadIdx.x >= uint32_t(d)) sum += v;
+      }
+      if (e <= b.experts) starts[e] = before + sum;
+      before += uint32_t(__shfl(int(sum), 63));
+    }
+  }
+  __syncthreads();
+  const uint32_t all = min(starts[b.experts], b.most);
+  if (threadIdx.x == 0) *global<u32x4>(b.table) = u32x4{all, 0, 0, 0};
+  for (uint32_t t = threadIdx.x; t < all; t += kThreads) {
+    uint32_t low = 0, high = b.experts;  // starts[low] <= t < starts[high]
+    while (high - low > 1) {
+      const uint32_t middle = (low + high) / 2;
+      (starts[middle] <= t ? low : high) = middle;
+    }
+    const uint32_t first = offset(low) + (t - starts[low]) * b.rows, end = offset(low + 1);
+    global<u32x4>(b.table)[t + 1] = u32x4{low, first, end < first + b.rows ? end : first + b.rows, 0u};
+  }
+}
+
 // Quantise m rows of k elements of type dt to rows of WC_I8_ROW_BYTES(k) bytes
 // (wc_i8.hip), or as many of them as the device int `limit` says; with `blocks`, one more
 // workgroup writes its table; with `copies`, their shifted copies (wc_i8_tile.h) too.
