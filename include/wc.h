@@ -8,7 +8,8 @@
  * wc_gemv_mx: MXFP4; wc_gemv_w4: int4 with group scales).  Compression runs on the host (wc_encode) or on the GPU
  * (wc_encode_device), to the same blob.  The layers of a decoded int8 checkpoint
  * run on wc_linear_i8 (activations quantised per token, scaled products),
- * wc_route and wc_experts_i8 (a mixture layer's routing and experts).
+ * wc_route and wc_experts_i8 (a mixture layer's routing and experts), those of a decoded
+ * MXFP4 checkpoint on wc_linear_mx, wc_experts_mx and wc_moe_mx.
  *
  * Paper: "Approaching Shannon Bound with Lossless LLM Weight Compression"
  * (Tan, Chen, Alonso, Wong, He).
@@ -657,6 +658,129 @@ wc_status wc_experts_i8(const void* dev_x, int32_t dtype, uint32_t tokens, uint6
                         const wc_i8_experts* gate, const wc_i8_experts* up,
                         const wc_i8_experts* down, void* dev_y, uint64_t ldy,
                         void* dev_workspace, uint64_t workspace_bytes, void* stream);
+
+/* --- Microscaled 4-bit layers --------------------------------------------------
+ * What a program runs on an MXFP4 checkpoint (the paper's fp4 format, Sec. VI-A) once
+ * wc_decode has given it back, with the activations in MXFP4 too: each 32 elements of a
+ * row are a block of e2m1 codes (two to a byte, the even one in the low nibble) and an
+ * e8m0 scale byte E, worth 2^(E - 127) (255: NaN, all of the block).  Rows of codes are
+ * whole blocks of 16 bytes, zeros past the row's k, and start at 16-byte aligned
+ * addresses; scales have any alignment.  All device pointers, all on `stream`,
+ * asynchronous, allocating nothing.  Element types of activations, biases and results
+ * are WC_BF16, WC_FP16 or WC_FP32; k is 1..65536. */
+#define WC_MX_BLOCKS(k) (((uint64_t)(k) + 31u) / 32u)
+#define WC_MX_ROW_BYTES(k) (WC_MX_BLOCKS(k) * 16u)
+
+/* wc_quantize_mx -- rows to MXFP4.  With a the largest magnitude of a block, E =
+ * max(floor(log2 a) + 125, 0), and a code is the e2m1 number nearest to x / 2^(E - 127),
+ * ties to the even code, at most 6 in magnitude (a / 2^(E - 127) is less than 8); a number that
+ * rounds to zero keeps its sign.  A block of zeros has E = 0, one that holds an
+ * infinity or a NaN E = 255 and zero codes: every product with its row is NaN.
+ *   dev_x, x_dtype  m rows of k elements, `ldx` elements apart, aligned to the element;
+ *   m               0..2^31 - 1 rows;
+ *   dev_q           m rows of WC_MX_ROW_BYTES(k) bytes, ldq bytes apart (a multiple of 16);
+ *   dev_scale       m rows of WC_MX_BLOCKS(k) bytes, lds bytes apart.
+ * Bytes between rows are left as they are.  Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_quantize_mx(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
+                         uint8_t* dev_q, uint64_t ldq, uint8_t* dev_scale, uint64_t lds,
+                         void* stream);
+
+/* wc_dequantize_mx -- the values of MXFP4 rows, rounded once to y's type (beyond its
+ * range: an infinity).  Arguments as for wc_quantize_mx; y has m rows of k elements, ldy
+ * elements apart.  Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_dequantize_mx(const uint8_t* dev_q, uint64_t ldq, const uint8_t* dev_scale,
+                           uint64_t lds, uint32_t m, uint32_t k, void* dev_y, int32_t y_dtype,
+                           uint64_t ldy, void* stream);
+
+/* One MXFP4 matrix that multiplies MXFP4 activations: y = x W^T + bias, summed in fp32
+ * and rounded once to y's type. */
+typedef struct {
+  const void* w;       /* n rows of WC_MX_ROW_BYTES(k) bytes, ldw bytes apart, 16-byte aligned */
+  const void* scale;   /* n rows of WC_MX_BLOCKS(k) bytes, lds bytes apart */
+  const void* bias;    /* NULL, or n values of bias_dtype */
+  void* y;             /* m rows of n elements of y_dtype, ldy elements apart (NULL if m = 0) */
+  uint64_t ldw, lds, ldy;
+  uint32_t n;
+  int32_t bias_dtype, y_dtype, reserved;
+} wc_mx_job;
+
+/* wc_matmul_mx -- the products of one batch of MXFP4 activations (as wc_quantize_mx writes
+ * them) with n_jobs (1..32) matrices.
+ *   dev_q, ldq, dev_scale, lds  m rows of k, 0..2^31 - 1 of them;
+ *   dev_workspace     at least wc_matmul_mx_workspace_bytes bytes, 256-byte aligned (NULL
+ *                     where that is 0); overwritten; calls that share it must not
+ *                     overlap in time.
+ * Codes past k in a row of W may be any; those of x must be zeros.  A sum has no error where
+ * its products' scales lie within 2^24 of each other and its value fits; otherwise that of
+ * fp32 sums.  The order of a sum goes by the sizes alone: the result is the same on every
+ * run.  The matrices have less than 2^27 rows together.  m = 0 is a call that does
+ * nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_matmul_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
+                                       const wc_mx_job* jobs, uint64_t* bytes);
+wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint8_t* dev_scale, uint64_t lds,
+                       uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs,
+                       void* dev_workspace, uint64_t workspace_bytes, void* stream);
+
+/* wc_linear_mx -- wc_quantize_mx and wc_matmul_mx in one call: linear layers that share
+ * their activations.  Up to 16 rows are quantised by the product's own launch; more in
+ * the workspace.  Returns WC_EINVAL, WC_EHIP. */
+wc_status wc_linear_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
+                                       const wc_mx_job* jobs, uint64_t* bytes);
+wc_status wc_linear_mx(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
+                       uint32_t n_jobs, const wc_mx_job* jobs, void* dev_workspace,
+                       uint64_t workspace_bytes, void* stream);
+
+/* The MXFP4 matrices of a mixture layer's experts: for expert e, n rows of
+ * WC_MX_ROW_BYTES(k) bytes at w + e * stride and of WC_MX_BLOCKS(k) scale bytes at
+ * scale + e * scale_stride (no padding between rows; w and stride multiples of 16). */
+typedef struct {
+  const void* w;
+  const void* scale;
+  uint64_t stride;        /* bytes between experts, at least n * WC_MX_ROW_BYTES(k) */
+  uint64_t scale_stride;  /* at least n * WC_MX_BLOCKS(k) */
+} wc_mx_experts;
+
+/* wc_experts_mx -- the gated feed-forward of a mixture layer: for every token y = sum over
+ * its slots of weight * down(h), h = silu(gate x) * (up x), with the matrices of the slot's
+ * expert; x and h are brought to MXFP4 (as by wc_quantize_mx, h from fp32) before each
+ * product, the experts' results are held in fp32, and the slots are added in fp32.
+ *   dev_x, dtype   tokens rows of hidden elements, ldx elements apart;
+ *   ids .. order   as wc_route writes them for tokens, experts and k: ids agree with
+ *                  offsets and order (the call goes by either); a slot whose id is
+ *                  negative adds weight * 0;
+ *   gate, up       matrices of ffn rows of hidden columns; down: hidden rows of ffn
+ *                  columns (hidden, ffn 1..65536, experts 1..512, k 1..experts, tokens * k
+ *                  < 2^24);
+ *   dev_y          tokens rows of hidden elements of x's type, ldy apart;
+ *   dev_workspace  at least wc_experts_mx_workspace_bytes bytes, 256-byte aligned;
+ *                  overwritten; calls that share it must not overlap.
+ * Entries of ids, offsets or order out of range are taken as the nearest in range: the
+ * result is then wrong, but nothing outside the arguments is touched.  The result is the
+ * same on every run.  Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_experts_mx_workspace_bytes(uint32_t tokens, uint32_t k, uint32_t experts,
+                                        uint32_t hidden, uint32_t ffn, uint64_t* bytes);
+wc_status wc_experts_mx(const void* dev_x, int32_t dtype, uint32_t tokens, uint64_t ldx,
+                        uint32_t k, uint32_t experts, uint32_t hidden, uint32_t ffn,
+                        const int32_t* dev_ids, const float* dev_weights,
+                        const int32_t* dev_offsets, const int32_t* dev_order,
+                        const wc_mx_experts* gate, const wc_mx_experts* up,
+                        const wc_mx_experts* down, void* dev_y, uint64_t ldy,
+                        void* dev_workspace, uint64_t workspace_bytes, void* stream);
+
+/* wc_moe_mx -- a whole mixture layer from the router's logits: wc_route and wc_experts_mx in
+ * one call.  Up to 16 tokens it is two launches: each workgroup of the first chooses the
+ * tokens' experts for itself.
+ *   dev_logits, logits_dtype, ld, p, dev_bias   as for wc_route (p->k slots a token);
+ *   the other arguments as for wc_experts_mx, the workspace by wc_moe_mx_workspace_bytes.
+ * Returns WC_EINVAL (argument), WC_EHIP. */
+wc_status wc_moe_mx_workspace_bytes(uint32_t tokens, const wc_route_params* p, uint32_t hidden,
+                                    uint32_t ffn, uint64_t* bytes);
+wc_status wc_moe_mx(const void* dev_x, int32_t dtype, uint32_t tokens, uint64_t ldx,
+                    const void* dev_logits, int32_t logits_dtype, uint64_t ld,
+                    const wc_route_params* p, const float* dev_bias, uint32_t hidden, uint32_t ffn,
+                    const wc_mx_experts* gate, const wc_mx_experts* up, const wc_mx_experts* down,
+                    void* dev_y, uint64_t ldy, void* dev_workspace, uint64_t workspace_bytes,
+                    void* stream);
 
 /* wc_free -- release a blob from wc_encode / wc_open.  NULL is a no-op. */
 void wc_free(wc_blob* b);

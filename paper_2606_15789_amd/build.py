@@ -14,11 +14,12 @@ SOURCES = [os.path.join(CSRC, "wc_host.cpp"), os.path.join(CSRC, "wc_decode.hip"
            os.path.join(CSRC, "wc_gemm_wide.hip"), os.path.join(CSRC, "wc_gemm_wide_bf16.hip"),
            os.path.join(CSRC, "wc_encode.hip"), os.path.join(CSRC, "wc_stream.hip"),
            os.path.join(CSRC, "wc_i8.hip"), os.path.join(CSRC, "wc_route.hip"),
-           os.path.join(CSRC, "wc_experts.hip")]
+           os.path.join(CSRC, "wc_experts.hip"), os.path.join(CSRC, "wc_mx.hip"),
+           os.path.join(CSRC, "wc_mx_experts.hip")]
 HEADERS = [os.path.join(CSRC, "wc_internal.h"), os.path.join(CSRC, "wc_decoder.h"),
            os.path.join(CSRC, "wc_ring.h"), os.path.join(CSRC, "wc_i8.h"),
            os.path.join(CSRC, "wc_i8_tile.h"), os.path.join(CSRC, "wc_i8_ring.h"),
-           os.path.join(CSRC, "wc_choose.h"),
+           os.path.join(CSRC, "wc_choose.h"), os.path.join(CSRC, "wc_mx.h"),
            os.path.join(os.path.dirname(HERE), "include", "wc.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = os.environ.get("WC_OFFLOAD_ARCH", "gfx950")

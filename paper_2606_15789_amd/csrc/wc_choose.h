@@ -196,7 +196,12 @@ __device__ __forceinline__ void choose(const RouteArgs& a, uint32_t token, float
   }
   weight *= a.scale;
   if (votes<kLanes>(bad)) weight = __builtin_nanf("");
-  if (live && lane < a.k) {
+}
+// Lane j's slot of a token to memory.
+template <int kLanes>
+__device__ __forceinline__ void store_choice(const RouteArgs& a, uint32_t token, int32_t id, float weight) {
+  const uint32_t lane = threadIdx.x % kLanes;
+  if (token < a.tokens && lane < a.k) {
     const uint64_t at = uint64_t(token) * a.k + lane;
     global<int32_t>(a.ids)[at] = id;
     global<float>(a.weights)[at] = weight;

@@ -1,0 +1,260 @@
+// wc_mx.h -- device helpers of the microscaled 4-bit layers: MXFP4 blocks (32 e2m1 codes, two
+// to a byte, the even one low, and an e8m0 scale) and their products on
+// v_mfma_scale_f32_16x16x128_f8f6f4.
+//
+// A product of two codes is a multiple of 1/4 up to 36, so a block's sum is exact in fp32, and so
+// is the sum over blocks as long as their scales keep it within 24 bits.
+#pragma once
+
+#include "wc_i8.h"
+
+namespace wc_mx {
+
+using namespace wc_i8;
+
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Blocks of 512 of k: four products of 128 of k, whose lane groups of sixteen take a block each.
+constexpr uint32_t kSuper = 16;
+
+inline uint32_t blocks_of(uint32_t k) { return uint32_t(WC_MX_BLOCKS(k)); }
+
+// The scale byte of a block from the bits of its largest magnitude as a float: two below its
+// exponent, so that the magnitude lies from 4 to 8 (e2m1's largest are 4 and 6). 255, a NaN,
+// where the block holds an infinity or a NaN.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t max_bits) {
+  const uint32_t field = max_bits >> 23;
+  return field == 255 ? 255u : max(field, 2u) - 2u;
+}
+// 2^(byte - 127) as the conversions take it.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return __uint_as_float(byte ? byte << 23 : 1u << 22);
+}
+
+// Eight elements in registers: four words of a 16-bit type, or eight floats.
+template <int kType>
+struct Eight {
+  static constexpr int kWords = kType == WC_FP32 ? 8 : 4;
+  uint32_t v[kWords];
+  // the largest magnitude, as bits that order like it: of the element's type
+  __device__ __forceinline__ uint32_t top() const {
+    if constexpr (kType == WC_FP32) {
+      uint32_t t = 0;
+#pragma unroll
+      for (int i = 0; i < 8; i++) t = max(t, v[i] & 0x7FFFFFFFu);
+      return t;
+    } else {
+      u16x2 t = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, v[i] & 0x7FFF7FFFu));
+      return max(uint32_t(t[0]), uint32_t(t[1]));
+    }
+  }
+  // its codes: to nearest, ties to the even code, at most 6
+  __device__ __forceinline__ uint32_t codes(float scale) const {
+    uint32_t c = 0;
+    if constexpr (kType == WC_FP32) {
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(v[0]), __uint_as_float(v[1]), scale, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(v[2]), __uint_as_float(v[3]), scale, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(v[4]), __uint_as_float(v[5]), scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(v[6]), __uint_as_float(v[7]), scale, 3);
+    } else if constexpr (kType == WC_BF16) {
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[0]), scale, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[1]), scale, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[2]), scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[3]), scale, 3);
+    } else {
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, v[0]), scale, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, v[1]), scale, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, v[2]), scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, v[3]), scale, 3);
+    }
+    return c;
+  }
+};
+// A largest magnitude of kType as a float's bits.
+template <int kType>
+__device__ __forceinline__ uint32_t float_bits(uint32_t top) {
+  if constexpr (kType == WC_FP32) return top;
+  return kType == WC_BF16 ? top << 16 : __float_as_uint(fp16_to_float(top));
+}
+// Eight elements at address p (aligned to the element), of which `left` are the row's; the
+// others are zeros and not read.
+template <int kType>
+__device__ __forceinline__ Eight<kType> load_eight(uint64_t p, int32_t left) {
+  Eight<kType> e;
+  if (left >= 8) {
+    const auto from = global<const u32x4u>(p);
+#pragma unroll
+    for (int i = 0; i < Eight<kType>::kWords / 4; i++) {
+      const u32x4 w = from[i];
+#pragma unroll
+      for (int j = 0; j < 4; j++) e.v[4 * i + j] = w[j];
+    }
+    return e;
+  }
+#pragma unroll
+  for (int i = 0; i < Eight<kType>::kWords; i++) e.v[i] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    if (i >= left) continue;
+    if constexpr (kType == WC_FP32) e.v[i] = global<const uint32_t>(p)[i];
+    else e.v[i / 2] |= uint32_t(global<const uint16_t>(p)[i]) << (16 * (i % 2));
+  }
+  return e;
+}
+
+// A lane's four blocks of 512 of k of one row: step s has block 4 s + lane / 16, the scale in the
+// low byte of its word.
+struct Part {
+  u32x4 codes[4];
+  u32x4 scales;
+};
+
+// The row of an MXFP4 matrix that a lane multiplies.
+struct Row {
+  uint64_t codes, scales;
+};
+__device__ __forceinline__ u32x4 load_scales(uint64_t scales, uint32_t super, uint32_t blocks) {
+  const uint32_t g = threadIdx.x % 64 / 16;
+  u32x4 s;
+  if (super * kSuper + kSuper <= blocks) {
+    s = *global<const u32x4u>(scales + super * kSuper);
+#pragma unroll
+    for (int i = 0; i < 4; i++) s[i] >>= 8 * g;
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i++)
+      s[i] = global<const uint8_t>(scales)[min(super * kSuper + 4 * i + g, blocks - 1)];
+  }
+  return s;
+}
+// Blocks past the row's are its last one again; kZero: their codes are zeros, so that a product
+// with anything but a NaN scale, which the row then has in its last block too, adds nothing.
+template <bool kZero>
+__device__ __forceinline__ Part load_part(const Row& r, uint32_t super, uint32_t blocks) {
+  const uint32_t g = threadIdx.x % 64 / 16;
+  Part p;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t b = super * kSuper + 4 * i + g;
+    p.codes[i] = global<const u32x4>(r.codes)[min(b, blocks - 1)];
+    if (kZero && b >= blocks) p.codes[i] = u32x4{0, 0, 0, 0};
+  }
+  p.scales = load_scales(r.scales, super, blocks);
+  return p;
+}
+// The same of a row of elements (k of them; none: all zeros), quantised in registers.
+template <int kType>
+__device__ __forceinline__ Part quantize_part(uint64_t row, uint32_t super, uint32_t k) {
+  constexpr uint32_t kSize = kType == WC_FP32 ? 4 : 2;
+  const uint32_t g = threadIdx.x % 64 / 16;
+  Part p;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t at = (super * kSuper + 4 * i + g) * 32;
+    Eight<kType> e[4];
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++)
+      e[j] = load_eight<kType>(row + uint64_t(at + 8 * j) * kSize, int32_t(k) - int32_t(at + 8 * j));
+    const uint32_t top = max(max(e[0].top(), e[1].top()), max(e[2].top(), e[3].top()));
+    const uint32_t byte = scale_byte(float_bits<kType>(top));
+    const float scale = scale_value(byte);
+#pragma unroll
+    for (int j = 0; j < 4; j++) p.codes[i][j] = byte == 255 ? 0u : e[j].codes(scale);
+    p.scales[i] = byte;
+  }
+  return p;
+}
+
+__device__ __forceinline__ i32x8 operand(u32x4 c) {
+  return __builtin_bit_cast(i32x8, __builtin_shufflevector(c, c, 0, 1, 2, 3, -1, -1, -1, -1));
+}
+// acc += 16 rows of W times 16 rows of x over 512 of k: lane l gets W rows 4 (l / 16) .. + 3 of
+// x row l mod 16.
+__device__ __forceinline__ void multiply(const Part& w, const Part& x, f32x4& acc) {
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w.codes[i]), operand(x.codes[i]), acc, 4,
+                                                           4, 0, int(w.scales[i]), 0, int(x.scales[i]));
+}
+
+// kN blocks of 16 rows of W by kM blocks of 16 rows of x, k split over the waves of a workgroup
+// in parts of 512: straight from memory to registers.  `load_x(m, super)` gives block m's Part.
+template <int kN, int kM, int kWaves>
+struct Slim {
+  static constexpr uint32_t kThreads = 64 * kWaves;
+  static constexpr uint32_t kPart = kN * kM * 64;  // groups of four sums to a wave
+  struct Shared {
+    f32x4 part[kWaves][kPart];
+  };
+  template <class LoadX>
+  static __device__ __forceinline__ void product(Shared& sh, const Row (&w)[kN], uint32_t blocks,
+                                                 LoadX load_x) {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const uint32_t supers = (blocks + kSuper - 1) / kSuper;
+    f32x4 acc[kN][kM];
+#pragma unroll
+    for (int n = 0; n < kN; n++)
+#pragma unroll
+      for (int m = 0; m < kM; m++) acc[n][m] = f32x4{0, 0, 0, 0};
+    for (uint32_t s = wave; s < supers; s += kWaves) {
+      Part wp[kN];
+#pragma unroll
+      for (int n = 0; n < kN; n++) wp[n] = load_part<false>(w[n], s, blocks);
+#pragma unroll
+      for (int m = 0; m < kM; m++) {
+        const Part xp = load_x(m, s);
+#pragma unroll
+        for (int n = 0; n < kN; n++) multiply(wp[n], xp, acc[n][m]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kN; n++)
+#pragma unroll
+      for (int m = 0; m < kM; m++) sh.part[wave][(n * kM + m) * 64 + lane] = acc[n][m];
+    __syncthreads();
+  }
+  // group i of the sums: block i / 64 (n kM + m), lane i mod 64 of it
+  static __device__ __forceinline__ f32x4 sum(const Shared& sh, uint32_t i) {
+    f32x4 v = sh.part[0][i];
+#pragma unroll
+    for (int w = 1; w < kWaves; w++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] += sh.part[w][i][j];
+    return v;
+  }
+};
+
+// Four neighbouring elements of type dt from element i on at address p, of which `left` are in
+// the row.
+__device__ __forceinline__ void store_four(uint64_t p, int32_t dt, uint64_t i, f32x4 v, uint32_t left) {
+  const uint64_t at = p + i * (dt == WC_FP32 ? 4 : 2);
+  if (left >= 4 && dt == WC_FP32 && at % 16 == 0) {
+    *global<f32x4>(at) = v;
+  } else if (left >= 4 && dt != WC_FP32 && at % 8 == 0) {
+    u32x2 h;
+    if (dt == WC_BF16)
+      h = {floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])};
+    else
+      h = {float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16, float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16};
+    *global<u32x2>(at) = h;
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++)
+      if (j < left) store_float(p, dt, i + j, v[j]);
+  }
+}
+
+// Quantise m rows of k elements of type dt to rows of `ldq` bytes of codes and `lds` of scales
+// (wc_mx.hip); with `blocks`, one more workgroup writes its table.  False on a launch error.
+bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
+                     uint64_t ldq, void* scale, uint64_t lds, hipStream_t stream,
+                     const Blocks* blocks = nullptr);
+
+inline bool off(const void* p, uint32_t to) { return !p || reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+}  // namespace wc_mx

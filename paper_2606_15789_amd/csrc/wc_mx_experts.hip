@@ -1,0 +1,539 @@
+// wc_mx_experts.hip -- mixture layers with MXFP4 experts: wc_experts_mx, wc_moe_mx.
+//
+// For a token t with experts e_j of weights g_j:
+//   h_j = silu(G_ej x_t) * (U_ej x_t),  y_t = sum_j g_j D_ej h_j,
+// x_t and every h_j in MXFP4.  The scale of a block of h needs 32 of its columns only, so the
+// product that makes them quantises them as well.  Two ways:
+//   - up to 16 tokens, which are the columns of a matrix instruction, two kernels: one finds the
+//     experts (and chooses them, from logits), multiplies by gate and up and writes h by slot, the
+//     other multiplies by down and adds a token's slots;
+//   - more tokens: the places of the router's order in blocks of one expert's, each expert's
+//     results stored by slot and then added.
+#include <algorithm>
+
+#include "wc_choose.h"
+#include "wc_mx.h"
+
+namespace {
+
+using namespace wc_mx;
+using wc_choose::RouteArgs;
+
+struct Bank {
+  uint64_t w, scale, stride, scale_stride;
+};
+struct ExpertArgs {
+  uint64_t table, order, ids, weights;
+  uint64_t x, ldx;
+  uint64_t xq, xs;  // quantised x, by token
+  uint64_t hq, hs;  // quantised h, by place in the order (few tokens: by slot)
+  uint64_t out;     // experts' results, fp32, by slot
+  uint64_t y, ldy;
+  uint32_t tokens, k, experts, hidden, ffn, slots;
+  uint32_t first;   // this launch's first block of places, or token
+  int32_t dtype;
+  Bank gate, up, down;
+};
+__device__ __forceinline__ Row row_of(const Bank& b, uint32_t e, uint32_t row, uint32_t blocks) {
+  return {b.w + e * b.stride + uint64_t(row) * (blocks * 16), b.scale + e * b.scale_stride + uint64_t(row) * blocks};
+}
+
+// g / (1 + exp(-g)), with an exponential of 1 ulp and a rounded division
+__device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
+
+// Four lanes to a row of 32 values of h in LDS: its codes and scale, eight codes to a lane, all
+// four lanes of a row alive or none.
+__device__ __forceinline__ void quantize_h(const float* row, uint64_t codes, uint64_t scale, bool live) {
+  const uint32_t q = threadIdx.x % 4;
+  Eight<WC_FP32> e;
+#pragma unroll
+  for (int i = 0; i < 8; i++) e.v[i] = __float_as_uint(row[q * 8 + i]);
+  uint32_t top = e.top();
+  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xF, 0xF, false)));  // lane ^ 1
+  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xF, 0xF, false)));  // lane ^ 2
+  if (!live) return;
+  const uint32_t byte = scale_byte(top);
+  global<uint32_t>(codes)[q] = byte == 255 ? 0u : e.codes(scale_value(byte));
+  if (q == 0) *global<uint8_t>(scale) = uint8_t(byte);
+}
+constexpr int kRowH = 36;  // floats of a row of h in LDS
+
+// --- few tokens ---------------------------------------------------------------
+
+constexpr uint32_t kFew = 16;  // tokens
+constexpr int kFewWaves = 8;
+
+inline bool is_few(uint64_t tokens, uint64_t k) { return tokens <= kFew && k <= wc_choose::kMaxChosen; }
+struct Chosen {
+  int32_t ids[kFew][wc_choose::kMaxChosen];
+  float weights[kFew][wc_choose::kMaxChosen];
+  uint8_t hit[kMaxExperts];
+  uint16_t list[kMaxExperts];  // the experts hit, in order
+  uint32_t count;
+};
+// Lists the experts that ids name.
+__device__ __forceinline__ void list_experts(Chosen& c, const ExpertArgs& a) {
+  for (uint32_t e = threadIdx.x; e < kMaxExperts; e += 64 * kFewWaves) c.hit[e] = 0;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < a.slots; i += 64 * kFewWaves) {
+    const int32_t id = c.ids[i / a.k][i % a.k];
+    if (id >= 0) c.hit[id] = 1;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    uint32_t count = 0;
+    for (uint32_t e0 = 0; e0 < a.experts; e0 += 64) {
+      const bool on = c.hit[e0 + threadIdx.x];
+      const uint64_t all = __ballot(on);
+      if (on) c.list[count + uint32_t(__popcll(all & ((1ull << threadIdx.x) - 1)))] = uint16_t(e0 + threadIdx.x);
+      count += uint32_t(__popcll(all));
+    }
+    if (threadIdx.x == 0) c.count = count;
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void load_choice(Chosen& c, const ExpertArgs& a) {
+  for (uint32_t i = threadIdx.x; i < a.slots; i += 64 * kFewWaves) {
+    const int32_t id = global<const int32_t>(a.ids)[i];
+    c.ids[i / a.k][i % a.k] = id < 0 ? -1 : min(id, int32_t(a.experts) - 1);
+    c.weights[i / a.k][i % a.k] = global<const float>(a.weights)[i];
+  }
+}
+// The first slot of a token with expert e, -1 if none.
+__device__ __forceinline__ int32_t slot_of(const Chosen& c, const ExpertArgs& a, uint32_t token, uint32_t e) {
+  int32_t slot = -1;
+  if (token < a.tokens)
+    for (int32_t j = int32_t(a.k) - 1; j >= 0; j--)
+      if (c.ids[token][j] == int32_t(e)) slot = int32_t(token * a.k) + j;
+  return slot;
+}
+
+// 32 columns of h for all tokens of one expert, quantised.  kPer: registers of logits to a
+// lane of the choice, 0 where the ids are given.
+template <int kType, int kPer>
+__global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
+  using S = Slim<4, 1, kFewWaves>;
+  __shared__ typename S::Shared sh;
+  __shared__ Chosen c;
+  __shared__ float h[kFew][kRowH];
+  if constexpr (kPer > 0) {
+    __shared__ float scratch[kFewWaves][64 * (kPer ? kPer : 1)];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    for (uint32_t token = wave; token < a.tokens; token += kFewWaves) {
+      int32_t id;
+      float weight;
+      wc_choose::choose<64, kPer>(route, token, scratch[wave], id, weight);
+      if (lane < a.k) {
+        c.ids[token][lane] = id;
+        c.weights[token][lane] = weight;
+      }
+      if (blockIdx.x + blockIdx.y == 0) wc_choose::store_choice<64>(route, token, id, weight);
+    }
+  } else {
+    load_choice(c, a);
+  }
+  __syncthreads();
+  list_experts(c, a);
+  if (blockIdx.y >= c.count) return;
+  const uint32_t e = c.list[blockIdx.y], r = threadIdx.x % 16, n0 = blockIdx.x * 32;
+  const uint32_t blocks = (a.hidden + 31) / 32;
+  Row w[4];
+#pragma unroll
+  for (uint32_t n = 0; n < 2; n++) {
+    const uint32_t row = min(n0 + 16 * n + r, a.ffn - 1);
+    w[n] = row_of(a.gate, e, row, blocks);
+    w[n + 2] = row_of(a.up, e, row, blocks);
+  }
+  const uint32_t mine = slot_of(c, a, r, e) >= 0 ? a.hidden : 0;
+  S::product(sh, w, blocks, [&](int, uint32_t super) {
+    return quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), super, mine);
+  });
+  if (threadIdx.x < 128) {
+    const uint32_t n = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const f32x4 g = S::sum(sh, threadIdx.x), u = S::sum(sh, 128 + threadIdx.x);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) {
+      const uint32_t column = 16 * n + lane / 16 * 4 + j;
+      h[lane % 16][column] = n0 + column < a.ffn ? silu(g[j]) * u[j] : 0.0f;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const uint32_t token = threadIdx.x / 4, all = (a.ffn + 31) / 32;
+    const int32_t slot = slot_of(c, a, token, e);
+    quantize_h(h[token], a.hq + (uint64_t(uint32_t(slot)) * all + blockIdx.x) * 16,
+               a.hs + uint64_t(uint32_t(slot)) * all + blockIdx.x, slot >= 0);
+  }
+}
+
+// 16 columns of y for all tokens: parts of 512 of every expert hit, spread over the waves.
+__global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_down_kernel(ExpertArgs a) {
+  __shared__ Chosen c;
+  __shared__ f32x4 part[kFewWaves][64];
+  load_choice(c, a);
+  __syncthreads();
+  list_experts(c, a);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, r = lane % 16;
+  const uint32_t blocks = (a.ffn + 31) / 32, supers = (blocks + kSuper - 1) / kSuper;
+  const uint32_t n0 = blockIdx.x * 16, all = c.count * supers;
+  const uint32_t last = uint32_t(uint64_t(all) * (wave + 1) / kFewWaves);
+  f32x4 y = {0, 0, 0, 0};
+  for (uint32_t u = uint32_t(uint64_t(all) * wave / kFewWaves); u < last;) {
+    const uint32_t at = u / supers, e = c.list[at], end = min(last, (at + 1) * supers);
+    const Row w = row_of(a.down, e, min(n0 + r, a.hidden - 1), blocks);
+    const int32_t slot = slot_of(c, a, r, e);
+    const Row x = {a.hq + uint64_t(max(slot, 0)) * blocks * 16, a.hs + uint64_t(max(slot, 0)) * blocks};
+    f32x4 acc = {0, 0, 0, 0};
+    for (; u < end; u++) {
+      const Part wp = load_part<false>(w, u - at * supers, blocks);
+      Part xp{};
+      if (slot >= 0) xp = load_part<true>(x, u - at * supers, blocks);
+      multiply(wp, xp, acc);
+    }
+    if (slot >= 0) {
+      float weight = 0.0f;
+      for (uint32_t j = 0; j < a.k; j++)
+        if (c.ids[r][j] == int32_t(e)) weight += c.weights[r][j];
+#pragma unroll
+      for (int i = 0; i < 4; i++) y[i] += weight * acc[i];
+    }
+  }
+  part[wave][lane] = y;
+  __syncthreads();
+  if (threadIdx.x >= 64 || r >= a.tokens) return;
+  f32x4 v = part[0][lane];
+#pragma unroll
+  for (int i = 1; i < kFewWaves; i++)
+#pragma unroll
+    for (int j = 0; j < 4; j++) v[j] += part[i][lane][j];
+  // slots without an expert: a NaN weight makes the token's results NaN
+  for (uint32_t j = 0; j < a.k; j++)
+    if (c.ids[r][j] < 0)
+#pragma unroll
+      for (int i = 0; i < 4; i++) v[i] += c.weights[r][j] * 0.0f;
+  const uint32_t n = n0 + lane / 16 * 4;
+  if (n < a.hidden) store_four(a.y, a.dtype, r * a.ldy + n, v, a.hidden - n);
+}
+
+// --- any number of tokens -----------------------------------------------------
+
+// The block-th block of places (Blocks).
+struct Place {
+  uint32_t expert, first, last;
+};
+__device__ __forceinline__ uint32_t block_count(const ExpertArgs& a) {
+  return __builtin_amdgcn_readfirstlane(*global<const uint32_t>(a.table));
+}
+__device__ __forceinline__ Place block_at(const ExpertArgs& a, uint32_t block) {
+  const u32x4 v = global<const u32x4>(a.table)[block + 1];
+  return {uint32_t(__builtin_amdgcn_readfirstlane(v[0])), uint32_t(__builtin_amdgcn_readfirstlane(v[1])),
+          uint32_t(__builtin_amdgcn_readfirstlane(v[2]))};
+}
+__device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place) {
+  return min(uint32_t(max(global<const int32_t>(a.order)[place], 0)), a.slots - 1);
+}
+
+// 32 columns of h for a block of 16 kM places, quantised.
+template <int kM>
+__global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a) {
+  using S = Slim<4, kM, 8>;
+  __shared__ typename S::Shared sh;
+  __shared__ float h[16 * kM][kRowH];
+  const uint32_t block = a.first + blockIdx.x;
+  if (block >= block_count(a)) return;
+  const auto [e, first, last] = block_at(a, block);
+  const uint32_t r = threadIdx.x % 16, n0 = blockIdx.y * 32, blocks = (a.hidden + 31) / 32;
+  Row w[4];
+#pragma unroll
+  for (uint32_t n = 0; n < 2; n++) {
+    const uint32_t row = min(n0 + 16 * n + r, a.ffn - 1);
+    w[n] = row_of(a.gate, e, row, blocks);
+    w[n + 2] = row_of(a.up, e, row, blocks);
+  }
+  Row x[kM];
+#pragma unroll
+  for (uint32_t m = 0; m < kM; m++) {
+    const uint64_t token = slot_at(a, min(first + 16 * m + r, last - 1)) / a.k;
+    x[m] = {a.xq + token * blocks * 16, a.xs + token * blocks};
+  }
+  S::product(sh, w, blocks, [&](int m, uint32_t super) { return load_part<true>(x[m], super, blocks); });
+  for (uint32_t i = threadIdx.x; i < 128 * kM; i += 512) {
+    const uint32_t tile = i / 64, lane = i % 64;
+    const f32x4 g = S::sum(sh, i), u = S::sum(sh, 128 * kM + i);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) {
+      const uint32_t column = tile / kM * 16 + lane / 16 * 4 + j;
+      h[tile % kM * 16 + lane % 16][column] = n0 + column < a.ffn ? silu(g[j]) * u[j] : 0.0f;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 64 * kM) {
+    const uint32_t row = threadIdx.x / 4, place = first + row, all = (a.ffn + 31) / 32;
+    quantize_h(h[row], a.hq + (uint64_t(place) * all + blockIdx.y) * 16, a.hs + uint64_t(place) * all + blockIdx.y,
+               place < last);
+  }
+}
+
+// down(h) of 32 columns for a block of places, stored by slot.
+template <int kM>
+__global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs a) {
+  using S = Slim<2, kM, 8>;
+  __shared__ typename S::Shared sh;
+  const uint32_t block = a.first + blockIdx.x;
+  if (block >= block_count(a)) return;
+  const auto [e, first, last] = block_at(a, block);
+  const uint32_t r = threadIdx.x % 16, n0 = blockIdx.y * 32, blocks = (a.ffn + 31) / 32;
+  Row w[2];
+#pragma unroll
+  for (uint32_t n = 0; n < 2; n++) w[n] = row_of(a.down, e, min(n0 + 16 * n + r, a.hidden - 1), blocks);
+  S::product(sh, w, blocks, [&](int m, uint32_t super) {
+    const uint64_t place = min(first + 16 * uint32_t(m) + r, last - 1);
+    return load_part<true>(Row{a.hq + place * blocks * 16, a.hs + place * blocks}, super, blocks);
+  });
+  for (uint32_t i = threadIdx.x; i < S::kPart; i += 512) {
+    const uint32_t tile = i / 64, lane = i % 64;
+    const uint32_t n = n0 + tile / kM * 16 + lane / 16 * 4, place = first + tile % kM * 16 + lane % 16;
+    if (place < last && n < a.hidden)
+      store_four(a.out, WC_FP32, uint64_t(slot_at(a, place)) * a.hidden + n, S::sum(sh, i), a.hidden - n);
+  }
+}
+
+// y of one token, four columns a thread: its slots' results in their order, times their weights.
+__global__ __launch_bounds__(256) void wc_experts_mx_join_kernel(ExpertArgs a) {
+  const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4;
+  const uint64_t token = a.first + blockIdx.x;
+  if (n >= a.hidden) return;
+  const uint32_t left = a.hidden - n;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint32_t j = 0; j < a.k; j++) {
+    const uint64_t slot = token * a.k + j;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (global<const int32_t>(a.ids)[slot] >= 0) {
+      const auto row = global<const float>(a.out) + slot * a.hidden + n;
+      if (a.hidden % 4 == 0)
+        v = *reinterpret_cast<global_ptr<const f32x4>>(row);
+      else
+#pragma unroll
+        for (uint32_t i = 0; i < 4; i++) v[i] = row[min(i, left - 1)];
+    }
+    const float w = global<const float>(a.weights)[slot];
+#pragma unroll
+    for (int i = 0; i < 4; i++) sum[i] += w * v[i];
+  }
+  store_four(a.y, a.dtype, token * a.ldy + n, sum, left);
+}
+
+// Blocks of `rows` places: every expert that has places ends in one that may not be full.
+uint64_t most_blocks(uint32_t slots, uint32_t experts, uint32_t rows) {
+  return uint64_t(slots) / rows + std::min(experts, slots);
+}
+struct Workspace {
+  uint64_t table, xq, xs, hq, hs, out, bytes;
+};
+Workspace layout(uint64_t tokens, uint64_t k, uint32_t experts, uint32_t hidden, uint32_t ffn) {
+  Workspace w{};
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t here = w.bytes;
+    w.bytes += pad256(bytes);
+    return here;
+  };
+  w.hq = take(tokens * k * WC_MX_ROW_BYTES(ffn));
+  w.hs = take(tokens * k * WC_MX_BLOCKS(ffn));
+  if (is_few(tokens, k)) return w;
+  w.table = take((1 + most_blocks(uint32_t(tokens * k), experts, 16)) * 16);
+  w.xq = take(tokens * WC_MX_ROW_BYTES(hidden));
+  w.xs = take(tokens * WC_MX_BLOCKS(hidden));
+  w.out = take(tokens * k * hidden * 4);
+  return w;
+}
+bool sizes_ok(uint32_t tokens, uint32_t k, uint32_t experts, uint32_t hidden, uint32_t ffn) {
+  return k >= 1 && experts >= 1 && experts <= kMaxExperts && k <= experts && hidden >= 1 &&
+         hidden <= kMaxK && ffn >= 1 && ffn <= kMaxK && uint64_t(tokens) * k < (1ull << 24);
+}
+bool bank_ok(const wc_mx_experts* b, uint64_t n, uint32_t k) {
+  return b && !off(b->w, 16) && b->scale && b->stride % 16 == 0 && b->stride >= n * WC_MX_ROW_BYTES(k) &&
+         b->scale_stride >= n * WC_MX_BLOCKS(k) && !(b->stride >> 40) && !(b->scale_stride >> 40);
+}
+Bank bank(const wc_mx_experts* b) {
+  return {reinterpret_cast<uint64_t>(b->w), reinterpret_cast<uint64_t>(b->scale), b->stride, b->scale_stride};
+}
+bool tensors_ok(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, uint32_t hidden, uint32_t ffn,
+                const wc_mx_experts* gate, const wc_mx_experts* up, const wc_mx_experts* down, const void* y,
+                uint64_t ldy) {
+  return float_ok(dtype) && ldx >= hidden && !(ldx >> 31) && ldy >= hidden && !(ldy >> 31) &&
+         bank_ok(gate, ffn, hidden) && bank_ok(up, ffn, hidden) && bank_ok(down, hidden, ffn) &&
+         (tokens == 0 || (!off(x, size_of(dtype)) && !off(y, size_of(dtype))));
+}
+ExpertArgs args_of(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, uint32_t k, uint32_t experts,
+                   uint32_t hidden, uint32_t ffn, const wc_mx_experts* gate, const wc_mx_experts* up,
+                   const wc_mx_experts* down, void* y, uint64_t ldy, const Workspace& w, uint64_t ws) {
+  ExpertArgs a{};
+  a.table = ws + w.table;
+  a.x = reinterpret_cast<uint64_t>(x);
+  a.ldx = ldx;
+  a.xq = ws + w.xq;
+  a.xs = ws + w.xs;
+  a.hq = ws + w.hq;
+  a.hs = ws + w.hs;
+  a.out = ws + w.out;
+  a.y = reinterpret_cast<uint64_t>(y);
+  a.ldy = ldy;
+  a.tokens = tokens;
+  a.k = k;
+  a.experts = experts;
+  a.hidden = hidden;
+  a.ffn = ffn;
+  a.slots = tokens * k;
+  a.dtype = dtype;
+  a.gate = bank(gate);
+  a.up = bank(up);
+  a.down = bank(down);
+  return a;
+}
+
+template <int kType>
+void start_up(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
+  const dim3 grid((a.ffn + 31) / 32, std::min(a.slots, a.experts)), block(64 * kFewWaves);
+  const RouteArgs r = route ? *route : RouteArgs{};
+  if (!route) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 0>), grid, block, 0, st, a, r);
+  else if (a.experts <= 64) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 1>), grid, block, 0, st, a, r);
+  else if (a.experts <= 128) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 2>), grid, block, 0, st, a, r);
+  else if (a.experts <= 256) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 4>), grid, block, 0, st, a, r);
+  else hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 8>), grid, block, 0, st, a, r);
+}
+// Up to kFew tokens, by `route` or the ids that a names.
+wc_status few(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
+  if (a.dtype == WC_BF16) start_up<WC_BF16>(a, route, st);
+  else if (a.dtype == WC_FP16) start_up<WC_FP16>(a, route, st);
+  else start_up<WC_FP32>(a, route, st);
+  if (hipGetLastError() != hipSuccess) return WC_EHIP;
+  hipLaunchKernelGGL(wc_moe_mx_down_kernel, dim3((a.hidden + 15) / 16), dim3(64 * kFewWaves), 0, st, a);
+  return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
+}
+
+template <int kM>
+bool start_slim(ExpertArgs a, uint32_t most, hipStream_t st) {
+  constexpr uint32_t kLaunch = 1u << 22;  // a grid's axis has less than 2^32 threads
+  for (a.first = 0; a.first < most; a.first += kLaunch) {
+    hipLaunchKernelGGL((wc_experts_mx_up_slim_kernel<kM>), dim3(std::min(most - a.first, kLaunch), (a.ffn + 31) / 32),
+                       dim3(512), 0, st, a);
+    if (hipGetLastError() != hipSuccess) return false;
+  }
+  for (a.first = 0; a.first < most; a.first += kLaunch) {
+    hipLaunchKernelGGL((wc_experts_mx_down_slim_kernel<kM>),
+                       dim3(std::min(most - a.first, kLaunch), (a.hidden + 31) / 32), dim3(512), 0, st, a);
+    if (hipGetLastError() != hipSuccess) return false;
+  }
+  return true;
+}
+
+wc_status experts(ExpertArgs a, const int32_t* offsets, hipStream_t st) {
+  if (is_few(a.tokens, a.k)) return few(a, nullptr, st);
+  const uint32_t rows = a.slots / a.experts <= 16 ? 16 : 32;
+  const uint32_t most = uint32_t(most_blocks(a.slots, a.experts, rows));
+  const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(offsets), a.experts, a.slots, rows, most};
+  if (!launch_quantize(reinterpret_cast<const void*>(a.x), a.dtype, a.tokens, a.hidden, a.ldx,
+                       reinterpret_cast<void*>(a.xq), WC_MX_ROW_BYTES(a.hidden), reinterpret_cast<void*>(a.xs),
+                       WC_MX_BLOCKS(a.hidden), st, &blocks))
+    return WC_EHIP;
+  if (!(rows == 16 ? start_slim<1>(a, most, st) : start_slim<2>(a, most, st))) return WC_EHIP;
+  hipLaunchKernelGGL(wc_experts_mx_join_kernel, dim3(a.tokens, (a.hidden + 1023) / 1024), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
+}
+
+// What wc_moe_mx keeps of the routing, before the rest.
+struct RouteSpace {
+  uint64_t ids, weights, offsets, order, scratch, scratch_bytes, bytes;
+};
+RouteSpace route_layout(uint32_t tokens, const wc_route_params* p) {
+  RouteSpace r{};
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t here = r.bytes;
+    r.bytes += pad256(bytes);
+    return here;
+  };
+  const uint64_t slots = uint64_t(tokens) * p->k;
+  r.ids = take(slots * 4);
+  r.weights = take(slots * 4);
+  if (is_few(tokens, p->k)) return r;
+  r.offsets = take((p->experts + 1) * 4);
+  r.order = take(slots * 4);
+  wc_route_workspace_bytes(tokens, p, &r.scratch_bytes);
+  r.scratch = take(r.scratch_bytes);
+  return r;
+}
+
+}  // namespace
+
+extern "C" wc_status wc_experts_mx_workspace_bytes(uint32_t tokens, uint32_t k, uint32_t experts,
+                                                   uint32_t hidden, uint32_t ffn, uint64_t* bytes) {
+  if (!bytes) return WC_EINVAL;
+  *bytes = 0;
+  if (!sizes_ok(tokens, k, experts, hidden, ffn)) return WC_EINVAL;
+  *bytes = layout(tokens, k, experts, hidden, ffn).bytes;
+  return WC_OK;
+}
+
+extern "C" wc_status wc_experts_mx(const void* dev_x, int32_t dtype, uint32_t tokens, uint64_t ldx, uint32_t k,
+                                   uint32_t n_experts, uint32_t hidden, uint32_t ffn, const int32_t* dev_ids,
+                                   const float* dev_weights, const int32_t* dev_offsets,
+                                   const int32_t* dev_order, const wc_mx_experts* gate, const wc_mx_experts* up,
+                                   const wc_mx_experts* down, void* dev_y, uint64_t ldy, void* dev_workspace,
+                                   uint64_t workspace_bytes, void* stream) {
+  if (!sizes_ok(tokens, k, n_experts, hidden, ffn) ||
+      !tensors_ok(dev_x, dtype, tokens, ldx, hidden, ffn, gate, up, down, dev_y, ldy))
+    return WC_EINVAL;
+  if (tokens == 0) return WC_OK;
+  if (off(dev_ids, 4) || off(dev_weights, 4) || off(dev_offsets, 4) || off(dev_order, 4)) return WC_EINVAL;
+  const Workspace w = layout(tokens, k, n_experts, hidden, ffn);
+  if (off(dev_workspace, 256) || workspace_bytes < w.bytes) return WC_EINVAL;
+  ExpertArgs a = args_of(dev_x, dtype, tokens, ldx, k, n_experts, hidden, ffn, gate, up, down, dev_y, ldy, w,
+                         reinterpret_cast<uint64_t>(dev_workspace));
+  a.order = reinterpret_cast<uint64_t>(dev_order);
+  a.ids = reinterpret_cast<uint64_t>(dev_ids);
+  a.weights = reinterpret_cast<uint64_t>(dev_weights);
+  return experts(a, dev_offsets, reinterpret_cast<hipStream_t>(stream));
+}
+
+extern "C" wc_status wc_moe_mx_workspace_bytes(uint32_t tokens, const wc_route_params* p, uint32_t hidden,
+                                               uint32_t ffn, uint64_t* bytes) {
+  if (!bytes) return WC_EINVAL;
+  *bytes = 0;
+  if (!wc_choose::params_ok(tokens, p) || !sizes_ok(tokens, p->k, p->experts, hidden, ffn)) return WC_EINVAL;
+  *bytes = route_layout(tokens, p).bytes + layout(tokens, p->k, p->experts, hidden, ffn).bytes;
+  return WC_OK;
+}
+
+extern "C" wc_status wc_moe_mx(const void* dev_x, int32_t dtype, uint32_t tokens, uint64_t ldx,
+                               const void* dev_logits, int32_t logits_dtype, uint64_t ld,
+                               const wc_route_params* p, const float* dev_bias, uint32_t hidden, uint32_t ffn,
+                               const wc_mx_experts* gate, const wc_mx_experts* up, const wc_mx_experts* down,
+                               void* dev_y, uint64_t ldy, void* dev_workspace, uint64_t workspace_bytes,
+                               void* stream) {
+  uint64_t need = 0;
+  if (wc_moe_mx_workspace_bytes(tokens, p, hidden, ffn, &need) != WC_OK ||
+      !tensors_ok(dev_x, dtype, tokens, ldx, hidden, ffn, gate, up, down, dev_y, ldy) ||
+      !float_ok(logits_dtype) || ld < p->experts || ld >> 31 || (dev_bias && off(dev_bias, 4)))
+    return WC_EINVAL;
+  if (tokens == 0) return WC_OK;
+  if (off(dev_logits, size_of(logits_dtype)) || off(dev_workspace, 256) || workspace_bytes < need) return WC_EINVAL;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const uint64_t ws = reinterpret_cast<uint64_t>(dev_workspace);
+  const RouteSpace r = route_layout(tokens, p);
+  ExpertArgs a = args_of(dev_x, dtype, tokens, ldx, p->k, p->experts, hidden, ffn, gate, up, down, dev_y, ldy,
+                         layout(tokens, p->k, p->experts, hidden, ffn), ws + r.bytes);
+  a.ids = ws + r.ids;
+  a.weights = ws + r.weights;
+  if (is_few(tokens, p->k)) {
+    const RouteArgs route = {reinterpret_cast<uint64_t>(dev_logits), reinterpret_cast<uint64_t>(dev_bias),
+                             a.ids, a.weights, ld, tokens, p->experts, p->k, p->groups, p->top_groups,
+                             p->group_top, 0, logits_dtype, p->score, p->renormalize, p->scale};
+    return few(a, &route, st);
+  }
+  a.order = ws + r.order;
+  const wc_status s = wc_route(dev_logits, logits_dtype, tokens, ld, p, dev_bias,
+                               reinterpret_cast<int32_t*>(a.ids), reinterpret_cast<float*>(a.weights),
+                               reinterpret_cast<int32_t*>(ws + r.offsets), reinterpret_cast<int32_t*>(a.order),
+                               reinterpret_cast<void*>(ws + r.scratch), r.scratch_bytes, stream);
+  return s == WC_OK ? experts(a, reinterpret_cast<const int32_t*>(ws + r.offsets), st) : s;
+}

@@ -32,7 +32,9 @@ __global__ __launch_bounds__(64 * kTokenWaves) void wc_route_choose_kernel(Route
   const uint32_t t = threadIdx.x / kLanes;
   int32_t id;
   float weight;
-  choose<kLanes, kPer>(a, a.first + blockIdx.x * kTokens + t, scratch[t], id, weight);
+  const uint32_t token = a.first + blockIdx.x * kTokens + t;
+  choose<kLanes, kPer>(a, token, scratch[t], id, weight);
+  store_choice<kLanes>(a, token, id, weight);
 }
 
 struct SortArgs {
@@ -209,6 +211,7 @@ __global__ __launch_bounds__(kSortThreads) void wc_route_small_kernel(RouteArgs 
     int32_t id;
     float weight;
     choose<kLanes, kPer>(a, first + t, scratch[t], id, weight);
+    store_choice<kLanes>(a, first + t, id, weight);
     if (first + t < a.tokens && lane < a.k)
       classes[(first + t) * a.k + lane] = uint16_t(id < 0 ? int32_t(a.experts) : id);
   }

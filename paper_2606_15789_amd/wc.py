@@ -32,7 +32,10 @@ EXPORTS = ["wc_analyze", "wc_encode", "wc_open", "wc_decode", "wc_gemv", "wc_fre
            "wc_stream", "wc_analyze_device_static", "wc_quantize_i8",
            "wc_matmul_i8_workspace_bytes", "wc_matmul_i8", "wc_linear_i8_workspace_bytes",
            "wc_linear_i8", "wc_route_workspace_bytes", "wc_route",
-           "wc_experts_i8_workspace_bytes", "wc_experts_i8"]
+           "wc_experts_i8_workspace_bytes", "wc_experts_i8", "wc_quantize_mx", "wc_dequantize_mx",
+           "wc_matmul_mx_workspace_bytes", "wc_matmul_mx", "wc_linear_mx_workspace_bytes",
+           "wc_linear_mx", "wc_experts_mx_workspace_bytes", "wc_experts_mx",
+           "wc_moe_mx_workspace_bytes", "wc_moe_mx"]
 
 ANALYZE_WORKSPACE_BYTES = 524288  # WC_ANALYZE_WORKSPACE_BYTES
 
@@ -89,6 +92,17 @@ class _RouteParams(C.Structure):
 class _I8Experts(C.Structure):
     _fields_ = [("w", C.c_void_p), ("scale", C.c_void_p), ("stride", C.c_uint64),
                 ("scale_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _MxJob(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("scale", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p),
+                ("ldw", C.c_uint64), ("lds", C.c_uint64), ("ldy", C.c_uint64), ("n", C.c_uint32),
+                ("bias_dtype", C.c_int32), ("y_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _MxExperts(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("scale", C.c_void_p), ("stride", C.c_uint64),
+                ("scale_stride", C.c_uint64)]
 
 
 _lib = None
@@ -171,6 +185,21 @@ def lib():
         L.wc_experts_i8.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint64] \
             + [C.c_uint32] * 4 + [C.c_void_p] * 4 + [experts] * 3 \
             + [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]
+        ptr, u32, u64, i32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32
+        bank = C.POINTER(_MxExperts)
+        L.wc_quantize_mx.argtypes = [ptr, i32, u32, u32, u64, ptr, u64, ptr, u64, ptr]
+        L.wc_dequantize_mx.argtypes = [ptr, u64, ptr, u64, u32, u32, ptr, i32, u64, ptr]
+        L.wc_matmul_mx_workspace_bytes.argtypes = L.wc_matmul_i8_workspace_bytes.argtypes
+        L.wc_matmul_mx.argtypes = [ptr, u64, ptr, u64, u32, u32, u32, job, ptr, u64, ptr]
+        L.wc_linear_mx_workspace_bytes.argtypes = L.wc_matmul_i8_workspace_bytes.argtypes
+        L.wc_linear_mx.argtypes = L.wc_linear_i8.argtypes
+        L.wc_experts_mx_workspace_bytes.argtypes = L.wc_experts_i8_workspace_bytes.argtypes
+        L.wc_experts_mx.argtypes = [ptr, i32, u32, u64] + [u32] * 4 + [ptr] * 4 + [bank] * 3 \
+            + [ptr, u64, ptr, u64, ptr]
+        L.wc_moe_mx_workspace_bytes.argtypes = [u32, C.POINTER(_RouteParams), u32, u32,
+                                                C.POINTER(u64)]
+        L.wc_moe_mx.argtypes = [ptr, i32, u32, u64, ptr, i32, u64, C.POINTER(_RouteParams), ptr,
+                                u32, u32] + [bank] * 3 + [ptr, u64, ptr, u64, ptr]
         for name in EXPORTS[EXPORTS.index("wc_quantize_i8"):]:
             getattr(L, name).restype = C.c_int
         L.wc_free.argtypes = [C.POINTER(_Blob)]
@@ -1031,4 +1060,283 @@ def experts_i8_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
                                  y.data_ptr(), ldy, _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_experts_i8", rc)
+    return y
+
+
+# --- microscaled 4-bit layers ---------------------------------------------------
+# The layers of a decoded MXFP4 checkpoint.  Codes are packed two to a byte in rows of whole
+# blocks (uint8, or torch's 4-bit type; mx_row_bytes(k) columns), scales one byte a block (uint8,
+# or torch's e8m0 type; mx_blocks(k) columns).
+
+_bytes_of_codes, _bytes_of_scales = (), ()
+
+
+def mx_blocks(k: int) -> int:
+    """WC_MX_BLOCKS: blocks of 32 of a row of k elements."""
+    return (k + 31) // 32
+
+
+def mx_row_bytes(k: int) -> int:
+    """WC_MX_ROW_BYTES: bytes of the codes of a row of k elements."""
+    return (k + 31) // 32 * 16
+
+
+def _mx_types():
+    global _bytes_of_codes, _bytes_of_scales
+    if not _bytes_of_codes:
+        import torch
+        named = [getattr(torch, n, torch.uint8) for n in ("float4_e2m1fn_x2", "float8_e8m0fnu")]
+        _bytes_of_codes = (torch.uint8, torch.int8, named[0])
+        _bytes_of_scales = (torch.uint8, named[1])
+    return _bytes_of_codes, _bytes_of_scales
+
+
+def _mx_rows(w, scale, k: int, what: str, dev: int):
+    """(n, row strides in bytes of codes and scales) of a 2-D MXFP4 matrix of k columns."""
+    codes, bytes_ = _mx_types()
+    if w.dtype not in codes:
+        raise ValueError(f"{what} must be packed 4-bit codes in bytes")
+    if scale.dtype not in bytes_:
+        raise ValueError(f"the scales of {what} must be e8m0 bytes")
+    ldw = _rows(w, what, dev, mx_row_bytes(k))
+    lds = _rows(scale, f"the scales of {what}", dev, mx_blocks(k))
+    n = w.shape[0]
+    if scale.shape[0] != n:
+        raise ValueError(f"{what} has {n} rows, its scales {scale.shape[0]}")
+    return n, ldw, lds
+
+
+def quantize_mx_torch(x, q=None, scale=None, stream=None):
+    """wc_quantize_mx of a 2-D tensor of m x k: (q, scale), q uint8 of m x mx_row_bytes(k)
+    (zero past column k), scale uint8 of m x mx_blocks(k)."""
+    import torch
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
+    dt = _float_type(x, "x")
+    m, k = x.shape
+    if (m | k) >> 32:
+        raise WcError("wc_quantize_mx", _EINVAL)
+    st, where = _stream_of(stream, x.device)
+    with where:
+        if q is None:
+            q = x.new_empty((m, mx_row_bytes(k)), dtype=torch.uint8)
+        if scale is None:
+            scale = x.new_empty((m, mx_blocks(k)), dtype=torch.uint8)
+        n, ldq, lds = _mx_rows(q, scale, k, "q", dev)
+        if n != m:
+            raise ValueError(f"q must have {m} rows")
+        rc = lib().wc_quantize_mx(x.data_ptr(), dt, m, k, ld, q.data_ptr(), ldq, scale.data_ptr(),
+                                  lds, st)
+    if rc:
+        raise WcError("wc_quantize_mx", rc)
+    return q, scale
+
+
+def dequantize_mx_torch(q, scale, k: int, y=None, dtype=None, stream=None):
+    """wc_dequantize_mx: the values of MXFP4 rows of k columns, in y or a new tensor of `dtype`
+    (bfloat16 if None)."""
+    import torch
+    dev = q.get_device()
+    m, ldq, lds = _mx_rows(q, scale, k, "q", dev)
+    if (m | k) >> 32:
+        raise WcError("wc_dequantize_mx", _EINVAL)
+    st, where = _stream_of(stream, q.device)
+    with where:
+        if y is None:
+            y = torch.empty((m, k), dtype=dtype or torch.bfloat16, device=q.device)
+        if tuple(y.shape) != (m, k):
+            raise ValueError(f"y must be {m} x {k}")
+        ldy = _rows(y, "y", dev)
+        rc = lib().wc_dequantize_mx(q.data_ptr(), ldq, scale.data_ptr(), lds, m, k, y.data_ptr(),
+                                    _float_type(y, "y"), ldy, st)
+    if rc:
+        raise WcError("wc_dequantize_mx", rc)
+    return y
+
+
+_MX_JOB = struct.Struct("=7QI3i")  # wc_mx_job
+
+
+def _mx_jobs(m: int, k: int, ws, scales, biases, ys, dtype, dev: int):
+    """The wc_mx_job array, packed, and the ys (allocated where None)."""
+    n_jobs = len(ws)
+    if len(scales) != n_jobs or (biases is not None and len(biases) != n_jobs) or \
+            (ys is not None and len(ys) != n_jobs):
+        raise ValueError("one scale tensor, bias entry and y a matrix")
+    floats = _types()
+    jobs, out = [], []
+    yt = floats.get(dtype)
+    for i in range(n_jobs):
+        w, s = ws[i], scales[i]
+        n, ldw, lds = _mx_rows(w, s, k, "w", dev)
+        b = None if biases is None else biases[i]
+        bp, bt = (0, 0) if b is None else (b.data_ptr(), _vector(b, n, "a bias", dev))
+        if ys is None:
+            if yt is None:
+                raise ValueError("y must be bfloat16, float16 or float32")
+            y, ldy = w.new_empty((m, n), dtype=dtype), n
+        else:
+            y = ys[i]
+            if y.shape != (m, n):
+                raise ValueError(f"y must be {m} x {n}")
+            ldy = _rows(y, "y", dev)
+            yt = _float_type(y, "y")
+        out.append(y)
+        if n >> 32:
+            raise WcError("wc_matmul_mx", _EINVAL)
+        jobs.append(_MX_JOB.pack(w.data_ptr(), s.data_ptr(), bp, y.data_ptr(), ldw, lds, ldy, n, bt,
+                                 yt, 0))
+    return b"".join(jobs), out
+
+
+def matmul_mx_torch(q, scale, k: int, ws, scales, biases=None, ys=None, dtype=None,
+                    workspace=None, stream=None):
+    """wc_matmul_mx: x @ W_i^T + biases_i for MXFP4 x (q, scale: from quantize_mx_torch) and
+    each MXFP4 W_i (n_i x mx_row_bytes(k)) of `ws`.  ys (of any float type, rows contiguous) are
+    allocated in `dtype` (bfloat16 if None) where None."""
+    import torch
+    dev = q.get_device()
+    m, ldq, lds = _mx_rows(q, scale, k, "q", dev)
+    if (m | k) >> 32:
+        raise WcError("wc_matmul_mx", _EINVAL)
+    st, where = _stream_of(stream, q.device)
+    need = C.c_uint64(0)
+    with where:
+        jobs, ys = _mx_jobs(m, k, ws, scales, biases, ys, dtype or torch.bfloat16, dev)
+        rc = lib().wc_matmul_mx_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
+        if not rc:
+            workspace = _workspace(workspace, need.value, q.device)
+            rc = lib().wc_matmul_mx(q.data_ptr(), ldq, scale.data_ptr(), lds, m, k, len(ws), jobs,
+                                    _ptr(workspace), _size(workspace), st)
+    if rc:
+        raise WcError("wc_matmul_mx", rc)
+    return ys
+
+
+def linear_mx_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=None,
+                    stream=None):
+    """wc_linear_mx: x brought to MXFP4, then as matmul_mx_torch; `dtype` defaults to x's type."""
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
+    dt = _float_type(x, "x")
+    m, k = x.shape
+    if (m | k) >> 32:
+        raise WcError("wc_linear_mx", _EINVAL)
+    st, where = _stream_of(stream, x.device)
+    need = C.c_uint64(0)
+    with where:
+        jobs, ys = _mx_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, dev)
+        # few rows need no workspace
+        rc = 0 if m <= 16 and workspace is None else \
+            lib().wc_linear_mx_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
+        if not rc:
+            workspace = _workspace(workspace, need.value, x.device)
+            rc = lib().wc_linear_mx(x.data_ptr(), dt, m, k, ld, len(ws), jobs, _ptr(workspace),
+                                    _size(workspace), st)
+    if rc:
+        raise WcError("wc_linear_mx", rc)
+    return ys
+
+
+def _mx_bank(w, scale, experts: int, n: int, k: int, what: str, dev: int):
+    codes, bytes_ = _mx_types()
+    if w.dtype not in codes or scale.dtype not in bytes_:
+        raise ValueError(f"{what} must be packed 4-bit codes in bytes, its scales e8m0 bytes")
+    strides = []
+    for t, cols, name in ((w, mx_row_bytes(k), what), (scale, mx_blocks(k), f"the scales of {what}")):
+        stride = t.stride()
+        if t.shape != (experts, n, cols) or t.get_device() != dev or (cols > 1 and stride[2] != 1) or \
+                (n > 1 and stride[1] != cols):
+            raise ValueError(f"{name} must be {experts} x {n} x {cols} bytes on device {dev}, contiguous "
+                             "in each expert")
+        strides.append(stride[0] if experts > 1 else n * cols)
+    return _MxExperts(w.data_ptr(), scale.data_ptr(), *strides)
+
+
+def _mx_banks(x, gate, gate_scale, up, up_scale, down, down_scale, dev: int):
+    """(experts, ffn, the three banks) of a mixture layer."""
+    if gate.dim() != 3:
+        raise ValueError("gate must be experts x ffn x mx_row_bytes(hidden)")
+    hidden = x.shape[1]
+    experts, ffn = gate.shape[:2]
+    return experts, ffn, (_mx_bank(gate, gate_scale, experts, ffn, hidden, "gate", dev),
+                          _mx_bank(up, up_scale, experts, ffn, hidden, "up", dev),
+                          _mx_bank(down, down_scale, experts, hidden, ffn, "down", dev))
+
+
+def _mx_result(y, x, dev: int):
+    if y is None:
+        y = x.new_empty(x.shape)
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("y must be of x's shape and type")
+    return y, _rows(y, "y", dev)
+
+
+def experts_mx_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, down_scale,
+                     y=None, workspace=None, stream=None):
+    """wc_experts_mx: the feed-forward of a mixture layer.  x tokens x hidden; gate, up MXFP4 of
+    experts x ffn rows of hidden, down of experts x hidden rows of ffn (codes experts x rows x
+    mx_row_bytes, scales experts x rows x mx_blocks); y of x's type."""
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
+    dt = _float_type(x, "x")
+    tokens, hidden = x.shape
+    if routing.ids.dim() != 2:
+        raise ValueError("the ids must be tokens x k")
+    k = routing.ids.shape[1]
+    experts, ffn, banks = _mx_banks(x, gate, gate_scale, up, up_scale, down, down_scale, dev)
+    if (tokens | k | experts | hidden | ffn) >> 32:
+        raise WcError("wc_experts_mx", _EINVAL)
+    _check_routing(routing, tokens, k, experts, dev)
+    st, where = _stream_of(stream, x.device)
+    need = C.c_uint64(0)
+    rc = lib().wc_experts_mx_workspace_bytes(tokens, k, experts, hidden, ffn, C.byref(need))
+    if rc:
+        raise WcError("wc_experts_mx", rc)
+    with where:
+        y, ldy = _mx_result(y, x, dev)
+        workspace = _workspace(workspace, need.value, x.device)
+        rc = lib().wc_experts_mx(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
+                                 *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
+                                 y.data_ptr(), ldy, _ptr(workspace), _size(workspace), st)
+    if rc:
+        raise WcError("wc_experts_mx", rc)
+    return y
+
+
+def moe_mx_torch(x, logits, k: int, gate, gate_scale, up, up_scale, down, down_scale,
+                 score: str = "softmax", bias=None, groups: int = 1, top_groups: int = 1,
+                 group_top: int = 1, renormalize: bool = True, scale: float = 1.0, y=None,
+                 workspace=None, stream=None):
+    """wc_moe_mx: route_torch of the logits (tokens x experts) and experts_mx_torch in one call."""
+    dev = x.get_device()
+    ld = _rows(x, "x", dev)
+    dt = _float_type(x, "x")
+    tokens, hidden = x.shape
+    experts, ffn, banks = _mx_banks(x, gate, gate_scale, up, up_scale, down, down_scale, dev)
+    ldl = _rows(logits, "logits", dev, experts)
+    lt = _float_type(logits, "logits")
+    if logits.shape[0] != tokens:
+        raise ValueError(f"logits must be {tokens} x {experts}")
+    if score not in SCORES:
+        raise ValueError(f"score must be one of {sorted(SCORES)}")
+    if bias is not None and _vector(bias, experts, "bias", dev) != _FP32:
+        raise ValueError("bias must be float32")
+    if (tokens | experts | hidden | ffn | k | groups | top_groups | group_top) >> 32:
+        raise WcError("wc_moe_mx", _EINVAL)
+    st, where = _stream_of(stream, x.device)
+    params = _RouteParams(experts, k, SCORES[score], int(renormalize), groups, top_groups,
+                          group_top, scale)
+    need = C.c_uint64(0)
+    rc = lib().wc_moe_mx_workspace_bytes(tokens, C.byref(params), hidden, ffn, C.byref(need))
+    if rc:
+        raise WcError("wc_moe_mx", rc)
+    with where:
+        y, ldy = _mx_result(y, x, dev)
+        workspace = _workspace(workspace, need.value, x.device)
+        rc = lib().wc_moe_mx(x.data_ptr(), dt, tokens, ld, logits.data_ptr(), lt, ldl,
+                             C.byref(params), _ptr(bias), hidden, ffn, *(C.byref(b) for b in banks),
+                             y.data_ptr(), ldy, _ptr(workspace), _size(workspace), st)
+    if rc:
+        raise WcError("wc_moe_mx", rc)
     return y
