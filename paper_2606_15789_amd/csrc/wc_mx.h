@@ -250,10 +250,19 @@ __device__ __forceinline__ void store_four(uint64_t p, int32_t dt, uint64_t i, f
 }
 
 // Quantise m rows of k elements of type dt to rows of `ldq` bytes of codes and `lds` of scales
-// (wc_mx.hip); with `blocks`, one more workgroup writes its table.  False on a launch error.
+// (wc_mx.hip), of which the first `scale_blocks` are written: zeros past the row's blocks.  With
+// `blocks`, one more workgroup writes its table.  False on a launch error.
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     uint64_t ldq, void* scale, uint64_t lds, hipStream_t stream,
+                     uint64_t ldq, void* scale, uint64_t lds, uint32_t scale_blocks, hipStream_t stream,
                      const Blocks* blocks = nullptr);
+
+// Scales for the tiles, which load them as whole words: rows of them at any address copied to rows
+// of scale_pitch(k) bytes, zeros past a row's blocks.  False on a launch error.
+inline uint32_t scale_pitch(uint32_t k) { return (blocks_of(k) + 3) / 4 * 4; }
+inline bool whole_words(const void* scale, uint64_t pitch, uint32_t k) {
+  return reinterpret_cast<uintptr_t>(scale) % 4 == 0 && pitch % 4 == 0 && blocks_of(k) % 4 == 0;
+}
+bool launch_copy_scales(const void* scale, uint64_t pitch, uint32_t rows, uint32_t k, void* to, hipStream_t stream);
 
 inline bool off(const void* p, uint32_t to) { return !p || reinterpret_cast<uintptr_t>(p) % to != 0; }
 

@@ -1,8 +1,9 @@
 // wc_mx.hip -- microscaled 4-bit (MXFP4) linear layers: wc_quantize_mx, wc_dequantize_mx,
 // wc_matmul_mx, wc_linear_mx.
 #include <algorithm>
+#include <cmath>
 
-#include "wc_mx.h"
+#include "wc_mx_tile.h"
 
 namespace {
 
@@ -13,7 +14,7 @@ constexpr uint32_t kLaunchRows = 1u << 23;  // a grid's axis has less than 2^32 
 
 struct QuantArgs {
   uint64_t x, ldx, q, ldq, scale, lds;
-  uint32_t m, k, each, groups;  // rows to a workgroup; workgroups of rows
+  uint32_t m, k, scale_blocks, each, groups;  // rows to a workgroup; workgroups of rows
   Blocks blocks;
 };
 
@@ -26,7 +27,7 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_mx_kernel(QuantArgs a) {
     if (blockIdx.y == 0) write_blocks<kThreads>(a.blocks, starts);
     return;
   }
-  const uint32_t units = (a.k + 31) / 32 * 4;
+  const uint32_t units = a.scale_blocks * 4;
   uint32_t row = blockIdx.x, unit = blockIdx.y * kThreads + threadIdx.x;
   if (a.each > 1) {
     row = blockIdx.x * a.each + threadIdx.x / units;
@@ -40,7 +41,8 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_mx_kernel(QuantArgs a) {
   top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xF, 0xF, false)));  // lane ^ 2
   if (!live) return;
   const uint32_t byte = scale_byte(top);
-  global<uint32_t>(a.q + row * a.ldq)[unit] = byte == 255 ? 0u : e.codes(scale_value(byte));
+  if (unit < (a.k + 31) / 32 * 4)
+    global<uint32_t>(a.q + row * a.ldq)[unit] = byte == 255 ? 0u : e.codes(scale_value(byte));
   if (unit % 4 == 0) global<uint8_t>(a.scale + row * a.lds)[unit / 4] = uint8_t(byte);
 }
 
@@ -89,14 +91,30 @@ __global__ __launch_bounds__(kThreads) void wc_dequantize_mx_kernel(DequantArgs 
   if (left > 4) store_four(a.y, kType, at + 4, v[1], left - 4);
 }
 
+// Scales to rows of whole words.
+__global__ __launch_bounds__(kThreads) void wc_copy_scales_mx_kernel(uint64_t from, uint64_t pitch, uint64_t to,
+                                                                     uint32_t rows, uint32_t blocks) {
+  const uint64_t row = blockIdx.x * 4 + threadIdx.x / 64;
+  const uint32_t words = (blocks + 3) / 4, word = blockIdx.y * 64 + threadIdx.x % 64;
+  if (row >= rows || word >= words) return;
+  const auto p = global<const uint8_t>(from + row * pitch + word * 4);
+  uint32_t v = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++)
+    if (word * 4 + i < blocks) v |= uint32_t(p[i]) << (8 * i);
+  global<uint32_t>(to)[row * words + word] = v;
+}
+
 struct MatJob {
   uint64_t w, scale, bias, y, ldw, lds, ldy;
+  uint64_t part;  // sums of the parts of k, in fp32: parts x m x n (to whole fours)
   uint32_t n, first;  // its first tile
   int32_t bias_dtype, y_dtype;
 };
 struct MatArgs {
   uint64_t x, ldx, xs, ldxs;  // rows of codes and scales, or of elements (ldx in bytes)
   uint32_t m, k, n_jobs;
+  uint32_t splits;  // parts of k
   MatJob job[kMaxJobs];
 };
 __device__ __forceinline__ uint32_t job_of(const MatArgs& a, uint32_t tile) {
@@ -142,6 +160,89 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
   }
 }
 
+// A tile of y, or of its sums over one part of k (blockIdx.y).
+template <class T>
+__global__ __launch_bounds__(T::kThreads) void wc_matmul_mx_tile_kernel(MatArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+  constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
+  const MatJob& J = a.job[job_of(a, blockIdx.x)];
+  uint32_t mt, nt;
+  if (!tile_at(blockIdx.x - J.first, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt)) return;
+  const uint32_t m0 = mt * kBM, n0 = nt * kBN, m_rows = min(kBM, a.m - m0), n_rows = min(kBN, J.n - n0);
+  const uint32_t blocks = (a.k + 31) / 32, words = (blocks + 3) / 4;
+  const uint32_t all = (blocks + kStageBlocks - 1) / kStageBlocks, each = (all + a.splits - 1) / a.splits;
+  const uint32_t first = blockIdx.y * each, stages = first < all ? min(each, all - first) : 0;
+  const uint32_t ldx = uint32_t(a.ldx), ldxs = uint32_t(a.ldxs), ldw = uint32_t(J.ldw), ldws = uint32_t(J.lds);
+  const RowsOf X = rows_of(a.x + m0 * a.ldx, ldx, a.xs + m0 * a.ldxs, ldxs, m_rows, blocks);
+  const RowsOf W = rows_of(J.w + n0 * J.ldw, ldw, J.scale + n0 * J.lds, ldws, n_rows, blocks);
+  const uint32_t chunk = T::chunk_of(), half = threadIdx.x % 2;
+  const uint32_t xoff = T::row_of(0) * ldx + chunk * 16, woff = T::row_of(0) * ldw + chunk * 16;
+  const uint32_t xsoff = T::scale_row() * ldxs + half * 4, wsoff = T::scale_row() * ldws + half * 4;
+  f32x16 acc[T::kMT][T::kNT];
+  // rows past the tile's last are past the buffers' ends
+  T::product(
+      lds, stages, m_rows,
+      [&](int i, uint32_t s, uint32_t to) {
+        s += first;
+        load_lds(X.codes, to, (s * kStageBlocks + chunk < blocks ? xoff : kNowhere) + (i * T::kStep * ldx + s * kStage));
+      },
+      [&](int i, uint32_t s, uint32_t to) { load_lds(W.codes, to, woff + (i * T::kStep * ldw + (s + first) * kStage)); },
+      [&](int i, uint32_t s, uint32_t to) {
+        s += first;
+        const bool in = s * 2 + half < words;
+        if (i < T::kXScales)
+          load_lds_words(X.scales, to, (in ? xsoff : kNowhere) + (i * T::kScaleStep * ldxs + s * 8));
+        else
+          load_lds_words(W.scales, to, (in ? wsoff : kNowhere) + ((i - T::kXScales) * T::kScaleStep * ldws + s * 8));
+      },
+      acc);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t wm0 = wave / T::kWN_ * (T::kMT * 32), wn0 = wave % T::kWN_ * (T::kNT * 32);
+  const uint32_t pitch = (J.n + 3) & ~3u;
+  const uint32_t n = n0 + wn0 + threadIdx.x % (T::kNT * 8) * 4;  // of all this lane's stores
+  f32x4 bias = {0, 0, 0, 0};
+  if (J.bias && a.splits == 1)
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) bias[j] = load_float(J.bias, J.bias_dtype, min(n + j, J.n - 1));
+#pragma unroll
+  for (int mb = 0; mb < T::kMT; mb++)
+    T::rows_out(
+        lds, [&](int c, int i) { return acc[mb][c][i]; },
+        [&](uint32_t row, uint32_t, f32x4 v) {
+          const uint32_t m = m0 + wm0 + mb * 32 + row;
+          if (m >= a.m || n >= J.n) return;
+          if (a.splits > 1) {
+            *global<f32x4>(J.part + ((uint64_t(blockIdx.y) * a.m + m) * pitch + n) * 4) = v;
+            return;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; j++) v[j] += bias[j];
+          store_four(J.y, J.y_dtype, m * J.ldy + n, v, J.n - n);
+        });
+}
+
+// y from the sums of the parts of k, in their order.
+__global__ __launch_bounds__(256) void wc_matmul_mx_join_kernel(MatArgs a) {
+  const MatJob& J = a.job[blockIdx.z];
+  const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4, pitch = (J.n + 3) & ~3u;
+  if (n >= J.n) return;
+  f32x4 bias = {0, 0, 0, 0};
+  if (J.bias)
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) bias[j] = load_float(J.bias, J.bias_dtype, min(n + j, J.n - 1));
+  for (uint64_t m = blockIdx.x; m < a.m; m += gridDim.x) {
+    f32x4 v = *global<f32x4>(J.part + (m * pitch + n) * 4);
+    for (uint32_t s = 1; s < a.splits; s++) {
+      const f32x4 p = *global<f32x4>(J.part + ((uint64_t(s) * a.m + m) * pitch + n) * 4);
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] += p[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) v[j] += bias[j];
+    store_four(J.y, J.y_dtype, m * J.ldy + n, v, J.n - n);
+  }
+}
+
 bool rows_ok(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ld) {
   return float_ok(dt) && k >= 1 && k <= kMaxK && !(m >> 31) && ld >= k && !(ld >> 31) &&
          (m == 0 || !off(x, size_of(dt)));
@@ -165,14 +266,58 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   return !(rows >> 27);
 }
 
-// What a call does, by the sizes alone.
+enum class Kernel { kSlim, kTile64, kTile128, kTile256 };
+using Tile64 = MxTile<64, 64, 1, 2, 4>;
+using Tile128 = MxTile<128, 128, 2, 2, 2>;
+using Tile256 = MxTile<256, 256, 2, 4, 2>;
+template <class F>
+void with_tile(Kernel k, F f) {
+  switch (k) {
+    case Kernel::kTile64: return f(Tile64{});
+    case Kernel::kTile128: return f(Tile128{});
+    case Kernel::kTile256: return f(Tile256{});
+    default: return;
+  }
+}
+uint32_t tiles_of(Kernel k, uint32_t m, uint32_t n) {
+  uint32_t tiles = (n + 31) / 32;
+  with_tile(k, [&](auto t) { tiles = (m + t.kRows - 1) / t.kRows * ((n + t.kCols - 1) / t.kCols); });
+  return tiles;
+}
+
+// What a call does, by the sizes and alignments alone.
 struct Plan {
+  Kernel kernel;
   bool inside;        // the product's kernel quantises x itself
-  uint64_t parts;     // bytes of the workspace, without the quantised x
+  uint32_t splits;    // parts of k
+  uint64_t parts;     // bytes of their sums
+  uint64_t scales;    // bytes of copies of scales
 };
-Plan plan_of(uint32_t m, uint32_t, uint32_t, const wc_mx_job*) { return {m <= 16, 0}; }
+Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
+  Plan p{Kernel::kSlim, m <= 16, 1, 0, 0};
+  if (m <= 64) return p;
+  bool narrow = m < (1u << 24);
+  uint64_t rows = 0;
+  for (uint32_t i = 0; i < n_jobs; i++) {
+    rows += jobs[i].n;
+    // offsets within a tile are 32-bit
+    narrow = narrow && jobs[i].ldw <= (1u << 22) && jobs[i].lds <= (1u << 22);
+  }
+  if (!narrow) return p;
+  const uint64_t large = uint64_t((m + 255) / 256) * ((rows + 255) / 256);
+  const uint64_t middle = uint64_t((m + 127) / 128) * ((rows + 127) / 128);
+  p.kernel = large >= 200 ? Kernel::kTile256 : middle >= 200 ? Kernel::kTile128 : Kernel::kTile64;
+  for (uint32_t i = 0; i < n_jobs; i++) {
+    if (!whole_words(jobs[i].scale, jobs[i].lds, k)) p.scales += pad256(uint64_t(jobs[i].n) * scale_pitch(k));
+    if (p.splits > 1) p.parts += pad256(uint64_t(m) * ((jobs[i].n + 3) & ~3u) * 4 * p.splits);
+  }
+  return p;
+}
+uint64_t workspace_of(const Plan& p) { return p.parts + p.scales; }
+// x in MXFP4, its scales in rows of whole words
+uint64_t codes_bytes(uint32_t m, uint32_t k) { return pad256(uint64_t(m) * WC_MX_ROW_BYTES(k)); }
 uint64_t quantized_bytes(uint32_t m, uint32_t k) {
-  return pad256(uint64_t(m) * WC_MX_ROW_BYTES(k)) + pad256(uint64_t(m) * WC_MX_BLOCKS(k));
+  return codes_bytes(m, k) + pad256(uint64_t(m) * scale_pitch(k));
 }
 bool workspace_ok(const void* p, uint64_t bytes, uint64_t need) {
   return need == 0 || (!off(p, 256) && bytes >= need);
@@ -184,8 +329,10 @@ void start_slim(uint32_t tiles, const MatArgs& a, hipStream_t st) {
                      dim3(512), 0, st, a);
 }
 
+// The products of x: rows of codes and scales, or (x_dtype) of elements; ldx in bytes.
 wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int32_t x_dtype, uint32_t m,
-                 uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs, hipStream_t st) {
+                 uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs, const Plan& p, void* workspace,
+                 hipStream_t st) {
   MatArgs a{};
   a.x = reinterpret_cast<uint64_t>(x);
   a.ldx = ldx;
@@ -193,13 +340,35 @@ wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int
   a.ldxs = ldxs;
   a.k = k;
   a.n_jobs = n_jobs;
-  uint32_t tiles = 0;
+  a.splits = p.splits;
+  uint32_t tiles = 0, widest = 0;
+  uint64_t part = reinterpret_cast<uint64_t>(workspace), copy = part + p.parts;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_mx_job& J = jobs[i];
     a.job[i] = {reinterpret_cast<uint64_t>(J.w), reinterpret_cast<uint64_t>(J.scale),
                 reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
-                J.ldw, J.lds, J.ldy, J.n, tiles, J.bias_dtype, J.y_dtype};
-    tiles += (J.n + 31) / 32;
+                J.ldw, J.lds, J.ldy, part, J.n, tiles, J.bias_dtype, J.y_dtype};
+    tiles += tiles_of(p.kernel, m, J.n);
+    widest = std::max(widest, J.n);
+    if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 3) & ~3u) * 4 * p.splits);
+    if (p.kernel != Kernel::kSlim && !whole_words(J.scale, J.lds, k)) {
+      if (!launch_copy_scales(J.scale, J.lds, J.n, k, reinterpret_cast<void*>(copy), st)) return WC_EHIP;
+      a.job[i].scale = copy;
+      a.job[i].lds = scale_pitch(k);
+      copy += pad256(uint64_t(J.n) * scale_pitch(k));
+    }
+  }
+  if (p.kernel != Kernel::kSlim) {
+    a.m = m;
+    with_tile(p.kernel, [&](auto t) {
+      using T = decltype(t);
+      hipLaunchKernelGGL(wc_matmul_mx_tile_kernel<T>, dim3(tiles, p.splits), dim3(T::kThreads), 0, st, a);
+    });
+    if (hipGetLastError() != hipSuccess) return WC_EHIP;
+    if (p.splits > 1)
+      hipLaunchKernelGGL(wc_matmul_mx_join_kernel, dim3(std::min(m, 65536u), (widest + 1023) / 1024, n_jobs),
+                         dim3(256), 0, st, a);
+    return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
   }
   // a grid's second axis holds 65535 blocks of 64 rows
   constexpr uint32_t kSlice = 65535u * 64;
@@ -224,20 +393,32 @@ wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int
 
 namespace wc_mx {
 
-bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     uint64_t ldq, void* scale, uint64_t lds, hipStream_t stream, const Blocks* blocks) {
-  const uint32_t units = blocks_of(k) * 4, each = units < kThreads ? kThreads / units : 1;
+bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q, uint64_t ldq,
+                     void* scale, uint64_t lds, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks) {
+  const uint32_t units = scale_blocks * 4, each = units < kThreads ? kThreads / units : 1;
   for (uint32_t first = 0; first < m; first += kLaunchRows) {
     const uint32_t rows = std::min(m - first, kLaunchRows), groups = (rows + each - 1) / each;
     const bool table = blocks && first == 0;
     const QuantArgs a = {reinterpret_cast<uint64_t>(x) + first * ldx * size_of(dt), ldx,
                          reinterpret_cast<uint64_t>(q) + first * ldq, ldq,
-                         reinterpret_cast<uint64_t>(scale) + first * lds, lds, rows, k, each, groups,
+                         reinterpret_cast<uint64_t>(scale) + first * lds, lds, rows, k, scale_blocks, each, groups,
                          table ? *blocks : Blocks{}};
     const dim3 grid(groups + table, (units + kThreads - 1) / kThreads), block(kThreads);
     if (dt == WC_BF16) hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_BF16>), grid, block, 0, stream, a);
     else if (dt == WC_FP16) hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_FP16>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_FP32>), grid, block, 0, stream, a);
+    if (hipGetLastError() != hipSuccess) return false;
+  }
+  return true;
+}
+
+bool launch_copy_scales(const void* scale, uint64_t pitch, uint32_t rows, uint32_t k, void* to, hipStream_t stream) {
+  const uint32_t blocks = blocks_of(k), words = (blocks + 3) / 4;
+  for (uint32_t first = 0; first < rows; first += kLaunchRows) {
+    const uint32_t some = std::min(rows - first, kLaunchRows);
+    hipLaunchKernelGGL(wc_copy_scales_mx_kernel, dim3((some + 3) / 4, (words + 63) / 64), dim3(kThreads), 0, stream,
+                       reinterpret_cast<uint64_t>(scale) + first * pitch, pitch,
+                       reinterpret_cast<uint64_t>(to) + uint64_t(first) * words * 4, some, blocks);
     if (hipGetLastError() != hipSuccess) return false;
   }
   return true;
@@ -251,7 +432,7 @@ extern "C" wc_status wc_quantize_mx(const void* dev_x, int32_t x_dtype, uint32_t
   if (!rows_ok(dev_x, x_dtype, m, k, ldx)) return WC_EINVAL;
   if (m == 0) return WC_OK;
   if (!coded_ok(dev_q, ldq, dev_scale, lds, k)) return WC_EINVAL;
-  return launch_quantize(dev_x, x_dtype, m, k, ldx, dev_q, ldq, dev_scale, lds,
+  return launch_quantize(dev_x, x_dtype, m, k, ldx, dev_q, ldq, dev_scale, lds, blocks_of(k),
                          reinterpret_cast<hipStream_t>(stream))
              ? WC_OK
              : WC_EHIP;
@@ -279,12 +460,21 @@ extern "C" wc_status wc_dequantize_mx(const uint8_t* dev_q, uint64_t ldq, const 
   return WC_OK;
 }
 
+// Workspace: the sums of the parts of k, copies of the matrices' scales, and then of x's, or x in
+// MXFP4.  Rows of x of matmul's own may need copies of their scales too: room for them always.
+namespace {
+uint64_t x_scales_bytes(const Plan& p, uint32_t m, uint32_t k) {
+  return p.kernel == Kernel::kSlim ? 0 : pad256(uint64_t(m) * scale_pitch(k));
+}
+}  // namespace
+
 extern "C" wc_status wc_matmul_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                                   const wc_mx_job* jobs, uint64_t* bytes) {
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
-  *bytes = plan_of(m, k, n_jobs, jobs).parts;
+  const Plan p = plan_of(m, k, n_jobs, jobs);
+  *bytes = workspace_of(p) + x_scales_bytes(p, m, k);
   return WC_OK;
 }
 
@@ -294,9 +484,18 @@ extern "C" wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
   if (m == 0) return WC_OK;
   if (!coded_ok(dev_q, ldq, dev_scale, lds, k)) return WC_EINVAL;
-  const Plan p = plan_of(m, k, n_jobs, jobs);
-  if (!workspace_ok(dev_workspace, workspace_bytes, p.parts)) return WC_EINVAL;
-  return matmul(dev_q, ldq, dev_scale, lds, 0, m, k, n_jobs, jobs, reinterpret_cast<hipStream_t>(stream));
+  Plan p = plan_of(m, k, n_jobs, jobs);
+  if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p) + x_scales_bytes(p, m, k))) return WC_EINVAL;
+  if (ldq > (1u << 22) || lds > (1u << 22)) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const void* scale = dev_scale;
+  if (p.kernel != Kernel::kSlim && !whole_words(dev_scale, lds, k)) {
+    void* const copy = static_cast<uint8_t*>(dev_workspace) + workspace_of(p);
+    if (!launch_copy_scales(dev_scale, lds, m, k, copy, st)) return WC_EHIP;
+    scale = copy;
+    lds = scale_pitch(k);
+  }
+  return matmul(dev_q, ldq, scale, lds, 0, m, k, n_jobs, jobs, p, dev_workspace, st);
 }
 
 extern "C" wc_status wc_linear_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
@@ -305,7 +504,7 @@ extern "C" wc_status wc_linear_mx_workspace_bytes(uint32_t m, uint32_t k, uint32
   *bytes = 0;
   if (!jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
   const Plan p = plan_of(m, k, n_jobs, jobs);
-  *bytes = p.parts + (p.inside ? 0 : quantized_bytes(m, k));
+  *bytes = workspace_of(p) + (p.inside ? 0 : quantized_bytes(m, k));
   return WC_OK;
 }
 
@@ -315,14 +514,14 @@ extern "C" wc_status wc_linear_mx(const void* dev_x, int32_t x_dtype, uint32_t m
   if (!rows_ok(dev_x, x_dtype, m, k, ldx) || !jobs_ok(m, k, n_jobs, jobs)) return WC_EINVAL;
   if (m == 0) return WC_OK;
   const Plan p = plan_of(m, k, n_jobs, jobs);
-  if (!workspace_ok(dev_workspace, workspace_bytes, p.parts + (p.inside ? 0 : quantized_bytes(m, k))))
+  if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p) + (p.inside ? 0 : quantized_bytes(m, k))))
     return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (p.inside)
-    return matmul(dev_x, ldx * size_of(x_dtype), nullptr, 0, x_dtype, m, k, n_jobs, jobs, st);
-  uint8_t* q = static_cast<uint8_t*>(dev_workspace);
-  uint8_t* scale = q + pad256(uint64_t(m) * WC_MX_ROW_BYTES(k));
-  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, WC_MX_ROW_BYTES(k), scale, WC_MX_BLOCKS(k), st))
+    return matmul(dev_x, ldx * size_of(x_dtype), nullptr, 0, x_dtype, m, k, n_jobs, jobs, p, nullptr, st);
+  uint8_t* q = static_cast<uint8_t*>(dev_workspace) + workspace_of(p);
+  uint8_t* scale = q + codes_bytes(m, k);
+  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, WC_MX_ROW_BYTES(k), scale, scale_pitch(k), scale_pitch(k), st))
     return WC_EHIP;
-  return matmul(q, WC_MX_ROW_BYTES(k), scale, WC_MX_BLOCKS(k), 0, m, k, n_jobs, jobs, st);
+  return matmul(q, WC_MX_ROW_BYTES(k), scale, scale_pitch(k), 0, m, k, n_jobs, jobs, p, dev_workspace, st);
 }

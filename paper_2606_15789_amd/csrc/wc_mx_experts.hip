@@ -434,7 +434,7 @@ wc_status experts(ExpertArgs a, const int32_t* offsets, hipStream_t st) {
   const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(offsets), a.experts, a.slots, rows, most};
   if (!launch_quantize(reinterpret_cast<const void*>(a.x), a.dtype, a.tokens, a.hidden, a.ldx,
                        reinterpret_cast<void*>(a.xq), WC_MX_ROW_BYTES(a.hidden), reinterpret_cast<void*>(a.xs),
-                       WC_MX_BLOCKS(a.hidden), st, &blocks))
+                       WC_MX_BLOCKS(a.hidden), blocks_of(a.hidden), st, &blocks))
     return WC_EHIP;
   if (!(rows == 16 ? start_slim<1>(a, most, st) : start_slim<2>(a, most, st))) return WC_EHIP;
   hipLaunchKernelGGL(wc_experts_mx_join_kernel, dim3(a.tokens, (a.hidden + 1023) / 1024), dim3(256), 0, st, a);
