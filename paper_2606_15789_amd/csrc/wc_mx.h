@@ -114,21 +114,38 @@ struct Part {
   u32x4 scales;
 };
 
+// Scales in groups of 16, those of 512 of k: rows of them `pitch` bytes apart, a row's groups `step`.
+// The public layout has step 16; x and h of a call have theirs group by group (pitch 16), so that a
+// tile's rows of a group are next to each other.
+struct Scales {
+  uint64_t at;
+  uint32_t pitch, step;
+};
+inline uint64_t groups_of(uint64_t k) { return (WC_MX_BLOCKS(k) + 15) / 16; }
+inline uint64_t own_scales_bytes(uint64_t rows, uint64_t k) { return rows * groups_of(k) * 16; }
+inline Scales own_scales(uint64_t at, uint64_t rows, uint64_t k) {
+  // offsets in a tile are 32-bit
+  if (own_scales_bytes(rows, k) >> 30) return {at, uint32_t(groups_of(k) * 16), 16};
+  return {at, 16, uint32_t(rows * 16)};
+}
+
 // The row of an MXFP4 matrix that a lane multiplies.
 struct Row {
   uint64_t codes, scales;
+  uint32_t step = 16;
 };
-__device__ __forceinline__ u32x4 load_scales(uint64_t scales, uint32_t super, uint32_t blocks) {
+__device__ __forceinline__ u32x4 load_scales(uint64_t row, uint32_t step, uint32_t super, uint32_t blocks) {
   const uint32_t g = threadIdx.x % 64 / 16;
+  const uint64_t scales = row + uint64_t(super) * step;
   u32x4 s;
   if (super * kSuper + kSuper <= blocks) {
-    s = *global<const u32x4u>(scales + super * kSuper);
+    s = *global<const u32x4u>(scales);
 #pragma unroll
     for (int i = 0; i < 4; i++) s[i] >>= 8 * g;
   } else {
 #pragma unroll
     for (uint32_t i = 0; i < 4; i++)
-      s[i] = global<const uint8_t>(scales)[min(super * kSuper + 4 * i + g, blocks - 1)];
+      s[i] = global<const uint8_t>(scales)[min(4 * i + g, blocks - 1 - super * kSuper)];
   }
   return s;
 }
@@ -144,7 +161,7 @@ __device__ __forceinline__ Part load_part(const Row& r, uint32_t super, uint32_t
     p.codes[i] = global<const u32x4>(r.codes)[min(b, blocks - 1)];
     if (kZero && b >= blocks) p.codes[i] = u32x4{0, 0, 0, 0};
   }
-  p.scales = load_scales(r.scales, super, blocks);
+  p.scales = load_scales(r.scales, r.step, super, blocks);
   return p;
 }
 // The same of a row of elements (k of them; none: all zeros), quantised in registers.
@@ -249,20 +266,20 @@ __device__ __forceinline__ void store_four(uint64_t p, int32_t dt, uint64_t i, f
   }
 }
 
-// Quantise m rows of k elements of type dt to rows of `ldq` bytes of codes and `lds` of scales
-// (wc_mx.hip), of which the first `scale_blocks` are written: zeros past the row's blocks.  With
-// `blocks`, one more workgroup writes its table.  False on a launch error.
-bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q,
-                     uint64_t ldq, void* scale, uint64_t lds, uint32_t scale_blocks, hipStream_t stream,
-                     const Blocks* blocks = nullptr);
+// Quantise m rows of k elements of type dt to rows of `ldq` bytes of codes and to scales, of which
+// each row has `scale_blocks` written, zeros past its blocks (wc_mx.hip).  With `blocks`, one more
+// workgroup writes its table.  False on a launch error.
+bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q, uint64_t ldq,
+                     const Scales& scales, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks = nullptr);
 
-// Scales for the tiles, which load them as whole words: rows of them at any address copied to rows
-// of scale_pitch(k) bytes, zeros past a row's blocks.  False on a launch error.
-inline uint32_t scale_pitch(uint32_t k) { return (blocks_of(k) + 3) / 4 * 4; }
+// Tiles load scales as whole words: others are copied, to own_scales of all `rows`, zeros past a
+// row's blocks; row r of them lies at scale + r / per * stride + r mod per * pitch.  False on a
+// launch error.
 inline bool whole_words(const void* scale, uint64_t pitch, uint32_t k) {
   return reinterpret_cast<uintptr_t>(scale) % 4 == 0 && pitch % 4 == 0 && blocks_of(k) % 4 == 0;
 }
-bool launch_copy_scales(const void* scale, uint64_t pitch, uint32_t rows, uint32_t k, void* to, hipStream_t stream);
+bool launch_copy_scales(const void* scale, uint64_t pitch, uint64_t per, uint64_t stride, uint64_t rows, uint32_t k,
+                        const Scales& to, hipStream_t stream);
 
 inline bool off(const void* p, uint32_t to) { return !p || reinterpret_cast<uintptr_t>(p) % to != 0; }
 

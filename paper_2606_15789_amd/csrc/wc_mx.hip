@@ -14,7 +14,7 @@ constexpr uint32_t kLaunchRows = 1u << 23;  // a grid's axis has less than 2^32 
 
 struct QuantArgs {
   uint64_t x, ldx, q, ldq, scale, lds;
-  uint32_t m, k, scale_blocks, each, groups;  // rows to a workgroup; workgroups of rows
+  uint32_t m, k, scale_blocks, scale_step, each, groups;  // rows to a workgroup; workgroups of rows
   Blocks blocks;
 };
 
@@ -43,7 +43,8 @@ __global__ __launch_bounds__(kThreads) void wc_quantize_mx_kernel(QuantArgs a) {
   const uint32_t byte = scale_byte(top);
   if (unit < (a.k + 31) / 32 * 4)
     global<uint32_t>(a.q + row * a.ldq)[unit] = byte == 255 ? 0u : e.codes(scale_value(byte));
-  if (unit % 4 == 0) global<uint8_t>(a.scale + row * a.lds)[unit / 4] = uint8_t(byte);
+  if (unit % 4 == 0)
+    *global<uint8_t>(a.scale + row * a.lds + uint64_t(unit / 64) * a.scale_step + unit / 4 % 16) = uint8_t(byte);
 }
 
 struct DequantArgs {
@@ -91,28 +92,31 @@ __global__ __launch_bounds__(kThreads) void wc_dequantize_mx_kernel(DequantArgs 
   if (left > 4) store_four(a.y, kType, at + 4, v[1], left - 4);
 }
 
-// Scales to rows of whole words.
-__global__ __launch_bounds__(kThreads) void wc_copy_scales_mx_kernel(uint64_t from, uint64_t pitch, uint64_t to,
-                                                                     uint32_t rows, uint32_t blocks) {
-  const uint64_t row = blockIdx.x * 4 + threadIdx.x / 64;
-  const uint32_t words = (blocks + 3) / 4, word = blockIdx.y * 64 + threadIdx.x % 64;
+// Scales to groups of whole words, rows from `first` on.
+__global__ __launch_bounds__(kThreads) void wc_copy_scales_mx_kernel(uint64_t from, uint64_t pitch, uint64_t per,
+                                                                     uint64_t stride, Scales to, uint64_t first,
+                                                                     uint64_t rows, uint32_t blocks) {
+  const uint64_t row = first + blockIdx.x * 4 + threadIdx.x / 64;
+  const uint32_t words = (blocks + 15) / 16 * 4, word = blockIdx.y * 64 + threadIdx.x % 64;
   if (row >= rows || word >= words) return;
-  const auto p = global<const uint8_t>(from + row * pitch + word * 4);
+  const auto p = global<const uint8_t>(from + row / per * stride + row % per * pitch + word * 4);
   uint32_t v = 0;
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++)
     if (word * 4 + i < blocks) v |= uint32_t(p[i]) << (8 * i);
-  global<uint32_t>(to)[row * words + word] = v;
+  *global<uint32_t>(to.at + row * to.pitch + uint64_t(word / 4) * to.step + word % 4 * 4) = v;
 }
 
 struct MatJob {
-  uint64_t w, scale, bias, y, ldw, lds, ldy;
-  uint64_t part;  // sums of the parts of k, in fp32: parts x m x n (to whole fours)
+  uint64_t w, bias, y, ldw, ldy;
+  Scales scales;
+  uint64_t part;  // sums of the parts of k, in fp32: parts x m x n (to whole eights)
   uint32_t n, first;  // its first tile
   int32_t bias_dtype, y_dtype;
 };
 struct MatArgs {
-  uint64_t x, ldx, xs, ldxs;  // rows of codes and scales, or of elements (ldx in bytes)
+  uint64_t x, ldx;  // rows of codes, or of elements (ldx in bytes)
+  Scales xs;
   uint32_t m, k, n_jobs;
   uint32_t splits;  // parts of k
   MatJob job[kMaxJobs];
@@ -136,14 +140,14 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
 #pragma unroll
   for (uint32_t n = 0; n < kN; n++) {
     const uint64_t row = min(n0 + 16 * n + r, J.n - 1);
-    w[n] = {J.w + row * J.ldw, J.scale + row * J.lds};
+    w[n] = {J.w + row * J.ldw, J.scales.at + row * J.scales.pitch, J.scales.step};
   }
   const uint32_t blocks = (a.k + 31) / 32;
   S::product(sh, w, blocks, [&](int m, uint32_t super) {
     const uint64_t row = m0 + 16 * uint32_t(m) + r;
     if constexpr (kType == 0) {
       const uint64_t at = min(row, uint64_t(a.m - 1));
-      return load_part<true>(Row{a.x + at * a.ldx, a.xs + at * a.ldxs}, super, blocks);
+      return load_part<true>(Row{a.x + at * a.ldx, a.xs.at + at * a.xs.pitch, a.xs.step}, super, blocks);
     } else {
       return quantize_part<kType>(a.x + row * a.ldx, super, row < a.m ? a.k : 0);
     }
@@ -170,61 +174,69 @@ __global__ __launch_bounds__(T::kThreads) void wc_matmul_mx_tile_kernel(MatArgs 
   if (!tile_at(blockIdx.x - J.first, (a.m + kBM - 1) / kBM, (J.n + kBN - 1) / kBN, mt, nt)) return;
   const uint32_t m0 = mt * kBM, n0 = nt * kBN, m_rows = min(kBM, a.m - m0), n_rows = min(kBN, J.n - n0);
   const uint32_t blocks = (a.k + 31) / 32, words = (blocks + 3) / 4;
-  const uint32_t all = (blocks + kStageBlocks - 1) / kStageBlocks, each = (all + a.splits - 1) / a.splits;
-  const uint32_t first = blockIdx.y * each, stages = first < all ? min(each, all - first) : 0;
-  const uint32_t ldx = uint32_t(a.ldx), ldxs = uint32_t(a.ldxs), ldw = uint32_t(J.ldw), ldws = uint32_t(J.lds);
-  const RowsOf X = rows_of(a.x + m0 * a.ldx, ldx, a.xs + m0 * a.ldxs, ldxs, m_rows, blocks);
-  const RowsOf W = rows_of(J.w + n0 * J.ldw, ldw, J.scale + n0 * J.lds, ldws, n_rows, blocks);
-  const uint32_t chunk = T::chunk_of(), half = threadIdx.x % 2;
+  // whole groups of stages to a part
+  const uint32_t groups = (blocks + 15) / 16, each = (groups + a.splits - 1) / a.splits * T::kGroup;
+  const uint32_t first = blockIdx.y * each, all = groups * T::kGroup, stages = first < all ? min(each, all - first) : 0;
+  const uint32_t ldx = uint32_t(a.ldx), ldw = uint32_t(J.ldw);
+  const RowsOf X = rows_of(a.x, ldx, a.xs, m0, m_rows, blocks), W = rows_of(J.w, ldw, J.scales, n0, n_rows, blocks);
+  const uint32_t chunk = T::chunk_of();
   const uint32_t xoff = T::row_of(0) * ldx + chunk * 16, woff = T::row_of(0) * ldw + chunk * 16;
-  const uint32_t xsoff = T::scale_row() * ldxs + half * 4, wsoff = T::scale_row() * ldws + half * 4;
+  ScaleLoad scales[T::kSLoads];
+#pragma unroll
+  for (int j = 0; j < T::kSLoads; j++)
+    if (T::first_scale_row(j) < kBM) scales[j].set(X, T::scale_row(j));
+    else scales[j].set(W, T::scale_row(j) - kBM);
   f32x16 acc[T::kMT][T::kNT];
-  // rows past the tile's last are past the buffers' ends
+  // rows past the tile's last are past the buffers' ends; chunks of x past its row are zeros
   T::product(
-      lds, stages, m_rows,
+      lds, stages, m_rows, words - min(words, first / T::kGroup * 4),
       [&](int i, uint32_t s, uint32_t to) {
         s += first;
-        load_lds(X.codes, to, (s * kStageBlocks + chunk < blocks ? xoff : kNowhere) + (i * T::kStep * ldx + s * kStage));
+        load_lds(X.codes, to, (s * T::kBlocks + chunk < blocks ? xoff : kNowhere) + (i * T::kStep * ldx + s * T::kBytes));
       },
-      [&](int i, uint32_t s, uint32_t to) { load_lds(W.codes, to, woff + (i * T::kStep * ldw + (s + first) * kStage)); },
-      [&](int i, uint32_t s, uint32_t to) {
-        s += first;
-        const bool in = s * 2 + half < words;
-        if (i < T::kXScales)
-          load_lds_words(X.scales, to, (in ? xsoff : kNowhere) + (i * T::kScaleStep * ldxs + s * 8));
-        else
-          load_lds_words(W.scales, to, (in ? wsoff : kNowhere) + ((i - T::kXScales) * T::kScaleStep * ldws + s * 8));
-      },
+      [&](int i, uint32_t s, uint32_t to) { load_lds(W.codes, to, woff + (i * T::kStep * ldw + (s + first) * T::kBytes)); },
+      [&](int j, uint32_t s, uint32_t to) { scales[j]((s + first) / T::kGroup, to); },
       acc);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t wm0 = wave / T::kWN_ * (T::kMT * 32), wn0 = wave % T::kWN_ * (T::kNT * 32);
-  const uint32_t pitch = (J.n + 3) & ~3u;
-  const uint32_t n = n0 + wn0 + threadIdx.x % (T::kNT * 8) * 4;  // of all this lane's stores
-  f32x4 bias = {0, 0, 0, 0};
-  if (J.bias && a.splits == 1)
+  const uint32_t pitch = (J.n + 7) & ~7u, lane = threadIdx.x % 64;
 #pragma unroll
-    for (uint32_t j = 0; j < 4; j++) bias[j] = load_float(J.bias, J.bias_dtype, min(n + j, J.n - 1));
+  for (int nb = 0; nb < T::kNT; nb++) {
+    const uint32_t c0 = n0 + wn0 + nb * 32;
+    f32x4 bias[2][2] = {};
+    if (J.bias && a.splits == 1)
 #pragma unroll
-  for (int mb = 0; mb < T::kMT; mb++)
-    T::rows_out(
-        lds, [&](int c, int i) { return acc[mb][c][i]; },
-        [&](uint32_t row, uint32_t, f32x4 v) {
-          const uint32_t m = m0 + wm0 + mb * 32 + row;
-          if (m >= a.m || n >= J.n) return;
-          if (a.splits > 1) {
-            *global<f32x4>(J.part + ((uint64_t(blockIdx.y) * a.m + m) * pitch + n) * 4) = v;
-            return;
-          }
+      for (uint32_t j = 0; j < 16; j++)
+        bias[j / 8][j / 4 % 2][j % 4] =
+            load_float(J.bias, J.bias_dtype, min(c0 + j / 8 * 16 + lane / 32 * 8 + j % 8, J.n - 1));
 #pragma unroll
-          for (int j = 0; j < 4; j++) v[j] += bias[j];
-          store_four(J.y, J.y_dtype, m * J.ldy + n, v, J.n - n);
-        });
+    for (int mb = 0; mb < T::kMT; mb++) {
+      const uint32_t m = m0 + wm0 + mb * 32 + lane % 32;
+      if (m0 + wm0 + mb * 32 >= a.m) break;
+      rows_out(acc[mb][nb], [&](uint32_t column, f32x4 low, f32x4 high) {
+        const uint32_t n = c0 + column;
+        if (m >= a.m || n >= J.n) return;
+        if (a.splits > 1) {
+          const auto to = global<f32x4>(J.part + ((uint64_t(blockIdx.y) * a.m + m) * pitch + n) * 4);
+          to[0] = low;
+          to[1] = high;
+          return;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          low[j] += bias[column / 16][0][j];
+          high[j] += bias[column / 16][1][j];
+        }
+        store_eight(J.y, J.y_dtype, m * J.ldy + n, low, high, J.n - n);
+      });
+    }
+  }
 }
 
 // y from the sums of the parts of k, in their order.
 __global__ __launch_bounds__(256) void wc_matmul_mx_join_kernel(MatArgs a) {
   const MatJob& J = a.job[blockIdx.z];
-  const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4, pitch = (J.n + 3) & ~3u;
+  const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4, pitch = (J.n + 7) & ~7u;
   if (n >= J.n) return;
   f32x4 bias = {0, 0, 0, 0};
   if (J.bias)
@@ -267,9 +279,9 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
 }
 
 enum class Kernel { kSlim, kTile64, kTile128, kTile256 };
-using Tile64 = MxTile<64, 64, 1, 2, 4>;
-using Tile128 = MxTile<128, 128, 2, 2, 2>;
-using Tile256 = MxTile<256, 256, 2, 4, 2>;
+using Tile64 = MxTile<64, 64, 1, 2, 128, 4>;
+using Tile128 = MxTile<128, 128, 2, 2, 128, 2>;
+using Tile256 = MxTile<256, 256, 2, 4, 128, 2>;
 template <class F>
 void with_tile(Kernel k, F f) {
   switch (k) {
@@ -308,16 +320,16 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   const uint64_t middle = uint64_t((m + 127) / 128) * ((rows + 127) / 128);
   p.kernel = large >= 200 ? Kernel::kTile256 : middle >= 200 ? Kernel::kTile128 : Kernel::kTile64;
   for (uint32_t i = 0; i < n_jobs; i++) {
-    if (!whole_words(jobs[i].scale, jobs[i].lds, k)) p.scales += pad256(uint64_t(jobs[i].n) * scale_pitch(k));
-    if (p.splits > 1) p.parts += pad256(uint64_t(m) * ((jobs[i].n + 3) & ~3u) * 4 * p.splits);
+    if (!whole_words(jobs[i].scale, jobs[i].lds, k)) p.scales += pad256(own_scales_bytes(jobs[i].n, k));
+    if (p.splits > 1) p.parts += pad256(uint64_t(m) * ((jobs[i].n + 7) & ~7u) * 4 * p.splits);
   }
   return p;
 }
 uint64_t workspace_of(const Plan& p) { return p.parts + p.scales; }
-// x in MXFP4, its scales in rows of whole words
+// x in MXFP4, its scales in groups
 uint64_t codes_bytes(uint32_t m, uint32_t k) { return pad256(uint64_t(m) * WC_MX_ROW_BYTES(k)); }
 uint64_t quantized_bytes(uint32_t m, uint32_t k) {
-  return codes_bytes(m, k) + pad256(uint64_t(m) * scale_pitch(k));
+  return codes_bytes(m, k) + pad256(own_scales_bytes(m, k));
 }
 bool workspace_ok(const void* p, uint64_t bytes, uint64_t need) {
   return need == 0 || (!off(p, 256) && bytes >= need);
@@ -330,14 +342,13 @@ void start_slim(uint32_t tiles, const MatArgs& a, hipStream_t st) {
 }
 
 // The products of x: rows of codes and scales, or (x_dtype) of elements; ldx in bytes.
-wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int32_t x_dtype, uint32_t m,
-                 uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs, const Plan& p, void* workspace,
+wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype, uint32_t m, uint32_t k,
+                 uint32_t n_jobs, const wc_mx_job* jobs, const Plan& p, void* workspace,
                  hipStream_t st) {
   MatArgs a{};
   a.x = reinterpret_cast<uint64_t>(x);
   a.ldx = ldx;
-  a.xs = reinterpret_cast<uint64_t>(xs);
-  a.ldxs = ldxs;
+  a.xs = xs;
   a.k = k;
   a.n_jobs = n_jobs;
   a.splits = p.splits;
@@ -345,17 +356,16 @@ wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int
   uint64_t part = reinterpret_cast<uint64_t>(workspace), copy = part + p.parts;
   for (uint32_t i = 0; i < n_jobs; i++) {
     const wc_mx_job& J = jobs[i];
-    a.job[i] = {reinterpret_cast<uint64_t>(J.w), reinterpret_cast<uint64_t>(J.scale),
-                reinterpret_cast<uint64_t>(J.bias), reinterpret_cast<uint64_t>(J.y),
-                J.ldw, J.lds, J.ldy, part, J.n, tiles, J.bias_dtype, J.y_dtype};
+    a.job[i] = {reinterpret_cast<uint64_t>(J.w), reinterpret_cast<uint64_t>(J.bias),
+                reinterpret_cast<uint64_t>(J.y), J.ldw, J.ldy,
+                {reinterpret_cast<uint64_t>(J.scale), uint32_t(J.lds), 16}, part, J.n, tiles, J.bias_dtype, J.y_dtype};
     tiles += tiles_of(p.kernel, m, J.n);
     widest = std::max(widest, J.n);
-    if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 3) & ~3u) * 4 * p.splits);
+    if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 7) & ~7u) * 4 * p.splits);
     if (p.kernel != Kernel::kSlim && !whole_words(J.scale, J.lds, k)) {
-      if (!launch_copy_scales(J.scale, J.lds, J.n, k, reinterpret_cast<void*>(copy), st)) return WC_EHIP;
-      a.job[i].scale = copy;
-      a.job[i].lds = scale_pitch(k);
-      copy += pad256(uint64_t(J.n) * scale_pitch(k));
+      a.job[i].scales = own_scales(copy, J.n, k);
+      if (!launch_copy_scales(J.scale, J.lds, J.n, 0, J.n, k, a.job[i].scales, st)) return WC_EHIP;
+      copy += pad256(own_scales_bytes(J.n, k));
     }
   }
   if (p.kernel != Kernel::kSlim) {
@@ -382,7 +392,7 @@ wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int
     else start_slim<4, 0>(tiles, a, st);
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
     a.x += uint64_t(a.m) * ldx;
-    a.xs += uint64_t(a.m) * ldxs;
+    a.xs.at += uint64_t(a.m) * a.xs.pitch;
     for (uint32_t i = 0; i < n_jobs; i++)
       a.job[i].y += uint64_t(a.m) * a.job[i].ldy * size_of(a.job[i].y_dtype);
   }
@@ -394,15 +404,15 @@ wc_status matmul(const void* x, uint64_t ldx, const void* xs, uint64_t ldxs, int
 namespace wc_mx {
 
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q, uint64_t ldq,
-                     void* scale, uint64_t lds, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks) {
+                     const Scales& scales, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks) {
   const uint32_t units = scale_blocks * 4, each = units < kThreads ? kThreads / units : 1;
   for (uint32_t first = 0; first < m; first += kLaunchRows) {
     const uint32_t rows = std::min(m - first, kLaunchRows), groups = (rows + each - 1) / each;
     const bool table = blocks && first == 0;
     const QuantArgs a = {reinterpret_cast<uint64_t>(x) + first * ldx * size_of(dt), ldx,
                          reinterpret_cast<uint64_t>(q) + first * ldq, ldq,
-                         reinterpret_cast<uint64_t>(scale) + first * lds, lds, rows, k, scale_blocks, each, groups,
-                         table ? *blocks : Blocks{}};
+                         scales.at + uint64_t(first) * scales.pitch, scales.pitch, rows, k, scale_blocks, scales.step,
+                         each, groups, table ? *blocks : Blocks{}};
     const dim3 grid(groups + table, (units + kThreads - 1) / kThreads), block(kThreads);
     if (dt == WC_BF16) hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_BF16>), grid, block, 0, stream, a);
     else if (dt == WC_FP16) hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_FP16>), grid, block, 0, stream, a);
@@ -412,13 +422,13 @@ bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t
   return true;
 }
 
-bool launch_copy_scales(const void* scale, uint64_t pitch, uint32_t rows, uint32_t k, void* to, hipStream_t stream) {
-  const uint32_t blocks = blocks_of(k), words = (blocks + 3) / 4;
-  for (uint32_t first = 0; first < rows; first += kLaunchRows) {
-    const uint32_t some = std::min(rows - first, kLaunchRows);
+bool launch_copy_scales(const void* scale, uint64_t pitch, uint64_t per, uint64_t stride, uint64_t rows, uint32_t k,
+                        const Scales& to, hipStream_t stream) {
+  const uint32_t words = uint32_t(groups_of(k)) * 4;
+  for (uint64_t first = 0; first < rows; first += kLaunchRows) {
+    const uint32_t some = uint32_t(std::min<uint64_t>(rows - first, kLaunchRows));
     hipLaunchKernelGGL(wc_copy_scales_mx_kernel, dim3((some + 3) / 4, (words + 63) / 64), dim3(kThreads), 0, stream,
-                       reinterpret_cast<uint64_t>(scale) + first * pitch, pitch,
-                       reinterpret_cast<uint64_t>(to) + uint64_t(first) * words * 4, some, blocks);
+                       reinterpret_cast<uint64_t>(scale), pitch, per, stride, to, first, rows, blocks_of(k));
     if (hipGetLastError() != hipSuccess) return false;
   }
   return true;
@@ -432,7 +442,8 @@ extern "C" wc_status wc_quantize_mx(const void* dev_x, int32_t x_dtype, uint32_t
   if (!rows_ok(dev_x, x_dtype, m, k, ldx)) return WC_EINVAL;
   if (m == 0) return WC_OK;
   if (!coded_ok(dev_q, ldq, dev_scale, lds, k)) return WC_EINVAL;
-  return launch_quantize(dev_x, x_dtype, m, k, ldx, dev_q, ldq, dev_scale, lds, blocks_of(k),
+  return launch_quantize(dev_x, x_dtype, m, k, ldx, dev_q, ldq,
+                         {reinterpret_cast<uint64_t>(dev_scale), uint32_t(lds), 16}, blocks_of(k),
                          reinterpret_cast<hipStream_t>(stream))
              ? WC_OK
              : WC_EHIP;
@@ -464,7 +475,7 @@ extern "C" wc_status wc_dequantize_mx(const uint8_t* dev_q, uint64_t ldq, const 
 // MXFP4.  Rows of x of matmul's own may need copies of their scales too: room for them always.
 namespace {
 uint64_t x_scales_bytes(const Plan& p, uint32_t m, uint32_t k) {
-  return p.kernel == Kernel::kSlim ? 0 : pad256(uint64_t(m) * scale_pitch(k));
+  return p.kernel == Kernel::kSlim ? 0 : pad256(own_scales_bytes(m, k));
 }
 }  // namespace
 
@@ -488,14 +499,12 @@ extern "C" wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint
   if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p) + x_scales_bytes(p, m, k))) return WC_EINVAL;
   if (ldq > (1u << 22) || lds > (1u << 22)) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const void* scale = dev_scale;
+  Scales xs = {reinterpret_cast<uint64_t>(dev_scale), uint32_t(lds), 16};
   if (p.kernel != Kernel::kSlim && !whole_words(dev_scale, lds, k)) {
-    void* const copy = static_cast<uint8_t*>(dev_workspace) + workspace_of(p);
-    if (!launch_copy_scales(dev_scale, lds, m, k, copy, st)) return WC_EHIP;
-    scale = copy;
-    lds = scale_pitch(k);
+    xs = own_scales(reinterpret_cast<uint64_t>(dev_workspace) + workspace_of(p), m, k);
+    if (!launch_copy_scales(dev_scale, lds, m, 0, m, k, xs, st)) return WC_EHIP;
   }
-  return matmul(dev_q, ldq, scale, lds, 0, m, k, n_jobs, jobs, p, dev_workspace, st);
+  return matmul(dev_q, ldq, xs, 0, m, k, n_jobs, jobs, p, dev_workspace, st);
 }
 
 extern "C" wc_status wc_linear_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
@@ -518,10 +527,10 @@ extern "C" wc_status wc_linear_mx(const void* dev_x, int32_t x_dtype, uint32_t m
     return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (p.inside)
-    return matmul(dev_x, ldx * size_of(x_dtype), nullptr, 0, x_dtype, m, k, n_jobs, jobs, p, nullptr, st);
+    return matmul(dev_x, ldx * size_of(x_dtype), Scales{}, x_dtype, m, k, n_jobs, jobs, p, nullptr, st);
   uint8_t* q = static_cast<uint8_t*>(dev_workspace) + workspace_of(p);
-  uint8_t* scale = q + codes_bytes(m, k);
-  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, WC_MX_ROW_BYTES(k), scale, scale_pitch(k), scale_pitch(k), st))
+  const Scales scales = own_scales(reinterpret_cast<uint64_t>(q) + codes_bytes(m, k), m, k);
+  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, WC_MX_ROW_BYTES(k), scales, uint32_t(groups_of(k)) * 16, st))
     return WC_EHIP;
-  return matmul(q, WC_MX_ROW_BYTES(k), scale, scale_pitch(k), 0, m, k, n_jobs, jobs, p, dev_workspace, st);
+  return matmul(q, WC_MX_ROW_BYTES(k), scales, 0, m, k, n_jobs, jobs, p, dev_workspace, st);
 }

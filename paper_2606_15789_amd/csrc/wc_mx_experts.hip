@@ -12,7 +12,7 @@
 #include <algorithm>
 
 #include "wc_choose.h"
-#include "wc_mx.h"
+#include "wc_mx_tile.h"
 
 namespace {
 
@@ -20,14 +20,16 @@ using namespace wc_mx;
 using wc_choose::RouteArgs;
 
 struct Bank {
-  uint64_t w, scale, stride, scale_stride;
+  uint64_t w, stride;
+  Scales scales;
+  uint64_t scale_stride;
 };
 struct ExpertArgs {
   uint64_t table, order, ids, weights;
   uint64_t x, ldx;
-  uint64_t xq, xs;  // quantised x, by token
-  uint64_t hq, hs;  // quantised h, by place in the order (few tokens: by slot)
-  uint64_t out;     // experts' results, fp32, by slot
+  uint64_t xq, hq;  // codes of x, by token, and of h, by place in the order (few tokens: by slot)
+  Scales xs, hs;
+  uint64_t out;     // experts' results, fp32, by slot, in rows of whole eights
   uint64_t y, ldy;
   uint32_t tokens, k, experts, hidden, ffn, slots;
   uint32_t first;   // this launch's first block of places, or token
@@ -35,15 +37,28 @@ struct ExpertArgs {
   Bank gate, up, down;
 };
 __device__ __forceinline__ Row row_of(const Bank& b, uint32_t e, uint32_t row, uint32_t blocks) {
-  return {b.w + e * b.stride + uint64_t(row) * (blocks * 16), b.scale + e * b.scale_stride + uint64_t(row) * blocks};
+  return {b.w + e * b.stride + uint64_t(row) * (blocks * 16),
+          b.scales.at + e * b.scale_stride + uint64_t(row) * b.scales.pitch, b.scales.step};
 }
 
 // g / (1 + exp(-g)), with an exponential of 1 ulp and a rounded division
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
 
-// Four lanes to a row of 32 values of h in LDS: its codes and scale, eight codes to a lane, all
-// four lanes of a row alive or none.
-__device__ __forceinline__ void quantize_h(const float* row, uint64_t codes, uint64_t scale, bool live) {
+// Codes and scales of row `at` of h.
+__device__ __forceinline__ uint64_t h_codes(const ExpertArgs& a, uint64_t at, uint32_t block) {
+  return a.hq + (at * ((a.ffn + 31) / 32) + block) * 16;
+}
+// A block's scale; after a row's last one zeros to a whole word.
+__device__ __forceinline__ void store_h_scale(const ExpertArgs& a, uint64_t at, uint32_t block, uint32_t byte) {
+  const auto to = global<uint8_t>(a.hs.at + at * a.hs.pitch + uint64_t(block / 16) * a.hs.step + block % 16);
+  *to = uint8_t(byte);
+  if (block + 1 == (a.ffn + 31) / 32)
+    for (uint32_t i = 1; (block + i) % 4; i++) to[i] = 0;
+}
+// Four lanes to a row of 32 values of h in LDS, block `block` of row `at`: its codes and scale, eight
+// codes to a lane, all four lanes of a row alive or none.
+__device__ __forceinline__ void quantize_h(const ExpertArgs& a, const float* row, uint64_t at, uint32_t block,
+                                           bool live) {
   const uint32_t q = threadIdx.x % 4;
   Eight<WC_FP32> e;
 #pragma unroll
@@ -53,8 +68,8 @@ __device__ __forceinline__ void quantize_h(const float* row, uint64_t codes, uin
   top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xF, 0xF, false)));  // lane ^ 2
   if (!live) return;
   const uint32_t byte = scale_byte(top);
-  global<uint32_t>(codes)[q] = byte == 255 ? 0u : e.codes(scale_value(byte));
-  if (q == 0) *global<uint8_t>(scale) = uint8_t(byte);
+  global<uint32_t>(h_codes(a, at, block))[q] = byte == 255 ? 0u : e.codes(scale_value(byte));
+  if (q == 0) store_h_scale(a, at, block, byte);
 }
 constexpr int kRowH = 36;  // floats of a row of h in LDS
 
@@ -159,10 +174,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs
   }
   __syncthreads();
   if (threadIdx.x < 64) {
-    const uint32_t token = threadIdx.x / 4, all = (a.ffn + 31) / 32;
-    const int32_t slot = slot_of(c, a, token, e);
-    quantize_h(h[token], a.hq + (uint64_t(uint32_t(slot)) * all + blockIdx.x) * 16,
-               a.hs + uint64_t(uint32_t(slot)) * all + blockIdx.x, slot >= 0);
+    const int32_t slot = slot_of(c, a, threadIdx.x / 4, e);
+    quantize_h(a, h[threadIdx.x / 4], uint32_t(slot), blockIdx.x, slot >= 0);
   }
 }
 
@@ -182,7 +195,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_down_kernel(ExpertAr
     const uint32_t at = u / supers, e = c.list[at], end = min(last, (at + 1) * supers);
     const Row w = row_of(a.down, e, min(n0 + r, a.hidden - 1), blocks);
     const int32_t slot = slot_of(c, a, r, e);
-    const Row x = {a.hq + uint64_t(max(slot, 0)) * blocks * 16, a.hs + uint64_t(max(slot, 0)) * blocks};
+    const Row x = {h_codes(a, max(slot, 0), 0), a.hs.at + uint64_t(max(slot, 0)) * a.hs.pitch, a.hs.step};
     f32x4 acc = {0, 0, 0, 0};
     for (; u < end; u++) {
       const Part wp = load_part<false>(w, u - at * supers, blocks);
@@ -233,6 +246,8 @@ __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place)
   return min(uint32_t(max(global<const int32_t>(a.order)[place], 0)), a.slots - 1);
 }
 
+__host__ __device__ constexpr uint32_t out_pitch(uint32_t hidden) { return (hidden + 7) & ~7u; }
+
 // 32 columns of h for a block of 16 kM places, quantised.
 template <int kM>
 __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a) {
@@ -254,7 +269,7 @@ __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a
 #pragma unroll
   for (uint32_t m = 0; m < kM; m++) {
     const uint64_t token = slot_at(a, min(first + 16 * m + r, last - 1)) / a.k;
-    x[m] = {a.xq + token * blocks * 16, a.xs + token * blocks};
+    x[m] = {a.xq + token * blocks * 16, a.xs.at + token * a.xs.pitch, a.xs.step};
   }
   S::product(sh, w, blocks, [&](int m, uint32_t super) { return load_part<true>(x[m], super, blocks); });
   for (uint32_t i = threadIdx.x; i < 128 * kM; i += 512) {
@@ -268,9 +283,8 @@ __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a
   }
   __syncthreads();
   if (threadIdx.x < 64 * kM) {
-    const uint32_t row = threadIdx.x / 4, place = first + row, all = (a.ffn + 31) / 32;
-    quantize_h(h[row], a.hq + (uint64_t(place) * all + blockIdx.y) * 16, a.hs + uint64_t(place) * all + blockIdx.y,
-               place < last);
+    const uint32_t row = threadIdx.x / 4;
+    quantize_h(a, h[row], first + row, blockIdx.y, first + row < last);
   }
 }
 
@@ -288,13 +302,148 @@ __global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs
   for (uint32_t n = 0; n < 2; n++) w[n] = row_of(a.down, e, min(n0 + 16 * n + r, a.hidden - 1), blocks);
   S::product(sh, w, blocks, [&](int m, uint32_t super) {
     const uint64_t place = min(first + 16 * uint32_t(m) + r, last - 1);
-    return load_part<true>(Row{a.hq + place * blocks * 16, a.hs + place * blocks}, super, blocks);
+    return load_part<true>(Row{h_codes(a, place, 0), a.hs.at + place * a.hs.pitch, a.hs.step}, super, blocks);
   });
   for (uint32_t i = threadIdx.x; i < S::kPart; i += 512) {
     const uint32_t tile = i / 64, lane = i % 64;
     const uint32_t n = n0 + tile / kM * 16 + lane / 16 * 4, place = first + tile % kM * 16 + lane % 16;
     if (place < last && n < a.hidden)
-      store_four(a.out, WC_FP32, uint64_t(slot_at(a, place)) * a.hidden + n, S::sum(sh, i), a.hidden - n);
+      store_four(a.out, WC_FP32, uint64_t(slot_at(a, place)) * out_pitch(a.hidden) + n, S::sum(sh, i), 4);
+  }
+}
+
+// The same on tiles through LDS: kCols / 2 columns of h, for which W's rows are those of gate and the
+// same of up, so that both products of a value of h meet in one lane, and a block of 32 of
+// its columns in two.
+template <class T>
+__global__ __launch_bounds__(T::kThreads) void wc_experts_mx_up_tile_kernel(ExpertArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+  constexpr uint32_t kBM = T::kRows, kColumns = T::kCols / 2;
+  static_assert(T::kNT % 2 == 0 && kColumns % 64 == 0 && kColumns % T::kStep == 0);
+  uint32_t mt, nt;
+  if (!tile_at(blockIdx.x, block_count(a), (a.ffn + kColumns - 1) / kColumns, mt, nt)) return;
+  const auto [e, first, last] = block_at(a, mt);
+  const uint32_t n0 = nt * kColumns, n_rows = min(kColumns, a.ffn - n0);
+  const uint32_t blocks = (a.hidden + 31) / 32, words = (blocks + 3) / 4, pitch = blocks * 16;
+  const auto matrix = [&](const Bank& b) {
+    return rows_of(b.w + e * b.stride, pitch, Scales{b.scales.at + e * b.scale_stride, b.scales.pitch, b.scales.step}, n0,
+                   n_rows, blocks);
+  };
+  const RowsOf G = matrix(a.gate), U = matrix(a.up);
+  const RowsOf X = rows_of(a.xq, pitch, a.xs, 0, a.tokens, blocks);
+  const uint32_t chunk = T::chunk_of(), woff = T::row_of(0) * pitch + chunk * 16;
+  const auto token_of = [&](uint32_t row) { return slot_at(a, min(first + row, last - 1)) / a.k; };
+  uint32_t xoff[T::kXLoads];
+#pragma unroll
+  for (int i = 0; i < T::kXLoads; i++) xoff[i] = token_of(T::row_of(i)) * pitch + chunk * 16;
+  ScaleLoad scales[T::kSLoads];
+#pragma unroll
+  for (int j = 0; j < T::kSLoads; j++) {
+    const uint32_t row = T::scale_row(j), at = T::first_scale_row(j);
+    if (at < kBM) scales[j].set(X, token_of(row));
+    else if (at < kBM + kColumns) scales[j].set(G, row - kBM);
+    else scales[j].set(U, row - kBM - kColumns);
+  }
+  f32x16 acc[T::kMT][T::kNT];
+  T::product(
+      lds, T::stages_of(blocks), last - first, words,
+      [&](int i, uint32_t s, uint32_t to) {
+        load_lds(X.codes, to, (s * T::kBlocks + chunk < blocks ? xoff[i] : kNowhere) + s * T::kBytes);
+      },
+      [&](int i, uint32_t s, uint32_t to) {
+        constexpr int kHalf = int(kColumns / T::kStep);
+        load_lds(i < kHalf ? G.codes : U.codes, to, woff + (i % kHalf * T::kStep * pitch + s * T::kBytes));
+      },
+      [&](int j, uint32_t s, uint32_t to) { scales[j](s / T::kGroup, to); }, acc);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const uint32_t wm0 = wave / T::kWN_ * (T::kMT * 32), wn0 = wave % T::kWN_ * (T::kNT * 16);
+#pragma unroll
+  for (int nb = 0; nb < T::kNT / 2; nb++)
+#pragma unroll
+    for (int mb = 0; mb < T::kMT; mb++) {
+      const uint32_t place = first + wm0 + mb * 32 + lane % 32, c0 = n0 + wn0 + nb * 32, block = c0 / 32;
+      if (first + wm0 + mb * 32 >= last || c0 >= a.ffn) continue;
+      float h[16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        const uint32_t column = c0 + i / 4 * 8 + lane / 32 * 4 + i % 4;
+        h[i] = silu(acc[mb][nb][i]) * acc[mb][nb + T::kNT / 2][i];
+        if (column >= a.ffn) h[i] = 0.0f;
+        top = max(top, __float_as_uint(h[i]) & 0x7FFFFFFFu);
+      }
+      const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+      const uint32_t byte = scale_byte(max(both[0], both[1]));
+      const float scale = scale_value(byte);
+      // this lane's codes of every eight columns: two bytes, the other lane's the next two
+      uint32_t mine[2];
+#pragma unroll
+      for (int p = 0; p < 2; p++) {
+        uint32_t c = 0;
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p], h[8 * p + 1], scale, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p + 2], h[8 * p + 3], scale, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p + 4], h[8 * p + 5], scale, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p + 6], h[8 * p + 7], scale, 3);
+        mine[p] = byte == 255 ? 0u : c;
+      }
+      u32x4 codes;
+#pragma unroll
+      for (int p = 0; p < 2; p++) {
+        const auto v = __builtin_amdgcn_permlane32_swap(mine[p], mine[p], false, false);
+        codes[2 * p] = (v[0] & 0xFFFFu) | v[1] << 16;       // the lower lanes' own, the upper lanes'
+        codes[2 * p + 1] = v[0] >> 16 | (v[1] & 0xFFFF0000u);
+      }
+      if (lane < 32 && place < last) {
+        *global<u32x4>(h_codes(a, place, block)) = codes;
+        store_h_scale(a, place, block, byte);
+      }
+    }
+}
+
+// down(h) of a block of places on tiles, stored by slot.
+template <class T>
+__global__ __launch_bounds__(T::kThreads) void wc_experts_mx_down_tile_kernel(ExpertArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+  constexpr uint32_t kBM = T::kRows, kBN = T::kCols;
+  uint32_t mt, nt;
+  if (!tile_at(blockIdx.x, block_count(a), (a.hidden + kBN - 1) / kBN, mt, nt)) return;
+  const auto [e, first, last] = block_at(a, mt);
+  const uint32_t n0 = nt * kBN, n_rows = min(kBN, a.hidden - n0);
+  const uint32_t blocks = (a.ffn + 31) / 32, words = (blocks + 3) / 4, pitch = blocks * 16;
+  const Bank& b = a.down;
+  const RowsOf W = rows_of(b.w + e * b.stride, pitch,
+                           Scales{b.scales.at + e * b.scale_stride, b.scales.pitch, b.scales.step}, n0, n_rows, blocks);
+  const RowsOf X = rows_of(a.hq, pitch, a.hs, first, last - first, blocks);
+  const uint32_t chunk = T::chunk_of(), off = T::row_of(0) * pitch + chunk * 16;
+  ScaleLoad scales[T::kSLoads];
+#pragma unroll
+  for (int j = 0; j < T::kSLoads; j++)
+    if (T::first_scale_row(j) < kBM) scales[j].set(X, T::scale_row(j));
+    else scales[j].set(W, T::scale_row(j) - kBM);
+  f32x16 acc[T::kMT][T::kNT];
+  T::product(
+      lds, T::stages_of(blocks), last - first, words,
+      [&](int i, uint32_t s, uint32_t to) {
+        load_lds(X.codes, to, (s * T::kBlocks + chunk < blocks ? off : kNowhere) + (i * T::kStep * pitch + s * T::kBytes));
+      },
+      [&](int i, uint32_t s, uint32_t to) { load_lds(W.codes, to, off + (i * T::kStep * pitch + s * T::kBytes)); },
+      [&](int j, uint32_t s, uint32_t to) { scales[j](s / T::kGroup, to); }, acc);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const uint32_t wm0 = wave / T::kWN_ * (T::kMT * 32), c0 = n0 + wave % T::kWN_ * (T::kNT * 32);
+#pragma unroll
+  for (int mb = 0; mb < T::kMT; mb++) {
+    const uint32_t place = first + wm0 + mb * 32 + lane % 32;
+    if (first + wm0 + mb * 32 >= last) break;
+    const uint64_t row = uint64_t(slot_at(a, min(place, last - 1))) * out_pitch(a.hidden);
+#pragma unroll
+    for (int nb = 0; nb < T::kNT; nb++)
+      rows_out(acc[mb][nb], [&](uint32_t column, f32x4 low, f32x4 high) {
+        const uint32_t n = c0 + nb * 32 + column;
+        if (place >= last || n >= a.hidden) return;
+        const auto to = global<f32x4>(a.out + (row + n) * 4);
+        to[0] = low;
+        to[1] = high;
+      });
   }
 }
 
@@ -308,14 +457,7 @@ __global__ __launch_bounds__(256) void wc_experts_mx_join_kernel(ExpertArgs a) {
   for (uint32_t j = 0; j < a.k; j++) {
     const uint64_t slot = token * a.k + j;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (global<const int32_t>(a.ids)[slot] >= 0) {
-      const auto row = global<const float>(a.out) + slot * a.hidden + n;
-      if (a.hidden % 4 == 0)
-        v = *reinterpret_cast<global_ptr<const f32x4>>(row);
-      else
-#pragma unroll
-        for (uint32_t i = 0; i < 4; i++) v[i] = row[min(i, left - 1)];
-    }
+    if (global<const int32_t>(a.ids)[slot] >= 0) v = *global<const f32x4>(a.out + (slot * out_pitch(a.hidden) + n) * 4);
     const float w = global<const float>(a.weights)[slot];
 #pragma unroll
     for (int i = 0; i < 4; i++) sum[i] += w * v[i];
@@ -328,7 +470,7 @@ uint64_t most_blocks(uint32_t slots, uint32_t experts, uint32_t rows) {
   return uint64_t(slots) / rows + std::min(experts, slots);
 }
 struct Workspace {
-  uint64_t table, xq, xs, hq, hs, out, bytes;
+  uint64_t table, xq, xs, hq, hs, out, gate, up, down, bytes;  // gate, up, down: copies of scales
 };
 Workspace layout(uint64_t tokens, uint64_t k, uint32_t experts, uint32_t hidden, uint32_t ffn) {
   Workspace w{};
@@ -338,12 +480,16 @@ Workspace layout(uint64_t tokens, uint64_t k, uint32_t experts, uint32_t hidden,
     return here;
   };
   w.hq = take(tokens * k * WC_MX_ROW_BYTES(ffn));
-  w.hs = take(tokens * k * WC_MX_BLOCKS(ffn));
+  w.hs = take(own_scales_bytes(tokens * k, ffn));
   if (is_few(tokens, k)) return w;
   w.table = take((1 + most_blocks(uint32_t(tokens * k), experts, 16)) * 16);
   w.xq = take(tokens * WC_MX_ROW_BYTES(hidden));
-  w.xs = take(tokens * WC_MX_BLOCKS(hidden));
-  w.out = take(tokens * k * hidden * 4);
+  w.xs = take(own_scales_bytes(tokens, hidden));
+  w.out = take(tokens * k * out_pitch(hidden) * 4);
+  // room for the copies at any alignment of the scales
+  w.gate = take(own_scales_bytes(uint64_t(experts) * ffn, hidden));
+  w.up = take(own_scales_bytes(uint64_t(experts) * ffn, hidden));
+  w.down = take(own_scales_bytes(uint64_t(experts) * hidden, ffn));
   return w;
 }
 bool sizes_ok(uint32_t tokens, uint32_t k, uint32_t experts, uint32_t hidden, uint32_t ffn) {
@@ -354,8 +500,9 @@ bool bank_ok(const wc_mx_experts* b, uint64_t n, uint32_t k) {
   return b && !off(b->w, 16) && b->scale && b->stride % 16 == 0 && b->stride >= n * WC_MX_ROW_BYTES(k) &&
          b->scale_stride >= n * WC_MX_BLOCKS(k) && !(b->stride >> 40) && !(b->scale_stride >> 40);
 }
-Bank bank(const wc_mx_experts* b) {
-  return {reinterpret_cast<uint64_t>(b->w), reinterpret_cast<uint64_t>(b->scale), b->stride, b->scale_stride};
+Bank bank(const wc_mx_experts* b, uint32_t k) {
+  return {reinterpret_cast<uint64_t>(b->w), b->stride,
+          {reinterpret_cast<uint64_t>(b->scale), blocks_of(k), 16}, b->scale_stride};
 }
 bool tensors_ok(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, uint32_t hidden, uint32_t ffn,
                 const wc_mx_experts* gate, const wc_mx_experts* up, const wc_mx_experts* down, const void* y,
@@ -372,9 +519,9 @@ ExpertArgs args_of(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, 
   a.x = reinterpret_cast<uint64_t>(x);
   a.ldx = ldx;
   a.xq = ws + w.xq;
-  a.xs = ws + w.xs;
+  a.xs = own_scales(ws + w.xs, tokens, hidden);
   a.hq = ws + w.hq;
-  a.hs = ws + w.hs;
+  a.hs = own_scales(ws + w.hs, uint64_t(tokens) * k, ffn);
   a.out = ws + w.out;
   a.y = reinterpret_cast<uint64_t>(y);
   a.ldy = ldy;
@@ -385,9 +532,9 @@ ExpertArgs args_of(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, 
   a.ffn = ffn;
   a.slots = tokens * k;
   a.dtype = dtype;
-  a.gate = bank(gate);
-  a.up = bank(up);
-  a.down = bank(down);
+  a.gate = bank(gate, hidden);
+  a.up = bank(up, hidden);
+  a.down = bank(down, ffn);
   return a;
 }
 
@@ -427,16 +574,76 @@ bool start_slim(ExpertArgs a, uint32_t most, hipStream_t st) {
   return true;
 }
 
-wc_status experts(ExpertArgs a, const int32_t* offsets, hipStream_t st) {
+// Tiles by the places of a block: up's columns are half of gate's and half of up's.
+template <int kPlaces>
+struct Tiles;
+template <>
+struct Tiles<64> {
+  using Up = MxTile<64, 128, 1, 2, 128, 3, true>;
+  using Down = MxTile<64, 128, 1, 2, 128, 3>;
+};
+template <>
+struct Tiles<128> {
+  using Up = MxTile<128, 128, 2, 2, 128, 2, true>;
+  using Down = MxTile<128, 128, 2, 2, 128, 2>;
+};
+template <>
+struct Tiles<256> {
+  using Up = MxTile<256, 256, 2, 4, 128, 2, true>;
+  using Down = MxTile<256, 256, 2, 4, 128, 2>;
+};
+uint32_t tiles(uint32_t n, uint32_t each) { return (n + each - 1) / each; }
+// Scales that the tiles cannot load as they are, copied.
+bool ready(Bank& b, uint64_t to, uint32_t experts, uint32_t n, uint32_t k, hipStream_t st) {
+  if (whole_words(reinterpret_cast<const void*>(b.scales.at), blocks_of(k), k) && b.scale_stride % 4 == 0) return true;
+  const Scales own = own_scales(to, uint64_t(experts) * n, k);
+  if (!launch_copy_scales(reinterpret_cast<const void*>(b.scales.at), blocks_of(k), n, b.scale_stride,
+                          uint64_t(experts) * n, k, own, st))
+    return false;
+  b.scales = own;
+  b.scale_stride = uint64_t(n) * own.pitch;
+  return true;
+}
+template <int kPlaces>
+bool start_tiles(const ExpertArgs& a, uint32_t most, hipStream_t st) {
+  using Up = typename Tiles<kPlaces>::Up;
+  using Down = typename Tiles<kPlaces>::Down;
+  hipLaunchKernelGGL(wc_experts_mx_up_tile_kernel<Up>, dim3(most * tiles(a.ffn, Up::kCols / 2)), dim3(Up::kThreads), 0,
+                     st, a);
+  if (hipGetLastError() != hipSuccess) return false;
+  hipLaunchKernelGGL(wc_experts_mx_down_tile_kernel<Down>, dim3(most * tiles(a.hidden, Down::kCols)),
+                     dim3(Down::kThreads), 0, st, a);
+  return hipGetLastError() == hipSuccess;
+}
+// Places to a block: 16 and 32 straight from memory to registers, more through LDS.
+uint32_t places(const ExpertArgs& a) {
+  const uint32_t average = a.slots / a.experts;
+  // x lies within 32-bit offsets, a grid's axis has less than 2^32 threads
+  if (a.tokens * WC_MX_ROW_BYTES(a.hidden) >> 31 || a.xs.step == 16 ||
+      most_blocks(a.slots, a.experts, 64) * std::max(tiles(a.ffn, 64), tiles(a.hidden, 128)) * 512 >> 32)
+    return average <= 16 ? 16 : 32;
+  return average <= 16 ? 16 : average <= 32 ? 32 : average <= 64 ? 64 : average <= 256 ? 128 : 256;
+}
+
+wc_status experts(ExpertArgs a, const Workspace& w, const int32_t* offsets, hipStream_t st) {
   if (is_few(a.tokens, a.k)) return few(a, nullptr, st);
-  const uint32_t rows = a.slots / a.experts <= 16 ? 16 : 32;
-  const uint32_t most = uint32_t(most_blocks(a.slots, a.experts, rows));
+  const uint32_t rows = places(a), most = uint32_t(most_blocks(a.slots, a.experts, rows));
   const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(offsets), a.experts, a.slots, rows, most};
   if (!launch_quantize(reinterpret_cast<const void*>(a.x), a.dtype, a.tokens, a.hidden, a.ldx,
-                       reinterpret_cast<void*>(a.xq), WC_MX_ROW_BYTES(a.hidden), reinterpret_cast<void*>(a.xs),
-                       WC_MX_BLOCKS(a.hidden), blocks_of(a.hidden), st, &blocks))
+                       reinterpret_cast<void*>(a.xq), WC_MX_ROW_BYTES(a.hidden), a.xs,
+                       uint32_t(groups_of(a.hidden)) * 16, st, &blocks))
     return WC_EHIP;
-  if (!(rows == 16 ? start_slim<1>(a, most, st) : start_slim<2>(a, most, st))) return WC_EHIP;
+  const uint64_t ws = a.hq - w.hq;
+  if (rows >= 64 && (!ready(a.gate, ws + w.gate, a.experts, a.ffn, a.hidden, st) ||
+                     !ready(a.up, ws + w.up, a.experts, a.ffn, a.hidden, st) ||
+                     !ready(a.down, ws + w.down, a.experts, a.hidden, a.ffn, st)))
+    return WC_EHIP;
+  const bool started = rows == 16   ? start_slim<1>(a, most, st)
+                       : rows == 32 ? start_slim<2>(a, most, st)
+                       : rows == 64 ? start_tiles<64>(a, most, st)
+                       : rows == 128 ? start_tiles<128>(a, most, st)
+                                     : start_tiles<256>(a, most, st);
+  if (!started) return WC_EHIP;
   hipLaunchKernelGGL(wc_experts_mx_join_kernel, dim3(a.tokens, (a.hidden + 1023) / 1024), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
 }
@@ -492,7 +699,7 @@ extern "C" wc_status wc_experts_mx(const void* dev_x, int32_t dtype, uint32_t to
   a.order = reinterpret_cast<uint64_t>(dev_order);
   a.ids = reinterpret_cast<uint64_t>(dev_ids);
   a.weights = reinterpret_cast<uint64_t>(dev_weights);
-  return experts(a, dev_offsets, reinterpret_cast<hipStream_t>(stream));
+  return experts(a, w, dev_offsets, reinterpret_cast<hipStream_t>(stream));
 }
 
 extern "C" wc_status wc_moe_mx_workspace_bytes(uint32_t tokens, const wc_route_params* p, uint32_t hidden,
@@ -520,8 +727,9 @@ extern "C" wc_status wc_moe_mx(const void* dev_x, int32_t dtype, uint32_t tokens
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const uint64_t ws = reinterpret_cast<uint64_t>(dev_workspace);
   const RouteSpace r = route_layout(tokens, p);
-  ExpertArgs a = args_of(dev_x, dtype, tokens, ldx, p->k, p->experts, hidden, ffn, gate, up, down, dev_y, ldy,
-                         layout(tokens, p->k, p->experts, hidden, ffn), ws + r.bytes);
+  const Workspace w = layout(tokens, p->k, p->experts, hidden, ffn);
+  ExpertArgs a = args_of(dev_x, dtype, tokens, ldx, p->k, p->experts, hidden, ffn, gate, up, down, dev_y, ldy, w,
+                         ws + r.bytes);
   a.ids = ws + r.ids;
   a.weights = ws + r.weights;
   if (is_few(tokens, p->k)) {
@@ -535,5 +743,5 @@ extern "C" wc_status wc_moe_mx(const void* dev_x, int32_t dtype, uint32_t tokens
                                reinterpret_cast<int32_t*>(a.ids), reinterpret_cast<float*>(a.weights),
                                reinterpret_cast<int32_t*>(ws + r.offsets), reinterpret_cast<int32_t*>(a.order),
                                reinterpret_cast<void*>(ws + r.scratch), r.scratch_bytes, stream);
-  return s == WC_OK ? experts(a, reinterpret_cast<const int32_t*>(ws + r.offsets), st) : s;
+  return s == WC_OK ? experts(a, w, reinterpret_cast<const int32_t*>(ws + r.offsets), st) : s;
 }

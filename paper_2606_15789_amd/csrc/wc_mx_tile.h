@@ -1,11 +1,12 @@
 // wc_mx_tile.h -- the product of one tile of MXFP4 matrices by one workgroup, operands through
 // LDS: C[n][m] = sum_k W[n][k] x[m][k] on v_mfma_scale_f32_32x32x64_f8f6f4.
 //
-// A stage is 256 of k: 128 bytes of codes and 8 scales of every row of the tile.  All of it goes
-// from memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1 stages
-// ahead of the products.  Product q (of four) of a stage takes block q from its lanes 0 .. 31 and
-// block 4 + q from the others, so that a lane's scales of a stage are one word, byte after byte.  A
-// row's 16-byte chunks are stored in the order chunk ^ turn(row): the sixteen lanes that read LDS
+// A stage is kStage (64 or 128) bytes of codes of every row of the tile, 2 kStage of k.  They go from
+// memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1 stages ahead of
+// the products, and so do the scales, of 512 of k at a time: a line of memory for 16 bytes of a row.
+// Product q of a stage's kStage / 32 takes block q from its lanes 0 .. 31 and block kStage / 32 + q
+// from the others, so that a lane's scales of a stage are neighbouring bytes of a word.  A row's
+// 16-byte chunks are stored in the order chunk ^ turn(row): the sixteen lanes that read LDS
 // together, the same chunk of sixteen rows, then touch all 64 banks once.
 #pragma once
 
@@ -18,58 +19,70 @@ namespace wc_mx {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr uint32_t kStageBlocks = 8;  // of 32 of k
-
-// 64 lanes x 4 bytes from rs + offset to LDS at lds, lane after lane; waited for as load_lds.
-__device__ __forceinline__ void load_lds_words(u32x4 rs, uint32_t lds, uint32_t offset) {
-  asm volatile("s_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"{m0}"(lds), "v"(offset), "s"(rs) : "memory");
-}
-
-// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages in LDS.
-template <int kBM, int kBN, int kWM, int kWN, int kDepth = 2>
+// kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages in LDS.  kPaired: W's rows are kBN / 2 of
+// one matrix and the same of another, and a wave's blocks of W the same of either.
+template <int kBM, int kBN, int kWM, int kWN, int kStage, int kDepth, bool kPaired = false>
 struct MxTile {
   static constexpr int kWM_ = kWM, kWN_ = kWN, kWaves = kWM * kWN, kThreads = 64 * kWaves;
   static constexpr int kMT = kBM / kWM / 32, kNT = kBN / kWN / 32;  // 32 x 32 blocks to a wave
-  static constexpr int kRows = kBM, kCols = kBN, kAll = kBM + kBN;
-  static constexpr int kXLoads = kBM / 8 / kWaves, kWLoads = kBN / 8 / kWaves;  // eight rows each
-  static constexpr int kSLoads = kAll / 32 / kWaves;                            // scales of 32 rows
-  static constexpr int kLoads = kXLoads + kWLoads + kSLoads;
-  static constexpr int kScales = kAll * kStage;  // where a stage's scales start
-  static constexpr int kBuffer = kAll * (kStage + 8);
-  static constexpr int kLds = kDepth * kBuffer;
-  static_assert(kBM % (8 * kWaves) == 0 && kBN % (8 * kWaves) == 0 && kAll % (32 * kWaves) == 0 &&
-                kBM % (32 * kWaves) == 0 && kLds <= 160 * 1024);
+  static constexpr int kRows = kBM, kCols = kBN, kAll = kBM + kBN, kBytes = kStage;
+  static constexpr int kSteps = kStage / 32;           // products of a block by a block to a stage
+  static constexpr uint32_t kBlocks = 2 * kSteps;      // MXFP4 blocks of a row in a stage
+  static constexpr int kGroup = 16 / int(kBlocks);     // stages that share a load of scales
+  static constexpr uint32_t kChunks = kStage / 16;     // lanes to a row of a load
+  static constexpr uint32_t kEach = 64 / kChunks;      // rows to a load of a wave
+  static constexpr int kXLoads = kBM / kEach / kWaves, kWLoads = kBN / kEach / kWaves;
+  static constexpr int kLoads = kXLoads + kWLoads;     // and those of scales at a group's first stage
+  static constexpr int kSLoads = (kAll / 64 + kWaves - 1) / kWaves;  // 64 rows each; not all waves have the last
+  static constexpr int kAhead = kDepth - 1;
+  static constexpr int kBuffer = kAll * kStage, kScaleBuffer = kAll * 16;
+  static constexpr int kScaleBuffers = kAhead < kGroup ? 2 : 4;
+  static constexpr int kScales = kDepth * kBuffer;     // where the scales start
+  static constexpr int kLds = kScales + kScaleBuffers * kScaleBuffer;
+  static_assert(kBM % (int(kEach) * kWaves) == 0 && kBN % (int(kEach) * kWaves) == 0 &&
+                kBM % 64 == 0 && kBN % 64 == 0 && kLds <= 160 * 1024);
+  static_assert(kAhead < kGroup + (kScaleBuffers > 2 ? 2 * kGroup : 0));
 
   // Row of x (or W) and 16-byte chunk of its stage that load 0 of this lane brings; load i: the
   // same chunk of a row kStep i further on.
-  static constexpr uint32_t kStep = 8 * kWaves;
+  static constexpr uint32_t kStep = kEach * kWaves;
   static __device__ __forceinline__ uint32_t row_of(int i) {
-    return 8 * __builtin_amdgcn_readfirstlane(threadIdx.x / 64) + threadIdx.x % 64 / 8 + kStep * i;
+    return kEach * __builtin_amdgcn_readfirstlane(threadIdx.x / 64) + threadIdx.x % 64 / kChunks + kStep * i;
   }
-  static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (row >> 1) & 7; }
+  static __device__ __forceinline__ uint32_t turn(uint32_t row) {
+    return kStage == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+  }
   static __device__ __forceinline__ uint32_t chunk_of() {
-    static_assert(kWaves % 2 == 0);  // rows kStep apart turn alike
-    return (threadIdx.x % 8) ^ turn(row_of(0));
+    static_assert(kStep % 16 == 0);  // rows kStep apart turn alike
+    return (threadIdx.x % kChunks) ^ turn(row_of(0));
   }
-  // The same of scales: two words a row, the first kXScales loads of x's rows, the others of W's.
-  static constexpr int kXScales = kBM / 32 / kWaves;
-  static constexpr uint32_t kScaleStep = 32 * kWaves;
-  static __device__ __forceinline__ uint32_t scale_row() {
-    return 32 * __builtin_amdgcn_readfirstlane(threadIdx.x / 64) + threadIdx.x % 64 / 2;
+  // Row of the tile (x's, then W's) of which load j of this lane brings scales: of x for a whole wave,
+  // or of W; none past kAll.
+  static __device__ __forceinline__ uint32_t scale_row(int j) { return threadIdx.x + kThreads * j; }
+  static __device__ __forceinline__ uint32_t first_scale_row(int j) {
+    return 64 * __builtin_amdgcn_readfirstlane(threadIdx.x / 64) + kThreads * j;
   }
+  // Stages of k: whole groups.
+  static __host__ __device__ constexpr uint32_t stages_of(uint32_t blocks) { return (blocks + 15) / 16 * kGroup; }
 
-  // Waits for all but the loads of the newest kLater stages, then for the other waves.
+  // Waits for all but the loads of the newest kLater stages (loads of scales among them count as
+  // ones of codes before them), then for the other waves.
   template <int kLater>
   static __device__ __forceinline__ void arrive() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater * kLoads) : "memory");
   }
 
-  // `load_x(i, stage, lds)`, `load_w` and `load_s` start load i of a stage's rows of x, of W, and of
-  // the scales.  Of a wave's blocks of 32 rows of x, those past the first `rows` are not
-  // multiplied; a wave without any only loads.
+  template <int kValue>
+  using Int = std::integral_constant<int, kValue>;
+
+  // `load_x(i, stage, lds)` and `load_w` start load i of a stage's rows of x and of W, `load_s(j,
+  // stage, lds)` load j of the scales of a group of stages, of which a row has `words` in all.  `stages`
+  // are whole groups (stages_of); x is zeros past its row.  Of a wave's blocks of 32 rows
+  // of x, those past the first `rows` are not multiplied; a wave without any only loads.
   template <class LoadX, class LoadW, class LoadS>
-  static __device__ __forceinline__ void product(uint8_t* lds, uint32_t stages, uint32_t rows, LoadX load_x,
-                                                 LoadW load_w, LoadS load_s, f32x16 (&acc)[kMT][kNT]) {
+  static __device__ __forceinline__ void product(uint8_t* lds, uint32_t stages, uint32_t rows, uint32_t words,
+                                                 LoadX load_x, LoadW load_w, LoadS load_s,
+                                                 f32x16 (&acc)[kMT][kNT]) {
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t wm = wave / kWN, wn = wave % kWN;
     const uint32_t base =
@@ -80,38 +93,48 @@ struct MxTile {
       for (int n = 0; n < kNT; n++)
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[m][n][i] = 0;
-    constexpr uint32_t kAhead = kDepth - 1;
-    // Load i of a stage.  Stages past the last are loaded too: the buffers' ends bound them,
-    // nothing reads them, and the loop has no branches.
-    const auto start = [&](int i, uint32_t s, uint32_t slot) {
+    // Load i of stage s, the kPhase-th of its group.  Stages past the last are loaded too: the
+    // buffers' ends bound them, nothing reads them, and the loop has no branches.
+    const auto start = [&]<int kPhase>(Int<kPhase>, int i, uint32_t s, uint32_t slot) {
       const uint32_t to = __builtin_amdgcn_readfirstlane(base + slot * kBuffer + wave * 1024);
       if (i < kXLoads) load_x(i, s, to + uint32_t(i) * kThreads * 16);
-      else if (i < kXLoads + kWLoads) load_w(i - kXLoads, s, to + kBM * kStage + uint32_t(i - kXLoads) * kThreads * 16);
-      else
-        load_s(i - kXLoads - kWLoads, s,
-               __builtin_amdgcn_readfirstlane(base + slot * kBuffer + kScales + wave * 256) +
-                   uint32_t(i - kXLoads - kWLoads) * kThreads * 4);
-    };
-    uint32_t at[4];
+      else load_w(i - kXLoads, s, to + kBM * kStage + uint32_t(i - kXLoads) * kThreads * 16);
+      if (i == kLoads - 1 && kPhase == 0)
 #pragma unroll
-    for (uint32_t q = 0; q < 4; q++) at[q] = lane % 32 * kStage + ((lane / 32 * 4 + q) ^ turn(lane % 32)) * 16;
-    const uint32_t xrow = wm * (kBM / kWM), wrow = kBM + wn * (kBN / kWN);
-    const uint32_t scale_at = kScales + lane % 32 * 8 + lane / 32 * 4;
-    u32x4 x[2][kMT], w[2][kNT];  // operands of two products' steps
+        for (int j = 0; j < kSLoads; j++)
+          if (kAll % kThreads == 0 || j < kSLoads - 1 || first_scale_row(j) < kAll)
+            load_s(j, s, __builtin_amdgcn_readfirstlane(base + kScales + s / kGroup % kScaleBuffers * kScaleBuffer +
+                                                        wave * 1024) + j * kThreads * 16);
+    };
+    uint32_t at[kSteps];
+#pragma unroll
+    for (uint32_t q = 0; q < kSteps; q++)
+      at[q] = lane % 32 * kStage + ((lane / 32 * kSteps + q) ^ turn(lane % 32)) * 16;
+    const uint32_t xrow = wm * (kBM / kWM), wrow = kBM + wn * (kBN / kWN / (kPaired ? 2 : 1));
+    // block n of W, from row wrow on
+    const auto w_at = [](int n) { return kPaired && n >= kNT / 2 ? kBN / 2 + (n - kNT / 2) * 32 : n * 32; };
+    u32x4 x[2][kMT], w[2][kNT];  // operands of two steps
     uint32_t xs[kMT], ws[kNT], xs_next[kMT], ws_next[kNT];
     const auto read = [&](int set, const uint8_t* b, int q, int i) {
-      if (i < kNT) w[set][i] = *reinterpret_cast<const u32x4*>(b + wrow * kStage + at[q] + i * 32 * kStage);
+      if (i < kNT) w[set][i] = *reinterpret_cast<const u32x4*>(b + wrow * kStage + at[q] + w_at(i) * kStage);
       else x[set][i - kNT] = *reinterpret_cast<const u32x4*>(b + xrow * kStage + at[q] + (i - kNT) * 32 * kStage);
     };
-    const auto read_scale = [&](const uint8_t* b, int i) {
-      if (i < kNT) ws_next[i] = *reinterpret_cast<const uint32_t*>(b + scale_at + wrow * 8 + i * 256);
-      else xs_next[i - kNT] = *reinterpret_cast<const uint32_t*>(b + scale_at + xrow * 8 + (i - kNT) * 256);
+    // the scales of stage s, the `phase`-th of its group: from byte 0 of their words on
+    const auto read_scale = [&](uint32_t s, int phase, int i) {
+      const uint8_t* b = lds + kScales + s / kGroup % kScaleBuffers * kScaleBuffer + lane % 32 * 16;
+      const uint32_t word = kStage == 128 ? uint32_t(phase) * 2 + lane / 32 : uint32_t(phase);
+      const uint32_t row = i < kNT ? wrow + w_at(i) : xrow + (i - kNT) * 32;
+      uint32_t v = *reinterpret_cast<const uint32_t*>(b + row * 16 + word * 4);
+      if (s / kGroup * 4 + word >= words) v = 0;  // past a row's end could be another's NaN
+      if (kStage == 64) v >>= lane / 32 * 16;
+      (i < kNT ? ws_next[i < kNT ? i : 0] : xs_next[i < kNT ? 0 : i - kNT]) = v;
     };
     // Step q of a stage.  Between its products, in the order written: the reads of the next step
-    // (the last one's: of the stage in `slot`, with its scales), and loads kFrom .. kTo - 1 of
-    // stage `s`, so that the matrix unit never waits for a queue of either to drain.
-    const auto step = [&]<int kQ, int kLive, int kFrom, int kTo>(std::integer_sequence<int, kQ, kLive, kFrom, kTo>,
-                                                                uint32_t slot, uint32_t s, uint32_t to) {
+    // (the last one's: of stage `next`, the kNext-th of its group, with its scales), and loads kFrom ..
+    // kTo - 1 of stage `s`, so that the matrix unit never waits for a queue of either to drain.
+    const auto step = [&]<int kQ, int kLive, int kFrom, int kTo, int kPhase, int kNext>(
+                          std::integer_sequence<int, kQ, kLive, kFrom, kTo, kPhase, kNext>, uint32_t slot, uint32_t s,
+                          uint32_t to, uint32_t next) {
       const uint8_t* b = lds + slot * kBuffer;
       constexpr int kProducts = kLive * kNT, kReads = kLive + kNT, kSet = kQ % 2, kNew = kTo - kFrom;
 #pragma unroll
@@ -122,115 +145,152 @@ struct MxTile {
 #pragma unroll
         for (int i = 0; i < kReads; i++)
           if (i * kProducts / kReads == p) {
-            read(kSet ^ 1, b, (kQ + 1) % 4, i);
-            if (kQ == 3) read_scale(b, i);
+            read(kSet ^ 1, b, (kQ + 1) % kSteps, i);
+            if (kQ == kSteps - 1) read_scale(next, kNext, i);
           }
 #pragma unroll
         for (int i = kFrom; i < kTo; i++)
-          if ((i - kFrom) * kProducts / (kNew ? kNew : 1) == p) start(i, s, to);
+          if ((i - kFrom) * kProducts / (kNew ? kNew : 1) == p) start(Int<kPhase>{}, i, s, to);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    constexpr int kHalf = kDepth == 2 ? kLoads : kLoads / 2;
+    // a stage's loads: the first in the last step of the stage before, the others in the next one or two
+    constexpr int kHalf = kLoads / 2, kMost = kLoads;
+    const auto begin = [&]<int... kS>(std::integer_sequence<int, kS...>) {
+      ([&] {
 #pragma unroll
-    for (uint32_t s = 0; s < kAhead; s++)
+        for (int i = 0; i < kLoads; i++) start(Int<kS % kGroup>{}, i, kS, kS);
+      }(), ...);
+    };
+    begin(std::make_integer_sequence<int, kAhead>{});
+    arrive<kAhead - 1>();
 #pragma unroll
-      for (int i = 0; i < kLoads; i++) start(i, s, s);
-    arrive<int(kAhead) - 1>();
-#pragma unroll
-    for (int i = 0; i < kHalf; i++) start(i, kAhead, kAhead);
+    for (int i = 0; i < kHalf; i++) start(Int<kAhead % kGroup>{}, i, kAhead, kAhead);
     uint32_t slot = 0, fill = kAhead;  // the stage's place, and that of the one it loads
+    const auto turn_over = [&] {
+      fill = slot;
+      slot = slot + 1 < kDepth ? slot + 1 : 0;
+    };
+    // all stages, a group at a time
+    const auto all = [&](auto stage) {
+      for (uint32_t s = 0; s < stages; s += kGroup)
+        [&]<int... kS>(std::integer_sequence<int, kS...>) {
+          (stage(Int<kS>{}, s + kS), ...);
+        }(std::make_integer_sequence<int, kGroup>{});
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      // the waves leave together: LDS is free for what comes
+      __syncthreads();
+    };
     const uint32_t row0 = __builtin_amdgcn_readfirstlane(wm) * (kBM / kWM);
     const uint32_t live = rows > row0 ? (rows - row0 + 31) / 32 : 0;
     if (live == 0) {
-      for (uint32_t s = 0; s < stages; s++) {
+      all([&]<int kPhase>(Int<kPhase>, uint32_t s) {
 #pragma unroll
-        for (int i = kHalf; i < kLoads; i++) start(i, s + kAhead, fill);
-        arrive<int(kAhead) - 1>();
-        fill = slot;
-        slot = slot + 1 < kDepth ? slot + 1 : 0;
+        for (int i = kHalf; i < kLoads; i++) start(Int<(kPhase + kAhead) % kGroup>{}, i, s + kAhead, fill);
+        arrive<kAhead - 1>();
+        turn_over();
 #pragma unroll
-        for (int i = 0; i < kHalf; i++) start(i, s + 1 + kAhead, fill);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
+        for (int i = 0; i < kHalf; i++) start(Int<(kPhase + 1 + kAhead) % kGroup>{}, i, s + 1 + kAhead, fill);
+      });
       return;
     }
-    const auto run = [&]<int kLive>(std::integer_sequence<int, kLive>) {
+    const auto run = [&]<int kLive>(Int<kLive>) {
 #pragma unroll
       for (int i = 0; i < kLive + kNT; i++) {
         read(0, lds, 0, i);
-        read_scale(lds, i);
+        read_scale(0, 0, i);
       }
-      for (uint32_t s = 0; s < stages; s++) {
+      all([&]<int kPhase>(Int<kPhase>, uint32_t s) {
+        constexpr int kLoad = (kPhase + kAhead) % kGroup, kNext = (kPhase + 1) % kGroup;
 #pragma unroll
         for (int i = 0; i < kNT; i++) ws[i] = ws_next[i];
 #pragma unroll
         for (int i = 0; i < kLive; i++) xs[i] = xs_next[i];
-        step(std::integer_sequence<int, 0, kLive, kHalf, kLoads>{}, slot, s + kAhead, fill);
-        step(std::integer_sequence<int, 1, kLive, 0, 0>{}, slot, 0, 0);
-        step(std::integer_sequence<int, 2, kLive, 0, 0>{}, slot, 0, 0);
+        step(std::integer_sequence<int, 0, kLive, kHalf, kMost, kLoad, 0>{}, slot, s + kAhead, fill, 0);
+        if constexpr (kSteps > 2) {
+          step(std::integer_sequence<int, 1, kLive, kMost, kLoads, kLoad, 0>{}, slot, s + kAhead, fill, 0);
+          step(std::integer_sequence<int, 2, kLive, 0, 0, 0, 0>{}, slot, 0, 0, 0);
+        }
         // Before the last step's products: the next stage's loads of this wave are in LDS and its
         // reads of this stage done, and so with the other waves behind the barrier.  The
         // stage after those in flight then replaces this one.
         // lgkmcnt(0) as the compiler knows it: no waits for these operands further on
         __builtin_amdgcn_s_waitcnt(0xC07F);
-        arrive<int(kAhead) - 1>();
-        fill = slot;
-        slot = slot + 1 < kDepth ? slot + 1 : 0;
-        step(std::integer_sequence<int, 3, kLive, 0, kHalf>{}, slot, s + 1 + kAhead, fill);
-      }
+        arrive<kAhead - 1>();
+        turn_over();
+        step(std::integer_sequence<int, kSteps - 1, kLive, 0, kHalf, (kLoad + 1) % kGroup, kNext>{}, slot, s + 1 + kAhead,
+             fill, s + 1);
+      });
     };
-    if (live >= kMT) run(std::integer_sequence<int, kMT>{});
-    else if (kMT > 3 && live == 3) run(std::integer_sequence<int, (kMT > 3 ? 3 : 1)>{});
-    else if (kMT > 2 && live == 2) run(std::integer_sequence<int, (kMT > 2 ? 2 : 1)>{});
-    else run(std::integer_sequence<int, 1>{});
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    // the waves leave together: LDS is free for the results
-    __syncthreads();
-  }
-
-  // The results of one 32-row block of x through the wave's own part of LDS, so that rows are
-  // written whole: `value(block, i)` is this lane's result i of the given 32 columns (W row 8
-  // (i / 4) + 4 (lane / 32) + i mod 4 of x row lane mod 32); `store(row, column, v)` writes four
-  // neighbouring columns.
-  template <class Value, class Store>
-  static __device__ __forceinline__ void rows_out(uint8_t* lds, Value value, Store store) {
-    constexpr int kRow = kNT * 32 + 4;  // floats: rows four banks apart
-    static_assert(kWaves * 32 * kRow * 4 <= kLds);
-    const uint32_t lane = threadIdx.x % 64;
-    float* t = reinterpret_cast<float*>(lds) + threadIdx.x / 64 * (32 * kRow);
-#pragma unroll
-    for (int c = 0; c < kNT; c++)
-#pragma unroll
-      for (int g = 0; g < 4; g++) {
-        f32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = value(c, 4 * g + i);
-        *reinterpret_cast<f32x4*>(t + lane % 32 * kRow + c * 32 + g * 8 + lane / 32 * 4) = v;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int kLanes = kNT * 8;  // lanes to a row
-#pragma unroll
-    for (int r = 0; r < 32; r += 64 / kLanes) {
-      const uint32_t row = r + lane / kLanes, col = lane % kLanes * 4;
-      store(row, col, *reinterpret_cast<const f32x4*>(t + row * kRow + col));
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (live >= kMT) run(Int<kMT>{});
+    else if (kMT > 3 && live == 3) run(Int<(kMT > 3 ? 3 : 1)>{});
+    else if (kMT > 2 && live == 2) run(Int<(kMT > 2 ? 2 : 1)>{});
+    else run(Int<1>{});
   }
 };
 
-// The loads of a tile: rows of codes and scales of x and W, by buffers that start at the tile's
-// first rows.  `codes` and `words`: bytes of a row's codes, words of its scales (whole rows of
-// words).  Chunks of x past its row are zeros (any of W times them are nothing), and so
-// are words of scales past either's (another row's could be NaN).
+// The results of a 32 x 32 block, acc[i] the sum of W row 8 (i / 4) + 4 (lane / 32) + i mod 4 and x row
+// lane mod 32: `store(column, low, high)` gets eight neighbouring columns of row lane mod 32, those
+// from `column` on, twice.  The lanes of a row trade the halves of eight columns that they lack.
+template <class Store>
+__device__ __forceinline__ void rows_out(const f32x16& acc, Store store) {
+#pragma unroll
+  for (int p = 0; p < 2; p++) {
+    f32x4 low, high;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * p + j]), __float_as_uint(acc[8 * p + 4 + j]),
+                                                      false, false);
+      low[j] = __uint_as_float(v[0]);
+      high[j] = __uint_as_float(v[1]);
+    }
+    store(p * 16 + threadIdx.x % 64 / 32 * 8, low, high);
+  }
+}
+
+// Eight neighbouring elements of type dt from element i on at address p, of which `left` are in the row.
+__device__ __forceinline__ void store_eight(uint64_t p, int32_t dt, uint64_t i, f32x4 low, f32x4 high, uint32_t left) {
+  const uint64_t at = p + i * 2;
+  if (left >= 8 && dt != WC_FP32 && at % 16 == 0) {
+    u32x4 h;
+    if (dt == WC_BF16)
+      h = {floats_to_bf16(low[0], low[1]), floats_to_bf16(low[2], low[3]), floats_to_bf16(high[0], high[1]),
+           floats_to_bf16(high[2], high[3])};
+    else
+      h = {float_to_fp16(low[0]) | float_to_fp16(low[1]) << 16, float_to_fp16(low[2]) | float_to_fp16(low[3]) << 16,
+           float_to_fp16(high[0]) | float_to_fp16(high[1]) << 16, float_to_fp16(high[2]) | float_to_fp16(high[3]) << 16};
+    *global<u32x4>(at) = h;
+    return;
+  }
+  store_four(p, dt, i, low, left);
+  if (left > 4) store_four(p, dt, i + 4, high, left - 4);
+}
+
+// The buffers of a tile's rows of codes and of scales (whole words).
 struct RowsOf {
   u32x4 codes, scales;
+  uint32_t pitch, step;  // of the scales
 };
-__device__ __forceinline__ RowsOf rows_of(uint64_t codes, uint32_t pitch, uint64_t scales, uint32_t scale_pitch,
+__device__ __forceinline__ RowsOf rows_of(uint64_t codes, uint32_t pitch, const Scales& s, uint32_t first,
                                           uint32_t rows, uint32_t blocks) {
-  return {rows_rsrc(codes, (rows - 1) * pitch + blocks * 16),
-          rows_rsrc(scales, (rows - 1) * scale_pitch + (blocks + 3) / 4 * 4)};
+  const uint32_t groups = (blocks + 15) / 16, words = (blocks + 3) / 4;
+  return {rows_rsrc(codes + first * uint64_t(pitch), (rows - 1) * pitch + blocks * 16),
+          rows_rsrc(s.at + first * uint64_t(s.pitch),
+                    (rows - 1) * s.pitch + (groups - 1) * s.step + words * 4 - (groups - 1) * 16),
+          s.pitch, s.step};
 }
+// A wave's loads of scales: row `row` of `from`, groups from the `first`-th on.
+struct ScaleLoad {
+  u32x4 rsrc;
+  uint32_t offset, step;
+  __device__ __forceinline__ void set(const RowsOf& from, uint32_t row) {
+    rsrc = from.scales;
+    step = from.step;
+    offset = row * from.pitch;
+  }
+  __device__ __forceinline__ void operator()(uint32_t group, uint32_t lds) const {
+    load_lds(rsrc, lds, offset + group * step);
+  }
+};
 
 }  // namespace wc_mx
