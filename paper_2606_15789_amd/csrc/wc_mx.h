@@ -6,6 +6,8 @@
 // is the sum over blocks as long as their scales keep it within 24 bits.
 #pragma once
 
+#include <type_traits>
+
 #include "wc_i8.h"
 
 namespace wc_mx {
@@ -107,11 +109,11 @@ __device__ __forceinline__ Eight<kType> load_eight(uint64_t p, int32_t left) {
   return e;
 }
 
-// A lane's four blocks of 512 of k of one row: step s has block 4 s + lane / 16, the scale in the
-// low byte of its word.
+// A lane's four blocks of 512 of k of one row: step s has block 4 s + lane / 16, and byte s of
+// `scales` is its scale.
 struct Part {
   u32x4 codes[4];
-  u32x4 scales;
+  uint32_t scales;
 };
 
 // Scales in groups of 16, those of 512 of k: rows of them `pitch` bytes apart, a row's groups `step`.
@@ -134,27 +136,33 @@ struct Row {
   uint64_t codes, scales;
   uint32_t step = 16;
 };
+// The scales of 512 of k as they lie, and the lane's of them.
 __device__ __forceinline__ u32x4 load_scales(uint64_t row, uint32_t step, uint32_t super, uint32_t blocks) {
-  const uint32_t g = threadIdx.x % 64 / 16;
-  const uint64_t scales = row + uint64_t(super) * step;
-  u32x4 s;
-  if (super * kSuper + kSuper <= blocks) {
-    s = *global<const u32x4u>(scales);
+  const uint64_t at = row + uint64_t(super) * step;
+  if (super * kSuper + kSuper <= blocks) return *global<const u32x4u>(at);
+  u32x4 s = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; i++) s[i] >>= 8 * g;
-  } else {
-#pragma unroll
-    for (uint32_t i = 0; i < 4; i++)
-      s[i] = global<const uint8_t>(scales)[min(4 * i + g, blocks - 1 - super * kSuper)];
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t g = threadIdx.x % 64 / 16;
+    s[i] = uint32_t(global<const uint8_t>(at)[min(4 * i + g, blocks - 1 - super * kSuper)]) << (8 * g);
   }
   return s;
 }
+__device__ __forceinline__ uint32_t lane_scales(u32x4 s) {
+  const uint32_t g = threadIdx.x % 64 / 16, pick = g | (g + 4) << 8;  // byte g of the second, then of the first
+  const uint32_t low = __builtin_amdgcn_perm(s[1], s[0], pick), high = __builtin_amdgcn_perm(s[3], s[2], pick);
+  return __builtin_amdgcn_perm(high, low, 0x05040100u);
+}
 // Blocks past the row's are its last one again; kZero: their codes are zeros, so that a product
 // with anything but a NaN scale, which the row then has in its last block too, adds nothing.
+struct RawPart {
+  u32x4 codes[4], scales;
+  __device__ __forceinline__ Part part() const { return {{codes[0], codes[1], codes[2], codes[3]}, lane_scales(scales)}; }
+};
 template <bool kZero>
-__device__ __forceinline__ Part load_part(const Row& r, uint32_t super, uint32_t blocks) {
+__device__ __forceinline__ RawPart load_raw(const Row& r, uint32_t super, uint32_t blocks) {
   const uint32_t g = threadIdx.x % 64 / 16;
-  Part p;
+  RawPart p;
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
     const uint32_t b = super * kSuper + 4 * i + g;
@@ -164,25 +172,48 @@ __device__ __forceinline__ Part load_part(const Row& r, uint32_t super, uint32_t
   p.scales = load_scales(r.scales, r.step, super, blocks);
   return p;
 }
-// The same of a row of elements (k of them; none: all zeros), quantised in registers.
+template <bool kZero>
+__device__ __forceinline__ Part load_part(const Row& r, uint32_t super, uint32_t blocks) {
+  return load_raw<kZero>(r, super, blocks).part();
+}
+// The same of a row of k elements, quantised in registers; zeros where the lane has no row.
 template <int kType>
-__device__ __forceinline__ Part quantize_part(uint64_t row, uint32_t super, uint32_t k) {
+__device__ __forceinline__ Part quantize_part(uint64_t row, bool live, uint32_t super, uint32_t k) {
   constexpr uint32_t kSize = kType == WC_FP32 ? 4 : 2;
-  const uint32_t g = threadIdx.x % 64 / 16;
-  Part p;
-#pragma unroll
-  for (uint32_t i = 0; i < 4; i++) {
-    const uint32_t at = (super * kSuper + 4 * i + g) * 32;
-    Eight<kType> e[4];
-#pragma unroll
-    for (uint32_t j = 0; j < 4; j++)
-      e[j] = load_eight<kType>(row + uint64_t(at + 8 * j) * kSize, int32_t(k) - int32_t(at + 8 * j));
+  const uint32_t first = super * (kSuper * 32) + threadIdx.x % 64 / 16 * 32;  // of step 0
+  Part p = {};
+  if (!live) return p;
+  const auto block = [&](const Eight<kType>(&e)[4], u32x4& codes, uint32_t step) {
     const uint32_t top = max(max(e[0].top(), e[1].top()), max(e[2].top(), e[3].top()));
     const uint32_t byte = scale_byte(float_bits<kType>(top));
     const float scale = scale_value(byte);
 #pragma unroll
-    for (int j = 0; j < 4; j++) p.codes[i][j] = byte == 255 ? 0u : e[j].codes(scale);
-    p.scales[i] = byte;
+    for (int j = 0; j < 4; j++) codes[j] = byte == 255 ? 0u : e[j].codes(scale);
+    p.scales |= byte << (8 * step);
+  };
+  if (super * (kSuper * 32) + kSuper * 32 <= k) {
+    Eight<kType> e[4][4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i++)
+#pragma unroll
+      for (uint32_t j = 0; j < 4; j++) e[i][j] = load_eight<kType>(row + uint64_t(first + 128 * i + 8 * j) * kSize, 8);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i++) block(e[i], p.codes[i], i);
+    return p;
+  }
+  // the row's last part: one block after another, to be short
+#pragma unroll 1
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t at = first + 128 * i;
+    Eight<kType> e[4];
+    u32x4 codes;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++)
+      e[j] = load_eight<kType>(row + uint64_t(at + 8 * j) * kSize, int32_t(k) - int32_t(at + 8 * j));
+    block(e, codes, i);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++)
+      if (i == j) p.codes[j] = codes;
   }
   return p;
 }
@@ -193,10 +224,14 @@ __device__ __forceinline__ i32x8 operand(u32x4 c) {
 // acc += 16 rows of W times 16 rows of x over 512 of k: lane l gets W rows 4 (l / 16) .. + 3 of
 // x row l mod 16.
 __device__ __forceinline__ void multiply(const Part& w, const Part& x, f32x4& acc) {
-#pragma unroll
-  for (int i = 0; i < 4; i++)
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w.codes[i]), operand(x.codes[i]), acc, 4,
-                                                           4, 0, int(w.scales[i]), 0, int(x.scales[i]));
+  const auto step = [&]<int kStep>(std::integral_constant<int, kStep>) {
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w.codes[kStep]), operand(x.codes[kStep]), acc, 4, 4,
+                                                           kStep, int(w.scales), kStep, int(x.scales));
+  };
+  step(std::integral_constant<int, 0>{});
+  step(std::integral_constant<int, 1>{});
+  step(std::integral_constant<int, 2>{});
+  step(std::integral_constant<int, 3>{});
 }
 
 // kN blocks of 16 rows of W by kM blocks of 16 rows of x, k split over the waves of a workgroup
@@ -243,6 +278,73 @@ struct Slim {
 #pragma unroll
       for (int j = 0; j < 4; j++) v[j] += sh.part[w][i][j];
     return v;
+  }
+};
+
+// 16 kN rows of W at a time by 16 rows of x, tile after tile: a workgroup's waves have parts of 512 of
+// k each, kHold of them at most, and keep x's in registers; the rows of the next part of W are on their
+// way while one is multiplied, across tiles too, so that reading W does not pause.
+template <int kN, int kWaves, int kHold>
+struct Stream {
+  static constexpr uint32_t kThreads = 64 * kWaves, kPart = kN * 64;
+  struct Shared {
+    f32x4 part[2][kWaves][kPart];
+  };
+  // Tiles first, first + step, ... below `tiles`: `rows_at(tile, w)` sets the lane's rows, `load_x(super)`
+  // gives x's Part, `finish(tile, sum)` is called by all threads, sum(i) for group i of the sums.
+  template <class RowsAt, class LoadX, class Finish>
+  static __device__ __forceinline__ void run(Shared& sh, uint32_t first, uint32_t tiles, uint32_t step,
+                                             uint32_t blocks, RowsAt rows_at, LoadX load_x, Finish finish) {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const uint32_t supers = (blocks + kSuper - 1) / kSuper;
+    const uint32_t count = supers > wave ? min((supers - wave + kWaves - 1) / kWaves, uint32_t(kHold)) : 0;
+    Row w[kN];
+    RawPart next[kN];
+    const auto load = [&](uint32_t i) {
+#pragma unroll
+      for (int n = 0; n < kN; n++) next[n] = load_raw<false>(w[n], wave + i * kWaves, blocks);
+    };
+    rows_at(first, w);
+    if (count) load(0);
+    Part x[kHold];
+#pragma unroll
+    for (uint32_t i = 0; i < kHold; i++) {
+      if (i < count) x[i] = load_x(wave + i * kWaves);
+      __builtin_amdgcn_sched_barrier(0);  // or the elements of all parts fill the registers at once
+    }
+    uint32_t turn = 0;
+    for (uint32_t tile = first; tile < tiles; tile += step, turn ^= 1) {
+      f32x4 acc[kN];
+#pragma unroll
+      for (int n = 0; n < kN; n++) acc[n] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (uint32_t i = 0; i < kHold; i++) {
+        if (i >= count) continue;
+        Part now[kN];
+#pragma unroll
+        for (int n = 0; n < kN; n++) now[n] = next[n].part();
+        if (i + 1 < count) {
+          load(i + 1);
+        } else if (tile + step < tiles) {
+          rows_at(tile + step, w);
+          load(0);
+        }
+#pragma unroll
+        for (int n = 0; n < kN; n++) multiply(now[n], x[i], acc[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < kN; n++) sh.part[turn][wave][n * 64 + lane] = acc[n];
+      // loads of the next tile stay on their way
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      finish(tile, [&](uint32_t i) {
+        f32x4 v = sh.part[turn][0][i];
+#pragma unroll
+        for (int u = 1; u < kWaves; u++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) v[j] += sh.part[turn][u][i][j];
+        return v;
+      });
+    }
   }
 };
 

@@ -128,8 +128,8 @@ __device__ __forceinline__ uint32_t job_of(const MatArgs& a, uint32_t tile) {
   return j;
 }
 
-// 16 kN rows of W by 16 kM rows of x, kType the elements of x, or 0: quantised.
-template <int kN, int kM, int kWaves, int kType>
+// 16 kN rows of W by 16 kM rows of quantised x.
+template <int kN, int kM, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs a) {
   using S = Slim<kN, kM, kWaves>;
   __shared__ typename S::Shared sh;
@@ -145,12 +145,8 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
   const uint32_t blocks = (a.k + 31) / 32;
   S::product(sh, w, blocks, [&](int m, uint32_t super) {
     const uint64_t row = m0 + 16 * uint32_t(m) + r;
-    if constexpr (kType == 0) {
-      const uint64_t at = min(row, uint64_t(a.m - 1));
-      return load_part<true>(Row{a.x + at * a.ldx, a.xs.at + at * a.xs.pitch, a.xs.step}, super, blocks);
-    } else {
-      return quantize_part<kType>(a.x + row * a.ldx, super, row < a.m ? a.k : 0);
-    }
+    const uint64_t at = min(row, uint64_t(a.m - 1));
+    return load_part<true>(Row{a.x + at * a.ldx, a.xs.at + at * a.xs.pitch, a.xs.step}, super, blocks);
   });
   for (uint32_t i = threadIdx.x; i < S::kPart; i += S::kThreads) {
     const uint32_t tile = i / 64, lane = i % 64;
@@ -162,6 +158,35 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
       for (uint32_t j = 0; j < 4; j++) v[j] += load_float(J.bias, J.bias_dtype, min(n + j, J.n - 1));
     store_four(J.y, J.y_dtype, m * J.ldy + n, v, J.n - n);
   }
+}
+
+// Up to 16 rows of x of kType elements, 16 kN rows of W at a time.
+template <int kN, int kWaves, int kHold, int kType>
+__global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_stream_kernel(MatArgs a, uint32_t tiles) {
+  using S = Stream<kN, kWaves, kHold>;
+  __shared__ typename S::Shared sh;
+  const uint32_t r = threadIdx.x % 16, blocks = (a.k + 31) / 32;
+  S::run(
+      sh, blockIdx.x, tiles, gridDim.x, blocks,
+      [&](uint32_t tile, Row(&w)[kN]) {
+        const MatJob& J = a.job[job_of(a, tile)];
+#pragma unroll
+        for (uint32_t n = 0; n < kN; n++) {
+          const uint64_t row = min((tile - J.first) * (16 * kN) + 16 * n + r, J.n - 1);
+          w[n] = {J.w + row * J.ldw, J.scales.at + row * J.scales.pitch, J.scales.step};
+        }
+      },
+      [&](uint32_t super) { return quantize_part<kType>(a.x + r * a.ldx, r < a.m, super, a.k); },
+      [&](uint32_t tile, auto sum) {
+        const MatJob& J = a.job[job_of(a, tile)];
+        const uint32_t m = threadIdx.x % 16, n = (tile - J.first) * (16 * kN) + threadIdx.x / 64 * 16 + threadIdx.x % 64 / 16 * 4;
+        if (threadIdx.x >= S::kPart || m >= a.m || n >= J.n) return;
+        f32x4 v = sum(threadIdx.x);
+        if (J.bias)
+#pragma unroll
+          for (uint32_t j = 0; j < 4; j++) v[j] += load_float(J.bias, J.bias_dtype, min(n + j, J.n - 1));
+        store_four(J.y, J.y_dtype, m * J.ldy + n, v, J.n - n);
+      });
 }
 
 // A tile of y, or of its sums over one part of k (blockIdx.y).
@@ -278,7 +303,9 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   return !(rows >> 27);
 }
 
-enum class Kernel { kSlim, kTile64, kTile128, kTile256 };
+// k up to which the waves of a workgroup hold x in registers
+constexpr uint32_t kStreamK = 16384;
+enum class Kernel { kStream, kSlim, kTile64, kTile128, kTile256 };
 using Tile64 = MxTile<64, 64, 1, 2, 128, 4>;
 using Tile128 = MxTile<128, 128, 2, 2, 128, 2>;
 using Tile256 = MxTile<256, 256, 2, 4, 128, 2>;
@@ -291,8 +318,8 @@ void with_tile(Kernel k, F f) {
     default: return;
   }
 }
-uint32_t tiles_of(Kernel k, uint32_t m, uint32_t n) {
-  uint32_t tiles = (n + 31) / 32;
+uint32_t tiles_of(Kernel k, bool narrow, uint32_t m, uint32_t n) {
+  uint32_t tiles = k == Kernel::kStream && narrow ? (n + 15) / 16 : (n + 31) / 32;
   with_tile(k, [&](auto t) { tiles = (m + t.kRows - 1) / t.kRows * ((n + t.kCols - 1) / t.kCols); });
   return tiles;
 }
@@ -306,7 +333,11 @@ struct Plan {
   uint64_t scales;    // bytes of copies of scales
 };
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
-  Plan p{Kernel::kSlim, m <= 16, 1, 0, 0};
+  Plan p{Kernel::kSlim, false, 1, 0, 0};
+  if (m <= 16 && k <= kStreamK) {
+    p.kernel = Kernel::kStream;
+    p.inside = true;
+  }
   if (m <= 64) return p;
   bool narrow = m < (1u << 24);
   uint64_t rows = 0;
@@ -335,10 +366,21 @@ bool workspace_ok(const void* p, uint64_t bytes, uint64_t need) {
   return need == 0 || (!off(p, 256) && bytes >= need);
 }
 
-template <int kM, int kType>
+template <int kM>
 void start_slim(uint32_t tiles, const MatArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((wc_matmul_mx_slim_kernel<2, kM, 8, kType>), dim3(tiles, (a.m + 16 * kM - 1) / (16 * kM)),
-                     dim3(512), 0, st, a);
+  hipLaunchKernelGGL((wc_matmul_mx_slim_kernel<2, kM, 8>), dim3(tiles, (a.m + 16 * kM - 1) / (16 * kM)), dim3(512), 0,
+                     st, a);
+}
+template <int kN, int kWaves, int kHold, int kType>
+void start_stream(uint32_t tiles, const MatArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, kWaves, kHold, kType>), dim3(std::min(tiles, 256u * 16 / kWaves)),
+                     dim3(64 * kWaves), 0, st, a, tiles);
+}
+template <int kType>
+void start_stream(uint32_t tiles, const MatArgs& a, hipStream_t st) {
+  if (a.k <= 4096) start_stream<2, 8, 1, kType>(tiles, a, st);
+  else if (a.k <= 8192) start_stream<2, 16, 1, kType>(tiles, a, st);
+  else start_stream<1, 16, 2, kType>(tiles, a, st);
 }
 
 // The products of x: rows of codes and scales, or (x_dtype) of elements; ldx in bytes.
@@ -359,14 +401,21 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
     a.job[i] = {reinterpret_cast<uint64_t>(J.w), reinterpret_cast<uint64_t>(J.bias),
                 reinterpret_cast<uint64_t>(J.y), J.ldw, J.ldy,
                 {reinterpret_cast<uint64_t>(J.scale), uint32_t(J.lds), 16}, part, J.n, tiles, J.bias_dtype, J.y_dtype};
-    tiles += tiles_of(p.kernel, m, J.n);
+    tiles += tiles_of(p.kernel, k > 8192, m, J.n);
     widest = std::max(widest, J.n);
     if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 7) & ~7u) * 4 * p.splits);
-    if (p.kernel != Kernel::kSlim && !whole_words(J.scale, J.lds, k)) {
+    if (p.kernel >= Kernel::kTile64 && !whole_words(J.scale, J.lds, k)) {
       a.job[i].scales = own_scales(copy, J.n, k);
       if (!launch_copy_scales(J.scale, J.lds, J.n, 0, J.n, k, a.job[i].scales, st)) return WC_EHIP;
       copy += pad256(own_scales_bytes(J.n, k));
     }
+  }
+  if (p.kernel == Kernel::kStream) {
+    a.m = m;
+    if (x_dtype == WC_BF16) start_stream<WC_BF16>(tiles, a, st);
+    else if (x_dtype == WC_FP16) start_stream<WC_FP16>(tiles, a, st);
+    else start_stream<WC_FP32>(tiles, a, st);
+    return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
   }
   if (p.kernel != Kernel::kSlim) {
     a.m = m;
@@ -384,12 +433,9 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
   constexpr uint32_t kSlice = 65535u * 64;
   for (uint32_t m0 = 0; m0 < m; m0 += kSlice) {
     a.m = std::min(m - m0, kSlice);
-    if (x_dtype == WC_BF16) start_slim<1, WC_BF16>(tiles, a, st);
-    else if (x_dtype == WC_FP16) start_slim<1, WC_FP16>(tiles, a, st);
-    else if (x_dtype == WC_FP32) start_slim<1, WC_FP32>(tiles, a, st);
-    else if (a.m <= 16) start_slim<1, 0>(tiles, a, st);
-    else if (a.m <= 32) start_slim<2, 0>(tiles, a, st);
-    else start_slim<4, 0>(tiles, a, st);
+    if (a.m <= 16) start_slim<1>(tiles, a, st);
+    else if (a.m <= 32) start_slim<2>(tiles, a, st);
+    else start_slim<4>(tiles, a, st);
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
     a.x += uint64_t(a.m) * ldx;
     a.xs.at += uint64_t(a.m) * a.xs.pitch;
@@ -475,7 +521,7 @@ extern "C" wc_status wc_dequantize_mx(const uint8_t* dev_q, uint64_t ldq, const 
 // MXFP4.  Rows of x of matmul's own may need copies of their scales too: room for them always.
 namespace {
 uint64_t x_scales_bytes(const Plan& p, uint32_t m, uint32_t k) {
-  return p.kernel == Kernel::kSlim ? 0 : pad256(own_scales_bytes(m, k));
+  return p.kernel < Kernel::kTile64 ? 0 : pad256(own_scales_bytes(m, k));
 }
 }  // namespace
 
@@ -496,6 +542,7 @@ extern "C" wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint
   if (m == 0) return WC_OK;
   if (!coded_ok(dev_q, ldq, dev_scale, lds, k)) return WC_EINVAL;
   Plan p = plan_of(m, k, n_jobs, jobs);
+  if (p.kernel == Kernel::kStream) p.kernel = Kernel::kSlim;
   if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p) + x_scales_bytes(p, m, k))) return WC_EINVAL;
   if (ldq > (1u << 22) || lds > (1u << 22)) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);

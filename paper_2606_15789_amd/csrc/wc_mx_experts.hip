@@ -159,9 +159,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs
     w[n] = row_of(a.gate, e, row, blocks);
     w[n + 2] = row_of(a.up, e, row, blocks);
   }
-  const uint32_t mine = slot_of(c, a, r, e) >= 0 ? a.hidden : 0;
+  const bool mine = slot_of(c, a, r, e) >= 0;
   S::product(sh, w, blocks, [&](int, uint32_t super) {
-    return quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), super, mine);
+    return quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), mine, super, a.hidden);
   });
   if (threadIdx.x < 128) {
     const uint32_t n = threadIdx.x / 64, lane = threadIdx.x % 64;
