@@ -131,20 +131,32 @@ inline Scales own_scales(uint64_t at, uint64_t rows, uint64_t k) {
   return {at, 16, uint32_t(rows * 16)};
 }
 
-// The row of an MXFP4 matrix that a lane multiplies.
+// The row of an MXFP4 matrix that a lane multiplies: `off` and `scale_off` bytes from `codes` and
+// `scales` (where those are the same for all lanes, addresses take one register a lane).
 struct Row {
   uint64_t codes, scales;
-  uint32_t step = 16;
+  uint32_t step, off, scale_off;
 };
+__device__ __forceinline__ uint64_t uniform(uint64_t v) {
+  return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(v >> 32)))) << 32 |
+         uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(v)));
+}
+// Row min(first + r, n - 1) of a matrix; `first` the same for all lanes, rows at most 2^27 bytes apart.
+__device__ __forceinline__ Row row_at(uint64_t codes, uint64_t pitch, const Scales& s, uint32_t first, uint32_t r,
+                                      uint32_t n) {
+  const uint32_t from = min(first, n - 1), in = min(r, n - 1 - from);
+  return {uniform(codes + from * pitch), uniform(s.at + from * uint64_t(s.pitch)), s.step, in * uint32_t(pitch),
+          in * s.pitch};
+}
 // The scales of 512 of k as they lie, and the lane's of them.
-__device__ __forceinline__ u32x4 load_scales(uint64_t row, uint32_t step, uint32_t super, uint32_t blocks) {
-  const uint64_t at = row + uint64_t(super) * step;
-  if (super * kSuper + kSuper <= blocks) return *global<const u32x4u>(at);
+__device__ __forceinline__ u32x4 load_scales(const Row& r, uint32_t super, uint32_t blocks) {
+  const uint64_t at = r.scales + uint64_t(super) * r.step;
+  if (super * kSuper + kSuper <= blocks) return *global<const u32x4u>(at + r.scale_off);
   u32x4 s = {0, 0, 0, 0};
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
     const uint32_t g = threadIdx.x % 64 / 16;
-    s[i] = uint32_t(global<const uint8_t>(at)[min(4 * i + g, blocks - 1 - super * kSuper)]) << (8 * g);
+    s[i] = uint32_t(*global<const uint8_t>(at + (r.scale_off + min(4 * i + g, blocks - 1 - super * kSuper)))) << (8 * g);
   }
   return s;
 }
@@ -166,10 +178,10 @@ __device__ __forceinline__ RawPart load_raw(const Row& r, uint32_t super, uint32
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
     const uint32_t b = super * kSuper + 4 * i + g;
-    p.codes[i] = global<const u32x4>(r.codes)[min(b, blocks - 1)];
+    p.codes[i] = *global<const u32x4>(r.codes + (r.off + min(b, blocks - 1) * 16));
     if (kZero && b >= blocks) p.codes[i] = u32x4{0, 0, 0, 0};
   }
-  p.scales = load_scales(r.scales, r.step, super, blocks);
+  p.scales = load_scales(r, super, blocks);
   return p;
 }
 template <bool kZero>
@@ -192,13 +204,19 @@ __device__ __forceinline__ Part quantize_part(uint64_t row, bool live, uint32_t 
     p.scales |= byte << (8 * step);
   };
   if (super * (kSuper * 32) + kSuper * 32 <= k) {
-    Eight<kType> e[4][4];
+    constexpr uint32_t kOnce = kType == WC_FP32 ? 1 : 4;  // blocks in registers at once
 #pragma unroll
-    for (uint32_t i = 0; i < 4; i++)
+    for (uint32_t i0 = 0; i0 < 4; i0 += kOnce) {
+      Eight<kType> e[kOnce][4];
 #pragma unroll
-      for (uint32_t j = 0; j < 4; j++) e[i][j] = load_eight<kType>(row + uint64_t(first + 128 * i + 8 * j) * kSize, 8);
+      for (uint32_t i = 0; i < kOnce; i++)
 #pragma unroll
-    for (uint32_t i = 0; i < 4; i++) block(e[i], p.codes[i], i);
+        for (uint32_t j = 0; j < 4; j++)
+          e[i][j] = load_eight<kType>(row + uint64_t(first + 128 * (i0 + i) + 8 * j) * kSize, 8);
+#pragma unroll
+      for (uint32_t i = 0; i < kOnce; i++) block(e[i], p.codes[i0 + i], i0 + i);
+      if (kOnce < 4) __builtin_amdgcn_sched_barrier(0);
+    }
     return p;
   }
   // the row's last part: one block after another, to be short
@@ -282,22 +300,24 @@ struct Slim {
 };
 
 // 16 kN rows of W at a time by 16 rows of x, tile after tile: a workgroup's waves have parts of 512 of
-// k each, kHold of them at most, and keep x's in registers; the rows of the next part of W are on their
-// way while one is multiplied, across tiles too, so that reading W does not pause.
+// k each, kHold of them at most with x's kept in registers, or (0) any number with x's in LDS; the
+// rows of the next part of W are on their way while one is multiplied, across tiles too, so that
+// reading W does not pause.
 template <int kN, int kWaves, int kHold>
 struct Stream {
   static constexpr uint32_t kThreads = 64 * kWaves, kPart = kN * 64;
   struct Shared {
     f32x4 part[2][kWaves][kPart];
   };
-  // Tiles first, first + step, ... below `tiles`: `rows_at(tile, w)` sets the lane's rows, `load_x(super)`
-  // gives x's Part, `finish(tile, sum)` is called by all threads, sum(i) for group i of the sums.
+  // Tiles first, first + step, ... below `tiles`: `rows_at(tile, w)` sets the lane's rows, `load_x(i,
+  // super)` gives part i of the wave's of x (kHold: once), `finish(tile, sum)` is called by all threads,
+  // sum(i) for group i of the sums.
   template <class RowsAt, class LoadX, class Finish>
   static __device__ __forceinline__ void run(Shared& sh, uint32_t first, uint32_t tiles, uint32_t step,
                                              uint32_t blocks, RowsAt rows_at, LoadX load_x, Finish finish) {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const uint32_t supers = (blocks + kSuper - 1) / kSuper;
-    const uint32_t count = supers > wave ? min((supers - wave + kWaves - 1) / kWaves, uint32_t(kHold)) : 0;
+    const uint32_t count = supers > wave ? (supers - wave + kWaves - 1) / kWaves : 0;
     Row w[kN];
     RawPart next[kN];
     const auto load = [&](uint32_t i) {
@@ -306,10 +326,10 @@ struct Stream {
     };
     rows_at(first, w);
     if (count) load(0);
-    Part x[kHold];
+    Part held[kHold ? kHold : 1];
 #pragma unroll
     for (uint32_t i = 0; i < kHold; i++) {
-      if (i < count) x[i] = load_x(wave + i * kWaves);
+      if (i < count) held[i] = load_x(i, wave + i * kWaves);
       __builtin_amdgcn_sched_barrier(0);  // or the elements of all parts fill the registers at once
     }
     uint32_t turn = 0;
@@ -317,20 +337,23 @@ struct Stream {
       f32x4 acc[kN];
 #pragma unroll
       for (int n = 0; n < kN; n++) acc[n] = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (uint32_t i = 0; i < kHold; i++) {
-        if (i >= count) continue;
+      const auto part = [&](uint32_t i, const Part& x) {
         Part now[kN];
 #pragma unroll
         for (int n = 0; n < kN; n++) now[n] = next[n].part();
-        if (i + 1 < count) {
-          load(i + 1);
-        } else if (tile + step < tiles) {
-          rows_at(tile + step, w);
-          load(0);
-        }
+        // one copy of the loads
+        const bool over = i + 1 == count;
+        if (over && tile + step < tiles) rows_at(tile + step, w);
+        if (!over || tile + step < tiles) load(over ? 0 : i + 1);
 #pragma unroll
-        for (int n = 0; n < kN; n++) multiply(now[n], x[i], acc[n]);
+        for (int n = 0; n < kN; n++) multiply(now[n], x, acc[n]);
+      };
+      if constexpr (kHold > 0) {
+#pragma unroll
+        for (uint32_t i = 0; i < kHold; i++)
+          if (i < count) part(i, held[i]);
+      } else {
+        for (uint32_t i = 0; i < count; i++) part(i, load_x(i, wave + i * kWaves));
       }
 #pragma unroll
       for (int n = 0; n < kN; n++) sh.part[turn][wave][n * 64 + lane] = acc[n];

@@ -140,13 +140,13 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
 #pragma unroll
   for (uint32_t n = 0; n < kN; n++) {
     const uint64_t row = min(n0 + 16 * n + r, J.n - 1);
-    w[n] = {J.w + row * J.ldw, J.scales.at + row * J.scales.pitch, J.scales.step};
+    w[n] = {J.w + row * J.ldw, J.scales.at + row * J.scales.pitch, J.scales.step, 0, 0};
   }
   const uint32_t blocks = (a.k + 31) / 32;
   S::product(sh, w, blocks, [&](int m, uint32_t super) {
     const uint64_t row = m0 + 16 * uint32_t(m) + r;
     const uint64_t at = min(row, uint64_t(a.m - 1));
-    return load_part<true>(Row{a.x + at * a.ldx, a.xs.at + at * a.xs.pitch, a.xs.step}, super, blocks);
+    return load_part<true>(Row{a.x + at * a.ldx, a.xs.at + at * a.xs.pitch, a.xs.step, 0, 0}, super, blocks);
   });
   for (uint32_t i = threadIdx.x; i < S::kPart; i += S::kThreads) {
     const uint32_t tile = i / 64, lane = i % 64;
@@ -171,12 +171,9 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_stream_kernel(MatArg
       [&](uint32_t tile, Row(&w)[kN]) {
         const MatJob& J = a.job[job_of(a, tile)];
 #pragma unroll
-        for (uint32_t n = 0; n < kN; n++) {
-          const uint64_t row = min((tile - J.first) * (16 * kN) + 16 * n + r, J.n - 1);
-          w[n] = {J.w + row * J.ldw, J.scales.at + row * J.scales.pitch, J.scales.step};
-        }
+        for (uint32_t n = 0; n < kN; n++) w[n] = row_at(J.w, J.ldw, J.scales, (tile - J.first) * (16 * kN) + 16 * n, r, J.n);
       },
-      [&](uint32_t super) { return quantize_part<kType>(a.x + r * a.ldx, r < a.m, super, a.k); },
+      [&](uint32_t, uint32_t super) { return quantize_part<kType>(a.x + r * a.ldx, r < a.m, super, a.k); },
       [&](uint32_t tile, auto sum) {
         const MatJob& J = a.job[job_of(a, tile)];
         const uint32_t m = threadIdx.x % 16, n = (tile - J.first) * (16 * kN) + threadIdx.x / 64 * 16 + threadIdx.x % 64 / 16 * 4;
@@ -334,12 +331,13 @@ struct Plan {
 };
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   Plan p{Kernel::kSlim, false, 1, 0, 0};
-  if (m <= 16 && k <= kStreamK) {
+  bool near = true, narrow = m < (1u << 24);
+  for (uint32_t i = 0; i < n_jobs; i++) near = near && jobs[i].ldw <= (1u << 27) && jobs[i].lds <= (1u << 27);
+  if (m <= 16 && k <= kStreamK && near) {
     p.kernel = Kernel::kStream;
     p.inside = true;
   }
   if (m <= 64) return p;
-  bool narrow = m < (1u << 24);
   uint64_t rows = 0;
   for (uint32_t i = 0; i < n_jobs; i++) {
     rows += jobs[i].n;

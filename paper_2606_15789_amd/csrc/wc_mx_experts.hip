@@ -36,9 +36,11 @@ struct ExpertArgs {
   int32_t dtype;
   Bank gate, up, down;
 };
-__device__ __forceinline__ Row row_of(const Bank& b, uint32_t e, uint32_t row, uint32_t blocks) {
-  return {b.w + e * b.stride + uint64_t(row) * (blocks * 16),
-          b.scales.at + e * b.scale_stride + uint64_t(row) * b.scales.pitch, b.scales.step};
+// Row min(first + r, n - 1) of expert e's matrix.
+__device__ __forceinline__ Row row_of(const Bank& b, uint32_t e, uint32_t first, uint32_t r, uint32_t n,
+                                      uint32_t blocks) {
+  return row_at(b.w + e * b.stride, blocks * 16, Scales{b.scales.at + e * b.scale_stride, b.scales.pitch, b.scales.step},
+                first, r, n);
 }
 
 // g / (1 + exp(-g)), with an exponential of 1 ulp and a rounded division
@@ -55,30 +57,17 @@ __device__ __forceinline__ void store_h_scale(const ExpertArgs& a, uint64_t at, 
   if (block + 1 == (a.ffn + 31) / 32)
     for (uint32_t i = 1; (block + i) % 4; i++) to[i] = 0;
 }
-// Four lanes to a row of 32 values of h in LDS, block `block` of row `at`: its codes and scale, eight
-// codes to a lane, all four lanes of a row alive or none.
-__device__ __forceinline__ void quantize_h(const ExpertArgs& a, const float* row, uint64_t at, uint32_t block,
-                                           bool live) {
-  const uint32_t q = threadIdx.x % 4;
-  Eight<WC_FP32> e;
-#pragma unroll
-  for (int i = 0; i < 8; i++) e.v[i] = __float_as_uint(row[q * 8 + i]);
-  uint32_t top = e.top();
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xF, 0xF, false)));  // lane ^ 1
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xF, 0xF, false)));  // lane ^ 2
-  if (!live) return;
-  const uint32_t byte = scale_byte(top);
-  global<uint32_t>(h_codes(a, at, block))[q] = byte == 255 ? 0u : e.codes(scale_value(byte));
-  if (q == 0) store_h_scale(a, at, block, byte);
-}
-constexpr int kRowH = 36;  // floats of a row of h in LDS
-
 // --- few tokens ---------------------------------------------------------------
 
-constexpr uint32_t kFew = 16;  // tokens
+constexpr uint32_t kFew = 16;            // tokens
+constexpr uint32_t kFewHidden = 8192;    // width of x that a workgroup holds in LDS
 constexpr int kFewWaves = 8;
 
-inline bool is_few(uint64_t tokens, uint64_t k) { return tokens <= kFew && k <= wc_choose::kMaxChosen; }
+inline bool is_few(uint64_t tokens, uint64_t k, uint64_t hidden) {
+  return tokens <= kFew && k <= wc_choose::kMaxChosen && hidden <= kFewHidden;
+}
+// The tokens' experts in a workgroup's LDS.
+constexpr uint32_t kFewThreads = 64 * kFewWaves;
 struct Chosen {
   int32_t ids[kFew][wc_choose::kMaxChosen];
   float weights[kFew][wc_choose::kMaxChosen];
@@ -88,9 +77,9 @@ struct Chosen {
 };
 // Lists the experts that ids name.
 __device__ __forceinline__ void list_experts(Chosen& c, const ExpertArgs& a) {
-  for (uint32_t e = threadIdx.x; e < kMaxExperts; e += 64 * kFewWaves) c.hit[e] = 0;
+  for (uint32_t e = threadIdx.x; e < kMaxExperts; e += kFewThreads) c.hit[e] = 0;
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < a.slots; i += 64 * kFewWaves) {
+  for (uint32_t i = threadIdx.x; i < a.slots; i += kFewThreads) {
     const int32_t id = c.ids[i / a.k][i % a.k];
     if (id >= 0) c.hit[id] = 1;
   }
@@ -108,7 +97,7 @@ __device__ __forceinline__ void list_experts(Chosen& c, const ExpertArgs& a) {
   __syncthreads();
 }
 __device__ __forceinline__ void load_choice(Chosen& c, const ExpertArgs& a) {
-  for (uint32_t i = threadIdx.x; i < a.slots; i += 64 * kFewWaves) {
+  for (uint32_t i = threadIdx.x; i < a.slots; i += kFewThreads) {
     const int32_t id = global<const int32_t>(a.ids)[i];
     c.ids[i / a.k][i % a.k] = id < 0 ? -1 : min(id, int32_t(a.experts) - 1);
     c.weights[i / a.k][i % a.k] = global<const float>(a.weights)[i];
@@ -123,92 +112,177 @@ __device__ __forceinline__ int32_t slot_of(const Chosen& c, const ExpertArgs& a,
   return slot;
 }
 
-// 32 columns of h for all tokens of one expert, quantised.  kPer: registers of logits to a
-// lane of the choice, 0 where the ids are given.
+// The greatest of the four lanes 16 apart that hold a token's columns.
+__device__ __forceinline__ uint32_t top_of_column(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(b[0], b[1]);
+}
+// A wave's 32 columns of h for 16 rows of x: the lane's two groups of four from gate's and up's sums
+// (columns 4 (lane / 16) on, and 16 further), quantised and stored for row `at` if `live`.
+__device__ __forceinline__ void store_h(const ExpertArgs& a, const f32x4 (&g)[2], const f32x4 (&u)[2], uint64_t at,
+                                        uint32_t block, bool live) {
+  const uint32_t quarter = threadIdx.x % 64 / 16;
+  float h[2][4];
+  uint32_t top = 0;
+#pragma unroll
+  for (uint32_t n = 0; n < 2; n++)
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) {
+      const float v = silu(g[n][j]) * u[n][j];
+      h[n][j] = block * 32 + 16 * n + 4 * quarter + j < a.ffn ? v : 0.0f;
+      top = max(top, __float_as_uint(h[n][j]) & 0x7FFFFFFFu);
+    }
+  const uint32_t byte = scale_byte(top_of_column(top));
+  const float scale = scale_value(byte);
+  if (!live) return;
+  const auto to = global<uint16_t>(h_codes(a, at, block)) + quarter;
+#pragma unroll
+  for (uint32_t n = 0; n < 2; n++) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[n][0], h[n][1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[n][2], h[n][3], scale, 1);
+    to[4 * n] = byte == 255 ? 0 : uint16_t(c);
+  }
+  if (quarter == 0) store_h_scale(a, at, block, byte);
+}
+
+// 32 columns of h at a time, for all tokens of one expert; the tokens are the columns of the matrix
+// instruction, whether they have the expert or not.  kPer: registers of logits to a lane of the
+// choice, 0 where the ids are given.
+using FewStream = Stream<4, kFewWaves, 0>;
+constexpr uint32_t kFewPart = 64 * 5 * 16;  // bytes in LDS of 512 of k of x: codes, then scales
 template <int kType, int kPer>
 __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
-  using S = Slim<4, 1, kFewWaves>;
+  using S = FewStream;
   __shared__ typename S::Shared sh;
   __shared__ Chosen c;
-  __shared__ float h[kFew][kRowH];
+  extern __shared__ u32x4 held[];  // x, by part, step and lane; only its own wave reads a part
+  const uint32_t lane = threadIdx.x % 64, r = lane % 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t blocks = (a.hidden + 31) / 32, supers = (blocks + kSuper - 1) / kSuper;
+  for (uint32_t super = wave; super < supers; super += kFewWaves) {
+    const Part p = quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), r < a.tokens, super, a.hidden);
+    u32x4* const to = held + super * (5 * 64);
+#pragma unroll
+    for (int i = 0; i < 4; i++) to[i * 64 + lane] = p.codes[i];
+    reinterpret_cast<uint32_t*>(to + 4 * 64)[lane] = p.scales;
+  }
   if constexpr (kPer > 0) {
-    __shared__ float scratch[kFewWaves][64 * (kPer ? kPer : 1)];
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    // the sums' place in LDS is free until then
+    static_assert(sizeof(float) * kFewWaves * 64 * (kPer ? kPer : 1) <= sizeof(sh));
+    float* const scratch = reinterpret_cast<float*>(&sh) + wave * (64 * kPer);
     for (uint32_t token = wave; token < a.tokens; token += kFewWaves) {
       int32_t id;
       float weight;
-      wc_choose::choose<64, kPer>(route, token, scratch[wave], id, weight);
+      wc_choose::choose<64, kPer>(route, token, scratch, id, weight);
       if (lane < a.k) {
         c.ids[token][lane] = id;
         c.weights[token][lane] = weight;
       }
-      if (blockIdx.x + blockIdx.y == 0) wc_choose::store_choice<64>(route, token, id, weight);
+      if (blockIdx.x == 0) wc_choose::store_choice<64>(route, token, id, weight);
     }
   } else {
     load_choice(c, a);
   }
   __syncthreads();
   list_experts(c, a);
-  if (blockIdx.y >= c.count) return;
-  const uint32_t e = c.list[blockIdx.y], r = threadIdx.x % 16, n0 = blockIdx.x * 32;
-  const uint32_t blocks = (a.hidden + 31) / 32;
-  Row w[4];
+  const uint32_t each = (a.ffn + 31) / 32, tiles = c.count * each;
+  if (blockIdx.x >= tiles) return;
+  S::run(
+      sh, blockIdx.x, tiles, gridDim.x, blocks,
+      [&](uint32_t tile, Row(&w)[4]) {
+        const uint32_t e = __builtin_amdgcn_readfirstlane(c.list[tile / each]), n0 = tile % each * 32;
 #pragma unroll
-  for (uint32_t n = 0; n < 2; n++) {
-    const uint32_t row = min(n0 + 16 * n + r, a.ffn - 1);
-    w[n] = row_of(a.gate, e, row, blocks);
-    w[n + 2] = row_of(a.up, e, row, blocks);
-  }
-  const bool mine = slot_of(c, a, r, e) >= 0;
-  S::product(sh, w, blocks, [&](int, uint32_t super) {
-    return quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), mine, super, a.hidden);
-  });
-  if (threadIdx.x < 128) {
-    const uint32_t n = threadIdx.x / 64, lane = threadIdx.x % 64;
-    const f32x4 g = S::sum(sh, threadIdx.x), u = S::sum(sh, 128 + threadIdx.x);
-#pragma unroll
-    for (uint32_t j = 0; j < 4; j++) {
-      const uint32_t column = 16 * n + lane / 16 * 4 + j;
-      h[lane % 16][column] = n0 + column < a.ffn ? silu(g[j]) * u[j] : 0.0f;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x < 64) {
-    const int32_t slot = slot_of(c, a, threadIdx.x / 4, e);
-    quantize_h(a, h[threadIdx.x / 4], uint32_t(slot), blockIdx.x, slot >= 0);
-  }
+        for (uint32_t n = 0; n < 2; n++) {
+          w[n] = row_of(a.gate, e, n0 + 16 * n, r, a.ffn, blocks);
+          w[n + 2] = row_of(a.up, e, n0 + 16 * n, r, a.ffn, blocks);
+        }
+      },
+      [&](uint32_t, uint32_t super) {
+        const u32x4* const from = held + super * (5 * 64);
+        return Part{{from[lane], from[64 + lane], from[128 + lane], from[192 + lane]},
+                    reinterpret_cast<const uint32_t*>(from + 4 * 64)[lane]};
+      },
+      [&](uint32_t tile, auto sum) {
+        if (wave) return;
+        const int32_t slot = slot_of(c, a, r, c.list[tile / each]);
+        const f32x4 g[2] = {sum(lane), sum(64 + lane)}, u[2] = {sum(128 + lane), sum(192 + lane)};
+        store_h(a, g, u, uint32_t(slot), tile % each, slot >= 0);
+      });
 }
 
-// 16 columns of y for all tokens: parts of 512 of every expert hit, spread over the waves.
+// 16 columns of y for all tokens: parts of 512 of every expert hit, spread over the waves.  Each
+// expert's first slot and weight of a token stand in a table in LDS.
 __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_down_kernel(ExpertArgs a) {
   __shared__ Chosen c;
   __shared__ f32x4 part[kFewWaves][64];
+  extern __shared__ float table[];  // weights, then slots
   load_choice(c, a);
   __syncthreads();
   list_experts(c, a);
+  float* const weights = table;
+  int16_t* const slots = reinterpret_cast<int16_t*>(table + c.count * 16);
+  for (uint32_t i = threadIdx.x; i < c.count * 16; i += kFewThreads) {
+    const int32_t e = c.list[i / 16];
+    const uint32_t token = i % 16;
+    int32_t slot = -1;
+    float weight = 0.0f;
+    if (token < a.tokens)
+      for (uint32_t j = 0; j < a.k; j++)
+        if (c.ids[token][j] == e) {
+          if (slot < 0) slot = int32_t(token * a.k + j);
+          weight += c.weights[token][j];
+        }
+    weights[i] = weight;
+    slots[i] = int16_t(slot);
+  }
+  __syncthreads();
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, r = lane % 16;
   const uint32_t blocks = (a.ffn + 31) / 32, supers = (blocks + kSuper - 1) / kSuper;
   const uint32_t n0 = blockIdx.x * 16, all = c.count * supers;
+  const uint32_t first = uint32_t(uint64_t(all) * wave / kFewWaves);
   const uint32_t last = uint32_t(uint64_t(all) * (wave + 1) / kFewWaves);
-  f32x4 y = {0, 0, 0, 0};
-  for (uint32_t u = uint32_t(uint64_t(all) * wave / kFewWaves); u < last;) {
-    const uint32_t at = u / supers, e = c.list[at], end = min(last, (at + 1) * supers);
-    const Row w = row_of(a.down, e, min(n0 + r, a.hidden - 1), blocks);
-    const int32_t slot = slot_of(c, a, r, e);
-    const Row x = {h_codes(a, max(slot, 0), 0), a.hs.at + uint64_t(max(slot, 0)) * a.hs.pitch, a.hs.step};
-    f32x4 acc = {0, 0, 0, 0};
-    for (; u < end; u++) {
-      const Part wp = load_part<false>(w, u - at * supers, blocks);
-      Part xp{};
-      if (slot >= 0) xp = load_part<true>(x, u - at * supers, blocks);
-      multiply(wp, xp, acc);
+  // the part that is on its way: of expert `at` of the list
+  uint32_t at = first / supers, super = first % supers;
+  int32_t slot = -1;
+  Row w{}, x{};
+  RawPart next_w, next_x = {};
+  const auto begin = [&] {
+    const uint32_t e = __builtin_amdgcn_readfirstlane(c.list[at]);
+    w = row_of(a.down, e, n0, r, a.hidden, blocks);
+    slot = slots[at * 16 + r];
+    x = {h_codes(a, max(slot, 0), 0), a.hs.at + uint64_t(max(slot, 0)) * a.hs.pitch, a.hs.step, 0, 0};
+  };
+  const auto load = [&] {
+    next_w = load_raw<false>(w, super, blocks);
+    if (slot >= 0) next_x = load_raw<true>(x, super, blocks);
+  };
+  f32x4 y = {0, 0, 0, 0}, acc = {0, 0, 0, 0};
+  if (first < last) {
+    begin();
+    load();
+  }
+  for (uint32_t u = first; u < last; u++) {
+    const Part wp = next_w.part(), xp = next_x.part();
+    const bool mine = slot >= 0;
+    const uint32_t here = at;
+    if (u + 1 < last) {
+      if (++super == supers) {
+        super = 0;
+        at++;
+        begin();
+      }
+      load();
     }
-    if (slot >= 0) {
-      float weight = 0.0f;
-      for (uint32_t j = 0; j < a.k; j++)
-        if (c.ids[r][j] == int32_t(e)) weight += c.weights[r][j];
+    multiply(wp, xp, acc);
+    if (at != here || u + 1 == last) {
+      // an expert that a token lacks adds nothing, not even a NaN of its scales
+      const float weight = weights[here * 16 + r];
+      if (mine)
 #pragma unroll
-      for (int i = 0; i < 4; i++) y[i] += weight * acc[i];
+        for (int i = 0; i < 4; i++) y[i] += weight * acc[i];
+      acc = f32x4{0, 0, 0, 0};
     }
   }
   part[wave][lane] = y;
@@ -253,7 +327,6 @@ template <int kM>
 __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a) {
   using S = Slim<4, kM, 8>;
   __shared__ typename S::Shared sh;
-  __shared__ float h[16 * kM][kRowH];
   const uint32_t block = a.first + blockIdx.x;
   if (block >= block_count(a)) return;
   const auto [e, first, last] = block_at(a, block);
@@ -261,31 +334,21 @@ __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a
   Row w[4];
 #pragma unroll
   for (uint32_t n = 0; n < 2; n++) {
-    const uint32_t row = min(n0 + 16 * n + r, a.ffn - 1);
-    w[n] = row_of(a.gate, e, row, blocks);
-    w[n + 2] = row_of(a.up, e, row, blocks);
+    w[n] = row_of(a.gate, e, n0 + 16 * n, r, a.ffn, blocks);
+    w[n + 2] = row_of(a.up, e, n0 + 16 * n, r, a.ffn, blocks);
   }
   Row x[kM];
 #pragma unroll
   for (uint32_t m = 0; m < kM; m++) {
     const uint64_t token = slot_at(a, min(first + 16 * m + r, last - 1)) / a.k;
-    x[m] = {a.xq + token * blocks * 16, a.xs.at + token * a.xs.pitch, a.xs.step};
+    x[m] = {a.xq + token * blocks * 16, a.xs.at + token * a.xs.pitch, a.xs.step, 0, 0};
   }
   S::product(sh, w, blocks, [&](int m, uint32_t super) { return load_part<true>(x[m], super, blocks); });
-  for (uint32_t i = threadIdx.x; i < 128 * kM; i += 512) {
-    const uint32_t tile = i / 64, lane = i % 64;
-    const f32x4 g = S::sum(sh, i), u = S::sum(sh, 128 * kM + i);
-#pragma unroll
-    for (uint32_t j = 0; j < 4; j++) {
-      const uint32_t column = tile / kM * 16 + lane / 16 * 4 + j;
-      h[tile % kM * 16 + lane % 16][column] = n0 + column < a.ffn ? silu(g[j]) * u[j] : 0.0f;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x < 64 * kM) {
-    const uint32_t row = threadIdx.x / 4;
-    quantize_h(a, h[row], first + row, blockIdx.y, first + row < last);
-  }
+  const uint32_t m = threadIdx.x / 64, place = first + 16 * m + r;
+  if (m >= kM) return;
+  const auto sum = [&](uint32_t n) { return S::sum(sh, (n * kM + m) * 64 + threadIdx.x % 64); };
+  const f32x4 g[2] = {sum(0), sum(1)}, u[2] = {sum(2), sum(3)};
+  store_h(a, g, u, place, blockIdx.y, place < last);
 }
 
 // down(h) of 32 columns for a block of places, stored by slot.
@@ -299,10 +362,10 @@ __global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs
   const uint32_t r = threadIdx.x % 16, n0 = blockIdx.y * 32, blocks = (a.ffn + 31) / 32;
   Row w[2];
 #pragma unroll
-  for (uint32_t n = 0; n < 2; n++) w[n] = row_of(a.down, e, min(n0 + 16 * n + r, a.hidden - 1), blocks);
+  for (uint32_t n = 0; n < 2; n++) w[n] = row_of(a.down, e, n0 + 16 * n, r, a.hidden, blocks);
   S::product(sh, w, blocks, [&](int m, uint32_t super) {
     const uint64_t place = min(first + 16 * uint32_t(m) + r, last - 1);
-    return load_part<true>(Row{h_codes(a, place, 0), a.hs.at + place * a.hs.pitch, a.hs.step}, super, blocks);
+    return load_part<true>(Row{h_codes(a, place, 0), a.hs.at + place * a.hs.pitch, a.hs.step, 0, 0}, super, blocks);
   });
   for (uint32_t i = threadIdx.x; i < S::kPart; i += 512) {
     const uint32_t tile = i / 64, lane = i % 64;
@@ -481,7 +544,7 @@ Workspace layout(uint64_t tokens, uint64_t k, uint32_t experts, uint32_t hidden,
   };
   w.hq = take(tokens * k * WC_MX_ROW_BYTES(ffn));
   w.hs = take(own_scales_bytes(tokens * k, ffn));
-  if (is_few(tokens, k)) return w;
+  if (is_few(tokens, k, hidden)) return w;
   w.table = take((1 + most_blocks(uint32_t(tokens * k), experts, 16)) * 16);
   w.xq = take(tokens * WC_MX_ROW_BYTES(hidden));
   w.xs = take(own_scales_bytes(tokens, hidden));
@@ -538,23 +601,28 @@ ExpertArgs args_of(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, 
   return a;
 }
 
+template <int kType, int kPer>
+void start_up(const ExpertArgs& a, const RouteArgs& route, hipStream_t st) {
+  const uint32_t most = (a.ffn + 31) / 32 * std::min(a.slots, a.experts);
+  hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, kPer>), dim3(std::min(most, 256u)), dim3(64 * kFewWaves),
+                     uint32_t(groups_of(a.hidden)) * kFewPart, st, a, route);
+}
 template <int kType>
 void start_up(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
-  const dim3 grid((a.ffn + 31) / 32, std::min(a.slots, a.experts)), block(64 * kFewWaves);
-  const RouteArgs r = route ? *route : RouteArgs{};
-  if (!route) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 0>), grid, block, 0, st, a, r);
-  else if (a.experts <= 64) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 1>), grid, block, 0, st, a, r);
-  else if (a.experts <= 128) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 2>), grid, block, 0, st, a, r);
-  else if (a.experts <= 256) hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 4>), grid, block, 0, st, a, r);
-  else hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, 8>), grid, block, 0, st, a, r);
+  if (!route) start_up<kType, 0>(a, RouteArgs{}, st);
+  else if (a.experts <= 64) start_up<kType, 1>(a, *route, st);
+  else if (a.experts <= 128) start_up<kType, 2>(a, *route, st);
+  else if (a.experts <= 256) start_up<kType, 4>(a, *route, st);
+  else start_up<kType, 8>(a, *route, st);
 }
-// Up to kFew tokens, by `route` or the ids that a names.
+// Few tokens, by `route` or the ids that a names.
 wc_status few(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
   if (a.dtype == WC_BF16) start_up<WC_BF16>(a, route, st);
   else if (a.dtype == WC_FP16) start_up<WC_FP16>(a, route, st);
   else start_up<WC_FP32>(a, route, st);
   if (hipGetLastError() != hipSuccess) return WC_EHIP;
-  hipLaunchKernelGGL(wc_moe_mx_down_kernel, dim3((a.hidden + 15) / 16), dim3(64 * kFewWaves), 0, st, a);
+  hipLaunchKernelGGL(wc_moe_mx_down_kernel, dim3((a.hidden + 15) / 16), dim3(64 * kFewWaves),
+                     std::min(a.slots, a.experts) * 16 * 6, st, a);
   return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
 }
 
@@ -626,7 +694,7 @@ uint32_t places(const ExpertArgs& a) {
 }
 
 wc_status experts(ExpertArgs a, const Workspace& w, const int32_t* offsets, hipStream_t st) {
-  if (is_few(a.tokens, a.k)) return few(a, nullptr, st);
+  if (is_few(a.tokens, a.k, a.hidden)) return few(a, nullptr, st);
   const uint32_t rows = places(a), most = uint32_t(most_blocks(a.slots, a.experts, rows));
   const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(offsets), a.experts, a.slots, rows, most};
   if (!launch_quantize(reinterpret_cast<const void*>(a.x), a.dtype, a.tokens, a.hidden, a.ldx,
@@ -652,7 +720,7 @@ wc_status experts(ExpertArgs a, const Workspace& w, const int32_t* offsets, hipS
 struct RouteSpace {
   uint64_t ids, weights, offsets, order, scratch, scratch_bytes, bytes;
 };
-RouteSpace route_layout(uint32_t tokens, const wc_route_params* p) {
+RouteSpace route_layout(uint32_t tokens, const wc_route_params* p, uint32_t hidden) {
   RouteSpace r{};
   const auto take = [&](uint64_t bytes) {
     const uint64_t here = r.bytes;
@@ -662,7 +730,7 @@ RouteSpace route_layout(uint32_t tokens, const wc_route_params* p) {
   const uint64_t slots = uint64_t(tokens) * p->k;
   r.ids = take(slots * 4);
   r.weights = take(slots * 4);
-  if (is_few(tokens, p->k)) return r;
+  if (is_few(tokens, p->k, hidden)) return r;
   r.offsets = take((p->experts + 1) * 4);
   r.order = take(slots * 4);
   wc_route_workspace_bytes(tokens, p, &r.scratch_bytes);
@@ -707,7 +775,7 @@ extern "C" wc_status wc_moe_mx_workspace_bytes(uint32_t tokens, const wc_route_p
   if (!bytes) return WC_EINVAL;
   *bytes = 0;
   if (!wc_choose::params_ok(tokens, p) || !sizes_ok(tokens, p->k, p->experts, hidden, ffn)) return WC_EINVAL;
-  *bytes = route_layout(tokens, p).bytes + layout(tokens, p->k, p->experts, hidden, ffn).bytes;
+  *bytes = route_layout(tokens, p, hidden).bytes + layout(tokens, p->k, p->experts, hidden, ffn).bytes;
   return WC_OK;
 }
 
@@ -726,13 +794,13 @@ extern "C" wc_status wc_moe_mx(const void* dev_x, int32_t dtype, uint32_t tokens
   if (off(dev_logits, size_of(logits_dtype)) || off(dev_workspace, 256) || workspace_bytes < need) return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const uint64_t ws = reinterpret_cast<uint64_t>(dev_workspace);
-  const RouteSpace r = route_layout(tokens, p);
+  const RouteSpace r = route_layout(tokens, p, hidden);
   const Workspace w = layout(tokens, p->k, p->experts, hidden, ffn);
   ExpertArgs a = args_of(dev_x, dtype, tokens, ldx, p->k, p->experts, hidden, ffn, gate, up, down, dev_y, ldy, w,
                          ws + r.bytes);
   a.ids = ws + r.ids;
   a.weights = ws + r.weights;
-  if (is_few(tokens, p->k)) {
+  if (is_few(tokens, p->k, hidden)) {
     const RouteArgs route = {reinterpret_cast<uint64_t>(dev_logits), reinterpret_cast<uint64_t>(dev_bias),
                              a.ids, a.weights, ld, tokens, p->experts, p->k, p->groups, p->top_groups,
                              p->group_top, 0, logits_dtype, p->score, p->renormalize, p->scale};
