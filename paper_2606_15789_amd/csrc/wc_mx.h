@@ -299,61 +299,46 @@ struct Slim {
   }
 };
 
-// 16 kN rows of W at a time by 16 rows of x, tile after tile: a workgroup's waves have parts of 512 of
-// k each, kHold of them at most with x's kept in registers, or (0) any number with x's in LDS; the
-// rows of the next part of W are on their way while one is multiplied, across tiles too, so that
-// reading W does not pause.
-template <int kN, int kWaves, int kHold>
+// 16 kN rows of W at a time by 16 rows of x, tile after tile: a workgroup's waves take parts of 512
+// of k in turn, and the rows of the next part of W are on their way while one is multiplied, across
+// tiles too, so that reading W does not pause.
+template <int kN, int kWaves>
 struct Stream {
   static constexpr uint32_t kThreads = 64 * kWaves, kPart = kN * 64;
   struct Shared {
     f32x4 part[2][kWaves][kPart];
   };
-  // Tiles first, first + step, ... below `tiles`: `rows_at(tile, w)` sets the lane's rows, `load_x(i,
-  // super)` gives part i of the wave's of x (kHold: once), `finish(tile, sum)` is called by all threads,
-  // sum(i) for group i of the sums.
+  // Tiles first, first + step, ... below `tiles`: `rows_at(tile, w)` sets the lane's rows, `load_x(super)`
+  // gives a part of x, `finish(tile, sum)` is called by all threads, sum(i) for group i of the sums.
   template <class RowsAt, class LoadX, class Finish>
   static __device__ __forceinline__ void run(Shared& sh, uint32_t first, uint32_t tiles, uint32_t step,
                                              uint32_t blocks, RowsAt rows_at, LoadX load_x, Finish finish) {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const uint32_t supers = (blocks + kSuper - 1) / kSuper;
-    const uint32_t count = supers > wave ? (supers - wave + kWaves - 1) / kWaves : 0;
     Row w[kN];
     RawPart next[kN];
-    const auto load = [&](uint32_t i) {
+    const auto load = [&](uint32_t super) {
 #pragma unroll
-      for (int n = 0; n < kN; n++) next[n] = load_raw<false>(w[n], wave + i * kWaves, blocks);
+      for (int n = 0; n < kN; n++) next[n] = load_raw<false>(w[n], super, blocks);
     };
     rows_at(first, w);
-    if (count) load(0);
-    Part held[kHold ? kHold : 1];
-#pragma unroll
-    for (uint32_t i = 0; i < kHold; i++) {
-      if (i < count) held[i] = load_x(i, wave + i * kWaves);
-      __builtin_amdgcn_sched_barrier(0);  // or the elements of all parts fill the registers at once
-    }
+    if (wave < supers) load(wave);
     uint32_t turn = 0;
     for (uint32_t tile = first; tile < tiles; tile += step, turn ^= 1) {
       f32x4 acc[kN];
 #pragma unroll
       for (int n = 0; n < kN; n++) acc[n] = f32x4{0, 0, 0, 0};
-      const auto part = [&](uint32_t i, const Part& x) {
+      for (uint32_t super = wave; super < supers; super += kWaves) {
+        const Part x = load_x(super);
         Part now[kN];
 #pragma unroll
         for (int n = 0; n < kN; n++) now[n] = next[n].part();
         // one copy of the loads
-        const bool over = i + 1 == count;
+        const bool over = super + kWaves >= supers;
         if (over && tile + step < tiles) rows_at(tile + step, w);
-        if (!over || tile + step < tiles) load(over ? 0 : i + 1);
+        if (!over || tile + step < tiles) load(over ? wave : super + kWaves);
 #pragma unroll
         for (int n = 0; n < kN; n++) multiply(now[n], x, acc[n]);
-      };
-      if constexpr (kHold > 0) {
-#pragma unroll
-        for (uint32_t i = 0; i < kHold; i++)
-          if (i < count) part(i, held[i]);
-      } else {
-        for (uint32_t i = 0; i < count; i++) part(i, load_x(i, wave + i * kWaves));
       }
 #pragma unroll
       for (int n = 0; n < kN; n++) sh.part[turn][wave][n * 64 + lane] = acc[n];
@@ -370,6 +355,22 @@ struct Stream {
     }
   }
 };
+
+// Parts of x in LDS, by part of k: codes by step and lane, then scales.
+constexpr uint32_t kHeldPart = 64 * 5 * 16;
+__device__ __forceinline__ void hold_part(u32x4* held, uint32_t super, const Part& p) {
+  const uint32_t lane = threadIdx.x % 64;
+  u32x4* const to = held + super * (kHeldPart / 16);
+#pragma unroll
+  for (int i = 0; i < 4; i++) to[i * 64 + lane] = p.codes[i];
+  reinterpret_cast<uint32_t*>(to + 4 * 64)[lane] = p.scales;
+}
+__device__ __forceinline__ Part held_part(const u32x4* held, uint32_t super) {
+  const uint32_t lane = threadIdx.x % 64;
+  const u32x4* const from = held + super * (kHeldPart / 16);
+  return {{from[lane], from[64 + lane], from[128 + lane], from[192 + lane]},
+          reinterpret_cast<const uint32_t*>(from + 4 * 64)[lane]};
+}
 
 // Four neighbouring elements of type dt from element i on at address p, of which `left` are in
 // the row.

@@ -160,12 +160,17 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
   }
 }
 
-// Up to 16 rows of x of kType elements, 16 kN rows of W at a time.
-template <int kN, int kWaves, int kHold, int kType>
-__global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_stream_kernel(MatArgs a, uint32_t tiles) {
-  using S = Stream<kN, kWaves, kHold>;
+// Up to 16 rows of x, 16 kN rows of W at a time.  kType: the elements of x, which the workgroup
+// quantises to LDS, or 0: quantised rows in memory.
+template <int kN, int kType>
+__global__ __launch_bounds__(512) void wc_matmul_mx_stream_kernel(MatArgs a, uint32_t tiles) {
+  using S = Stream<kN, 8>;
   __shared__ typename S::Shared sh;
-  const uint32_t r = threadIdx.x % 16, blocks = (a.k + 31) / 32;
+  extern __shared__ u32x4 held[];  // only its own wave reads a part
+  const uint32_t lane = threadIdx.x % 64, r = lane % 16, blocks = (a.k + 31) / 32;
+  if constexpr (kType != 0)
+    for (uint32_t super = threadIdx.x / 64; super < (blocks + kSuper - 1) / kSuper; super += 8)
+      hold_part(held, super, quantize_part<kType>(a.x + r * a.ldx, r < a.m, super, a.k));
   S::run(
       sh, blockIdx.x, tiles, gridDim.x, blocks,
       [&](uint32_t tile, Row(&w)[kN]) {
@@ -173,16 +178,20 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_stream_kernel(MatArg
 #pragma unroll
         for (uint32_t n = 0; n < kN; n++) w[n] = row_at(J.w, J.ldw, J.scales, (tile - J.first) * (16 * kN) + 16 * n, r, J.n);
       },
-      [&](uint32_t, uint32_t super) { return quantize_part<kType>(a.x + r * a.ldx, r < a.m, super, a.k); },
+      [&](uint32_t super) {
+        if constexpr (kType != 0) return held_part(held, super);
+        const uint64_t row = min(r, a.m - 1);
+        return load_part<true>(Row{a.x + row * a.ldx, a.xs.at + row * a.xs.pitch, a.xs.step, 0, 0}, super, blocks);
+      },
       [&](uint32_t tile, auto sum) {
         const MatJob& J = a.job[job_of(a, tile)];
-        const uint32_t m = threadIdx.x % 16, n = (tile - J.first) * (16 * kN) + threadIdx.x / 64 * 16 + threadIdx.x % 64 / 16 * 4;
-        if (threadIdx.x >= S::kPart || m >= a.m || n >= J.n) return;
+        const uint32_t n = (tile - J.first) * (16 * kN) + threadIdx.x / 64 * 16 + lane / 16 * 4;
+        if (threadIdx.x >= S::kPart || r >= a.m || n >= J.n) return;
         f32x4 v = sum(threadIdx.x);
         if (J.bias)
 #pragma unroll
           for (uint32_t j = 0; j < 4; j++) v[j] += load_float(J.bias, J.bias_dtype, min(n + j, J.n - 1));
-        store_four(J.y, J.y_dtype, m * J.ldy + n, v, J.n - n);
+        store_four(J.y, J.y_dtype, r * J.ldy + n, v, J.n - n);
       });
 }
 
@@ -300,26 +309,49 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   return !(rows >> 27);
 }
 
-// k up to which the waves of a workgroup hold x in registers
-constexpr uint32_t kStreamK = 16384;
-enum class Kernel { kStream, kSlim, kTile64, kTile128, kTile256 };
+// k up to which a workgroup holds 16 rows of x in LDS
+constexpr uint32_t kHeldK = 12288;
+enum class Kernel { kStream16, kStream32, kStream64, kSlim, kTile64, kTile128, kTile128Deep, kTile256 };
+constexpr bool streams(Kernel k) { return k <= Kernel::kStream64; }
 using Tile64 = MxTile<64, 64, 1, 2, 128, 4>;
 using Tile128 = MxTile<128, 128, 2, 2, 128, 2>;
+using Tile128Deep = MxTile<128, 128, 2, 2, 128, 4>;
 using Tile256 = MxTile<256, 256, 2, 4, 128, 2>;
 template <class F>
 void with_tile(Kernel k, F f) {
   switch (k) {
     case Kernel::kTile64: return f(Tile64{});
     case Kernel::kTile128: return f(Tile128{});
+    case Kernel::kTile128Deep: return f(Tile128Deep{});
     case Kernel::kTile256: return f(Tile256{});
     default: return;
   }
 }
-uint32_t tiles_of(Kernel k, bool narrow, uint32_t m, uint32_t n) {
-  uint32_t tiles = k == Kernel::kStream && narrow ? (n + 15) / 16 : (n + 31) / 32;
+uint32_t tiles_of(Kernel k, uint32_t m, uint32_t n) {
+  if (streams(k)) return (n + (16u << int(k)) - 1) / (16u << int(k));
+  uint32_t tiles = (n + 31) / 32;
   with_tile(k, [&](auto t) { tiles = (m + t.kRows - 1) / t.kRows * ((n + t.kCols - 1) / t.kCols); });
   return tiles;
 }
+
+// What a tile's kernel takes, in us: a stage of 256 of k, one workgroup's and two's where two fit a
+// compute unit, and all else of a round of workgroups.  Taken so that the least sum is the fastest
+// kernel, or within 5 % of it, at each of these (m, k, n; in us on tiles of 64, of 128 with two and
+// with four stages in LDS, and of 256, in the best number of parts of k; with the quantisation):
+//   32, 4096, 14336 12.9, 19.4, 16.8, 19.8; 64, 8192, 8192 17.9, 27.6, 20.6, 25.8; 100, 14336,
+//   4096 21.1, 38.4, 23.2, 36.6; 128, 8192, 28672 52.1, 44.2, 39.0, 50.6; 333, 5461, 2047 20.7,
+//   25.4, 24.0, 34.7; 512, 28672, 8192 143, 102, 91, 91; 1024, 4096, 4096 26.4, 22.9, 21.2,
+//   33.1; 1024, 8192, 28672 291, 186, 191, 137; 2000, 2048, 2048 18.5, 15.6, 15.1, 22.5; 4096, 4096,
+//   14336 302, 188, 227, 157; 8192, 8192, 28672 1864, 1227, 1467, 993.
+struct TileCost {
+  Kernel kernel;
+  double stage, stage_of_two, round;
+};
+constexpr TileCost kCosts[] = {{Kernel::kTile64, 0.37, 0.65, 3},
+                               {Kernel::kTile128, 1.05, 1.2, 4},
+                               {Kernel::kTile128Deep, 0.75, 0, 4},
+                               {Kernel::kTile256, 1.85, 0, 6}};
+constexpr double kUnits = 256, kJoin = 4.0, kBytesPerUs = 4e6, kReadPerUs = 5e6;
 
 // What a call does, by the sizes and alignments alone.
 struct Plan {
@@ -332,22 +364,48 @@ struct Plan {
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   Plan p{Kernel::kSlim, false, 1, 0, 0};
   bool near = true, narrow = m < (1u << 24);
-  for (uint32_t i = 0; i < n_jobs; i++) near = near && jobs[i].ldw <= (1u << 27) && jobs[i].lds <= (1u << 27);
-  if (m <= 16 && k <= kStreamK && near) {
-    p.kernel = Kernel::kStream;
-    p.inside = true;
-  }
-  if (m <= 64) return p;
-  uint64_t rows = 0;
+  uint64_t n = 0, sums = 0;
   for (uint32_t i = 0; i < n_jobs; i++) {
-    rows += jobs[i].n;
-    // offsets within a tile are 32-bit
-    narrow = narrow && jobs[i].ldw <= (1u << 22) && jobs[i].lds <= (1u << 22);
+    const wc_mx_job& J = jobs[i];
+    n += J.n;
+    sums += uint64_t(m) * ((J.n + 7) & ~7u) * 4;
+    // offsets within a row of tiles are 32-bit
+    near = near && J.ldw <= (1u << 27) && J.lds <= (1u << 27);
+    narrow = narrow && J.ldw <= (1u << 22) && J.lds <= (1u << 22);
   }
-  if (!narrow) return p;
-  const uint64_t large = uint64_t((m + 255) / 256) * ((rows + 255) / 256);
-  const uint64_t middle = uint64_t((m + 127) / 128) * ((rows + 127) / 128);
-  p.kernel = large >= 200 ? Kernel::kTile256 : middle >= 200 ? Kernel::kTile128 : Kernel::kTile64;
+  if (m <= 16 && near) {
+    // by the rows of W to a tile, 16, 32 and 64: 2 x 2048 -> 4096 5.0, 6.1, 7.5 us; 16 x 14336 -> 4096
+    // 13.3, 16.7, 24.5; 1 x 4096 -> 6144 8.3, 7.6, 9.6; 13 x 8192 -> 28672 36.8, 35.8, 34.1; 13 x
+    // 28672 -> 8192 36.2, 31.6, 46.8
+    p.kernel = n <= 4096 ? Kernel::kStream16 : n >= 16384 && k <= 8192 ? Kernel::kStream64 : Kernel::kStream32;
+    p.inside = k <= kHeldK;
+    return p;
+  }
+  // small products: 20 x 4096 -> 4096 9.2 us, on tiles of 64 10.2; 100 x 512 -> 512 6.0 and 6.6
+  if (!narrow || (m <= 32 && n * k <= (1u << 24)) || uint64_t(m) * n * k <= (1u << 25)) return p;
+  const uint32_t stages = (k + 255) / 256;
+  double best = 0;
+  for (const TileCost& c : kCosts) {
+    uint64_t tiles = 0, threads = 0;
+    with_tile(c.kernel, [&](auto t) { threads = t.kThreads; });
+    for (uint32_t i = 0; i < n_jobs; i++) tiles += tiles_of(c.kernel, m, jobs[i].n);
+    if (tiles * threads >> 32) continue;  // a grid's axis has less than 2^32 threads
+    for (uint32_t splits : {1u, 2u, 4u, 8u}) {
+      if (splits > 1 && stages < 4 * splits) break;
+      const double groups = double(tiles * splits);
+      const bool two = c.stage_of_two > 0 && groups > kUnits;
+      const double rounds = std::ceil(groups / (two ? 2 * kUnits : kUnits));
+      double us = rounds * (c.round + (stages + splits - 1) / splits * (two ? c.stage_of_two : c.stage));
+      us = std::max(us, double(n) * k * 17 / 32 / kReadPerUs);
+      if (splits > 1) us += kJoin + 2.0 * double(sums) * splits / kBytesPerUs;
+      if (best == 0 || us < best) {
+        best = us;
+        p.kernel = c.kernel;
+        p.splits = splits;
+      }
+    }
+  }
+  if (p.kernel == Kernel::kSlim) return p;
   for (uint32_t i = 0; i < n_jobs; i++) {
     if (!whole_words(jobs[i].scale, jobs[i].lds, k)) p.scales += pad256(own_scales_bytes(jobs[i].n, k));
     if (p.splits > 1) p.parts += pad256(uint64_t(m) * ((jobs[i].n + 7) & ~7u) * 4 * p.splits);
@@ -369,16 +427,16 @@ void start_slim(uint32_t tiles, const MatArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((wc_matmul_mx_slim_kernel<2, kM, 8>), dim3(tiles, (a.m + 16 * kM - 1) / (16 * kM)), dim3(512), 0,
                      st, a);
 }
-template <int kN, int kWaves, int kHold, int kType>
-void start_stream(uint32_t tiles, const MatArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, kWaves, kHold, kType>), dim3(std::min(tiles, 256u * 16 / kWaves)),
-                     dim3(64 * kWaves), 0, st, a, tiles);
-}
-template <int kType>
-void start_stream(uint32_t tiles, const MatArgs& a, hipStream_t st) {
-  if (a.k <= 4096) start_stream<2, 8, 1, kType>(tiles, a, st);
-  else if (a.k <= 8192) start_stream<2, 16, 1, kType>(tiles, a, st);
-  else start_stream<1, 16, 2, kType>(tiles, a, st);
+template <int kN>
+void start_stream(const MatArgs& a, uint32_t tiles, int32_t x_dtype, hipStream_t st) {
+  // as many tiles to every workgroup, one to a compute unit
+  const uint32_t held = x_dtype ? uint32_t(groups_of(a.k)) * kHeldPart : 0;
+  const uint32_t rounds = (tiles + 255) / 256;
+  const dim3 grid((tiles + rounds - 1) / rounds), block(512);
+  if (x_dtype == WC_BF16) hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, WC_BF16>), grid, block, held, st, a, tiles);
+  else if (x_dtype == WC_FP16) hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, WC_FP16>), grid, block, held, st, a, tiles);
+  else if (x_dtype == WC_FP32) hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, WC_FP32>), grid, block, held, st, a, tiles);
+  else hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, 0>), grid, block, 0, st, a, tiles);
 }
 
 // The products of x: rows of codes and scales, or (x_dtype) of elements; ldx in bytes.
@@ -399,7 +457,7 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
     a.job[i] = {reinterpret_cast<uint64_t>(J.w), reinterpret_cast<uint64_t>(J.bias),
                 reinterpret_cast<uint64_t>(J.y), J.ldw, J.ldy,
                 {reinterpret_cast<uint64_t>(J.scale), uint32_t(J.lds), 16}, part, J.n, tiles, J.bias_dtype, J.y_dtype};
-    tiles += tiles_of(p.kernel, k > 8192, m, J.n);
+    tiles += tiles_of(p.kernel, m, J.n);
     widest = std::max(widest, J.n);
     if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 7) & ~7u) * 4 * p.splits);
     if (p.kernel >= Kernel::kTile64 && !whole_words(J.scale, J.lds, k)) {
@@ -408,14 +466,14 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
       copy += pad256(own_scales_bytes(J.n, k));
     }
   }
-  if (p.kernel == Kernel::kStream) {
+  if (streams(p.kernel)) {
     a.m = m;
-    if (x_dtype == WC_BF16) start_stream<WC_BF16>(tiles, a, st);
-    else if (x_dtype == WC_FP16) start_stream<WC_FP16>(tiles, a, st);
-    else start_stream<WC_FP32>(tiles, a, st);
+    if (p.kernel == Kernel::kStream16) start_stream<1>(a, tiles, x_dtype, st);
+    else if (p.kernel == Kernel::kStream32) start_stream<2>(a, tiles, x_dtype, st);
+    else start_stream<4>(a, tiles, x_dtype, st);
     return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
   }
-  if (p.kernel != Kernel::kSlim) {
+  if (p.kernel >= Kernel::kTile64) {
     a.m = m;
     with_tile(p.kernel, [&](auto t) {
       using T = decltype(t);
@@ -540,12 +598,12 @@ extern "C" wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint
   if (m == 0) return WC_OK;
   if (!coded_ok(dev_q, ldq, dev_scale, lds, k)) return WC_EINVAL;
   Plan p = plan_of(m, k, n_jobs, jobs);
-  if (p.kernel == Kernel::kStream) p.kernel = Kernel::kSlim;
+  p.inside = false;
   if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p) + x_scales_bytes(p, m, k))) return WC_EINVAL;
-  if (ldq > (1u << 22) || lds > (1u << 22)) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
+  if (p.kernel >= Kernel::kTile64 && (ldq > (1u << 22) || lds > (1u << 22))) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   Scales xs = {reinterpret_cast<uint64_t>(dev_scale), uint32_t(lds), 16};
-  if (p.kernel != Kernel::kSlim && !whole_words(dev_scale, lds, k)) {
+  if (p.kernel >= Kernel::kTile64 && !whole_words(dev_scale, lds, k)) {
     xs = own_scales(reinterpret_cast<uint64_t>(dev_workspace) + workspace_of(p), m, k);
     if (!launch_copy_scales(dev_scale, lds, m, 0, m, k, xs, st)) return WC_EHIP;
   }

@@ -7,8 +7,8 @@
 //   - up to 16 tokens, which are the columns of a matrix instruction, two kernels: one finds the
 //     experts (and chooses them, from logits), multiplies by gate and up and writes h by slot, the
 //     other multiplies by down and adds a token's slots;
-//   - more tokens: the places of the router's order in blocks of one expert's, each expert's
-//     results stored by slot and then added.
+//   - more tokens: the places of the router's order in blocks of one expert's, on tiles through
+//     LDS, each expert's results stored by slot and then added.
 #include <algorithm>
 
 #include "wc_choose.h"
@@ -151,23 +151,17 @@ __device__ __forceinline__ void store_h(const ExpertArgs& a, const f32x4 (&g)[2]
 // 32 columns of h at a time, for all tokens of one expert; the tokens are the columns of the matrix
 // instruction, whether they have the expert or not.  kPer: registers of logits to a lane of the
 // choice, 0 where the ids are given.
-using FewStream = Stream<4, kFewWaves, 0>;
-constexpr uint32_t kFewPart = 64 * 5 * 16;  // bytes in LDS of 512 of k of x: codes, then scales
 template <int kType, int kPer>
 __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
-  using S = FewStream;
+  using S = Stream<4, kFewWaves>;
   __shared__ typename S::Shared sh;
   __shared__ Chosen c;
-  extern __shared__ u32x4 held[];  // x, by part, step and lane; only its own wave reads a part
+  extern __shared__ u32x4 held[];  // x; only its own wave reads a part
   const uint32_t lane = threadIdx.x % 64, r = lane % 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t blocks = (a.hidden + 31) / 32, supers = (blocks + kSuper - 1) / kSuper;
-  for (uint32_t super = wave; super < supers; super += kFewWaves) {
-    const Part p = quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), r < a.tokens, super, a.hidden);
-    u32x4* const to = held + super * (5 * 64);
-#pragma unroll
-    for (int i = 0; i < 4; i++) to[i * 64 + lane] = p.codes[i];
-    reinterpret_cast<uint32_t*>(to + 4 * 64)[lane] = p.scales;
-  }
+  for (uint32_t super = wave; super < supers; super += kFewWaves)
+    hold_part(held, super,
+              quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), r < a.tokens, super, a.hidden));
   if constexpr (kPer > 0) {
     // the sums' place in LDS is free until then
     static_assert(sizeof(float) * kFewWaves * 64 * (kPer ? kPer : 1) <= sizeof(sh));
@@ -199,11 +193,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs
           w[n + 2] = row_of(a.up, e, n0 + 16 * n, r, a.ffn, blocks);
         }
       },
-      [&](uint32_t, uint32_t super) {
-        const u32x4* const from = held + super * (5 * 64);
-        return Part{{from[lane], from[64 + lane], from[128 + lane], from[192 + lane]},
-                    reinterpret_cast<const uint32_t*>(from + 4 * 64)[lane]};
-      },
+      [&](uint32_t super) { return held_part(held, super); },
       [&](uint32_t tile, auto sum) {
         if (wave) return;
         const int32_t slot = slot_of(c, a, r, c.list[tile / each]);
@@ -322,39 +312,31 @@ __device__ __forceinline__ uint32_t slot_at(const ExpertArgs& a, uint32_t place)
 
 __host__ __device__ constexpr uint32_t out_pitch(uint32_t hidden) { return (hidden + 7) & ~7u; }
 
-// 32 columns of h for a block of 16 kM places, quantised.
-template <int kM>
+// 32 columns of h for a block of 16 places, quantised.
 __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a) {
-  using S = Slim<4, kM, 8>;
+  using S = Slim<4, 1, 8>;
   __shared__ typename S::Shared sh;
   const uint32_t block = a.first + blockIdx.x;
   if (block >= block_count(a)) return;
   const auto [e, first, last] = block_at(a, block);
-  const uint32_t r = threadIdx.x % 16, n0 = blockIdx.y * 32, blocks = (a.hidden + 31) / 32;
+  const uint32_t lane = threadIdx.x % 64, r = lane % 16, n0 = blockIdx.y * 32, blocks = (a.hidden + 31) / 32;
   Row w[4];
 #pragma unroll
   for (uint32_t n = 0; n < 2; n++) {
     w[n] = row_of(a.gate, e, n0 + 16 * n, r, a.ffn, blocks);
     w[n + 2] = row_of(a.up, e, n0 + 16 * n, r, a.ffn, blocks);
   }
-  Row x[kM];
-#pragma unroll
-  for (uint32_t m = 0; m < kM; m++) {
-    const uint64_t token = slot_at(a, min(first + 16 * m + r, last - 1)) / a.k;
-    x[m] = {a.xq + token * blocks * 16, a.xs.at + token * a.xs.pitch, a.xs.step, 0, 0};
-  }
-  S::product(sh, w, blocks, [&](int m, uint32_t super) { return load_part<true>(x[m], super, blocks); });
-  const uint32_t m = threadIdx.x / 64, place = first + 16 * m + r;
-  if (m >= kM) return;
-  const auto sum = [&](uint32_t n) { return S::sum(sh, (n * kM + m) * 64 + threadIdx.x % 64); };
-  const f32x4 g[2] = {sum(0), sum(1)}, u[2] = {sum(2), sum(3)};
-  store_h(a, g, u, place, blockIdx.y, place < last);
+  const uint64_t token = slot_at(a, min(first + r, last - 1)) / a.k;
+  const Row x = {a.xq + token * blocks * 16, a.xs.at + token * a.xs.pitch, a.xs.step, 0, 0};
+  S::product(sh, w, blocks, [&](int, uint32_t super) { return load_part<true>(x, super, blocks); });
+  if (threadIdx.x >= 64) return;
+  const f32x4 g[2] = {S::sum(sh, lane), S::sum(sh, 64 + lane)}, u[2] = {S::sum(sh, 128 + lane), S::sum(sh, 192 + lane)};
+  store_h(a, g, u, first + r, blockIdx.y, first + r < last);
 }
 
 // down(h) of 32 columns for a block of places, stored by slot.
-template <int kM>
 __global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs a) {
-  using S = Slim<2, kM, 8>;
+  using S = Slim<2, 1, 8>;
   __shared__ typename S::Shared sh;
   const uint32_t block = a.first + blockIdx.x;
   if (block >= block_count(a)) return;
@@ -363,16 +345,13 @@ __global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs
   Row w[2];
 #pragma unroll
   for (uint32_t n = 0; n < 2; n++) w[n] = row_of(a.down, e, n0 + 16 * n, r, a.hidden, blocks);
-  S::product(sh, w, blocks, [&](int m, uint32_t super) {
-    const uint64_t place = min(first + 16 * uint32_t(m) + r, last - 1);
-    return load_part<true>(Row{h_codes(a, place, 0), a.hs.at + place * a.hs.pitch, a.hs.step, 0, 0}, super, blocks);
-  });
-  for (uint32_t i = threadIdx.x; i < S::kPart; i += 512) {
-    const uint32_t tile = i / 64, lane = i % 64;
-    const uint32_t n = n0 + tile / kM * 16 + lane / 16 * 4, place = first + tile % kM * 16 + lane % 16;
-    if (place < last && n < a.hidden)
-      store_four(a.out, WC_FP32, uint64_t(slot_at(a, place)) * out_pitch(a.hidden) + n, S::sum(sh, i), 4);
-  }
+  const uint64_t place = min(first + r, last - 1);
+  const Row x = {h_codes(a, place, 0), a.hs.at + place * a.hs.pitch, a.hs.step, 0, 0};
+  S::product(sh, w, blocks, [&](int, uint32_t super) { return load_part<true>(x, super, blocks); });
+  if (threadIdx.x >= S::kPart) return;
+  const uint32_t n = n0 + threadIdx.x / 64 * 16 + threadIdx.x % 64 / 16 * 4;
+  if (first + r < last && n < a.hidden)
+    store_four(a.out, WC_FP32, uint64_t(slot_at(a, first + r)) * out_pitch(a.hidden) + n, S::sum(sh, threadIdx.x), 4);
 }
 
 // The same on tiles through LDS: kCols / 2 columns of h, for which W's rows are those of gate and the
@@ -605,7 +584,7 @@ template <int kType, int kPer>
 void start_up(const ExpertArgs& a, const RouteArgs& route, hipStream_t st) {
   const uint32_t most = (a.ffn + 31) / 32 * std::min(a.slots, a.experts);
   hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, kPer>), dim3(std::min(most, 256u)), dim3(64 * kFewWaves),
-                     uint32_t(groups_of(a.hidden)) * kFewPart, st, a, route);
+                     uint32_t(groups_of(a.hidden)) * kHeldPart, st, a, route);
 }
 template <int kType>
 void start_up(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
@@ -626,17 +605,16 @@ wc_status few(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
 }
 
-template <int kM>
 bool start_slim(ExpertArgs a, uint32_t most, hipStream_t st) {
   constexpr uint32_t kLaunch = 1u << 22;  // a grid's axis has less than 2^32 threads
   for (a.first = 0; a.first < most; a.first += kLaunch) {
-    hipLaunchKernelGGL((wc_experts_mx_up_slim_kernel<kM>), dim3(std::min(most - a.first, kLaunch), (a.ffn + 31) / 32),
+    hipLaunchKernelGGL(wc_experts_mx_up_slim_kernel, dim3(std::min(most - a.first, kLaunch), (a.ffn + 31) / 32),
                        dim3(512), 0, st, a);
     if (hipGetLastError() != hipSuccess) return false;
   }
   for (a.first = 0; a.first < most; a.first += kLaunch) {
-    hipLaunchKernelGGL((wc_experts_mx_down_slim_kernel<kM>),
-                       dim3(std::min(most - a.first, kLaunch), (a.hidden + 31) / 32), dim3(512), 0, st, a);
+    hipLaunchKernelGGL(wc_experts_mx_down_slim_kernel, dim3(std::min(most - a.first, kLaunch), (a.hidden + 31) / 32),
+                       dim3(512), 0, st, a);
     if (hipGetLastError() != hipSuccess) return false;
   }
   return true;
@@ -647,8 +625,8 @@ template <int kPlaces>
 struct Tiles;
 template <>
 struct Tiles<64> {
-  using Up = MxTile<64, 128, 1, 2, 128, 3, true>;
-  using Down = MxTile<64, 128, 1, 2, 128, 3>;
+  using Up = MxTile<64, 128, 2, 2, 128, 2, true>;
+  using Down = MxTile<64, 128, 2, 2, 128, 2>;
 };
 template <>
 struct Tiles<128> {
@@ -683,14 +661,19 @@ bool start_tiles(const ExpertArgs& a, uint32_t most, hipStream_t st) {
                      dim3(Down::kThreads), 0, st, a);
   return hipGetLastError() == hipSuccess;
 }
-// Places to a block: 16 and 32 straight from memory to registers, more through LDS.
+// Places to a block; 16: straight from memory to registers, at any sizes.  us with 64, 128 and 256:
+//   8 experts, 2 a token, of 4096 x 14336: 64 tokens 172, 181, 215; 128 177, 192, 226; 256 217,
+//     203, 236; 600 (tiles of 64 with two waves less) 426, 275, 270; 1500 876, 518, 384
+//   64, 6, 2048 x 1408: 60 78, 80, 89; 200 83, 84, 92; 700 123, 103, 111; 2000 293, 175, 156
+//   7, 3, 2049 x 1365: 77 39, 40, 47; 256 43, 45, 54
+//   128, 8, 4096 x 1536: 40 248, 254, 283; 1000 403, 367, 387
 uint32_t places(const ExpertArgs& a) {
-  const uint32_t average = a.slots / a.experts;
   // x lies within 32-bit offsets, a grid's axis has less than 2^32 threads
   if (a.tokens * WC_MX_ROW_BYTES(a.hidden) >> 31 || a.xs.step == 16 ||
-      most_blocks(a.slots, a.experts, 64) * std::max(tiles(a.ffn, 64), tiles(a.hidden, 128)) * 512 >> 32)
-    return average <= 16 ? 16 : 32;
-  return average <= 16 ? 16 : average <= 32 ? 32 : average <= 64 ? 64 : average <= 256 ? 128 : 256;
+      most_blocks(a.slots, a.experts, 64) * std::max(tiles(a.ffn, 64), tiles(a.hidden, 128)) * 256 >> 32)
+    return 16;
+  const uint32_t average = a.slots / a.experts;
+  return average < 48 ? 64 : average < 160 ? 128 : 256;
 }
 
 wc_status experts(ExpertArgs a, const Workspace& w, const int32_t* offsets, hipStream_t st) {
@@ -706,8 +689,7 @@ wc_status experts(ExpertArgs a, const Workspace& w, const int32_t* offsets, hipS
                      !ready(a.up, ws + w.up, a.experts, a.ffn, a.hidden, st) ||
                      !ready(a.down, ws + w.down, a.experts, a.hidden, a.ffn, st)))
     return WC_EHIP;
-  const bool started = rows == 16   ? start_slim<1>(a, most, st)
-                       : rows == 32 ? start_slim<2>(a, most, st)
+  const bool started = rows == 16   ? start_slim(a, most, st)
                        : rows == 64 ? start_tiles<64>(a, most, st)
                        : rows == 128 ? start_tiles<128>(a, most, st)
                                      : start_tiles<256>(a, most, st);

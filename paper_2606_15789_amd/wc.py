@@ -1226,8 +1226,8 @@ def linear_mx_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
     need = C.c_uint64(0)
     with where:
         jobs, ys = _mx_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, dev)
-        # few rows of no more than 16384 need no workspace
-        rc = 0 if m <= 16 and k <= 16384 and workspace is None else \
+        # few rows of no more than 12288 need no workspace
+        rc = 0 if m <= 16 and k <= 12288 and workspace is None else \
             lib().wc_linear_mx_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
         if not rc:
             workspace = _workspace(workspace, need.value, x.device)
