@@ -372,19 +372,19 @@ __device__ __forceinline__ Part held_part(const u32x4* held, uint32_t super) {
           reinterpret_cast<const uint32_t*>(from + 4 * 64)[lane]};
 }
 
-// Four neighbouring elements of type dt from element i on at address p, of which `left` are in
-// the row.
+// Four neighbouring elements of type dt from element i on at address p (any element's), of which
+// `left` are in the row.
 __device__ __forceinline__ void store_four(uint64_t p, int32_t dt, uint64_t i, f32x4 v, uint32_t left) {
   const uint64_t at = p + i * (dt == WC_FP32 ? 4 : 2);
-  if (left >= 4 && dt == WC_FP32 && at % 16 == 0) {
-    *global<f32x4>(at) = v;
-  } else if (left >= 4 && dt != WC_FP32 && at % 8 == 0) {
+  if (left >= 4 && dt == WC_FP32) {
+    *global<u32x4u>(at) = __builtin_bit_cast(u32x4, v);
+  } else if (left >= 4) {
     u32x2 h;
     if (dt == WC_BF16)
       h = {floats_to_bf16(v[0], v[1]), floats_to_bf16(v[2], v[3])};
     else
       h = {float_to_fp16(v[0]) | float_to_fp16(v[1]) << 16, float_to_fp16(v[2]) | float_to_fp16(v[3]) << 16};
-    *global<u32x2>(at) = h;
+    *global<u32x2u>(at) = h;
   } else {
 #pragma unroll
     for (uint32_t j = 0; j < 4; j++)
@@ -392,20 +392,48 @@ __device__ __forceinline__ void store_four(uint64_t p, int32_t dt, uint64_t i, f
   }
 }
 
-// Quantise m rows of k elements of type dt to rows of `ldq` bytes of codes and to scales, of which
-// each row has `scale_blocks` written, zeros past its blocks (wc_mx.hip).  With `blocks`, one more
-// workgroup writes its table.  False on a launch error.
-bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q, uint64_t ldq,
-                     const Scales& scales, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks = nullptr);
+// Eight neighbouring elements of type dt from element i on at address p, of which `left` are in the row.
+__device__ __forceinline__ void store_eight(uint64_t p, int32_t dt, uint64_t i, f32x4 low, f32x4 high, uint32_t left) {
+  const uint64_t at = p + i * 2;
+  if (left >= 8 && dt != WC_FP32) {
+    u32x4 h;
+    if (dt == WC_BF16)
+      h = {floats_to_bf16(low[0], low[1]), floats_to_bf16(low[2], low[3]), floats_to_bf16(high[0], high[1]),
+           floats_to_bf16(high[2], high[3])};
+    else
+      h = {float_to_fp16(low[0]) | float_to_fp16(low[1]) << 16, float_to_fp16(low[2]) | float_to_fp16(low[3]) << 16,
+           float_to_fp16(high[0]) | float_to_fp16(high[1]) << 16, float_to_fp16(high[2]) | float_to_fp16(high[3]) << 16};
+    *global<u32x4u>(at) = h;
+    return;
+  }
+  store_four(p, dt, i, low, left);
+  if (left > 4) store_four(p, dt, i + 4, high, left - 4);
+}
 
 // Tiles load scales as whole words: others are copied, to own_scales of all `rows`, zeros past a
-// row's blocks; row r of them lies at scale + r / per * stride + r mod per * pitch.  False on a
-// launch error.
+// row's blocks; row r of them lies at `from` + r / per * stride + r mod per * pitch.
 inline bool whole_words(const void* scale, uint64_t pitch, uint32_t k) {
   return reinterpret_cast<uintptr_t>(scale) % 4 == 0 && pitch % 4 == 0 && blocks_of(k) % 4 == 0;
 }
-bool launch_copy_scales(const void* scale, uint64_t pitch, uint64_t per, uint64_t stride, uint64_t rows, uint32_t k,
-                        const Scales& to, hipStream_t stream);
+struct ScaleCopy {
+  uint64_t from, pitch, per, stride;
+  Scales to;
+  uint64_t rows;
+  uint32_t blocks, first;  // first: its first workgroup
+};
+struct ScaleCopies {
+  uint32_t n, groups;  // groups: workgroups of them all
+  ScaleCopy copy[kMaxJobs];
+  void add(uint64_t from, uint64_t pitch, uint64_t per, uint64_t stride, uint64_t rows, uint32_t k, const Scales& to);
+};
+
+// Quantise m rows of k elements of type dt to rows of `ldq` bytes of codes and to scales, of which
+// each row has `scale_blocks` written, zeros past its blocks (wc_mx.hip).  In the same launch, with
+// `blocks`, one more workgroup writes its table, and with `copies` some copy scales.  False on a
+// launch error.
+bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q, uint64_t ldq,
+                     const Scales& scales, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks = nullptr,
+                     const ScaleCopies* copies = nullptr);
 
 inline bool off(const void* p, uint32_t to) { return !p || reinterpret_cast<uintptr_t>(p) % to != 0; }
 

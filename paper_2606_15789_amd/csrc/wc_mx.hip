@@ -18,33 +18,80 @@ struct QuantArgs {
   Blocks blocks;
 };
 
+// A workgroup's rows of one copy, four words a thread: neighbouring threads have neighbouring rows.
+__device__ __forceinline__ void copy_scales(const ScaleCopies& all, uint32_t group) {
+  uint32_t c = 0;
+  for (uint32_t i = 1; i < all.n; i++)
+    if (group >= all.copy[i].first) c = i;
+  const ScaleCopy& C = all.copy[c];
+  const uint32_t groups = (C.blocks + 15) / 16, each = kThreads / groups;
+  const uint64_t row = uint64_t(group - C.first) * each + threadIdx.x % each;
+  const uint32_t at = threadIdx.x / each;
+  if (at >= groups || row >= C.rows) return;
+  const auto from = global<const uint8_t>(C.from + row / C.per * C.stride + row % C.per * C.pitch + at * 16);
+  u32x4 v = {0, 0, 0, 0};
+  if (at * 16 + 16 <= C.blocks)
+    v = *reinterpret_cast<global_ptr<const u32x4u>>(from);
+  else
+#pragma unroll
+    for (uint32_t i = 0; i < 16; i++)
+      if (at * 16 + i < C.blocks) v[i / 4] |= uint32_t(from[i]) << (8 * (i % 4));
+  *global<u32x4>(C.to.at + row * C.to.pitch + uint64_t(at) * C.to.step) = v;
+}
+
+__global__ __launch_bounds__(kThreads) void wc_copy_scales_mx_kernel(ScaleCopies copies) {
+  copy_scales(copies, blockIdx.x);
+}
+bool launch_copies(const ScaleCopies& copies, hipStream_t stream) {
+  hipLaunchKernelGGL(wc_copy_scales_mx_kernel, dim3(copies.groups), dim3(kThreads), 0, stream, copies);
+  return hipGetLastError() == hipSuccess;
+}
+
 // Four lanes to a block of 32, eight elements each: loads and stores of neighbouring lanes are
-// next to each other. Rows of less than a workgroup's elements share one.
-template <int kType>
-__global__ __launch_bounds__(kThreads) void wc_quantize_mx_kernel(QuantArgs a) {
-  if (blockIdx.x == a.groups) {
-    __shared__ uint32_t starts[kMaxExperts + 1];
-    if (blockIdx.y == 0) write_blocks<kThreads>(a.blocks, starts);
+// next to each other.  Long rows have kUnits units of eight to a thread, all on their way at once;
+// rows of less than a workgroup's elements share one.  After the rows' workgroups one that writes the
+// table of blocks of places, if there is one, then those that copy scales.
+struct NoCopies {};
+template <int kType, int kUnits, class Copies>
+__global__ __launch_bounds__(kThreads) void wc_quantize_mx_kernel(QuantArgs a, Copies copies) {
+  if (blockIdx.x >= a.groups) {
+    if (blockIdx.y) return;
+    const uint32_t extra = blockIdx.x - a.groups, table = a.blocks.table != 0;
+    if (extra < table) {
+      __shared__ uint32_t starts[kMaxExperts + 1];
+      write_blocks<kThreads>(a.blocks, starts);
+    } else if constexpr (std::is_same_v<Copies, ScaleCopies>) {
+      copy_scales(copies, extra - table);
+    }
     return;
   }
   const uint32_t units = a.scale_blocks * 4;
-  uint32_t row = blockIdx.x, unit = blockIdx.y * kThreads + threadIdx.x;
+  uint64_t row = blockIdx.x;
+  uint32_t first = blockIdx.y * (kThreads * kUnits) + threadIdx.x;
   if (a.each > 1) {
-    row = blockIdx.x * a.each + threadIdx.x / units;
-    unit = threadIdx.x / units < a.each ? threadIdx.x % units : units;
+    row = uint64_t(blockIdx.x) * a.each + threadIdx.x / units;
+    first = threadIdx.x / units < a.each ? threadIdx.x % units : units;
   }
-  const bool live = row < a.m && unit < units;
-  Eight<kType> e = load_eight<kType>(a.x + (row * a.ldx + unit * 8) * (kType == WC_FP32 ? 4 : 2),
-                                     live ? int32_t(a.k) - int32_t(unit * 8) : 0);
-  uint32_t top = float_bits<kType>(e.top());
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xF, 0xF, false)));  // lane ^ 1
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xF, 0xF, false)));  // lane ^ 2
-  if (!live) return;
-  const uint32_t byte = scale_byte(top);
-  if (unit < (a.k + 31) / 32 * 4)
-    global<uint32_t>(a.q + row * a.ldq)[unit] = byte == 255 ? 0u : e.codes(scale_value(byte));
-  if (unit % 4 == 0)
-    *global<uint8_t>(a.scale + row * a.lds + uint64_t(unit / 64) * a.scale_step + unit / 4 % 16) = uint8_t(byte);
+  Eight<kType> e[kUnits];
+#pragma unroll
+  for (uint32_t i = 0; i < kUnits; i++) {
+    const uint32_t unit = first + i * kThreads;
+    e[i] = load_eight<kType>(a.x + (row * a.ldx + unit * 8) * (kType == WC_FP32 ? 4 : 2),
+                             row < a.m && unit < units ? int32_t(a.k) - int32_t(unit * 8) : 0);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kUnits; i++) {
+    const uint32_t unit = first + i * kThreads;
+    uint32_t top = float_bits<kType>(e[i].top());
+    top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xF, 0xF, false)));  // lane ^ 1
+    top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xF, 0xF, false)));  // lane ^ 2
+    if (row >= a.m || unit >= units) continue;
+    const uint32_t byte = scale_byte(top);
+    if (unit < (a.k + 31) / 32 * 4)
+      global<uint32_t>(a.q + row * a.ldq)[unit] = byte == 255 ? 0u : e[i].codes(scale_value(byte));
+    if (unit % 4 == 0)
+      *global<uint8_t>(a.scale + row * a.lds + uint64_t(unit / 64) * a.scale_step + unit / 4 % 16) = uint8_t(byte);
+  }
 }
 
 struct DequantArgs {
@@ -54,57 +101,40 @@ struct DequantArgs {
 
 // The same the other way: eight codes a lane.  Values are exact in fp32, and rounded once to
 // y's type.
-template <int kType>
+template <int kType, int kUnits>
 __global__ __launch_bounds__(kThreads) void wc_dequantize_mx_kernel(DequantArgs a) {
   const uint32_t units = (a.k + 7) / 8;
-  uint32_t row = blockIdx.x, unit = blockIdx.y * kThreads + threadIdx.x;
+  uint64_t row = blockIdx.x;
+  uint32_t first = blockIdx.y * (kThreads * kUnits) + threadIdx.x;
   if (a.each > 1) {
-    row = blockIdx.x * a.each + threadIdx.x / units;
-    unit = threadIdx.x / units < a.each ? threadIdx.x % units : units;
+    row = uint64_t(blockIdx.x) * a.each + threadIdx.x / units;
+    first = threadIdx.x / units < a.each ? threadIdx.x % units : units;
   }
-  if (row >= a.m || unit >= units) return;
-  const uint32_t codes = global<const uint32_t>(a.q + row * a.ldq)[unit];
-  const uint32_t byte = global<const uint8_t>(a.scale + row * a.lds)[unit / 4];
-  const float scale = byte == 255 ? __builtin_nanf("") : scale_value(byte);
-  f32x4 v[2];
+  if (row >= a.m) return;
+  uint32_t codes[kUnits], bytes[kUnits];
 #pragma unroll
-  for (int j = 0; j < 4; j++) {
-    const f32x2 p = j == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0)
-                    : j == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1)
-                    : j == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 2)
-                             : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3);
-    v[j / 2][j % 2 * 2] = p[0] * scale;
-    v[j / 2][j % 2 * 2 + 1] = p[1] * scale;
+  for (uint32_t i = 0; i < kUnits; i++) {
+    const uint32_t unit = min(first + i * kThreads, units - 1);
+    codes[i] = global<const uint32_t>(a.q + row * a.ldq)[unit];
+    bytes[i] = global<const uint8_t>(a.scale + row * a.lds)[unit / 4];
   }
-  const uint32_t left = a.k - unit * 8;
-  const uint64_t at = row * a.ldy + unit * 8, to = a.y + at * (kType == WC_FP32 ? 4 : 2);
-  if (kType != WC_FP32 && left >= 8 && to % 16 == 0) {
-    u32x4 h;
+#pragma unroll
+  for (uint32_t i = 0; i < kUnits; i++) {
+    const uint32_t unit = first + i * kThreads;
+    if (unit >= units) return;
+    const float scale = bytes[i] == 255 ? __builtin_nanf("") : scale_value(bytes[i]);
+    f32x4 v[2];
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-      const float low = v[j / 2][j % 2 * 2], high = v[j / 2][j % 2 * 2 + 1];
-      h[j] = kType == WC_BF16 ? floats_to_bf16(low, high) : float_to_fp16(low) | float_to_fp16(high) << 16;
+      const f32x2 p = j == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], 1.0f, 0)
+                      : j == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], 1.0f, 1)
+                      : j == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], 1.0f, 2)
+                               : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], 1.0f, 3);
+      v[j / 2][j % 2 * 2] = p[0] * scale;
+      v[j / 2][j % 2 * 2 + 1] = p[1] * scale;
     }
-    *global<u32x4>(to) = h;
-    return;
+    store_eight(a.y, kType, row * a.ldy + unit * 8, v[0], v[1], a.k - unit * 8);
   }
-  store_four(a.y, kType, at, v[0], left);
-  if (left > 4) store_four(a.y, kType, at + 4, v[1], left - 4);
-}
-
-// Scales to groups of whole words, rows from `first` on.
-__global__ __launch_bounds__(kThreads) void wc_copy_scales_mx_kernel(uint64_t from, uint64_t pitch, uint64_t per,
-                                                                     uint64_t stride, Scales to, uint64_t first,
-                                                                     uint64_t rows, uint32_t blocks) {
-  const uint64_t row = first + blockIdx.x * 4 + threadIdx.x / 64;
-  const uint32_t words = (blocks + 15) / 16 * 4, word = blockIdx.y * 64 + threadIdx.x % 64;
-  if (row >= rows || word >= words) return;
-  const auto p = global<const uint8_t>(from + row / per * stride + row % per * pitch + word * 4);
-  uint32_t v = 0;
-#pragma unroll
-  for (uint32_t i = 0; i < 4; i++)
-    if (word * 4 + i < blocks) v |= uint32_t(p[i]) << (8 * i);
-  *global<uint32_t>(to.at + row * to.pitch + uint64_t(word / 4) * to.step + word % 4 * 4) = v;
 }
 
 struct MatJob {
@@ -439,10 +469,24 @@ void start_stream(const MatArgs& a, uint32_t tiles, int32_t x_dtype, hipStream_t
   else hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, 0>), grid, block, 0, st, a, tiles);
 }
 
+// The copies of scales of a plan.
+ScaleCopies copies_of(const Plan& p, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs, const void* workspace) {
+  ScaleCopies c;
+  c.n = c.groups = 0;
+  uint64_t to = reinterpret_cast<uint64_t>(workspace) + p.parts;
+  for (uint32_t i = 0; p.scales && i < n_jobs; i++) {
+    const wc_mx_job& J = jobs[i];
+    if (whole_words(J.scale, J.lds, k)) continue;
+    c.add(reinterpret_cast<uint64_t>(J.scale), J.lds, J.n, 0, J.n, k, own_scales(to, J.n, k));
+    to += pad256(own_scales_bytes(J.n, k));
+  }
+  return c;
+}
+
 // The products of x: rows of codes and scales, or (x_dtype) of elements; ldx in bytes.
+// Copies of scales that the plan has are written by the caller (copies_of).
 wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype, uint32_t m, uint32_t k,
-                 uint32_t n_jobs, const wc_mx_job* jobs, const Plan& p, void* workspace,
-                 hipStream_t st) {
+                 uint32_t n_jobs, const wc_mx_job* jobs, const Plan& p, void* workspace, hipStream_t st) {
   MatArgs a{};
   a.x = reinterpret_cast<uint64_t>(x);
   a.ldx = ldx;
@@ -462,7 +506,6 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
     if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 7) & ~7u) * 4 * p.splits);
     if (p.kernel >= Kernel::kTile64 && !whole_words(J.scale, J.lds, k)) {
       a.job[i].scales = own_scales(copy, J.n, k);
-      if (!launch_copy_scales(J.scale, J.lds, J.n, 0, J.n, k, a.job[i].scales, st)) return WC_EHIP;
       copy += pad256(own_scales_bytes(J.n, k));
     }
   }
@@ -505,32 +548,39 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
 
 namespace wc_mx {
 
+void ScaleCopies::add(uint64_t from, uint64_t pitch, uint64_t per, uint64_t stride, uint64_t rows, uint32_t k,
+                      const Scales& to) {
+  copy[n++] = {from, pitch, per, stride, to, rows, blocks_of(k), groups};
+  const uint32_t each = kThreads / uint32_t(groups_of(k));
+  groups += uint32_t((rows + each - 1) / each);
+}
+
+template <int kType, int kUnits>
+void start_quantize(const dim3& grid, const QuantArgs& a, const ScaleCopies* copies, hipStream_t stream) {
+  if (copies)
+    hipLaunchKernelGGL((wc_quantize_mx_kernel<kType, kUnits, ScaleCopies>), grid, dim3(kThreads), 0, stream, a, *copies);
+  else
+    hipLaunchKernelGGL((wc_quantize_mx_kernel<kType, kUnits, NoCopies>), grid, dim3(kThreads), 0, stream, a, NoCopies{});
+}
+
 bool launch_quantize(const void* x, int32_t dt, uint32_t m, uint32_t k, uint64_t ldx, void* q, uint64_t ldq,
-                     const Scales& scales, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks) {
+                     const Scales& scales, uint32_t scale_blocks, hipStream_t stream, const Blocks* blocks,
+                     const ScaleCopies* copies) {
   const uint32_t units = scale_blocks * 4, each = units < kThreads ? kThreads / units : 1;
-  for (uint32_t first = 0; first < m; first += kLaunchRows) {
+  const bool wide = units > kThreads && m >= 64;
+  const uint32_t span = kThreads * (wide ? 4 : 1);
+  for (uint32_t first = 0; first == 0 || first < m; first += kLaunchRows) {
     const uint32_t rows = std::min(m - first, kLaunchRows), groups = (rows + each - 1) / each;
-    const bool table = blocks && first == 0;
+    const bool more = first == 0, copying = more && copies && copies->n;
     const QuantArgs a = {reinterpret_cast<uint64_t>(x) + first * ldx * size_of(dt), ldx,
                          reinterpret_cast<uint64_t>(q) + first * ldq, ldq,
                          scales.at + uint64_t(first) * scales.pitch, scales.pitch, rows, k, scale_blocks, scales.step,
-                         each, groups, table ? *blocks : Blocks{}};
-    const dim3 grid(groups + table, (units + kThreads - 1) / kThreads), block(kThreads);
-    if (dt == WC_BF16) hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_BF16>), grid, block, 0, stream, a);
-    else if (dt == WC_FP16) hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_FP16>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((wc_quantize_mx_kernel<WC_FP32>), grid, block, 0, stream, a);
-    if (hipGetLastError() != hipSuccess) return false;
-  }
-  return true;
-}
-
-bool launch_copy_scales(const void* scale, uint64_t pitch, uint64_t per, uint64_t stride, uint64_t rows, uint32_t k,
-                        const Scales& to, hipStream_t stream) {
-  const uint32_t words = uint32_t(groups_of(k)) * 4;
-  for (uint64_t first = 0; first < rows; first += kLaunchRows) {
-    const uint32_t some = uint32_t(std::min<uint64_t>(rows - first, kLaunchRows));
-    hipLaunchKernelGGL(wc_copy_scales_mx_kernel, dim3((some + 3) / 4, (words + 63) / 64), dim3(kThreads), 0, stream,
-                       reinterpret_cast<uint64_t>(scale), pitch, per, stride, to, first, rows, blocks_of(k));
+                         each, groups, blocks && more ? *blocks : Blocks{}};
+    const dim3 grid(groups + (blocks && more) + (copying ? copies->groups : 0), (units + span - 1) / span);
+    const ScaleCopies* const some = copying ? copies : nullptr;
+    if (dt == WC_BF16) wide ? start_quantize<WC_BF16, 4>(grid, a, some, stream) : start_quantize<WC_BF16, 1>(grid, a, some, stream);
+    else if (dt == WC_FP16) wide ? start_quantize<WC_FP16, 4>(grid, a, some, stream) : start_quantize<WC_FP16, 1>(grid, a, some, stream);
+    else wide ? start_quantize<WC_FP32, 4>(grid, a, some, stream) : start_quantize<WC_FP32, 1>(grid, a, some, stream);
     if (hipGetLastError() != hipSuccess) return false;
   }
   return true;
@@ -559,15 +609,21 @@ extern "C" wc_status wc_dequantize_mx(const uint8_t* dev_q, uint64_t ldq, const 
   if (!coded_ok(dev_q, ldq, dev_scale, lds, k)) return WC_EINVAL;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const uint32_t units = (k + 7) / 8, each = units < kThreads ? kThreads / units : 1;
+  const bool wide = units > kThreads && m >= 64;
+  const uint32_t span = kThreads * (wide ? 4 : 1);
   for (uint32_t first = 0; first < m; first += kLaunchRows) {
     const uint32_t rows = std::min(m - first, kLaunchRows);
     const DequantArgs a = {reinterpret_cast<uint64_t>(dev_q) + first * ldq, ldq,
                            reinterpret_cast<uint64_t>(dev_scale) + first * lds, lds,
                            reinterpret_cast<uint64_t>(dev_y) + first * ldy * size_of(y_dtype), ldy, rows, k, each};
-    const dim3 grid((rows + each - 1) / each, (units + kThreads - 1) / kThreads), block(kThreads);
-    if (y_dtype == WC_BF16) hipLaunchKernelGGL((wc_dequantize_mx_kernel<WC_BF16>), grid, block, 0, st, a);
-    else if (y_dtype == WC_FP16) hipLaunchKernelGGL((wc_dequantize_mx_kernel<WC_FP16>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((wc_dequantize_mx_kernel<WC_FP32>), grid, block, 0, st, a);
+    const dim3 grid((rows + each - 1) / each, (units + span - 1) / span);
+    const auto start = [&]<int kType>(std::integral_constant<int, kType>) {
+      if (wide) hipLaunchKernelGGL((wc_dequantize_mx_kernel<kType, 4>), grid, dim3(kThreads), 0, st, a);
+      else hipLaunchKernelGGL((wc_dequantize_mx_kernel<kType, 1>), grid, dim3(kThreads), 0, st, a);
+    };
+    if (y_dtype == WC_BF16) start(std::integral_constant<int, WC_BF16>{});
+    else if (y_dtype == WC_FP16) start(std::integral_constant<int, WC_FP16>{});
+    else start(std::integral_constant<int, WC_FP32>{});
     if (hipGetLastError() != hipSuccess) return WC_EHIP;
   }
   return WC_OK;
@@ -603,9 +659,15 @@ extern "C" wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint
   if (p.kernel >= Kernel::kTile64 && (ldq > (1u << 22) || lds > (1u << 22))) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   Scales xs = {reinterpret_cast<uint64_t>(dev_scale), uint32_t(lds), 16};
-  if (p.kernel >= Kernel::kTile64 && !whole_words(dev_scale, lds, k)) {
-    xs = own_scales(reinterpret_cast<uint64_t>(dev_workspace) + workspace_of(p), m, k);
-    if (!launch_copy_scales(dev_scale, lds, m, 0, m, k, xs, st)) return WC_EHIP;
+  if (p.kernel >= Kernel::kTile64) {
+    ScaleCopies copies = copies_of(p, k, n_jobs, jobs, dev_workspace);
+    if (copies.n && !launch_copies(copies, st)) return WC_EHIP;
+    if (!whole_words(dev_scale, lds, k)) {
+      xs = own_scales(reinterpret_cast<uint64_t>(dev_workspace) + workspace_of(p), m, k);
+      copies.n = copies.groups = 0;
+      copies.add(reinterpret_cast<uint64_t>(dev_scale), lds, m, 0, m, k, xs);
+      if (!launch_copies(copies, st)) return WC_EHIP;
+    }
   }
   return matmul(dev_q, ldq, xs, 0, m, k, n_jobs, jobs, p, dev_workspace, st);
 }
@@ -633,7 +695,9 @@ extern "C" wc_status wc_linear_mx(const void* dev_x, int32_t x_dtype, uint32_t m
     return matmul(dev_x, ldx * size_of(x_dtype), Scales{}, x_dtype, m, k, n_jobs, jobs, p, nullptr, st);
   uint8_t* q = static_cast<uint8_t*>(dev_workspace) + workspace_of(p);
   const Scales scales = own_scales(reinterpret_cast<uint64_t>(q) + codes_bytes(m, k), m, k);
-  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, WC_MX_ROW_BYTES(k), scales, uint32_t(groups_of(k)) * 16, st))
+  const ScaleCopies copies = copies_of(p, k, n_jobs, jobs, dev_workspace);
+  if (!launch_quantize(dev_x, x_dtype, m, k, ldx, q, WC_MX_ROW_BYTES(k), scales, uint32_t(groups_of(k)) * 16, st,
+                       nullptr, &copies))
     return WC_EHIP;
   return matmul(q, WC_MX_ROW_BYTES(k), scales, 0, m, k, n_jobs, jobs, p, dev_workspace, st);
 }

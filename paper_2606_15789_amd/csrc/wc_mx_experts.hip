@@ -76,10 +76,11 @@ struct Chosen {
   uint32_t count;
 };
 // Lists the experts that ids name.
+template <uint32_t kThreads>
 __device__ __forceinline__ void list_experts(Chosen& c, const ExpertArgs& a) {
-  for (uint32_t e = threadIdx.x; e < kMaxExperts; e += kFewThreads) c.hit[e] = 0;
+  for (uint32_t e = threadIdx.x; e < kMaxExperts; e += kThreads) c.hit[e] = 0;
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < a.slots; i += kFewThreads) {
+  for (uint32_t i = threadIdx.x; i < a.slots; i += kThreads) {
     const int32_t id = c.ids[i / a.k][i % a.k];
     if (id >= 0) c.hit[id] = 1;
   }
@@ -96,8 +97,9 @@ __device__ __forceinline__ void list_experts(Chosen& c, const ExpertArgs& a) {
   }
   __syncthreads();
 }
+template <uint32_t kThreads>
 __device__ __forceinline__ void load_choice(Chosen& c, const ExpertArgs& a) {
-  for (uint32_t i = threadIdx.x; i < a.slots; i += kFewThreads) {
+  for (uint32_t i = threadIdx.x; i < a.slots; i += kThreads) {
     const int32_t id = global<const int32_t>(a.ids)[i];
     c.ids[i / a.k][i % a.k] = id < 0 ? -1 : min(id, int32_t(a.experts) - 1);
     c.weights[i / a.k][i % a.k] = global<const float>(a.weights)[i];
@@ -151,22 +153,22 @@ __device__ __forceinline__ void store_h(const ExpertArgs& a, const f32x4 (&g)[2]
 // 32 columns of h at a time, for all tokens of one expert; the tokens are the columns of the matrix
 // instruction, whether they have the expert or not.  kPer: registers of logits to a lane of the
 // choice, 0 where the ids are given.
-template <int kType, int kPer>
-__global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
-  using S = Stream<4, kFewWaves>;
+template <int kType, int kPer, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
+  using S = Stream<4, kWaves>;
   __shared__ typename S::Shared sh;
   __shared__ Chosen c;
   extern __shared__ u32x4 held[];  // x; only its own wave reads a part
   const uint32_t lane = threadIdx.x % 64, r = lane % 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t blocks = (a.hidden + 31) / 32, supers = (blocks + kSuper - 1) / kSuper;
-  for (uint32_t super = wave; super < supers; super += kFewWaves)
+  for (uint32_t super = wave; super < supers; super += kWaves)
     hold_part(held, super,
               quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), r < a.tokens, super, a.hidden));
   if constexpr (kPer > 0) {
     // the sums' place in LDS is free until then
-    static_assert(sizeof(float) * kFewWaves * 64 * (kPer ? kPer : 1) <= sizeof(sh));
+    static_assert(sizeof(float) * kWaves * 64 * (kPer ? kPer : 1) <= sizeof(sh));
     float* const scratch = reinterpret_cast<float*>(&sh) + wave * (64 * kPer);
-    for (uint32_t token = wave; token < a.tokens; token += kFewWaves) {
+    for (uint32_t token = wave; token < a.tokens; token += kWaves) {
       int32_t id;
       float weight;
       wc_choose::choose<64, kPer>(route, token, scratch, id, weight);
@@ -177,10 +179,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_up_kernel(ExpertArgs
       if (blockIdx.x == 0) wc_choose::store_choice<64>(route, token, id, weight);
     }
   } else {
-    load_choice(c, a);
+    load_choice<64 * kWaves>(c, a);
   }
   __syncthreads();
-  list_experts(c, a);
+  list_experts<64 * kWaves>(c, a);
   const uint32_t each = (a.ffn + 31) / 32, tiles = c.count * each;
   if (blockIdx.x >= tiles) return;
   S::run(
@@ -208,9 +210,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_down_kernel(ExpertAr
   __shared__ Chosen c;
   __shared__ f32x4 part[kFewWaves][64];
   extern __shared__ float table[];  // weights, then slots
-  load_choice(c, a);
+  load_choice<kFewThreads>(c, a);
   __syncthreads();
-  list_experts(c, a);
+  list_experts<kFewThreads>(c, a);
   float* const weights = table;
   int16_t* const slots = reinterpret_cast<int16_t*>(table + c.count * 16);
   for (uint32_t i = threadIdx.x; i < c.count * 16; i += kFewThreads) {
@@ -583,8 +585,12 @@ ExpertArgs args_of(const void* x, int32_t dtype, uint32_t tokens, uint64_t ldx, 
 template <int kType, int kPer>
 void start_up(const ExpertArgs& a, const RouteArgs& route, hipStream_t st) {
   const uint32_t most = (a.ffn + 31) / 32 * std::min(a.slots, a.experts);
-  hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, kPer>), dim3(std::min(most, 256u)), dim3(64 * kFewWaves),
-                     uint32_t(groups_of(a.hidden)) * kHeldPart, st, a, route);
+  const uint32_t held = uint32_t(groups_of(a.hidden)) * kHeldPart;
+  // two workgroups of four waves to a compute unit, or one of eight
+  if (a.hidden <= 2048)
+    hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, kPer, 4>), dim3(std::min(most, 512u)), dim3(256), held, st, a, route);
+  else
+    hipLaunchKernelGGL((wc_moe_mx_up_kernel<kType, kPer, 8>), dim3(std::min(most, 256u)), dim3(512), held, st, a, route);
 }
 template <int kType>
 void start_up(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
@@ -639,16 +645,13 @@ struct Tiles<256> {
   using Down = MxTile<256, 256, 2, 4, 128, 2>;
 };
 uint32_t tiles(uint32_t n, uint32_t each) { return (n + each - 1) / each; }
-// Scales that the tiles cannot load as they are, copied.
-bool ready(Bank& b, uint64_t to, uint32_t experts, uint32_t n, uint32_t k, hipStream_t st) {
-  if (whole_words(reinterpret_cast<const void*>(b.scales.at), blocks_of(k), k) && b.scale_stride % 4 == 0) return true;
+// Scales that the tiles cannot load as they are: their copies instead.
+void copy_of(Bank& b, uint64_t to, uint32_t experts, uint32_t n, uint32_t k, ScaleCopies& copies) {
+  if (whole_words(reinterpret_cast<const void*>(b.scales.at), blocks_of(k), k) && b.scale_stride % 4 == 0) return;
   const Scales own = own_scales(to, uint64_t(experts) * n, k);
-  if (!launch_copy_scales(reinterpret_cast<const void*>(b.scales.at), blocks_of(k), n, b.scale_stride,
-                          uint64_t(experts) * n, k, own, st))
-    return false;
+  copies.add(b.scales.at, blocks_of(k), n, b.scale_stride, uint64_t(experts) * n, k, own);
   b.scales = own;
   b.scale_stride = uint64_t(n) * own.pitch;
-  return true;
 }
 template <int kPlaces>
 bool start_tiles(const ExpertArgs& a, uint32_t most, hipStream_t st) {
@@ -680,14 +683,17 @@ wc_status experts(ExpertArgs a, const Workspace& w, const int32_t* offsets, hipS
   if (is_few(a.tokens, a.k, a.hidden)) return few(a, nullptr, st);
   const uint32_t rows = places(a), most = uint32_t(most_blocks(a.slots, a.experts, rows));
   const Blocks blocks = {a.table, reinterpret_cast<uint64_t>(offsets), a.experts, a.slots, rows, most};
+  ScaleCopies copies;
+  copies.n = copies.groups = 0;
+  const uint64_t ws = a.hq - w.hq;
+  if (rows >= 64) {
+    copy_of(a.gate, ws + w.gate, a.experts, a.ffn, a.hidden, copies);
+    copy_of(a.up, ws + w.up, a.experts, a.ffn, a.hidden, copies);
+    copy_of(a.down, ws + w.down, a.experts, a.hidden, a.ffn, copies);
+  }
   if (!launch_quantize(reinterpret_cast<const void*>(a.x), a.dtype, a.tokens, a.hidden, a.ldx,
                        reinterpret_cast<void*>(a.xq), WC_MX_ROW_BYTES(a.hidden), a.xs,
-                       uint32_t(groups_of(a.hidden)) * 16, st, &blocks))
-    return WC_EHIP;
-  const uint64_t ws = a.hq - w.hq;
-  if (rows >= 64 && (!ready(a.gate, ws + w.gate, a.experts, a.ffn, a.hidden, st) ||
-                     !ready(a.up, ws + w.up, a.experts, a.ffn, a.hidden, st) ||
-                     !ready(a.down, ws + w.down, a.experts, a.hidden, a.ffn, st)))
+                       uint32_t(groups_of(a.hidden)) * 16, st, &blocks, &copies))
     return WC_EHIP;
   const bool started = rows == 16   ? start_slim(a, most, st)
                        : rows == 64 ? start_tiles<64>(a, most, st)

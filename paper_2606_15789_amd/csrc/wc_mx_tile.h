@@ -248,24 +248,6 @@ __device__ __forceinline__ void rows_out(const f32x16& acc, Store store) {
   }
 }
 
-// Eight neighbouring elements of type dt from element i on at address p, of which `left` are in the row.
-__device__ __forceinline__ void store_eight(uint64_t p, int32_t dt, uint64_t i, f32x4 low, f32x4 high, uint32_t left) {
-  const uint64_t at = p + i * 2;
-  if (left >= 8 && dt != WC_FP32 && at % 16 == 0) {
-    u32x4 h;
-    if (dt == WC_BF16)
-      h = {floats_to_bf16(low[0], low[1]), floats_to_bf16(low[2], low[3]), floats_to_bf16(high[0], high[1]),
-           floats_to_bf16(high[2], high[3])};
-    else
-      h = {float_to_fp16(low[0]) | float_to_fp16(low[1]) << 16, float_to_fp16(low[2]) | float_to_fp16(low[3]) << 16,
-           float_to_fp16(high[0]) | float_to_fp16(high[1]) << 16, float_to_fp16(high[2]) | float_to_fp16(high[3]) << 16};
-    *global<u32x4>(at) = h;
-    return;
-  }
-  store_four(p, dt, i, low, left);
-  if (left > 4) store_four(p, dt, i + 4, high, left - 4);
-}
-
 // The buffers of a tile's rows of codes and of scales (whole words).
 struct RowsOf {
   u32x4 codes, scales;
