@@ -144,14 +144,18 @@ struct MatJob {
   uint32_t n, first;  // its first tile
   int32_t bias_dtype, y_dtype;
 };
-struct MatArgs {
+template <uint32_t kJobs>
+struct MatArgsOf {
   uint64_t x, ldx;  // rows of codes, or of elements (ldx in bytes)
   Scales xs;
   uint32_t m, k, n_jobs;
   uint32_t splits;  // parts of k
-  MatJob job[kMaxJobs];
+  MatJob job[kJobs];
 };
-__device__ __forceinline__ uint32_t job_of(const MatArgs& a, uint32_t tile) {
+using MatArgs = MatArgsOf<kMaxJobs>;
+constexpr uint32_t kFewJobs = 4;  // 2.5 KB less of arguments, which the host takes 0.8 us for
+template <uint32_t kJobs>
+__device__ __forceinline__ uint32_t job_of(const MatArgsOf<kJobs>& a, uint32_t tile) {
   uint32_t j = 0;
   for (uint32_t i = 1; i < a.n_jobs; i++)
     if (tile >= a.job[i].first) j = i;
@@ -192,8 +196,8 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
 
 // Up to 16 rows of x, 16 kN rows of W at a time.  kType: the elements of x, which the workgroup
 // quantises to LDS, or 0: quantised rows in memory.
-template <int kN, int kType>
-__global__ __launch_bounds__(512) void wc_matmul_mx_stream_kernel(MatArgs a, uint32_t tiles) {
+template <int kN, int kType, uint32_t kJobs>
+__global__ __launch_bounds__(512) void wc_matmul_mx_stream_kernel(MatArgsOf<kJobs> a, uint32_t tiles) {
   using S = Stream<kN, 8>;
   __shared__ typename S::Shared sh;
   extern __shared__ u32x4 held[];  // only its own wave reads a part
@@ -457,16 +461,26 @@ void start_slim(uint32_t tiles, const MatArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((wc_matmul_mx_slim_kernel<2, kM, 8>), dim3(tiles, (a.m + 16 * kM - 1) / (16 * kM)), dim3(512), 0,
                      st, a);
 }
-template <int kN>
-void start_stream(const MatArgs& a, uint32_t tiles, int32_t x_dtype, hipStream_t st) {
+template <int kN, uint32_t kJobs>
+void start_stream(const MatArgsOf<kJobs>& a, uint32_t tiles, int32_t x_dtype, hipStream_t st) {
   // as many tiles to every workgroup, one to a compute unit
   const uint32_t held = x_dtype ? uint32_t(groups_of(a.k)) * kHeldPart : 0;
   const uint32_t rounds = (tiles + 255) / 256;
   const dim3 grid((tiles + rounds - 1) / rounds), block(512);
-  if (x_dtype == WC_BF16) hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, WC_BF16>), grid, block, held, st, a, tiles);
-  else if (x_dtype == WC_FP16) hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, WC_FP16>), grid, block, held, st, a, tiles);
-  else if (x_dtype == WC_FP32) hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, WC_FP32>), grid, block, held, st, a, tiles);
-  else hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, 0>), grid, block, 0, st, a, tiles);
+  const auto start = [&]<int kType>(std::integral_constant<int, kType>) {
+    hipLaunchKernelGGL((wc_matmul_mx_stream_kernel<kN, kType, kJobs>), grid, block, held, st, a, tiles);
+  };
+  if (x_dtype == WC_BF16) start(std::integral_constant<int, WC_BF16>{});
+  else if (x_dtype == WC_FP16) start(std::integral_constant<int, WC_FP16>{});
+  else if (x_dtype == WC_FP32) start(std::integral_constant<int, WC_FP32>{});
+  else start(std::integral_constant<int, 0>{});
+}
+template <int kN>
+void start_stream(const MatArgs& a, uint32_t tiles, int32_t x_dtype, hipStream_t st) {
+  if (a.n_jobs > kFewJobs) return start_stream<kN, kMaxJobs>(a, tiles, x_dtype, st);
+  MatArgsOf<kFewJobs> f{a.x, a.ldx, a.xs, a.m, a.k, a.n_jobs, a.splits, {}};
+  for (uint32_t i = 0; i < a.n_jobs; i++) f.job[i] = a.job[i];
+  start_stream<kN, kFewJobs>(f, tiles, x_dtype, st);
 }
 
 // The copies of scales of a plan.

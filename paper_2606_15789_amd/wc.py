@@ -186,7 +186,7 @@ def lib():
             + [C.c_uint32] * 4 + [C.c_void_p] * 4 + [experts] * 3 \
             + [C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]
         ptr, u32, u64, i32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32
-        bank = C.POINTER(_MxExperts)
+        bank = ptr  # wc_mx_experts: packed bytes or a ctypes structure
         L.wc_quantize_mx.argtypes = [ptr, i32, u32, u32, u64, ptr, u64, ptr, u64, ptr]
         L.wc_dequantize_mx.argtypes = [ptr, u64, ptr, u64, u32, u32, ptr, i32, u64, ptr]
         L.wc_matmul_mx_workspace_bytes.argtypes = L.wc_matmul_i8_workspace_bytes.argtypes
@@ -196,10 +196,8 @@ def lib():
         L.wc_experts_mx_workspace_bytes.argtypes = L.wc_experts_i8_workspace_bytes.argtypes
         L.wc_experts_mx.argtypes = [ptr, i32, u32, u64] + [u32] * 4 + [ptr] * 4 + [bank] * 3 \
             + [ptr, u64, ptr, u64, ptr]
-        L.wc_moe_mx_workspace_bytes.argtypes = [u32, C.POINTER(_RouteParams), u32, u32,
-                                                C.POINTER(u64)]
-        L.wc_moe_mx.argtypes = [ptr, i32, u32, u64, ptr, i32, u64, C.POINTER(_RouteParams), ptr,
-                                u32, u32] + [bank] * 3 + [ptr, u64, ptr, u64, ptr]
+        L.wc_moe_mx_workspace_bytes.argtypes = [u32, ptr, u32, u32, C.POINTER(u64)]
+        L.wc_moe_mx.argtypes = [ptr, i32, u32, u64, ptr, i32, u64, ptr, ptr, u32, u32] + [bank] * 3 + [ptr, u64, ptr, u64, ptr]
         for name in EXPORTS[EXPORTS.index("wc_quantize_i8"):]:
             getattr(L, name).restype = C.c_int
         L.wc_free.argtypes = [C.POINTER(_Blob)]
@@ -1093,10 +1091,21 @@ def _mx_types():
 
 def _mx_rows(w, scale, k: int, what: str, dev: int):
     """(n, row strides in bytes of codes and scales) of a 2-D MXFP4 matrix of k columns."""
-    codes, bytes_ = _mx_types()
-    if w.dtype not in codes:
+    codes, bytes_ = _bytes_of_codes or _mx_types()[0], _bytes_of_scales or _mx_types()[1]
+    # (each look at a tensor costs the host as much as a microsecond's tenth)
+    shape, stride, s_shape, s_stride = w.shape, w.stride(), scale.shape, scale.stride()
+    if w.dtype not in codes or scale.dtype not in bytes_ or len(shape) != 2 or len(s_shape) != 2 or \
+            dev < 0 or w.get_device() != dev or scale.get_device() != dev or s_shape[0] != shape[0] or \
+            shape[1] != (k + 31) // 32 * 16 or s_shape[1] != (k + 31) // 32 or stride[1] != 1 or \
+            s_stride[1] != 1 or shape[0] == 1:
+        return _mx_rows_or_raise(w, scale, k, what, dev)
+    return shape[0], stride[0], s_stride[0]
+
+
+def _mx_rows_or_raise(w, scale, k: int, what: str, dev: int):
+    if w.dtype not in _bytes_of_codes:
         raise ValueError(f"{what} must be packed 4-bit codes in bytes")
-    if scale.dtype not in bytes_:
+    if scale.dtype not in _bytes_of_scales:
         raise ValueError(f"the scales of {what} must be e8m0 bytes")
     ldw = _rows(w, what, dev, mx_row_bytes(k))
     lds = _rows(scale, f"the scales of {what}", dev, mx_blocks(k))
@@ -1118,11 +1127,14 @@ def quantize_mx_torch(x, q=None, scale=None, stream=None):
         raise WcError("wc_quantize_mx", _EINVAL)
     st, where = _stream_of(stream, x.device)
     with where:
+        n, ldq, lds = m, mx_row_bytes(k), mx_blocks(k)
+        own = q is None and scale is None
         if q is None:
-            q = x.new_empty((m, mx_row_bytes(k)), dtype=torch.uint8)
+            q = x.new_empty((m, ldq), dtype=torch.uint8)
         if scale is None:
-            scale = x.new_empty((m, mx_blocks(k)), dtype=torch.uint8)
-        n, ldq, lds = _mx_rows(q, scale, k, "q", dev)
+            scale = x.new_empty((m, lds), dtype=torch.uint8)
+        if not own:
+            n, ldq, lds = _mx_rows(q, scale, k, "q", dev)
         if n != m:
             raise ValueError(f"q must have {m} rows")
         rc = lib().wc_quantize_mx(x.data_ptr(), dt, m, k, ld, q.data_ptr(), ldq, scale.data_ptr(),
@@ -1143,10 +1155,11 @@ def dequantize_mx_torch(q, scale, k: int, y=None, dtype=None, stream=None):
     st, where = _stream_of(stream, q.device)
     with where:
         if y is None:
-            y = torch.empty((m, k), dtype=dtype or torch.bfloat16, device=q.device)
-        if tuple(y.shape) != (m, k):
-            raise ValueError(f"y must be {m} x {k}")
-        ldy = _rows(y, "y", dev)
+            y, ldy = q.new_empty((m, k), dtype=dtype or torch.bfloat16), k
+        else:
+            if y.shape != (m, k):
+                raise ValueError(f"y must be {m} x {k}")
+            ldy = _rows(y, "y", dev)
         rc = lib().wc_dequantize_mx(q.data_ptr(), ldq, scale.data_ptr(), lds, m, k, y.data_ptr(),
                                     _float_type(y, "y"), ldy, st)
     if rc:
@@ -1155,6 +1168,8 @@ def dequantize_mx_torch(q, scale, k: int, y=None, dtype=None, stream=None):
 
 
 _MX_JOB = struct.Struct("=7QI3i")  # wc_mx_job
+_MX_BANK = struct.Struct("=4Q")  # wc_mx_experts
+_ROUTE = struct.Struct("=2I2i3If")  # wc_route_params
 
 
 def _mx_jobs(m: int, k: int, ws, scales, biases, ys, dtype, dev: int):
@@ -1223,15 +1238,18 @@ def linear_mx_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
     if (m | k) >> 32:
         raise WcError("wc_linear_mx", _EINVAL)
     st, where = _stream_of(stream, x.device)
-    need = C.c_uint64(0)
+    n_jobs = len(ws)
     with where:
         jobs, ys = _mx_jobs(m, k, ws, scales, biases, ys, dtype or x.dtype, dev)
-        # few rows of no more than 12288 need no workspace
-        rc = 0 if m <= 16 and k <= 12288 and workspace is None else \
-            lib().wc_linear_mx_workspace_bytes(m, k, len(ws), jobs, C.byref(need))
+        # few rows mostly need no workspace, and the call refuses those that do
+        if m <= 16 and workspace is None and \
+                not lib().wc_linear_mx(x.data_ptr(), dt, m, k, ld, n_jobs, jobs, None, 0, st):
+            return ys
+        need = C.c_uint64(0)
+        rc = lib().wc_linear_mx_workspace_bytes(m, k, n_jobs, jobs, C.byref(need))
         if not rc:
             workspace = _workspace(workspace, need.value, x.device)
-            rc = lib().wc_linear_mx(x.data_ptr(), dt, m, k, ld, len(ws), jobs, _ptr(workspace),
+            rc = lib().wc_linear_mx(x.data_ptr(), dt, m, k, ld, n_jobs, jobs, _ptr(workspace),
                                     _size(workspace), st)
     if rc:
         raise WcError("wc_linear_mx", rc)
@@ -1239,18 +1257,18 @@ def linear_mx_torch(x, ws, scales, biases=None, ys=None, dtype=None, workspace=N
 
 
 def _mx_bank(w, scale, experts: int, n: int, k: int, what: str, dev: int):
-    codes, bytes_ = _mx_types()
+    codes, bytes_ = _bytes_of_codes or _mx_types()[0], _bytes_of_scales or _mx_types()[1]
     if w.dtype not in codes or scale.dtype not in bytes_:
         raise ValueError(f"{what} must be packed 4-bit codes in bytes, its scales e8m0 bytes")
     strides = []
-    for t, cols, name in ((w, mx_row_bytes(k), what), (scale, mx_blocks(k), f"the scales of {what}")):
+    for t, cols in ((w, (k + 31) // 32 * 16), (scale, (k + 31) // 32)):
         stride = t.stride()
         if t.shape != (experts, n, cols) or t.get_device() != dev or (cols > 1 and stride[2] != 1) or \
                 (n > 1 and stride[1] != cols):
-            raise ValueError(f"{name} must be {experts} x {n} x {cols} bytes on device {dev}, contiguous "
-                             "in each expert")
+            raise ValueError(f"{what if t is w else 'the scales of ' + what} must be {experts} x {n} x {cols} "
+                             f"bytes on device {dev}, contiguous in each expert")
         strides.append(stride[0] if experts > 1 else n * cols)
-    return _MxExperts(w.data_ptr(), scale.data_ptr(), *strides)
+    return _MX_BANK.pack(w.data_ptr(), scale.data_ptr(), *strides)
 
 
 def _mx_banks(x, gate, gate_scale, up, up_scale, down, down_scale, dev: int):
@@ -1266,7 +1284,7 @@ def _mx_banks(x, gate, gate_scale, up, up_scale, down, down_scale, dev: int):
 
 def _mx_result(y, x, dev: int):
     if y is None:
-        y = x.new_empty(x.shape)
+        return x.new_empty(x.shape), x.shape[1]
     if y.shape != x.shape or y.dtype != x.dtype:
         raise ValueError("y must be of x's shape and type")
     return y, _rows(y, "y", dev)
@@ -1297,7 +1315,7 @@ def experts_mx_torch(x, routing: Routing, gate, gate_scale, up, up_scale, down, 
         y, ldy = _mx_result(y, x, dev)
         workspace = _workspace(workspace, need.value, x.device)
         rc = lib().wc_experts_mx(x.data_ptr(), dt, tokens, ld, k, experts, hidden, ffn,
-                                 *(t.data_ptr() for t in routing), *(C.byref(b) for b in banks),
+                                 *(t.data_ptr() for t in routing), *banks,
                                  y.data_ptr(), ldy, _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_experts_mx", rc)
@@ -1325,17 +1343,17 @@ def moe_mx_torch(x, logits, k: int, gate, gate_scale, up, up_scale, down, down_s
     if (tokens | experts | hidden | ffn | k | groups | top_groups | group_top) >> 32:
         raise WcError("wc_moe_mx", _EINVAL)
     st, where = _stream_of(stream, x.device)
-    params = _RouteParams(experts, k, SCORES[score], int(renormalize), groups, top_groups,
-                          group_top, scale)
+    params = _ROUTE.pack(experts, k, SCORES[score], int(renormalize), groups, top_groups, group_top,
+                         scale)
     need = C.c_uint64(0)
-    rc = lib().wc_moe_mx_workspace_bytes(tokens, C.byref(params), hidden, ffn, C.byref(need))
+    rc = lib().wc_moe_mx_workspace_bytes(tokens, params, hidden, ffn, C.byref(need))
     if rc:
         raise WcError("wc_moe_mx", rc)
     with where:
         y, ldy = _mx_result(y, x, dev)
         workspace = _workspace(workspace, need.value, x.device)
         rc = lib().wc_moe_mx(x.data_ptr(), dt, tokens, ld, logits.data_ptr(), lt, ldl,
-                             C.byref(params), _ptr(bias), hidden, ffn, *(C.byref(b) for b in banks),
+                             params, _ptr(bias), hidden, ffn, *banks,
                              y.data_ptr(), ldy, _ptr(workspace), _size(workspace), st)
     if rc:
         raise WcError("wc_moe_mx", rc)
