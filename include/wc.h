@@ -710,10 +710,10 @@ typedef struct {
  *   dev_workspace     at least wc_matmul_mx_workspace_bytes bytes, 256-byte aligned (NULL
  *                     where that is 0); overwritten; calls that share it must not
  *                     overlap in time.
- * Codes past k in a row of W may be any; those of x must be zeros.  A sum has no error where
- * its products' scales lie within 2^24 of each other and its value fits; otherwise that of
- * fp32 sums.  The order of a sum goes by the sizes alone: the result is the same on every
- * run.  The matrices have less than 2^27 rows together.  m = 0 is a call that does
+ * Codes past k in a row of W may be any; those of x must be zeros.  A block's sum of 32 products
+ * is exact; blocks are added in fp32, without an error as long as their sums are multiples of one
+ * power of two less than 2^24 times it, in an order that goes by the call's sizes and
+ * alignments alone: the result is the same on every run.  The matrices have less than 2^27 rows together.  m = 0 is a call that does
  * nothing.  Returns WC_EINVAL (argument), WC_EHIP. */
 wc_status wc_matmul_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                        const wc_mx_job* jobs, uint64_t* bytes);
@@ -722,8 +722,9 @@ wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint8_t* dev_sc
                        void* dev_workspace, uint64_t workspace_bytes, void* stream);
 
 /* wc_linear_mx -- wc_quantize_mx and wc_matmul_mx in one call: linear layers that share
- * their activations.  Up to 16 rows are quantised by the product's own launch; more in
- * the workspace.  Returns WC_EINVAL, WC_EHIP. */
+ * their activations.  Up to 16 rows of at most 12288 are quantised by the product's own
+ * launch, which then needs no workspace (unless rows of W or their scales are more than
+ * 2^27 bytes apart); others in the workspace.  Returns WC_EINVAL, WC_EHIP. */
 wc_status wc_linear_mx_workspace_bytes(uint32_t m, uint32_t k, uint32_t n_jobs,
                                        const wc_mx_job* jobs, uint64_t* bytes);
 wc_status wc_linear_mx(const void* dev_x, int32_t x_dtype, uint32_t m, uint32_t k, uint64_t ldx,
@@ -743,7 +744,8 @@ typedef struct {
 /* wc_experts_mx -- the gated feed-forward of a mixture layer: for every token y = sum over
  * its slots of weight * down(h), h = silu(gate x) * (up x), with the matrices of the slot's
  * expert; x and h are brought to MXFP4 (as by wc_quantize_mx, h from fp32) before each
- * product, the experts' results are held in fp32, and the slots are added in fp32.
+ * product, the experts' results are held in fp32, and the slots are added in fp32 (above 16 tokens
+ * in their order).
  *   dev_x, dtype   tokens rows of hidden elements, ldx elements apart;
  *   ids .. order   as wc_route writes them for tokens, experts and k: ids agree with
  *                  offsets and order (the call goes by either); a slot whose id is
@@ -768,8 +770,9 @@ wc_status wc_experts_mx(const void* dev_x, int32_t dtype, uint32_t tokens, uint6
                         void* dev_workspace, uint64_t workspace_bytes, void* stream);
 
 /* wc_moe_mx -- a whole mixture layer from the router's logits: wc_route and wc_experts_mx in
- * one call.  Up to 16 tokens it is two launches: each workgroup of the first chooses the
- * tokens' experts for itself.
+ * one call.  Up to 16 tokens (of at most 8192, k at most 32) it is two launches: each workgroup of
+ * the first chooses the tokens' experts for itself, and a token's slots are added in an
+ * order that goes by the call's experts.
  *   dev_logits, logits_dtype, ld, p, dev_bias   as for wc_route (p->k slots a token);
  *   the other arguments as for wc_experts_mx, the workspace by wc_moe_mx_workspace_bytes.
  * Returns WC_EINVAL (argument), WC_EHIP. */

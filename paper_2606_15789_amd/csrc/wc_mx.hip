@@ -347,7 +347,7 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
 constexpr uint32_t kHeldK = 12288;
 enum class Kernel { kStream16, kStream32, kStream64, kSlim, kTile64, kTile128, kTile128Deep, kTile256 };
 constexpr bool streams(Kernel k) { return k <= Kernel::kStream64; }
-using Tile64 = MxTile<64, 64, 1, 2, 128, 4>;
+using Tile64 = MxTile<64, 64, 2, 2, 128, 4>;
 using Tile128 = MxTile<128, 128, 2, 2, 128, 2>;
 using Tile128Deep = MxTile<128, 128, 2, 2, 128, 4>;
 using Tile256 = MxTile<256, 256, 2, 4, 128, 2>;
@@ -394,9 +394,17 @@ struct Plan {
   uint32_t splits;    // parts of k
   uint64_t parts;     // bytes of their sums
   uint64_t scales;    // bytes of copies of scales
+  uint32_t m;
+  // Whether a tile's kernel gets a copy of a matrix's scales, with the rows of a group next to each
+  // other: where it cannot load them as they are, and where enough rows of x make up for it.  us
+  // without and with: 512 x 28672 -> 8192 93.5 and 88.6, 512 x 8192 -> 8192 35.1 and 32.0, 8192 x
+  // 8192 -> 28672 992 and 970; 256 x 4096 -> 14336 21.5 and 21.3, 48 x 8192 -> 28672 34.8 and 38.2.
+  bool copies(const void* scale, uint64_t pitch, uint32_t k) const {
+    return kernel >= Kernel::kTile64 && (m >= 256 || !whole_words(scale, pitch, k));
+  }
 };
 Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
-  Plan p{Kernel::kSlim, false, 1, 0, 0};
+  Plan p{Kernel::kSlim, false, 1, 0, 0, m};
   bool near = true, narrow = m < (1u << 24);
   uint64_t n = 0, sums = 0;
   for (uint32_t i = 0; i < n_jobs; i++) {
@@ -441,7 +449,7 @@ Plan plan_of(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
   }
   if (p.kernel == Kernel::kSlim) return p;
   for (uint32_t i = 0; i < n_jobs; i++) {
-    if (!whole_words(jobs[i].scale, jobs[i].lds, k)) p.scales += pad256(own_scales_bytes(jobs[i].n, k));
+    if (p.copies(jobs[i].scale, jobs[i].lds, k)) p.scales += pad256(own_scales_bytes(jobs[i].n, k));
     if (p.splits > 1) p.parts += pad256(uint64_t(m) * ((jobs[i].n + 7) & ~7u) * 4 * p.splits);
   }
   return p;
@@ -490,7 +498,7 @@ ScaleCopies copies_of(const Plan& p, uint32_t k, uint32_t n_jobs, const wc_mx_jo
   uint64_t to = reinterpret_cast<uint64_t>(workspace) + p.parts;
   for (uint32_t i = 0; p.scales && i < n_jobs; i++) {
     const wc_mx_job& J = jobs[i];
-    if (whole_words(J.scale, J.lds, k)) continue;
+    if (!p.copies(J.scale, J.lds, k)) continue;
     c.add(reinterpret_cast<uint64_t>(J.scale), J.lds, J.n, 0, J.n, k, own_scales(to, J.n, k));
     to += pad256(own_scales_bytes(J.n, k));
   }
@@ -518,7 +526,7 @@ wc_status matmul(const void* x, uint64_t ldx, const Scales& xs, int32_t x_dtype,
     tiles += tiles_of(p.kernel, m, J.n);
     widest = std::max(widest, J.n);
     if (p.splits > 1) part += pad256(uint64_t(m) * ((J.n + 7) & ~7u) * 4 * p.splits);
-    if (p.kernel >= Kernel::kTile64 && !whole_words(J.scale, J.lds, k)) {
+    if (p.copies(J.scale, J.lds, k)) {
       a.job[i].scales = own_scales(copy, J.n, k);
       copy += pad256(own_scales_bytes(J.n, k));
     }
@@ -670,7 +678,7 @@ extern "C" wc_status wc_matmul_mx(const uint8_t* dev_q, uint64_t ldq, const uint
   Plan p = plan_of(m, k, n_jobs, jobs);
   p.inside = false;
   if (!workspace_ok(dev_workspace, workspace_bytes, workspace_of(p) + x_scales_bytes(p, m, k))) return WC_EINVAL;
-  if (p.kernel >= Kernel::kTile64 && (ldq > (1u << 22) || lds > (1u << 22))) p = Plan{Kernel::kSlim, false, 1, 0, 0};  // 32-bit offsets in a tile
+  if (p.kernel >= Kernel::kTile64 && (ldq > (1u << 22) || lds > (1u << 22))) p = Plan{Kernel::kSlim, false, 1, 0, 0, m};  // 32-bit offsets in a tile
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   Scales xs = {reinterpret_cast<uint64_t>(dev_scale), uint32_t(lds), 16};
   if (p.kernel >= Kernel::kTile64) {

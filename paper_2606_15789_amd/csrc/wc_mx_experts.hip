@@ -161,9 +161,14 @@ __global__ __launch_bounds__(64 * kWaves) void wc_moe_mx_up_kernel(ExpertArgs a,
   extern __shared__ u32x4 held[];  // x; only its own wave reads a part
   const uint32_t lane = threadIdx.x % 64, r = lane % 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t blocks = (a.hidden + 31) / 32, supers = (blocks + kSuper - 1) / kSuper;
+  // the first token's logits are on their way to the cache while x is quantised
+  float logit = 0.0f;
+  if constexpr (kPer > 0)
+    logit = load_float(route.logits, route.dtype, min(wave, a.tokens - 1) * route.ld + min(lane, a.experts - 1));
   for (uint32_t super = wave; super < supers; super += kWaves)
     hold_part(held, super,
               quantize_part<kType>(a.x + r * a.ldx * (kType == WC_FP32 ? 4 : 2), r < a.tokens, super, a.hidden));
+  asm volatile("" ::"v"(logit));
   if constexpr (kPer > 0) {
     // the sums' place in LDS is free until then
     static_assert(sizeof(float) * kWaves * 64 * (kPer ? kPer : 1) <= sizeof(sh));

@@ -275,6 +275,86 @@ def test_nothing_behind_the_rows(dev, m):
     assert bool((Y[m:] == 9.0).all())
 
 
+@pytest.mark.parametrize("m", [1, 9, 16])
+@pytest.mark.parametrize("k", [8192, 8193, 12288, 12289, 16400])
+@pytest.mark.parametrize("n", [48, 5000, 17000])
+def test_few_rows_of_many(dev, m, k, n):
+    """Up to 16 rows: x held on chip and not, tiles of 16, 32 and 64 rows of W, several to a
+    workgroup."""
+    g = torch.Generator(device=dev).manual_seed(m + k + n)
+    w = torch.randint(0, 256, (n, mx.blocks(k) * 16), generator=g, device=dev, dtype=torch.uint8)
+    s = torch.randint(120, 123, (n, mx.blocks(k)), generator=g, device=dev, dtype=torch.uint8)
+    x = _x(_gen(m), m, k, list(DT)[m % 3])
+    bias = torch.randn(n, generator=g, device=dev)
+    y, = wc.linear_mx_torch(x.to(dev), [w], [s], [bias], dtype=torch.float32)
+    some = torch.unique(torch.cat([torch.arange(0, n, 257), torch.arange(n - 40, n)]))
+    on = some.to(dev)
+    _check(y[:, on], _xv(x), w[on].cpu(), s[on].cpu(), bias[on].cpu())
+
+
+def test_many_jobs(dev):
+    """As many matrices as a call takes, of every tile's sizes."""
+    g = _gen(4)
+    k = 288
+    mats = [mx.matrix(g, 1 + 13 * i, k) for i in range(32)]
+    for m in (2, 30, 140):
+        x = _x(g, m, k, "bf16")
+        ys = wc.linear_mx_torch(x.to(dev), [w.to(dev) for w, _ in mats], [s.to(dev) for _, s in mats])
+        for y, (w, s) in zip(ys, mats):
+            _check(y, _xv(x), w, s)
+
+
+@pytest.mark.parametrize("m,k,n", [(300, 2048, 700), (520, 4096, 1030), (1100, 1024, 2300), (90, 20000, 300)])
+def test_tiles_and_parts(dev, m, k, n):
+    """Tiles of every size, parts of k, in every type of result."""
+    g = _gen(m)
+    x = _x(g, m, k, "bf16")
+    w, s = mx.matrix(g, n, k)
+    bias = torch.randn(n, generator=g)
+    for dtype in DT.values():
+        y, = wc.linear_mx_torch(x.to(dev), [w.to(dev)], [s.to(dev)], [bias.to(dev)], dtype=dtype)
+        _check(y, _xv(x), w, s, bias)
+
+
+def test_scales_past_a_gigabyte(dev):
+    """So many rows that a group's scales of all of them lie further apart than a tile's offsets
+    reach: they are kept in rows."""
+    m, k, n = (1 << 20) + 77, 32768, 40
+    if torch.cuda.mem_get_info(dev)[0] < 120 << 30:
+        pytest.skip("needs 120 GiB")
+    g = torch.Generator(device=dev).manual_seed(1)
+    some = torch.randn((64, k), generator=g, device=dev).bfloat16()
+    x = torch.empty((m, k), dtype=torch.bfloat16, device=dev)
+    for i in range(0, m, 64):
+        x[i:i + 64] = some[:min(64, m - i)]
+    x[-1] = some[5] * 3
+    w, s = (t.to(dev) for t in mx.matrix(_gen(1), n, k))
+    y, = wc.linear_mx_torch(x, [w], [s], dtype=torch.float32)
+    rows = torch.tensor([0, 63, 64, 65535 * 16, (1 << 20) - 1, 1 << 20, m - 2, m - 1])
+    on = rows.to(dev)
+    _check(y[on], _xv(x[on].cpu()), w.cpu(), s.cpu())
+    assert torch.equal(y[:64], y[64:128]) and torch.equal(y[:64], y[(1 << 20) - 64:1 << 20])
+
+
+def test_two_streams_at_once(dev):
+    """Calls on two streams at the same time, each with its own workspace."""
+    g = _gen(8)
+    k, n = 1024, 640
+    w, s = (t.to(dev) for t in mx.matrix(g, n, k))
+    xs = [_x(g, m, k, "bf16").to(dev) for m in (3, 400)]
+    want = [wc.linear_mx_torch(x, [w], [s])[0].clone() for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(wc.linear_mx_torch(xs[i], [w], [s])[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, want[i]) for y in got[i])
+
+
 def test_padding_of_weights(dev):
     """Codes past k of W's rows may be any (mx.matrix makes them random); those of x are zeros."""
     g = _gen(3)

@@ -114,7 +114,8 @@ SIZES = [(1, 1, 1, 1, 1), (1, 4, 2, 64, 48), (3, 8, 8, 130, 257), (16, 2, 1, 128
          (16, 64, 6, 544, 96), (17, 2, 2, 100, 300), (65, 5, 3, 272, 96), (33, 64, 6, 256, 160),
          (128, 3, 2, 515, 129), (300, 8, 2, 384, 512), (520, 4, 2, 256, 640), (40, 100, 1, 31, 17),
          (2, 16, 4, 2048, 1408), (1200, 2, 1, 160, 144), (900, 2, 1, 131, 77), (10, 40, 33, 96, 64),
-         (1300, 3, 1, 97, 258), (3000, 2, 1, 515, 640), (2500, 5, 2, 1056, 352)]
+         (1300, 3, 1, 97, 258), (3000, 2, 1, 515, 640), (2500, 5, 2, 1056, 352), (4, 4, 2, 8192, 64),
+         (3, 3, 2, 8193, 96), (16, 300, 8, 2049, 33), (5, 2, 1, 4097, 700), (100, 4, 2, 1024, 2048)]
 
 
 @pytest.mark.parametrize("dtype", list(DT))
@@ -293,6 +294,22 @@ def test_streams_graphs_and_runs(dev, tokens):
         torch.cuda.synchronize()
         assert torch.equal(ya, want[i]) and torch.equal(yb, want[i])
         space.fill_(255)
+
+
+def test_same_order_in_any_workspace(dev):
+    """A workspace full of NaN and one of zeros: nothing in it is read before it is written."""
+    E, k = 5, 2
+    for tokens, hidden, ffn in ((7, 100, 70), (90, 100, 70), (500, 1000, 200)):
+        layer = _on(dev, _layer(7, E, hidden, ffn))
+        g = torch.Generator().manual_seed(tokens)
+        x = torch.randn((tokens, hidden), generator=g).to(dev)
+        r = _routing(_ids(g, tokens, E, k), torch.rand((tokens, k), generator=g), E)
+        r = wc.Routing(*(t.to(dev) for t in r))
+        ys = []
+        for fill in (0, 255):
+            space = torch.full((1 << 26,), fill, dtype=torch.uint8, device=dev)
+            ys.append(wc.experts_mx_torch(x, r, *layer, workspace=space))
+        assert torch.equal(*ys) and not bool(torch.isnan(ys[0]).any())
 
 
 def test_garbage_routing_stays_inside(dev):
