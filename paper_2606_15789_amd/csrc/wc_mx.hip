@@ -50,7 +50,8 @@ bool launch_copies(const ScaleCopies& copies, hipStream_t stream) {
 // Four lanes to a block of 32, eight elements each: loads and stores of neighbouring lanes are
 // next to each other.  Long rows have kUnits units of eight to a thread, all on their way at once;
 // rows of less than a workgroup's elements share one.  After the rows' workgroups one that writes the
-// table of blocks of places, if there is one, then those that copy scales.
+// table of blocks of places, if there is one, then those that copy scales.  Bound by memory:
+// 28672 x 8192 bf16 133 us, 4.5 TB/s (a large copy 4.8); 333 x 5461 fp32 3.6.
 struct NoCopies {};
 template <int kType, int kUnits, class Copies>
 __global__ __launch_bounds__(kThreads) void wc_quantize_mx_kernel(QuantArgs a, Copies copies) {
@@ -100,7 +101,7 @@ struct DequantArgs {
 };
 
 // The same the other way: eight codes a lane.  Values are exact in fp32, and rounded once to
-// y's type.
+// y's type.  28672 x 8192 to bf16 88 us, 6.7 TB/s, the codes just written.
 template <int kType, int kUnits>
 __global__ __launch_bounds__(kThreads) void wc_dequantize_mx_kernel(DequantArgs a) {
   const uint32_t units = (a.k + 7) / 8;
@@ -162,7 +163,9 @@ __device__ __forceinline__ uint32_t job_of(const MatArgsOf<kJobs>& a, uint32_t t
   return j;
 }
 
-// 16 kN rows of W by 16 kM rows of quantised x.
+// 16 kN rows of W by 16 kM rows of quantised x, for what is too small for a tile, or rows too far
+// apart: each load touches sixteen rows.  100 x 512 -> 512 6.0 us with the quantisation, on tiles
+// 6.6; 512 x 28672 -> 8192 360, on tiles 91.
 template <int kN, int kM, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs a) {
   using S = Slim<kN, kM, kWaves>;
@@ -195,7 +198,10 @@ __global__ __launch_bounds__(64 * kWaves) void wc_matmul_mx_slim_kernel(MatArgs 
 }
 
 // Up to 16 rows of x, 16 kN rows of W at a time.  kType: the elements of x, which the workgroup
-// quantises to LDS, or 0: quantised rows in memory.
+// quantises to LDS, or 0: quantised rows in memory.  Bound by reading W: 13 x 8192 -> 28672 30 us
+// (125 MB of W, 4.1 TB/s from the launch on; a large copy 4.8); one row of 4096 -> 6144 7.2, a
+// chain of latencies.  With a launch for the quantisation and a workgroup for every tile, which
+// waits for its first rows of W, 13 x 8192 -> 28672 took 58.
 template <int kN, int kType, uint32_t kJobs>
 __global__ __launch_bounds__(512) void wc_matmul_mx_stream_kernel(MatArgsOf<kJobs> a, uint32_t tiles) {
   using S = Stream<kN, 8>;
@@ -229,7 +235,14 @@ __global__ __launch_bounds__(512) void wc_matmul_mx_stream_kernel(MatArgsOf<kJob
       });
 }
 
-// A tile of y, or of its sums over one part of k (blockIdx.y).
+// A tile of y, or of its sums over one part of k (blockIdx.y).  Tiles of 256: 8192 x 8192 -> 28672
+// 933 to 966 us, 4.0 PFLOP/s, the matrix units busy 58 % of the cycles.  What bounds them is the
+// loads first (without any, an earlier state of the kernel took 663 us of 1012), then the card's
+// power: on zeros the call takes 824 us instead of 955, and the units alone reach 9.2 PFLOP/s on
+// zeros and 6.4 on random codes.  Tiles of 128 wait for their stages: 512 x 28672 -> 8192 75 us,
+// 0.67 a stage, the matrix units busy 33 % of the cycles.  Four
+// waves of 128 x 128 to a tile of 256 took 1.6 times as long, stages of 64 bytes with four of them
+// in LDS 8 % longer, operands read from LDS two steps ahead the same.
 template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_matmul_mx_tile_kernel(MatArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
@@ -347,10 +360,10 @@ bool jobs_ok(uint32_t m, uint32_t k, uint32_t n_jobs, const wc_mx_job* jobs) {
 constexpr uint32_t kHeldK = 12288;
 enum class Kernel { kStream16, kStream32, kStream64, kSlim, kTile64, kTile128, kTile128Deep, kTile256 };
 constexpr bool streams(Kernel k) { return k <= Kernel::kStream64; }
-using Tile64 = MxTile<64, 64, 2, 2, 128, 4>;
-using Tile128 = MxTile<128, 128, 2, 2, 128, 2>;
-using Tile128Deep = MxTile<128, 128, 2, 2, 128, 4>;
-using Tile256 = MxTile<256, 256, 2, 4, 128, 2>;
+using Tile64 = MxTile<64, 64, 2, 2, 4>;
+using Tile128 = MxTile<128, 128, 2, 2, 2>;
+using Tile128Deep = MxTile<128, 128, 2, 2, 4>;
+using Tile256 = MxTile<256, 256, 2, 4, 2>;
 template <class F>
 void with_tile(Kernel k, F f) {
   switch (k) {
@@ -371,12 +384,12 @@ uint32_t tiles_of(Kernel k, uint32_t m, uint32_t n) {
 // What a tile's kernel takes, in us: a stage of 256 of k, one workgroup's and two's where two fit a
 // compute unit, and all else of a round of workgroups.  Taken so that the least sum is the fastest
 // kernel, or within 5 % of it, at each of these (m, k, n; in us on tiles of 64, of 128 with two and
-// with four stages in LDS, and of 256, in the best number of parts of k; with the quantisation):
-//   32, 4096, 14336 12.9, 19.4, 16.8, 19.8; 64, 8192, 8192 17.9, 27.6, 20.6, 25.8; 100, 14336,
-//   4096 21.1, 38.4, 23.2, 36.6; 128, 8192, 28672 52.1, 44.2, 39.0, 50.6; 333, 5461, 2047 20.7,
-//   25.4, 24.0, 34.7; 512, 28672, 8192 143, 102, 91, 91; 1024, 4096, 4096 26.4, 22.9, 21.2,
-//   33.1; 1024, 8192, 28672 291, 186, 191, 137; 2000, 2048, 2048 18.5, 15.6, 15.1, 22.5; 4096, 4096,
-//   14336 302, 188, 227, 157; 8192, 8192, 28672 1864, 1227, 1467, 993.
+// with four stages in LDS, and of 256, in the best of 1, 2 and 4 parts of k; with the quantisation):
+//   32, 4096, 14336 13.2, 19.6, 16.9, 19.9; 64, 8192, 8192 19.2, 28.9, 21.4, 27.0; 100, 14336,
+//   4096 21.9, 39.4, 24.8, 37.6; 128, 8192, 28672 53.7, 45.0, 39.3, 51.4; 333, 5461, 2047 16.7,
+//   23.9, 22.3, 33.2; 512, 28672, 8192 133, 100, 88, 93; 1024, 4096, 4096 25.5, 22.9, 21.3,
+//   31.9; 1024, 8192, 28672 256, 173, 180, 135; 2000, 2048, 2048 17.8, 15.8, 15.4, 22.1; 4096, 4096,
+//   14336 285, 176, 225, 153; 8192, 8192, 28672 1872, 1240, 1392, 992.
 struct TileCost {
   Kernel kernel;
   double stage, stage_of_two, round;

@@ -1,10 +1,10 @@
 // wc_mx_tile.h -- the product of one tile of MXFP4 matrices by one workgroup, operands through
 // LDS: C[n][m] = sum_k W[n][k] x[m][k] on v_mfma_scale_f32_32x32x64_f8f6f4.
 //
-// A stage is kStage (64 or 128) bytes of codes of every row of the tile, 2 kStage of k.  They go from
+// A stage is 128 bytes of codes of every row of the tile, 256 of k.  They go from
 // memory to LDS without passing through registers (buffer_load ... lds), kDepth - 1 stages ahead of
 // the products, and so do the scales, of 512 of k at a time: a line of memory for 16 bytes of a row.
-// Product q of a stage's kStage / 32 takes block q from its lanes 0 .. 31 and block kStage / 32 + q
+// Product q of a stage's four takes block q from its lanes 0 .. 31 and block 4 + q
 // from the others, so that a lane's scales of a stage are neighbouring bytes of a word.  A row's
 // 16-byte chunks are stored in the order chunk ^ turn(row): the sixteen lanes that read LDS
 // together, the same chunk of sixteen rows, then touch all 64 banks once.
@@ -21,21 +21,21 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // kBM rows of x by kBN rows of W, kWM x kWN waves, kDepth stages in LDS.  kPaired: W's rows are kBN / 2 of
 // one matrix and the same of another, and a wave's blocks of W the same of either.
-template <int kBM, int kBN, int kWM, int kWN, int kStage, int kDepth, bool kPaired = false>
+template <int kBM, int kBN, int kWM, int kWN, int kDepth, bool kPaired = false>
 struct MxTile {
   static constexpr int kWM_ = kWM, kWN_ = kWN, kWaves = kWM * kWN, kThreads = 64 * kWaves;
   static constexpr int kMT = kBM / kWM / 32, kNT = kBN / kWN / 32;  // 32 x 32 blocks to a wave
-  static constexpr int kRows = kBM, kCols = kBN, kAll = kBM + kBN, kBytes = kStage;
-  static constexpr int kSteps = kStage / 32;           // products of a block by a block to a stage
+  static constexpr int kRows = kBM, kCols = kBN, kAll = kBM + kBN, kBytes = 128;
+  static constexpr int kSteps = kBytes / 32;           // products of a block by a block to a stage
   static constexpr uint32_t kBlocks = 2 * kSteps;      // MXFP4 blocks of a row in a stage
   static constexpr int kGroup = 16 / int(kBlocks);     // stages that share a load of scales
-  static constexpr uint32_t kChunks = kStage / 16;     // lanes to a row of a load
+  static constexpr uint32_t kChunks = kBytes / 16;     // lanes to a row of a load
   static constexpr uint32_t kEach = 64 / kChunks;      // rows to a load of a wave
   static constexpr int kXLoads = kBM / kEach / kWaves, kWLoads = kBN / kEach / kWaves;
   static constexpr int kLoads = kXLoads + kWLoads;     // and those of scales at a group's first stage
   static constexpr int kSLoads = (kAll / 64 + kWaves - 1) / kWaves;  // 64 rows each; not all waves have the last
   static constexpr int kAhead = kDepth - 1;
-  static constexpr int kBuffer = kAll * kStage, kScaleBuffer = kAll * 16;
+  static constexpr int kBuffer = kAll * kBytes, kScaleBuffer = kAll * 16;
   static constexpr int kScaleBuffers = kAhead < kGroup ? 2 : 4;
   static constexpr int kScales = kDepth * kBuffer;     // where the scales start
   static constexpr int kLds = kScales + kScaleBuffers * kScaleBuffer;
@@ -50,7 +50,7 @@ struct MxTile {
     return kEach * __builtin_amdgcn_readfirstlane(threadIdx.x / 64) + threadIdx.x % 64 / kChunks + kStep * i;
   }
   static __device__ __forceinline__ uint32_t turn(uint32_t row) {
-    return kStage == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+    return (row >> 1) & 7;
   }
   static __device__ __forceinline__ uint32_t chunk_of() {
     static_assert(kStep % 16 == 0);  // rows kStep apart turn alike
@@ -98,7 +98,7 @@ struct MxTile {
     const auto start = [&]<int kPhase>(Int<kPhase>, int i, uint32_t s, uint32_t slot) {
       const uint32_t to = __builtin_amdgcn_readfirstlane(base + slot * kBuffer + wave * 1024);
       if (i < kXLoads) load_x(i, s, to + uint32_t(i) * kThreads * 16);
-      else load_w(i - kXLoads, s, to + kBM * kStage + uint32_t(i - kXLoads) * kThreads * 16);
+      else load_w(i - kXLoads, s, to + kBM * kBytes + uint32_t(i - kXLoads) * kThreads * 16);
       if (i == kLoads - 1 && kPhase == 0)
 #pragma unroll
         for (int j = 0; j < kSLoads; j++)
@@ -109,24 +109,23 @@ struct MxTile {
     uint32_t at[kSteps];
 #pragma unroll
     for (uint32_t q = 0; q < kSteps; q++)
-      at[q] = lane % 32 * kStage + ((lane / 32 * kSteps + q) ^ turn(lane % 32)) * 16;
+      at[q] = lane % 32 * kBytes + ((lane / 32 * kSteps + q) ^ turn(lane % 32)) * 16;
     const uint32_t xrow = wm * (kBM / kWM), wrow = kBM + wn * (kBN / kWN / (kPaired ? 2 : 1));
     // block n of W, from row wrow on
     const auto w_at = [](int n) { return kPaired && n >= kNT / 2 ? kBN / 2 + (n - kNT / 2) * 32 : n * 32; };
     u32x4 x[2][kMT], w[2][kNT];  // operands of two steps
     uint32_t xs[kMT], ws[kNT], xs_next[kMT], ws_next[kNT];
     const auto read = [&](int set, const uint8_t* b, int q, int i) {
-      if (i < kNT) w[set][i] = *reinterpret_cast<const u32x4*>(b + wrow * kStage + at[q] + w_at(i) * kStage);
-      else x[set][i - kNT] = *reinterpret_cast<const u32x4*>(b + xrow * kStage + at[q] + (i - kNT) * 32 * kStage);
+      if (i < kNT) w[set][i] = *reinterpret_cast<const u32x4*>(b + wrow * kBytes + at[q] + w_at(i) * kBytes);
+      else x[set][i - kNT] = *reinterpret_cast<const u32x4*>(b + xrow * kBytes + at[q] + (i - kNT) * 32 * kBytes);
     };
     // the scales of stage s, the `phase`-th of its group: from byte 0 of their words on
     const auto read_scale = [&](uint32_t s, int phase, int i) {
       const uint8_t* b = lds + kScales + s / kGroup % kScaleBuffers * kScaleBuffer + lane % 32 * 16;
-      const uint32_t word = kStage == 128 ? uint32_t(phase) * 2 + lane / 32 : uint32_t(phase);
+      const uint32_t word = uint32_t(phase) * 2 + lane / 32;
       const uint32_t row = i < kNT ? wrow + w_at(i) : xrow + (i - kNT) * 32;
       uint32_t v = *reinterpret_cast<const uint32_t*>(b + row * 16 + word * 4);
       if (s / kGroup * 4 + word >= words) v = 0;  // past a row's end could be another's NaN
-      if (kStage == 64) v >>= lane / 32 * 16;
       (i < kNT ? ws_next[i < kNT ? i : 0] : xs_next[i < kNT ? 0 : i - kNT]) = v;
     };
     // Step q of a stage.  Between its products, in the order written: the reads of the next step
@@ -154,8 +153,8 @@ struct MxTile {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // a stage's loads: the first in the last step of the stage before, the others in the next one or two
-    constexpr int kHalf = kLoads / 2, kMost = kLoads;
+    // a stage's loads: the first half in the last step of the stage before, the others in the next
+    constexpr int kHalf = kLoads / 2;
     const auto begin = [&]<int... kS>(std::integer_sequence<int, kS...>) {
       ([&] {
 #pragma unroll
@@ -206,11 +205,9 @@ struct MxTile {
         for (int i = 0; i < kNT; i++) ws[i] = ws_next[i];
 #pragma unroll
         for (int i = 0; i < kLive; i++) xs[i] = xs_next[i];
-        step(std::integer_sequence<int, 0, kLive, kHalf, kMost, kLoad, 0>{}, slot, s + kAhead, fill, 0);
-        if constexpr (kSteps > 2) {
-          step(std::integer_sequence<int, 1, kLive, kMost, kLoads, kLoad, 0>{}, slot, s + kAhead, fill, 0);
-          step(std::integer_sequence<int, 2, kLive, 0, 0, 0, 0>{}, slot, 0, 0, 0);
-        }
+        step(std::integer_sequence<int, 0, kLive, kHalf, kLoads, kLoad, 0>{}, slot, s + kAhead, fill, 0);
+        step(std::integer_sequence<int, 1, kLive, 0, 0, 0, 0>{}, slot, 0, 0, 0);
+        step(std::integer_sequence<int, 2, kLive, 0, 0, 0, 0>{}, slot, 0, 0, 0);
         // Before the last step's products: the next stage's loads of this wave are in LDS and its
         // reads of this stage done, and so with the other waves behind the barrier.  The
         // stage after those in flight then replaces this one.
