@@ -743,9 +743,10 @@ typedef struct {
 
 /* wc_experts_mx -- the gated feed-forward of a mixture layer: for every token y = sum over
  * its slots of weight * down(h), h = silu(gate x) * (up x), with the matrices of the slot's
- * expert; x and h are brought to MXFP4 (as by wc_quantize_mx, h from fp32) before each
- * product, the experts' results are held in fp32, and the slots are added in fp32 (above 16 tokens
- * in their order).
+ * expert; x and h are brought to MXFP4 (as by wc_quantize_mx) before each product, the experts'
+ * results are held in fp32, and the slots are added in fp32 (above 16 tokens in their order).
+ * gate x and up x are sums in fp32; the codes of h are those of the exact silu(gate x) * (up x) of
+ * these (of one rounded to fp32 where gate x is below -88 or h below 2^-126 in magnitude).
  *   dev_x, dtype   tokens rows of hidden elements, ldx elements apart;
  *   ids .. order   as wc_route writes them for tokens, experts and k: ids agree with
  *                  offsets and order (the call goes by either); a slot whose id is

@@ -19,6 +19,8 @@ namespace {
 using namespace wc_mx;
 using wc_choose::RouteArgs;
 
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
 struct Bank {
   uint64_t w, stride;
   Scales scales;
@@ -43,8 +45,91 @@ __device__ __forceinline__ Row row_of(const Bank& b, uint32_t e, uint32_t first,
                 first, r, n);
 }
 
-// g / (1 + exp(-g)), with an exponential of 1 ulp and a rounded division
-__device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
+// h = silu(g) u in MXFP4.  The borders that a code or a block's scale goes by, 0.25, 0.75, 1.25, 1.75,
+// 2.5, 3.5, 5 and 1 times a power of two, have zeros for the low 21 bits of a float.  fp32's h, with
+// an exponential of 1 ulp and a rounded sum, division and product, is at most 2.5 * 2^-23 of its size
+// off, 5 ulps: where it is further from such a float, it is on the right side of all borders.  Where it
+// is not, one value in 160 thousand, and the border is one of its block's, h is found in 64 bits and
+// rounded to odd, which leaves it on its side.  (Not so for h of less than 2^-126 and where silu(g)
+// underflows, g < -88: those are fp32's.)  us with fp32's h and with this: 16 tokens, 8 of 128 experts of
+// 4096 x 1536 159.5 and 159.9; 2000 tokens, 6 of 64 of 2048 x 1408 154.5 and 156.5; 4096 tokens, 2 of 8 of
+// 6144 x 16384 1525 and 1535.  With 64 bits for every value near such a float the last took 1560: the
+// instructions of that path come from memory.
+constexpr uint32_t kUlps = 6;
+// ulps past a float with `kBits` zeros, kUlps of them on it, times a power of two
+template <int kBits>
+__device__ __forceinline__ bool next_to(uint32_t bits) {
+  return (bits << (32 - kBits)) + (kUlps << (32 - kBits)) <= 2 * kUlps << (32 - kBits);
+}
+__device__ __forceinline__ float hidden_fp32(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+__device__ __forceinline__ float hidden_odd(float g, float u) {
+  const double d = double(g) / (1.0 + exp(-double(g))) * double(u);
+  const float f = float(d);
+  if (__builtin_isinf(f) || double(f) == d) return f;  // beyond fp32: an infinity
+  const uint32_t bits = __float_as_uint(f);
+  return __uint_as_float((__builtin_fabs(double(f)) > __builtin_fabs(d) ? bits - 1 : bits) | 1u);
+}
+// Codes of eight values from h[i] on, times `by`.
+template <class V>
+__device__ __forceinline__ uint32_t eight_codes(const V& h, int i, float scale, float by) {
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[i] * by, h[i + 1] * by, scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[i + 2] * by, h[i + 3] * by, scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[i + 4] * by, h[i + 5] * by, scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[i + 6] * by, h[i + 7] * by, scale, 3);
+}
+template <int kN>
+struct Hidden {
+  uint32_t byte, codes[kN / 8];
+};
+// A lane's kN values: those of a row have in(i), the others are zeros; `across` gives the greatest of
+// the lanes that share a block.  Of lanes without `live` any.
+template <int kN, class V, class In, class Across>
+__device__ __forceinline__ Hidden<kN> hidden(const V& g, const V& u, bool live, In in, Across across) {
+  V h;
+  uint32_t least = ~0u;
+#pragma unroll
+  for (int i = 0; i < kN; i++) {
+    h[i] = hidden_fp32(g[i], u[i]);
+    least = min(least, (__float_as_uint(h[i]) << 11) + (kUlps << 11));
+    if (!in(i)) h[i] = 0.0f;
+  }
+  Hidden<kN> r;
+  for (bool sure = false;; sure = true) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kN; i++) top = max(top, __float_as_uint(h[i]) & 0x7FFFFFFFu);
+    top = across(top);
+    r.byte = scale_byte(top);
+    const float scale = scale_value(r.byte);
+#pragma unroll
+    for (int i = 0; i < kN; i += 8) r.codes[i / 8] = r.byte == 255 ? 0u : eight_codes(h, i, scale, 1.0f);
+    if (sure || __builtin_expect(!__ballot(live && least <= 2 * kUlps << 11), 1)) return r;
+    uint32_t apart = top && next_to<23>(top);
+#pragma unroll
+    for (int i = 0; i < kN; i += 8)
+      apart |= eight_codes(h, i, scale, 1 - 0x1p-20f) ^ eight_codes(h, i, scale, 1 + 0x1p-20f);
+    if (__builtin_expect(!__ballot(live && apart), 1)) return r;
+    uint32_t near = 0;  // bit i: h[i]
+#pragma unroll
+    for (int i = 0; i < kN; i++)
+      if (next_to<21>(__float_as_uint(h[i])) && in(i)) near |= 1u << i;
+    if (!live || !apart) near = 0;
+#pragma unroll 1
+    for (; __ballot(near != 0); near &= near - 1) {
+      const int at = near ? __builtin_ctz(near) : kN;
+      float gi = 0.0f, ui = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kN; i++) {
+        gi = at == i ? g[i] : gi;
+        ui = at == i ? u[i] : ui;
+      }
+      const float v = hidden_odd(gi, ui);
+#pragma unroll
+      for (int i = 0; i < kN; i++) h[i] = at == i ? v : h[i];
+    }
+  }
+}
 
 // Codes and scales of row `at` of h.
 __device__ __forceinline__ uint64_t h_codes(const ExpertArgs& a, uint64_t at, uint32_t block) {
@@ -126,28 +211,15 @@ __device__ __forceinline__ uint32_t top_of_column(uint32_t v) {
 __device__ __forceinline__ void store_h(const ExpertArgs& a, const f32x4 (&g)[2], const f32x4 (&u)[2], uint64_t at,
                                         uint32_t block, bool live) {
   const uint32_t quarter = threadIdx.x % 64 / 16;
-  float h[2][4];
-  uint32_t top = 0;
-#pragma unroll
-  for (uint32_t n = 0; n < 2; n++)
-#pragma unroll
-    for (uint32_t j = 0; j < 4; j++) {
-      const float v = silu(g[n][j]) * u[n][j];
-      h[n][j] = block * 32 + 16 * n + 4 * quarter + j < a.ffn ? v : 0.0f;
-      top = max(top, __float_as_uint(h[n][j]) & 0x7FFFFFFFu);
-    }
-  const uint32_t byte = scale_byte(top_of_column(top));
-  const float scale = scale_value(byte);
+  const auto h = hidden<8>(
+      __builtin_shufflevector(g[0], g[1], 0, 1, 2, 3, 4, 5, 6, 7),
+      __builtin_shufflevector(u[0], u[1], 0, 1, 2, 3, 4, 5, 6, 7), live,
+      [&](uint32_t i) { return block * 32 + 16 * (i / 4) + 4 * quarter + i % 4 < a.ffn; }, top_of_column);
   if (!live) return;
   const auto to = global<uint16_t>(h_codes(a, at, block)) + quarter;
-#pragma unroll
-  for (uint32_t n = 0; n < 2; n++) {
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[n][0], h[n][1], scale, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[n][2], h[n][3], scale, 1);
-    to[4 * n] = byte == 255 ? 0 : uint16_t(c);
-  }
-  if (quarter == 0) store_h_scale(a, at, block, byte);
+  to[0] = uint16_t(h.codes[0]);
+  to[4] = uint16_t(h.codes[0] >> 16);
+  if (quarter == 0) store_h_scale(a, at, block, h.byte);
 }
 
 // 32 columns of h at a time, for all tokens of one expert; the tokens are the columns of the matrix
@@ -158,7 +230,7 @@ __device__ __forceinline__ void store_h(const ExpertArgs& a, const f32x4 (&g)[2]
 // choice by a workgroup for every tile, 16 tokens of 128 experts without groups took 389 us, 267
 // from a plan.
 template <int kType, int kPer, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
+__global__ __launch_bounds__(64 * kWaves, 2) void wc_moe_mx_up_kernel(ExpertArgs a, RouteArgs route) {
   using S = Stream<4, kWaves>;
   __shared__ typename S::Shared sh;
   __shared__ Chosen c;
@@ -420,39 +492,24 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_mx_up_tile_kernel(Expe
     for (int mb = 0; mb < T::kMT; mb++) {
       const uint32_t place = first + wm0 + mb * 32 + lane % 32, c0 = n0 + wn0 + nb * 32, block = c0 / 32;
       if (first + wm0 + mb * 32 >= last || c0 >= a.ffn) continue;
-      float h[16];
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 16; i++) {
-        const uint32_t column = c0 + i / 4 * 8 + lane / 32 * 4 + i % 4;
-        h[i] = silu(acc[mb][nb][i]) * acc[mb][nb + T::kNT / 2][i];
-        if (column >= a.ffn) h[i] = 0.0f;
-        top = max(top, __float_as_uint(h[i]) & 0x7FFFFFFFu);
-      }
-      const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-      const uint32_t byte = scale_byte(max(both[0], both[1]));
-      const float scale = scale_value(byte);
-      // this lane's codes of every eight columns: two bytes, the other lane's the next two
-      uint32_t mine[2];
-#pragma unroll
-      for (int p = 0; p < 2; p++) {
-        uint32_t c = 0;
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p], h[8 * p + 1], scale, 0);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p + 2], h[8 * p + 3], scale, 1);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p + 4], h[8 * p + 5], scale, 2);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, h[8 * p + 6], h[8 * p + 7], scale, 3);
-        mine[p] = byte == 255 ? 0u : c;
-      }
+      const auto h = hidden<16>(
+          acc[mb][nb], acc[mb][nb + T::kNT / 2], true,
+          [&](uint32_t i) { return c0 + i / 4 * 8 + lane / 32 * 4 + i % 4 < a.ffn; },
+          [](uint32_t top) {
+            const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+            return max(both[0], both[1]);
+          });
+      // this lane's codes of every eight columns are two bytes, the other lane's the next two
       u32x4 codes;
 #pragma unroll
       for (int p = 0; p < 2; p++) {
-        const auto v = __builtin_amdgcn_permlane32_swap(mine[p], mine[p], false, false);
+        const auto v = __builtin_amdgcn_permlane32_swap(h.codes[p], h.codes[p], false, false);
         codes[2 * p] = (v[0] & 0xFFFFu) | v[1] << 16;       // the lower lanes' own, the upper lanes'
         codes[2 * p + 1] = v[0] >> 16 | (v[1] & 0xFFFF0000u);
       }
       if (lane < 32 && place < last) {
         *global<u32x4>(h_codes(a, place, block)) = codes;
-        store_h_scale(a, place, block, byte);
+        store_h_scale(a, place, block, h.byte);
       }
     }
 }
