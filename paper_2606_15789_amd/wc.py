@@ -1084,8 +1084,8 @@ def _mx_types():
     if not _bytes_of_codes:
         import torch
         named = [getattr(torch, n, torch.uint8) for n in ("float4_e2m1fn_x2", "float8_e8m0fnu")]
-        _bytes_of_codes = (torch.uint8, torch.int8, named[0])
         _bytes_of_scales = (torch.uint8, named[1])
+        _bytes_of_codes = (torch.uint8, torch.int8, named[0])  # last: what other threads look at
     return _bytes_of_codes, _bytes_of_scales
 
 
