@@ -735,15 +735,18 @@ bool start_tiles(const ExpertArgs& a, uint32_t most, hipStream_t st) {
                      dim3(Down::kThreads), 0, st, a);
   return hipGetLastError() == hipSuccess;
 }
-// Places to a block; 16: straight from memory to registers, at any sizes.  us with 64, 128 and 256:
+// Places to a block; 16: straight from memory to registers, at any sizes.  Up to 16 tokens, which are all
+// the places that an expert has, us with 16 and 64: 8 experts, 2 a token, of 8224 x 16384: 1 token 115,
+// 190; 2 196, 249; 4 363, 337; 16 418, 475; 64, 6, 8224 x 2048: 1 58, 121; 16 333, 340; 4, 1, 12288 x
+// 4096: 1 33, 50; 8 78, 84; 16 89, 86; 1, 1, 16384 x 53248: 3 316, 376.  More with 64, 128 and 256:
 //   8 experts, 2 a token, of 4096 x 14336: 64 tokens 172, 181, 215; 128 177, 192, 226; 256 217,
 //     203, 236; 600 (tiles of 64 with two waves less) 426, 275, 270; 1500 876, 518, 384
 //   64, 6, 2048 x 1408: 60 78, 80, 89; 200 83, 84, 92; 700 123, 103, 111; 2000 293, 175, 156
 //   7, 3, 2049 x 1365: 77 39, 40, 47; 256 43, 45, 54
 //   128, 8, 4096 x 1536: 40 248, 254, 283; 1000 403, 367, 387
 uint32_t places(const ExpertArgs& a) {
-  // x lies within 32-bit offsets, a grid's axis has less than 2^32 threads
-  if (a.tokens * WC_MX_ROW_BYTES(a.hidden) >> 31 || a.xs.step == 16 ||
+  // on tiles x lies within 32-bit offsets, its scales group by group; a grid's axis has less than 2^32 threads
+  if (a.tokens <= kFew || a.tokens * WC_MX_ROW_BYTES(a.hidden) >> 31 || own_scales_bytes(a.tokens, a.hidden) >> 30 ||
       most_blocks(a.slots, a.experts, 64) * std::max(tiles(a.ffn, 64), tiles(a.hidden, 128)) * 256 >> 32)
     return 16;
   const uint32_t average = a.slots / a.experts;
