@@ -34,7 +34,6 @@ struct ExpertArgs {
   uint64_t out;     // experts' results, fp32, by slot, in rows of whole eights
   uint64_t y, ldy;
   uint32_t tokens, k, experts, hidden, ffn, slots;
-  uint32_t first;   // this launch's first block of places, or token
   int32_t dtype;
   Bank gate, up, down;
 };
@@ -400,7 +399,7 @@ __host__ __device__ constexpr uint32_t out_pitch(uint32_t hidden) { return (hidd
 __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a) {
   using S = Slim<4, 1, 8>;
   __shared__ typename S::Shared sh;
-  const uint32_t block = a.first + blockIdx.x;
+  const uint32_t block = blockIdx.x;
   if (block >= block_count(a)) return;
   const auto [e, first, last] = block_at(a, block);
   const uint32_t lane = threadIdx.x % 64, r = lane % 16, n0 = blockIdx.y * 32, blocks = (a.hidden + 31) / 32;
@@ -422,7 +421,7 @@ __global__ __launch_bounds__(512) void wc_experts_mx_up_slim_kernel(ExpertArgs a
 __global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs a) {
   using S = Slim<2, 1, 8>;
   __shared__ typename S::Shared sh;
-  const uint32_t block = a.first + blockIdx.x;
+  const uint32_t block = blockIdx.x;
   if (block >= block_count(a)) return;
   const auto [e, first, last] = block_at(a, block);
   const uint32_t r = threadIdx.x % 16, n0 = blockIdx.y * 32, blocks = (a.ffn + 31) / 32;
@@ -565,7 +564,7 @@ __global__ __launch_bounds__(T::kThreads) void wc_experts_mx_down_tile_kernel(Ex
 // Bound by memory: 4096 tokens of 6144, 2 slots each, 46 us (5.5 TB/s).
 __global__ __launch_bounds__(256) void wc_experts_mx_join_kernel(ExpertArgs a) {
   const uint32_t n = (blockIdx.y * 256 + threadIdx.x) * 4;
-  const uint64_t token = a.first + blockIdx.x;
+  const uint64_t token = blockIdx.x;
   if (n >= a.hidden) return;
   const uint32_t left = a.hidden - n;
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -682,19 +681,12 @@ wc_status few(const ExpertArgs& a, const RouteArgs* route, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? WC_OK : WC_EHIP;
 }
 
-bool start_slim(ExpertArgs a, uint32_t most, hipStream_t st) {
-  constexpr uint32_t kLaunch = 1u << 22;  // a grid's axis has less than 2^32 threads
-  for (a.first = 0; a.first < most; a.first += kLaunch) {
-    hipLaunchKernelGGL(wc_experts_mx_up_slim_kernel, dim3(std::min(most - a.first, kLaunch), (a.ffn + 31) / 32),
-                       dim3(512), 0, st, a);
-    if (hipGetLastError() != hipSuccess) return false;
-  }
-  for (a.first = 0; a.first < most; a.first += kLaunch) {
-    hipLaunchKernelGGL(wc_experts_mx_down_slim_kernel, dim3(std::min(most - a.first, kLaunch), (a.hidden + 31) / 32),
-                       dim3(512), 0, st, a);
-    if (hipGetLastError() != hipSuccess) return false;
-  }
-  return true;
+// tokens * k < 2^24: at most 2^20 + 512 blocks, of less than 2^32 threads, a grid axis's limit.
+bool start_slim(const ExpertArgs& a, uint32_t most, hipStream_t st) {
+  hipLaunchKernelGGL(wc_experts_mx_up_slim_kernel, dim3(most, (a.ffn + 31) / 32), dim3(512), 0, st, a);
+  if (hipGetLastError() != hipSuccess) return false;
+  hipLaunchKernelGGL(wc_experts_mx_down_slim_kernel, dim3(most, (a.hidden + 31) / 32), dim3(512), 0, st, a);
+  return hipGetLastError() == hipSuccess;
 }
 
 // Tiles by the places of a block: up's columns are half of gate's and half of up's.
