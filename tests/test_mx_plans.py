@@ -5,7 +5,8 @@ import subprocess
 
 import pytest
 
-from paper_2606_15789_amd import build
+from mx_plans import PLANS
+from paper_2606_15789_amd import build, wc
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -46,3 +47,21 @@ def test_places_of_experts(tmp_path):
     """The kernels go by the sizes' orders: one token's are not others than two tokens'."""
     got = _answers(tmp_path, "mx_places_driver", [c for c, _ in PLACES])
     assert [int(v) for v in got] == [p for _, p in PLACES]
+
+
+def test_every_kernel_of_a_product(tmp_path):
+    calls = [(m, k, n, wc.mx_row_bytes(k), wc.mx_blocks(k)) for (m, k, n), _ in PLANS]
+    assert _answers(tmp_path, "mx_plan_driver", calls) == [plan for _, plan in PLANS]
+    seen = {tuple(plan.split()[:2]) for _, plan in PLANS}
+    assert seen >= {(tile, parts) for tile in ("tile64", "tile128", "tile128deep", "tile256") for parts in "1248"}
+
+
+def test_rows_far_apart(tmp_path):
+    """Rows that tiles' offsets do not reach go without tiles, or without streams."""
+    far, further = (1 << 22) + 16, (1 << 27) + 16
+    got = _answers(tmp_path, "mx_plan_driver", [
+        (300, 4096, 4096, 2048, 128), (300, 4096, 4096, far, 128), (300, 4096, 4096, 2048, far),
+        (5, 4096, 4096, far, far), (5, 4096, 4096, further, 128), (5, 4096, 4096, 2048, further),
+        ((1 << 24) - 1, 64, 64, 32, 2), (1 << 24, 64, 64, 32, 2)])
+    kinds = [g[:4] for g in got]
+    assert kinds == ["tile", "slim", "slim", "stre", "slim", "slim", "tile", "slim"]
