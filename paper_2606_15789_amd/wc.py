@@ -1343,8 +1343,9 @@ def moe_mx_torch(x, logits, k: int, gate, gate_scale, up, up_scale, down, down_s
     if (tokens | experts | hidden | ffn | k | groups | top_groups | group_top) >> 32:
         raise WcError("wc_moe_mx", _EINVAL)
     st, where = _stream_of(stream, x.device)
+    # (a factor beyond fp32 as an infinity, which the call refuses)
     params = _ROUTE.pack(experts, k, SCORES[score], int(renormalize), groups, top_groups, group_top,
-                         scale)
+                         C.c_float(scale).value)
     need = C.c_uint64(0)
     rc = lib().wc_moe_mx_workspace_bytes(tokens, params, hidden, ffn, C.byref(need))
     if rc:

@@ -97,3 +97,15 @@ def test_eight_waves_nan_logit_and_graph(dev):
         assert torch.equal(wc.moe_mx_torch(xs[0], ls[0], k, *banks), want[0])
         torch.cuda.synchronize()
         assert torch.equal(y.nan_to_num(7.0), want[i].nan_to_num(7.0))
+
+
+def test_scale_beyond_fp32_is_refused(dev):
+    """A factor of the weights that is no fp32 number is refused like any other argument."""
+    E, hidden, ffn = 4, 96, 64
+    layer = [t.to(dev) for pair in ex._layer(3, E, hidden, ffn) for t in pair]
+    x, lo = torch.zeros((3, hidden), device=dev), torch.zeros((3, E), device=dev)
+    for scale in (1e39, float("inf"), float("nan")):
+        with pytest.raises(wc.WcError):
+            wc.route_torch(lo, 2, scale=scale)
+        with pytest.raises(wc.WcError):
+            wc.moe_mx_torch(x, lo, 2, *layer, scale=scale)
