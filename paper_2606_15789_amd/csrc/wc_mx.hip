@@ -238,8 +238,8 @@ __global__ __launch_bounds__(512) void wc_matmul_mx_stream_kernel(MatArgsOf<kJob
 // A tile of y, or of its sums over one part of k (blockIdx.y).  Tiles of 256: 8192 x 8192 -> 28672
 // 933 to 966 us, 4.0 PFLOP/s, the matrix units busy 58 % of the cycles.  What bounds them is the
 // loads first (without any, an earlier state of the kernel took 663 us of 1012), then the card's
-// power: on zeros the call takes 824 us instead of 955, and the units alone reach 9.2 PFLOP/s on
-// zeros and 6.4 on random codes.  Tiles of 128 wait for their stages: 512 x 28672 -> 8192 75 us,
+// power: on zeros the call takes 829 us instead of 976, and the units alone, a loop of their
+// instruction on registers, reach 9.5 PFLOP/s on zeros and 6.4 on random codes.  Tiles of 128 wait for their stages: 512 x 28672 -> 8192 75 us,
 // 0.67 a stage, the matrix units busy 33 % of the cycles.  Four
 // waves of 128 x 128 to a tile of 256 took 1.6 times as long, stages of 64 bytes with four of them
 // in LDS 8 % longer, operands read from LDS two steps ahead the same.

@@ -7,8 +7,8 @@
 //   - up to 16 tokens, which are the columns of a matrix instruction, two kernels: one finds the
 //     experts (and chooses them, from logits), multiplies by gate and up and writes h by slot, the
 //     other multiplies by down and adds a token's slots;
-//   - more tokens: the places of the router's order in blocks of one expert's, on tiles through
-//     LDS, each expert's results stored by slot and then added.
+//   - more tokens, or wider ones: the places of the router's order in blocks of one expert's, on tiles
+//     through LDS, each expert's results stored by slot and then added.
 #include <algorithm>
 
 #include "wc_choose.h"
@@ -224,8 +224,8 @@ __device__ __forceinline__ void store_h(const ExpertArgs& a, const f32x4 (&g)[2]
 // 32 columns of h at a time, for all tokens of one expert; the tokens are the columns of the matrix
 // instruction, whether they have the expert or not.  kPer: registers of logits to a lane of the
 // choice, 0 where the ids are given.  Bound by reading the experts hit: 16 tokens, 8 of 128 experts
-// of 4096 x 1536 in groups, 73 us for the 350 MB of the some 53 that are hit, 4.8 TB/s; one token, 6 of
-// 64 of 2048 x 1408, 12.8, a chain of latencies (x, the logits, the choice, W, the sums).  With the
+// of 4096 x 1536 in groups, 73 to 76 us for the 350 MB of the some 53 that are hit, 4.7 TB/s; one token, 6
+// of 64 of 2048 x 1408, 13.0, a chain of latencies (x, the logits, the choice, W, the sums).  With the
 // choice by a workgroup for every tile, 16 tokens of 128 experts without groups took 389 us, 267
 // from a plan.
 template <int kType, int kPer, int kWaves>
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void wc_moe_mx_up_kernel(ExpertArgs
 }
 
 // 16 columns of y for all tokens: parts of 512 of every expert hit, spread over the waves.  Each
-// expert's first slot and weight of a token stand in a table in LDS.  35 us (5 TB/s) and 7.4 after
+// expert's first slot and weight of a token stand in a table in LDS.  33 to 35 us (5 TB/s) and 7.5 after
 // the calls above.
 __global__ __launch_bounds__(64 * kFewWaves) void wc_moe_mx_down_kernel(ExpertArgs a) {
   __shared__ Chosen c;
@@ -440,8 +440,8 @@ __global__ __launch_bounds__(512) void wc_experts_mx_down_slim_kernel(ExpertArgs
 // The same on tiles through LDS: kCols / 2 columns of h, for which W's rows are those of gate and the
 // same of up, so that both products of a value of h meet in one lane, and a block of 32 of
 // its columns in two: the scale of a block of h is found where its values are, and h is never stored
-// in more than 4 bits.  32 tokens, 2 each, of 8 experts of 6144 x 16384 164 us up and 86 down (5.2
-// TB/s of the weights); 4096 tokens 1006 and 517: 3.3 and 3.2 PFLOP/s, in 36 blocks of
+// in more than 4 bits.  32 tokens, 2 each, of 8 experts of 6144 x 16384 163 us up and 86 to 97 down
+// (4.4 to 5.2 TB/s of the weights); 4096 tokens 1016 and 515: 3.3 and 3.2 PFLOP/s, in 36 blocks of
 // places where 32 full ones would do.
 template <class T>
 __global__ __launch_bounds__(T::kThreads) void wc_experts_mx_up_tile_kernel(ExpertArgs a) {
